@@ -465,6 +465,171 @@ int mpm_compose_unmerge(const void* z, const int32_t* z_off, const int32_t* map_
                         int32_t* map_ab, const void* z_spec, int32_t E, int32_t B, int32_t N, int32_t D, int32_t dt,
                         void* out, void* stream);
 
+/* ---- The blocks between the merges: attention over packed images with a learned relative
+ * position bias, and the norms around a block. Conventions as above; NaN and infinities in the
+ * inputs flow through as in the formulas (checked mode validates the offsets only). ---- */
+
+#define MPM_MAX_HEADS 1024   /* query heads of an attention call */
+#define MPM_MAX_HEAD_DIM 128 /* channels of a head */
+#define MPM_MAX_SPAN 63      /* largest axis offset with a bias of its own */
+
+/* Rows of several heads: head j of row r is dh contiguous elements at p + r * row + j * head
+ * (strides in elements, each a whole number of 16 bytes, >= 0; p 16-byte aligned). Views into the
+ * rows of one fused projection are taken as they are. */
+typedef struct mpm_heads {
+    void* p;
+    int64_t row;
+    int64_t head;
+} mpm_heads;
+
+/*
+ * The shape and the optional inputs of an attention call.
+ *   B images; queries dense (q_off NULL: Nq rows an image) or packed (q_off int32[B+1], at most Nq
+ *   rows an image), keys and values likewise by k_off and Nk. Nq, Nk <= MPM_MAX_N.
+ *   H query heads share Hk key heads (H a multiple of Hk): query head h reads key head h / (H / Hk).
+ *   dh channels a head, a multiple of 8 (bf16) or 4 (f32), at most MPM_MAX_HEAD_DIM.
+ *   scale: the factor of q . k (finite).
+ *   bias (may be NULL): float[H][W][W], W = 2 span + 1, 0 <= span <= MPM_MAX_SPAN, as
+ *     mpm_bias_expand writes it: bias[h][span + r][span + c] is added to the score of a query and a
+ *     key whose grid positions differ by r rows and c columns (query minus key), each offset held
+ *     to [-span, span]. Positions are raster indices on a grid of grid_h x grid_w cells
+ *     (1 <= grid_h, grid_w <= MPM_MAX_N): q_pos, k_pos int32 per row, packed like q and k, or
+ *     NULL for each row's index in its image (the raster order of a full grid). Any order of
+ *     positions is taken; one outside the grid counts as the nearest cell index.
+ *   k_bias (may be NULL): float per key row, added to its scores for every query and head (for
+ *     merged rows the log of the tokens they stand for). A key with -inf is dropped: its rows of
+ *     k and v take no part, whatever they hold, and their gradients are zero. A constant: no
+ *     gradient is computed for it.
+ */
+typedef struct mpm_attention_call {
+    int32_t B, Nq, Nk, H, Hk, dh, dt;
+    float scale;
+    const int32_t* q_off;
+    const int32_t* k_off;
+    const float* bias;
+    int32_t span, grid_h, grid_w;
+    const int32_t* q_pos;
+    const int32_t* k_pos;
+    const float* k_bias;
+} mpm_attention_call;
+
+/*
+ * Attention of each image's queries over its keys:
+ *   s = scale q . k + bias + k_bias,  out = softmax(s) v,
+ * scores, softmax statistics and sums in float32, out rounded once to dt. A query without a key
+ * (an image with none, or all dropped or at -inf) gets zeros. Bfloat16 rounds the
+ * probabilities (relative to the row's maximum) to bfloat16 for their product with v.
+ *   lse (may be NULL): float [query row][H][2], contiguous, 8-byte aligned, needed for the gradients: the
+ *     maximum m that was taken from the scores and l = log2 sum 2^(s log2(e) - m), both in base 2: the
+ *     log-sum-exp is (m + l) ln 2 (a query without a key: -inf, 0). Two numbers, since under a mask
+ *     value such as -1e9 on every key one float32 would not hold both;
+ *   ws: device workspace of mpm_attention_workspace_bytes(call) bytes (0 for many shapes: may be
+ *     NULL then), 256-byte aligned, used where few queries have their keys split over workgroups.
+ * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned pointers, sizes below 1, dh, H or strides as
+ * above, bad dt, a span, grid or scale outside its range; MPM_ERR_UNSUPPORTED for B, Nq, Nk,
+ * H or dh above their maxima; MPM_ERR_WORKSPACE; MPM_ERR_HIP.
+ */
+size_t mpm_attention_workspace_bytes(const mpm_attention_call* call);
+int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_heads* k, const mpm_heads* v,
+                  const mpm_heads* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The gradients of mpm_attention from its inputs, its out and lse, and dout (dtype dt):
+ *   dq, dk, dv (dtype dt; rows and strides of their own), dk and dv summed over the query heads
+ *     that share a key head;
+ *   dbias (may be NULL; only with bias): float[H][W][W], the sum of the score gradients of every
+ *     pair at each offset, over all images (mpm_bias_gradient takes it to the table's).
+ * Rows of dq, dk and dv that exist are all written. Results do not depend on the order workgroups run in.
+ * ws: mpm_attention_backward_workspace_bytes(call) bytes. Errors as mpm_attention, plus
+ * MPM_ERR_INVALID_ARG for dbias without bias.
+ */
+size_t mpm_attention_backward_workspace_bytes(const mpm_attention_call* call);
+int mpm_attention_backward(const mpm_attention_call* call, const mpm_heads* dout, const mpm_heads* q,
+                           const mpm_heads* k, const mpm_heads* v, const mpm_heads* out, const float* lse,
+                           const mpm_heads* dq, const mpm_heads* dk, const mpm_heads* dv, float* dbias, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/*
+ * The learned relative position bias by buckets. lut int32[2 span + 1] gives the bucket, in
+ * [0, nb), of an axis offset -span ... span; a pair's bucket is lut[row offset] * nb + lut[column
+ * offset]; table [nb * nb][H] of dtype dt holds the learned values.
+ *   mpm_bias_expand: bias[h][r][c] = table[lut[r] * nb + lut[c]][h], float [H][W][W];
+ *   mpm_bias_gradient: dtable[bucket][h] = the sum of dbias[h] over the bucket's offsets in a fixed
+ *     order, rounded once to dt; buckets without an offset get zeros.
+ * A lut value outside [0, nb) counts as the nearest bucket in mpm_bias_expand and as none in
+ * mpm_bias_gradient. Errors: MPM_ERR_INVALID_ARG for bad pointers, nb < 1, H < 1, span < 0 or dt;
+ * MPM_ERR_UNSUPPORTED for span > MPM_MAX_SPAN, H > MPM_MAX_HEADS or nb > 2 * MPM_MAX_SPAN + 1.
+ */
+int mpm_bias_expand(const void* table, const int32_t* lut, int32_t nb, int32_t span, int32_t H, int32_t dt,
+                    float* bias, void* stream);
+int mpm_bias_gradient(const float* dbias, const int32_t* lut, int32_t nb, int32_t span, int32_t H, int32_t dt,
+                      void* dtable, void* stream);
+
+typedef enum {
+    MPM_NORM_LAYER = 0, /* (t - mean) / sqrt(variance + eps) * w + b */
+    MPM_NORM_RMS = 1    /* t / sqrt(mean square + eps) * w (+ b where given) */
+} mpm_norm_kind;
+
+/*
+ * The parameters of the norms around a block, each of D values of dtype dt unless said otherwise:
+ *   R rows of D values (16-byte rows, as tokens), contiguous;
+ *   w, b: the norm before the next block (w NULL: none; b NULL: no shift);
+ *   post_w, post_b: the norm after this block (post_w NULL: none);
+ *   scale (may be NULL): the residual scale;
+ *   gate (may be NULL): gate_per_row 0: one row an image, [B][D], the rows of image b given by
+ *     off (int32[B+1]; NULL: R / B rows each); gate_per_row 1: [R][D] (B and off are not used).
+ */
+typedef struct mpm_norm_call {
+    int32_t R, D, dt, kind;
+    float eps;
+    int32_t B, gate_per_row;
+    const int32_t* off;
+    const void* w;
+    const void* b;
+    const void* post_w;
+    const void* post_b;
+    const void* scale;
+    const void* gate;
+} mpm_norm_call;
+
+/*
+ * A block's output f into the residual stream x, and the next block's input:
+ *   u = post_norm(f) or f,  y = x + scale * gate * u,  h = norm(y),
+ * in float32 with y and h rounded once to dt (h is of the sum before y's rounding).
+ *   h: NULL if and only if w is; y may alias x;
+ *   stats (may be NULL): float[R][4], (mean, 1 / deviation) of f and of y, for the gradients.
+ * Rows outside every image (with a gate by image and off) are not written.
+ * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned (16-byte) pointers, sizes below 1, D as for
+ * tokens, eps < 0 or not finite, a shift without its weight, B that does not divide R (gate by image,
+ * off NULL), bad dt or kind; MPM_ERR_UNSUPPORTED for D > MPM_MAX_D or B > MPM_MAX_B; MPM_ERR_HIP.
+ */
+int mpm_residual_norm(const mpm_norm_call* call, const void* x, const void* f, void* y, void* h, float* stats,
+                      void* stream);
+
+/*
+ * Its gradients, from dy (into y from past this block; NULL: zero) and dh (into h; NULL if and only if
+ * w is), the stored y, f and stats:
+ *   dx, df [R][D]; dw, db, dpost_w, dpost_b, dscale [D]; dgate shaped as gate: each needed if and
+ *   only if its parameter is given. All of dtype dt; sums over rows are kept in float32, in a fixed order.
+ * ws: mpm_residual_norm_backward_workspace_bytes(call) bytes. Errors as mpm_residual_norm,
+ * plus MPM_ERR_WORKSPACE.
+ */
+typedef struct mpm_norm_grads {
+    void* dx;
+    void* df;
+    void* dw;
+    void* db;
+    void* dpost_w;
+    void* dpost_b;
+    void* dscale;
+    void* dgate;
+} mpm_norm_grads;
+
+size_t mpm_residual_norm_backward_workspace_bytes(const mpm_norm_call* call);
+int mpm_residual_norm_backward(const mpm_norm_call* call, const void* dy, const void* dh, const void* y,
+                               const void* f, const float* stats, const mpm_norm_grads* grads, void* ws,
+                               size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

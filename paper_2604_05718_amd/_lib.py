@@ -24,12 +24,45 @@ MPM_SCHEDULE_AUTO = 0
 MPM_SCHEDULE_FULL = 1
 MPM_SCHEDULE_SYMMETRIC = 2
 MPM_SCHEDULE_FULL_64 = 3
+MPM_NORM_LAYER = 0
+MPM_NORM_RMS = 1
+MPM_MAX_SPAN = 63
 
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _sz = ctypes.c_size_t
 
 _szp = ctypes.POINTER(ctypes.c_size_t)
+
+
+
+class Heads(ctypes.Structure):
+    """mpm_heads: rows of several heads."""
+    _fields_ = [("p", _vp), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class AttentionCall(ctypes.Structure):
+    """mpm_attention_call."""
+    _fields_ = [(n, _i32) for n in ("B", "Nq", "Nk", "H", "Hk", "dh", "dt")] + [("scale", ctypes.c_float)] + [
+        (n, _vp) for n in ("q_off", "k_off", "bias")] + [(n, _i32) for n in ("span", "grid_h", "grid_w")] + [
+        (n, _vp) for n in ("q_pos", "k_pos", "k_bias")]
+
+
+class NormCall(ctypes.Structure):
+    """mpm_norm_call."""
+    _fields_ = [(n, _i32) for n in ("R", "D", "dt", "kind")] + [("eps", ctypes.c_float)] + [
+        (n, _i32) for n in ("B", "gate_per_row")] + [
+        (n, _vp) for n in ("off", "w", "b", "post_w", "post_b", "scale", "gate")]
+
+
+class NormGrads(ctypes.Structure):
+    """mpm_norm_grads."""
+    _fields_ = [(n, _vp) for n in ("dx", "df", "dw", "db", "dpost_w", "dpost_b", "dscale", "dgate")]
+
+
+_hp = ctypes.POINTER(Heads)
+_ap = ctypes.POINTER(AttentionCall)
+_np = ctypes.POINTER(NormCall)
 
 # name -> (restype, argtypes); mirrors include/mpm.h
 SIGNATURES = {
@@ -63,6 +96,16 @@ SIGNATURES = {
     "mpm_unpad": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, _vp, _vp]),
     "mpm_compose": (ctypes.c_int, [_vp, _vp, _i32, _i32, _vp, _vp]),
     "mpm_compose_unmerge": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "mpm_attention_workspace_bytes": (_sz, [_ap]),
+    "mpm_attention": (ctypes.c_int, [_ap, _hp, _hp, _hp, _hp, _vp, _vp, _sz, _vp]),
+    "mpm_attention_backward_workspace_bytes": (_sz, [_ap]),
+    "mpm_attention_backward": (ctypes.c_int, [_ap] + [_hp] * 5 + [_vp] + [_hp] * 3 + [_vp, _vp, _sz, _vp]),
+    "mpm_bias_expand": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "mpm_bias_gradient": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "mpm_residual_norm": (ctypes.c_int, [_np, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mpm_residual_norm_backward_workspace_bytes": (_sz, [_np]),
+    "mpm_residual_norm_backward": (ctypes.c_int, [_np, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(NormGrads), _vp, _sz,
+                                                  _vp]),
     "mpm_unmerge": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
 }
 

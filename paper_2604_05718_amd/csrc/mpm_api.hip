@@ -322,7 +322,121 @@ hipError_t scratch_for_current_device(hipStream_t st, void** out)
     return hipSuccess;
 }
 
+// ---- attention and norms: argument checks --------------------------------------------
+
+bool finite(float v) { return v - v == 0.0f; }
+
+// Rows of heads of dh values of dtype dt: 16-byte rows and strides.
+bool ok_heads(const mpm_heads* x, int32_t dt)
+{
+    const int64_t per = dt == MPM_BF16 ? 8 : 4;
+    return x != nullptr && ok_rows_ptr(x->p) && x->row >= 0 && x->head >= 0 && x->row % per == 0 && x->head % per == 0;
+}
+
+mpm::HeadRows heads(const mpm_heads* x)
+{
+    return mpm::HeadRows{static_cast<uint8_t*>(x->p), (long)x->row, (long)x->head};
+}
+
+int check_attention(const mpm_attention_call* c)
+{
+    if (c == nullptr) return MPM_ERR_INVALID_ARG;
+    if (c->B < 1 || c->Nq < 1 || c->Nk < 1 || c->H < 1 || c->Hk < 1 || c->dh < 1) return MPM_ERR_INVALID_ARG;
+    if (c->dt != MPM_F32 && c->dt != MPM_BF16) return MPM_ERR_INVALID_ARG;
+    if (c->dh % (c->dt == MPM_BF16 ? 8 : 4) != 0 || c->H % c->Hk != 0 || !finite(c->scale)) return MPM_ERR_INVALID_ARG;
+    if (!ok_opt_int_ptr(c->q_off) || !ok_opt_int_ptr(c->k_off) || !ok_opt_int_ptr(c->k_bias)) return MPM_ERR_INVALID_ARG;
+    if (c->bias) {
+        if (!aligned(c->bias, 4) || !ok_opt_int_ptr(c->q_pos) || !ok_opt_int_ptr(c->k_pos)) return MPM_ERR_INVALID_ARG;
+        if (c->span < 0 || c->span > MPM_MAX_SPAN || c->grid_h < 1 || c->grid_w < 1 || c->grid_h > MPM_MAX_N ||
+            c->grid_w > MPM_MAX_N)
+            return MPM_ERR_INVALID_ARG;
+    }
+    if (c->B > MPM_MAX_B || c->Nq > MPM_MAX_N || c->Nk > MPM_MAX_N || c->H > MPM_MAX_HEADS ||
+        c->dh > MPM_MAX_HEAD_DIM)
+        return MPM_ERR_UNSUPPORTED;
+    return MPM_OK;
+}
+
+mpm::AttentionCall attention_call(const mpm_attention_call* c)
+{
+    const bool bias = c->bias != nullptr;  // what belongs to the bias is not read without one
+    return mpm::AttentionCall{c->B, c->Nq, c->Nk, c->H, c->Hk, c->dh, c->dt, c->scale, c->q_off, c->k_off, c->bias,
+                              bias ? c->span : 0, bias ? c->grid_h : 1, bias ? c->grid_w : 1,
+                              bias ? c->q_pos : nullptr, bias ? c->k_pos : nullptr, c->k_bias};
+}
+
+// Checks a workspace of `need` bytes (none needed: any pointer).
+int check_workspace(const void* ws, size_t ws_bytes, size_t need)
+{
+    if (need == 0) return MPM_OK;
+    if (ws == nullptr || !aligned(ws, kAlign)) return MPM_ERR_INVALID_ARG;
+    return ws_bytes < need ? MPM_ERR_WORKSPACE : MPM_OK;
+}
+
+// Checked mode: the packed offsets of queries and keys.
+int checked_attention(const mpm_attention_call* c, hipStream_t st)
+{
+    std::lock_guard<std::mutex> lock(g_check_mutex);
+    return run_checks(st, [&](int32_t* v) {
+        hipError_t e = hipSuccess;
+        if (c->q_off) e = mpm::launch_check_offsets(c->q_off, c->B, c->Nq, 0, -1, nullptr, v, st);
+        if (e == hipSuccess && c->k_off) e = mpm::launch_check_offsets(c->k_off, c->B, c->Nk, 0, -1, nullptr, v, st);
+        return e;
+    });
+}
+
+int check_bias_table(const int32_t* lut, int32_t nb, int32_t span, int32_t H, int32_t dt)
+{
+    if (!ok_int_ptr(lut) || nb < 1 || span < 0 || H < 1 || (dt != MPM_F32 && dt != MPM_BF16)) return MPM_ERR_INVALID_ARG;
+    if (span > MPM_MAX_SPAN || H > MPM_MAX_HEADS || nb > 2 * MPM_MAX_SPAN + 1) return MPM_ERR_UNSUPPORTED;
+    return MPM_OK;
+}
+
+bool ok_opt_rows_ptr(const void* p) { return aligned(p, 16); }
+
+int check_norm(const mpm_norm_call* c)
+{
+    if (c == nullptr || c->R < 1 || c->D < 1) return MPM_ERR_INVALID_ARG;
+    if (c->dt != MPM_F32 && c->dt != MPM_BF16) return MPM_ERR_INVALID_ARG;
+    if (c->kind != MPM_NORM_LAYER && c->kind != MPM_NORM_RMS) return MPM_ERR_INVALID_ARG;
+    if (c->D % (c->dt == MPM_BF16 ? 8 : 4) != 0 || !finite(c->eps) || c->eps < 0.0f) return MPM_ERR_INVALID_ARG;
+    if ((c->b && !c->w) || (c->post_b && !c->post_w)) return MPM_ERR_INVALID_ARG;
+    for (const void* p : {c->w, c->b, c->post_w, c->post_b, c->scale, c->gate})
+        if (!ok_opt_rows_ptr(p)) return MPM_ERR_INVALID_ARG;
+    if (c->gate && !c->gate_per_row) {
+        if (c->B < 1 || !ok_opt_int_ptr(c->off) || (!c->off && c->R % c->B != 0)) return MPM_ERR_INVALID_ARG;
+        if (c->B > MPM_MAX_B) return MPM_ERR_UNSUPPORTED;
+    }
+    if (c->D > MPM_MAX_D) return MPM_ERR_UNSUPPORTED;
+    return MPM_OK;
+}
+
+mpm::NormCall norm_call(const mpm_norm_call* c)
+{
+    const bool by_image = c->gate && !c->gate_per_row;
+    const int B = by_image ? c->B : 1;
+    return mpm::NormCall{c->R, c->D, B, c->R / B, 1, c->dt, c->kind == MPM_NORM_LAYER, c->eps,
+                         by_image ? c->off : nullptr, c->w, c->b, c->post_w, c->post_b, c->scale, c->gate,
+                         c->gate && c->gate_per_row};
+}
+
+// Checked mode: the offsets of a gate by image.
+int checked_norm(const mpm::NormCall& a, hipStream_t st)
+{
+    if (!a.off) return MPM_OK;
+    std::lock_guard<std::mutex> lock(g_check_mutex);
+    return run_checks(st, [&](int32_t* v) { return mpm::launch_check_offsets(a.off, a.B, a.R, 0, a.R, nullptr, v, st); });
+}
+
 }  // namespace
+
+namespace mpm {
+hipError_t allow_lds(const void* kernel, size_t bytes)
+{
+    if (bytes <= (64u << 10)) return hipSuccess;
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+}  // namespace mpm
 
 extern "C" {
 
@@ -698,6 +812,111 @@ int mpm_unmerge(const void* z, const int32_t* z_off, const int32_t* map, const v
     MPM_LAUNCH_GATE();
     MPM_DATA_CHECK(checked_maps(z_off, N, map, nullptr, B, N, as_stream(stream)));
     return hip_status(mpm::launch_unmerge(z, z_off, map, z_spec, E, B, N, D, dt, out, as_stream(stream)));
+}
+
+size_t mpm_attention_workspace_bytes(const mpm_attention_call* call)
+{
+    return 0;
+}
+
+int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_heads* k, const mpm_heads* v,
+                  const mpm_heads* out, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    int s = check_attention(call);
+    if (s != MPM_OK) return s;
+    for (const mpm_heads* x : {q, k, v, out})
+        if (!ok_heads(x, call->dt)) return MPM_ERR_INVALID_ARG;
+    if (!aligned(lse, 8)) return MPM_ERR_INVALID_ARG;
+    if ((s = check_workspace(ws, ws_bytes, mpm_attention_workspace_bytes(call))) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_attention(call, as_stream(stream)));
+    return hip_status(mpm::launch_attention(attention_call(call), heads(q), heads(k), heads(v), heads(out), lse,
+                                            as_stream(stream)));
+}
+
+size_t mpm_attention_backward_workspace_bytes(const mpm_attention_call* call)
+{
+    return check_attention(call) == MPM_OK ? mpm::attention_backward_bytes(attention_call(call)) : 0;
+}
+
+int mpm_attention_backward(const mpm_attention_call* call, const mpm_heads* dout, const mpm_heads* q,
+                           const mpm_heads* k, const mpm_heads* v, const mpm_heads* out, const float* lse,
+                           const mpm_heads* dq, const mpm_heads* dk, const mpm_heads* dv, float* dbias, void* ws,
+                           size_t ws_bytes, void* stream)
+{
+    int s = check_attention(call);
+    if (s != MPM_OK) return s;
+    for (const mpm_heads* x : {dout, q, k, v, out, dq, dk, dv})
+        if (!ok_heads(x, call->dt)) return MPM_ERR_INVALID_ARG;
+    if (lse == nullptr || !aligned(lse, 8) || !aligned(dbias, 4) || (dbias && !call->bias)) return MPM_ERR_INVALID_ARG;
+    const mpm::AttentionCall a = attention_call(call);
+    if ((s = check_workspace(ws, ws_bytes, mpm::attention_backward_bytes(a))) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_attention(call, as_stream(stream)));
+    return hip_status(mpm::launch_attention_backward(a, heads(dout), heads(q), heads(k), heads(v), heads(out), lse,
+                                                     heads(dq), heads(dk), heads(dv), dbias, ws, as_stream(stream)));
+}
+
+int mpm_bias_expand(const void* table, const int32_t* lut, int32_t nb, int32_t span, int32_t H, int32_t dt,
+                    float* bias, void* stream)
+{
+    const int s = check_bias_table(lut, nb, span, H, dt);
+    if (s != MPM_OK) return s;
+    if (table == nullptr || !aligned(table, dt == MPM_BF16 ? 2 : 4) || !ok_int_ptr(bias)) return MPM_ERR_INVALID_ARG;
+    MPM_LAUNCH_GATE();
+    return hip_status(mpm::launch_bias_expand(table, lut, nb, span, H, dt, bias, as_stream(stream)));
+}
+
+int mpm_bias_gradient(const float* dbias, const int32_t* lut, int32_t nb, int32_t span, int32_t H, int32_t dt,
+                      void* dtable, void* stream)
+{
+    const int s = check_bias_table(lut, nb, span, H, dt);
+    if (s != MPM_OK) return s;
+    if (dtable == nullptr || !aligned(dtable, dt == MPM_BF16 ? 2 : 4) || !ok_int_ptr(dbias)) return MPM_ERR_INVALID_ARG;
+    MPM_LAUNCH_GATE();
+    return hip_status(mpm::launch_bias_gradient(dbias, lut, nb, span, H, dt, dtable, as_stream(stream)));
+}
+
+int mpm_residual_norm(const mpm_norm_call* call, const void* x, const void* f, void* y, void* h, float* stats,
+                      void* stream)
+{
+    const int s = check_norm(call);
+    if (s != MPM_OK) return s;
+    if (!ok_rows_ptr(x) || !ok_rows_ptr(f) || !ok_rows_ptr(y) || !aligned(h, 16) || !aligned(stats, 16) ||
+        (h == nullptr) != (call->w == nullptr))
+        return MPM_ERR_INVALID_ARG;
+    const mpm::NormCall a = norm_call(call);
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_norm(a, as_stream(stream)));
+    return hip_status(mpm::launch_norm(a, x, f, y, h, stats, as_stream(stream)));
+}
+
+size_t mpm_residual_norm_backward_workspace_bytes(const mpm_norm_call* call)
+{
+    return check_norm(call) == MPM_OK ? mpm::norm_backward_bytes(norm_call(call)) : 0;
+}
+
+int mpm_residual_norm_backward(const mpm_norm_call* call, const void* dy, const void* dh, const void* y,
+                               const void* f, const float* stats, const mpm_norm_grads* grads, void* ws,
+                               size_t ws_bytes, void* stream)
+{
+    int s = check_norm(call);
+    if (s != MPM_OK) return s;
+    if (!aligned(dy, 16) || !aligned(dh, 16) || (dh == nullptr) != (call->w == nullptr) || !ok_rows_ptr(y) ||
+        !ok_rows_ptr(f) || !ok_rows_ptr(stats) || grads == nullptr || !ok_rows_ptr(grads->dx) || !ok_rows_ptr(grads->df))
+        return MPM_ERR_INVALID_ARG;
+    const void* given[] = {call->w, call->b, call->post_w, call->post_b, call->scale, call->gate};
+    const void* asked[] = {grads->dw, grads->db, grads->dpost_w, grads->dpost_b, grads->dscale, grads->dgate};
+    for (int i = 0; i < 6; ++i)
+        if ((given[i] == nullptr) != (asked[i] == nullptr) || !aligned(asked[i], 16)) return MPM_ERR_INVALID_ARG;
+    const mpm::NormCall a = norm_call(call);
+    if ((s = check_workspace(ws, ws_bytes, mpm::norm_backward_bytes(a))) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_norm(a, as_stream(stream)));
+    return hip_status(mpm::launch_norm_backward(a, dy, dh, y, f, stats,
+                                                mpm::NormGrads{grads->dx, grads->df, grads->dw, grads->db, grads->dpost_w,
+                                                               grads->dpost_b, grads->dscale, grads->dgate},
+                                                ws, as_stream(stream)));
 }
 
 }  // extern "C"

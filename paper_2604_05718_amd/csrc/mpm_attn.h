@@ -1,0 +1,234 @@
+// Shared by the attention kernels: the call's layout, tiles in LDS, matrix fragments.
+//
+// Matrix products run on 32 x 32 MFMA tiles. A wave holds its 32 own rows (queries in the
+// forward and query-gradient kernels, keys in the key-gradient kernel) as the B operand, so
+// that in every score tile a lane owns one of them (lane % 32) and 16 rows of the other side:
+// register r of half h = lane / 32 is row 8 (r / 4) + 4 h + r % 4. A score tile is then the B
+// operand of the next product without leaving its registers: a step of 16 contracted rows
+// takes registers 8 s ... 8 s + 7, rows 16 s + 8 (i / 4) + 4 h + i % 4 of element i, and the A
+// operand's rows are read in that order (cols_frag).
+#pragma once
+
+#include "mpm_device.h"
+#include "mpm_launch.h"
+
+namespace mpm {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.4028234663852886e38f;
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Eight consecutive values along the contracted axis of a 32 x 32 x 16 product step, for one
+// lane: rows of one operand lane % 32, contracted indices 8 (lane / 32) ... + 7.
+template <class S> struct FragOf;
+template <> struct FragOf<Bf16> { typedef bf16x8 type; };
+template <> struct FragOf<F32> { typedef f32x8 type; };
+
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// Float32: eight products of contracted depth 2, element i of both halves in one.
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// A tile of rows of DH values in LDS. Rows hold 16-byte chunks; chunk c of row r is stored at
+// chunk c ^ mix(r), so that the 16 rows one phase of a wave's 16-byte reads covers hit all 64
+// banks once, and the 8 rows x 64 bytes of a transposing read hit each bank twice (its least).
+template <class S, int DH>
+struct Tile {
+    static constexpr int kRowBytes = DH * S::kBytes;
+    static constexpr int kChunks = kRowBytes / 16;
+
+    __device__ static __forceinline__ int mix(int r)
+    {
+        if constexpr (kChunks == 4) return ((r >> 2) & 1) * 2 + ((r >> 3) & 1);
+        if constexpr (kChunks == 8) return ((r >> 1) & 1) * 4 + ((r >> 2) & 1) * 2 + ((r >> 3) & 1);
+        return (r & 1) * 8 + ((r >> 1) & 1) * 4 + ((r >> 2) & 1) * 2 + ((r >> 3) & 1);
+    }
+    __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ mix(r)) << 4); }
+};
+
+__device__ __forceinline__ bf16x8 as_frag(u32x4 v, Bf16) { return __builtin_bit_cast(bf16x8, v); }
+
+// Contracted step s of row r (lane % 32 of its 32-row group): values 16 s + 8 h ... + 7 of it.
+template <class S, int DH>
+__device__ __forceinline__ typename FragOf<S>::type rows_frag(const uint8_t* tile, int r, int s, int h)
+{
+    typedef Tile<S, DH> T;
+    if constexpr (S::kBytes == 2) {
+        return __builtin_bit_cast(bf16x8, load16(tile + T::at(r, 2 * s + h)));
+    } else {
+        const f32x4 a = __builtin_bit_cast(f32x4, load16(tile + T::at(r, 4 * s + 2 * h)));
+        const f32x4 b = __builtin_bit_cast(f32x4, load16(tile + T::at(r, 4 * s + 2 * h + 1)));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+
+// The transposed operand: column d0 + lane % 32 of rows r0 + 8 (i / 4) + 4 h + i % 4, i < 8 (r0 a
+// multiple of 16). Bfloat16: two transposing reads, each giving a group of 16 lanes one column
+// each of a 4 x 16 block whose rows the group's lanes address, four lanes a row.
+template <class S, int DH>
+__device__ __forceinline__ typename FragOf<S>::type cols_frag(const uint8_t* tile, int r0, int d0, int lane)
+{
+    typedef Tile<S, DH> T;
+    const int h = lane >> 5;
+    if constexpr (S::kBytes == 2) {
+        const int d = d0 + (lane & 16) + 4 * (lane & 3);
+        const int r = r0 + 4 * h + ((lane & 15) >> 2);
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        s16x4 v[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(tile + T::at(r + 8 * u, d >> 3) + (d & 7) * 2));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const s16x8 w = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(bf16x8, w);
+    } else {
+        const int d = d0 + (lane & 31);
+        f32x8 w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = *reinterpret_cast<const float*>(tile + T::at(r0 + 8 * (i >> 2) + 4 * h + (i & 3), d >> 2) + (d & 3) * 4);
+        return w;
+    }
+}
+
+// Registers 8 s ... 8 s + 7 of a score tile as an operand; bfloat16: rounded to nearest even.
+__device__ __forceinline__ bf16x8 tile_frag(const f32x16& p, int s, Bf16)
+{
+    bf16x8 w;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const f32x2 v = {p[8 * s + i], p[8 * s + i + 1]};
+        const bf16x2 b = __builtin_convertvector(v, bf16x2);
+        w[i] = b[0];
+        w[i + 1] = b[1];
+    }
+    return w;
+}
+__device__ __forceinline__ f32x8 tile_frag(const f32x16& p, int s, F32)
+{
+    f32x8 w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = p[8 * s + i];
+    return w;
+}
+
+// Sum and maximum of a value over the two halves of a wave (lanes l and l ^ 32).
+__device__ __forceinline__ float halves_max(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float halves_sum(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+// One 16-byte chunk of a row of dh values: zero past the row's end or for a row that is not live.
+template <class S>
+__device__ __forceinline__ u32x4 load_chunk(const uint8_t* row, int c, int dh, bool live)
+{
+    u32x4 v = {0, 0, 0, 0};
+    if (live && c * (16 / S::kBytes) < dh) v = load16(row + c * 16);
+    return v;
+}
+
+// The rows of one operand fragment set straight from memory: row r's values 16 s + 8 h ... for all s.
+template <class S, int DH>
+__device__ __forceinline__ void load_frags(typename FragOf<S>::type (&f)[DH / 16], const uint8_t* row, int dh,
+                                           bool live, int h)
+{
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) {
+        if constexpr (S::kBytes == 2) {
+            f[s] = __builtin_bit_cast(bf16x8, load_chunk<S>(row, 2 * s + h, dh, live));
+        } else {
+            const f32x4 a = __builtin_bit_cast(f32x4, load_chunk<S>(row, 4 * s + 2 * h, dh, live));
+            const f32x4 b = __builtin_bit_cast(f32x4, load_chunk<S>(row, 4 * s + 2 * h + 1, dh, live));
+            f[s] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+}
+
+// Four consecutive float32 results of a row stored as its type, rounded to nearest even.
+__device__ __forceinline__ void store4(uint8_t* p, float a, float b, float c, float d, Bf16)
+{
+    const f32x2 lo = {a, b}, hi = {c, d};
+    uint2 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2));
+    *reinterpret_cast<uint2*>(p) = w;
+}
+__device__ __forceinline__ void store4(uint8_t* p, float a, float b, float c, float d, F32)
+{
+    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+
+// Row range of image b: packed offsets or N rows each, its count held to [0, N].
+struct Rows {
+    long first;
+    int count;
+};
+__device__ __forceinline__ Rows image_rows(const int32_t* off, int b, int N)
+{
+    if (off == nullptr) return Rows{(long)b * N, N};
+    const int o = off[b];
+    return Rows{(long)o, min(max(off[b + 1] - o, 0), N)};
+}
+
+// How a kernel takes the position bias of a pair.
+enum BiasKind : int {
+    kBiasNone = 0,
+    kBiasGrid = 1,  // no offset of the grid is past the span: one subtraction an entry
+    kBiasFar = 2    // offsets are held to the span, one axis at a time
+};
+
+// A grid position in the form its side of the bias entry needs. kBiasGrid: the byte offset of
+// row * W + column (W = 2 span + 1), so that a pair's entry is query - key + middle. kBiasFar:
+// row and column as two 16-bit halves. Positions outside the grid are held to it, so that a
+// pair's entry is inside the table whatever the caller passed.
+template <int BIAS>
+__device__ __forceinline__ int bias_code(int pos, int gh, int gw, int W)
+{
+    if constexpr (BIAS == kBiasNone) return 0;
+    const int p = min(max(pos, 0), gh * gw - 1);
+    const int r = (int)((unsigned)p / (unsigned)gw), c = p - r * gw;
+    if constexpr (BIAS == kBiasGrid) return (r * W + c) * 4;
+    return (r << 16) | c;
+}
+// Byte offset of the pair's entry in a [W][W] float table.
+template <int BIAS>
+__device__ __forceinline__ int bias_entry(int qcode, int kcode, int span, int W)
+{
+    if constexpr (BIAS == kBiasGrid) return qcode - kcode;  // the query's code has the middle added
+    const int dr = (qcode >> 16) - (kcode >> 16), dc = (qcode & 0xffff) - (kcode & 0xffff);
+    return ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * 4;
+}
+template <int BIAS>
+__device__ __forceinline__ int query_code(int pos, int gh, int gw, int span, int W)
+{
+    const int c = bias_code<BIAS>(pos, gh, gw, W);
+    return BIAS == kBiasGrid ? c + (span * W + span) * 4 : c;
+}
+
+// A score term in the exponent's base: x log2(e), a finite value kept finite (a mask may use the
+// type's lowest value, whose rows then average all of their keys as the softmax of equal scores).
+__device__ __forceinline__ float to_log2(float x)
+{
+    const float y = x * kLog2e;
+    return x >= kLowest ? fmaxf(y, kLowest) : y;
+}
+
+}  // namespace mpm

@@ -127,4 +127,68 @@ hipError_t launch_check_inv(const float* inv, const int32_t* x_off, int B, int N
 hipError_t launch_check_finite(const void* x, const int32_t* x_off, int B, int N, int D, int dt, int32_t* verdict,
                                hipStream_t stream);
 
+// ---- attention over packed images, its position bias, and the norms around a block ----
+
+// Rows of several heads: head j of row r is `dh` values at p + (r row + j head) elements.
+struct HeadRows {
+    uint8_t* p;
+    long row, head;
+};
+
+// The shape and the optional inputs of an attention call (as the C ABI's mpm_attention_call).
+struct AttentionCall {
+    int B, Nq, Nk, H, Hk, dh, dt;
+    float scale;
+    const int32_t *q_off, *k_off;
+    const float* bias;  // [H][2 span + 1][2 span + 1], may be null
+    int span, grid_h, grid_w;
+    const int32_t *q_pos, *k_pos;
+    const float* k_bias;
+};
+
+// Which form of the bias a call takes (the BiasKind values of mpm_attn.h).
+inline int bias_kind(const AttentionCall& a)
+{
+    if (!a.bias) return 0;
+    return (a.grid_h > a.grid_w ? a.grid_h : a.grid_w) - 1 <= a.span ? 1 : 2;
+}
+
+// Lets a kernel take `bytes` of dynamic LDS (more than 64 KB has to be asked for).
+hipError_t allow_lds(const void* kernel, size_t bytes);
+
+// Attention; lse (may be null) receives [row][head] pairs: the maximum taken and the log of the sum, base 2.
+hipError_t launch_attention(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
+                            const HeadRows& out, float* lse, hipStream_t stream);
+// Its gradients; ws holds attention_backward_bytes(a) bytes; dbias may be null.
+size_t attention_backward_bytes(const AttentionCall& a);
+hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dout, const HeadRows& q,
+                                     const HeadRows& k, const HeadRows& v, const HeadRows& out, const float* lse,
+                                     const HeadRows& dq, const HeadRows& dk, const HeadRows& dv, float* dbias, void* ws,
+                                     hipStream_t stream);
+
+// The bias of every offset from the table of buckets, and the table's gradient from the offsets'.
+hipError_t launch_bias_expand(const void* table, const int32_t* lut, int nb, int span, int H, int dt, float* bias,
+                              hipStream_t stream);
+hipError_t launch_bias_gradient(const float* dbias, const int32_t* lut, int nb, int span, int H, int dt, void* dtable,
+                                hipStream_t stream);
+
+// Norms around a block. Rows belong to images only for a gate by image (off, or N rows each);
+// otherwise B = 1, N = R. `chunks` is set by the launcher.
+struct NormCall {
+    int R, D, B, N, chunks, dt;
+    bool layer;
+    float eps;
+    const int32_t* off;
+    const void *w, *b, *post_w, *post_b, *scale, *gate;
+    bool gate_rows;  // one gate row a token instead of one an image
+};
+struct NormGrads {
+    void *dx, *df, *dw, *db, *dpost_w, *dpost_b, *dscale, *dgate;
+};
+hipError_t launch_norm(const NormCall& a, const void* x, const void* f, void* y, void* h, float* stats,
+                       hipStream_t stream);
+size_t norm_backward_bytes(const NormCall& a);
+hipError_t launch_norm_backward(const NormCall& a, const void* dy, const void* dh, const void* y, const void* f,
+                                const float* stats, const NormGrads& g, void* ws, hipStream_t stream);
+
 }  // namespace mpm
