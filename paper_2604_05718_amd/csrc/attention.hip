@@ -10,15 +10,14 @@
 namespace mpm {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
-constexpr int kQueriesPerBlock = 32 * kWaves;
 constexpr int kXcds = 8;
+// Largest running maximum that the score products start from; past it their rounding would show.
+constexpr float kStartMost = 64.0f;
 // The running maximum is raised only when a tile's exceeds it by more than this many powers of
 // two: probabilities then stay below 256, exact to scale, and most tiles skip the rescaling.
 constexpr float kSlack = 8.0f;
 
-template <class S, int DH>
+template <class S>
 constexpr int key_tile()
 {
     return S::kBytes == 2 ? 64 : 32;
@@ -41,164 +40,298 @@ __device__ __forceinline__ bool block_item(int blocks, int pairs, int* blk, int*
     return *pair < pairs;
 }
 
-template <class S, int DH, int BIAS, bool KB>
-__global__ __launch_bounds__(kThreads) void attention_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
-                                                             HeadRows out, float* __restrict__ lse, int blocks)
-{
+// The keys and values of one tile on their way to LDS: loaded to registers a tile ahead.
+template <class S, int DH, int BIAS, bool KB, int THREADS>
+struct Stage {
     typedef Tile<S, DH> T;
+    static constexpr int KT = key_tile<S>();
+    static constexpr int kTileBytes = KT * T::kRowBytes;
+    static constexpr int kBytes = 2 * kTileBytes + KT * 8;  // keys, values, position codes, key biases
+    static constexpr int kPer = KT * T::kChunks / THREADS;
+    static_assert(KT * T::kChunks % THREADS == 0 && THREADS >= KT, "whole chunks a thread");
+    u32x4 k[kPer], v[kPer];
+    const uint8_t *kp[kPer], *vp[kPer];  // this thread's chunks of the next tile
+    int code;
+    float kb;
+
+    __device__ __forceinline__ void init(const HeadRows& kr, const HeadRows& vr, const Rows& rk, int hk, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = t + i * THREADS, ch = e % T::kChunks;
+            const long row = rk.first + e / T::kChunks;
+            kp[i] = kr.p + (row * kr.row + (long)hk * kr.head) * S::kBytes + ch * 16;
+            vp[i] = vr.p + (row * vr.row + (long)hk * vr.head) * S::kBytes + ch * 16;
+        }
+    }
+    // Loads the tile of keys k0 ... and moves on; past the last key or a row's end zeros.
+    __device__ __forceinline__ void load(const AttentionCall& a, const HeadRows& kr, const HeadRows& vr, const Rows& rk,
+                                         int k0, int t)
+    {
+        const long kstep = (long)KT * kr.row * S::kBytes, vstep = (long)KT * vr.row * S::kBytes;
+        const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = t + i * THREADS, ch = e % T::kChunks, kk = k0 + e / T::kChunks;
+            bool in = ch * (16 / S::kBytes) < a.dh && kk < rk.count;
+            if (KB && in) in = a.k_bias[rk.first + kk] > -__builtin_inff();  // a dropped key's rows are not read
+            k[i] = v[i] = zero;
+            if (in) {
+                k[i] = load16(kp[i]);
+                v[i] = load16(vp[i]);
+            }
+            kp[i] += kstep;
+            vp[i] += vstep;
+        }
+        if (t < KT) {
+            const int kk = k0 + t;
+            const bool in = kk < rk.count;
+            if (BIAS != kBiasNone) code = in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
+            if (KB) kb = in ? a.k_bias[rk.first + kk] : -__builtin_inff();
+        }
+    }
+    __device__ __forceinline__ void store(uint8_t* lds, const AttentionCall& a, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = t + i * THREADS, at = T::at(e / T::kChunks, e % T::kChunks);
+            store16(lds + at, k[i]);
+            store16(lds + kTileBytes + at, v[i]);
+        }
+        if (t < KT) {
+            if (BIAS != kBiasNone)
+                reinterpret_cast<int*>(lds + 2 * kTileBytes)[t] = bias_code<BIAS>(code, a.grid_h, a.grid_w, 2 * a.span + 1);
+            if (KB) reinterpret_cast<float*>(lds + 2 * kTileBytes)[KT + t] = to_log2(kb);
+        }
+    }
+};
+
+// Waves a SIMD the registers are held to: three of 32 queries (64 channels, bfloat16; 168 registers and
+// 250 us, 64 images of about 717 tokens, against 170 and 295 us with two), two elsewhere.
+template <class S, int DH, int QT>
+constexpr int waves_per_simd()
+{
+    return S::kBytes == 2 && DH == 64 && QT == 1 ? 3 : 2;
+}
+
+// WAVES waves of QT tiles of 32 queries each share the key tiles.
+template <class S, int DH, int BIAS, bool KB, int WAVES, int QT>
+__global__ __launch_bounds__(WAVES* kWave, waves_per_simd<S, DH, QT>()) void attention_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
+                                                                HeadRows out, float* __restrict__ lse, int blocks)
+{
+    constexpr int THREADS = WAVES * kWave;
+    typedef Stage<S, DH, BIAS, KB, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
-    constexpr int KT = key_tile<S, DH>();
-    constexpr int kTileBytes = KT * T::kRowBytes;
+    constexpr int KT = Staged::KT;
+    constexpr bool kBf = S::kBytes == 2;
     extern __shared__ __align__(16) uint8_t lds[];
-    uint8_t* kt = lds;
-    uint8_t* vt = lds + kTileBytes;
-    int* codes = reinterpret_cast<int*>(lds + 2 * kTileBytes);
-    float* kbs = reinterpret_cast<float*>(codes + KT);
-    float* table = reinterpret_cast<float*>(kbs + KT);
+    float* table = reinterpret_cast<float*>(lds + 2 * Staged::kBytes);
+    const int table_at = lds_address(table);
 
     int blk, pair;
     if (!block_item(blocks, a.B * a.H, &blk, &pair)) return;
     const int b = pair / a.H, hd = pair - b * a.H, hk = hd / (a.H / a.Hk);
     const Rows rq = image_rows(a.q_off, b, a.Nq), rk = image_rows(a.k_off, b, a.Nk);
-    if (blk * kQueriesPerBlock >= rq.count) return;
+    const int q0 = blk * 32 * WAVES * QT;
+    if (q0 >= rq.count) return;
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, h = lane >> 5;
-    const int qi = blk * kQueriesPerBlock + wave * 32 + l32;
-    const bool live = qi < rq.count;
     const int W = 2 * a.span + 1;
     const float c = a.scale * kLog2e;
+    // The score products may start from -maximum / c, which takes the maximum off for nothing
+    // (bfloat16: the sum's rounding is far below the operands' own).
+    const bool can_start = kBf && fabsf(c) > 1e-3f && fabsf(c) < 1e3f;
 
-    Frag qf[DH / 16];
-    const uint8_t* qrow = q.p + ((rq.first + (live ? qi : 0)) * q.row + (long)hd * q.head) * S::kBytes;
-    load_frags<S, DH>(qf, qrow, a.dh, live, h);
-    int qcode = 0;
-    if (BIAS != kBiasNone) {
-        qcode = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0, a.grid_h, a.grid_w, a.span, W);
-        const float* src = a.bias + (long)hd * W * W;
-        for (int e = t; e < W * W; e += kThreads) table[e] = to_log2(src[e]);
+    Staged stage;
+    stage.init(k, v, rk, hk, t);
+    stage.load(a, k, v, rk, 0, t);
+
+    Frag qf[QT][DH / 16];
+    int qcode[QT];
+    f32x16 acc[QT][DH / 32], start[QT];
+    float m[QT], sum[QT];  // the maximum taken (-inf: no key yet) and the sum
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int qi = q0 + (wave * QT + i) * 32 + l32;
+        const bool live = qi < rq.count;
+        load_frags<S, DH>(qf[i], q.p + ((rq.first + (live ? qi : 0)) * q.row + (long)hd * q.head) * S::kBytes, a.dh, live,
+                          h);
+        qcode[i] = 0;
+        if (BIAS != kBiasNone)
+            qcode[i] = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0, a.grid_h, a.grid_w, a.span, W, table_at);
+        m[i] = -__builtin_inff();
+        sum[i] = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            start[i][r] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d) acc[i][d][r] = 0.0f;
+        }
     }
+    if (BIAS != kBiasNone) {
+        load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
+    }
+    stage.store(lds, a, t);
+    __syncthreads();
 
-    f32x16 acc[DH / 32];
+    const bool works = q0 + wave * QT * 32 < rq.count;  // a wave past the image's end only brings tiles
+    bool apart = !can_start;  // whether the maximum is subtracted instead
+    for (int k0 = 0, buf = 0; k0 < rk.count; k0 += KT, buf ^= 1) {
+        const uint8_t* kt = lds + buf * Staged::kBytes;
+        const uint8_t* vt = kt + Staged::kTileBytes;
+        const int* codes = reinterpret_cast<const int*>(vt + Staged::kTileBytes);
+        const float* kbs = reinterpret_cast<const float*>(codes + KT);
+        const bool more = k0 + KT < rk.count;
+        if (more) stage.load(a, k, v, rk, k0 + KT, t);
+#pragma unroll 1
+        for (int u = 0; u < (works ? KT / 32 : 0); ++u) {
+            f32x16 s[QT];
 #pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
+            for (int st = 0; st < DH / 16; ++st) {
+                const Frag kf = rows_frag<S, DH>(kt, 32 * u + l32, st, h);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
-    float m = -__builtin_inff(), sum = 0.0f;
-
-    for (int k0 = 0; k0 < rk.count; k0 += KT) {
-        __syncthreads();
-        if (t < KT) {
-            const int kk = k0 + t;
-            const bool in = kk < rk.count;
-            if (BIAS != kBiasNone)
-                codes[t] = bias_code<BIAS>(in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0, a.grid_h, a.grid_w, W);
-            if (KB) kbs[t] = in ? to_log2(a.k_bias[rk.first + kk]) : -__builtin_inff();
-        }
-        for (int e = t; e < KT * T::kChunks; e += kThreads) {
-            const int r = e / T::kChunks, ch = e % T::kChunks, kk = k0 + r;
-            bool in = kk < rk.count;
-            if (KB && in) in = a.k_bias[rk.first + kk] > -__builtin_inff();  // a dropped key's rows are not read
-            const long row = rk.first + (in ? kk : 0);
-            store16(kt + T::at(r, ch), load_chunk<S>(k.p + (row * k.row + (long)hk * k.head) * S::kBytes, ch, a.dh, in));
-            store16(vt + T::at(r, ch), load_chunk<S>(v.p + (row * v.row + (long)hk * v.head) * S::kBytes, ch, a.dh, in));
-        }
-        __syncthreads();
-
-        f32x16 s[KT / 32];
+                for (int i = 0; i < QT; ++i) s[i] = mma(kf, qf[i][st], st == 0 ? start[i] : s[i]);
+            }
+            bool any_up = false;
+            float top[QT];
 #pragma unroll
-        for (int u = 0; u < KT / 32; ++u) {
+            for (int i = 0; i < QT; ++i) {
+                top[i] = -__builtin_inff();
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = 0.0f;
+                for (int g = 0; g < 4; ++g) {
+                    const int at = 32 * u + 8 * g + 4 * h;
+                    i32x4 kc = {0, 0, 0, 0};
+                    f32x4 kb = {0, 0, 0, 0};
+                    if (BIAS != kBiasNone) kc = *reinterpret_cast<const i32x4*>(codes + at);
+                    if (KB) kb = *reinterpret_cast<const f32x4*>(kbs + at);
 #pragma unroll
-            for (int st = 0; st < DH / 16; ++st) s[u] = mma(rows_frag<S, DH>(kt, 32 * u + l32, st, h), qf[st], s[u]);
-        }
-        float top = -__builtin_inff();
-#pragma unroll
-        for (int u = 0; u < KT / 32; ++u)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = 32 * u + 8 * g + 4 * h;
-                i32x4 kc = {0, 0, 0, 0};
-                f32x4 kb = {0, 0, 0, 0};
-                if (BIAS != kBiasNone) kc = *reinterpret_cast<const i32x4*>(codes + at);
-                if (KB) kb = *reinterpret_cast<const f32x4*>(kbs + at);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float x = s[u][4 * g + e];
-                    if (BIAS != kBiasNone) {
-                        const int en = bias_entry<BIAS>(qcode, kc[e], a.span, W);
-                        x = fmaf(x, c, *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(table) + en));
-                    } else {
-                        x *= c;
+                    for (int e = 0; e < 4; ++e) {
+                        float x = s[i][4 * g + e];
+                        if (BIAS != kBiasNone) {
+                            x = fmaf(x, c, lds_at(bias_entry<BIAS>(qcode[i], kc[e], a.span, W, table_at)));
+                        } else {
+                            x *= c;
+                        }
+                        if (KB) x = kb[e] > -__builtin_inff() ? x + kb[e] : -__builtin_inff();
+                        s[i][4 * g + e] = x;
                     }
-                    if (KB) x = kb[e] > -__builtin_inff() ? x + kb[e] : -__builtin_inff();
-                    else if (k0 + KT > rk.count) x = k0 + at + e < rk.count ? x : -__builtin_inff();
-                    s[u][4 * g + e] = x;
-                    top = fmaxf(top, x);
+                }
+                if (!KB && k0 + 32 * u + 32 > rk.count) {
+                    int left = rk.count - k0 - 32 * u - 4 * h;
+                    asm volatile("" : "+v"(left));  // keeps this a branch: no selects in whole tiles
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (8 * (r / 4) + r % 4 >= left) s[i][r] = -__builtin_inff();
+                }
+                if (apart) {
+                    float base = m[i] == -__builtin_inff() ? 0.0f : m[i];
+                    asm volatile("" : "+v"(base));
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[i][r] -= base;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top[i] = fmaxf(top[i], s[i][r]);
+                any_up |= top[i] >= (m[i] == -__builtin_inff() ? kLowest : kSlack);
+            }
+            if (__any(any_up)) {
+                bool far = false;
+#pragma unroll
+                for (int i = 0; i < QT; ++i) {
+                    const float full = halves_max(top[i]);
+                    const bool fresh = m[i] == -__builtin_inff();
+                    // What the maximum rises by (a first key: all of its score).
+                    const float up = fresh ? (full == -__builtin_inff() ? 0.0f : full) : fmaxf(full, 0.0f);
+                    if (!fresh) m[i] += up;
+                    else if (full > -__builtin_inff()) m[i] = up;
+                    const float f = fresh ? 0.0f : __builtin_amdgcn_exp2f(-up);
+                    sum[i] *= f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[i][r] -= up;
+#pragma unroll
+                    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][d][r] *= f;
+                    far |= fabsf(m[i]) > kStartMost && m[i] > -__builtin_inff();
+                }
+                apart = !can_start || __any(far);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) {
+                    const float x = apart || m[i] == -__builtin_inff() ? 0.0f : -m[i] / c;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) start[i][r] = x;
                 }
             }
-        top = halves_max(top);
-        if (__any(top > m + kSlack)) {
-            const float up = fmaxf(m, top);
-            const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - up);
-            m = up;
-            sum *= f;
 #pragma unroll
-            for (int d = 0; d < DH / 32; ++d)
+            for (int i = 0; i < QT; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[d][r] *= f;
-        }
-        const float base = m == -__builtin_inff() ? 0.0f : m;  // every key so far masked
-#pragma unroll
-        for (int u = 0; u < KT / 32; ++u) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[u][r] = __builtin_amdgcn_exp2f(s[u][r] - base);
-                sum += s[u][r];
-            }
+                for (int r = 0; r < 16; ++r) {
+                    s[i][r] = __builtin_amdgcn_exp2f(s[i][r]);
+                    sum[i] += s[i][r];
+                }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const Frag p = tile_frag(s[u], st, S{});
+                Frag p[QT];
 #pragma unroll
-                for (int d = 0; d < DH / 32; ++d)
-                    acc[d] = mma(cols_frag<S, DH>(vt, 32 * u + 16 * st, 32 * d, lane), p, acc[d]);
+                for (int i = 0; i < QT; ++i) p[i] = tile_frag(s[i], st, S{});
+#pragma unroll
+                for (int d = 0; d < DH / 32; ++d) {
+                    const Frag vf = cols_frag<S, DH>(vt, 32 * u + 16 * st, 32 * d, lane);
+#pragma unroll
+                    for (int i = 0; i < QT; ++i) acc[i][d] = mma(vf, p[i], acc[i][d]);
+                }
             }
         }
+        if (more) stage.store(lds + (buf ^ 1) * Staged::kBytes, a, t);
+        __syncthreads();
     }
 
-    sum = halves_sum(sum);
-    if (!live) return;
-    const float inv = sum > 0.0f ? 1.0f / sum : (sum == 0.0f ? 0.0f : sum);  // no key: zeros
-    uint8_t* orow = out.p + ((rq.first + qi) * out.row + (long)hd * out.head) * S::kBytes;
 #pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int at = 32 * d + 8 * g + 4 * h;
-            if (at < a.dh)
-                store4(orow + at * S::kBytes, acc[d][4 * g] * inv, acc[d][4 * g + 1] * inv, acc[d][4 * g + 2] * inv,
-                       acc[d][4 * g + 3] * inv, S{});
-        }
-    if (lse && h == 0)
-        reinterpret_cast<float2*>(lse)[(rq.first + qi) * a.H + hd] =
-            sum == 0.0f ? make_float2(-__builtin_inff(), 0.0f) : make_float2(m, __builtin_log2f(sum));
+    for (int i = 0; i < QT; ++i) {
+        const int qi = q0 + (wave * QT + i) * 32 + l32;
+        const float total = halves_sum(sum[i]);
+        const bool live = qi < rq.count;
+        const float inv = total > 0.0f ? 1.0f / total : (total == 0.0f ? 0.0f : total);  // no key: zeros
+        store_rows(out.p + ((rq.first + (live ? qi : 0)) * out.row + (long)hd * out.head) * S::kBytes, acc[i], inv, a.dh,
+                   live, h, S{});
+        if (lse && live && h == 0)
+            reinterpret_cast<float2*>(lse)[(rq.first + qi) * a.H + hd] =
+                total == 0.0f ? make_float2(-__builtin_inff(), 0.0f) : make_float2(m[i], __builtin_log2f(total));
+    }
 }
 
+template <class S, int DH, int BIAS, bool KB, int WAVES, int QT>
+hipError_t launch_as(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
+                     const HeadRows& out, float* lse, hipStream_t stream)
+{
+    constexpr int THREADS = WAVES * kWave, kQueries = 32 * WAVES * QT;
+    const int W = 2 * a.span + 1;
+    const size_t bytes = 2 * Stage<S, DH, BIAS, KB, THREADS>::kBytes + (BIAS != kBiasNone ? (size_t)W * W * 4 : 0);
+    const int blocks = (a.Nq + kQueries - 1) / kQueries;
+    const long pairs = (long)a.B * a.H;
+    const long grid = (pairs >= 4 * kXcds ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * blocks;
+    if (grid * THREADS > UINT32_MAX) return hipErrorInvalidConfiguration;
+    auto kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT>;
+    hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(THREADS), bytes, stream, a, q, k, v, out, lse, blocks);
+    return hipGetLastError();
+}
+
+// Eight waves of 64 queries where an image has queries for several such blocks, or where the bias
+// table leaves LDS for one workgroup only; otherwise four waves of 32, three workgroups a compute
+// unit. Bfloat16, 64 channels, 12 heads, four waves / eight: 8 images of 4096 tokens without a bias
+// 527 / 484 us, with one of 127 x 127 (16 heads) 1810 / 770, 8 of 2304 with one of 95 x 95 288 / 236, 8 of
+// about 1380 144 / 149, 64 of about 717 with one of 63 x 63 254 / 287, one of 1024 41 / 60.
 template <class S, int DH, int BIAS, bool KB>
 hipError_t launch(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v, const HeadRows& out,
                   float* lse, hipStream_t stream)
 {
-    constexpr int KT = key_tile<S, DH>();
-    const int W = 2 * a.span + 1;
-    const size_t bytes = 2 * KT * Tile<S, DH>::kRowBytes + KT * 8 + (BIAS != kBiasNone ? (size_t)W * W * 4 : 0);
-    const int blocks = (a.Nq + kQueriesPerBlock - 1) / kQueriesPerBlock;
-    const long pairs = (long)a.B * a.H;
-    const long grid = (pairs >= 4 * kXcds ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * blocks;
-    if (grid * kThreads > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = attention_kernel<S, DH, BIAS, KB>;
-    hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), bytes, stream, a, q, k, v, out, lse, blocks);
-    return hipGetLastError();
+    constexpr long kLargeTable = 48 << 10;
+    if constexpr (S::kBytes == 2 && DH == 64) {
+        const long W = 2 * a.span + 1;
+        if (a.Nq >= 1792 || (BIAS != kBiasNone && W * W * 4 > kLargeTable && a.Nq > 256))
+            return launch_as<S, DH, BIAS, KB, 8, 2>(a, q, k, v, out, lse, stream);
+    }
+    return launch_as<S, DH, BIAS, KB, 4, 1>(a, q, k, v, out, lse, stream);
 }
 
 template <class S, int DH>

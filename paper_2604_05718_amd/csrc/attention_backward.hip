@@ -101,6 +101,7 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
     float* deltas = lows + QT;
     int* apart = reinterpret_cast<int*>(deltas + QT);  // whether a query of the tile has its terms taken apart
     float* table = reinterpret_cast<float*>(apart + 4);
+    const int table_at = lds_address(table);
 
     const int pair = blockIdx.x / blocks, blk = blockIdx.x % blocks;
     const int b = pair / a.Hk, hk = pair - b * a.Hk, group = a.H / a.Hk;
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
                 const bool in = qi < rq.count;
                 if (BIAS != kBiasNone)
                     codes[t] = query_code<BIAS>(in ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0, a.grid_h, a.grid_w,
-                                                a.span, W);
+                                                a.span, W, table_at);
                 const float2 l = in ? lse[(rq.first + qi) * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
                 const bool split = __any(split_taken(l));
                 const Taken tk = taken(l, split);
@@ -175,8 +176,7 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
                         float x = s[4 * g + e] * c;
                         if (BIAS != kBiasNone)
                             x = fmaf(s[4 * g + e], c,
-                                     *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(table) +
-                                                                     bias_entry<BIAS>(qc[e], kcode, a.span, W)));
+                                     lds_at(bias_entry<BIAS>(qc[e], kcode, a.span, W, table_at)));
                         x = x + kb - ls[e];
                         if (split) x -= lo[e];
                         const float p = live ? __builtin_amdgcn_exp2f(x) : 0.0f;
@@ -197,24 +197,15 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
         }
     }
 
-    if (!exists) return;
-    uint8_t* krow_out = dk.p + (krow * dk.row + (long)hk * dk.head) * S::kBytes;
-    uint8_t* vrow_out = dv.p + (krow * dv.row + (long)hk * dv.head) * S::kBytes;
+    // A dropped key's gradients are zero, whatever its rows hold.
+    if (!live) {
 #pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
+        for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int at = 32 * d + 8 * g + 4 * h;
-            if (at >= a.dh) continue;
-            float x[4], y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = live ? gk[d][4 * g + e] * a.scale : 0.0f;  // a dropped key's gradients are zero
-                y[e] = live ? gv[d][4 * g + e] : 0.0f;
-            }
-            store4(krow_out + at * S::kBytes, x[0], x[1], x[2], x[3], S{});
-            store4(vrow_out + at * S::kBytes, y[0], y[1], y[2], y[3], S{});
-        }
+            for (int r = 0; r < 16; ++r) gk[d][r] = gv[d][r] = 0.0f;
+    }
+    store_rows(dk.p + (krow * dk.row + (long)hk * dk.head) * S::kBytes, gk, a.scale, a.dh, exists, h, S{});
+    store_rows(dv.p + (krow * dv.row + (long)hk * dv.head) * S::kBytes, gv, 1.0f, a.dh, exists, h, S{});
 }
 
 // dQ of 128 queries of one head, and their part of dbias: every dS is added into a table in LDS,
@@ -237,6 +228,7 @@ __global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall 
     int* codes = reinterpret_cast<int*>(lds + 2 * kTileBytes);
     float* kbs = reinterpret_cast<float*>(codes + KT);
     float* table = kbs + KT;
+    const int table_at = lds_address(table);
 
     const int pair = blockIdx.x / blocks, blk = blockIdx.x % blocks;
     const int b = pair / a.H, hd = pair - b * a.H, hk = hd / (a.H / a.Hk);
@@ -259,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall 
     load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
     int qcode = 0;
     if (BIAS != kBiasNone) {
-        qcode = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0, a.grid_h, a.grid_w, a.span, W);
+        qcode = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0, a.grid_h, a.grid_w, a.span, W, table_at);
         const float* src = a.bias + (long)hd * W * W;
         for (int e = t; e < W * W; e += kThreads) {
             table[e] = to_log2(src[e]);
@@ -305,8 +297,7 @@ __global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall 
                     float x = s[4 * g + e] * c;
                     if (BIAS != kBiasNone)
                         x = fmaf(s[4 * g + e], c,
-                                 *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(table) +
-                                                                 bias_entry<BIAS>(qcode, kc[e], a.span, W)));
+                                 lds_at(bias_entry<BIAS>(qcode, kc[e], a.span, W, table_at)));
                     x = x + kb[e] - ls.first;
                     if (split) x -= ls.second;
                     const float p = kb[e] > -__builtin_inff() ? __builtin_amdgcn_exp2f(x) : 0.0f;
@@ -333,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall 
                             if (k0 + at < rk.count)
                                 __hip_atomic_fetch_add(
                                     reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(sums) +
-                                                             bias_entry<BIAS>(qcode, codes[at], a.span, W)),
+                                                             bias_entry<BIAS>(qcode, codes[at], a.span, W, table_at) - table_at),
                                     dsum[u][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
                         }
                 }
@@ -347,17 +338,7 @@ __global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall 
         float* part = parts + (long)blockIdx.x * W * W;
         for (int e = t; e < W * W; e += kThreads) part[e] = sums[e];
     }
-    if (!live) return;
-    uint8_t* row = dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes;
-#pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int at = 32 * d + 8 * g + 4 * h;
-            if (at < a.dh)
-                store4(row + at * S::kBytes, gq[d][4 * g] * a.scale, gq[d][4 * g + 1] * a.scale,
-                       gq[d][4 * g + 2] * a.scale, gq[d][4 * g + 3] * a.scale, S{});
-        }
+    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale, a.dh, live, h, S{});
 }
 
 // dbias[head][e] = the workgroups' parts, images and query blocks in order.

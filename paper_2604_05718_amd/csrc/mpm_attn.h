@@ -162,18 +162,44 @@ __device__ __forceinline__ void load_frags(typename FragOf<S>::type (&f)[DH / 16
     }
 }
 
-// Four consecutive float32 results of a row stored as its type, rounded to nearest even.
-__device__ __forceinline__ void store4(uint8_t* p, float a, float b, float c, float d, Bf16)
+// Stores a wave's 32 result rows from product tiles: lane's row (lane % 32) at `row`, column
+// 32 d + 8 g + 4 h + e of it in register 4 g + e of tile d, times f, rounded to nearest even.
+// Bfloat16: the halves of a wave exchange their four-column pieces of two groups, so that every
+// store is 16 bytes of one row.
+template <int D>
+__device__ __forceinline__ void store_rows(uint8_t* row, const f32x16 (&x)[D], float f, int dh, bool live, int h, Bf16)
 {
-    const f32x2 lo = {a, b}, hi = {c, d};
-    uint2 w;
-    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2));
-    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2));
-    *reinterpret_cast<uint2*>(p) = w;
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+            u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const f32x2 a = {x[d][4 * g + 2 * j] * f, x[d][4 * g + 2 * j + 1] * f};
+                const f32x2 b = {x[d][4 * g + 4 + 2 * j] * f, x[d][4 * g + 5 + 2 * j] * f};
+                const auto p = __builtin_amdgcn_permlane32_swap(
+                    __builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)),
+                    __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2)), false, false);
+                w[j] = p[0];
+                w[2 + j] = p[1];
+            }
+            const int at = 32 * d + 8 * (g + h);
+            if (live && at < dh) store16(row + at * 2, w);
+        }
 }
-__device__ __forceinline__ void store4(uint8_t* p, float a, float b, float c, float d, F32)
+template <int D>
+__device__ __forceinline__ void store_rows(uint8_t* row, const f32x16 (&x)[D], float f, int dh, bool live, int h, F32)
 {
-    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int at = 32 * d + 8 * g + 4 * h;
+            if (live && at < dh)
+                *reinterpret_cast<float4*>(row + at * 4) =
+                    make_float4(x[d][4 * g] * f, x[d][4 * g + 1] * f, x[d][4 * g + 2] * f, x[d][4 * g + 3] * f);
+        }
 }
 
 // Row range of image b: packed offsets or N rows each, its count held to [0, N].
@@ -208,20 +234,30 @@ __device__ __forceinline__ int bias_code(int pos, int gh, int gw, int W)
     if constexpr (BIAS == kBiasGrid) return (r * W + c) * 4;
     return (r << 16) | c;
 }
-// Byte offset of the pair's entry in a [W][W] float table.
+// Where the pair's entry is: qcode's side holds the table's address (kBiasFar: base does).
 template <int BIAS>
-__device__ __forceinline__ int bias_entry(int qcode, int kcode, int span, int W)
+__device__ __forceinline__ int bias_entry(int qcode, int kcode, int span, int W, int base)
 {
-    if constexpr (BIAS == kBiasGrid) return qcode - kcode;  // the query's code has the middle added
+    if constexpr (BIAS == kBiasGrid) return qcode - kcode;
     const int dr = (qcode >> 16) - (kcode >> 16), dc = (qcode & 0xffff) - (kcode & 0xffff);
-    return ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * 4;
+    return base + ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * 4;
 }
+// A query's side: with the middle of the table at LDS address `base` added (kBiasGrid).
 template <int BIAS>
-__device__ __forceinline__ int query_code(int pos, int gh, int gw, int span, int W)
+__device__ __forceinline__ int query_code(int pos, int gh, int gw, int span, int W, int base)
 {
     const int c = bias_code<BIAS>(pos, gh, gw, W);
-    return BIAS == kBiasGrid ? c + (span * W + span) * 4 : c;
+    return BIAS == kBiasGrid ? c + (span * W + span) * 4 + base : c;
 }
+
+// An LDS address as the 32-bit number the hardware takes, and a float at one: a pair's bias is read at
+// the table's address plus its entry, whose query part holds the address already.
+typedef __attribute__((address_space(3))) const float lds_float;
+__device__ __forceinline__ int lds_address(const void* p)
+{
+    return (int)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)p;
+}
+__device__ __forceinline__ float lds_at(int address) { return *(lds_float*)(uintptr_t)(uint32_t)address; }
 
 // A score term in the exponent's base: x log2(e), a finite value kept finite (a mask may use the
 // type's lowest value, whose rows then average all of their keys as the softmax of equal scores).
@@ -229,6 +265,21 @@ __device__ __forceinline__ float to_log2(float x)
 {
     const float y = x * kLog2e;
     return x >= kLowest ? fmaxf(y, kLowest) : y;
+}
+
+// A head's bias table to LDS, in base 2: eight loads a thread in flight.
+template <int THREADS>
+__device__ __forceinline__ void load_table(float* table, const float* src, int n, int t)
+{
+    constexpr int kFlight = 8;
+    for (int e0 = t; e0 < n; e0 += THREADS * kFlight) {
+        float v[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) v[i] = src[min(e0 + i * THREADS, n - 1)];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+            if (e0 + i * THREADS < n) table[e0 + i * THREADS] = to_log2(v[i]);
+    }
 }
 
 }  // namespace mpm
