@@ -116,7 +116,7 @@ constexpr int waves_per_simd()
 
 // WAVES waves of QT tiles of 32 queries each share the key tiles.
 template <class S, int DH, int BIAS, bool KB, int WAVES, int QT>
-__global__ __launch_bounds__(WAVES* kWave, waves_per_simd<S, DH, QT>()) void attention_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
+__global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void attention_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
                                                                 HeadRows out, float* __restrict__ lse, int blocks)
 {
     constexpr int THREADS = WAVES * kWave;
