@@ -10,7 +10,6 @@
 namespace mpm {
 namespace {
 
-constexpr int kXcds = 8;
 // Largest running maximum that the score products start from; past it their rounding would show.
 constexpr float kStartMost = 64.0f;
 // The running maximum is raised only when a tile's exceeds it by more than this many powers of
@@ -23,88 +22,12 @@ constexpr int key_tile()
     return S::kBytes == 2 ? 64 : 32;
 }
 
-// The workgroup's query block and (image, head) pair. Blocks are dealt round-robin to the 8
-// XCDs, each with its own L2: pairs are dealt to XCDs whole, so that the blocks that read one
-// pair's keys share an L2 (few pairs: in order, since whole pairs would leave XCDs idle).
-__device__ __forceinline__ bool block_item(int blocks, int pairs, int* blk, int* pair)
+// One of the two buffers: a tile of keys and of values, their position codes and biases.
+template <class S, int DH>
+constexpr int buffer_bytes()
 {
-    const int i = blockIdx.x;
-    if (pairs >= 4 * kXcds) {
-        const int slot = i / kXcds;
-        *pair = slot / blocks * kXcds + i % kXcds;
-        *blk = slot % blocks;
-    } else {
-        *pair = i / blocks;
-        *blk = i % blocks;
-    }
-    return *pair < pairs;
+    return key_tile<S>() * (2 * Tile<S, DH>::kRowBytes + 8);
 }
-
-// The keys and values of one tile on their way to LDS: loaded to registers a tile ahead.
-template <class S, int DH, int BIAS, bool KB, int THREADS>
-struct Stage {
-    typedef Tile<S, DH> T;
-    static constexpr int KT = key_tile<S>();
-    static constexpr int kTileBytes = KT * T::kRowBytes;
-    static constexpr int kBytes = 2 * kTileBytes + KT * 8;  // keys, values, position codes, key biases
-    static constexpr int kPer = KT * T::kChunks / THREADS;
-    static_assert(KT * T::kChunks % THREADS == 0 && THREADS >= KT, "whole chunks a thread");
-    u32x4 k[kPer], v[kPer];
-    const uint8_t *kp[kPer], *vp[kPer];  // this thread's chunks of the next tile
-    int code;
-    float kb;
-
-    __device__ __forceinline__ void init(const HeadRows& kr, const HeadRows& vr, const Rows& rk, int hk, int t)
-    {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int e = t + i * THREADS, ch = e % T::kChunks;
-            const long row = rk.first + e / T::kChunks;
-            kp[i] = kr.p + (row * kr.row + (long)hk * kr.head) * S::kBytes + ch * 16;
-            vp[i] = vr.p + (row * vr.row + (long)hk * vr.head) * S::kBytes + ch * 16;
-        }
-    }
-    // Loads the tile of keys k0 ... and moves on; past the last key or a row's end zeros.
-    __device__ __forceinline__ void load(const AttentionCall& a, const HeadRows& kr, const HeadRows& vr, const Rows& rk,
-                                         int k0, int t)
-    {
-        const long kstep = (long)KT * kr.row * S::kBytes, vstep = (long)KT * vr.row * S::kBytes;
-        const u32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int e = t + i * THREADS, ch = e % T::kChunks, kk = k0 + e / T::kChunks;
-            bool in = ch * (16 / S::kBytes) < a.dh && kk < rk.count;
-            if (KB && in) in = a.k_bias[rk.first + kk] > -__builtin_inff();  // a dropped key's rows are not read
-            k[i] = v[i] = zero;
-            if (in) {
-                k[i] = load16(kp[i]);
-                v[i] = load16(vp[i]);
-            }
-            kp[i] += kstep;
-            vp[i] += vstep;
-        }
-        if (t < KT) {
-            const int kk = k0 + t;
-            const bool in = kk < rk.count;
-            if (BIAS != kBiasNone) code = in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
-            if (KB) kb = in ? a.k_bias[rk.first + kk] : -__builtin_inff();
-        }
-    }
-    __device__ __forceinline__ void store(uint8_t* lds, const AttentionCall& a, int t) const
-    {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int e = t + i * THREADS, at = T::at(e / T::kChunks, e % T::kChunks);
-            store16(lds + at, k[i]);
-            store16(lds + kTileBytes + at, v[i]);
-        }
-        if (t < KT) {
-            if (BIAS != kBiasNone)
-                reinterpret_cast<int*>(lds + 2 * kTileBytes)[t] = bias_code<BIAS>(code, a.grid_h, a.grid_w, 2 * a.span + 1);
-            if (KB) reinterpret_cast<float*>(lds + 2 * kTileBytes)[KT + t] = to_log2(kb);
-        }
-    }
-};
 
 // Waves a SIMD the registers are held to: three of 32 queries (64 channels, bfloat16; 168 registers and
 // 250 us, 64 images of about 717 tokens, against 170 and 295 us with two), two elsewhere.
@@ -120,12 +43,13 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                                                                 HeadRows out, float* __restrict__ lse, int blocks)
 {
     constexpr int THREADS = WAVES * kWave;
-    typedef Stage<S, DH, BIAS, KB, THREADS> Staged;
+    constexpr int KT = key_tile<S>();
+    typedef PairStage<S, DH, KT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
-    constexpr int KT = Staged::KT;
+    constexpr int kBuffer = buffer_bytes<S, DH>();
     constexpr bool kBf = S::kBytes == 2;
     extern __shared__ __align__(16) uint8_t lds[];
-    float* table = reinterpret_cast<float*>(lds + 2 * Staged::kBytes);
+    float* table = reinterpret_cast<float*>(lds + 2 * kBuffer);
     const int table_at = lds_address(table);
 
     int blk, pair;
@@ -142,8 +66,29 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     const bool can_start = kBf && fabsf(c) > 1e-3f && fabsf(c) < 1e3f;
 
     Staged stage;
-    stage.init(k, v, rk, hk, t);
-    stage.load(a, k, v, rk, 0, t);
+    int pos = 0;
+    float kbias = 0.0f;
+    const float* drop = KB ? a.k_bias + rk.first : nullptr;
+    auto load = [&](int k0) {
+        stage.template load<KB>(k, v, a.dh, rk.count, drop, k0, t);
+        if (t < KT) {
+            const int kk = k0 + t;
+            const bool in = kk < rk.count;
+            if (BIAS != kBiasNone) pos = in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
+            if (KB) kbias = in ? drop[kk] : -__builtin_inff();
+        }
+    };
+    auto store = [&](int buf) {
+        uint8_t* at = lds + buf * kBuffer;
+        stage.store(at, t);
+        if (t < KT) {
+            int* codes = reinterpret_cast<int*>(at + 2 * Staged::kTileBytes);
+            if (BIAS != kBiasNone) codes[t] = bias_code<BIAS>(pos, a.grid_h, a.grid_w, W);
+            if (KB) reinterpret_cast<float*>(codes + KT)[t] = to_log2(kbias);
+        }
+    };
+    stage.init(k, v, rk.first, hk, t);
+    load(0);
 
     Frag qf[QT][DH / 16];
     int qcode[QT];
@@ -170,18 +115,18 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     if (BIAS != kBiasNone) {
         load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
     }
-    stage.store(lds, a, t);
+    store(0);
     __syncthreads();
 
     const bool works = q0 + wave * QT * 32 < rq.count;  // a wave past the image's end only brings tiles
     bool apart = !can_start;  // whether the maximum is subtracted instead
     for (int k0 = 0, buf = 0; k0 < rk.count; k0 += KT, buf ^= 1) {
-        const uint8_t* kt = lds + buf * Staged::kBytes;
+        const uint8_t* kt = lds + buf * kBuffer;
         const uint8_t* vt = kt + Staged::kTileBytes;
         const int* codes = reinterpret_cast<const int*>(vt + Staged::kTileBytes);
         const float* kbs = reinterpret_cast<const float*>(codes + KT);
         const bool more = k0 + KT < rk.count;
-        if (more) stage.load(a, k, v, rk, k0 + KT, t);
+        if (more) load(k0 + KT);
 #pragma unroll 1
         for (int u = 0; u < (works ? KT / 32 : 0); ++u) {
             f32x16 s[QT];
@@ -280,7 +225,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                 }
             }
         }
-        if (more) stage.store(lds + (buf ^ 1) * Staged::kBytes, a, t);
+        if (more) store(buf ^ 1);
         __syncthreads();
     }
 
@@ -304,10 +249,9 @@ hipError_t launch_as(const AttentionCall& a, const HeadRows& q, const HeadRows& 
 {
     constexpr int THREADS = WAVES * kWave, kQueries = 32 * WAVES * QT;
     const int W = 2 * a.span + 1;
-    const size_t bytes = 2 * Stage<S, DH, BIAS, KB, THREADS>::kBytes + (BIAS != kBiasNone ? (size_t)W * W * 4 : 0);
+    const size_t bytes = 2 * buffer_bytes<S, DH>() + (BIAS != kBiasNone ? (size_t)W * W * 4 : 0);
     const int blocks = (a.Nq + kQueries - 1) / kQueries;
-    const long pairs = (long)a.B * a.H;
-    const long grid = (pairs >= 4 * kXcds ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * blocks;
+    const long grid = block_grid((long)a.B * a.H, blocks);
     if (grid * THREADS > UINT32_MAX) return hipErrorInvalidConfiguration;
     auto kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);

@@ -3,33 +3,76 @@
 //   P = 2^(s - maximum - log2 sum), dP = dO V^T, D_i = dO_i . o_i, dS = P (dP - D),
 //   dV = P^T dO, dK = scale dS^T Q, dQ = scale dS K, dbias[offset] = sum of dS over its pairs.
 //
-// No two workgroups add to one value: a workgroup of the key kernel owns 128 keys and walks the
-// queries, one of the query kernel owns 128 queries and walks the keys. That is seven products
+// No two workgroups add to one value: a workgroup of the key kernel owns its keys and walks the
+// queries, one of the query kernel owns its queries and walks the keys. That is seven products
 // instead of the five of a single pass, for results that are the same on every run.
+//
+// dbias is a histogram: every score gradient belongs to the offset of its pair. Each workgroup of
+// the query kernel keeps a table of all offsets in LDS and adds to it with integer atomics, whose
+// sum does not depend on their order: score gradients are multiplied by a power of two for which
+// no sum can pass the integer's range, found from the largest ones, which the key kernel, running
+// first, leaves for every image and head (SumKind).
 #include "mpm_attn.h"
 
 namespace mpm {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
-constexpr int kRowsPerBlock = 32 * kWaves;
+constexpr int kDeltaThreads = 256;
+constexpr int kMaxRows = 256;  // query rows of a workgroup at most
 
-template <class S>
+// How the query kernel sums dbias.
+enum SumKind : int {
+    kSumNone = 0,
+    // 32-bit fixed point (bfloat16, no offset held to the span). Where an image's keys have
+    // distinct positions, a query meets an offset once, so a sum is at most 256 max|dS|; otherwise at
+    // most 256 max|dP - D|, as probabilities add to one. The largest term is 2^21 to 2^22 units.
+    kSum32 = 1,
+    // 64-bit fixed point, the largest |dP - D| 2^45 to 2^46 units: float32, or offsets held to the
+    // span (whose sums of many terms would leave 32 bits too few), where the table fits.
+    kSum64 = 2,
+    // Float32, one half of a wave after the other, so that the order of the additions is fixed.
+    kSumTurns = 3
+};
+
+template <class S, int DH>
 constexpr int tile_rows()
 {
-    return S::kBytes == 2 ? 64 : 32;
+    return S::kBytes == 2 && DH == 64 ? 64 : 32;
+}
+// Buffers of row tiles in LDS: two, or one where two would not leave room for the tables.
+template <class S, int DH>
+constexpr int buffers()
+{
+    return S::kBytes == 4 && DH == 128 ? 1 : 2;
+}
+template <class S, int DH>
+constexpr int tile_bytes()
+{
+    return 2 * tile_rows<S, DH>() * Tile<S, DH>::kRowBytes;
 }
 
-// D[row][head] = dO . o: eight lanes a (row, head), 16-byte loads.
+// What the kernels leave for each other: D of every query and head, the largest |dS| and |dP - D| of
+// every image and head (as bits), and whether an image's keys repeat a position.
+struct Scratch {
+    float* delta;
+    uint32_t* largest;  // [B][H][2]
+    int32_t* repeats;   // [B]
+    float* parts;       // [pair][block][W * W]
+};
+
+// D[row][head] = dO . o: eight lanes a (row, head), 16-byte loads. Also clears the words that the
+// key kernel collects in.
 template <class S>
-__global__ __launch_bounds__(kThreads) void delta_kernel(AttentionCall a, HeadRows dout, HeadRows out,
-                                                         float* __restrict__ delta)
+__global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, HeadRows dout, HeadRows out, Scratch w)
 {
     constexpr int kLanes = 8;
     const int b = blockIdx.y;
+    if (blockIdx.x == 0) {
+        for (int i = threadIdx.x; i < 2 * a.H; i += kDeltaThreads) w.largest[2L * b * a.H + i] = 0;
+        if (threadIdx.x == 0) w.repeats[b] = 0;
+    }
     const Rows rq = image_rows(a.q_off, b, a.Nq);
-    const long item = ((long)blockIdx.x * kThreads + threadIdx.x) / kLanes;
+    const long item = ((long)blockIdx.x * kDeltaThreads + threadIdx.x) / kLanes;
     const int j = threadIdx.x % kLanes;
     if (item >= (long)rq.count * a.H) return;
     const long row = rq.first + item / a.H;
@@ -38,84 +81,83 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(AttentionCall a, HeadRo
     const uint8_t* y = out.p + (row * out.row + (long)hd * out.head) * S::kBytes;
     float sum = 0.0f;
     for (int c = j; c * (16 / S::kBytes) < a.dh; c += kLanes) {
-        const u32x4 u = load16(x + c * 16), w = load16(y + c * 16);
+        const u32x4 u = load16(x + c * 16), v = load16(y + c * 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (S::kBytes == 2) sum += bf16_lo(u[e]) * bf16_lo(w[e]) + bf16_hi(u[e]) * bf16_hi(w[e]);
-            else sum += __uint_as_float(u[e]) * __uint_as_float(w[e]);
+            if (S::kBytes == 2) sum += bf16_lo(u[e]) * bf16_lo(v[e]) + bf16_hi(u[e]) * bf16_hi(v[e]);
+            else sum += __uint_as_float(u[e]) * __uint_as_float(v[e]);
         }
     }
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (j == 0) delta[row * a.H + hd] = sum;
+    if (j == 0) w.delta[row * a.H + hd] = sum;
 }
 
-// What is taken from a query's scores before the exponential: the maximum and the log of the sum, or
-// their sum where it is small enough to hold both (its rounding, below 2^-18, is the error of the
-// exponent). A mask value such as -1e9 on every key makes the maximum too large for that: then
-// the two go one after the other, as in the forward pass. No key: +inf, so that P = 0.
+// What is taken from a query's scores before the exponential: the maximum and the log of the sum
+// (`apart`), or their sum where it is small enough to hold both (its rounding, below 2^-18, is the
+// error of the exponent). A mask value such as -1e9 on every key makes the maximum too large for
+// that: then the two go one after the other, as in the forward pass. In bfloat16 calls the sum is
+// not subtracted at all: the score products start from minus it over the factor of the scores.
 constexpr float kJoinMost = 64.0f;
-struct Taken {
-    float first, second;
-};
-__device__ __forceinline__ bool split_taken(float2 l) { return fabsf(l.x) > kJoinMost && l.x != -__builtin_inff(); }
-__device__ __forceinline__ Taken taken(float2 l, bool split)
+__device__ __forceinline__ bool too_large(float2 l) { return fabsf(l.x) > kJoinMost && l.x > -__builtin_inff(); }
+
+template <class S>
+__device__ __forceinline__ bool can_start(float c)
 {
-    if (l.x == -__builtin_inff()) return Taken{__builtin_inff(), 0.0f};
-    return split ? Taken{l.x, l.y} : Taken{l.x + l.y, 0.0f};
+    return S::kBytes == 2 && c > 1e-3f && c < 1e3f;
 }
 
-// Copies KT rows of two operands into their LDS tiles, zero rows past the end or where dropped.
-template <class S, int DH, int ROWS>
-__device__ __forceinline__ void stage(uint8_t* ta, uint8_t* tb, const HeadRows& x, const HeadRows& y, long first,
-                                      int r0, int count, int head_x, int head_y, int dh, const float* drop, int t)
+// Two numbers for a query with statistics l: (where the score products start, 0), or, apart, what is
+// subtracted first and second. No key: probabilities of zero. lg: a power of two they are raised by.
+__device__ __forceinline__ float2 taken(float2 l, bool apart, float c, float lg)
 {
-    typedef Tile<S, DH> T;
-    for (int e = t; e < ROWS * T::kChunks; e += kThreads) {
-        const int r = e / T::kChunks, ch = e % T::kChunks;
-        bool in = r0 + r < count;
-        if (drop && in) in = drop[first + r0 + r] > -__builtin_inff();
-        const long row = first + (in ? r0 + r : 0);
-        store16(ta + T::at(r, ch), load_chunk<S>(x.p + (row * x.row + (long)head_x * x.head) * S::kBytes, ch, dh, in));
-        store16(tb + T::at(r, ch), load_chunk<S>(y.p + (row * y.row + (long)head_y * y.head) * S::kBytes, ch, dh, in));
-    }
+    const bool none = l.x == -__builtin_inff();
+    if (apart) return none ? make_float2(__builtin_inff(), 0.0f) : make_float2(l.x, l.y - lg);
+    return make_float2(none ? -__builtin_inff() : (lg - l.x - l.y) / c, 0.0f);
 }
 
-// dK and dV of 128 keys of one key head: all queries of all heads that share it.
-template <class S, int DH, int BIAS>
-__global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q, HeadRows k,
-                                                                HeadRows v, const float2* __restrict__ lse,
-                                                                const float* __restrict__ delta, HeadRows dk,
-                                                                HeadRows dv, int blocks)
+// dK and dV of WAVES x 32 keys of one key head: all queries of all heads that share it.
+template <class S, int DH, int BIAS, bool KB, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
+                                                                      HeadRows k, HeadRows v,
+                                                                      const float2* __restrict__ lse, Scratch w,
+                                                                      HeadRows dk, HeadRows dv, int blocks)
 {
-    typedef Tile<S, DH> T;
+    constexpr int THREADS = WAVES * kWave, QT = tile_rows<S, DH>(), BUFS = buffers<S, DH>();
+    typedef PairStage<S, DH, QT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
-    constexpr int QT = tile_rows<S>();
-    constexpr int kTileBytes = QT * T::kRowBytes;
+    constexpr int kBuffer = tile_bytes<S, DH>() + QT * 16 + 16;
     extern __shared__ __align__(16) uint8_t lds[];
-    uint8_t* qt = lds;
-    uint8_t* ot = lds + kTileBytes;
-    int* codes = reinterpret_cast<int*>(lds + 2 * kTileBytes);
-    float* lses = reinterpret_cast<float*>(codes + QT);
-    float* lows = lses + QT;
-    float* deltas = lows + QT;
-    int* apart = reinterpret_cast<int*>(deltas + QT);  // whether a query of the tile has its terms taken apart
-    float* table = reinterpret_cast<float*>(apart + 4);
+    float* table = reinterpret_cast<float*>(lds + BUFS * kBuffer);
     const int table_at = lds_address(table);
 
-    const int pair = blockIdx.x / blocks, blk = blockIdx.x % blocks;
+    int blk, pair;
+    if (!block_item(blocks, (long)a.B * a.Hk, &blk, &pair)) return;
     const int b = pair / a.Hk, hk = pair - b * a.Hk, group = a.H / a.Hk;
     const Rows rq = image_rows(a.q_off, b, a.Nq), rk = image_rows(a.k_off, b, a.Nk);
-    if (blk * kRowsPerBlock >= rk.count) return;
+    const int k0 = blk * 32 * WAVES;
+    if (k0 >= rk.count) return;
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, h = lane >> 5;
-    const int ki = blk * kRowsPerBlock + wave * 32 + l32;
+    const int ki = k0 + wave * 32 + l32;
     const bool exists = ki < rk.count;
+    const bool works = k0 + wave * 32 < rk.count;  // a wave past the image's end only brings tiles
     const int W = 2 * a.span + 1;
     const float c = a.scale * kLog2e;
-    float kb = exists ? 0.0f : -__builtin_inff();
-    if (exists && a.k_bias) kb = to_log2(a.k_bias[rk.first + ki]);
-    const bool live = kb > -__builtin_inff();
-    const int kcode = bias_code<BIAS>(exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0, a.grid_h, a.grid_w, W);
+    const bool start = can_start<S>(c);
+    float kb = 0.0f;
+    if (KB) kb = exists ? to_log2(a.k_bias[rk.first + ki]) : -__builtin_inff();
+    const bool live = exists && kb > -__builtin_inff();
+    int kcode = 0;
+    if (BIAS != kBiasNone) {
+        const int cells = a.grid_h * a.grid_w;
+        const int p = exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0;
+        kcode = bias_code<BIAS>(p, a.grid_h, a.grid_w, W);
+        if (hk == 0 && h == 0 && ki + 1 < rk.count) {
+            const int next = a.k_pos ? a.k_pos[rk.first + ki + 1] : ki + 1;
+            if (min(max(p, 0), cells - 1) >= min(max(next, 0), cells - 1))
+                __hip_atomic_fetch_or(w.repeats + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
 
     Frag kf[DH / 16], vf[DH / 16];
     const long krow = rk.first + (exists ? ki : 0);
@@ -128,36 +170,66 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
 #pragma unroll
         for (int r = 0; r < 16; ++r) gk[d][r] = gv[d][r] = 0.0f;
 
+    Staged stage;
+    int pos = 0;
+    float2 stat;
+    float del = 0.0f;
     for (int hd = hk * group; hd < (hk + 1) * group; ++hd) {
-        if (BIAS != kBiasNone) {
-            __syncthreads();
-            const float* src = a.bias + (long)hd * W * W;
-            for (int e = t; e < W * W; e += kThreads) table[e] = to_log2(src[e]);
-        }
-        for (int q0 = 0; q0 < rq.count; q0 += QT) {
-            __syncthreads();
+        auto load = [&](int q0) {
+            stage.template load<false>(q, dout, a.dh, rq.count, nullptr, q0, t);
             if (t < QT) {
                 const int qi = q0 + t;
                 const bool in = qi < rq.count;
-                if (BIAS != kBiasNone)
-                    codes[t] = query_code<BIAS>(in ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0, a.grid_h, a.grid_w,
-                                                a.span, W, table_at);
-                const float2 l = in ? lse[(rq.first + qi) * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
-                const bool split = __any(split_taken(l));
-                const Taken tk = taken(l, split);
-                lses[t] = tk.first;
-                lows[t] = tk.second;
-                if (t == 0) *apart = split;
-                deltas[t] = in ? delta[(rq.first + qi) * a.H + hd] : 0.0f;
+                if (BIAS != kBiasNone) pos = in ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0;
+                stat = in ? lse[(rq.first + qi) * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
+                del = in ? w.delta[(rq.first + qi) * a.H + hd] : 0.0f;
             }
-            stage<S, DH, QT>(qt, ot, q, dout, rq.first, q0, rq.count, hd, hd, a.dh, nullptr, t);
-            __syncthreads();
-            const bool split = *apart;
-#pragma unroll
-            for (int u = 0; u < QT / 32; ++u) {
+        };
+        auto store = [&](int buf) {
+            uint8_t* at = lds + buf * kBuffer;
+            stage.store(at, t);
+            if (t < QT) {  // one wave (or half of one)
+                int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH>());
+                float* first = reinterpret_cast<float*>(codes + QT);
+                if (BIAS != kBiasNone) codes[t] = query_code<BIAS>(pos, a.grid_h, a.grid_w, a.span, W, table_at);
+                const bool apart = !start || __any(too_large(stat));
+                const float2 tk = taken(stat, apart, c, 0.0f);
+                first[t] = tk.x;
+                first[QT + t] = tk.y;
+                first[2 * QT + t] = -del;
+                if (t == 0) reinterpret_cast<int*>(first + 3 * QT)[0] = apart;
+            }
+        };
+        __syncthreads();
+        stage.init(q, dout, rq.first, hd, t);
+        load(0);
+        if (BIAS != kBiasNone) load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
+        store(0);
+        __syncthreads();
+        float most_ds = 0.0f, most_dp = 0.0f;
+        for (int q0 = 0, buf = 0; q0 < rq.count; q0 += QT, buf ^= BUFS - 1) {
+            const uint8_t* qt = lds + buf * kBuffer;
+            const uint8_t* ot = qt + Staged::kTileBytes;
+            const int* codes = reinterpret_cast<const int*>(ot + Staged::kTileBytes);
+            const float* first = reinterpret_cast<const float*>(codes + QT);
+            const bool more = q0 + QT < rq.count;
+            if (more) load(q0 + QT);
+            const bool apart = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(first + 3 * QT)[0]);
+#pragma unroll 1
+            for (int u = 0; u < (works ? QT / 32 : 0); ++u) {
                 f32x16 s, dp;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+                for (int g = 0; g < 4; ++g) {
+                    const int at = 32 * u + 8 * g + 4 * h;
+                    f32x4 x = {0, 0, 0, 0};
+                    if (!apart) x = *reinterpret_cast<const f32x4*>(first + at);
+                    const f32x4 y = *reinterpret_cast<const f32x4*>(first + 2 * QT + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[4 * g + e] = x[e];
+                        dp[4 * g + e] = y[e];
+                    }
+                }
 #pragma unroll
                 for (int st = 0; st < DH / 16; ++st) {
                     s = mma(rows_frag<S, DH>(qt, 32 * u + l32, st, h), kf[st], s);
@@ -165,24 +237,32 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
                 }
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int at = 32 * u + 8 * g + 4 * h;
                     i32x4 qc = {0, 0, 0, 0};
-                    if (BIAS != kBiasNone) qc = *reinterpret_cast<const i32x4*>(codes + at);
-                    const f32x4 ls = *reinterpret_cast<const f32x4*>(lses + at);
-                    const f32x4 lo = *reinterpret_cast<const f32x4*>(lows + at);
-                    const f32x4 de = *reinterpret_cast<const f32x4*>(deltas + at);
+                    if (BIAS != kBiasNone) qc = *reinterpret_cast<const i32x4*>(codes + 32 * u + 8 * g + 4 * h);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float x = s[4 * g + e] * c;
-                        if (BIAS != kBiasNone)
-                            x = fmaf(s[4 * g + e], c,
-                                     lds_at(bias_entry<BIAS>(qc[e], kcode, a.span, W, table_at)));
-                        x = x + kb - ls[e];
-                        if (split) x -= lo[e];
-                        const float p = live ? __builtin_amdgcn_exp2f(x) : 0.0f;
-                        s[4 * g + e] = p;
-                        dp[4 * g + e] = p * (dp[4 * g + e] - de[e]);
+                        float x = s[4 * g + e];
+                        if (BIAS != kBiasNone) x = fmaf(x, c, lds_at(bias_entry<BIAS>(qc[e], kcode, a.span, W, table_at)));
+                        else x *= c;
+                        if (KB) x += kb;
+                        s[4 * g + e] = x;
                     }
+                }
+                if (apart) {
+                    const float* from = first;
+                    asm volatile("" : "+v"(from));  // keeps this a branch
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int at = 32 * u + 8 * (r / 4) + 4 * h + r % 4;
+                        s[r] = s[r] - from[at] - from[QT + at];
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = __builtin_amdgcn_exp2f(s[r]);
+                    if (BIAS != kBiasNone) most_dp = fmaxf(most_dp, fabsf(dp[r]));
+                    dp[r] *= s[r];
+                    if (BIAS != kBiasNone) most_ds = fmaxf(most_ds, fabsf(dp[r]));
                 }
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
@@ -193,6 +273,22 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
                         gk[d] = mma(cols_frag<S, DH>(qt, 32 * u + 16 * st, 32 * d, lane), ds, gk[d]);
                     }
                 }
+            }
+            if (BUFS == 1) __syncthreads();
+            if (more) store(buf ^ (BUFS - 1));
+            __syncthreads();
+        }
+        if (BIAS != kBiasNone) {
+            if (!live) most_ds = most_dp = 0.0f;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                most_ds = fmaxf(most_ds, __shfl_xor(most_ds, o));
+                most_dp = fmaxf(most_dp, __shfl_xor(most_dp, o));
+            }
+            if (lane == 0) {
+                uint32_t* at = w.largest + 2 * ((long)b * a.H + hd);
+                __hip_atomic_fetch_max(at, __float_as_uint(most_ds), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_fetch_max(at + 1, __float_as_uint(most_dp), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
         }
     }
@@ -208,102 +304,170 @@ __global__ __launch_bounds__(kThreads) void key_gradient_kernel(AttentionCall a,
     store_rows(dv.p + (krow * dv.row + (long)hk * dv.head) * S::kBytes, gv, 1.0f, a.dh, exists, h, S{});
 }
 
-// dQ of 128 queries of one head, and their part of dbias: every dS is added into a table in LDS,
-// one wave after the other and the halves of a wave one after the other, so that the order of
-// the additions is fixed; the workgroup's table goes to its own slot of `parts`.
-template <class S, int DH, int BIAS, bool GRAD>
-__global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
-                                                                  HeadRows k, HeadRows v,
-                                                                  const float2* __restrict__ lse,
-                                                                  const float* __restrict__ delta, HeadRows dq,
-                                                                  float* __restrict__ parts, int blocks)
+// Largest power of two lg for which x 2^lg < 2^bits, within what the exponents bear.
+__device__ __forceinline__ int raise_to(float x, int bits)
 {
-    typedef Tile<S, DH> T;
+    if (!(x > 0.0f) || !(x < __builtin_inff())) return 0;
+    return min(max(bits - (__builtin_amdgcn_frexp_expf(x)), -100), 100);
+}
+
+// Bytes of the query kernel's tables.
+__host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
+{
+    if (bias == kBiasNone) return 0;
+    return (size_t)W * W * (sum == kSumNone ? 4 : sum == kSum64 ? 12 : 8);
+}
+
+// dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: kSum32 pairs of
+// (bias, sum), otherwise the biases and then the sums (kSum64: the sums first).
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
+                                                                        HeadRows k, HeadRows v,
+                                                                        const float2* __restrict__ lse, Scratch w,
+                                                                        HeadRows dq, int blocks)
+{
+    constexpr int THREADS = WAVES * kWave, KT = tile_rows<S, DH>(), BUFS = buffers<S, DH>();
+    constexpr int SIZE = SUM == kSum32 ? 8 : 4;
+    typedef PairStage<S, DH, KT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
-    constexpr int KT = tile_rows<S>();
-    constexpr int kTileBytes = KT * T::kRowBytes;
+    typedef __attribute__((address_space(3))) int32_t lds_int;
+    typedef __attribute__((address_space(3))) unsigned long long lds_long;
+    constexpr int kBuffer = tile_bytes<S, DH>() + KT * 8;
+    static_assert(32 * WAVES <= kMaxRows, "the fixed point's range");
     extern __shared__ __align__(16) uint8_t lds[];
-    uint8_t* kt = lds;
-    uint8_t* vt = lds + kTileBytes;
-    int* codes = reinterpret_cast<int*>(lds + 2 * kTileBytes);
-    float* kbs = reinterpret_cast<float*>(codes + KT);
-    float* table = kbs + KT;
+    const int W = 2 * a.span + 1, W2 = W * W;
+    uint8_t* tables = lds + BUFS * kBuffer;
+    float* table = reinterpret_cast<float*>(tables + (SUM == kSum64 ? (size_t)W2 * 8 : 0));
     const int table_at = lds_address(table);
 
-    const int pair = blockIdx.x / blocks, blk = blockIdx.x % blocks;
+    int blk, pair;
+    if (!block_item(blocks, (long)a.B * a.H, &blk, &pair)) return;
     const int b = pair / a.H, hd = pair - b * a.H, hk = hd / (a.H / a.Hk);
     const Rows rq = image_rows(a.q_off, b, a.Nq), rk = image_rows(a.k_off, b, a.Nk);
-    if (blk * kRowsPerBlock >= rq.count) return;
+    const int q0 = blk * 32 * WAVES;
+    if (q0 >= rq.count) return;
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, h = lane >> 5;
-    const int qi = blk * kRowsPerBlock + wave * 32 + l32;
+    const int qi = q0 + wave * 32 + l32;
     const bool live = qi < rq.count;
-    const int W = 2 * a.span + 1;
-    float* sums = table + W * W;
+    const bool works = q0 + wave * 32 < rq.count;  // a wave past the image's end only brings tiles
     const float c = a.scale * kLog2e;
     const long qrow = rq.first + (live ? qi : 0);
-    const float2 stat = live ? lse[qrow * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
-    const bool split = __any(split_taken(stat));
-    const Taken ls = taken(stat, split);
-    const float de = live ? delta[qrow * a.H + hd] : 0.0f;
 
+    Staged stage;
+    int pos = 0;
+    float kbias = 0.0f;
+    const float* drop = KB ? a.k_bias + rk.first : nullptr;
+    auto load = [&](int k0) {
+        stage.template load<KB>(k, v, a.dh, rk.count, drop, k0, t);
+        if (t < KT) {
+            const int kk = k0 + t;
+            const bool in = kk < rk.count;
+            if (BIAS != kBiasNone) pos = in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
+            if (KB) kbias = in ? drop[kk] : -__builtin_inff();
+        }
+    };
+    auto store = [&](int buf) {
+        uint8_t* at = lds + buf * kBuffer;
+        stage.store(at, t);
+        if (t < KT) {
+            int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH>());
+            if (BIAS != kBiasNone) codes[t] = bias_code<BIAS, SIZE>(pos, a.grid_h, a.grid_w, W);
+            if (KB) reinterpret_cast<float*>(codes + KT)[t] = to_log2(kbias);
+        }
+    };
+    stage.init(k, v, rk.first, hk, t);
+    load(0);
+
+    // The power of two that score gradients are multiplied by, by way of the probabilities.
+    int lg = 0;
+    if (SUM == kSum32 || SUM == kSum64) {
+        const uint32_t* most = w.largest + 2 * ((long)b * a.H + hd);
+        const bool once = SUM == kSum32 && w.repeats[b] == 0;
+        lg = __builtin_amdgcn_readfirstlane(raise_to(__uint_as_float(most[once ? 0 : 1]), SUM == kSum32 ? 22 : 46));
+    }
+    const float2 stat = live ? lse[qrow * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
+    const bool apart = !can_start<S>(c) || __any(too_large(stat));
+    const float2 tk = taken(stat, apart, c, (float)lg);
+    const float nd = live ? -w.delta[qrow * a.H + hd] : 0.0f;
+    f32x16 s0, dp0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        s0[r] = apart ? 0.0f : tk.x;
+        dp0[r] = nd;
+    }
     Frag qf[DH / 16], of[DH / 16];
     load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)hd * q.head) * S::kBytes, a.dh, live, h);
     load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
     int qcode = 0;
     if (BIAS != kBiasNone) {
-        qcode = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0, a.grid_h, a.grid_w, a.span, W, table_at);
-        const float* src = a.bias + (long)hd * W * W;
-        for (int e = t; e < W * W; e += kThreads) {
-            table[e] = to_log2(src[e]);
-            if (GRAD) sums[e] = 0.0f;
-        }
+        qcode = query_code<BIAS, SIZE>(live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0, a.grid_h, a.grid_w, a.span, W, table_at);
+        load_table<THREADS, SIZE / 4>(table, a.bias + (long)hd * W2, W2, t);
+        if (SUM == kSum32)
+            for (int e = t; e < W2; e += THREADS) reinterpret_cast<int32_t*>(table)[2 * e + 1] = 0;
+        if (SUM == kSum64)
+            for (int e = t; e < W2; e += THREADS) reinterpret_cast<unsigned long long*>(tables)[e] = 0;
+        if (SUM == kSumTurns)
+            for (int e = t; e < W2; e += THREADS) table[W2 + e] = 0.0f;
     }
     f32x16 gq[DH / 32];
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) gq[d][r] = 0.0f;
+    store(0);
+    __syncthreads();
 
-    for (int k0 = 0; k0 < rk.count; k0 += KT) {
-        __syncthreads();
-        if (t < KT) {
-            const int kk = k0 + t;
-            const bool in = kk < rk.count;
-            if (BIAS != kBiasNone)
-                codes[t] = bias_code<BIAS>(in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0, a.grid_h, a.grid_w, W);
-            kbs[t] = in ? (a.k_bias ? to_log2(a.k_bias[rk.first + kk]) : 0.0f) : -__builtin_inff();
-        }
-        stage<S, DH, KT>(kt, vt, k, v, rk.first, k0, rk.count, hk, hk, a.dh, a.k_bias, t);
-        __syncthreads();
-        f32x16 dsum[KT / 32];
-#pragma unroll
-        for (int u = 0; u < KT / 32; ++u) {
+    for (int k0 = 0, buf = 0; k0 < rk.count; k0 += KT, buf ^= BUFS - 1) {
+        const uint8_t* kt = lds + buf * kBuffer;
+        const uint8_t* vt = kt + Staged::kTileBytes;
+        const int* codes = reinterpret_cast<const int*>(vt + Staged::kTileBytes);
+        const float* kbs = reinterpret_cast<const float*>(codes + KT);
+        const bool more = k0 + KT < rk.count;
+        if (more) load(k0 + KT);
+#pragma unroll 1
+        for (int u = 0; u < (works || SUM == kSumTurns ? KT / 32 : 0); ++u) {
             f32x16 s, dp;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
-                s = mma(rows_frag<S, DH>(kt, 32 * u + l32, st, h), qf[st], s);
-                dp = mma(rows_frag<S, DH>(vt, 32 * u + l32, st, h), of[st], dp);
+                s = mma(rows_frag<S, DH>(kt, 32 * u + l32, st, h), qf[st], st == 0 ? s0 : s);
+                dp = mma(rows_frag<S, DH>(vt, 32 * u + l32, st, h), of[st], st == 0 ? dp0 : dp);
             }
+            int entry[16];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int at = 32 * u + 8 * g + 4 * h;
                 i32x4 kc = {0, 0, 0, 0};
+                f32x4 kb = {0, 0, 0, 0};
                 if (BIAS != kBiasNone) kc = *reinterpret_cast<const i32x4*>(codes + at);
-                const f32x4 kb = *reinterpret_cast<const f32x4*>(kbs + at);
+                if (KB) kb = *reinterpret_cast<const f32x4*>(kbs + at);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float x = s[4 * g + e] * c;
-                    if (BIAS != kBiasNone)
-                        x = fmaf(s[4 * g + e], c,
-                                 lds_at(bias_entry<BIAS>(qcode, kc[e], a.span, W, table_at)));
-                    x = x + kb[e] - ls.first;
-                    if (split) x -= ls.second;
-                    const float p = kb[e] > -__builtin_inff() ? __builtin_amdgcn_exp2f(x) : 0.0f;
-                    dp[4 * g + e] = p * (dp[4 * g + e] - de);
+                    float x = s[4 * g + e];
+                    if (BIAS != kBiasNone) {
+                        entry[4 * g + e] = bias_entry<BIAS, SIZE>(qcode, kc[e], a.span, W, table_at);
+                        x = fmaf(x, c, lds_at(entry[4 * g + e]));
+                    } else {
+                        x *= c;
+                    }
+                    if (KB) x += kb[e];
+                    s[4 * g + e] = x;
                 }
             }
+            if (!KB && k0 + 32 * u + 32 > rk.count) {
+                int left = rk.count - k0 - 32 * u - 4 * h;
+                asm volatile("" : "+v"(left));  // keeps this a branch: no selects in whole tiles
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (8 * (r / 4) + r % 4 >= left) s[r] = -__builtin_inff();
+            }
+            if (apart) {
+                float one = tk.x;
+                asm volatile("" : "+v"(one));
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = s[r] - one - tk.y;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] *= __builtin_amdgcn_exp2f(s[r]);
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
                 const Frag ds = tile_frag(dp, st, S{});
@@ -311,139 +475,224 @@ __global__ __launch_bounds__(kThreads) void query_gradient_kernel(AttentionCall 
                 for (int d = 0; d < DH / 32; ++d)
                     gq[d] = mma(cols_frag<S, DH>(kt, 32 * u + 16 * st, 32 * d, lane), ds, gq[d]);
             }
-            dsum[u] = dp;
-        }
-        if (GRAD) {
-            for (int w = 0; w < 2 * kWaves; ++w) {
-                if (wave == w / 2 && h == w % 2 && live) {
+            if (SUM == kSum32) {
 #pragma unroll
-                    for (int u = 0; u < KT / 32; ++u)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const int at = 32 * u + 8 * (r / 4) + 4 * h + r % 4;
-                            if (k0 + at < rk.count)
-                                __hip_atomic_fetch_add(
-                                    reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(sums) +
-                                                             bias_entry<BIAS>(qcode, codes[at], a.span, W, table_at) - table_at),
-                                    dsum[u][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                        }
+                for (int r = 0; r < 16; ++r) {
+                    int n;  // to the nearest
+                    asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(n) : "v"(dp[r]));
+                    __hip_atomic_fetch_add((lds_int*)(uintptr_t)(uint32_t)(entry[r] + 4), n, __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
-                __syncthreads();
+            }
+            if (SUM == kSum64) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    __hip_atomic_fetch_add(
+                        (lds_long*)(uintptr_t)(uint32_t)((entry[r] - table_at) * 2 + lds_address(tables)),
+                        (unsigned long long)(long long)dp[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+            if (SUM == kSumTurns) {
+                for (int turn = 0; turn < 2 * WAVES; ++turn) {
+                    if (wave == turn / 2 && h == turn % 2 && live) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            __hip_atomic_fetch_add((__attribute__((address_space(3))) float*)(uintptr_t)(uint32_t)(
+                                                       entry[r] + W2 * 4),
+                                                   dp[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
+                    __syncthreads();
+                }
             }
         }
+        if (BUFS == 1) __syncthreads();
+        if (more) store(buf ^ (BUFS - 1));
+        __syncthreads();
     }
 
-    if (GRAD) {
-        __syncthreads();
-        float* part = parts + (long)blockIdx.x * W * W;
-        for (int e = t; e < W * W; e += kThreads) part[e] = sums[e];
+    const float back = __builtin_ldexpf(1.0f, -lg);
+    if (SUM != kSumNone) {
+        // A gradient that is not a number is not one in the sums either: it has reached dq.
+        bool bad = false;
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) bad |= !(fabsf(gq[d][r]) < __builtin_inff());
+        const bool any_bad = __syncthreads_or(bad && live);
+        float* part = w.parts + ((long)pair * blocks + blk) * W2;
+        for (int e = t; e < W2; e += THREADS) {
+            float x;
+            if (SUM == kSum32) x = (float)reinterpret_cast<const int32_t*>(table)[2 * e + 1] * back;
+            else if (SUM == kSum64) x = (float)reinterpret_cast<const long long*>(tables)[e] * back;
+            else x = table[W2 + e];
+            part[e] = any_bad ? __builtin_nanf("") : x;
+        }
     }
-    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale, a.dh, live, h, S{});
+    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale * back, a.dh, live, h, S{});
 }
 
-// dbias[head][e] = the workgroups' parts, images and query blocks in order.
-__global__ __launch_bounds__(kThreads) void bias_parts_kernel(AttentionCall a, const float* __restrict__ parts,
-                                                              int blocks, float* __restrict__ dbias)
+// dbias[head][e] = the workgroups' parts, in the order of images and query blocks: four threads an
+// entry take every fourth image, joined in order.
+constexpr int kJoinEntries = 64, kJoinWays = 4;
+__global__ __launch_bounds__(kJoinEntries* kJoinWays) void bias_parts_kernel(AttentionCall a,
+                                                                           const float* __restrict__ parts, int blocks,
+                                                                           int rows, float* __restrict__ dbias)
 {
+    __shared__ float joined[kJoinWays][kJoinEntries];
     const int W2 = (2 * a.span + 1) * (2 * a.span + 1);
-    const int e = blockIdx.x * kThreads + threadIdx.x, hd = blockIdx.y;
-    if (e >= W2) return;
+    const int col = threadIdx.x % kJoinEntries, way = threadIdx.x / kJoinEntries, hd = blockIdx.y;
+    const int e = min((int)blockIdx.x * kJoinEntries + col, W2 - 1);
     float sum = 0.0f;
-    for (int b = 0; b < a.B; ++b) {
-        const int n = image_rows(a.q_off, b, a.Nq).count;
-        for (int i = 0; i * kRowsPerBlock < n; ++i) sum += parts[(((long)b * a.H + hd) * blocks + i) * W2 + e];
+    for (int b = way; b < a.B; b += kJoinWays) {
+        const int n = (image_rows(a.q_off, b, a.Nq).count + rows - 1) / rows;
+        const float* part = parts + ((long)b * a.H + hd) * blocks * W2 + e;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) sum += part[(long)i * W2];
     }
+    joined[way][col] = sum;
+    __syncthreads();
+    if (way != 0 || (int)blockIdx.x * kJoinEntries + col >= W2) return;
+#pragma unroll
+    for (int x = 1; x < kJoinWays; ++x) sum += joined[x][col];
     dbias[(long)hd * W2 + e] = sum;
 }
 
 struct Grads {
     HeadRows dq, dk, dv;
-    float* delta;
-    float* parts;
     float* dbias;
+    Scratch w;
 };
 
-int query_blocks(const AttentionCall& a) { return (a.Nq + kRowsPerBlock - 1) / kRowsPerBlock; }
+struct Inputs {
+    HeadRows dout, q, k, v, out;
+    const float2* lse;
+};
 
-template <class S, int DH, int BIAS>
-hipError_t launch_all(const AttentionCall& a, const HeadRows& dout, const HeadRows& q, const HeadRows& k,
-                      const HeadRows& v, const HeadRows& out, const float2* lse, const Grads& g, hipStream_t st)
+// Query rows of a workgroup: eight waves where the tables leave LDS for one workgroup only.
+constexpr long kLargeTable = 24 << 10;
+bool large(const AttentionCall& a)
 {
-    constexpr int R = tile_rows<S>();
-    const size_t W2 = (size_t)(2 * a.span + 1) * (2 * a.span + 1);
-    const size_t tiles = 2 * R * Tile<S, DH>::kRowBytes, table = BIAS != kBiasNone ? W2 * 4 : 0;
-    const long per_image = (long)a.Nq * a.H * 8;
-    hipLaunchKernelGGL(delta_kernel<S>, dim3((unsigned)((per_image + kThreads - 1) / kThreads), (unsigned)a.B),
-                       dim3(kThreads), 0, st, a, dout, out, g.delta);
-    hipError_t e = hipGetLastError();
+    const long W = 2 * a.span + 1;
+    return a.dt == kBf16 && a.dh <= 64 && a.bias && W * W * 4 > kLargeTable;
+}
+int block_rows(const AttentionCall& a) { return large(a) ? 256 : 128; }
+int query_blocks(const AttentionCall& a) { return (a.Nq + block_rows(a) - 1) / block_rows(a); }
+
+template <class S, int DH, int BIAS, bool KB, int WAVES>
+hipError_t launch_keys(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
+{
+    const size_t W = 2 * a.span + 1;
+    const int blocks = (a.Nk + 32 * WAVES - 1) / (32 * WAVES);
+    const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH>() + tile_rows<S, DH>() * 16 + 16) +
+                         (BIAS != kBiasNone ? W * W * 4 : 0);
+    const long grid = block_grid((long)a.B * a.Hk, blocks);
+    if (grid * WAVES * kWave > UINT32_MAX) return hipErrorInvalidConfiguration;
+    auto kernel = key_gradient_kernel<S, DH, BIAS, KB, WAVES>;
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
-    {
-        const int blocks = (a.Nk + kRowsPerBlock - 1) / kRowsPerBlock;
-        const size_t bytes = tiles + R * 16 + 16 + table;
-        const long grid = (long)a.B * a.Hk * blocks;
-        if (grid * kThreads > UINT32_MAX) return hipErrorInvalidConfiguration;
-        auto kernel = key_gradient_kernel<S, DH, BIAS>;
-        if ((e = allow_lds(reinterpret_cast<const void*>(kernel), bytes)) != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), bytes, st, a, dout, q,
-                           k, v, lse, g.delta, g.dk, g.dv, blocks);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), bytes, st, a, in.dout, in.q, in.k, in.v,
+                       in.lse, g.w, g.dk, g.dv, blocks);
+    return hipGetLastError();
+}
+
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES>
+hipError_t launch_queries(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
+{
     const int blocks = query_blocks(a);
-    const long grid = (long)a.B * a.H * blocks;
-    if (grid * kThreads > UINT32_MAX) return hipErrorInvalidConfiguration;
-    const bool grad = BIAS != kBiasNone && g.dbias;
-    const size_t bytes = tiles + R * 8 + (grad ? 2 : 1) * table;
-    auto kernel = grad ? query_gradient_kernel<S, DH, BIAS, BIAS != kBiasNone>
-                       : query_gradient_kernel<S, DH, BIAS, false>;
-    if ((e = allow_lds(reinterpret_cast<const void*>(kernel), bytes)) != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kThreads), bytes, st, a, dout, q, k, v,
-                       lse, g.delta, g.dq, g.parts, blocks);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (grad) {
-        hipLaunchKernelGGL(bias_parts_kernel, dim3((unsigned)((W2 + kThreads - 1) / kThreads), (unsigned)a.H),
-                           dim3(kThreads), 0, st, a, g.parts, blocks, g.dbias);
-        e = hipGetLastError();
+    const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH>() + tile_rows<S, DH>() * 8) +
+                         table_bytes(BIAS, SUM, 2 * a.span + 1);
+    const long grid = block_grid((long)a.B * a.H, blocks);
+    if (grid * WAVES * kWave > UINT32_MAX) return hipErrorInvalidConfiguration;
+    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES>;
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), bytes, st, a, in.dout, in.q, in.k, in.v,
+                       in.lse, g.w, g.dq, blocks);
+    return hipGetLastError();
+}
+
+constexpr size_t kLdsBytes = 160 << 10;
+
+template <class S, int DH, int BIAS, bool KB, int WAVES>
+hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
+{
+    const int W = 2 * a.span + 1;
+    const long per_image = (long)a.Nq * a.H * 8;
+    hipLaunchKernelGGL(delta_kernel<S>, dim3((unsigned)((per_image + kDeltaThreads - 1) / kDeltaThreads), (unsigned)a.B),
+                       dim3(kDeltaThreads), 0, st, a, in.dout, in.out, g.w);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) e = launch_keys<S, DH, BIAS, KB, WAVES>(a, in, g, st);
+    if (e != hipSuccess) return e;
+    if constexpr (BIAS == kBiasNone) {
+        return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES>(a, in, g, st);
+    } else {
+        constexpr size_t tiles = buffers<S, DH>() * (tile_bytes<S, DH>() + tile_rows<S, DH>() * 8);
+        if (!g.dbias) return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES>(a, in, g, st);
+        if constexpr (S::kBytes == 2 && BIAS == kBiasGrid) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES>(a, in, g, st);
+        else if (tiles + table_bytes(BIAS, kSum64, W) <= kLdsBytes)
+            e = launch_queries<S, DH, BIAS, KB, kSum64, WAVES>(a, in, g, st);
+        else e = launch_queries<S, DH, BIAS, KB, kSumTurns, WAVES>(a, in, g, st);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(bias_parts_kernel, dim3((unsigned)((W * W + kJoinEntries - 1) / kJoinEntries), (unsigned)a.H),
+                           dim3(kJoinEntries * kJoinWays), 0, st, a, g.w.parts, query_blocks(a), 32 * WAVES, g.dbias);
+        return hipGetLastError();
     }
-    return e;
+}
+
+template <class S, int DH, int BIAS, int WAVES>
+hipError_t pick_drop(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
+{
+    return a.k_bias ? launch_all<S, DH, BIAS, true, WAVES>(a, in, g, st)
+                    : launch_all<S, DH, BIAS, false, WAVES>(a, in, g, st);
 }
 
 template <class S, int DH>
-hipError_t pick(const AttentionCall& a, const HeadRows& dout, const HeadRows& q, const HeadRows& k, const HeadRows& v,
-                const HeadRows& out, const float2* lse, const Grads& g, hipStream_t st)
+hipError_t pick(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
-    switch (bias_kind(a)) {
-    case kBiasNone: return launch_all<S, DH, kBiasNone>(a, dout, q, k, v, out, lse, g, st);
-    case kBiasGrid: return launch_all<S, DH, kBiasGrid>(a, dout, q, k, v, out, lse, g, st);
-    default: return launch_all<S, DH, kBiasFar>(a, dout, q, k, v, out, lse, g, st);
+    const int kind = bias_kind(a);
+    if (kind == kBiasNone) return pick_drop<S, DH, kBiasNone, 4>(a, in, g, st);
+    if constexpr (S::kBytes == 2 && DH == 64) {
+        if (large(a))
+            return kind == kBiasGrid ? pick_drop<S, DH, kBiasGrid, 8>(a, in, g, st)
+                                     : pick_drop<S, DH, kBiasFar, 8>(a, in, g, st);
     }
+    return kind == kBiasGrid ? pick_drop<S, DH, kBiasGrid, 4>(a, in, g, st) : pick_drop<S, DH, kBiasFar, 4>(a, in, g, st);
 }
 
 size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
+
+// The scratch regions' sizes, in order.
+struct Sizes {
+    size_t delta, largest, repeats, parts;
+};
+Sizes sizes(const AttentionCall& a)
+{
+    const size_t W = 2 * a.span + 1;
+    return Sizes{aligned256((size_t)a.B * a.Nq * a.H * 4), aligned256((size_t)a.B * a.H * 8), aligned256((size_t)a.B * 4),
+                 a.bias ? aligned256((size_t)a.B * a.H * query_blocks(a) * W * W * 4) : 0};
+}
 
 }  // namespace
 
 size_t attention_backward_bytes(const AttentionCall& a)
 {
-    const size_t W2 = (size_t)(2 * a.span + 1) * (2 * a.span + 1);
-    size_t n = aligned256((size_t)a.B * a.Nq * a.H * 4);
-    if (a.bias) n += aligned256((size_t)a.B * a.H * query_blocks(a) * W2 * 4);
-    return n;
+    const Sizes n = sizes(a);
+    return n.delta + n.largest + n.repeats + n.parts;
 }
 
 hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dout, const HeadRows& q,
-                                     const HeadRows& k, const HeadRows& v, const HeadRows& out, const float* lse_pairs,
+                                     const HeadRows& k, const HeadRows& v, const HeadRows& out, const float* lse,
                                      const HeadRows& dq, const HeadRows& dk, const HeadRows& dv, float* dbias, void* ws,
                                      hipStream_t st)
 {
-    const float2* lse = reinterpret_cast<const float2*>(lse_pairs);
-    float* delta = static_cast<float*>(ws);
-    float* parts = reinterpret_cast<float*>(static_cast<char*>(ws) + aligned256((size_t)a.B * a.Nq * a.H * 4));
-    const Grads g{dq, dk, dv, delta, parts, dbias};
-    if (a.dt == kBf16)
-        return a.dh <= 64 ? pick<Bf16, 64>(a, dout, q, k, v, out, lse, g, st)
-                          : pick<Bf16, 128>(a, dout, q, k, v, out, lse, g, st);
-    return a.dh <= 64 ? pick<F32, 64>(a, dout, q, k, v, out, lse, g, st)
-                      : pick<F32, 128>(a, dout, q, k, v, out, lse, g, st);
+    const Sizes n = sizes(a);
+    char* p = static_cast<char*>(ws);
+    const Scratch w{reinterpret_cast<float*>(p), reinterpret_cast<uint32_t*>(p + n.delta),
+                    reinterpret_cast<int32_t*>(p + n.delta + n.largest),
+                    reinterpret_cast<float*>(p + n.delta + n.largest + n.repeats)};
+    const Inputs in{dout, q, k, v, out, reinterpret_cast<const float2*>(lse)};
+    const Grads g{dq, dk, dv, dbias, w};
+    if (a.dt == kBf16) return a.dh <= 64 ? pick<Bf16, 64>(a, in, g, st) : pick<Bf16, 128>(a, in, g, st);
+    return a.dh <= 64 ? pick<F32, 64>(a, in, g, st) : pick<F32, 128>(a, in, g, st);
 }
 
 }  // namespace mpm

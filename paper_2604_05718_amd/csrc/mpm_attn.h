@@ -221,33 +221,34 @@ enum BiasKind : int {
     kBiasFar = 2    // offsets are held to the span, one axis at a time
 };
 
-// A grid position in the form its side of the bias entry needs. kBiasGrid: the byte offset of
-// row * W + column (W = 2 span + 1), so that a pair's entry is query - key + middle. kBiasFar:
+// A grid position in the form its side of the bias entry needs (entries of `size` bytes).
+// kBiasGrid: the byte offset of row * W + column (W = 2 span + 1), so that a pair's entry is
+// query - key + middle. kBiasFar:
 // row and column as two 16-bit halves. Positions outside the grid are held to it, so that a
 // pair's entry is inside the table whatever the caller passed.
-template <int BIAS>
+template <int BIAS, int SIZE = 4>
 __device__ __forceinline__ int bias_code(int pos, int gh, int gw, int W)
 {
     if constexpr (BIAS == kBiasNone) return 0;
     const int p = min(max(pos, 0), gh * gw - 1);
     const int r = (int)((unsigned)p / (unsigned)gw), c = p - r * gw;
-    if constexpr (BIAS == kBiasGrid) return (r * W + c) * 4;
+    if constexpr (BIAS == kBiasGrid) return (r * W + c) * SIZE;
     return (r << 16) | c;
 }
 // Where the pair's entry is: qcode's side holds the table's address (kBiasFar: base does).
-template <int BIAS>
+template <int BIAS, int SIZE = 4>
 __device__ __forceinline__ int bias_entry(int qcode, int kcode, int span, int W, int base)
 {
     if constexpr (BIAS == kBiasGrid) return qcode - kcode;
     const int dr = (qcode >> 16) - (kcode >> 16), dc = (qcode & 0xffff) - (kcode & 0xffff);
-    return base + ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * 4;
+    return base + ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * SIZE;
 }
 // A query's side: with the middle of the table at LDS address `base` added (kBiasGrid).
-template <int BIAS>
+template <int BIAS, int SIZE = 4>
 __device__ __forceinline__ int query_code(int pos, int gh, int gw, int span, int W, int base)
 {
-    const int c = bias_code<BIAS>(pos, gh, gw, W);
-    return BIAS == kBiasGrid ? c + (span * W + span) * 4 + base : c;
+    const int c = bias_code<BIAS, SIZE>(pos, gh, gw, W);
+    return BIAS == kBiasGrid ? c + (span * W + span) * SIZE + base : c;
 }
 
 // An LDS address as the 32-bit number the hardware takes, and a float at one: a pair's bias is read at
@@ -267,8 +268,84 @@ __device__ __forceinline__ float to_log2(float x)
     return x >= kLowest ? fmaxf(y, kLowest) : y;
 }
 
-// A head's bias table to LDS, in base 2: eight loads a thread in flight.
-template <int THREADS>
+constexpr int kXcds = 8;
+// The workgroup's row block and (image, head) pair. Blocks are dealt round-robin to the 8 XCDs,
+// each with its own L2: pairs are dealt to XCDs whole, so that the blocks that read one pair's
+// rows share an L2 (few pairs: in order, since whole pairs would leave XCDs idle).
+__device__ __forceinline__ bool block_item(int blocks, long pairs, int* blk, int* pair)
+{
+    const int i = blockIdx.x;
+    if (pairs >= 4 * kXcds) {
+        const int slot = i / kXcds;
+        *pair = slot / blocks * kXcds + i % kXcds;
+        *blk = slot % blocks;
+    } else {
+        *pair = i / blocks;
+        *blk = i % blocks;
+    }
+    return *pair < pairs;
+}
+// Workgroups of such a launch.
+inline long block_grid(long pairs, int blocks)
+{
+    return (pairs >= 4 * kXcds ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * blocks;
+}
+
+// Tiles of ROWS rows of two operands on their way to LDS: loaded to registers a tile ahead.
+template <class S, int DH, int ROWS, int THREADS>
+struct PairStage {
+    typedef Tile<S, DH> T;
+    static constexpr int kTileBytes = ROWS * T::kRowBytes;
+    static constexpr int kPer = ROWS * T::kChunks / THREADS;
+    static_assert(ROWS * T::kChunks % THREADS == 0 && THREADS >= ROWS, "whole chunks a thread");
+    u32x4 x[kPer], y[kPer];
+    const uint8_t *xp[kPer], *yp[kPer];  // this thread's chunks of the next tile
+
+    __device__ __forceinline__ void init(const HeadRows& xr, const HeadRows& yr, long first, int head, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = t + i * THREADS, ch = e % T::kChunks;
+            const long row = first + e / T::kChunks;
+            xp[i] = xr.p + (row * xr.row + (long)head * xr.head) * S::kBytes + ch * 16;
+            yp[i] = yr.p + (row * yr.row + (long)head * yr.head) * S::kBytes + ch * 16;
+        }
+    }
+    // Loads rows r0 ... of `count` and moves on; zeros past the last row, past a row's end, and
+    // for rows dropped by drop[row] = -inf, which are not read.
+    template <bool DROP>
+    __device__ __forceinline__ void load(const HeadRows& xr, const HeadRows& yr, int dh, int count, const float* drop,
+                                         int r0, int t)
+    {
+        const long xstep = (long)ROWS * xr.row * S::kBytes, ystep = (long)ROWS * yr.row * S::kBytes;
+        const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = t + i * THREADS, ch = e % T::kChunks, r = r0 + e / T::kChunks;
+            bool in = ch * (16 / S::kBytes) < dh && r < count;
+            if (DROP && in) in = drop[r] > -__builtin_inff();
+            x[i] = y[i] = zero;
+            if (in) {
+                x[i] = load16(xp[i]);
+                y[i] = load16(yp[i]);
+            }
+            xp[i] += xstep;
+            yp[i] += ystep;
+        }
+    }
+    __device__ __forceinline__ void store(uint8_t* lds, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = t + i * THREADS, at = T::at(e / T::kChunks, e % T::kChunks);
+            store16(lds + at, x[i]);
+            store16(lds + kTileBytes + at, y[i]);
+        }
+    }
+};
+
+// A head's bias table to LDS, in base 2, every STRIDE words: eight loads a thread in flight.
+template <int THREADS, int STRIDE = 1>
 __device__ __forceinline__ void load_table(float* table, const float* src, int n, int t)
 {
     constexpr int kFlight = 8;
@@ -278,7 +355,7 @@ __device__ __forceinline__ void load_table(float* table, const float* src, int n
         for (int i = 0; i < kFlight; ++i) v[i] = src[min(e0 + i * THREADS, n - 1)];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i)
-            if (e0 + i * THREADS < n) table[e0 + i * THREADS] = to_log2(v[i]);
+            if (e0 + i * THREADS < n) table[(e0 + i * THREADS) * STRIDE] = to_log2(v[i]);
     }
 }
 
