@@ -816,7 +816,9 @@ int mpm_unmerge(const void* z, const int32_t* z_off, const int32_t* map, const v
 
 size_t mpm_attention_workspace_bytes(const mpm_attention_call* call)
 {
-    return 0;
+    if (check_attention(call) != MPM_OK) return 0;
+    const mpm::AttentionCall a = attention_call(call);
+    return mpm::attention_is_few(a) ? mpm::attention_few_bytes(a) : 0;
 }
 
 int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_heads* k, const mpm_heads* v,
@@ -830,8 +832,11 @@ int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_
     if ((s = check_workspace(ws, ws_bytes, mpm_attention_workspace_bytes(call))) != MPM_OK) return s;
     MPM_LAUNCH_GATE();
     MPM_DATA_CHECK(checked_attention(call, as_stream(stream)));
-    return hip_status(mpm::launch_attention(attention_call(call), heads(q), heads(k), heads(v), heads(out), lse,
-                                            as_stream(stream)));
+    const mpm::AttentionCall a = attention_call(call);
+    if (mpm::attention_is_few(a))
+        return hip_status(mpm::launch_attention_few(a, heads(q), heads(k), heads(v), heads(out), lse, ws,
+                                                    as_stream(stream)));
+    return hip_status(mpm::launch_attention(a, heads(q), heads(k), heads(v), heads(out), lse, as_stream(stream)));
 }
 
 size_t mpm_attention_backward_workspace_bytes(const mpm_attention_call* call)

@@ -159,6 +159,13 @@ hipError_t allow_lds(const void* kernel, size_t bytes);
 // Attention; lse (may be null) receives [row][head] pairs: the maximum taken and the log of the sum, base 2.
 hipError_t launch_attention(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
                             const HeadRows& out, float* lse, hipStream_t stream);
+// The same for a few queries (attention_is_few: at most 32 columns of queries a key head), keys split
+// over workgroups; ws holds attention_few_bytes(a) bytes.
+bool attention_is_few(const AttentionCall& a);
+int attention_few_splits(const AttentionCall& a);
+size_t attention_few_bytes(const AttentionCall& a);
+hipError_t launch_attention_few(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
+                                const HeadRows& out, float* lse, void* ws, hipStream_t stream);
 // Its gradients; ws holds attention_backward_bytes(a) bytes; dbias may be null.
 size_t attention_backward_bytes(const AttentionCall& a);
 hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dout, const HeadRows& q,

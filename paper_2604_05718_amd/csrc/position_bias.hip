@@ -28,32 +28,47 @@ __global__ __launch_bounds__(kThreads) void bias_expand_kernel(const void* __res
     bias[(long)h * W * W + e] = table_value(table, ((long)r * nb + c) * H + h, dt);
 }
 
-// dtable[bucket][h] = sum of dbias[h] over the bucket's offsets, in the order of the offsets: one
-// wave a bucket and head. Row offsets are scanned for the row bucket; in a row that has it,
-// lanes take columns lane, lane + 64, ... and those of the column bucket are added; a butterfly
-// joins the lanes, so the order is the same on every run.
-__global__ __launch_bounds__(kThreads) void bias_gradient_kernel(const float* __restrict__ dbias,
-                                                                 const int32_t* __restrict__ lut, int nb, int W, int H,
-                                                                 int dt, void* __restrict__ dtable)
+// dtable[bucket][h] = sum of dbias[h] over the bucket's offsets: a workgroup takes a row bucket of
+// a head. The row offsets that have it are listed; every thread adds its column offset's entries of
+// those rows, in order; then a thread a column bucket adds its columns' sums, in order.
+constexpr int kMaxWidth = 128;
+__global__ __launch_bounds__(kMaxWidth) void bias_gradient_kernel(const float* __restrict__ dbias,
+                                                                  const int32_t* __restrict__ lut, int nb, int W, int H,
+                                                                  int dt, void* __restrict__ dtable)
 {
-    __shared__ int32_t axis[256];
-    if (threadIdx.x < W) axis[threadIdx.x] = lut[threadIdx.x];
+    constexpr int kFlight = 8;
+    __shared__ int32_t axis[kMaxWidth];
+    __shared__ float sums[kMaxWidth];
+    __shared__ int32_t rows[kMaxWidth];
+    __shared__ int32_t first_wave;
+    const int t = threadIdx.x, lane = t % kWave, br = blockIdx.x, h = blockIdx.y;
+    const int32_t own = t < W ? lut[t] : -1;
+    axis[t] = own;
+    const unsigned long long has = __ballot(own == br);
+    const int before = __popcll(has & ((1ull << lane) - 1));
+    if (t == 0) first_wave = __popcll(has);
     __syncthreads();
-    const int lane = threadIdx.x % kWave;
-    const long item = (long)blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
-    if (item >= (long)nb * nb * H) return;
-    const int h = (int)(item % H), bucket = (int)(item / H), br = bucket / nb, bc = bucket % nb;
+    if (own == br) rows[before + (t >= kWave ? first_wave : 0)] = t;
+    const int count = __syncthreads_count(own == br);
     float sum = 0.0f;
-    for (int r = 0; r < W; ++r) {
-        if (axis[r] != br) continue;
-        for (int c = lane; c < W; c += kWave)
-            if (axis[c] == bc) sum += dbias[((long)h * W + r) * W + c];
-    }
+    const float* col = dbias + (long)h * W * W + min(t, W - 1);
+    for (int i = 0; i < count; i += kFlight) {
+        float v[kFlight];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (lane != 0) return;
-    if (dt == kBf16) reinterpret_cast<uint16_t*>(dtable)[item] = (uint16_t)f32_to_bf16_rne(sum);
-    else reinterpret_cast<float*>(dtable)[item] = sum;
+        for (int u = 0; u < kFlight; ++u) v[u] = col[(long)rows[min(i + u, count - 1)] * W];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u)
+            if (i + u < count) sum += v[u];
+    }
+    sums[t] = sum;
+    __syncthreads();
+    if (t >= nb) return;
+    sum = 0.0f;
+    for (int c = 0; c < W; ++c)
+        if (axis[c] == t) sum += sums[c];
+    const long at = ((long)br * nb + t) * H + h;
+    if (dt == kBf16) reinterpret_cast<uint16_t*>(dtable)[at] = (uint16_t)f32_to_bf16_rne(sum);
+    else reinterpret_cast<float*>(dtable)[at] = sum;
 }
 
 }  // namespace
@@ -70,10 +85,8 @@ hipError_t launch_bias_expand(const void* table, const int32_t* lut, int nb, int
 hipError_t launch_bias_gradient(const float* dbias, const int32_t* lut, int nb, int span, int H, int dt, void* dtable,
                                 hipStream_t stream)
 {
-    const long items = (long)nb * nb * H;
-    const int per = kThreads / kWave;
-    hipLaunchKernelGGL(bias_gradient_kernel, dim3((unsigned)((items + per - 1) / per)), dim3(kThreads), 0, stream,
-                       dbias, lut, nb, 2 * span + 1, H, dt, dtable);
+    hipLaunchKernelGGL(bias_gradient_kernel, dim3((unsigned)nb, (unsigned)H), dim3(kMaxWidth), 0, stream, dbias, lut,
+                       nb, 2 * span + 1, H, dt, dtable);
     return hipGetLastError();
 }
 

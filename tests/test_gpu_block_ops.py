@@ -145,6 +145,40 @@ def test_attention_backward(dtype, i):
         assert a is None or torch.equal(a, b)
 
 
+FEW = [
+    # nq, nk, H, Hk, dh, grid, span, k_bias: at most 32 columns of queries a key head
+    ([1, 1, 1], [5000, 31, 900], 4, 4, 64, (80, 70), 63, True),
+    ([1] * 5, [600] * 5, 3, 3, 64, (25, 25), 24, False),
+    ([2, 0, 1], [700, 33, 0], 6, 2, 40, (30, 30), 29, False),
+    ([7], [16384], 2, 2, 64, (128, 128), 63, True),
+    ([4, 3], [2000, 1999], 8, 1, 128, None, None, True),
+    ([20], [333], 1, 1, 8, (20, 20), 3, False),
+    ([16], [1], 4, 2, 64, (9, 9), 8, False),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("i", range(len(FEW)))
+def test_attention_of_few_queries(dtype, i):
+    nq, nk, H, Hk, dh, grid, span, kb = FEW[i]
+    c = Case(dtype, nq, nk, H, Hk, dh, grid, span, "sorted", kb, seed=200 + i)
+    print(f"few queries {i} {dtype}", flush=True)
+    if kb:
+        c.k_bias[-20:] = -math.inf
+    k, v = c.k.to(DEV), c.v.to(DEV)
+    if kb:
+        k[torch.isinf(c.k_bias).to(DEV)] = math.nan
+        v[torch.isinf(c.k_bias).to(DEV)] = math.nan
+    out, lse = mpm.attention(c.q.to(DEV), k, v, with_lse=True, **c.kw())
+    torch.cuda.synchronize()
+    want, wl = c.plain()
+    assert ref.rel(out, want) <= FWD[dtype]
+    empty = torch.isinf(wl)
+    lse = lse.cpu().double().sum(-1) * math.log(2.0)
+    assert torch.equal(torch.isinf(lse), empty) and torch.all(out.cpu()[empty] == 0)
+    assert ref.rel(lse[~empty], wl[~empty]) <= 144 * 2.0 ** -24
+
+
 def test_attention_gradients_against_differences():
     """Float32 gradients against central differences of the 64-bit form along random directions
     (error: the gradient's own tolerance of the directional derivative's scale, and step^2)."""
