@@ -80,7 +80,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     };
     auto store = [&](int buf) {
         uint8_t* at = lds + buf * kBuffer;
-        stage.store(at, t);
+        stage.template store<KB>(at, t);
         if (t < KT) {
             int* codes = reinterpret_cast<int*>(at + 2 * Staged::kTileBytes);
             if (BIAS != kBiasNone) codes[t] = bias_code<BIAS>(pos, a.grid_h, a.grid_w, W);

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
         };
         auto store = [&](int buf) {
             uint8_t* at = lds + buf * kBuffer;
-            stage.store(at, t);
+            stage.template store<false>(at, t);
             if (t < QT) {  // one wave (or half of one)
                 int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH>());
                 float* first = reinterpret_cast<float*>(codes + QT);
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
     };
     auto store = [&](int buf) {
         uint8_t* at = lds + buf * kBuffer;
-        stage.store(at, t);
+        stage.template store<KB>(at, t);
         if (t < KT) {
             int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH>());
             if (BIAS != kBiasNone) codes[t] = bias_code<BIAS, SIZE>(pos, a.grid_h, a.grid_w, W);

@@ -87,19 +87,15 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
     float kbias = 0.0f;
     auto load = [&](int tile) {
         const int kk = 32 * tile + l32;
-        bool in = kk < rk.count;
+        const bool in = kk < rk.count;
         if (BIAS != kBiasNone) pos = in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
-        if (KB) {
-            kbias = in ? a.k_bias[rk.first + kk] : -__builtin_inff();
-            in = kbias > -__builtin_inff();
-        }
+        if (KB) kbias = in ? a.k_bias[rk.first + kk] : -__builtin_inff();
         const long row = rk.first + (in ? kk : 0);
         load_frags<S, DH>(kn, k.p + (row * k.row + (long)hk * k.head) * S::kBytes, a.dh, in, h);
 #pragma unroll
         for (int i = 0; i < kChunksLane; ++i) {
             const int e = lane + i * kWave, ch = e % T::kChunks, kv = 32 * tile + e / T::kChunks;
-            bool have = kv < rk.count;
-            if (KB && have) have = a.k_bias[rk.first + kv] > -__builtin_inff();
+            const bool have = kv < rk.count;
             vn[i] = load_chunk<S>(v.p + ((rk.first + (have ? kv : 0)) * v.row + (long)hk * v.head) * S::kBytes, ch, a.dh,
                                   have);
         }
@@ -124,6 +120,10 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
 #pragma unroll
         for (int i = 0; i < kChunksLane; ++i) {
             const int e = lane + i * kWave;
+            if (KB && __shfl(kbias, e / T::kChunks) == -__builtin_inff()) {  // dropped: whatever it holds
+                const u32x4 zero = {0, 0, 0, 0};
+                vn[i] = zero;
+            }
             store16(vt + T::at(e / T::kChunks, e % T::kChunks), vn[i]);
         }
         if (h == 0) {
@@ -131,7 +131,10 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
             if (KB) kbs[l32] = to_log2(kbias);
         }
 #pragma unroll
-        for (int st = 0; st < DH / 16; ++st) kf[st] = kn[st];
+        for (int st = 0; st < DH / 16; ++st) {
+            kf[st] = kn[st];
+            if (KB && kbias == -__builtin_inff()) kf[st] = Frag{};
+        }
         if (tile + kWaves < t1) load(tile + kWaves);
         __builtin_amdgcn_wave_barrier();  // one wave's own LDS: in order
 

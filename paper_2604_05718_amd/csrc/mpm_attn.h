@@ -300,6 +300,7 @@ struct PairStage {
     static_assert(ROWS * T::kChunks % THREADS == 0 && THREADS >= ROWS, "whole chunks a thread");
     u32x4 x[kPer], y[kPer];
     const uint8_t *xp[kPer], *yp[kPer];  // this thread's chunks of the next tile
+    float dropped[kPer];
 
     __device__ __forceinline__ void init(const HeadRows& xr, const HeadRows& yr, long first, int head, int t)
     {
@@ -311,8 +312,9 @@ struct PairStage {
             yp[i] = yr.p + (row * yr.row + (long)head * yr.head) * S::kBytes + ch * 16;
         }
     }
-    // Loads rows r0 ... of `count` and moves on; zeros past the last row, past a row's end, and
-    // for rows dropped by drop[row] = -inf, which are not read.
+    // Loads rows r0 ... of `count` and moves on; zeros past the last row and past a row's end. Rows
+    // dropped by drop[row] = -inf are stored as zeros, whatever they hold (loaded all the same: a
+    // load that waits for its drop value would take twice the latency).
     template <bool DROP>
     __device__ __forceinline__ void load(const HeadRows& xr, const HeadRows& yr, int dh, int count, const float* drop,
                                          int r0, int t)
@@ -323,9 +325,10 @@ struct PairStage {
         for (int i = 0; i < kPer; ++i) {
             const int e = t + i * THREADS, ch = e % T::kChunks, r = r0 + e / T::kChunks;
             bool in = ch * (16 / S::kBytes) < dh && r < count;
-            if (DROP && in) in = drop[r] > -__builtin_inff();
             x[i] = y[i] = zero;
+            if (DROP) dropped[i] = 0.0f;
             if (in) {
+                if (DROP) dropped[i] = drop[r];
                 x[i] = load16(xp[i]);
                 y[i] = load16(yp[i]);
             }
@@ -333,10 +336,15 @@ struct PairStage {
             yp[i] += ystep;
         }
     }
-    __device__ __forceinline__ void store(uint8_t* lds, int t) const
+    template <bool DROP>
+    __device__ __forceinline__ void store(uint8_t* lds, int t)
     {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
+            if (DROP && dropped[i] == -__builtin_inff()) {
+                const u32x4 zero = {0, 0, 0, 0};
+                x[i] = y[i] = zero;
+            }
             const int e = t + i * THREADS, at = T::at(e / T::kChunks, e % T::kChunks);
             store16(lds + at, x[i]);
             store16(lds + kTileBytes + at, y[i]);
