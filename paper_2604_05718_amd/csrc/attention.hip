@@ -16,17 +16,17 @@ constexpr float kStartMost = 64.0f;
 // two: probabilities then stay below 256, exact to scale, and most tiles skip the rescaling.
 constexpr float kSlack = 8.0f;
 
-template <class S>
+template <class S, int SPLIT>
 constexpr int key_tile()
 {
-    return S::kBytes == 2 ? 64 : 32;
+    return S::kBytes == 2 ? 64 : 32 * SPLIT;
 }
 
 // One of the two buffers: a tile of keys and of values, their position codes and biases.
-template <class S, int DH>
+template <class S, int DH, int SPLIT>
 constexpr int buffer_bytes()
 {
-    return key_tile<S>() * (2 * Tile<S, DH>::kRowBytes + 8);
+    return key_tile<S, SPLIT>() * (2 * Tile<S, DH>::kRowBytes + 8);
 }
 
 // Waves a SIMD the registers are held to: three of 32 queries (64 channels, bfloat16; 168 registers and
@@ -37,16 +37,18 @@ constexpr int waves_per_simd()
     return S::kBytes == 2 && DH == 64 && QT == 1 ? 3 : 2;
 }
 
-// WAVES waves of QT tiles of 32 queries each share the key tiles.
-template <class S, int DH, int BIAS, bool KB, int WAVES, int QT>
+// WAVES waves of QT tiles of 32 queries each share the key tiles. SPLIT 2: two waves share 32 queries,
+// each taking every other 32 keys, and join their maxima, sums and outputs at the end.
+template <class S, int DH, int BIAS, bool KB, int WAVES, int QT, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void attention_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
                                                                 HeadRows out, float* __restrict__ lse, int blocks)
 {
     constexpr int THREADS = WAVES * kWave;
-    constexpr int KT = key_tile<S>();
+    static_assert(SPLIT == 1 || (SPLIT == 2 && QT == 1), "a split tile is one tile");
+    constexpr int KT = key_tile<S, SPLIT>();
     typedef PairStage<S, DH, KT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
-    constexpr int kBuffer = buffer_bytes<S, DH>();
+    constexpr int kBuffer = buffer_bytes<S, DH, SPLIT>();
     constexpr bool kBf = S::kBytes == 2;
     extern __shared__ __align__(16) uint8_t lds[];
     float* table = reinterpret_cast<float*>(lds + 2 * kBuffer);
@@ -56,9 +58,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     if (!block_item(blocks, a.B * a.H, &blk, &pair)) return;
     const int b = pair / a.H, hd = pair - b * a.H, hk = hd / (a.H / a.Hk);
     const Rows rq = image_rows(a.q_off, b, a.Nq), rk = image_rows(a.k_off, b, a.Nk);
-    const int q0 = blk * 32 * WAVES * QT;
+    const int q0 = blk * (32 * WAVES * QT / SPLIT);
     if (q0 >= rq.count) return;
-    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave / SPLIT, l32 = lane & 31, h = lane >> 5;
+    const int part = t / kWave % SPLIT;
     const int W = 2 * a.span + 1;
     const float c = a.scale * kLog2e;
     // The score products may start from -maximum / c, which takes the maximum off for nothing
@@ -128,10 +131,11 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         const bool more = k0 + KT < rk.count;
         if (more) load(k0 + KT);
 #pragma unroll 1
-        for (int u = 0; u < (works ? KT / 32 : 0); ++u) {
+        for (int u = works ? part : KT / 32; u < KT / 32; u += SPLIT) {
             f32x16 s[QT];
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
+                if (!kBf && st > 0 && 16 * st >= a.dh) continue;  // (a float32 step is worth a branch)
                 const Frag kf = rows_frag<S, DH>(kt, 32 * u + l32, st, h);
 #pragma unroll
                 for (int i = 0; i < QT; ++i) s[i] = mma(kf, qf[i][st], st == 0 ? start[i] : s[i]);
@@ -219,6 +223,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                 for (int i = 0; i < QT; ++i) p[i] = tile_frag(s[i], st, S{});
 #pragma unroll
                 for (int d = 0; d < DH / 32; ++d) {
+                    if (!kBf && d > 0 && 32 * d >= a.dh) continue;
                     const Frag vf = cols_frag<S, DH>(vt, 32 * u + 16 * st, 32 * d, lane);
 #pragma unroll
                     for (int i = 0; i < QT; ++i) acc[i][d] = mma(vf, p[i], acc[i][d]);
@@ -229,6 +234,37 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         __syncthreads();
     }
 
+    if constexpr (SPLIT == 2) {
+        constexpr int kPad = DH + 4;  // floats of a query's outputs, apart in banks
+        float* mine = reinterpret_cast<float*>(lds) + (wave * 32 + l32) * kPad;
+        float2* stats = reinterpret_cast<float2*>(reinterpret_cast<float*>(lds) + WAVES / 2 * 32 * kPad) + wave * kWave + lane;
+        static_assert((WAVES / 2 * 32 * kPad + WAVES / 2 * kWave * 2) * 4 <= 2 * kBuffer, "the joined outputs fit");
+        if (part == 1) {
+            *stats = make_float2(m[0], sum[0]);
+#pragma unroll
+            for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<float4*>(mine + 32 * d + 8 * g + 4 * h) =
+                        make_float4(acc[0][d][4 * g], acc[0][d][4 * g + 1], acc[0][d][4 * g + 2], acc[0][d][4 * g + 3]);
+        }
+        __syncthreads();
+        if (part == 1) return;
+        const float2 other = *stats;
+        const float top = fmaxf(m[0], other.x);
+        const float f = m[0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[0] - top);
+        const float o = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(other.x - top);
+        m[0] = top;
+        sum[0] = f * sum[0] + o * other.y;
+#pragma unroll
+        for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(mine + 32 * d + 8 * g + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][d][4 * g + e] = f * acc[0][d][4 * g + e] + o * x[e];
+            }
+    }
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
         const int qi = q0 + (wave * QT + i) * 32 + l32;
@@ -243,17 +279,17 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     }
 }
 
-template <class S, int DH, int BIAS, bool KB, int WAVES, int QT>
+template <class S, int DH, int BIAS, bool KB, int WAVES, int QT, int SPLIT>
 hipError_t launch_as(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
                      const HeadRows& out, float* lse, hipStream_t stream)
 {
-    constexpr int THREADS = WAVES * kWave, kQueries = 32 * WAVES * QT;
+    constexpr int THREADS = WAVES * kWave, kQueries = 32 * WAVES * QT / SPLIT;
     const int W = 2 * a.span + 1;
-    const size_t bytes = 2 * buffer_bytes<S, DH>() + (BIAS != kBiasNone ? (size_t)W * W * 4 : 0);
+    const size_t bytes = 2 * buffer_bytes<S, DH, SPLIT>() + (BIAS != kBiasNone ? (size_t)W * W * 4 : 0);
     const int blocks = (a.Nq + kQueries - 1) / kQueries;
     const long grid = block_grid((long)a.B * a.H, blocks);
     if (grid * THREADS > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT>;
+    auto kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT, SPLIT>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(THREADS), bytes, stream, a, q, k, v, out, lse, blocks);
@@ -270,12 +306,17 @@ hipError_t launch(const AttentionCall& a, const HeadRows& q, const HeadRows& k, 
                   float* lse, hipStream_t stream)
 {
     constexpr long kLargeTable = 48 << 10;
+    constexpr long kFewGroups = 512;
     if constexpr (S::kBytes == 2 && DH == 64) {
         const long W = 2 * a.span + 1;
         if (a.Nq >= 1792 || (BIAS != kBiasNone && W * W * 4 > kLargeTable && a.Nq > 256))
-            return launch_as<S, DH, BIAS, KB, 8, 2>(a, q, k, v, out, lse, stream);
+            return launch_as<S, DH, BIAS, KB, 8, 2, 1>(a, q, k, v, out, lse, stream);
     }
-    return launch_as<S, DH, BIAS, KB, 4, 1>(a, q, k, v, out, lse, stream);
+    if constexpr (DH == 64) {
+        const long groups = (long)a.B * a.H * ((a.Nq + 127) / 128);
+        if (groups < kFewGroups && a.Nk > 32) return launch_as<S, DH, BIAS, KB, 4, 1, 2>(a, q, k, v, out, lse, stream);
+    }
+    return launch_as<S, DH, BIAS, KB, 4, 1, 1>(a, q, k, v, out, lse, stream);
 }
 
 template <class S, int DH>
