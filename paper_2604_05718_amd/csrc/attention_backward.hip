@@ -34,10 +34,10 @@ enum SumKind : int {
     kSumTurns = 3
 };
 
-template <class S, int DH>
+template <class S, int DH, int SPLIT>
 constexpr int tile_rows()
 {
-    return S::kBytes == 2 && DH == 64 ? 64 : 32;
+    return S::kBytes == 2 && DH == 64 ? 64 : 32 * SPLIT;
 }
 // Buffers of row tiles in LDS: two, or one where two would not leave room for the tables.
 template <class S, int DH>
@@ -45,10 +45,34 @@ constexpr int buffers()
 {
     return S::kBytes == 4 && DH == 128 ? 1 : 2;
 }
-template <class S, int DH>
+template <class S, int DH, int SPLIT>
 constexpr int tile_bytes()
 {
-    return 2 * tile_rows<S, DH>() * Tile<S, DH>::kRowBytes;
+    return 2 * tile_rows<S, DH, SPLIT>() * Tile<S, DH>::kRowBytes;
+}
+
+// A split wave's sums join its partner's through LDS: N tiles a lane, in tile order.
+template <int N>
+__device__ __forceinline__ void give(float* lds, const f32x16 (&x)[N], int lane)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<float4*>(lds + ((n * 4 + r / 4) * kWave + lane) * 4) =
+                make_float4(x[n][r], x[n][r + 1], x[n][r + 2], x[n][r + 3]);
+}
+template <int N>
+__device__ __forceinline__ void take(const float* lds, f32x16 (&x)[N], int lane)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(lds + ((n * 4 + r / 4) * kWave + lane) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[n][r + e] += v[e];
+        }
 }
 
 // What the kernels leave for each other: D of every query and head, the largest |dS| and |dP - D| of
@@ -116,17 +140,18 @@ __device__ __forceinline__ float2 taken(float2 l, bool apart, float c, float lg)
     return make_float2(none ? -__builtin_inff() : (lg - l.x - l.y) / c, 0.0f);
 }
 
-// dK and dV of WAVES x 32 keys of one key head: all queries of all heads that share it.
-template <class S, int DH, int BIAS, bool KB, int WAVES>
+// dK and dV of WAVES x 32 keys of one key head: all queries of all heads that share it. SPLIT 2 (here and
+// below): two waves share 32 rows, each taking every other 32 of the other side, and add up at the end.
+template <class S, int DH, int BIAS, bool KB, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                       HeadRows k, HeadRows v,
                                                                       const float2* __restrict__ lse, Scratch w,
                                                                       HeadRows dk, HeadRows dv, int blocks)
 {
-    constexpr int THREADS = WAVES * kWave, QT = tile_rows<S, DH>(), BUFS = buffers<S, DH>();
+    constexpr int THREADS = WAVES * kWave, QT = tile_rows<S, DH, SPLIT>(), BUFS = buffers<S, DH>();
     typedef PairStage<S, DH, QT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
-    constexpr int kBuffer = tile_bytes<S, DH>() + QT * 16 + 16;
+    constexpr int kBuffer = tile_bytes<S, DH, SPLIT>() + QT * 16 + 16;
     extern __shared__ __align__(16) uint8_t lds[];
     float* table = reinterpret_cast<float*>(lds + BUFS * kBuffer);
     const int table_at = lds_address(table);
@@ -135,9 +160,10 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
     if (!block_item(blocks, (long)a.B * a.Hk, &blk, &pair)) return;
     const int b = pair / a.Hk, hk = pair - b * a.Hk, group = a.H / a.Hk;
     const Rows rq = image_rows(a.q_off, b, a.Nq), rk = image_rows(a.k_off, b, a.Nk);
-    const int k0 = blk * 32 * WAVES;
+    const int k0 = blk * (32 * WAVES / SPLIT);
     if (k0 >= rk.count) return;
-    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave / SPLIT, l32 = lane & 31, h = lane >> 5;
+    const int share = t / kWave % SPLIT;
     const int ki = k0 + wave * 32 + l32;
     const bool exists = ki < rk.count;
     const bool works = k0 + wave * 32 < rk.count;  // a wave past the image's end only brings tiles
@@ -189,7 +215,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
             uint8_t* at = lds + buf * kBuffer;
             stage.template store<false>(at, t);
             if (t < QT) {  // one wave (or half of one)
-                int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH>());
+                int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH, SPLIT>());
                 float* first = reinterpret_cast<float*>(codes + QT);
                 if (BIAS != kBiasNone) codes[t] = query_code<BIAS>(pos, a.grid_h, a.grid_w, a.span, W, table_at);
                 const bool apart = !start || __any(too_large(stat));
@@ -216,7 +242,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
             if (more) load(q0 + QT);
             const bool apart = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(first + 3 * QT)[0]);
 #pragma unroll 1
-            for (int u = 0; u < (works ? QT / 32 : 0); ++u) {
+            for (int u = works ? share : QT / 32; u < QT / 32; u += SPLIT) {
                 f32x16 s, dp;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -232,6 +258,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
                 }
 #pragma unroll
                 for (int st = 0; st < DH / 16; ++st) {
+                    if (S::kBytes == 4 && 16 * st >= a.dh) continue;  // (a float32 step is worth a branch)
                     s = mma(rows_frag<S, DH>(qt, 32 * u + l32, st, h), kf[st], s);
                     dp = mma(rows_frag<S, DH>(ot, 32 * u + l32, st, h), vf[st], dp);
                 }
@@ -269,6 +296,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
                     const Frag p = tile_frag(s, st, S{}), ds = tile_frag(dp, st, S{});
 #pragma unroll
                     for (int d = 0; d < DH / 32; ++d) {
+                        if (S::kBytes == 4 && 32 * d >= a.dh) continue;
                         gv[d] = mma(cols_frag<S, DH>(ot, 32 * u + 16 * st, 32 * d, lane), p, gv[d]);
                         gk[d] = mma(cols_frag<S, DH>(qt, 32 * u + 16 * st, 32 * d, lane), ds, gk[d]);
                     }
@@ -293,6 +321,18 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(Attention
         }
     }
 
+    if constexpr (SPLIT == 2) {
+        float* mine = reinterpret_cast<float*>(lds) + wave * (2 * DH / 32 * 16 * kWave);
+        static_assert(WAVES / 2 * 2 * DH / 32 * 16 * kWave * 4 <= BUFS * kBuffer, "the shared sums fit");
+        if (share == 1) {
+            give(mine, gk, lane);
+            give(mine + DH / 32 * 16 * kWave, gv, lane);
+        }
+        __syncthreads();
+        if (share == 1) return;
+        take(mine, gk, lane);
+        take(mine + DH / 32 * 16 * kWave, gv, lane);
+    }
     // A dropped key's gradients are zero, whatever its rows hold.
     if (!live) {
 #pragma unroll
@@ -320,19 +360,19 @@ __host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
 
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: kSum32 pairs of
 // (bias, sum), otherwise the biases and then the sums (kSum64: the sums first).
-template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES>
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                         HeadRows k, HeadRows v,
                                                                         const float2* __restrict__ lse, Scratch w,
                                                                         HeadRows dq, int blocks)
 {
-    constexpr int THREADS = WAVES * kWave, KT = tile_rows<S, DH>(), BUFS = buffers<S, DH>();
+    constexpr int THREADS = WAVES * kWave, KT = tile_rows<S, DH, SPLIT>(), BUFS = buffers<S, DH>();
     constexpr int SIZE = SUM == kSum32 ? 8 : 4;
     typedef PairStage<S, DH, KT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
     typedef __attribute__((address_space(3))) int32_t lds_int;
     typedef __attribute__((address_space(3))) unsigned long long lds_long;
-    constexpr int kBuffer = tile_bytes<S, DH>() + KT * 8;
+    constexpr int kBuffer = tile_bytes<S, DH, SPLIT>() + KT * 8;
     static_assert(32 * WAVES <= kMaxRows, "the fixed point's range");
     extern __shared__ __align__(16) uint8_t lds[];
     const int W = 2 * a.span + 1, W2 = W * W;
@@ -344,9 +384,10 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
     if (!block_item(blocks, (long)a.B * a.H, &blk, &pair)) return;
     const int b = pair / a.H, hd = pair - b * a.H, hk = hd / (a.H / a.Hk);
     const Rows rq = image_rows(a.q_off, b, a.Nq), rk = image_rows(a.k_off, b, a.Nk);
-    const int q0 = blk * 32 * WAVES;
+    const int q0 = blk * (32 * WAVES / SPLIT);
     if (q0 >= rq.count) return;
-    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, h = lane >> 5;
+    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave / SPLIT, l32 = lane & 31, h = lane >> 5;
+    const int share = t / kWave % SPLIT;
     const int qi = q0 + wave * 32 + l32;
     const bool live = qi < rq.count;
     const bool works = q0 + wave * 32 < rq.count;  // a wave past the image's end only brings tiles
@@ -370,7 +411,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
         uint8_t* at = lds + buf * kBuffer;
         stage.template store<KB>(at, t);
         if (t < KT) {
-            int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH>());
+            int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH, SPLIT>());
             if (BIAS != kBiasNone) codes[t] = bias_code<BIAS, SIZE>(pos, a.grid_h, a.grid_w, W);
             if (KB) reinterpret_cast<float*>(codes + KT)[t] = to_log2(kbias);
         }
@@ -425,10 +466,11 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
         const bool more = k0 + KT < rk.count;
         if (more) load(k0 + KT);
 #pragma unroll 1
-        for (int u = 0; u < (works || SUM == kSumTurns ? KT / 32 : 0); ++u) {
+        for (int u = works || SUM == kSumTurns ? share : KT / 32; u < KT / 32; u += SPLIT) {
             f32x16 s, dp;
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
+                if (S::kBytes == 4 && st > 0 && 16 * st >= a.dh) continue;
                 s = mma(rows_frag<S, DH>(kt, 32 * u + l32, st, h), qf[st], st == 0 ? s0 : s);
                 dp = mma(rows_frag<S, DH>(vt, 32 * u + l32, st, h), of[st], st == 0 ? dp0 : dp);
             }
@@ -473,7 +515,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
                 const Frag ds = tile_frag(dp, st, S{});
 #pragma unroll
                 for (int d = 0; d < DH / 32; ++d)
-                    gq[d] = mma(cols_frag<S, DH>(kt, 32 * u + 16 * st, 32 * d, lane), ds, gq[d]);
+                    if (S::kBytes == 2 || 32 * d < a.dh) gq[d] = mma(cols_frag<S, DH>(kt, 32 * u + 16 * st, 32 * d, lane), ds, gq[d]);
             }
             if (SUM == kSum32) {
 #pragma unroll
@@ -493,7 +535,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
             }
             if (SUM == kSumTurns) {
                 for (int turn = 0; turn < 2 * WAVES; ++turn) {
-                    if (wave == turn / 2 && h == turn % 2 && live) {
+                    if (t / kWave == turn / 2 && h == turn % 2 && live) {
 #pragma unroll
                         for (int r = 0; r < 16; ++r)
                             __hip_atomic_fetch_add((__attribute__((address_space(3))) float*)(uintptr_t)(uint32_t)(
@@ -510,6 +552,13 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
     }
 
     const float back = __builtin_ldexpf(1.0f, -lg);
+    if constexpr (SPLIT == 2) {
+        float* mine = reinterpret_cast<float*>(lds) + wave * (DH / 32 * 16 * kWave);
+        static_assert(WAVES / 2 * DH / 32 * 16 * kWave * 4 <= BUFS * kBuffer, "the shared sums fit");
+        if (share == 1) give(mine, gq, lane);
+        __syncthreads();
+        if (share == 0) take(mine, gq, lane);
+    }
     if (SUM != kSumNone) {
         // A gradient that is not a number is not one in the sums either: it has reached dq.
         bool bad = false;
@@ -517,7 +566,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
         for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) bad |= !(fabsf(gq[d][r]) < __builtin_inff());
-        const bool any_bad = __syncthreads_or(bad && live);
+        const bool any_bad = __syncthreads_or(bad && live && share == 0);
         float* part = w.parts + ((long)pair * blocks + blk) * W2;
         for (int e = t; e < W2; e += THREADS) {
             float x;
@@ -527,7 +576,7 @@ __global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(Attenti
             part[e] = any_bad ? __builtin_nanf("") : x;
         }
     }
-    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale * back, a.dh, live, h, S{});
+    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale * back, a.dh, live && share == 0, h, S{});
 }
 
 // dbias[head][e] = the workgroups' parts, in the order of images and query blocks: four threads an
@@ -569,24 +618,40 @@ struct Inputs {
 
 // Query rows of a workgroup: eight waves where the tables leave LDS for one workgroup only.
 constexpr long kLargeTable = 24 << 10;
-bool large(const AttentionCall& a)
+bool large_table(const AttentionCall& a)
 {
     const long W = 2 * a.span + 1;
     return a.dt == kBf16 && a.dh <= 64 && a.bias && W * W * 4 > kLargeTable;
 }
-int block_rows(const AttentionCall& a) { return large(a) ? 256 : 128; }
+// Waves of a workgroup and how many share a tile: split where workgroups of 128 rows would leave
+// compute units idle (and the tables of a float32 call leave room for the longer tiles).
+struct Shape {
+    int waves, split;
+    int rows() const { return 32 * waves / split; }
+};
+constexpr long kFewGroups = 512;
+constexpr size_t kLdsBytes = 160 << 10;
+Shape shape(const AttentionCall& a)
+{
+    if (large_table(a)) return Shape{8, 1};
+    const long groups = (long)a.B * a.H * ((a.Nq + 127) / 128), W = 2 * a.span + 1;
+    const bool room = a.dt == kBf16 || !a.bias || W * W * 12 + (66L << 10) <= (long)kLdsBytes;
+    return Shape{4, a.dh <= 64 && groups < kFewGroups && room ? 2 : 1};
+}
+int block_rows(const AttentionCall& a) { return shape(a).rows(); }
 int query_blocks(const AttentionCall& a) { return (a.Nq + block_rows(a) - 1) / block_rows(a); }
 
-template <class S, int DH, int BIAS, bool KB, int WAVES>
+template <class S, int DH, int BIAS, bool KB, int WAVES, int SPLIT>
 hipError_t launch_keys(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
     const size_t W = 2 * a.span + 1;
-    const int blocks = (a.Nk + 32 * WAVES - 1) / (32 * WAVES);
-    const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH>() + tile_rows<S, DH>() * 16 + 16) +
+    constexpr int kRows = 32 * WAVES / SPLIT;
+    const int blocks = (a.Nk + kRows - 1) / kRows;
+    const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 16 + 16) +
                          (BIAS != kBiasNone ? W * W * 4 : 0);
     const long grid = block_grid((long)a.B * a.Hk, blocks);
     if (grid * WAVES * kWave > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = key_gradient_kernel<S, DH, BIAS, KB, WAVES>;
+    auto kernel = key_gradient_kernel<S, DH, BIAS, KB, WAVES, SPLIT>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), bytes, st, a, in.dout, in.q, in.k, in.v,
@@ -594,15 +659,15 @@ hipError_t launch_keys(const AttentionCall& a, const Inputs& in, const Grads& g,
     return hipGetLastError();
 }
 
-template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES>
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 hipError_t launch_queries(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
     const int blocks = query_blocks(a);
-    const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH>() + tile_rows<S, DH>() * 8) +
+    const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8) +
                          table_bytes(BIAS, SUM, 2 * a.span + 1);
     const long grid = block_grid((long)a.B * a.H, blocks);
     if (grid * WAVES * kWave > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES>;
+    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES, SPLIT>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), bytes, st, a, in.dout, in.q, in.k, in.v,
@@ -610,9 +675,7 @@ hipError_t launch_queries(const AttentionCall& a, const Inputs& in, const Grads&
     return hipGetLastError();
 }
 
-constexpr size_t kLdsBytes = 160 << 10;
-
-template <class S, int DH, int BIAS, bool KB, int WAVES>
+template <class S, int DH, int BIAS, bool KB, int WAVES, int SPLIT>
 hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
     const int W = 2 * a.span + 1;
@@ -620,42 +683,50 @@ hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, 
     hipLaunchKernelGGL(delta_kernel<S>, dim3((unsigned)((per_image + kDeltaThreads - 1) / kDeltaThreads), (unsigned)a.B),
                        dim3(kDeltaThreads), 0, st, a, in.dout, in.out, g.w);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess) e = launch_keys<S, DH, BIAS, KB, WAVES>(a, in, g, st);
+    if (e == hipSuccess) e = launch_keys<S, DH, BIAS, KB, WAVES, SPLIT>(a, in, g, st);
     if (e != hipSuccess) return e;
     if constexpr (BIAS == kBiasNone) {
-        return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES>(a, in, g, st);
+        return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES, SPLIT>(a, in, g, st);
     } else {
-        constexpr size_t tiles = buffers<S, DH>() * (tile_bytes<S, DH>() + tile_rows<S, DH>() * 8);
-        if (!g.dbias) return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES>(a, in, g, st);
-        if constexpr (S::kBytes == 2 && BIAS == kBiasGrid) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES>(a, in, g, st);
+        constexpr size_t tiles = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8);
+        if (!g.dbias) return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES, SPLIT>(a, in, g, st);
+        if constexpr (S::kBytes == 2 && BIAS == kBiasGrid) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT>(a, in, g, st);
         else if (tiles + table_bytes(BIAS, kSum64, W) <= kLdsBytes)
-            e = launch_queries<S, DH, BIAS, KB, kSum64, WAVES>(a, in, g, st);
-        else e = launch_queries<S, DH, BIAS, KB, kSumTurns, WAVES>(a, in, g, st);
+            e = launch_queries<S, DH, BIAS, KB, kSum64, WAVES, SPLIT>(a, in, g, st);
+        else e = launch_queries<S, DH, BIAS, KB, kSumTurns, WAVES, SPLIT>(a, in, g, st);
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(bias_parts_kernel, dim3((unsigned)((W * W + kJoinEntries - 1) / kJoinEntries), (unsigned)a.H),
-                           dim3(kJoinEntries * kJoinWays), 0, st, a, g.w.parts, query_blocks(a), 32 * WAVES, g.dbias);
+                           dim3(kJoinEntries * kJoinWays), 0, st, a, g.w.parts, query_blocks(a), 32 * WAVES / SPLIT, g.dbias);
         return hipGetLastError();
     }
 }
 
-template <class S, int DH, int BIAS, int WAVES>
+template <class S, int DH, int BIAS, int WAVES, int SPLIT>
 hipError_t pick_drop(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
-    return a.k_bias ? launch_all<S, DH, BIAS, true, WAVES>(a, in, g, st)
-                    : launch_all<S, DH, BIAS, false, WAVES>(a, in, g, st);
+    return a.k_bias ? launch_all<S, DH, BIAS, true, WAVES, SPLIT>(a, in, g, st)
+                    : launch_all<S, DH, BIAS, false, WAVES, SPLIT>(a, in, g, st);
+}
+
+template <class S, int DH, int BIAS>
+hipError_t pick_shape(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
+{
+    const Shape s = shape(a);
+    if constexpr (S::kBytes == 2 && DH == 64 && BIAS != kBiasNone)
+        if (s.waves == 8) return pick_drop<S, DH, BIAS, 8, 1>(a, in, g, st);
+    if constexpr (DH == 64)
+        if (s.split == 2) return pick_drop<S, DH, BIAS, 4, 2>(a, in, g, st);
+    return pick_drop<S, DH, BIAS, 4, 1>(a, in, g, st);
 }
 
 template <class S, int DH>
 hipError_t pick(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
-    const int kind = bias_kind(a);
-    if (kind == kBiasNone) return pick_drop<S, DH, kBiasNone, 4>(a, in, g, st);
-    if constexpr (S::kBytes == 2 && DH == 64) {
-        if (large(a))
-            return kind == kBiasGrid ? pick_drop<S, DH, kBiasGrid, 8>(a, in, g, st)
-                                     : pick_drop<S, DH, kBiasFar, 8>(a, in, g, st);
+    switch (bias_kind(a)) {
+    case kBiasNone: return pick_shape<S, DH, kBiasNone>(a, in, g, st);
+    case kBiasGrid: return pick_shape<S, DH, kBiasGrid>(a, in, g, st);
+    default: return pick_shape<S, DH, kBiasFar>(a, in, g, st);
     }
-    return kind == kBiasGrid ? pick_drop<S, DH, kBiasGrid, 4>(a, in, g, st) : pick_drop<S, DH, kBiasFar, 4>(a, in, g, st);
 }
 
 size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
