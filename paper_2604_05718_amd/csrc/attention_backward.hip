@@ -75,6 +75,13 @@ __device__ __forceinline__ void take(const float* lds, f32x16 (&x)[N], int lane)
         }
 }
 
+// Waves a SIMD the registers are held to: float32 fragments take twice the registers.
+template <class S>
+constexpr int waves_per_simd()
+{
+    return S::kBytes == 2 ? 2 : 1;
+}
+
 // What the kernels leave for each other: D of every query and head, the largest |dS| and |dP - D| of
 // every image and head (as bits), and whether an image's keys repeat a position.
 struct Scratch {
@@ -143,7 +150,7 @@ __device__ __forceinline__ float2 taken(float2 l, bool apart, float c, float lg)
 // dK and dV of WAVES x 32 keys of one key head: all queries of all heads that share it. SPLIT 2 (here and
 // below): two waves share 32 rows, each taking every other 32 of the other side, and add up at the end.
 template <class S, int DH, int BIAS, bool KB, int WAVES, int SPLIT>
-__global__ __launch_bounds__(WAVES* kWave, 2) void key_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
+__global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                       HeadRows k, HeadRows v,
                                                                       const float2* __restrict__ lse, Scratch w,
                                                                       HeadRows dk, HeadRows dv, int blocks)
@@ -361,7 +368,7 @@ __host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: kSum32 pairs of
 // (bias, sum), otherwise the biases and then the sums (kSum64: the sums first).
 template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
-__global__ __launch_bounds__(WAVES* kWave, 2) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
+__global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                         HeadRows k, HeadRows v,
                                                                         const float2* __restrict__ lse, Scratch w,
                                                                         HeadRows dq, int blocks)
