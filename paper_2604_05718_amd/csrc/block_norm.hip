@@ -18,20 +18,6 @@ constexpr int kSumGroups = 512;
 constexpr int kSums = 5;  // dw, db, dscale, dpost_w, dpost_b (a gate's sums are by image)
 
 template <class S>
-__device__ __forceinline__ void unpack(u32x4 v, float* out)
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (S::kBytes == 2) {
-            out[2 * e] = bf16_lo(v[e]);
-            out[2 * e + 1] = bf16_hi(v[e]);
-        } else {
-            out[e] = __uint_as_float(v[e]);
-        }
-    }
-}
-
-template <class S>
 __device__ __forceinline__ u32x4 pack(const float* v)
 {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -55,18 +41,42 @@ constexpr int threads()
     return LANES > kMinThreads ? LANES : kMinThreads;
 }
 
-// The sums of two values over the lanes of a row (in a fixed order).
+// A value plus its counterpart's by a fixed lane pattern inside 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v)
+{
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+
+// The sum of a value over 32 or 64 lanes, in every lane: exchanges inside 16 lanes (neighbour, pair,
+// half and whole mirror), then between the 16s and the 32s. No LDS: two sums of a row by LDS
+// exchanges took a third of a row's time.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v = dpp_add<0xb1>(v);   // lane ^ 1
+    v = dpp_add<0x4e>(v);   // lane ^ 2
+    v = dpp_add<0x141>(v);  // 7 - lane of 8
+    v = dpp_add<0x140>(v);  // 15 - lane of 16
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    if constexpr (LANES >= kWave) {
+        const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+    }
+    return v;
+}
+
+// The sums of two values over the lanes of a row, in a fixed order. Rows of several waves meet in LDS:
+// every row group of the workgroup has to call.
 template <int LANES>
 __device__ __forceinline__ void row_sums(float& a, float& b, float* lds)
 {
-#pragma unroll
-    for (int o = (LANES < kWave ? LANES : kWave) / 2; o > 0; o >>= 1) {
-        a += __shfl_xor(a, o);
-        b += __shfl_xor(b, o);
-    }
+    a = lanes_sum<LANES>(a);
+    b = lanes_sum<LANES>(b);
     if constexpr (LANES > kWave) {
         constexpr int kWaves = LANES / kWave;
-        const int wave = threadIdx.x / kWave;
+        const int wave = threadIdx.x / kWave, first = wave / kWaves * kWaves;
         __syncthreads();  // the sums before have been read
         if (threadIdx.x % kWave == 0) {
             lds[2 * wave] = a;
@@ -76,51 +86,49 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float* lds)
         a = b = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            a += lds[2 * w];
-            b += lds[2 * w + 1];
+            a += lds[2 * (first + w)];
+            b += lds[2 * (first + w) + 1];
         }
     }
 }
 
-// A row's values in one lane: VPL vectors of 16 bytes, vector lane + u LANES of the row.
+// A row's part in one lane as it is stored: VPL vectors of 16 bytes, vector lane + u LANES of the row.
 template <class S, int LANES, int VPL>
-struct RowPart {
+struct RawPart {
     static constexpr int kPer = 16 / S::kBytes;
     static constexpr int kVals = VPL * kPer;
-    float v[kVals];
+    u32x4 v[VPL];
 
-    __device__ __forceinline__ void load(const void* base, long row, int D, int lane)
+    // (base null, or not live: zeros)
+    __device__ __forceinline__ void load(const void* base, long row, int D, int lane, bool live = true)
     {
         const uint8_t* p = static_cast<const uint8_t*>(base) + row * D * S::kBytes;
 #pragma unroll
         for (int u = 0; u < VPL; ++u) {
             const int c = lane + u * LANES;
-            u32x4 w = {0, 0, 0, 0};
-            if (c * kPer < D) w = load16(p + c * 16);
-            unpack<S>(w, v + u * kPer);
+            const u32x4 zero = {0, 0, 0, 0};
+            v[u] = zero;
+            if (base && live && c * kPer < D) v[u] = load16(p + c * 16);
         }
     }
-    __device__ __forceinline__ void fill(float x)
+    __device__ __forceinline__ float get(int e) const
     {
-#pragma unroll
-        for (int e = 0; e < kVals; ++e) v[e] = x;
+        const u32x4 w = v[e / kPer];
+        const int k = e % kPer;
+        if constexpr (S::kBytes == 2) return k % 2 ? bf16_hi(w[k / 2]) : bf16_lo(w[k / 2]);
+        return __uint_as_float(w[k]);
     }
-    __device__ __forceinline__ void load_or(const void* base, long row, int D, int lane, float x)
-    {
-        if (base) load(base, row, D, lane);
-        else fill(x);
-    }
-    __device__ __forceinline__ void store(void* base, long row, int D, int lane) const
+    // Whether value e of this lane lies inside the row.
+    __device__ static __forceinline__ bool in(int e, int lane, int D) { return (lane + e / kPer * LANES) * kPer < D; }
+    __device__ static __forceinline__ void store(const float (&x)[kVals], void* base, long row, int D, int lane)
     {
         uint8_t* p = static_cast<uint8_t*>(base) + row * D * S::kBytes;
 #pragma unroll
         for (int u = 0; u < VPL; ++u) {
             const int c = lane + u * LANES;
-            if (c * kPer < D) store16(p + c * 16, pack<S>(v + u * kPer));
+            if (c * kPer < D) store16(p + c * 16, pack<S>(x + u * kPer));
         }
     }
-    // Whether value e of this lane lies inside the row.
-    __device__ static __forceinline__ bool in(int e, int lane, int D) { return (lane + e / kPer * LANES) * kPer < D; }
 };
 
 struct Item {
@@ -139,22 +147,22 @@ __device__ __forceinline__ Item item_rows(const NormCall& a, long i)
 
 // Mean and reciprocal deviation of a row's values (rms: mean 0).
 template <class S, int LANES, int VPL>
-__device__ __forceinline__ void row_stats(const RowPart<S, LANES, VPL>& x, int D, int lane, bool layer, float eps,
-                                          float* lds, float& mean, float& rstd)
+__device__ __forceinline__ void row_stats(const float (&x)[RawPart<S, LANES, VPL>::kVals], int D, int lane, bool layer,
+                                          float eps, float* lds, float& mean, float& rstd)
 {
-    typedef RowPart<S, LANES, VPL> Part;
+    typedef RawPart<S, LANES, VPL> Raw;
     mean = 0.0f;
     float none = 0.0f;
     if (layer) {
 #pragma unroll
-        for (int e = 0; e < Part::kVals; ++e) mean += x.v[e];  // zeros past the row's end
+        for (int e = 0; e < Raw::kVals; ++e) mean += Raw::in(e, lane, D) ? x[e] : 0.0f;
         row_sums<LANES>(mean, none, lds);
         mean /= (float)D;
     }
     float sq = 0.0f;
 #pragma unroll
-    for (int e = 0; e < Part::kVals; ++e) {
-        const float d = Part::in(e, lane, D) ? x.v[e] - mean : 0.0f;
+    for (int e = 0; e < Raw::kVals; ++e) {
+        const float d = Raw::in(e, lane, D) ? x[e] - mean : 0.0f;
         sq = fmaf(d, d, sq);
     }
     none = 0.0f;
@@ -162,56 +170,68 @@ __device__ __forceinline__ void row_stats(const RowPart<S, LANES, VPL>& x, int D
     rstd = 1.0f / sqrtf(sq / (float)D + eps);
 }
 
+// Forward: a row group of LANES lanes takes every kRows-th row of the workgroup's, the next row's x and
+// f on their way while one is computed; the parameters stay in registers.
 template <class S, int LANES, int VPL>
 __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, const void* __restrict__ x,
                                                                const void* __restrict__ f, void* __restrict__ y,
                                                                void* __restrict__ hout, float* __restrict__ stats)
 {
-    typedef RowPart<S, LANES, VPL> Part;
+    typedef RawPart<S, LANES, VPL> Raw;
     __shared__ float lds[2 * threads<LANES>() / kWave];
-    constexpr int kRows = threads<LANES>() / LANES;
+    constexpr int kRows = threads<LANES>() / LANES, kVals = Raw::kVals;
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, D = a.D;
     const Item it = item_rows(a, blockIdx.x);
-    for (long row = it.first + sub; row < it.end; row += kRows) {
-        Part u, r;
-        float pmean = 0.0f, prstd = 1.0f;
-        u.load(f, row, D, lane);
-        r.load(x, row, D, lane);
-        if (a.post_w) {
-            row_stats(u, D, lane, a.layer, a.eps, lds, pmean, prstd);
-            Part w, b;
-            w.load(a.post_w, 0, D, lane);
-            b.load_or(a.post_b, 0, D, lane, 0.0f);
+    if (it.first >= it.end) return;
+    Raw fn, xn, pw, pb, sc, ga, w, b;
+    const bool one = it.first + sub < it.end;
+    fn.load(f, it.first + sub, D, lane, one);
+    xn.load(x, it.first + sub, D, lane, one);
+    pw.load(a.post_w, 0, D, lane);
+    pb.load(a.post_b, 0, D, lane);
+    sc.load(a.scale, 0, D, lane);
+    if (a.gate && !a.gate_rows) ga.load(a.gate, it.image, D, lane);
+    w.load(a.w, 0, D, lane);
+    b.load(a.b, 0, D, lane);
+    for (long base = it.first; base < it.end; base += kRows) {
+        const long row = base + sub;
+        const bool live = row < it.end;
+        float u[kVals], r[kVals];
 #pragma unroll
-            for (int e = 0; e < Part::kVals; ++e) u.v[e] = fmaf((u.v[e] - pmean) * prstd, w.v[e], b.v[e]);
+        for (int e = 0; e < kVals; ++e) {
+            u[e] = fn.get(e);
+            r[e] = xn.get(e);
+        }
+        if (a.gate && a.gate_rows) ga.load(a.gate, live ? row : it.first, D, lane);
+        const bool next = row + kRows < it.end;
+        fn.load(f, row + kRows, D, lane, next);
+        xn.load(x, row + kRows, D, lane, next);
+        float pmean = 0.0f, prstd = 1.0f;
+        if (a.post_w) {
+            row_stats<S, LANES, VPL>(u, D, lane, a.layer, a.eps, lds, pmean, prstd);
+#pragma unroll
+            for (int e = 0; e < kVals; ++e) u[e] = fmaf((u[e] - pmean) * prstd, pw.get(e), pb.get(e));
         }
         if (a.scale) {
-            Part w;
-            w.load(a.scale, 0, D, lane);
 #pragma unroll
-            for (int e = 0; e < Part::kVals; ++e) u.v[e] *= w.v[e];
+            for (int e = 0; e < kVals; ++e) u[e] *= sc.get(e);
         }
         if (a.gate) {
-            Part w;
-            w.load(a.gate, a.gate_rows ? row : it.image, D, lane);
 #pragma unroll
-            for (int e = 0; e < Part::kVals; ++e) u.v[e] *= w.v[e];
+            for (int e = 0; e < kVals; ++e) u[e] *= ga.get(e);
         }
 #pragma unroll
-        for (int e = 0; e < Part::kVals; ++e) r.v[e] += u.v[e];
-        r.store(y, row, D, lane);
+        for (int e = 0; e < kVals; ++e) r[e] += u[e];
+        if (live) Raw::store(r, y, row, D, lane);
         float mean = 0.0f, rstd = 1.0f;
         if (a.w) {
             // Of the sum before its rounding to y's type, which only the stored y has.
-            row_stats(r, D, lane, a.layer, a.eps, lds, mean, rstd);
-            Part w, b;
-            w.load(a.w, 0, D, lane);
-            b.load_or(a.b, 0, D, lane, 0.0f);
+            row_stats<S, LANES, VPL>(r, D, lane, a.layer, a.eps, lds, mean, rstd);
 #pragma unroll
-            for (int e = 0; e < Part::kVals; ++e) r.v[e] = fmaf((r.v[e] - mean) * rstd, w.v[e], b.v[e]);
-            r.store(hout, row, D, lane);
+            for (int e = 0; e < kVals; ++e) r[e] = fmaf((r[e] - mean) * rstd, w.get(e), b.get(e));
+            if (live) Raw::store(r, hout, row, D, lane);
         }
-        if (stats && lane == 0) reinterpret_cast<float4*>(stats)[row] = make_float4(pmean, prstd, mean, rstd);
+        if (stats && live && lane == 0) reinterpret_cast<float4*>(stats)[row] = make_float4(pmean, prstd, mean, rstd);
     }
 }
 
@@ -219,7 +239,7 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, cons
 template <class S, int LANES, int VPL>
 __device__ __forceinline__ void store_sums(const float* v, float* out, long slot, int D, int lane, int sub, float* lds)
 {
-    typedef RowPart<S, LANES, VPL> Part;
+    typedef RawPart<S, LANES, VPL> Part;
     constexpr int kRows = threads<LANES>() / LANES;
     if constexpr (kRows > 1) __syncthreads();
 #pragma unroll
@@ -243,112 +263,129 @@ __device__ __forceinline__ void store_sums(const float* v, float* out, long slot
 }
 
 // dx and df of every row, and the workgroup's column sums: sums[k][group][D] (kSums of them) and, for
-// a gate by image, gate_sums[item][D].
+// a gate by image, gate_sums[item][D]. Rows and parameters as in the forward kernel.
 template <class S, int LANES, int VPL>
 __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     NormCall a, const void* __restrict__ dy, const void* __restrict__ dh, const void* __restrict__ y,
     const void* __restrict__ f, const float* __restrict__ stats, void* __restrict__ dx, void* __restrict__ df,
     void* __restrict__ dgate, float* __restrict__ sums, float* __restrict__ gate_sums, long items)
 {
-    typedef RowPart<S, LANES, VPL> Part;
-    constexpr int kRows = threads<LANES>() / LANES;
+    typedef RawPart<S, LANES, VPL> Raw;
+    constexpr int kRows = threads<LANES>() / LANES, kVals = Raw::kVals;
     __shared__ float lds[threads<LANES>()];
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, D = a.D;
     const float inv = 1.0f / (float)D;
-    Part sw, sb, ss, spw, spb;
-    sw.fill(0.0f), sb.fill(0.0f), ss.fill(0.0f), spw.fill(0.0f), spb.fill(0.0f);
+    float sw[kVals], sb[kVals], ss[kVals], spw[kVals], spb[kVals];
+#pragma unroll
+    for (int e = 0; e < kVals; ++e) sw[e] = sb[e] = ss[e] = spw[e] = spb[e] = 0.0f;
+    Raw w, pw, pb, sc, ga;
+    w.load(a.w, 0, D, lane);
+    pw.load(a.post_w, 0, D, lane);
+    pb.load(a.post_b, 0, D, lane);
+    sc.load(a.scale, 0, D, lane);
     for (long i = blockIdx.x; i < items; i += gridDim.x) {
         const Item it = item_rows(a, i);
-        Part sg;
-        sg.fill(0.0f);
+        float sg[kVals];
+#pragma unroll
+        for (int e = 0; e < kVals; ++e) sg[e] = 0.0f;
+        if (a.gate && !a.gate_rows) ga.load(a.gate, it.image, D, lane);
+        Raw yn, hn, gn, fn;
+        float4 stn = make_float4(0, 0, 0, 0);
+        // (rows past the end: zeros, which add nothing to the sums)
+        auto load = [&](long row) {
+            const bool live = row < it.end;
+            gn.load(dy, row, D, lane, live);
+            if (a.w) {
+                yn.load(y, row, D, lane, live);
+                hn.load(dh, row, D, lane, live);
+            }
+            fn.load(f, row, D, lane, live);
+            if (live) stn = reinterpret_cast<const float4*>(stats)[row];
+        };
+        if (it.first < it.end) load(it.first + sub);
         // Every row group takes the same number of turns: the sums of a row of several waves meet
         // at barriers.
         for (long base = it.first; base < it.end; base += kRows) {
-            const bool live = base + sub < it.end;
-            const long row = live ? base + sub : it.first;
-            const float4 st = reinterpret_cast<const float4*>(stats)[row];
-            Part g, t;
-            g.load_or(dy, row, D, lane, 0.0f);
+            const long row = base + sub;
+            const bool live = row < it.end;
+            const float4 st = stn;
+            if (a.gate && a.gate_rows) ga.load(a.gate, row, D, lane, live);
+            float g[kVals], t[kVals], n[kVals];
             if (a.w) {
-                Part w;
-                Part n;
-                n.load(y, row, D, lane);
-                t.load(dh, row, D, lane);
-                w.load(a.w, 0, D, lane);
+#pragma unroll
+                for (int e = 0; e < kVals; ++e) {
+                    n[e] = live && Raw::in(e, lane, D) ? (yn.get(e) - st.z) * st.w : 0.0f;
+                    t[e] = hn.get(e);
+                }
+            }
+            const Raw fr = fn;
+#pragma unroll
+            for (int e = 0; e < kVals; ++e) g[e] = gn.get(e);
+            load(row + kRows);
+            if (a.w) {
                 float m1 = 0.0f, m2 = 0.0f;
 #pragma unroll
-                for (int e = 0; e < Part::kVals; ++e) {
-                    n.v[e] = Part::in(e, lane, D) ? (n.v[e] - st.z) * st.w : 0.0f;
-                    if (live) {
-                        sb.v[e] += t.v[e];
-                        sw.v[e] = fmaf(t.v[e], n.v[e], sw.v[e]);
-                    }
-                    t.v[e] *= w.v[e];
-                    m1 += t.v[e];
-                    m2 = fmaf(t.v[e], n.v[e], m2);
+                for (int e = 0; e < kVals; ++e) {
+                    sb[e] += t[e];
+                    sw[e] = fmaf(t[e], n[e], sw[e]);
+                    t[e] *= w.get(e);
+                    m1 += t[e];
+                    m2 = fmaf(t[e], n[e], m2);
                 }
                 row_sums<LANES>(m1, m2, lds);
                 m1 = a.layer ? m1 * inv : 0.0f;
                 m2 *= inv;
 #pragma unroll
-                for (int e = 0; e < Part::kVals; ++e) g.v[e] = fmaf(st.w, t.v[e] - m1 - n.v[e] * m2, g.v[e]);
+                for (int e = 0; e < kVals; ++e) g[e] = fmaf(st.w, t[e] - m1 - n[e] * m2, g[e]);
             }
-            if (live) g.store(dx, row, D, lane);
-            // t: the unit rows of f (or f), then u
-            Part w, b;
-            t.load(f, row, D, lane);
-            if (a.post_w) {
-                w.load(a.post_w, 0, D, lane);
-                b.load_or(a.post_b, 0, D, lane, 0.0f);
+            if (live) Raw::store(g, dx, row, D, lane);
+            // t: the unit rows of f (or f)
 #pragma unroll
-                for (int e = 0; e < Part::kVals; ++e) t.v[e] = Part::in(e, lane, D) ? (t.v[e] - st.x) * st.y : 0.0f;
+            for (int e = 0; e < kVals; ++e) {
+                t[e] = fr.get(e);
+                if (a.post_w) t[e] = live && Raw::in(e, lane, D) ? (t[e] - st.x) * st.y : 0.0f;
             }
-            Part sc, ga;
-            sc.load_or(a.scale, 0, D, lane, 1.0f);
-            ga.load_or(a.gate, a.gate_rows ? row : it.image, D, lane, 1.0f);
             float n1 = 0.0f, n2 = 0.0f;
 #pragma unroll
-            for (int e = 0; e < Part::kVals; ++e) {
-                const float u = a.post_w ? fmaf(t.v[e], w.v[e], b.v[e]) : t.v[e];
-                const float gu = g.v[e] * u;
-                if (live) {
-                    ss.v[e] = fmaf(gu, ga.v[e], ss.v[e]);
-                    sg.v[e] = fmaf(gu, sc.v[e], sg.v[e]);
-                }
-                const float du = g.v[e] * (sc.v[e] * ga.v[e]);
-                if (a.gate_rows) ga.v[e] = gu * sc.v[e];
-                g.v[e] = du;
+            for (int e = 0; e < kVals; ++e) {
+                const float u = a.post_w ? fmaf(t[e], pw.get(e), pb.get(e)) : t[e];
+                const float scale = a.scale ? sc.get(e) : 1.0f, gate = a.gate ? ga.get(e) : 1.0f;
+                if (!live) g[e] = 0.0f;
+                const float gu = g[e] * u;
+                ss[e] = fmaf(gu, gate, ss[e]);
+                sg[e] = fmaf(gu, scale, sg[e]);
+                n[e] = gu * scale;
+                const float du = g[e] * (scale * gate);
+                g[e] = du;
                 if (a.post_w) {
-                    if (live) {
-                        spb.v[e] += du;
-                        spw.v[e] = fmaf(du, t.v[e], spw.v[e]);
-                    }
-                    g.v[e] = du * w.v[e];
-                    n1 += Part::in(e, lane, D) ? g.v[e] : 0.0f;
-                    n2 = fmaf(g.v[e], t.v[e], n2);
+                    spb[e] += du;
+                    spw[e] = fmaf(du, t[e], spw[e]);
+                    g[e] = du * pw.get(e);
+                    n1 += g[e];
+                    n2 = fmaf(g[e], t[e], n2);
                 }
             }
-            if (a.gate_rows && live) ga.store(dgate, row, D, lane);
+            if (a.gate_rows && live) Raw::store(n, dgate, row, D, lane);
             if (a.post_w) {
                 row_sums<LANES>(n1, n2, lds);
                 n1 = a.layer ? n1 * inv : 0.0f;
                 n2 *= inv;
 #pragma unroll
-                for (int e = 0; e < Part::kVals; ++e) g.v[e] = st.y * (g.v[e] - n1 - t.v[e] * n2);
+                for (int e = 0; e < kVals; ++e) g[e] = st.y * (g[e] - n1 - t[e] * n2);
             }
-            if (live) g.store(df, row, D, lane);
+            if (live) Raw::store(g, df, row, D, lane);
         }
-        if (gate_sums) store_sums<S, LANES, VPL>(sg.v, gate_sums, i, D, lane, sub, lds);
+        if (gate_sums) store_sums<S, LANES, VPL>(sg, gate_sums, i, D, lane, sub, lds);
     }
     const long G = gridDim.x, at = blockIdx.x;
     if (a.w) {
-        store_sums<S, LANES, VPL>(sw.v, sums, at, D, lane, sub, lds);
-        if (a.b) store_sums<S, LANES, VPL>(sb.v, sums, G + at, D, lane, sub, lds);
+        store_sums<S, LANES, VPL>(sw, sums, at, D, lane, sub, lds);
+        if (a.b) store_sums<S, LANES, VPL>(sb, sums, G + at, D, lane, sub, lds);
     }
-    if (a.scale) store_sums<S, LANES, VPL>(ss.v, sums, 2 * G + at, D, lane, sub, lds);
+    if (a.scale) store_sums<S, LANES, VPL>(ss, sums, 2 * G + at, D, lane, sub, lds);
     if (a.post_w) {
-        store_sums<S, LANES, VPL>(spw.v, sums, 3 * G + at, D, lane, sub, lds);
-        if (a.post_b) store_sums<S, LANES, VPL>(spb.v, sums, 4 * G + at, D, lane, sub, lds);
+        store_sums<S, LANES, VPL>(spw, sums, 3 * G + at, D, lane, sub, lds);
+        if (a.post_b) store_sums<S, LANES, VPL>(spb, sums, 4 * G + at, D, lane, sub, lds);
     }
 }
 
@@ -387,16 +424,19 @@ int chunk_count(const NormCall& a, int groups, int rows)
     return (int)std::max(1L, std::min(((long)groups + a.B - 1) / a.B, (per + rows - 1) / rows));
 }
 
-// Lanes a row: each lane holds at most 16 values of it (two vectors of bfloat16, four of float32).
+// Lanes a row: two vectors of 16 bytes a lane (four in the widest float32 rows), for registers that
+// leave two waves a SIMD in the backward kernel.
 template <class S, class F>
 hipError_t with_lanes(int D, F&& go)
 {
-    constexpr int V = S::kBytes == 2 ? 2 : 4;
     const int vpr = D * S::kBytes / 16;
-    if (vpr <= 32 * V) return go(std::integral_constant<int, 32>{}, std::integral_constant<int, V>{});
-    if (vpr <= 64 * V) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, V>{});
-    if (vpr <= 256 * V) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, V>{});
-    return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, V>{});
+    constexpr std::integral_constant<int, 2> two{};
+    if (vpr <= 64) return go(std::integral_constant<int, 32>{}, two);
+    if (vpr <= 128) return go(std::integral_constant<int, 64>{}, two);
+    if (vpr <= 256) return go(std::integral_constant<int, 128>{}, two);
+    if (vpr <= 512) return go(std::integral_constant<int, 256>{}, two);
+    if (vpr <= 2048) return go(std::integral_constant<int, 1024>{}, two);
+    return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, S::kBytes>{});
 }
 
 template <class S>
