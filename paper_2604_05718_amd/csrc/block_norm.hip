@@ -4,6 +4,7 @@
 // and the gradients of all of it. Bound by memory: forward reads x and f and writes y and h,
 // backward reads dy, dh, y and f and writes dx and df; everything between stays in registers.
 #include <algorithm>
+#include <type_traits>
 
 #include "mpm_device.h"
 #include "mpm_launch.h"
@@ -15,6 +16,8 @@ constexpr int kMinThreads = 256;
 // Workgroups of the column sums: enough to fill the chip, few enough that their partial sums
 // (a few rows of D floats each) are small beside the rows.
 constexpr int kSumGroups = 512;
+// Workgroups of the forward kernel: a few rows for each row group, so that loads run ahead.
+constexpr int kForwardGroups = 2048;
 constexpr int kSums = 5;  // dw, db, dscale, dpost_w, dpost_b (a gate's sums are by image)
 
 template <class S>
@@ -99,17 +102,34 @@ struct RawPart {
     static constexpr int kVals = VPL * kPer;
     u32x4 v[VPL];
 
-    // (base null, or not live: zeros)
-    __device__ __forceinline__ void load(const void* base, long row, int D, int lane, bool live = true)
+    // A row's vectors. Lanes past the row's end read its last vector again (`in` tells them apart), so
+    // that loads are never behind a branch.
+    __device__ __forceinline__ void load(const void* base, long row, int D, int lane)
     {
+        const uint8_t* p = static_cast<const uint8_t*>(base) + row * D * S::kBytes;
+        const int last = D / kPer - 1;
+#pragma unroll
+        for (int u = 0; u < VPL; ++u) v[u] = load16(p + min(lane + u * LANES, last) * 16);
+    }
+    // A row of parameters: zeros past the row's end; `missing` where there is none.
+    __device__ __forceinline__ void param(const void* base, long row, int D, int lane, float missing)
+    {
+        const uint32_t word = S::kBytes == 2 ? f32_to_bf16_rne(missing) * 0x10001u : __float_as_uint(missing);
         const uint8_t* p = static_cast<const uint8_t*>(base) + row * D * S::kBytes;
 #pragma unroll
         for (int u = 0; u < VPL; ++u) {
             const int c = lane + u * LANES;
-            const u32x4 zero = {0, 0, 0, 0};
-            v[u] = zero;
-            if (base && live && c * kPer < D) v[u] = load16(p + c * 16);
+            const uint32_t fill = c * kPer < D ? word : 0;
+            const u32x4 none = {fill, fill, fill, fill};
+            v[u] = none;
+            if (base && c * kPer < D) v[u] = load16(p + c * 16);
         }
+    }
+    __device__ __forceinline__ void clear()
+    {
+        const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < VPL; ++u) v[u] = zero;
     }
     __device__ __forceinline__ float get(int e) const
     {
@@ -170,9 +190,12 @@ __device__ __forceinline__ void row_stats(const float (&x)[RawPart<S, LANES, VPL
     rstd = 1.0f / sqrtf(sq / (float)D + eps);
 }
 
+// What a kernel is compiled for: a norm after the block, a norm before the next one.
+// Parameters that are not given are ones (scale, gate) or zeros (shifts).
+//
 // Forward: a row group of LANES lanes takes every kRows-th row of the workgroup's, the next row's x and
 // f on their way while one is computed; the parameters stay in registers.
-template <class S, int LANES, int VPL>
+template <class S, int LANES, int VPL, bool POST, bool PRE>
 __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, const void* __restrict__ x,
                                                                const void* __restrict__ f, void* __restrict__ y,
                                                                void* __restrict__ hout, float* __restrict__ stats)
@@ -184,47 +207,42 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, cons
     const Item it = item_rows(a, blockIdx.x);
     if (it.first >= it.end) return;
     Raw fn, xn, pw, pb, sc, ga, w, b;
-    const bool one = it.first + sub < it.end;
-    fn.load(f, it.first + sub, D, lane, one);
-    xn.load(x, it.first + sub, D, lane, one);
-    pw.load(a.post_w, 0, D, lane);
-    pb.load(a.post_b, 0, D, lane);
-    sc.load(a.scale, 0, D, lane);
-    if (a.gate && !a.gate_rows) ga.load(a.gate, it.image, D, lane);
-    w.load(a.w, 0, D, lane);
-    b.load(a.b, 0, D, lane);
+    fn.load(f, min(it.first + sub, it.end - 1), D, lane);
+    xn.load(x, min(it.first + sub, it.end - 1), D, lane);
+    if (POST) {
+        pw.param(a.post_w, 0, D, lane, 0.0f);
+        pb.param(a.post_b, 0, D, lane, 0.0f);
+    }
+    sc.param(a.scale, 0, D, lane, 1.0f);
+    ga.param(a.gate_rows ? nullptr : a.gate, it.image, D, lane, 1.0f);
+    if (PRE) {
+        w.param(a.w, 0, D, lane, 0.0f);
+        b.param(a.b, 0, D, lane, 0.0f);
+    }
     for (long base = it.first; base < it.end; base += kRows) {
-        const long row = base + sub;
-        const bool live = row < it.end;
+        const long row = min(base + sub, it.end - 1);
+        const bool live = base + sub < it.end;
         float u[kVals], r[kVals];
 #pragma unroll
         for (int e = 0; e < kVals; ++e) {
             u[e] = fn.get(e);
             r[e] = xn.get(e);
         }
-        if (a.gate && a.gate_rows) ga.load(a.gate, live ? row : it.first, D, lane);
-        const bool next = row + kRows < it.end;
-        fn.load(f, row + kRows, D, lane, next);
-        xn.load(x, row + kRows, D, lane, next);
+        if (a.gate_rows) ga.load(a.gate, row, D, lane);
+        const long next = min(base + sub + kRows, it.end - 1);
+        fn.load(f, next, D, lane);
+        xn.load(x, next, D, lane);
         float pmean = 0.0f, prstd = 1.0f;
-        if (a.post_w) {
+        if (POST) {
             row_stats<S, LANES, VPL>(u, D, lane, a.layer, a.eps, lds, pmean, prstd);
 #pragma unroll
             for (int e = 0; e < kVals; ++e) u[e] = fmaf((u[e] - pmean) * prstd, pw.get(e), pb.get(e));
         }
-        if (a.scale) {
 #pragma unroll
-            for (int e = 0; e < kVals; ++e) u[e] *= sc.get(e);
-        }
-        if (a.gate) {
-#pragma unroll
-            for (int e = 0; e < kVals; ++e) u[e] *= ga.get(e);
-        }
-#pragma unroll
-        for (int e = 0; e < kVals; ++e) r[e] += u[e];
+        for (int e = 0; e < kVals; ++e) r[e] = fmaf(u[e] * sc.get(e), ga.get(e), r[e]);
         if (live) Raw::store(r, y, row, D, lane);
         float mean = 0.0f, rstd = 1.0f;
-        if (a.w) {
+        if (PRE) {
             // Of the sum before its rounding to y's type, which only the stored y has.
             row_stats<S, LANES, VPL>(r, D, lane, a.layer, a.eps, lds, mean, rstd);
 #pragma unroll
@@ -264,7 +282,7 @@ __device__ __forceinline__ void store_sums(const float* v, float* out, long slot
 
 // dx and df of every row, and the workgroup's column sums: sums[k][group][D] (kSums of them) and, for
 // a gate by image, gate_sums[item][D]. Rows and parameters as in the forward kernel.
-template <class S, int LANES, int VPL>
+template <class S, int LANES, int VPL, bool POST, bool PRE>
 __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     NormCall a, const void* __restrict__ dy, const void* __restrict__ dh, const void* __restrict__ y,
     const void* __restrict__ f, const float* __restrict__ stats, void* __restrict__ dx, void* __restrict__ df,
@@ -274,116 +292,120 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     constexpr int kRows = threads<LANES>() / LANES, kVals = Raw::kVals;
     __shared__ float lds[threads<LANES>()];
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, D = a.D;
-    const float inv = 1.0f / (float)D;
+    const float inv = 1.0f / (float)D, centred = a.layer ? inv : 0.0f;
     float sw[kVals], sb[kVals], ss[kVals], spw[kVals], spb[kVals];
 #pragma unroll
     for (int e = 0; e < kVals; ++e) sw[e] = sb[e] = ss[e] = spw[e] = spb[e] = 0.0f;
     Raw w, pw, pb, sc, ga;
-    w.load(a.w, 0, D, lane);
-    pw.load(a.post_w, 0, D, lane);
-    pb.load(a.post_b, 0, D, lane);
-    sc.load(a.scale, 0, D, lane);
+    if (PRE) w.param(a.w, 0, D, lane, 0.0f);
+    if (POST) {
+        pw.param(a.post_w, 0, D, lane, 0.0f);
+        pb.param(a.post_b, 0, D, lane, 0.0f);
+    }
+    sc.param(a.scale, 0, D, lane, 1.0f);
     for (long i = blockIdx.x; i < items; i += gridDim.x) {
         const Item it = item_rows(a, i);
         float sg[kVals];
 #pragma unroll
         for (int e = 0; e < kVals; ++e) sg[e] = 0.0f;
-        if (a.gate && !a.gate_rows) ga.load(a.gate, it.image, D, lane);
+        ga.param(a.gate_rows ? nullptr : a.gate, it.image, D, lane, 1.0f);
         Raw yn, hn, gn, fn;
-        float4 stn = make_float4(0, 0, 0, 0);
-        // (rows past the end: zeros, which add nothing to the sums)
-        auto load = [&](long row) {
-            const bool live = row < it.end;
-            gn.load(dy, row, D, lane, live);
-            if (a.w) {
-                yn.load(y, row, D, lane, live);
-                hn.load(dh, row, D, lane, live);
+        float4 stn;
+        auto load = [&](long at) {
+            const long row = min(at, it.end - 1);
+            if (dy) gn.load(dy, row, D, lane);
+            if (PRE) {
+                yn.load(y, row, D, lane);
+                hn.load(dh, row, D, lane);
             }
-            fn.load(f, row, D, lane, live);
-            if (live) stn = reinterpret_cast<const float4*>(stats)[row];
+            fn.load(f, row, D, lane);
+            stn = reinterpret_cast<const float4*>(stats)[row];
         };
+        if (!dy) gn.clear();
         if (it.first < it.end) load(it.first + sub);
         // Every row group takes the same number of turns: the sums of a row of several waves meet
         // at barriers.
         for (long base = it.first; base < it.end; base += kRows) {
-            const long row = base + sub;
-            const bool live = row < it.end;
+            const bool live = base + sub < it.end;
+            const long row = live ? base + sub : it.end - 1;
+            if (!live) {  // a row past the end adds nothing to the sums
+                gn.clear();
+                hn.clear();
+            }
             const float4 st = stn;
-            if (a.gate && a.gate_rows) ga.load(a.gate, row, D, lane, live);
+            if (a.gate_rows) ga.load(a.gate, row, D, lane);
             float g[kVals], t[kVals], n[kVals];
-            if (a.w) {
+            if (PRE) {
 #pragma unroll
                 for (int e = 0; e < kVals; ++e) {
-                    n[e] = live && Raw::in(e, lane, D) ? (yn.get(e) - st.z) * st.w : 0.0f;
+                    n[e] = (yn.get(e) - st.z) * st.w;
                     t[e] = hn.get(e);
                 }
             }
             const Raw fr = fn;
 #pragma unroll
             for (int e = 0; e < kVals; ++e) g[e] = gn.get(e);
-            load(row + kRows);
-            if (a.w) {
+            load(base + sub + kRows);
+            if (PRE) {
                 float m1 = 0.0f, m2 = 0.0f;
 #pragma unroll
                 for (int e = 0; e < kVals; ++e) {
                     sb[e] += t[e];
                     sw[e] = fmaf(t[e], n[e], sw[e]);
-                    t[e] *= w.get(e);
+                    t[e] *= w.get(e);  // zero past the row's end
                     m1 += t[e];
                     m2 = fmaf(t[e], n[e], m2);
                 }
                 row_sums<LANES>(m1, m2, lds);
-                m1 = a.layer ? m1 * inv : 0.0f;
-                m2 *= inv;
+                m1 *= -st.w * centred;
+                m2 *= -st.w * inv;
 #pragma unroll
-                for (int e = 0; e < kVals; ++e) g[e] = fmaf(st.w, t[e] - m1 - n[e] * m2, g[e]);
+                for (int e = 0; e < kVals; ++e) g[e] += fmaf(st.w, t[e], fmaf(n[e], m2, m1));
             }
             if (live) Raw::store(g, dx, row, D, lane);
             // t: the unit rows of f (or f)
 #pragma unroll
-            for (int e = 0; e < kVals; ++e) {
-                t[e] = fr.get(e);
-                if (a.post_w) t[e] = live && Raw::in(e, lane, D) ? (t[e] - st.x) * st.y : 0.0f;
+            for (int e = 0; e < kVals; ++e) t[e] = POST ? (fr.get(e) - st.x) * st.y : fr.get(e);
+            if (!live) {
+#pragma unroll
+                for (int e = 0; e < kVals; ++e) g[e] = 0.0f;
             }
             float n1 = 0.0f, n2 = 0.0f;
 #pragma unroll
             for (int e = 0; e < kVals; ++e) {
-                const float u = a.post_w ? fmaf(t[e], pw.get(e), pb.get(e)) : t[e];
-                const float scale = a.scale ? sc.get(e) : 1.0f, gate = a.gate ? ga.get(e) : 1.0f;
-                if (!live) g[e] = 0.0f;
-                const float gu = g[e] * u;
-                ss[e] = fmaf(gu, gate, ss[e]);
-                sg[e] = fmaf(gu, scale, sg[e]);
-                n[e] = gu * scale;
-                const float du = g[e] * (scale * gate);
+                const float u = POST ? fmaf(t[e], pw.get(e), pb.get(e)) : t[e];
+                const float gu = g[e] * u, du = g[e] * (sc.get(e) * ga.get(e));
+                ss[e] = fmaf(gu, ga.get(e), ss[e]);
+                n[e] = gu * sc.get(e);
+                sg[e] += n[e];
                 g[e] = du;
-                if (a.post_w) {
+                if (POST) {
                     spb[e] += du;
                     spw[e] = fmaf(du, t[e], spw[e]);
-                    g[e] = du * pw.get(e);
+                    g[e] = du * pw.get(e);  // zero past the row's end
                     n1 += g[e];
                     n2 = fmaf(g[e], t[e], n2);
                 }
             }
             if (a.gate_rows && live) Raw::store(n, dgate, row, D, lane);
-            if (a.post_w) {
+            if (POST) {
                 row_sums<LANES>(n1, n2, lds);
-                n1 = a.layer ? n1 * inv : 0.0f;
-                n2 *= inv;
+                n1 *= -st.y * centred;
+                n2 *= -st.y * inv;
 #pragma unroll
-                for (int e = 0; e < kVals; ++e) g[e] = st.y * (g[e] - n1 - t[e] * n2);
+                for (int e = 0; e < kVals; ++e) g[e] = fmaf(st.y, g[e], fmaf(t[e], n2, n1));
             }
             if (live) Raw::store(g, df, row, D, lane);
         }
         if (gate_sums) store_sums<S, LANES, VPL>(sg, gate_sums, i, D, lane, sub, lds);
     }
     const long G = gridDim.x, at = blockIdx.x;
-    if (a.w) {
+    if (PRE) {
         store_sums<S, LANES, VPL>(sw, sums, at, D, lane, sub, lds);
         if (a.b) store_sums<S, LANES, VPL>(sb, sums, G + at, D, lane, sub, lds);
     }
     if (a.scale) store_sums<S, LANES, VPL>(ss, sums, 2 * G + at, D, lane, sub, lds);
-    if (a.post_w) {
+    if (POST) {
         store_sums<S, LANES, VPL>(spw, sums, 3 * G + at, D, lane, sub, lds);
         if (a.post_b) store_sums<S, LANES, VPL>(spb, sums, 4 * G + at, D, lane, sub, lds);
     }
@@ -393,26 +415,31 @@ struct SumOut {
     void* p[kSums];
 };
 
-// out[column] = the groups' sums in order: 16 threads a column take every 16th group, joined in order.
-// y > 0 of the grid in sums mode: which sum; in gate mode: which image (its `groups` slots).
-__global__ __launch_bounds__(1024) void join_sums_kernel(const float* __restrict__ parts, int groups, int D, int dt,
+// The column sums of all workgroups: 16 threads a column take every 16th part, joined in order. Rows
+// 0 ... kSums - 1 of the grid: the parameters' (`groups` parts each), further rows: the gates of the
+// images (`chunks` parts each).
+__global__ __launch_bounds__(1024) void join_sums_kernel(const float* __restrict__ sums, int groups,
+                                                         const float* __restrict__ gate_sums, int chunks, int D, int dt,
                                                          SumOut out, void* __restrict__ gate)
 {
     constexpr int kCols = 64, kWays = 16;
     __shared__ float lds[kWays][kCols];
     const int col = blockIdx.x * kCols + threadIdx.x % kCols, way = threadIdx.x / kCols;
-    const long k = blockIdx.y;
-    void* dst = gate ? gate : out.p[k];
+    const bool param = blockIdx.y < kSums;
+    const long k = param ? blockIdx.y : blockIdx.y - kSums;
+    void* dst = param ? out.p[k] : gate;
     if (dst == nullptr) return;
+    const int parts = param ? groups : chunks;
+    const float* from = (param ? sums : gate_sums) + k * parts * D + min(col, D - 1);
     float s = 0.0f;
-    if (col < D)
-        for (int g = way; g < groups; g += kWays) s += parts[(k * groups + g) * D + col];
+#pragma unroll 8
+    for (int g = way; g < parts; g += kWays) s += from[(long)g * D];
     lds[way][threadIdx.x % kCols] = s;
     __syncthreads();
     if (way != 0 || col >= D) return;
 #pragma unroll
     for (int w = 1; w < kWays; ++w) s += lds[w][threadIdx.x];
-    const long at = gate ? k * D + col : col;
+    const long at = param ? col : k * D + col;
     if (dt == kBf16) reinterpret_cast<uint16_t*>(dst)[at] = (uint16_t)f32_to_bf16_rne(s);
     else reinterpret_cast<float*>(dst)[at] = s;
 }
@@ -439,15 +466,26 @@ hipError_t with_lanes(int D, F&& go)
     return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, S::kBytes>{});
 }
 
+// ... and the norms that are given.
+template <class F>
+hipError_t with_norms(const NormCall& a, F&& go)
+{
+    if (a.post_w) return a.w ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+    return a.w ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
+}
+
 template <class S>
 hipError_t forward(NormCall a, const void* x, const void* f, void* y, void* h, float* stats, hipStream_t st)
 {
     return with_lanes<S>(a.D, [&](auto lanes, auto vpl) {
-        constexpr int L = decltype(lanes)::value, V = decltype(vpl)::value;
-        a.chunks = chunk_count(a, 4 * kSumGroups, threads<L>() / L);
-        hipLaunchKernelGGL((norm_kernel<S, L, V>), dim3((unsigned)((long)a.B * a.chunks)), dim3(threads<L>()), 0, st, a,
-                           x, f, y, h, stats);
-        return hipGetLastError();
+        return with_norms(a, [&](auto post, auto pre) {
+            constexpr int L = decltype(lanes)::value, V = decltype(vpl)::value;
+            constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value;
+            a.chunks = chunk_count(a, kForwardGroups, threads<L>() / L);
+            hipLaunchKernelGGL((norm_kernel<S, L, V, POST, PRE>), dim3((unsigned)((long)a.B * a.chunks)),
+                               dim3(threads<L>()), 0, st, a, x, f, y, h, stats);
+            return hipGetLastError();
+        });
     });
 }
 
@@ -462,25 +500,22 @@ hipError_t backward(NormCall a, const void* dy, const void* dh, const void* y, c
     const long items = (long)a.B * a.chunks, groups = backward_groups(a);
     const bool by_image = g.dgate && !a.gate_rows;
     hipError_t e = with_lanes<S>(a.D, [&](auto lanes, auto vpl) {
-        constexpr int L = decltype(lanes)::value, V = decltype(vpl)::value;
-        hipLaunchKernelGGL((norm_backward_kernel<S, L, V>), dim3((unsigned)groups), dim3(threads<L>()), 0, st, a, dy, dh,
-                           y, f, stats, g.dx, g.df, g.dgate, sums, by_image ? gate_sums : nullptr, items);
-        return hipGetLastError();
+        return with_norms(a, [&](auto post, auto pre) {
+            constexpr int L = decltype(lanes)::value, V = decltype(vpl)::value;
+            constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value;
+            hipLaunchKernelGGL((norm_backward_kernel<S, L, V, POST, PRE>), dim3((unsigned)groups), dim3(threads<L>()), 0,
+                               st, a, dy, dh, y, f, stats, g.dx, g.df, g.dgate, sums, by_image ? gate_sums : nullptr,
+                               items);
+            return hipGetLastError();
+        });
     });
     if (e != hipSuccess) return e;
-    const unsigned cols = (unsigned)((a.D + 63) / 64);
     const SumOut out{{g.dw, g.db, g.dscale, g.dpost_w, g.dpost_b}};
-    if (g.dw || g.db || g.dscale || g.dpost_w || g.dpost_b) {
-        hipLaunchKernelGGL(join_sums_kernel, dim3(cols, kSums), dim3(1024), 0, st, sums, (int)groups, a.D, a.dt, out,
-                           (void*)nullptr);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (by_image) {
-        hipLaunchKernelGGL(join_sums_kernel, dim3(cols, (unsigned)a.B), dim3(1024), 0, st, gate_sums, a.chunks, a.D,
-                           a.dt, SumOut{}, g.dgate);
-        e = hipGetLastError();
-    }
-    return e;
+    if (!by_image && !g.dw && !g.dscale && !g.dpost_w) return e;
+    hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.D + 63) / 64), (unsigned)(kSums + (by_image ? a.B : 0))),
+                       dim3(1024), 0, st, sums, (int)groups, gate_sums, a.chunks, a.D, a.dt, out,
+                       by_image ? g.dgate : nullptr);
+    return hipGetLastError();
 }
 
 size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
