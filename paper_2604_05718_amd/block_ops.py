@@ -19,9 +19,10 @@ from dataclasses import dataclass
 import torch
 
 from . import _lib
-from .api import _DTYPES, _dt, _stream
+from .api import _dt
 
 _BYREF = ctypes.byref
+_raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle, without its Python object
 _NORMS = {"layer": _lib.MPM_NORM_LAYER, "rms": _lib.MPM_NORM_RMS}
 
 
@@ -29,15 +30,16 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _void(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+def _stream(t):
+    """The current stream of a tensor's device."""
+    return _raw_stream(t.get_device())
 
 
 def _device(t, what, dtype, ref, numel=None):
     """Checks an optional contiguous device tensor; returns its address or None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != ref.device or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != ref.get_device() or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor on {ref.device}")
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{what} has {t.numel()} entries, expected {numel}")
@@ -46,17 +48,20 @@ def _device(t, what, dtype, ref, numel=None):
 
 def _heads(t, what, ref, rows=None, heads=None):
     """The mpm_heads of rows of heads [R, H, dh] or [B, N, H, dh]."""
-    if not t.is_cuda or t.device != ref.device:
+    if t.get_device() != ref.get_device():
         raise ValueError(f"{what} must be on the GPU, on {ref.device}")
-    if t.dtype != ref.dtype:
+    if t.dtype is not ref.dtype:
         raise TypeError(f"{what} must be {ref.dtype}, got {t.dtype}")
     st, sh = t.stride(), t.shape
-    if len(sh) not in (3, 4) or (sh[-1] > 1 and st[-1] != 1):
+    dims, dh = len(sh), sh[-1]
+    if (dims != 3 and dims != 4) or (st[-1] != 1 and dh > 1):
         raise ValueError(f"{what} must be [R, H, dh] or [B, N, H, dh] with contiguous channels")
-    if len(sh) == 4 and sh[0] > 1 and sh[1] > 0 and st[0] != sh[1] * st[1]:
-        raise ValueError(f"{what}: dense images must follow each other at the rows' stride")
-    n = sh[0] if len(sh) == 3 else sh[0] * sh[1]
-    if (rows is not None and n != rows) or sh[-1] != ref.shape[-1] or (heads is not None and sh[-2] != heads):
+    n = sh[0]
+    if dims == 4:
+        if n > 1 and sh[1] > 0 and st[0] != sh[1] * st[1]:
+            raise ValueError(f"{what}: dense images must follow each other at the rows' stride")
+        n *= sh[1]
+    if (rows is not None and n != rows) or dh != ref.shape[-1] or (heads is not None and sh[-2] != heads):
         raise ValueError(f"{what} has shape {tuple(sh)}, expected {rows} rows of {heads} heads of {ref.shape[-1]}")
     return _lib.Heads(t.data_ptr(), st[-3], st[-2])
 
@@ -129,8 +134,8 @@ def bias_expand(table, lut, out=None):
     if out is None:
         out = torch.empty((H, W, W), dtype=torch.float32, device=table.device)
     _lib.check("mpm_bias_expand", _lib.load().mpm_bias_expand(
-        _void(table), _device(lut, "lut", torch.int32, table), nb, W // 2, H, _dt(table),
-        _device(out, "out", torch.float32, table, H * W * W), _stream()))
+        table.data_ptr(), _device(lut, "lut", torch.int32, table), nb, W // 2, H, _dt(table),
+        _device(out, "out", torch.float32, table, H * W * W), _stream(table)))
     return out
 
 
@@ -141,7 +146,7 @@ def bias_gradient(dbias, lut, nb: int, dtype=torch.float32, out=None):
         out = torch.empty((nb * nb, H), dtype=dtype, device=dbias.device)
     _lib.check("mpm_bias_gradient", _lib.load().mpm_bias_gradient(
         _device(dbias, "dbias", torch.float32, dbias, H * W * W), _device(lut, "lut", torch.int32, dbias), int(nb),
-        W // 2, H, _dt(out), _device(out, "out", out.dtype, dbias, nb * nb * H), _stream()))
+        W // 2, H, _dt(out), _device(out, "out", out.dtype, dbias, nb * nb * H), _stream(dbias)))
     return out
 
 
@@ -156,15 +161,15 @@ def attention(q, k, v, q_off=None, k_off=None, Nq=None, Nk=None, scale=None, bia
     (None: each row's index in its image). ``k_bias``: float32 per key row, -inf drops a key."""
     c, hq, hk, hv = _call(q, k, v, q_off, k_off, Nq, Nk, scale, bias, q_pos, k_pos, grid, k_bias)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     rows = _rows_of(q)
     ho = _heads(out, "out", q, rows, c.H)
     lse = torch.empty((rows, c.H, 2), dtype=torch.float32, device=q.device) if with_lse else None
     lib = _lib.load()
     need = lib.mpm_attention_workspace_bytes(_BYREF(c))
     ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
-    _lib.check("mpm_attention", lib.mpm_attention(_BYREF(c), _BYREF(hq), _BYREF(hk), _BYREF(hv), _BYREF(ho), _void(lse),
-                                                  _void(ws), need, _stream()))
+    _lib.check("mpm_attention", lib.mpm_attention(_BYREF(c), _BYREF(hq), _BYREF(hk), _BYREF(hv), _BYREF(ho), _ptr(lse),
+                                                  _ptr(ws), need, _stream(q)))
     return (out, lse) if with_lse else out
 
 
@@ -194,7 +199,7 @@ def attention_backward(dout, q, k, v, out, lse, q_off=None, k_off=None, Nq=None,
     ws = torch.empty((need,), dtype=torch.uint8, device=q.device)
     _lib.check("mpm_attention_backward", lib.mpm_attention_backward(
         _BYREF(c), *(_BYREF(x) for x in hs), _device(lse, "lse", torch.float32, q, 2 * rq * c.H), *(_BYREF(x) for x in gs),
-        _void(dbias), _void(ws), need, _stream()))
+        _ptr(dbias), _ptr(ws), need, _stream(q)))
     return AttentionGrads(dq, dk, dv, dbias)
 
 
@@ -238,7 +243,7 @@ def residual_norm(x, f, weight=None, bias=None, post_weight=None, post_bias=None
     h = torch.empty_like(x) if weight is not None else None
     stats = torch.empty((x.shape[0], 4), dtype=torch.float32, device=x.device) if with_stats else None
     _lib.check("mpm_residual_norm", _lib.load().mpm_residual_norm(
-        _BYREF(c), _ptr(x), fp, _device(y, "out", x.dtype, x, x.numel()), _ptr(h), _ptr(stats), _stream()))
+        _BYREF(c), _ptr(x), fp, _device(y, "out", x.dtype, x, x.numel()), _ptr(h), _ptr(stats), _stream(x)))
     return (y, h, stats) if with_stats else (y, h)
 
 
@@ -271,5 +276,5 @@ def residual_norm_backward(dy, dh, y, f, stats, weight=None, bias=None, post_wei
     _lib.check("mpm_residual_norm_backward", lib.mpm_residual_norm_backward(
         _BYREF(c), _device(dy, "dy", y.dtype, y, n), _device(dh, "dh", y.dtype, y, n), _ptr(y),
         _device(f, "f", y.dtype, y, n), _device(stats, "stats", torch.float32, y, 4 * y.shape[0]), _BYREF(grads),
-        _ptr(ws), need, _stream()))
+        _ptr(ws), need, _stream(y)))
     return g
