@@ -103,9 +103,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         const bool live = qi < rq.count;
         load_frags<S, DH>(qf[i], q.p + ((rq.first + (live ? qi : 0)) * q.row + (long)hd * q.head) * S::kBytes, a.dh, live,
                           h);
-        qcode[i] = 0;
-        if (BIAS != kBiasNone)
-            qcode[i] = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0, a.grid_h, a.grid_w, a.span, W, table_at);
+        // (the position for now: the first loads are all under way before one is waited for)
+        qcode[i] = BIAS != kBiasNone && live ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0;
         m[i] = -__builtin_inff();
         sum[i] = 0.0f;
 #pragma unroll
@@ -117,6 +116,9 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     }
     if (BIAS != kBiasNone) {
         load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+            qcode[i] = query_code<BIAS>(qcode[i], a.grid_h, a.grid_w, a.span, W, table_at);
     }
     store(0);
     __syncthreads();

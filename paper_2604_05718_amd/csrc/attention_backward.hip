@@ -179,17 +179,14 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
     const bool start = can_start<S>(c);
     float kb = 0.0f;
     if (KB) kb = exists ? to_log2(a.k_bias[rk.first + ki]) : -__builtin_inff();
-    const bool live = exists && kb > -__builtin_inff();
     int kcode = 0;
+    const bool live = exists && kb > -__builtin_inff();
+    // (all of the first loads are under way before one is waited for)
+    int own = 0, next = 0;  // this key's position and the next one's
+    const bool pairs_next = hk == 0 && ki + 1 < rk.count;
     if (BIAS != kBiasNone) {
-        const int cells = a.grid_h * a.grid_w;
-        const int p = exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0;
-        kcode = bias_code<BIAS>(p, a.grid_h, a.grid_w, W);
-        if (hk == 0 && h == 0 && ki + 1 < rk.count) {
-            const int next = a.k_pos ? a.k_pos[rk.first + ki + 1] : ki + 1;
-            if (min(max(p, 0), cells - 1) >= min(max(next, 0), cells - 1))
-                __hip_atomic_fetch_or(w.repeats + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
+        own = exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0;
+        next = pairs_next ? (a.k_pos ? a.k_pos[rk.first + ki + 1] : ki + 1) : 0;
     }
 
     Frag kf[DH / 16], vf[DH / 16];
@@ -236,7 +233,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
         __syncthreads();
         stage.init(q, dout, rq.first, hd, t);
         load(0);
-        if (BIAS != kBiasNone) load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
+        if (BIAS != kBiasNone) {
+            load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
+            kcode = bias_code<BIAS>(own, a.grid_h, a.grid_w, W);
+        }
         store(0);
         __syncthreads();
         float most_ds = 0.0f, most_dp = 0.0f;
@@ -340,6 +340,11 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
         take(mine, gk, lane);
         take(mine + DH / 32 * 16 * kWave, gv, lane);
     }
+    if (BIAS != kBiasNone && pairs_next && h == 0) {
+        const int cells = a.grid_h * a.grid_w;
+        if (min(max(own, 0), cells - 1) >= min(max(next, 0), cells - 1))
+            __hip_atomic_fetch_or(w.repeats + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     // A dropped key's gradients are zero, whatever its rows hold.
     if (!live) {
 #pragma unroll
@@ -425,6 +430,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     };
     stage.init(k, v, rk.first, hk, t);
     load(0);
+    const int qpos = BIAS != kBiasNone && live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0;
+    Frag qf[DH / 16], of[DH / 16];
+    load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)hd * q.head) * S::kBytes, a.dh, live, h);
+    load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
 
     // The power of two that score gradients are multiplied by, by way of the probabilities.
     int lg = 0;
@@ -443,13 +452,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         s0[r] = apart ? 0.0f : tk.x;
         dp0[r] = nd;
     }
-    Frag qf[DH / 16], of[DH / 16];
-    load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)hd * q.head) * S::kBytes, a.dh, live, h);
-    load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
     int qcode = 0;
     if (BIAS != kBiasNone) {
-        qcode = query_code<BIAS, SIZE>(live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0, a.grid_h, a.grid_w, a.span, W, table_at);
         load_table<THREADS, SIZE / 4>(table, a.bias + (long)hd * W2, W2, t);
+        qcode = query_code<BIAS, SIZE>(qpos, a.grid_h, a.grid_w, a.span, W, table_at);
         if (SUM == kSum32)
             for (int e = t; e < W2; e += THREADS) reinterpret_cast<int32_t*>(table)[2 * e + 1] = 0;
         if (SUM == kSum64)

@@ -352,11 +352,11 @@ struct PairStage {
     }
 };
 
-// A head's bias table to LDS, in base 2, every STRIDE words: eight loads a thread in flight.
+// A head's bias table to LDS, in base 2, every STRIDE words: sixteen loads a thread in flight.
 template <int THREADS, int STRIDE = 1>
 __device__ __forceinline__ void load_table(float* table, const float* src, int n, int t)
 {
-    constexpr int kFlight = 8;
+    constexpr int kFlight = 16;
     for (int e0 = t; e0 < n; e0 += THREADS * kFlight) {
         float v[kFlight];
 #pragma unroll
