@@ -10,11 +10,10 @@
 namespace mpm {
 namespace {
 
-// Largest running maximum that the score products start from; past it their rounding would show.
-constexpr float kStartMost = 64.0f;
-// The running maximum is raised only when a tile's exceeds it by more than this many powers of
-// two: probabilities then stay below 256, exact to scale, and most tiles skip the rescaling.
-constexpr float kSlack = 8.0f;
+// What is taken from a query's scores (base 2) before the exponential need not be their maximum: floats
+// keep their precision at any scale. It is zero as long as the scores stay within this many powers of two
+// of it, so that most calls subtract nothing, and else follows the running maximum with that slack.
+constexpr float kSlack = 60.0f;
 
 template <class S, int SPLIT>
 constexpr int key_tile()
@@ -64,16 +63,13 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     const int part = t / kWave % SPLIT;
     const int W = 2 * a.span + 1;
     const float c = a.scale * kLog2e;
-    // The score products may start from -maximum / c, which takes the maximum off for nothing
-    // (bfloat16: the sum's rounding is far below the operands' own).
-    const bool can_start = kBf && fabsf(c) > 1e-3f && fabsf(c) < 1e3f;
 
     Staged stage;
     int pos = 0;
     float kbias = 0.0f;
     const float* drop = KB ? a.k_bias + rk.first : nullptr;
     auto load = [&](int k0) {
-        stage.template load<KB>(k, v, a.dh, rk.count, drop, k0, t);
+        stage.template load<KB>(a.dh, rk.count, drop, k0, t);
         if (t < KT) {
             const int kk = k0 + t;
             const bool in = kk < rk.count;
@@ -90,13 +86,14 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
             if (KB) reinterpret_cast<float*>(codes + KT)[t] = to_log2(kbias);
         }
     };
-    stage.init(k, v, rk.first, hk, t);
+    stage.init(k, v, rk.first, hk, a.dh, t);
     load(0);
 
     Frag qf[QT][DH / 16];
     int qcode[QT];
-    f32x16 acc[QT][DH / 32], start[QT];
-    float m[QT], sum[QT];  // the maximum taken (-inf: no key yet) and the sum
+    f32x16 acc[QT][DH / 32];
+    float m[QT], sum[QT];  // what is taken from the scores, and the sum
+    bool fresh[QT];        // no key yet
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
         const int qi = q0 + (wave * QT + i) * 32 + l32;
@@ -105,14 +102,12 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                           h);
         // (the position for now: the first loads are all under way before one is waited for)
         qcode[i] = BIAS != kBiasNone && live ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0;
-        m[i] = -__builtin_inff();
-        sum[i] = 0.0f;
+        m[i] = sum[i] = 0.0f;
+        fresh[i] = true;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            start[i][r] = 0.0f;
+        for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
-            for (int d = 0; d < DH / 32; ++d) acc[i][d][r] = 0.0f;
-        }
+            for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
     }
     if (BIAS != kBiasNone) {
         load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
@@ -124,7 +119,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     __syncthreads();
 
     const bool works = q0 + wave * QT * 32 < rq.count;  // a wave past the image's end only brings tiles
-    bool apart = !can_start;  // whether the maximum is subtracted instead
+    bool shifted = false, any_fresh = true;  // whether a query of the wave has m != 0, or no key yet
     for (int k0 = 0, buf = 0; k0 < rk.count; k0 += KT, buf ^= 1) {
         const uint8_t* kt = lds + buf * kBuffer;
         const uint8_t* vt = kt + Staged::kTileBytes;
@@ -132,17 +127,17 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         const float* kbs = reinterpret_cast<const float*>(codes + KT);
         const bool more = k0 + KT < rk.count;
         if (more) load(k0 + KT);
-#pragma unroll 1
-        for (int u = works ? part : KT / 32; u < KT / 32; u += SPLIT) {
+        auto compute = [&](int u) {
             f32x16 s[QT];
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
                 if (!kBf && st > 0 && 16 * st >= a.dh) continue;  // (a float32 step is worth a branch)
                 const Frag kf = rows_frag<S, DH>(kt, 32 * u + l32, st, h);
+                const f32x16 zero = {};
 #pragma unroll
-                for (int i = 0; i < QT; ++i) s[i] = mma(kf, qf[i][st], st == 0 ? start[i] : s[i]);
+                for (int i = 0; i < QT; ++i) s[i] = mma(kf, qf[i][st], st == 0 ? zero : s[i]);
             }
-            bool any_up = false;
+            bool up_any = any_fresh;
             float top[QT];
 #pragma unroll
             for (int i = 0; i < QT; ++i) {
@@ -173,42 +168,44 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                     for (int r = 0; r < 16; ++r)
                         if (8 * (r / 4) + r % 4 >= left) s[i][r] = -__builtin_inff();
                 }
-                if (apart) {
-                    float base = m[i] == -__builtin_inff() ? 0.0f : m[i];
-                    asm volatile("" : "+v"(base));
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[i][r] -= base;
-                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top[i] = fmaxf(top[i], s[i][r]);
-                any_up |= top[i] >= (m[i] == -__builtin_inff() ? kLowest : kSlack);
+                up_any |= top[i] > m[i] + kSlack;
             }
-            if (__any(any_up)) {
-                bool far = false;
+            if (__any(up_any)) {
+                shifted = any_fresh = false;
 #pragma unroll
                 for (int i = 0; i < QT; ++i) {
                     const float full = halves_max(top[i]);
-                    const bool fresh = m[i] == -__builtin_inff();
-                    // What the maximum rises by (a first key: all of its score).
-                    const float up = fresh ? (full == -__builtin_inff() ? 0.0f : full) : fmaxf(full, 0.0f);
-                    if (!fresh) m[i] += up;
-                    else if (full > -__builtin_inff()) m[i] = up;
-                    const float f = fresh ? 0.0f : __builtin_amdgcn_exp2f(-up);
+                    float to = m[i];
+                    const bool first = fresh[i];
+                    if (first) {
+                        // A first key: zero does for scores that are neither large nor all very small.
+                        if (full > -__builtin_inff()) {
+                            to = fabsf(full) <= kSlack ? 0.0f : full;
+                            fresh[i] = false;
+                        }
+                    } else if (full > m[i] + kSlack) {
+                        to = full;
+                    }
+                    const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[i] - to);
+                    m[i] = to;
                     sum[i] *= f;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[i][r] -= up;
 #pragma unroll
                     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[i][d][r] *= f;
-                    far |= fabsf(m[i]) > kStartMost && m[i] > -__builtin_inff();
+                    shifted |= __any(to != 0.0f);
+                    any_fresh |= __any(fresh[i]);
                 }
-                apart = !can_start || __any(far);
+            }
+            if (shifted) {
 #pragma unroll
                 for (int i = 0; i < QT; ++i) {
-                    const float x = apart || m[i] == -__builtin_inff() ? 0.0f : -m[i] / c;
+                    float by = m[i];
+                    asm volatile("" : "+v"(by));  // keeps this a branch
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) start[i][r] = x;
+                    for (int r = 0; r < 16; ++r) s[i][r] -= by;
                 }
             }
 #pragma unroll
@@ -231,6 +228,18 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                     for (int i = 0; i < QT; ++i) acc[i][d] = mma(vf, p[i], acc[i][d]);
                 }
             }
+        };
+        if (works) {
+            if constexpr (SPLIT == 1) {
+                // Unrolled for constant LDS offsets; one tile's registers at a time.
+#pragma unroll
+                for (int u = 0; u < KT / 32; ++u) {
+                    compute(u);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                for (int u = part; u < KT / 32; u += SPLIT) compute(u);
+            }
         }
         if (more) store(buf ^ 1);
         __syncthreads();
@@ -242,7 +251,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         float2* stats = reinterpret_cast<float2*>(reinterpret_cast<float*>(lds) + WAVES / 2 * 32 * kPad) + wave * kWave + lane;
         static_assert((WAVES / 2 * 32 * kPad + WAVES / 2 * kWave * 2) * 4 <= 2 * kBuffer, "the joined outputs fit");
         if (part == 1) {
-            *stats = make_float2(m[0], sum[0]);
+            *stats = make_float2(fresh[0] ? -__builtin_inff() : m[0], sum[0]);
 #pragma unroll
             for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -253,8 +262,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         __syncthreads();
         if (part == 1) return;
         const float2 other = *stats;
-        const float top = fmaxf(m[0], other.x);
-        const float f = m[0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[0] - top);
+        const float own = fresh[0] ? -__builtin_inff() : m[0], top = fmaxf(own, other.x);
+        const float f = fresh[0] ? 0.0f : __builtin_amdgcn_exp2f(own - top);
         const float o = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(other.x - top);
         m[0] = top;
         sum[0] = f * sum[0] + o * other.y;

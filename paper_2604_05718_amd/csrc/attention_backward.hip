@@ -206,7 +206,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
     float del = 0.0f;
     for (int hd = hk * group; hd < (hk + 1) * group; ++hd) {
         auto load = [&](int q0) {
-            stage.template load<false>(q, dout, a.dh, rq.count, nullptr, q0, t);
+            stage.template load<false>(a.dh, rq.count, nullptr, q0, t);
             if (t < QT) {
                 const int qi = q0 + t;
                 const bool in = qi < rq.count;
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
             }
         };
         __syncthreads();
-        stage.init(q, dout, rq.first, hd, t);
+        stage.init(q, dout, rq.first, hd, a.dh, t);
         load(0);
         if (BIAS != kBiasNone) {
             load_table<THREADS>(table, a.bias + (long)hd * W * W, W * W, t);
@@ -248,8 +248,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
             const bool more = q0 + QT < rq.count;
             if (more) load(q0 + QT);
             const bool apart = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int*>(first + 3 * QT)[0]);
-#pragma unroll 1
-            for (int u = works ? share : QT / 32; u < QT / 32; u += SPLIT) {
+            auto compute = [&](int u) {
                 f32x16 s, dp;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -308,6 +307,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
                         gk[d] = mma(cols_frag<S, DH>(qt, 32 * u + 16 * st, 32 * d, lane), ds, gk[d]);
                     }
                 }
+            };
+            if (works) {
+#pragma unroll 1
+                for (int u = share; u < QT / 32; u += SPLIT) compute(u);
             }
             if (BUFS == 1) __syncthreads();
             if (more) store(buf ^ (BUFS - 1));
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     float kbias = 0.0f;
     const float* drop = KB ? a.k_bias + rk.first : nullptr;
     auto load = [&](int k0) {
-        stage.template load<KB>(k, v, a.dh, rk.count, drop, k0, t);
+        stage.template load<KB>(a.dh, rk.count, drop, k0, t);
         if (t < KT) {
             const int kk = k0 + t;
             const bool in = kk < rk.count;
@@ -428,7 +431,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
             if (KB) reinterpret_cast<float*>(codes + KT)[t] = to_log2(kbias);
         }
     };
-    stage.init(k, v, rk.first, hk, t);
+    stage.init(k, v, rk.first, hk, a.dh, t);
     load(0);
     const int qpos = BIAS != kBiasNone && live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0;
     Frag qf[DH / 16], of[DH / 16];
@@ -478,8 +481,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         const float* kbs = reinterpret_cast<const float*>(codes + KT);
         const bool more = k0 + KT < rk.count;
         if (more) load(k0 + KT);
-#pragma unroll 1
-        for (int u = works || SUM == kSumTurns ? share : KT / 32; u < KT / 32; u += SPLIT) {
+        auto compute = [&](int u) {
             f32x16 s, dp;
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
@@ -557,6 +559,18 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                     }
                     __syncthreads();
                 }
+            }
+        };
+        if (works || SUM == kSumTurns) {  // (turns have barriers)
+            if constexpr (SPLIT == 1) {
+                // Unrolled for constant LDS offsets; one tile's registers at a time.
+#pragma unroll
+                for (int u = 0; u < KT / 32; ++u) {
+                    compute(u);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                for (int u = share; u < KT / 32; u += SPLIT) compute(u);
             }
         }
         if (BUFS == 1) __syncthreads();

@@ -252,7 +252,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionCall 
     if (column >= (long)a.B * a.Hk * cols) return;
     const int pair = (int)(column / cols), col = (int)(column % cols), b = pair / a.Hk;
     const int q_i = col % a.Nq, head = (pair - b * a.Hk) * group + col / a.Nq;
-    const Rows rq = image_rows(a.q_off, b, a.Nq);
+    const Rows rq = lane_rows(a.q_off, b, a.Nq);
     if (q_i >= rq.count) return;
     const float* part = parts + ((long)pair * splits * cols + col) * part_floats<DH>();
     const long step = (long)cols * part_floats<DH>();

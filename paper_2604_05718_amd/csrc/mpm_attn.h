@@ -202,12 +202,20 @@ __device__ __forceinline__ void store_rows(uint8_t* row, const f32x16 (&x)[D], f
         }
 }
 
-// Row range of image b: packed offsets or N rows each, its count held to [0, N].
+// Row range of image b (the same in all lanes of a wave): packed offsets or N rows each, its count held to [0, N].
 struct Rows {
     long first;
     int count;
 };
 __device__ __forceinline__ Rows image_rows(const int32_t* off, int b, int N)
+{
+    if (off == nullptr) return Rows{(long)b * N, N};
+    // (the same for every lane: kept in scalar registers)
+    const int o = __builtin_amdgcn_readfirstlane(off[b]), e = __builtin_amdgcn_readfirstlane(off[b + 1]);
+    return Rows{(long)o, min(max(e - o, 0), N)};
+}
+// ... of images that differ between lanes.
+__device__ __forceinline__ Rows lane_rows(const int32_t* off, int b, int N)
 {
     if (off == nullptr) return Rows{(long)b * N, N};
     const int o = off[b];
@@ -291,7 +299,8 @@ inline long block_grid(long pairs, int blocks)
     return (pairs >= 4 * kXcds ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * blocks;
 }
 
-// Tiles of ROWS rows of two operands on their way to LDS: loaded to registers a tile ahead.
+// Tiles of ROWS rows of two operands on their way to LDS: loaded to registers a tile ahead. A whole
+// tile's loads take a scalar address and an offset of the thread's own, the same for every tile.
 template <class S, int DH, int ROWS, int THREADS>
 struct PairStage {
     typedef Tile<S, DH> T;
@@ -299,41 +308,54 @@ struct PairStage {
     static constexpr int kPer = ROWS * T::kChunks / THREADS;
     static_assert(ROWS * T::kChunks % THREADS == 0 && THREADS >= ROWS, "whole chunks a thread");
     u32x4 x[kPer], y[kPer];
-    const uint8_t *xp[kPer], *yp[kPer];  // this thread's chunks of the next tile
     float dropped[kPer];
+    const uint8_t *xb, *yb;  // the first row
+    long xs, ys;             // bytes from row to row
+    uint32_t xo[kPer], yo[kPer];
+    bool narrow;  // offsets inside a tile fit 32 bits, rows are whole
 
-    __device__ __forceinline__ void init(const HeadRows& xr, const HeadRows& yr, long first, int head, int t)
+    __device__ __forceinline__ void init(const HeadRows& xr, const HeadRows& yr, long first, int head, int dh, int t)
     {
+        xs = xr.row * S::kBytes;
+        ys = yr.row * S::kBytes;
+        xb = xr.p + first * xs + (long)head * xr.head * S::kBytes;
+        yb = yr.p + first * ys + (long)head * yr.head * S::kBytes;
+        constexpr long kMost = (1L << 31) / ROWS;
+        narrow = dh == DH && xs < kMost && ys < kMost;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int e = t + i * THREADS, ch = e % T::kChunks;
-            const long row = first + e / T::kChunks;
-            xp[i] = xr.p + (row * xr.row + (long)head * xr.head) * S::kBytes + ch * 16;
-            yp[i] = yr.p + (row * yr.row + (long)head * yr.head) * S::kBytes + ch * 16;
+            const int e = t + i * THREADS;
+            xo[i] = (uint32_t)(e / T::kChunks) * (uint32_t)xs + e % T::kChunks * 16;
+            yo[i] = (uint32_t)(e / T::kChunks) * (uint32_t)ys + e % T::kChunks * 16;
         }
     }
-    // Loads rows r0 ... of `count` and moves on; zeros past the last row and past a row's end. Rows
-    // dropped by drop[row] = -inf are stored as zeros, whatever they hold (loaded all the same: a
-    // load that waits for its drop value would take twice the latency).
+    // Loads rows r0 ... of `count`; zeros past the last row and past a row's end. Rows dropped by
+    // drop[row] = -inf are stored as zeros, whatever they hold (loaded all the same: a load that
+    // waits for its drop value would take twice the latency).
     template <bool DROP>
-    __device__ __forceinline__ void load(const HeadRows& xr, const HeadRows& yr, int dh, int count, const float* drop,
-                                         int r0, int t)
+    __device__ __forceinline__ void load(int dh, int count, const float* drop, int r0, int t)
     {
-        const long xstep = (long)ROWS * xr.row * S::kBytes, ystep = (long)ROWS * yr.row * S::kBytes;
+        const uint8_t *xt = xb + r0 * xs, *yt = yb + r0 * ys;
+        if (narrow && r0 + ROWS <= count) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                x[i] = load16(xt + xo[i]);
+                y[i] = load16(yt + yo[i]);
+                if (DROP) dropped[i] = drop[r0 + (t + i * THREADS) / T::kChunks];
+            }
+            return;
+        }
         const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int e = t + i * THREADS, ch = e % T::kChunks, r = r0 + e / T::kChunks;
-            bool in = ch * (16 / S::kBytes) < dh && r < count;
+            const int e = t + i * THREADS, ch = e % T::kChunks, r = e / T::kChunks;
             x[i] = y[i] = zero;
             if (DROP) dropped[i] = 0.0f;
-            if (in) {
-                if (DROP) dropped[i] = drop[r];
-                x[i] = load16(xp[i]);
-                y[i] = load16(yp[i]);
+            if (ch * (16 / S::kBytes) < dh && r0 + r < count) {
+                if (DROP) dropped[i] = drop[r0 + r];
+                x[i] = load16(xt + r * xs + ch * 16);
+                y[i] = load16(yt + r * ys + ch * 16);
             }
-            xp[i] += xstep;
-            yp[i] += ystep;
         }
     }
     template <bool DROP>

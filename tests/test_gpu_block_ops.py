@@ -232,6 +232,46 @@ def test_dropped_keys_are_not_read(dtype, lowest):
     assert torch.all(g.dk.cpu()[drop] == 0) and torch.all(g.dv.cpu()[drop] == 0)
 
 
+@pytest.mark.parametrize("low", [torch.finfo(F32).min, -1e9, -1e4, -200.0])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_masks_before_real_keys(dtype, low):
+    """Finite mask values on the first keys, several tiles of them, and none on later ones: only the later
+    keys count, in the few-query form too (the masked weights are below 2^-100)."""
+    c = Case(dtype, [150, 40, 3], [400, 90, 700], 2, 2, 64, (30, 30), 29, "sorted", True, seed=9)
+    c.k_bias = torch.zeros(1190)
+    for a, b in ((0, 300), (400, 489), (490, 1100)):
+        c.k_bias[a:b] = low
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **c.kw())
+    few = dict(c.kw(), q_off=offsets([5, 0, 3]).to(DEV), Nq=5, q_pos=c.q_pos[:8].contiguous().to(DEV))
+    some = mpm.attention(q[:8], k, v, **few)
+    torch.cuda.synchronize()
+    want, _, wg = c.plain(grads=True)
+    assert ref.rel(out, want) <= FWD[dtype]
+    for got, w in zip((g.dq, g.dk, g.dv, g.dbias), wg):
+        assert ref.rel(got, w) <= BWD[dtype]
+    assert ref.rel(some[:5], want[:5]) <= FWD[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [30.0, 300.0])
+def test_large_scores(dtype, size):
+    """Scores of either sign far from zero, rising along the keys: what is taken from them follows. The
+    exponent's error is 2^-24 of the scores (times the products' depth), which bounds float32."""
+    c = Case(dtype, [70], [300], 2, 2, 32, (18, 18), 17, "sorted", True, seed=10)
+    c.k_bias = torch.linspace(-size, size, 300) - size * 0.5
+    out, lse = mpm.attention(*c.dev(), with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), *c.dev(), out, lse, **c.kw())
+    torch.cuda.synchronize()
+    want, wl, wg = c.plain(grads=True)
+    tol = {BF: BWD[BF], F32: 2 * (144 + 4 * size) * 2.0 ** -24}[dtype]
+    assert ref.rel(out, want) <= tol
+    assert ref.rel(lse.cpu().double().sum(-1) * math.log(2.0), wl) <= 144 * 2.0 ** -24
+    for got, w in zip((g.dq, g.dk, g.dv), wg):
+        assert ref.rel(got, w) <= tol
+
+
 def test_bias_of_minus_infinity_masks():
     """Offsets whose bias is -inf take no part, and a query all of whose keys are masked gets zeros."""
     c = Case(F32, [50, 3], None, 2, 2, 32, (8, 8), 7, "sorted", False, seed=8, inf_bias=True)
