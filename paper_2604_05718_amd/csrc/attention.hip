@@ -320,8 +320,18 @@ hipError_t launch(const AttentionCall& a, const HeadRows& q, const HeadRows& k, 
     constexpr long kFewGroups = 512;
     if constexpr (S::kBytes == 2 && DH == 64) {
         const long W = 2 * a.span + 1;
+        const bool one = BIAS != kBiasNone && W * W * 4 > kLargeTable;  // one workgroup a compute unit
         if (a.Nq >= 1792 || (BIAS != kBiasNone && W * W * 4 > kLargeTable && a.Nq > 256))
+        {
+            // Rounds over the compute units, in units of the 512-query workgroup's time: one of 256 queries
+            // takes 0.6 of it (8 images of 4096 tokens, 16 heads: 918 us against 770 in full rounds; 3
+            // images, 768 workgroups against 384, 360 against 408).
+            const long pairs = (long)a.B * a.H;
+            const long wide = (pairs * ((a.Nq + 511) / 512) + 255) / 256, narrow = (pairs * ((a.Nq + 255) / 256) + 255) / 256;
+            if (one && 0.6 * (double)narrow < (double)wide)
+                return launch_as<S, DH, BIAS, KB, 8, 1, 1>(a, q, k, v, out, lse, stream);
             return launch_as<S, DH, BIAS, KB, 8, 2, 1>(a, q, k, v, out, lse, stream);
+        }
     }
     if constexpr (DH == 64) {
         const long groups = (long)a.B * a.H * ((a.Nq + 127) / 128);

@@ -366,23 +366,28 @@ __device__ __forceinline__ int raise_to(float x, int bits)
     return min(max(bits - (__builtin_amdgcn_frexp_expf(x)), -100), 100);
 }
 
+// kSum32: the sums lie a constant behind the biases, so that one address serves both (pairs of a bias and
+// a sum would need one address too, but met in the banks: 5% of the kernel). Tables of up to 63 x 63,
+// 77 x 77 (the widest of the four-wave form) and 127 x 127 entries.
+constexpr int kGapSmall = 15888, kGapMiddle = 23728, kGapLarge = 64528;
+
 // Bytes of the query kernel's tables.
-__host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
+__host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W, int gap)
 {
     if (bias == kBiasNone) return 0;
+    if (sum == kSum32) return gap + (size_t)W * W * 4;
     return (size_t)W * W * (sum == kSumNone ? 4 : sum == kSum64 ? 12 : 8);
 }
 
-// dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: kSum32 pairs of
-// (bias, sum), otherwise the biases and then the sums (kSum64: the sums first).
-template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
+// dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: the biases and then the sums
+// (kSum64: the sums first).
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT, int GAP>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                         HeadRows k, HeadRows v,
                                                                         const float2* __restrict__ lse, Scratch w,
                                                                         HeadRows dq, int blocks)
 {
     constexpr int THREADS = WAVES * kWave, KT = tile_rows<S, DH, SPLIT>(), BUFS = buffers<S, DH>();
-    constexpr int SIZE = SUM == kSum32 ? 8 : 4;
     typedef PairStage<S, DH, KT, THREADS> Staged;
     typedef typename FragOf<S>::type Frag;
     typedef __attribute__((address_space(3))) int32_t lds_int;
@@ -427,7 +432,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         stage.template store<KB>(at, t);
         if (t < KT) {
             int* codes = reinterpret_cast<int*>(at + tile_bytes<S, DH, SPLIT>());
-            if (BIAS != kBiasNone) codes[t] = bias_code<BIAS, SIZE>(pos, a.grid_h, a.grid_w, W);
+            if (BIAS != kBiasNone) codes[t] = bias_code<BIAS>(pos, a.grid_h, a.grid_w, W);
             if (KB) reinterpret_cast<float*>(codes + KT)[t] = to_log2(kbias);
         }
     };
@@ -457,10 +462,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     }
     int qcode = 0;
     if (BIAS != kBiasNone) {
-        load_table<THREADS, SIZE / 4>(table, a.bias + (long)hd * W2, W2, t);
-        qcode = query_code<BIAS, SIZE>(qpos, a.grid_h, a.grid_w, a.span, W, table_at);
+        load_table<THREADS>(table, a.bias + (long)hd * W2, W2, t);
+        qcode = query_code<BIAS>(qpos, a.grid_h, a.grid_w, a.span, W, table_at);
         if (SUM == kSum32)
-            for (int e = t; e < W2; e += THREADS) reinterpret_cast<int32_t*>(table)[2 * e + 1] = 0;
+            for (int e = t; e < W2; e += THREADS) reinterpret_cast<int32_t*>(tables + GAP)[e] = 0;
         if (SUM == kSum64)
             for (int e = t; e < W2; e += THREADS) reinterpret_cast<unsigned long long*>(tables)[e] = 0;
         if (SUM == kSumTurns)
@@ -501,7 +506,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                 for (int e = 0; e < 4; ++e) {
                     float x = s[4 * g + e];
                     if (BIAS != kBiasNone) {
-                        entry[4 * g + e] = bias_entry<BIAS, SIZE>(qcode, kc[e], a.span, W, table_at);
+                        entry[4 * g + e] = bias_entry<BIAS>(qcode, kc[e], a.span, W, table_at);
                         x = fmaf(x, c, lds_at(entry[4 * g + e]));
                     } else {
                         x *= c;
@@ -537,7 +542,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                 for (int r = 0; r < 16; ++r) {
                     int n;  // to the nearest
                     asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(n) : "v"(dp[r]));
-                    __hip_atomic_fetch_add((lds_int*)(uintptr_t)(uint32_t)(entry[r] + 4), n, __ATOMIC_RELAXED,
+                    __hip_atomic_fetch_add((lds_int*)(uintptr_t)(uint32_t)entry[r] + GAP / 4, n, __ATOMIC_RELAXED,
                                            __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
             }
@@ -597,7 +602,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         float* part = w.parts + ((long)pair * blocks + blk) * W2;
         for (int e = t; e < W2; e += THREADS) {
             float x;
-            if (SUM == kSum32) x = (float)reinterpret_cast<const int32_t*>(table)[2 * e + 1] * back;
+            if (SUM == kSum32) x = (float)reinterpret_cast<const int32_t*>(tables + GAP)[e] * back;
             else if (SUM == kSum64) x = (float)reinterpret_cast<const long long*>(tables)[e] * back;
             else x = table[W2 + e];
             part[e] = any_bad ? __builtin_nanf("") : x;
@@ -644,7 +649,7 @@ struct Inputs {
 };
 
 // Query rows of a workgroup: eight waves where the tables leave LDS for one workgroup only.
-constexpr long kLargeTable = 24 << 10;
+constexpr long kLargeTable = kGapMiddle;
 bool large_table(const AttentionCall& a)
 {
     const long W = 2 * a.span + 1;
@@ -686,15 +691,15 @@ hipError_t launch_keys(const AttentionCall& a, const Inputs& in, const Grads& g,
     return hipGetLastError();
 }
 
-template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT, int GAP = 0>
 hipError_t launch_queries(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
     const int blocks = query_blocks(a);
     const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8) +
-                         table_bytes(BIAS, SUM, 2 * a.span + 1);
+                         table_bytes(BIAS, SUM, 2 * a.span + 1, GAP);
     const long grid = block_grid((long)a.B * a.H, blocks);
     if (grid * WAVES * kWave > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES, SPLIT>;
+    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES, SPLIT, GAP>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), bytes, st, a, in.dout, in.q, in.k, in.v,
@@ -717,8 +722,12 @@ hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, 
     } else {
         constexpr size_t tiles = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8);
         if (!g.dbias) return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES, SPLIT>(a, in, g, st);
-        if constexpr (S::kBytes == 2 && BIAS == kBiasGrid) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT>(a, in, g, st);
-        else if (tiles + table_bytes(BIAS, kSum64, W) <= kLdsBytes)
+        if constexpr (S::kBytes == 2 && BIAS == kBiasGrid) {
+            if constexpr (WAVES == 8) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapLarge>(a, in, g, st);
+            else if (W <= 63) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapSmall>(a, in, g, st);
+            else if (DH == 64) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapMiddle>(a, in, g, st);
+            else e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapLarge>(a, in, g, st);
+        } else if (tiles + table_bytes(BIAS, kSum64, W, 0) <= kLdsBytes)
             e = launch_queries<S, DH, BIAS, KB, kSum64, WAVES, SPLIT>(a, in, g, st);
         else e = launch_queries<S, DH, BIAS, KB, kSumTurns, WAVES, SPLIT>(a, in, g, st);
         if (e != hipSuccess) return e;

@@ -229,34 +229,34 @@ enum BiasKind : int {
     kBiasFar = 2    // offsets are held to the span, one axis at a time
 };
 
-// A grid position in the form its side of the bias entry needs (entries of `size` bytes).
+// A grid position in the form its side of the bias entry needs (entries of 4 bytes).
 // kBiasGrid: the byte offset of row * W + column (W = 2 span + 1), so that a pair's entry is
 // query - key + middle. kBiasFar:
 // row and column as two 16-bit halves. Positions outside the grid are held to it, so that a
 // pair's entry is inside the table whatever the caller passed.
-template <int BIAS, int SIZE = 4>
+template <int BIAS>
 __device__ __forceinline__ int bias_code(int pos, int gh, int gw, int W)
 {
     if constexpr (BIAS == kBiasNone) return 0;
     const int p = min(max(pos, 0), gh * gw - 1);
     const int r = (int)((unsigned)p / (unsigned)gw), c = p - r * gw;
-    if constexpr (BIAS == kBiasGrid) return (r * W + c) * SIZE;
+    if constexpr (BIAS == kBiasGrid) return (r * W + c) * 4;
     return (r << 16) | c;
 }
 // Where the pair's entry is: qcode's side holds the table's address (kBiasFar: base does).
-template <int BIAS, int SIZE = 4>
+template <int BIAS>
 __device__ __forceinline__ int bias_entry(int qcode, int kcode, int span, int W, int base)
 {
     if constexpr (BIAS == kBiasGrid) return qcode - kcode;
     const int dr = (qcode >> 16) - (kcode >> 16), dc = (qcode & 0xffff) - (kcode & 0xffff);
-    return base + ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * SIZE;
+    return base + ((min(max(dr, -span), span) + span) * W + min(max(dc, -span), span) + span) * 4;
 }
 // A query's side: with the middle of the table at LDS address `base` added (kBiasGrid).
-template <int BIAS, int SIZE = 4>
+template <int BIAS>
 __device__ __forceinline__ int query_code(int pos, int gh, int gw, int span, int W, int base)
 {
-    const int c = bias_code<BIAS, SIZE>(pos, gh, gw, W);
-    return BIAS == kBiasGrid ? c + (span * W + span) * SIZE + base : c;
+    const int c = bias_code<BIAS>(pos, gh, gw, W);
+    return BIAS == kBiasGrid ? c + (span * W + span) * 4 + base : c;
 }
 
 // An LDS address as the 32-bit number the hardware takes, and a float at one: a pair's bias is read at
@@ -374,8 +374,8 @@ struct PairStage {
     }
 };
 
-// A head's bias table to LDS, in base 2, every STRIDE words: sixteen loads a thread in flight.
-template <int THREADS, int STRIDE = 1>
+// A head's bias table to LDS, in base 2: sixteen loads a thread in flight.
+template <int THREADS>
 __device__ __forceinline__ void load_table(float* table, const float* src, int n, int t)
 {
     constexpr int kFlight = 16;
@@ -385,7 +385,7 @@ __device__ __forceinline__ void load_table(float* table, const float* src, int n
         for (int i = 0; i < kFlight; ++i) v[i] = src[min(e0 + i * THREADS, n - 1)];
 #pragma unroll
         for (int i = 0; i < kFlight; ++i)
-            if (e0 + i * THREADS < n) table[(e0 + i * THREADS) * STRIDE] = to_log2(v[i]);
+            if (e0 + i * THREADS < n) table[e0 + i * THREADS] = to_log2(v[i]);
     }
 }
 
