@@ -45,7 +45,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     constexpr int THREADS = WAVES * kWave;
     static_assert(SPLIT == 1 || (SPLIT == 2 && QT == 1), "a split tile is one tile");
     constexpr int KT = key_tile<S, SPLIT>();
-    typedef PairStage<S, DH, KT, THREADS> Staged;
+    typedef PairStage<S, DH, KT, THREADS, true> Staged;
     typedef typename FragOf<S>::type Frag;
     constexpr int kBuffer = buffer_bytes<S, DH, SPLIT>();
     constexpr bool kBf = S::kBytes == 2;

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
                                                                       HeadRows dk, HeadRows dv, int blocks)
 {
     constexpr int THREADS = WAVES * kWave, QT = tile_rows<S, DH, SPLIT>(), BUFS = buffers<S, DH>();
-    typedef PairStage<S, DH, QT, THREADS> Staged;
+    typedef PairStage<S, DH, QT, THREADS, false> Staged;
     typedef typename FragOf<S>::type Frag;
     constexpr int kBuffer = tile_bytes<S, DH, SPLIT>() + QT * 16 + 16;
     extern __shared__ __align__(16) uint8_t lds[];
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                                                                         HeadRows dq, int blocks)
 {
     constexpr int THREADS = WAVES * kWave, KT = tile_rows<S, DH, SPLIT>(), BUFS = buffers<S, DH>();
-    typedef PairStage<S, DH, KT, THREADS> Staged;
+    typedef PairStage<S, DH, KT, THREADS, true> Staged;
     typedef typename FragOf<S>::type Frag;
     typedef __attribute__((address_space(3))) int32_t lds_int;
     typedef __attribute__((address_space(3))) unsigned long long lds_long;

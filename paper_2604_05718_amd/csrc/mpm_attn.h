@@ -299,9 +299,11 @@ inline long block_grid(long pairs, int blocks)
     return (pairs >= 4 * kXcds ? (pairs + kXcds - 1) / kXcds * kXcds : pairs) * blocks;
 }
 
-// Tiles of ROWS rows of two operands on their way to LDS: loaded to registers a tile ahead. A whole
-// tile's loads take a scalar address and an offset of the thread's own, the same for every tile.
-template <class S, int DH, int ROWS, int THREADS>
+// Tiles of ROWS rows of two operands on their way to LDS: loaded to registers a tile ahead. SCALAR: a whole
+// tile's loads take a scalar address and an offset of the thread's own, the same for every tile; otherwise
+// each thread walks its chunks by their addresses (the key kernel, whose scalar registers are full: 640
+// against 690 us on 3 images of 4096 tokens, where the other two kernels gain 2 to 4%).
+template <class S, int DH, int ROWS, int THREADS, bool SCALAR>
 struct PairStage {
     typedef Tile<S, DH> T;
     static constexpr int kTileBytes = ROWS * T::kRowBytes;
@@ -313,6 +315,7 @@ struct PairStage {
     long xs, ys;             // bytes from row to row
     uint32_t xo[kPer], yo[kPer];
     bool narrow;  // offsets inside a tile fit 32 bits, rows are whole
+    const uint8_t *xp[kPer], *yp[kPer];  // (not SCALAR) the chunks of the next tile
 
     __device__ __forceinline__ void init(const HeadRows& xr, const HeadRows& yr, long first, int head, int dh, int t)
     {
@@ -327,16 +330,20 @@ struct PairStage {
             const int e = t + i * THREADS;
             xo[i] = (uint32_t)(e / T::kChunks) * (uint32_t)xs + e % T::kChunks * 16;
             yo[i] = (uint32_t)(e / T::kChunks) * (uint32_t)ys + e % T::kChunks * 16;
+            if (!SCALAR) {
+                xp[i] = xb + e / T::kChunks * xs + e % T::kChunks * 16;
+                yp[i] = yb + e / T::kChunks * ys + e % T::kChunks * 16;
+            }
         }
     }
-    // Loads rows r0 ... of `count`; zeros past the last row and past a row's end. Rows dropped by
+    // Loads rows r0 ... of `count` (tiles in order); zeros past the last row and past a row's end. Rows dropped by
     // drop[row] = -inf are stored as zeros, whatever they hold (loaded all the same: a load that
     // waits for its drop value would take twice the latency).
     template <bool DROP>
     __device__ __forceinline__ void load(int dh, int count, const float* drop, int r0, int t)
     {
         const uint8_t *xt = xb + r0 * xs, *yt = yb + r0 * ys;
-        if (narrow && r0 + ROWS <= count) {
+        if (SCALAR && narrow && r0 + ROWS <= count) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 x[i] = load16(xt + xo[i]);
@@ -353,8 +360,12 @@ struct PairStage {
             if (DROP) dropped[i] = 0.0f;
             if (ch * (16 / S::kBytes) < dh && r0 + r < count) {
                 if (DROP) dropped[i] = drop[r0 + r];
-                x[i] = load16(xt + r * xs + ch * 16);
-                y[i] = load16(yt + r * ys + ch * 16);
+                x[i] = load16(SCALAR ? xt + r * xs + ch * 16 : xp[i]);
+                y[i] = load16(SCALAR ? yt + r * ys + ch * 16 : yp[i]);
+            }
+            if (!SCALAR) {
+                xp[i] += ROWS * xs;
+                yp[i] += ROWS * ys;
             }
         }
     }
