@@ -104,6 +104,14 @@ SHAPES = [
     ([130], None, 1, 1, 8, (12, 12), 0, "sorted", False),
     ([300], None, 1, 1, 16, (64, 64), 63, "sorted", False),
     ([40, 1], None, 2, 2, 24, (200, 3), 63, "shuffled", False),
+    # the widest heads with the largest table, tables of the middle size, long images in wide blocks
+    ([300, 5], None, 2, 1, 128, (64, 64), 63, "sorted", True),
+    ([90, 270], None, 2, 2, 64, (36, 30), 35, "sorted", False),
+    ([600], None, 4, 2, 64, (64, 50), 63, "shuffled", True),
+    ([1800, 100], None, 2, 2, 64, None, None, "sorted", False),
+    ([1900], None, 1, 1, 64, (64, 64), 20, "sorted", False),
+    ([1850], None, 1, 1, 64, (64, 64), 63, "sorted", True),
+    ([200] * 50, None, 6, 6, 32, (16, 16), 15, "sorted", False),
 ]
 
 
