@@ -443,7 +443,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)hd * q.head) * S::kBytes, a.dh, live, h);
     load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
 
-    // The power of two that score gradients are multiplied by, by way of the probabilities.
+    // The power of two that score gradients are multiplied by: kSum32 by way of the probabilities'
+    // exponents (free, and bfloat16 does not see the exponents' rounding), kSum64 as they are summed.
     int lg = 0;
     if (SUM == kSum32 || SUM == kSum64) {
         const uint32_t* most = w.largest + 2 * ((long)b * a.H + hd);
@@ -452,7 +453,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     }
     const float2 stat = live ? lse[qrow * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
     const bool apart = !can_start<S>(c) || __any(too_large(stat));
-    const float2 tk = taken(stat, apart, c, (float)lg);
+    const float2 tk = taken(stat, apart, c, SUM == kSum32 ? (float)lg : 0.0f);
+    const float raise = SUM == kSum64 ? __builtin_ldexpf(1.0f, lg) : 1.0f;
     const float nd = live ? -w.delta[qrow * a.H + hd] : 0.0f;
     f32x16 s0, dp0;
 #pragma unroll
@@ -551,7 +553,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                 for (int r = 0; r < 16; ++r)
                     __hip_atomic_fetch_add(
                         (lds_long*)(uintptr_t)(uint32_t)((entry[r] - table_at) * 2 + lds_address(tables)),
-                        (unsigned long long)(long long)dp[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        (unsigned long long)(long long)(dp[r] * raise), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             }
             if (SUM == kSumTurns) {
                 for (int turn = 0; turn < 2 * WAVES; ++turn) {
@@ -608,7 +610,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
             part[e] = any_bad ? __builtin_nanf("") : x;
         }
     }
-    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale * back, a.dh, live && share == 0, h, S{});
+    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, SUM == kSum32 ? a.scale * back : a.scale, a.dh, live && share == 0, h, S{});
 }
 
 // dbias[head][e] = the workgroups' parts, in the order of images and query blocks: four threads an
