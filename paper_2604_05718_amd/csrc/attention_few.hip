@@ -3,9 +3,12 @@
 // and over workgroups, whose running maxima, sums and unscaled outputs are joined afterwards.
 //
 // Bound by memory: every key and value is read once. A wave keeps its own tile of 32 values in LDS
-// and the next tile's keys and values in registers on their way, so waves never wait for each
-// other; with one live column in 32 the products cost less than the bytes. Bias entries are read
-// from memory (a table in LDS would cost more to bring than the few columns read of it).
+// and the next tile's keys, values and bias entries in registers on their way, so waves never wait
+// for each other; with one live column in 32 the products cost less than the bytes. Bias entries are
+// read from memory (a table in LDS would cost more to bring than the few columns read of it), their
+// keys' positions a tile earlier still: entries asked for only when needed made every tile wait for
+// its successor's loads (82 -> 72 us). One query an image over 16384 keys, 4 images of 16 heads of 64,
+// bfloat16: 268 MB in 55 us (4.9 TB/s), and 6 us to join the splits.
 #include <algorithm>
 
 #include "mpm_attn.h"
@@ -16,9 +19,10 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kCols = 32;
-constexpr float kSlack = 8.0f;  // as the forward kernel's
-// Workgroups asked for (three a compute unit) and the fewest 32-key tiles a wave is left with.
-constexpr long kGroups = 768;
+constexpr float kSlack = 8.0f;  // scores may pass the maximum taken by this many powers of two
+// Workgroups asked for (two a compute unit; 4 images of 16384 keys, 16 heads: 82 us with three, 77 with
+// two, 97 with one) and the fewest 32-key tiles a wave is left with.
+constexpr long kGroups = 512;
 constexpr int kLeastTiles = 2;
 
 template <class S, int DH>
@@ -55,8 +59,17 @@ __device__ __forceinline__ void store_column(uint8_t* row, float4 o, float top, 
             total == 0.0f ? make_float2(-__builtin_inff(), 0.0f) : make_float2(top, __builtin_log2f(total));
 }
 
+// Waves a SIMD the registers are held to: three (bfloat16, 64 channels: 64 images of up to 4096 keys, one
+// query each, 165 us with two, 149 with three) where no key bias is carried along, which then spills
+// (4 images of 16384 keys: 71 us with two, 93 with three).
+template <class S, int DH, bool KB>
+constexpr int waves_per_simd()
+{
+    return S::kBytes == 2 && DH == 64 && !KB ? 3 : 2;
+}
+
 template <class S, int DH, int BIAS, bool KB>
-__global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
+__global__ __launch_bounds__(kThreads, (waves_per_simd<S, DH, KB>())) void attention_few_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
                                                                    HeadRows out, float* __restrict__ lse,
                                                                    float* __restrict__ parts, int splits)
 {
@@ -81,17 +94,39 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
     int* codes = reinterpret_cast<int*>(vt + 32 * T::kRowBytes);
     float* kbs = reinterpret_cast<float*>(codes + 32);
 
-    Frag qf[DH / 16], kf[DH / 16], kn[DH / 16];
+    Frag qf[DH / 16], kf[DH / 16];
     u32x4 vn[kChunksLane];
     int pos = 0;
-    float kbias = 0.0f;
+    float kbias = 0.0f, bn[16];
+    auto load_positions = [&](int tile) {
+        const int kk = 32 * tile + l32;
+        pos = kk < rk.count ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
+    };
+    const bool biased = BIAS != kBiasNone && live;
+    int qcode = 0;
+    const uint8_t* bias = nullptr;
+    // The bias entries of the tile whose positions are there: their codes go through LDS, as each lane
+    // reads those of 16 keys for its column.
+    auto load_bias = [&]() {
+        if (h == 0) codes[l32] = bias_code<BIAS>(pos, a.grid_h, a.grid_w, W);
+        __builtin_amdgcn_wave_barrier();
+        if (biased) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const i32x4 kc = *reinterpret_cast<const i32x4*>(codes + 8 * g + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    bn[4 * g + e] = *reinterpret_cast<const float*>(bias + bias_entry<BIAS>(qcode, kc[e], a.span, W, 0));
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
     auto load = [&](int tile) {
         const int kk = 32 * tile + l32;
         const bool in = kk < rk.count;
-        if (BIAS != kBiasNone) pos = in ? (a.k_pos ? a.k_pos[rk.first + kk] : kk) : 0;
         if (KB) kbias = in ? a.k_bias[rk.first + kk] : -__builtin_inff();
         const long row = rk.first + (in ? kk : 0);
-        load_frags<S, DH>(kn, k.p + (row * k.row + (long)hk * k.head) * S::kBytes, a.dh, in, h);
+        load_frags<S, DH>(kf, k.p + (row * k.row + (long)hk * k.head) * S::kBytes, a.dh, in, h);
 #pragma unroll
         for (int i = 0; i < kChunksLane; ++i) {
             const int e = lane + i * kWave, ch = e % T::kChunks, kv = 32 * tile + e / T::kChunks;
@@ -100,14 +135,20 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
                                   have);
         }
     };
-    if (t0 + wave < t1) load(t0 + wave);
+    const int first = t0 + wave;
+    if (BIAS != kBiasNone && first < t1) load_positions(first);
     const long qrow = rq.first + (live ? qi : 0);
     load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)(live ? hd : 0) * q.head) * S::kBytes, a.dh, live, h);
-    int qcode = 0;
-    const float* bias = nullptr;
     if (BIAS != kBiasNone) {
         qcode = query_code<BIAS>(live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0, a.grid_h, a.grid_w, a.span, W, 0);
-        bias = a.bias + (long)(live ? hd : 0) * W * W;
+        bias = reinterpret_cast<const uint8_t*>(a.bias + (long)(live ? hd : 0) * W * W);
+    }
+    if (first < t1) {
+        load(first);
+        if (BIAS != kBiasNone) {
+            load_bias();
+            if (first + kWaves < t1) load_positions(first + kWaves);
+        }
     }
     f32x16 acc[DH / 32];
 #pragma unroll
@@ -116,7 +157,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
         for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
     float m = -__builtin_inff(), sum = 0.0f;
 
-    for (int tile = t0 + wave; tile < t1; tile += kWaves) {
+    for (int tile = first; tile < t1; tile += kWaves) {
 #pragma unroll
         for (int i = 0; i < kChunksLane; ++i) {
             const int e = lane + i * kWave;
@@ -126,34 +167,27 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
             }
             store16(vt + T::at(e / T::kChunks, e % T::kChunks), vn[i]);
         }
-        if (h == 0) {
-            if (BIAS != kBiasNone) codes[l32] = bias_code<BIAS>(pos, a.grid_h, a.grid_w, W);
-            if (KB) kbs[l32] = to_log2(kbias);
-        }
-#pragma unroll
-        for (int st = 0; st < DH / 16; ++st) {
-            kf[st] = kn[st];
-            if (KB && kbias == -__builtin_inff()) kf[st] = Frag{};
-        }
-        if (tile + kWaves < t1) load(tile + kWaves);
-        __builtin_amdgcn_wave_barrier();  // one wave's own LDS: in order
-
+        if (KB && h == 0) kbs[l32] = to_log2(kbias);
         f32x16 s;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll
-        for (int st = 0; st < DH / 16; ++st) s = mma(kf[st], qf[st], s);
-        float bv[16];
-        if (BIAS != kBiasNone && live) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const i32x4 kc = *reinterpret_cast<const i32x4*>(codes + 8 * g + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    bv[4 * g + e] = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(bias) +
-                                                                    bias_entry<BIAS>(qcode, kc[e], a.span, W, 0));
-            }
+        for (int st = 0; st < DH / 16; ++st) {
+            if (KB && kbias == -__builtin_inff()) kf[st] = Frag{};
+            s = mma(kf[st], qf[st], s);
         }
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            s[r] = BIAS != kBiasNone ? fmaf(s[r], c, biased ? to_log2(bn[r]) : 0.0f) : s[r] * c;
+        // What the next tile needs goes out here, and the positions of the one after: loads return in
+        // order, so that one wait a tile covers all of them.
+        if (tile + kWaves < t1) {
+            if (BIAS != kBiasNone) load_bias();
+            if (BIAS != kBiasNone && tile + 2 * kWaves < t1) load_positions(tile + 2 * kWaves);
+            load(tile + kWaves);
+        }
+        __builtin_amdgcn_wave_barrier();  // one wave's own LDS: in order
+
         float top = -__builtin_inff();
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -162,7 +196,6 @@ __global__ __launch_bounds__(kThreads, 2) void attention_few_kernel(AttentionCal
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float x = s[4 * g + e];
-                x = BIAS != kBiasNone ? fmaf(x, c, live ? to_log2(bv[4 * g + e]) : 0.0f) : x * c;
                 if (KB) x = kb[e] > -__builtin_inff() ? x + kb[e] : -__builtin_inff();
                 else if (32 * tile + 8 * g + 4 * h + e >= rk.count) x = -__builtin_inff();
                 s[4 * g + e] = x;
@@ -310,6 +343,10 @@ hipError_t pick(const AttentionCall& a, const HeadRows& q, const HeadRows& k, co
 
 }  // namespace
 
+// The queries of the heads that share a key head fit a tile's columns. Tiles of queries instead (12 heads,
+// one query an image, us there / here): 4 images of 16384 keys, 16 heads 477 / 71, 64 of up to 4096
+// 330 / 149, 64 of up to 1024 43 / 41, 64 of 256 24 / 26, one of up to 1024 26 / 23; 20 queries an image:
+// 64 of up to 4096 331 / 204, 64 of up to 1024 44 / 55.
 bool attention_is_few(const AttentionCall& a) { return (long)a.H / a.Hk * a.Nq <= kCols; }
 
 int attention_few_splits(const AttentionCall& a)

@@ -57,7 +57,6 @@ struct Tile {
     __device__ static __forceinline__ int at(int r, int c) { return r * kRowBytes + ((c ^ mix(r)) << 4); }
 };
 
-__device__ __forceinline__ bf16x8 as_frag(u32x4 v, Bf16) { return __builtin_bit_cast(bf16x8, v); }
 
 // Contracted step s of row r (lane % 32 of its 32-row group): values 16 s + 8 h ... + 7 of it.
 template <class S, int DH>
