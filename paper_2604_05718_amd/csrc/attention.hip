@@ -5,6 +5,14 @@
 //
 // One pass over the keys with a running maximum and sum. Scores are kept in base 2 (everything
 // is multiplied by log2 e once), so an exponential is one instruction.
+//
+// Bound by instruction issue: a score costs an exponential, its share of a bias read, a maximum, a sum and
+// a conversion, and those and the products hardly overlap (3 images of 4096 tokens: vector instructions
+// 58% and products 32% of the busy cycles). A score tile's registers are the next product's operand,
+// so scores never pass through LDS; one barrier a key tile. Bfloat16, heads of 64: 8 images of 4096
+// tokens, 16 heads, 745 us, 740 TFLOP/s (a product of 8192 reaches 1227); 64 of about 717, 12 heads, 207
+// us, 490 TFLOP/s (a sixth of a workgroup's time is its first loads and its last stores); float32, 5
+// images of about 590, 6 heads of 40, 62 us.
 #include "mpm_attn.h"
 
 namespace mpm {
@@ -312,12 +320,15 @@ hipError_t launch_as(const AttentionCall& a, const HeadRows& q, const HeadRows& 
 // unit. Bfloat16, 64 channels, 12 heads, four waves / eight: 8 images of 4096 tokens without a bias
 // 527 / 484 us, with one of 127 x 127 (16 heads) 1810 / 770, 8 of 2304 with one of 95 x 95 288 / 236, 8 of
 // about 1380 144 / 149, 64 of about 717 with one of 63 x 63 254 / 287, one of 1024 41 / 60.
+// Two waves share 32 queries where workgroups of 128 would be few (not split / split): bfloat16, 12 heads of
+// up to 1024 tokens, 72 workgroups 35 / 28 us, 288 42 / 37, 576 48 / 56, 1152 79 / 88; float32, 6 heads of
+// up to 576, 96 workgroups 71 / 49, 384 100 / 106, 768 174 / 173.
 template <class S, int DH, int BIAS, bool KB>
 hipError_t launch(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v, const HeadRows& out,
                   float* lse, hipStream_t stream)
 {
     constexpr long kLargeTable = 48 << 10;
-    constexpr long kFewGroups = 512;
+    constexpr long kFewGroups = 384;
     if constexpr (S::kBytes == 2 && DH == 64) {
         const long W = 2 * a.span + 1;
         const bool one = BIAS != kBiasNone && W * W * 4 > kLargeTable;  // one workgroup a compute unit
