@@ -94,6 +94,13 @@ struct Scratch {
 
 // D[row][head] = dO . o: eight lanes a (row, head), 16-byte loads. Also clears the words that the
 // key kernel collects in. Bound by memory: 32 images of about 717 rows of 768, bfloat16, 71 MB in 13 us.
+//
+// In bfloat16 the output carries its own rounding and that of the probabilities, and so does D: an error
+// of one sign along a query's row of dS. It is lost among the other roundings in dq, dk, dv and dbias,
+// and shows where few buckets sum many offsets, whose terms cancel: 5 x 5 buckets over 9 x 9 offsets,
+// images of 25 tokens, the table's gradient differs from 64 bits by 0.0024 of its norm against 0.0017
+// with fine buckets; over 63 x 63 offsets, images of 1024, by 0.0035 (estimated). D from unrounded probabilities would
+// take a pass of two more products over all pairs.
 template <class S>
 __global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, HeadRows dout, HeadRows out, Scratch w)
 {
