@@ -288,7 +288,13 @@ __device__ __forceinline__ void store_sums(const float* v, float* out, long slot
 
 // dx and df of every row, and the workgroup's column sums: sums[k][group][D] (kSums of them) and, for
 // a gate by image, gate_sums[item][D]. Rows and parameters as in the forward kernel.
-template <class S, int LANES, int VPL, bool POST, bool PRE>
+//
+// With u = post_w t + post_b and g the gradient of y, every parameter beside the block is a combination of two
+// sums over rows, A = sum of gate g t and B = sum of gate g: dpost_w = scale A, dpost_b = scale B, dscale =
+// post_w A + post_b B, and an image's dgate = scale (post_w A' + post_b B') from its own, ungated. A row
+// costs two sums a value instead of four and their factors (a step of 16 images of about 2870 rows of
+// 1024, bfloat16: 234 -> 219 us).
+template <class S, int LANES, int VPL, bool POST, bool PRE, bool GATE_ROWS>
 __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     NormCall a, const void* __restrict__ dy, const void* __restrict__ dh, const void* __restrict__ y,
     const void* __restrict__ f, const float* __restrict__ stats, void* __restrict__ dx, void* __restrict__ df,
@@ -299,9 +305,9 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     __shared__ float lds[threads<LANES>()];
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, D = a.D;
     const float inv = 1.0f / (float)D, centred = a.layer ? inv : 0.0f;
-    float sw[kVals], sb[kVals], ss[kVals], spw[kVals], spb[kVals];
+    float sw[kVals], sb[kVals], sa[kVals], sg[kVals];  // sa, sg: A and B
 #pragma unroll
-    for (int e = 0; e < kVals; ++e) sw[e] = sb[e] = ss[e] = spw[e] = spb[e] = 0.0f;
+    for (int e = 0; e < kVals; ++e) sw[e] = sb[e] = sa[e] = sg[e] = 0.0f;
     Raw w, pw, pb, sc, ga;
     if (PRE) w.param(a.w, 0, D, lane, 0.0f);
     if (POST) {
@@ -311,10 +317,13 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     sc.param(a.scale, 0, D, lane, 1.0f);
     for (long i = blockIdx.x; i < items; i += gridDim.x) {
         const Item it = item_rows(a, i);
-        float sg[kVals];
+        float ia[kVals], ig[kVals], factor[kVals];  // the item's sums; of g t in the gradient of t
+        ga.param(GATE_ROWS ? nullptr : a.gate, it.image, D, lane, 1.0f);
 #pragma unroll
-        for (int e = 0; e < kVals; ++e) sg[e] = 0.0f;
-        ga.param(a.gate_rows ? nullptr : a.gate, it.image, D, lane, 1.0f);
+        for (int e = 0; e < kVals; ++e) {
+            ia[e] = ig[e] = 0.0f;
+            factor[e] = sc.get(e) * ga.get(e) * (POST ? pw.get(e) : 1.0f);  // POST: zero past the row's end
+        }
         Raw yn, hn, gn, fn;
         float4 stn;
         auto load = [&](long at) {
@@ -339,7 +348,7 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
                 hn.clear();
             }
             const float4 st = stn;
-            if (a.gate_rows) ga.load(a.gate, row, D, lane);
+            if (GATE_ROWS) ga.load(a.gate, row, D, lane);
             float g[kVals], t[kVals], n[kVals];
             if (PRE) {
 #pragma unroll
@@ -379,21 +388,19 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
             float n1 = 0.0f, n2 = 0.0f;
 #pragma unroll
             for (int e = 0; e < kVals; ++e) {
-                const float u = POST ? fmaf(t[e], pw.get(e), pb.get(e)) : t[e];
-                const float gu = g[e] * u, du = g[e] * (sc.get(e) * ga.get(e));
-                ss[e] = fmaf(gu, ga.get(e), ss[e]);
-                n[e] = gu * sc.get(e);
-                sg[e] += n[e];
-                g[e] = du;
+                if (GATE_ROWS) {
+                    n[e] = g[e] * (sc.get(e) * (POST ? fmaf(t[e], pw.get(e), pb.get(e)) : t[e]));
+                    g[e] *= ga.get(e);
+                }
+                ia[e] = fmaf(g[e], t[e], ia[e]);
+                if (POST) ig[e] += g[e];
+                g[e] *= factor[e];
                 if (POST) {
-                    spb[e] += du;
-                    spw[e] = fmaf(du, t[e], spw[e]);
-                    g[e] = du * pw.get(e);  // zero past the row's end
                     n1 += g[e];
                     n2 = fmaf(g[e], t[e], n2);
                 }
             }
-            if (a.gate_rows && live) Raw::store(n, dgate, row, D, lane);
+            if (GATE_ROWS && live) Raw::store(n, dgate, row, D, lane);
             if (POST) {
                 row_sums<LANES>(n1, n2, lds);
                 n1 *= -st.y * centred;
@@ -403,17 +410,30 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
             }
             if (live) Raw::store(g, df, row, D, lane);
         }
-        if (gate_sums) store_sums<S, LANES, VPL>(sg, gate_sums, i, D, lane, sub, lds);
+#pragma unroll
+        for (int e = 0; e < kVals; ++e) {
+            const float gate = GATE_ROWS ? 1.0f : ga.get(e);
+            sa[e] = fmaf(gate, ia[e], sa[e]);
+            if (POST) sg[e] = fmaf(gate, ig[e], sg[e]);
+            ia[e] = sc.get(e) * (POST ? fmaf(pw.get(e), ia[e], pb.get(e) * ig[e]) : ia[e]);
+        }
+        if (gate_sums) store_sums<S, LANES, VPL>(ia, gate_sums, i, D, lane, sub, lds);
     }
     const long G = gridDim.x, at = blockIdx.x;
     if (PRE) {
         store_sums<S, LANES, VPL>(sw, sums, at, D, lane, sub, lds);
         if (a.b) store_sums<S, LANES, VPL>(sb, sums, G + at, D, lane, sub, lds);
     }
-    if (a.scale) store_sums<S, LANES, VPL>(ss, sums, 2 * G + at, D, lane, sub, lds);
+#pragma unroll
+    for (int e = 0; e < kVals; ++e) {
+        sw[e] = POST ? fmaf(pw.get(e), sa[e], pb.get(e) * sg[e]) : sa[e];
+        sa[e] *= sc.get(e);
+        sg[e] *= sc.get(e);
+    }
+    if (a.scale) store_sums<S, LANES, VPL>(sw, sums, 2 * G + at, D, lane, sub, lds);
     if (POST) {
-        store_sums<S, LANES, VPL>(spw, sums, 3 * G + at, D, lane, sub, lds);
-        if (a.post_b) store_sums<S, LANES, VPL>(spb, sums, 4 * G + at, D, lane, sub, lds);
+        store_sums<S, LANES, VPL>(sa, sums, 3 * G + at, D, lane, sub, lds);
+        if (a.post_b) store_sums<S, LANES, VPL>(sg, sums, 4 * G + at, D, lane, sub, lds);
     }
 }
 
@@ -509,9 +529,10 @@ hipError_t backward(NormCall a, const void* dy, const void* dh, const void* y, c
         return with_norms(a, [&](auto post, auto pre) {
             constexpr int L = decltype(lanes)::value, V = decltype(vpl)::value;
             constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value;
-            hipLaunchKernelGGL((norm_backward_kernel<S, L, V, POST, PRE>), dim3((unsigned)groups), dim3(threads<L>()), 0,
-                               st, a, dy, dh, y, f, stats, g.dx, g.df, g.dgate, sums, by_image ? gate_sums : nullptr,
-                               items);
+            auto kernel = a.gate_rows ? norm_backward_kernel<S, L, V, POST, PRE, true>
+                                      : norm_backward_kernel<S, L, V, POST, PRE, false>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads<L>()), 0, st, a, dy, dh, y, f, stats, g.dx,
+                               g.df, g.dgate, sums, by_image ? gate_sums : nullptr, items);
             return hipGetLastError();
         });
     });
