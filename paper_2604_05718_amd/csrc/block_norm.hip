@@ -5,8 +5,9 @@
 // backward reads dy, dh, y and f and writes dx and df; everything between stays in registers. Rows of
 // the next turn load while one is computed. Layer norms on both sides, bfloat16: 64 images of about 717
 // rows of 768 (282 MB) 58 us forward, 4.9 TB/s; 16 of about 2870 rows of 1024 (376 and 564 MB) 68 us forward,
-// 5.5 TB/s, and 153 us backward, 3.7 TB/s, with 5 us to join the column sums: the backward's two norms
-// are four sums of a row one after another, which two waves a SIMD do not hide in full.
+// 5.5 TB/s, and 141 us backward, 4.0 TB/s, with 5 us to join the column sums: the backward's two norms
+// are four sums of a row one after another, which two waves a SIMD do not hide in full (registers held
+// to three or four spill: a step 219 -> 552 and 742 us).
 #include <algorithm>
 #include <type_traits>
 
