@@ -84,9 +84,10 @@ constexpr int waves_per_simd()
 }
 
 // What the kernels leave for each other: D of every query and head, the largest |dS| and |dP - D| of
-// every image and head (as bits), and whether an image's keys repeat a position.
+// every image and head (as bits), and whether an image's keys repeat a position. D is kept by image slot, not by
+// packed row: the packed offsets of a call on some images of a larger tensor start past zero.
 struct Scratch {
-    float* delta;
+    float* delta;       // [B][Nq][H]
     uint32_t* largest;  // [B][H][2]
     int32_t* repeats;   // [B]
     float* parts;       // [pair][block][W * W]
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, H
     const int j = threadIdx.x % kLanes;
     if (item >= (long)rq.count * a.H) return;
     const long row = rq.first + item / a.H;
-    const int hd = (int)(item % a.H);
+    const int hd = (int)(item % a.H);  // (item: also the entry in this image's slots)
     const uint8_t* x = dout.p + (row * dout.row + (long)hd * dout.head) * S::kBytes;
     const uint8_t* y = out.p + (row * out.row + (long)hd * out.head) * S::kBytes;
     float sum = 0.0f;
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, H
     }
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    if (j == 0) w.delta[row * a.H + hd] = sum;
+    if (j == 0) w.delta[(long)b * a.Nq * a.H + item] = sum;
 }
 
 // What is taken from a query's scores before the exponential: the maximum and the log of the sum
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
                 const bool in = qi < rq.count;
                 if (BIAS != kBiasNone) pos = in ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0;
                 stat = in ? lse[(rq.first + qi) * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
-                del = in ? w.delta[(rq.first + qi) * a.H + hd] : 0.0f;
+                del = in ? w.delta[((long)b * a.Nq + qi) * a.H + hd] : 0.0f;
             }
         };
         auto store = [&](int buf) {
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     const bool apart = !can_start<S>(c) || __any(too_large(stat));
     const float2 tk = taken(stat, apart, c, SUM == kSum32 ? (float)lg : 0.0f);
     const float raise = SUM == kSum64 ? __builtin_ldexpf(1.0f, lg) : 1.0f;
-    const float nd = live ? -w.delta[qrow * a.H + hd] : 0.0f;
+    const float nd = live ? -w.delta[((long)b * a.Nq + qi) * a.H + hd] : 0.0f;
     f32x16 s0, dp0;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {

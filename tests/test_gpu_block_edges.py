@@ -1,0 +1,40 @@
+"""The operators of the blocks at the edges of what they take: images out of the middle of a packed
+tensor. Tolerances as in test_gpu_block_ops.py."""
+import pytest
+import torch
+
+import block_refs as ref
+import paper_2604_05718_amd as mpm
+from test_gpu_block_ops import BF, BWD, DEV, F32, FWD, Case, offsets
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("biased", [True, False])
+@pytest.mark.parametrize("first", [1, 3])
+def test_images_in_the_middle_of_a_packed_tensor(dtype, biased, first):
+    """Offsets that start past zero (some images of a larger tensor): the results and gradients of the same
+    images packed from zero, bit for bit, and nothing written outside them."""
+    ns = [300, 40, 129, 7]
+    c = Case(dtype, ns, None, 4, 2, 32, *(((20, 20), 19, "sorted", True) if biased else (None, None)), seed=300)
+    a, b = int(c.q_off[first]), int(c.q_off[-1])
+    print(f"images {first} to 3, {dtype}, biased {biased}", flush=True)
+    most, part = max(ns[first:]), c.q_off[first:].to(DEV)
+    kw = dict(c.kw(), q_off=part, k_off=part, Nq=most, Nk=most)
+    q, k, v, dout = *c.dev(), c.dout.to(DEV)
+    seven = [torch.full_like(t, 7) for t in (q, q, k, v)]
+    out, lse = mpm.attention(q, k, v, with_lse=True, out=seven[0], **kw)
+    g = mpm.attention_backward(dout, q, k, v, out, lse, dq=seven[1], dk=seven[2], dv=seven[3], **kw)
+    torch.cuda.synchronize()
+    own = offsets(ns[first:]).to(DEV)
+    kw.update(q_off=own, k_off=own, **{n: kw[n][a:b].contiguous() for n in ("q_pos", "k_pos", "k_bias") if kw.get(n) is not None})
+    q, k, v, dout = (t[a:b].contiguous() for t in (q, k, v, dout))
+    want, wl = mpm.attention(q, k, v, with_lse=True, **kw)
+    w = mpm.attention_backward(dout, q, k, v, want, wl, **kw)
+    torch.cuda.synchronize()
+    for got, t in zip(seven, (want, w.dq, w.dk, w.dv)):
+        assert torch.equal(got[a:b], t)
+        assert torch.all(got[:a] == 7) and torch.all(got[b:] == 7)
+    assert torch.equal(lse[a:b], wl)
+    assert g.dbias is None if not biased else torch.equal(g.dbias, w.dbias)
