@@ -142,6 +142,8 @@ def bias_expand(table, lut, out=None):
 def bias_gradient(dbias, lut, nb: int, dtype=torch.float32, out=None):
     """The table's gradient [nb * nb, H] from attention_backward's dbias [H, W, W] (mpm_bias_gradient)."""
     H, W = dbias.shape[0], lut.numel()
+    if not dbias.is_cuda or dbias.shape != (H, W, W) or W % 2 == 0:
+        raise ValueError("dbias must be a device tensor [H, W, W], lut of its odd length W")
     if out is None:
         out = torch.empty((nb * nb, H), dtype=dtype, device=dbias.device)
     _lib.check("mpm_bias_gradient", _lib.load().mpm_bias_gradient(
