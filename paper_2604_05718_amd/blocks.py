@@ -13,8 +13,34 @@ import torch
 from . import api, block_ops
 
 
+class _Once(torch.autograd.Function):
+    """The first n tensors as they are, with a history that refuses to be differentiated."""
+
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tuple(t.view_as(t) for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients of the blocks' operators have no gradients of their own: they can be "
+                           "differentiated once only")
+
+
+def _once(grads, *sources):
+    """Gradients that the kernels computed from `sources` (None entries pass). Under create_graph they are
+    joined to their sources by a node that raises, so that a second differentiation never misses their
+    terms in silence (once_differentiable's node hangs on nothing: torch.autograd.grad to given inputs
+    would walk past it)."""
+    if not torch.is_grad_enabled():
+        return tuple(grads)
+    some = [g for g in grads if g is not None]
+    tied = iter(_Once.apply(len(some), *some, *(t for t in sources if t is not None)))
+    return tuple(None if g is None else next(tied) for g in grads)
+
+
 class _Attention(torch.autograd.Function):
-    """attention() of the parts of one projection, and of the bias table by way of its offsets."""
+    """attention() of the parts of one projection, and of the bias table by way of its offsets;
+    differentiable once."""
 
     @staticmethod
     def forward(ctx, qkv, table, lut, heads, where):
@@ -22,22 +48,23 @@ class _Attention(torch.autograd.Function):
         q, k, v = qkv[:, :H], qkv[:, H:2 * H], qkv[:, 2 * H:]
         bias = block_ops.bias_expand(table, lut)
         out, lse = block_ops.attention(q, k, v, bias=bias, with_lse=True, **where)
-        ctx.save_for_backward(qkv, bias, lut, out, lse)
-        ctx.heads, ctx.where, ctx.buckets, ctx.dtype = H, where, int(table.shape[0] ** 0.5 + 0.5), table.dtype
+        ctx.save_for_backward(qkv, table, bias, lut, out, lse)
+        ctx.heads, ctx.where, ctx.buckets = H, where, int(table.shape[0] ** 0.5 + 0.5)
         return out
 
     @staticmethod
     def backward(ctx, dout):
-        qkv, bias, lut, out, lse = ctx.saved_tensors
+        qkv, table, bias, lut, out, lse = ctx.saved_tensors
         H, grad = ctx.heads, torch.empty_like(qkv)
         parts = [slice(0, H), slice(H, 2 * H), slice(2 * H, 3 * H)]
         g = block_ops.attention_backward(dout.contiguous(), *(qkv[:, p] for p in parts), out, lse, bias=bias,
                                          dq=grad[:, parts[0]], dk=grad[:, parts[1]], dv=grad[:, parts[2]], **ctx.where)
-        return grad, block_ops.bias_gradient(g.dbias, lut, ctx.buckets, dtype=ctx.dtype), None, None, None
+        dtable = block_ops.bias_gradient(g.dbias, lut, ctx.buckets, dtype=table.dtype)
+        return *_once((grad, dtable), dout, qkv, table), None, None, None
 
 
 class _ResidualNorm(torch.autograd.Function):
-    """residual_norm(): (y, h), differentiable in every tensor."""
+    """residual_norm(): (y, h), differentiable in every tensor, once."""
 
     NAMES = ("weight", "bias", "post_weight", "post_bias", "scale", "gate")
 
@@ -55,7 +82,8 @@ class _ResidualNorm(torch.autograd.Function):
         g = block_ops.residual_norm_backward(None if dy is None else dy.contiguous(),
                                              None if dh is None else dh.contiguous(), y, f.contiguous(), stats, *given,
                                              **ctx.rest)
-        return (g.dx, g.df, g.dweight, g.dbias, g.dpost_weight, g.dpost_bias, g.dscale, g.dgate, None, None, None)
+        grads = (g.dx, g.df, g.dweight, g.dbias, g.dpost_weight, g.dpost_bias, g.dscale, g.dgate)
+        return *_once(grads, dy, dh, y, f, *given), None, None, None
 
 
 class RelativeBlock(torch.nn.Module):
