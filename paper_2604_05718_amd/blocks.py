@@ -48,17 +48,21 @@ class _Attention(torch.autograd.Function):
         q, k, v = qkv[:, :H], qkv[:, H:2 * H], qkv[:, 2 * H:]
         bias = block_ops.bias_expand(table, lut)
         out, lse = block_ops.attention(q, k, v, bias=bias, with_lse=True, **where)
-        ctx.save_for_backward(qkv, table, bias, lut, out, lse)
-        ctx.heads, ctx.where, ctx.buckets = H, where, int(table.shape[0] ** 0.5 + 0.5)
+        # (the call's offsets and positions too, so that a buffer written before the backward pass is noticed)
+        ctx.tensors = [n for n, t in where.items() if torch.is_tensor(t)]
+        ctx.save_for_backward(qkv, table, bias, lut, out, lse, *(where[n] for n in ctx.tensors))
+        ctx.rest = {n: t for n, t in where.items() if n not in ctx.tensors}
+        ctx.heads, ctx.buckets = H, int(table.shape[0] ** 0.5 + 0.5)
         return out
 
     @staticmethod
     def backward(ctx, dout):
-        qkv, table, bias, lut, out, lse = ctx.saved_tensors
+        qkv, table, bias, lut, out, lse, *tensors = ctx.saved_tensors
         H, grad = ctx.heads, torch.empty_like(qkv)
         parts = [slice(0, H), slice(H, 2 * H), slice(2 * H, 3 * H)]
         g = block_ops.attention_backward(dout.contiguous(), *(qkv[:, p] for p in parts), out, lse, bias=bias,
-                                         dq=grad[:, parts[0]], dk=grad[:, parts[1]], dv=grad[:, parts[2]], **ctx.where)
+                                         dq=grad[:, parts[0]], dk=grad[:, parts[1]], dv=grad[:, parts[2]], **ctx.rest,
+                                         **dict(zip(ctx.tensors, tensors)))
         dtable = block_ops.bias_gradient(g.dbias, lut, ctx.buckets, dtype=table.dtype)
         return *_once((grad, dtable), dout, qkv, table), None, None, None
 
@@ -72,16 +76,16 @@ class _ResidualNorm(torch.autograd.Function):
     def forward(ctx, x, f, weight, bias, post_weight, post_bias, scale, gate, off, norm, eps):
         given = (weight, bias, post_weight, post_bias, scale, gate)
         y, h, stats = block_ops.residual_norm(x, f.contiguous(), *given, off=off, norm=norm, eps=eps, with_stats=True)
-        ctx.save_for_backward(y, f, stats, *given)
-        ctx.rest = dict(off=off, norm=norm, eps=eps)
+        ctx.save_for_backward(y, f, stats, off, *given)
+        ctx.rest = dict(norm=norm, eps=eps)
         return y, h
 
     @staticmethod
     def backward(ctx, dy, dh):
-        y, f, stats, *given = ctx.saved_tensors
+        y, f, stats, off, *given = ctx.saved_tensors
         g = block_ops.residual_norm_backward(None if dy is None else dy.contiguous(),
                                              None if dh is None else dh.contiguous(), y, f.contiguous(), stats, *given,
-                                             **ctx.rest)
+                                             off=off, **ctx.rest)
         grads = (g.dx, g.df, g.dweight, g.dbias, g.dpost_weight, g.dpost_bias, g.dscale, g.dgate)
         return *_once(grads, dy, dh, y, f, *given), None, None, None
 

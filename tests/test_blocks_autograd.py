@@ -118,3 +118,23 @@ def test_second_order_raises(operators):
             loss, x = penalty(case, alone)
             with pytest.raises(RuntimeError, match="differentiated once"):
                 loss.backward()
+
+
+@pytest.mark.parametrize("name", ["q_off", "k_off", "q_pos", "k_pos"])
+def test_written_buffers_of_the_attention_are_noticed(operators, name):
+    """A buffer of offsets or positions that is reused before the backward pass is an error, not another
+    gradient."""
+    qkv, table, lut, heads, where = attention_inputs()
+    where = {**where, "k_off": where["k_off"].clone(), "k_pos": where["k_pos"].clone()}
+    out = blocks._Attention.apply(qkv, table, lut, heads, where)
+    where[name].zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+def test_written_offsets_of_the_norms_are_noticed(operators):
+    *p, off, norm, eps = norm_inputs()
+    y, h = blocks._ResidualNorm.apply(*p, off, norm, eps)
+    off.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (y + h).sum().backward()
