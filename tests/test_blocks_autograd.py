@@ -138,3 +138,12 @@ def test_written_offsets_of_the_norms_are_noticed(operators):
     off.zero_()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         (y + h).sum().backward()
+
+
+@pytest.mark.parametrize("learned", [True, False])
+def test_a_frozen_table_costs_no_gradient(operators, learned):
+    qkv, table, *rest = attention_inputs()
+    table.requires_grad_(learned)
+    blocks._Attention.apply(qkv, table, *rest).sum().backward()
+    assert operators.calls == dict(attention=dict(with_dbias=learned), **(dict(table=True) if learned else {}))
+    assert qkv.grad is not None and (table.grad is not None) == learned
