@@ -540,7 +540,9 @@ int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_
  *   dbias (may be NULL; only with bias): float[H][W][W], the sum of the score gradients of every
  *     pair at each offset, over all images (mpm_bias_gradient takes it to the table's).
  * Rows of dq, dk and dv that exist are all written. Results do not depend on the order workgroups run in.
- * ws: mpm_attention_backward_workspace_bytes(call) bytes. Errors as mpm_attention, plus
+ * ws: mpm_attention_backward_workspace_bytes(call) bytes. With a bias most of them are dbias's partial
+ * sums, W * W floats for every image, head and 64 to 256 queries; a call whose dbias is NULL needs only
+ * what the size of the same call without its bias is (bias NULL). Errors as mpm_attention, plus
  * MPM_ERR_INVALID_ARG for dbias without bias.
  */
 size_t mpm_attention_backward_workspace_bytes(const mpm_attention_call* call);

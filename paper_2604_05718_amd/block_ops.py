@@ -197,7 +197,11 @@ def attention_backward(dout, q, k, v, out, lse, q_off=None, k_off=None, Nq=None,
     gs = [_heads(dq, "dq", q, rq, c.H), _heads(dk, "dk", q, rk, c.Hk), _heads(dv, "dv", q, rk, c.Hk)]
     dbias = torch.empty_like(bias) if bias is not None and with_dbias else None
     lib = _lib.load()
+    if dbias is None:  # (the size without the partial sums of dbias)
+        kept, c.bias = c.bias, None
     need = lib.mpm_attention_backward_workspace_bytes(_BYREF(c))
+    if dbias is None:
+        c.bias = kept
     ws = torch.empty((need,), dtype=torch.uint8, device=q.device)
     _lib.check("mpm_attention_backward", lib.mpm_attention_backward(
         _BYREF(c), *(_BYREF(x) for x in hs), _device(lse, "lse", torch.float32, q, 2 * rq * c.H), *(_BYREF(x) for x in gs),

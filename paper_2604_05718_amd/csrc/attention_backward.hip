@@ -788,7 +788,8 @@ hipError_t pick(const AttentionCall& a, const Inputs& in, const Grads& g, hipStr
 
 size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
 
-// The scratch regions' sizes, in order.
+// The scratch regions' sizes, in order (the last one for dbias only, so that a call without it has the others
+// where they are).
 struct Sizes {
     size_t delta, largest, repeats, parts;
 };
@@ -801,10 +802,10 @@ Sizes sizes(const AttentionCall& a)
 
 }  // namespace
 
-size_t attention_backward_bytes(const AttentionCall& a)
+size_t attention_backward_bytes(const AttentionCall& a, bool with_dbias)
 {
     const Sizes n = sizes(a);
-    return n.delta + n.largest + n.repeats + n.parts;
+    return n.delta + n.largest + n.repeats + (with_dbias ? n.parts : 0);
 }
 
 hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dout, const HeadRows& q,

@@ -841,7 +841,7 @@ int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_
 
 size_t mpm_attention_backward_workspace_bytes(const mpm_attention_call* call)
 {
-    return check_attention(call) == MPM_OK ? mpm::attention_backward_bytes(attention_call(call)) : 0;
+    return check_attention(call) == MPM_OK ? mpm::attention_backward_bytes(attention_call(call), call->bias) : 0;
 }
 
 int mpm_attention_backward(const mpm_attention_call* call, const mpm_heads* dout, const mpm_heads* q,
@@ -855,7 +855,7 @@ int mpm_attention_backward(const mpm_attention_call* call, const mpm_heads* dout
         if (!ok_heads(x, call->dt)) return MPM_ERR_INVALID_ARG;
     if (lse == nullptr || !aligned(lse, 8) || !aligned(dbias, 4) || (dbias && !call->bias)) return MPM_ERR_INVALID_ARG;
     const mpm::AttentionCall a = attention_call(call);
-    if ((s = check_workspace(ws, ws_bytes, mpm::attention_backward_bytes(a))) != MPM_OK) return s;
+    if ((s = check_workspace(ws, ws_bytes, mpm::attention_backward_bytes(a, dbias))) != MPM_OK) return s;
     MPM_LAUNCH_GATE();
     MPM_DATA_CHECK(checked_attention(call, as_stream(stream)));
     return hip_status(mpm::launch_attention_backward(a, heads(dout), heads(q), heads(k), heads(v), heads(out), lse,

@@ -166,8 +166,8 @@ int attention_few_splits(const AttentionCall& a);
 size_t attention_few_bytes(const AttentionCall& a);
 hipError_t launch_attention_few(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
                                 const HeadRows& out, float* lse, void* ws, hipStream_t stream);
-// Its gradients; ws holds attention_backward_bytes(a) bytes; dbias may be null.
-size_t attention_backward_bytes(const AttentionCall& a);
+// Its gradients; ws holds attention_backward_bytes(a, dbias != nullptr) bytes; dbias may be null.
+size_t attention_backward_bytes(const AttentionCall& a, bool with_dbias);
 hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dout, const HeadRows& q,
                                      const HeadRows& k, const HeadRows& v, const HeadRows& out, const float* lse,
                                      const HeadRows& dq, const HeadRows& dk, const HeadRows& dv, float* dbias, void* ws,

@@ -38,3 +38,17 @@ def test_images_in_the_middle_of_a_packed_tensor(dtype, biased, first):
         assert torch.all(got[:a] == 7) and torch.all(got[b:] == 7)
     assert torch.equal(lse[a:b], wl)
     assert g.dbias is None if not biased else torch.equal(g.dbias, w.dbias)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_gradients_without_the_bias_gradient(dtype):
+    """with_dbias=False: no dbias, in the smaller workspace, and the other gradients of the formulas."""
+    c = Case(dtype, [200, 33], None, 4, 2, 64, (16, 15), 15, "sorted", True, seed=310)
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, with_dbias=False, **c.kw())
+    torch.cuda.synchronize()
+    _, _, want = c.plain(grads=True)
+    assert g.dbias is None
+    for got, w in zip((g.dq, g.dk, g.dv), want):
+        assert ref.rel(got, w) <= BWD[dtype]
