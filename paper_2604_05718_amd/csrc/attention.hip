@@ -21,7 +21,9 @@ namespace {
 // What is taken from a query's scores (base 2) before the exponential need not be their maximum: floats
 // keep their precision at any scale. It is zero as long as the scores stay within this many powers of two
 // of it, so that most calls subtract nothing, and else follows the running maximum with that slack.
-constexpr float kSlack = 60.0f;
+// The slack comes out of the range of the values: the sums of 2^14 keys hold values up to 2^(128 - 14 - 16),
+// and the terms of weight 2^-24 beside the largest are normal numbers for values from 2^(16 + 24 - 126).
+constexpr float kSlack = 16.0f;
 
 template <class S, int SPLIT>
 constexpr int key_tile()

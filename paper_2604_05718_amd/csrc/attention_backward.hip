@@ -134,8 +134,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, H
 }
 
 // What is taken from a query's scores before the exponential: the maximum and the log of the sum
-// (`apart`), or their sum where it is small enough to hold both (its rounding, below 2^-18, is the
-// error of the exponent). A mask value such as -1e9 on every key makes the maximum too large for
+// (`apart`), or their sum where it is small enough to hold both (the log is at most 16, the forward's slack, and
+// 14 for the keys: the sum stays below 128 and its rounding, the error of the exponent, below 2^-18). A mask value such as -1e9 on every key makes the maximum too large for
 // that: then the two go one after the other, as in the forward pass. In bfloat16 calls the sum is
 // not subtracted at all: the score products start from minus it over the factor of the scores.
 constexpr float kJoinMost = 64.0f;

@@ -52,3 +52,25 @@ def test_gradients_without_the_bias_gradient(dtype):
     assert g.dbias is None
     for got, w in zip((g.dq, g.dk, g.dv), want):
         assert ref.rel(got, w) <= BWD[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [2.0 ** 93, 1e21, 1e-20, 2.0 ** -80])
+@pytest.mark.parametrize("shift", [-41.0, -11.0, 11.0, 41.0])
+def test_values_of_any_size(dtype, size, shift):
+    """Values far from one under scores far from zero (shift: every score's, in nats): the sums before the
+    division neither overflow nor sink into denormals, in the form for few queries too. The exponent's error
+    is 2^-24 of the scores, as in test_large_scores."""
+    c = Case(dtype, [70, 3], [300, 2000], 2, 2, 32, (50, 50), 49, "sorted", True, seed=320)
+    c.k_bias = torch.full((2300,), shift)
+    c.v = (c.v.float() * size).to(dtype)
+    print(f"values of {size} at {shift}, {dtype}", flush=True)
+    q, k, v = c.dev()
+    out = mpm.attention(q, k, v, **c.kw())
+    few = dict(c.kw(), q_off=offsets([5, 0]).to(DEV), Nq=5, q_pos=c.q_pos[:5].contiguous().to(DEV))
+    some = mpm.attention(q[:5], k, v, **few)
+    torch.cuda.synchronize()
+    want, _ = c.plain()
+    tol = FWD[BF] if dtype == BF else (144 + 4 * abs(shift)) * 2.0 ** -24
+    assert torch.isfinite(out).all() and ref.rel(out, want) <= tol
+    assert torch.isfinite(some).all() and ref.rel(some, want[:5]) <= tol
