@@ -28,10 +28,12 @@ enum SumKind : int {
     // most 256 max|dP - D|, as probabilities add to one. The largest term is 2^21 to 2^22 units.
     kSum32 = 1,
     // 64-bit fixed point, the largest |dP - D| 2^45 to 2^46 units: float32, or offsets held to the
-    // span (whose sums of many terms would leave 32 bits too few), where the table fits.
+    // span (whose sums of many terms would leave 32 bits too few).
     kSum64 = 2,
-    // Float32, one half of a wave after the other, so that the order of the additions is fixed.
-    kSumTurns = 3
+    // ... where biases and sums do not fit LDS together (more than 103 x 103 entries): the sums in LDS, the
+    // biases read from memory, on their way during a tile's products. A step of 3 images of 4096 tokens, 16 heads
+    // of 64, bfloat16, 111 x 111 entries: 2.2 ms.
+    kSum64Alone = 3
 };
 
 template <class S, int DH, int SPLIT>
@@ -389,11 +391,11 @@ __host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W, int g
 {
     if (bias == kBiasNone) return 0;
     if (sum == kSum32) return gap + (size_t)W * W * 4;
-    return (size_t)W * W * (sum == kSumNone ? 4 : sum == kSum64 ? 12 : 8);
+    return (size_t)W * W * (sum == kSumNone ? 4 : sum == kSum64 ? 12 : 8);  // (kSum64Alone: the sums)
 }
 
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: the biases and then the sums
-// (kSum64: the sums first). Three products a tile, and an LDS atomic a score: 3 images of 4096 tokens, 16
+// (kSum64: the sums first; kSum64Alone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096 tokens, 16
 // heads of 64, bfloat16, 468 us, 660 TFLOP/s; 32 of about 717, 12 heads, 206 us; float32, 4 of about 460, 6
 // heads, 73 us. Products 31% of the busy cycles, vector instructions 44%, the atomics most of the rest.
 template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT, int GAP>
@@ -411,9 +413,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     static_assert(32 * WAVES <= kMaxRows, "the fixed point's range");
     extern __shared__ __align__(16) uint8_t lds[];
     const int W = 2 * a.span + 1, W2 = W * W;
+    constexpr bool k64 = SUM == kSum64 || SUM == kSum64Alone;
     uint8_t* tables = lds + BUFS * kBuffer;
-    float* table = reinterpret_cast<float*>(tables + (SUM == kSum64 ? (size_t)W2 * 8 : 0));
-    const int table_at = lds_address(table);
+    float* table = reinterpret_cast<float*>(tables + (k64 ? (size_t)W2 * 8 : 0));
+    const int table_at = SUM == kSum64Alone ? 0 : lds_address(table);
 
     int blk, pair;
     if (!block_item(blocks, (long)a.B * a.H, &blk, &pair)) return;
@@ -461,7 +464,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     // The power of two that score gradients are multiplied by: kSum32 by way of the probabilities'
     // exponents (free, and bfloat16 does not see the exponents' rounding), kSum64 as they are summed.
     int lg = 0;
-    if (SUM == kSum32 || SUM == kSum64) {
+    if (SUM == kSum32 || k64) {
         const uint32_t* most = w.largest + 2 * ((long)b * a.H + hd);
         const bool once = SUM == kSum32 && w.repeats[b] == 0;
         lg = __builtin_amdgcn_readfirstlane(raise_to(__uint_as_float(most[once ? 0 : 1]), SUM == kSum32 ? 22 : 46));
@@ -469,7 +472,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     const float2 stat = live ? lse[qrow * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
     const bool apart = !can_start<S>(c) || __any(too_large(stat));
     const float2 tk = taken(stat, apart, c, SUM == kSum32 ? (float)lg : 0.0f);
-    const float raise = SUM == kSum64 ? __builtin_ldexpf(1.0f, lg) : 1.0f;
+    const float raise = k64 ? __builtin_ldexpf(1.0f, lg) : 1.0f;
     const float nd = live ? -w.delta[((long)b * a.Nq + qi) * a.H + hd] : 0.0f;
     f32x16 s0, dp0;
 #pragma unroll
@@ -478,15 +481,14 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         dp0[r] = nd;
     }
     int qcode = 0;
+    const float* bias = BIAS != kBiasNone ? a.bias + (long)hd * W2 : nullptr;
     if (BIAS != kBiasNone) {
-        load_table<THREADS>(table, a.bias + (long)hd * W2, W2, t);
+        if (SUM != kSum64Alone) load_table<THREADS>(table, bias, W2, t);
         qcode = query_code<BIAS>(qpos, a.grid_h, a.grid_w, a.span, W, table_at);
         if (SUM == kSum32)
             for (int e = t; e < W2; e += THREADS) reinterpret_cast<int32_t*>(tables + GAP)[e] = 0;
-        if (SUM == kSum64)
+        if (k64)
             for (int e = t; e < W2; e += THREADS) reinterpret_cast<unsigned long long*>(tables)[e] = 0;
-        if (SUM == kSumTurns)
-            for (int e = t; e < W2; e += THREADS) table[W2 + e] = 0.0f;
     }
     f32x16 gq[DH / 32];
 #pragma unroll
@@ -505,29 +507,39 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         if (more) load(k0 + KT);
         auto compute = [&](int u) {
             f32x16 s, dp;
+            int entry[16];
+            float beside[16];  // kSum64Alone: the biases, on their way during the products
+            auto find = [&]() {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const i32x4 kc = *reinterpret_cast<const i32x4*>(codes + 32 * u + 8 * g + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int at = bias_entry<BIAS>(qcode, kc[e], a.span, W, table_at);
+                        entry[4 * g + e] = at;
+                        if (SUM == kSum64Alone)
+                            beside[4 * g + e] = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(bias) + at);
+                    }
+                }
+            };
+            if constexpr (SUM == kSum64Alone) find();
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
                 if (S::kBytes == 4 && st > 0 && 16 * st >= a.dh) continue;
                 s = mma(rows_frag<S, DH>(kt, 32 * u + l32, st, h), qf[st], st == 0 ? s0 : s);
                 dp = mma(rows_frag<S, DH>(vt, 32 * u + l32, st, h), of[st], st == 0 ? dp0 : dp);
             }
-            int entry[16];
+            if constexpr (BIAS != kBiasNone && SUM != kSum64Alone) find();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int at = 32 * u + 8 * g + 4 * h;
-                i32x4 kc = {0, 0, 0, 0};
                 f32x4 kb = {0, 0, 0, 0};
-                if (BIAS != kBiasNone) kc = *reinterpret_cast<const i32x4*>(codes + at);
-                if (KB) kb = *reinterpret_cast<const f32x4*>(kbs + at);
+                if (KB) kb = *reinterpret_cast<const f32x4*>(kbs + 32 * u + 8 * g + 4 * h);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float x = s[4 * g + e];
-                    if (BIAS != kBiasNone) {
-                        entry[4 * g + e] = bias_entry<BIAS>(qcode, kc[e], a.span, W, table_at);
-                        x = fmaf(x, c, lds_at(entry[4 * g + e]));
-                    } else {
-                        x *= c;
-                    }
+                    if (BIAS == kBiasNone) x *= c;
+                    else if (SUM == kSum64Alone) x = fmaf(x, c, to_log2(beside[4 * g + e]));
+                    else x = fmaf(x, c, lds_at(entry[4 * g + e]));
                     if (KB) x += kb[e];
                     s[4 * g + e] = x;
                 }
@@ -563,27 +575,15 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                                            __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
             }
-            if (SUM == kSum64) {
+            if (k64) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     __hip_atomic_fetch_add(
                         (lds_long*)(uintptr_t)(uint32_t)((entry[r] - table_at) * 2 + lds_address(tables)),
                         (unsigned long long)(long long)(dp[r] * raise), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             }
-            if (SUM == kSumTurns) {
-                for (int turn = 0; turn < 2 * WAVES; ++turn) {
-                    if (t / kWave == turn / 2 && h == turn % 2 && live) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            __hip_atomic_fetch_add((__attribute__((address_space(3))) float*)(uintptr_t)(uint32_t)(
-                                                       entry[r] + W2 * 4),
-                                                   dp[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                    }
-                    __syncthreads();
-                }
-            }
         };
-        if (works || SUM == kSumTurns) {  // (turns have barriers)
+        if (works) {
             if constexpr (SPLIT == 1) {
                 // Unrolled for constant LDS offsets; one tile's registers at a time.
 #pragma unroll
@@ -620,8 +620,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         for (int e = t; e < W2; e += THREADS) {
             float x;
             if (SUM == kSum32) x = (float)reinterpret_cast<const int32_t*>(tables + GAP)[e] * back;
-            else if (SUM == kSum64) x = (float)reinterpret_cast<const long long*>(tables)[e] * back;
-            else x = table[W2 + e];
+            else x = (float)reinterpret_cast<const long long*>(tables)[e] * back;
             part[e] = any_bad ? __builtin_nanf("") : x;
         }
     }
@@ -750,7 +749,7 @@ hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, 
             else e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapLarge>(a, in, g, st);
         } else if (tiles + table_bytes(BIAS, kSum64, W, 0) <= kLdsBytes)
             e = launch_queries<S, DH, BIAS, KB, kSum64, WAVES, SPLIT>(a, in, g, st);
-        else e = launch_queries<S, DH, BIAS, KB, kSumTurns, WAVES, SPLIT>(a, in, g, st);
+        else e = launch_queries<S, DH, BIAS, KB, kSum64Alone, WAVES, SPLIT>(a, in, g, st);
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(bias_parts_kernel, dim3((unsigned)((W * W + kJoinEntries - 1) / kJoinEntries), (unsigned)a.H),
                            dim3(kJoinEntries * kJoinWays), 0, st, a, g.w.parts, query_blocks(a), 32 * WAVES / SPLIT, g.dbias);

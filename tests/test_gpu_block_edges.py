@@ -74,3 +74,27 @@ def test_values_of_any_size(dtype, size, shift):
     tol = FWD[BF] if dtype == BF else (144 + 4 * abs(shift)) * 2.0 ** -24
     assert torch.isfinite(out).all() and ref.rel(out, want) <= tol
     assert torch.isfinite(some).all() and ref.rel(some, want[:5]) <= tol
+
+
+ORDERS = [(F32, 63, (64, 64)), (F32, 55, (64, 64)), (F32, 53, (200, 50)), (F32, 23, (24, 24)), (F32, 9, (24, 24)),
+          (BF, 55, (64, 64)), (BF, 53, (200, 50)), (BF, 9, (24, 24))]
+
+
+@pytest.mark.parametrize("dtype,span,grid", ORDERS)
+def test_bias_gradient_does_not_depend_on_the_order_of_keys(dtype, span, grid):
+    """The same keys in another order, with the call's own output and statistics: every score gradient is the
+    same number, and so has to be their sum at every offset, bit for bit."""
+    c = Case(dtype, [60], [500], 2, 1, 64, grid, span, "sorted", False, seed=330)
+    print(f"order of keys, span {span}, grid {grid}, {dtype}", flush=True)
+    q, k, v = c.dev()
+    kw = c.kw()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **kw)
+    order = torch.randperm(500, generator=torch.Generator().manual_seed(1)).to(DEV)
+    a = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **kw)
+    kw["k_pos"] = kw["k_pos"][order].contiguous()
+    b = mpm.attention_backward(c.dout.to(DEV), q, k[order], v[order], out, lse, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(a.dk[order], b.dk) and torch.equal(a.dv[order], b.dv)
+    _, _, want = c.plain(grads=True)
+    assert ref.rel(a.dbias, want[3]) <= BWD[dtype]
+    assert torch.equal(a.dbias, b.dbias)
