@@ -8,32 +8,27 @@
 // instead of the five of a single pass, for results that are the same on every run.
 //
 // dbias is a histogram: every score gradient belongs to the offset of its pair. Each workgroup of
-// the query kernel keeps a table of all offsets in LDS and adds to it with integer atomics, whose
-// sum does not depend on their order: score gradients are multiplied by a power of two for which
-// no sum can pass the integer's range, found from the largest ones, which the key kernel, running
-// first, leaves for every image and head (SumKind).
+// the query kernel keeps a table of all offsets in LDS and adds to it with 64-bit integer atomics, whose
+// sum does not depend on their order. The unit is a power of two for which no sum can pass the integer's
+// range, found from the largest |dS|, which the key kernel, running first, leaves for every image and head:
+// at most 2^-39 of it (256 queries and 16384 keys; 2^-44 for 128 and 1024), so that far offsets under sharp
+// attention keep their gradients. (32 bits cost 2% less of a step of 32 images of about 717 tokens, 9% less of one of 3 of 4096 with
+// 127 x 127 entries, and lose every term below 2^-23 of the largest.)
 #include "mpm_attn.h"
 
 namespace mpm {
 namespace {
 
 constexpr int kDeltaThreads = 256;
-constexpr int kMaxRows = 256;  // query rows of a workgroup at most
 
 // How the query kernel sums dbias.
 enum SumKind : int {
     kSumNone = 0,
-    // 32-bit fixed point (bfloat16, no offset held to the span). Where an image's keys have
-    // distinct positions, a query meets an offset once, so a sum is at most 256 max|dS|; otherwise at
-    // most 256 max|dP - D|, as probabilities add to one. The largest term is 2^21 to 2^22 units.
-    kSum32 = 1,
-    // 64-bit fixed point, the largest |dP - D| 2^45 to 2^46 units: float32, or offsets held to the
-    // span (whose sums of many terms would leave 32 bits too few).
-    kSum64 = 2,
-    // ... where biases and sums do not fit LDS together (more than 103 x 103 entries): the sums in LDS, the
-    // biases read from memory, on their way during a tile's products. A step of 3 images of 4096 tokens, 16 heads
-    // of 64, bfloat16, 111 x 111 entries: 2.2 ms.
-    kSum64Alone = 3
+    kSumBeside = 1,  // biases and sums in LDS
+    // Tables too wide for both (more than 103 x 103 entries): the sums in LDS, the biases read from memory, on
+    // their way during a tile's products. A step of 3 images of 4096 tokens, 16 heads of 64, bfloat16: 1.46 ms
+    // with 127 x 127 entries, 1.99 with 111 x 111 (offsets held to the span).
+    kSumAlone = 2
 };
 
 template <class S, int DH, int SPLIT>
@@ -85,13 +80,12 @@ constexpr int waves_per_simd()
     return S::kBytes == 2 ? 2 : 1;
 }
 
-// What the kernels leave for each other: D of every query and head, the largest |dS| and |dP - D| of
-// every image and head (as bits), and whether an image's keys repeat a position. D is kept by image slot, not by
+// What the kernels leave for each other: D of every query and head, the largest |dS| of every image and head
+// (as bits). D is kept by image slot, not by
 // packed row: the packed offsets of a call on some images of a larger tensor start past zero.
 struct Scratch {
     float* delta;       // [B][Nq][H]
-    uint32_t* largest;  // [B][H][2]
-    int32_t* repeats;   // [B]
+    uint32_t* largest;  // [B][H]
     float* parts;       // [pair][block][W * W]
 };
 
@@ -109,10 +103,8 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, H
 {
     constexpr int kLanes = 8;
     const int b = blockIdx.y;
-    if (blockIdx.x == 0) {
-        for (int i = threadIdx.x; i < 2 * a.H; i += kDeltaThreads) w.largest[2L * b * a.H + i] = 0;
-        if (threadIdx.x == 0) w.repeats[b] = 0;
-    }
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < a.H; i += kDeltaThreads) w.largest[(long)b * a.H + i] = 0;
     const Rows rq = image_rows(a.q_off, b, a.Nq);
     const long item = ((long)blockIdx.x * kDeltaThreads + threadIdx.x) / kLanes;
     const int j = threadIdx.x % kLanes;
@@ -150,18 +142,18 @@ __device__ __forceinline__ bool can_start(float c)
 }
 
 // Two numbers for a query with statistics l: (where the score products start, 0), or, apart, what is
-// subtracted first and second. No key: probabilities of zero. lg: a power of two they are raised by.
-__device__ __forceinline__ float2 taken(float2 l, bool apart, float c, float lg)
+// subtracted first and second. No key: probabilities of zero.
+__device__ __forceinline__ float2 taken(float2 l, bool apart, float c)
 {
     const bool none = l.x == -__builtin_inff();
-    if (apart) return none ? make_float2(__builtin_inff(), 0.0f) : make_float2(l.x, l.y - lg);
-    return make_float2(none ? -__builtin_inff() : (lg - l.x - l.y) / c, 0.0f);
+    if (apart) return none ? make_float2(__builtin_inff(), 0.0f) : l;
+    return make_float2(none ? -__builtin_inff() : -(l.x + l.y) / c, 0.0f);
 }
 
 // dK and dV of WAVES x 32 keys of one key head: all queries of all heads that share it. SPLIT 2 (here and
 // below): two waves share 32 rows, each taking every other 32 of the other side, and add up at the end.
 // Four products a tile, of which two read their operand transposed from LDS. 3 images of 4096 tokens,
-// 16 heads of 64, bfloat16: 630 us, 655 TFLOP/s; 32 of about 717, 12 heads: 221 us. Products 28% of the
+// 16 heads of 64, bfloat16: 589 us, 700 TFLOP/s; 32 of about 717, 12 heads: 219 us. Products 28% of the
 // busy cycles, vector instructions 40%, LDS 34%, and a wave waits for one of them half of its time: two
 // waves a SIMD are what the fragments and two gradient tiles of a wave leave room for.
 template <class S, int DH, int BIAS, bool KB, int WAVES, int SPLIT>
@@ -197,12 +189,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
     int kcode = 0;
     const bool live = exists && kb > -__builtin_inff();
     // (all of the first loads are under way before one is waited for)
-    int own = 0, next = 0;  // this key's position and the next one's
-    const bool pairs_next = hk == 0 && ki + 1 < rk.count;
-    if (BIAS != kBiasNone) {
-        own = exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0;
-        next = pairs_next ? (a.k_pos ? a.k_pos[rk.first + ki + 1] : ki + 1) : 0;
-    }
+    int own = 0;  // this key's position
+    if (BIAS != kBiasNone) own = exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0;
 
     Frag kf[DH / 16], vf[DH / 16];
     const long krow = rk.first + (exists ? ki : 0);
@@ -238,7 +226,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
                 float* first = reinterpret_cast<float*>(codes + QT);
                 if (BIAS != kBiasNone) codes[t] = query_code<BIAS>(pos, a.grid_h, a.grid_w, a.span, W, table_at);
                 const bool apart = !start || __any(too_large(stat));
-                const float2 tk = taken(stat, apart, c, 0.0f);
+                const float2 tk = taken(stat, apart, c);
                 first[t] = tk.x;
                 first[QT + t] = tk.y;
                 first[2 * QT + t] = -del;
@@ -254,7 +242,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
         }
         store(0);
         __syncthreads();
-        float most_ds = 0.0f, most_dp = 0.0f;
+        float most = 0.0f;
         for (int q0 = 0, buf = 0; q0 < rq.count; q0 += QT, buf ^= BUFS - 1) {
             const uint8_t* qt = lds + buf * kBuffer;
             const uint8_t* ot = qt + Staged::kTileBytes;
@@ -308,9 +296,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     s[r] = __builtin_amdgcn_exp2f(s[r]);
-                    if (BIAS != kBiasNone) most_dp = fmaxf(most_dp, fabsf(dp[r]));
                     dp[r] *= s[r];
-                    if (BIAS != kBiasNone) most_ds = fmaxf(most_ds, fabsf(dp[r]));
+                    if (BIAS != kBiasNone) most = fmaxf(most, fabsf(dp[r]));
                 }
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
@@ -332,17 +319,12 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
             __syncthreads();
         }
         if (BIAS != kBiasNone) {
-            if (!live) most_ds = most_dp = 0.0f;
+            if (!live) most = 0.0f;
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                most_ds = fmaxf(most_ds, __shfl_xor(most_ds, o));
-                most_dp = fmaxf(most_dp, __shfl_xor(most_dp, o));
-            }
-            if (lane == 0) {
-                uint32_t* at = w.largest + 2 * ((long)b * a.H + hd);
-                __hip_atomic_fetch_max(at, __float_as_uint(most_ds), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __hip_atomic_fetch_max(at + 1, __float_as_uint(most_dp), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
+            for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+            if (lane == 0)
+                __hip_atomic_fetch_max(w.largest + (long)b * a.H + hd, __float_as_uint(most), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
         }
     }
 
@@ -357,11 +339,6 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
         if (share == 1) return;
         take(mine, gk, lane);
         take(mine + DH / 32 * 16 * kWave, gv, lane);
-    }
-    if (BIAS != kBiasNone && pairs_next && h == 0) {
-        const int cells = a.grid_h * a.grid_w;
-        if (min(max(own, 0), cells - 1) >= min(max(next, 0), cells - 1))
-            __hip_atomic_fetch_or(w.repeats + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     // A dropped key's gradients are zero, whatever its rows hold.
     if (!live) {
@@ -380,25 +357,21 @@ __device__ __forceinline__ int raise_to(float x, int bits)
     if (!(x > 0.0f) || !(x < __builtin_inff())) return 0;
     return min(max(bits - (__builtin_amdgcn_frexp_expf(x)), -100), 100);
 }
-
-// kSum32: the sums lie a constant behind the biases, so that one address serves both (pairs of a bias and
-// a sum would need one address too, but met in the banks: 5% of the kernel). Tables of up to 63 x 63,
-// 77 x 77 (the widest of the four-wave form) and 127 x 127 entries.
-constexpr int kGapSmall = 15888, kGapMiddle = 23728, kGapLarge = 64528;
+// Bits of a term, so that `terms` of them stay within 62 (and one within the 51 that a double's fixed point holds).
+__device__ __forceinline__ int term_bits(int terms) { return min(50, 62 - (32 - __builtin_clz(max(terms - 1, 1)))); }
 
 // Bytes of the query kernel's tables.
-__host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W, int gap)
+__host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
 {
     if (bias == kBiasNone) return 0;
-    if (sum == kSum32) return gap + (size_t)W * W * 4;
-    return (size_t)W * W * (sum == kSumNone ? 4 : sum == kSum64 ? 12 : 8);  // (kSum64Alone: the sums)
+    return (size_t)W * W * (sum == kSumNone ? 4 : sum == kSumBeside ? 12 : 8);
 }
 
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: the biases and then the sums
-// (kSum64: the sums first; kSum64Alone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096 tokens, 16
-// heads of 64, bfloat16, 468 us, 660 TFLOP/s; 32 of about 717, 12 heads, 206 us; float32, 4 of about 460, 6
-// heads, 73 us. Products 31% of the busy cycles, vector instructions 44%, the atomics most of the rest.
-template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT, int GAP>
+// (the sums first; kSumAlone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096 tokens, 16
+// heads of 64, bfloat16, 669 us, 460 TFLOP/s (biases from memory); 32 of about 717, 12 heads, 238 us; float32, 4 of
+// about 460, 6 heads, 71 us.
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                         HeadRows k, HeadRows v,
                                                                         const float2* __restrict__ lse, Scratch w,
@@ -407,16 +380,14 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     constexpr int THREADS = WAVES * kWave, KT = tile_rows<S, DH, SPLIT>(), BUFS = buffers<S, DH>();
     typedef PairStage<S, DH, KT, THREADS, true> Staged;
     typedef typename FragOf<S>::type Frag;
-    typedef __attribute__((address_space(3))) int32_t lds_int;
     typedef __attribute__((address_space(3))) unsigned long long lds_long;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     constexpr int kBuffer = tile_bytes<S, DH, SPLIT>() + KT * 8;
-    static_assert(32 * WAVES <= kMaxRows, "the fixed point's range");
     extern __shared__ __align__(16) uint8_t lds[];
     const int W = 2 * a.span + 1, W2 = W * W;
-    constexpr bool k64 = SUM == kSum64 || SUM == kSum64Alone;
-    uint8_t* tables = lds + BUFS * kBuffer;
-    float* table = reinterpret_cast<float*>(tables + (k64 ? (size_t)W2 * 8 : 0));
-    const int table_at = SUM == kSum64Alone ? 0 : lds_address(table);
+    unsigned long long* sums = reinterpret_cast<unsigned long long*>(lds + BUFS * kBuffer);
+    float* table = reinterpret_cast<float*>(sums + (SUM == kSumNone ? 0 : W2));
+    const int table_at = SUM == kSumAlone ? 0 : lds_address(table), sums_at = lds_address(sums) - 2 * table_at;
 
     int blk, pair;
     if (!block_item(blocks, (long)a.B * a.H, &blk, &pair)) return;
@@ -461,18 +432,15 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)hd * q.head) * S::kBytes, a.dh, live, h);
     load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
 
-    // The power of two that score gradients are multiplied by: kSum32 by way of the probabilities'
-    // exponents (free, and bfloat16 does not see the exponents' rounding), kSum64 as they are summed.
+    // Score gradients in fixed point: added to 1.5 x 2^(52 - lg), a double's bits count units of 2^-lg.
     int lg = 0;
-    if (SUM == kSum32 || k64) {
-        const uint32_t* most = w.largest + 2 * ((long)b * a.H + hd);
-        const bool once = SUM == kSum32 && w.repeats[b] == 0;
-        lg = __builtin_amdgcn_readfirstlane(raise_to(__uint_as_float(most[once ? 0 : 1]), SUM == kSum32 ? 22 : 46));
-    }
+    if (SUM != kSumNone)
+        lg = __builtin_amdgcn_readfirstlane(raise_to(__uint_as_float(w.largest[(long)b * a.H + hd]),
+                                                     term_bits(32 * WAVES / SPLIT * rk.count)));
+    const double middle = __builtin_ldexp(1.5, 52 - lg);
     const float2 stat = live ? lse[qrow * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
     const bool apart = !can_start<S>(c) || __any(too_large(stat));
-    const float2 tk = taken(stat, apart, c, SUM == kSum32 ? (float)lg : 0.0f);
-    const float raise = k64 ? __builtin_ldexpf(1.0f, lg) : 1.0f;
+    const float2 tk = taken(stat, apart, c);
     const float nd = live ? -w.delta[((long)b * a.Nq + qi) * a.H + hd] : 0.0f;
     f32x16 s0, dp0;
 #pragma unroll
@@ -483,12 +451,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     int qcode = 0;
     const float* bias = BIAS != kBiasNone ? a.bias + (long)hd * W2 : nullptr;
     if (BIAS != kBiasNone) {
-        if (SUM != kSum64Alone) load_table<THREADS>(table, bias, W2, t);
+        if (SUM != kSumAlone) load_table<THREADS>(table, bias, W2, t);
         qcode = query_code<BIAS>(qpos, a.grid_h, a.grid_w, a.span, W, table_at);
-        if (SUM == kSum32)
-            for (int e = t; e < W2; e += THREADS) reinterpret_cast<int32_t*>(tables + GAP)[e] = 0;
-        if (k64)
-            for (int e = t; e < W2; e += THREADS) reinterpret_cast<unsigned long long*>(tables)[e] = 0;
+        if (SUM != kSumNone)
+            for (int e = t; e < W2; e += THREADS) sums[e] = 0;
     }
     f32x16 gq[DH / 32];
 #pragma unroll
@@ -508,7 +474,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         auto compute = [&](int u) {
             f32x16 s, dp;
             int entry[16];
-            float beside[16];  // kSum64Alone: the biases, on their way during the products
+            float beside[16];  // kSumAlone: the biases, on their way during the products
             auto find = [&]() {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -517,19 +483,19 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                     for (int e = 0; e < 4; ++e) {
                         const int at = bias_entry<BIAS>(qcode, kc[e], a.span, W, table_at);
                         entry[4 * g + e] = at;
-                        if (SUM == kSum64Alone)
+                        if (SUM == kSumAlone)
                             beside[4 * g + e] = *reinterpret_cast<const float*>(reinterpret_cast<const uint8_t*>(bias) + at);
                     }
                 }
             };
-            if constexpr (SUM == kSum64Alone) find();
+            if constexpr (SUM == kSumAlone) find();
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
                 if (S::kBytes == 4 && st > 0 && 16 * st >= a.dh) continue;
                 s = mma(rows_frag<S, DH>(kt, 32 * u + l32, st, h), qf[st], st == 0 ? s0 : s);
                 dp = mma(rows_frag<S, DH>(vt, 32 * u + l32, st, h), of[st], st == 0 ? dp0 : dp);
             }
-            if constexpr (BIAS != kBiasNone && SUM != kSum64Alone) find();
+            if constexpr (BIAS != kBiasNone && SUM != kSumAlone) find();
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 f32x4 kb = {0, 0, 0, 0};
@@ -538,7 +504,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                 for (int e = 0; e < 4; ++e) {
                     float x = s[4 * g + e];
                     if (BIAS == kBiasNone) x *= c;
-                    else if (SUM == kSum64Alone) x = fmaf(x, c, to_log2(beside[4 * g + e]));
+                    else if (SUM == kSumAlone) x = fmaf(x, c, to_log2(beside[4 * g + e]));
                     else x = fmaf(x, c, lds_at(entry[4 * g + e]));
                     if (KB) x += kb[e];
                     s[4 * g + e] = x;
@@ -566,21 +532,15 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                 for (int d = 0; d < DH / 32; ++d)
                     if (S::kBytes == 2 || 32 * d < a.dh) gq[d] = mma(cols_frag<S, DH>(kt, 32 * u + 16 * st, 32 * d, lane), ds, gq[d]);
             }
-            if (SUM == kSum32) {
+            if (SUM != kSumNone) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    int n;  // to the nearest
-                    asm("v_cvt_rpi_i32_f32 %0, %1" : "=v"(n) : "v"(dp[r]));
-                    __hip_atomic_fetch_add((lds_int*)(uintptr_t)(uint32_t)entry[r] + GAP / 4, n, __ATOMIC_RELAXED,
+                    const u32x2 d = __builtin_bit_cast(u32x2, (double)dp[r] + middle);
+                    const u32x2 n = {d[0], d[1] - (uint32_t)__double2hiint(middle)};  // (middle's low word is zero)
+                    __hip_atomic_fetch_add((lds_long*)(uintptr_t)(uint32_t)(entry[r] * 2 + sums_at),
+                                           __builtin_bit_cast(unsigned long long, n), __ATOMIC_RELAXED,
                                            __HIP_MEMORY_SCOPE_WORKGROUP);
                 }
-            }
-            if (k64) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    __hip_atomic_fetch_add(
-                        (lds_long*)(uintptr_t)(uint32_t)((entry[r] - table_at) * 2 + lds_address(tables)),
-                        (unsigned long long)(long long)(dp[r] * raise), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             }
         };
         if (works) {
@@ -617,14 +577,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
             for (int r = 0; r < 16; ++r) bad |= !(fabsf(gq[d][r]) < __builtin_inff());
         const bool any_bad = __syncthreads_or(bad && live && share == 0);
         float* part = w.parts + ((long)pair * blocks + blk) * W2;
-        for (int e = t; e < W2; e += THREADS) {
-            float x;
-            if (SUM == kSum32) x = (float)reinterpret_cast<const int32_t*>(tables + GAP)[e] * back;
-            else x = (float)reinterpret_cast<const long long*>(tables)[e] * back;
-            part[e] = any_bad ? __builtin_nanf("") : x;
-        }
+        for (int e = t; e < W2; e += THREADS)
+            part[e] = any_bad ? __builtin_nanf("") : (float)(long long)sums[e] * back;
     }
-    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, SUM == kSum32 ? a.scale * back : a.scale, a.dh, live && share == 0, h, S{});
+    store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale, a.dh, live && share == 0, h, S{});
 }
 
 // dbias[head][e] = the workgroups' parts, in the order of images and query blocks: four threads an
@@ -664,15 +620,11 @@ struct Inputs {
     const float2* lse;
 };
 
-// Eight waves where the tables leave LDS for one workgroup of the query kernel only. With 63 x 63
-// entries four waves are better (either kernel of 32 images of about 717 tokens: 219 and 224 us with
+// Eight waves where the query kernel's tables (12 bytes an entry beside 33 KB of tiles) leave LDS for one
+// workgroup only. With 63 x 63 entries, the widest for two, four waves are better (summed in 32 bits, either kernel of 32 images of about 717 tokens: 219 and 224 us with
 // four, 248 and 255 with eight).
-constexpr long kLargeTable = kGapMiddle;
-bool large_table(const AttentionCall& a)
-{
-    const long W = 2 * a.span + 1;
-    return a.dt == kBf16 && a.dh <= 64 && a.bias && W * W * 4 > kLargeTable;
-}
+constexpr int kWidestTwice = 63;
+bool large_table(const AttentionCall& a) { return a.dt == kBf16 && a.dh <= 64 && a.bias && 2 * a.span + 1 > kWidestTwice; }
 // Waves of a workgroup and how many share a tile: split where workgroups of 128 rows would leave
 // compute units idle (and the tables of a float32 call leave room for the longer tiles). A whole step,
 // not split / split: bfloat16, 12 heads of up to 1024 tokens, 72 workgroups 118 / 103 us, 288 159 / 174, 576
@@ -711,15 +663,15 @@ hipError_t launch_keys(const AttentionCall& a, const Inputs& in, const Grads& g,
     return hipGetLastError();
 }
 
-template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT, int GAP = 0>
+template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 hipError_t launch_queries(const AttentionCall& a, const Inputs& in, const Grads& g, hipStream_t st)
 {
     const int blocks = query_blocks(a);
     const size_t bytes = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8) +
-                         table_bytes(BIAS, SUM, 2 * a.span + 1, GAP);
+                         table_bytes(BIAS, SUM, 2 * a.span + 1);
     const long grid = block_grid((long)a.B * a.H, blocks);
     if (grid * WAVES * kWave > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES, SPLIT, GAP>;
+    auto kernel = query_gradient_kernel<S, DH, BIAS, KB, SUM, WAVES, SPLIT>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(WAVES * kWave), bytes, st, a, in.dout, in.q, in.k, in.v,
@@ -742,14 +694,9 @@ hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, 
     } else {
         constexpr size_t tiles = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8);
         if (!g.dbias) return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES, SPLIT>(a, in, g, st);
-        if constexpr (S::kBytes == 2 && BIAS == kBiasGrid) {
-            if constexpr (WAVES == 8) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapLarge>(a, in, g, st);
-            else if (W <= 63) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapSmall>(a, in, g, st);
-            else if (DH == 64) e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapMiddle>(a, in, g, st);
-            else e = launch_queries<S, DH, BIAS, KB, kSum32, WAVES, SPLIT, kGapLarge>(a, in, g, st);
-        } else if (tiles + table_bytes(BIAS, kSum64, W, 0) <= kLdsBytes)
-            e = launch_queries<S, DH, BIAS, KB, kSum64, WAVES, SPLIT>(a, in, g, st);
-        else e = launch_queries<S, DH, BIAS, KB, kSum64Alone, WAVES, SPLIT>(a, in, g, st);
+        if (tiles + table_bytes(BIAS, kSumBeside, W) <= kLdsBytes)
+            e = launch_queries<S, DH, BIAS, KB, kSumBeside, WAVES, SPLIT>(a, in, g, st);
+        else e = launch_queries<S, DH, BIAS, KB, kSumAlone, WAVES, SPLIT>(a, in, g, st);
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(bias_parts_kernel, dim3((unsigned)((W * W + kJoinEntries - 1) / kJoinEntries), (unsigned)a.H),
                            dim3(kJoinEntries * kJoinWays), 0, st, a, g.w.parts, query_blocks(a), 32 * WAVES / SPLIT, g.dbias);
@@ -790,12 +737,12 @@ size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
 // The scratch regions' sizes, in order (the last one for dbias only, so that a call without it has the others
 // where they are).
 struct Sizes {
-    size_t delta, largest, repeats, parts;
+    size_t delta, largest, parts;
 };
 Sizes sizes(const AttentionCall& a)
 {
     const size_t W = 2 * a.span + 1;
-    return Sizes{aligned256((size_t)a.B * a.Nq * a.H * 4), aligned256((size_t)a.B * a.H * 8), aligned256((size_t)a.B * 4),
+    return Sizes{aligned256((size_t)a.B * a.Nq * a.H * 4), aligned256((size_t)a.B * a.H * 4),
                  a.bias ? aligned256((size_t)a.B * a.H * query_blocks(a) * W * W * 4) : 0};
 }
 
@@ -804,7 +751,7 @@ Sizes sizes(const AttentionCall& a)
 size_t attention_backward_bytes(const AttentionCall& a, bool with_dbias)
 {
     const Sizes n = sizes(a);
-    return n.delta + n.largest + n.repeats + (with_dbias ? n.parts : 0);
+    return n.delta + n.largest + (with_dbias ? n.parts : 0);
 }
 
 hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dout, const HeadRows& q,
@@ -815,8 +762,7 @@ hipError_t launch_attention_backward(const AttentionCall& a, const HeadRows& dou
     const Sizes n = sizes(a);
     char* p = static_cast<char*>(ws);
     const Scratch w{reinterpret_cast<float*>(p), reinterpret_cast<uint32_t*>(p + n.delta),
-                    reinterpret_cast<int32_t*>(p + n.delta + n.largest),
-                    reinterpret_cast<float*>(p + n.delta + n.largest + n.repeats)};
+                    reinterpret_cast<float*>(p + n.delta + n.largest)};
     const Inputs in{dout, q, k, v, out, reinterpret_cast<const float2*>(lse)};
     const Grads g{dq, dk, dv, dbias, w};
     if (a.dt == kBf16) return a.dh <= 64 ? pick<Bf16, 64>(a, in, g, st) : pick<Bf16, 128>(a, in, g, st);

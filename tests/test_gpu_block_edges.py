@@ -77,7 +77,8 @@ def test_values_of_any_size(dtype, size, shift):
 
 
 ORDERS = [(F32, 63, (64, 64)), (F32, 55, (64, 64)), (F32, 53, (200, 50)), (F32, 23, (24, 24)), (F32, 9, (24, 24)),
-          (BF, 55, (64, 64)), (BF, 53, (200, 50)), (BF, 9, (24, 24))]
+          (BF, 55, (64, 64)), (BF, 53, (200, 50)), (BF, 9, (24, 24)), (BF, 63, (64, 64)), (BF, 35, (36, 36)),
+          (BF, 23, (24, 24))]
 
 
 @pytest.mark.parametrize("dtype,span,grid", ORDERS)
@@ -98,3 +99,45 @@ def test_bias_gradient_does_not_depend_on_the_order_of_keys(dtype, span, grid):
     _, _, want = c.plain(grads=True)
     assert ref.rel(a.dbias, want[3]) <= BWD[dtype]
     assert torch.equal(a.dbias, b.dbias)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("how", ["sorted", "shuffled"])
+@pytest.mark.parametrize("span", [19, 7])
+def test_bias_gradient_beside_keys_of_no_weight(dtype, how, span):
+    """Keys at a finite mask value, whose values are large: their probability is zero and so is their part
+    of every gradient; the others keep theirs."""
+    c = Case(dtype, [300, 90], None, 2, 2, 64, (20, 20), span, how, True, seed=340)
+    c.k_bias = torch.zeros(390)
+    low = torch.arange(0, 390, 13)
+    c.k_bias[low] = -1e9
+    c.v[low] = (c.v[low].float() * (1e6 if dtype == BF else 1e12)).to(dtype)
+    print(f"keys of no weight, {dtype}, {how}, span {span}", flush=True)
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **c.kw())
+    torch.cuda.synchronize()
+    _, _, want = c.plain(grads=True)
+    for got, w in zip((g.dq, g.dk, g.dv, g.dbias), want):
+        assert ref.rel(got, w) <= BWD[dtype]
+
+
+@pytest.mark.parametrize("dtype,far", [(BF, -20.8), (F32, -13.9), (BF, -10.0)])
+@pytest.mark.parametrize("span", [23, 63])
+def test_bias_gradient_of_far_offsets(dtype, far, span):
+    """Attention that a table has made sharp: the far offsets' score gradients are 2^-30 (2^-20 in float32) of the
+    near ones', and stay exact on their own."""
+    grid = (span + 1, span + 1)
+    c = Case(dtype, [250], None, 2, 2, 64, grid, span, "sorted", False, seed=350)
+    near = torch.zeros(2 * span + 1, 2 * span + 1, dtype=torch.bool)
+    reach = 2 if span == 23 else 6
+    near[span - reach:span + reach + 1, span - reach:span + reach + 1] = True
+    c.bias = torch.where(near, c.bias, c.bias + far)
+    print(f"far offsets, {dtype}, {far}, span {span}", flush=True)
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **c.kw())
+    torch.cuda.synchronize()
+    _, _, want = c.plain(grads=True)
+    assert ref.rel(g.dbias[:, near.to(DEV)], want[3][:, near]) <= BWD[dtype]
+    assert ref.rel(g.dbias[:, ~near.to(DEV)], want[3][:, ~near]) <= BWD[dtype]
