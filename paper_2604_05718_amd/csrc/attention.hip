@@ -167,7 +167,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                         } else {
                             x *= c;
                         }
-                        if (KB) x = kb[e] > -__builtin_inff() ? x + kb[e] : -__builtin_inff();
+                        if (KB) x = kb[e] == -__builtin_inff() ? kb[e] : x + kb[e];
                         s[i][4 * g + e] = x;
                     }
                 }

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
     float kb = 0.0f;
     if (KB) kb = exists ? to_log2(a.k_bias[rk.first + ki]) : -__builtin_inff();
     int kcode = 0;
-    const bool live = exists && kb > -__builtin_inff();
+    const bool live = exists && kb != -__builtin_inff();
     // (all of the first loads are under way before one is waited for)
     int own = 0;  // this key's position
     if (BIAS != kBiasNone) own = exists ? (a.k_pos ? a.k_pos[rk.first + ki] : ki) : 0;

@@ -196,7 +196,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<S, DH, KB>())) void atten
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float x = s[4 * g + e];
-                if (KB) x = kb[e] > -__builtin_inff() ? x + kb[e] : -__builtin_inff();
+                if (KB) x = kb[e] == -__builtin_inff() ? kb[e] : x + kb[e];
                 else if (32 * tile + 8 * g + 4 * h + e >= rk.count) x = -__builtin_inff();
                 s[4 * g + e] = x;
                 top = fmaxf(top, x);

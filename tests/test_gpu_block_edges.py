@@ -141,3 +141,29 @@ def test_bias_gradient_of_far_offsets(dtype, far, span):
     _, _, want = c.plain(grads=True)
     assert ref.rel(g.dbias[:, near.to(DEV)], want[3][:, near]) <= BWD[dtype]
     assert ref.rel(g.dbias[:, ~near.to(DEV)], want[3][:, ~near]) <= BWD[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_key_bias_that_is_no_number(dtype):
+    """A NaN among the key biases is not a dropped key: every query of its image gets NaN, forward (the form
+    for few queries too) and in the gradients; other images are as without it."""
+    c = Case(dtype, [70, 40], None, 2, 2, 64, (10, 9), 9, "sorted", True, seed=360)
+    c.k_bias = torch.zeros(110)
+    clean = c.kw()
+    c.k_bias[33] = float("nan")
+    q, k, v = c.dev()
+
+    def results(kw):
+        out, lse = mpm.attention(q, k, v, with_lse=True, **kw)
+        g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **kw)
+        few = dict(kw, q_off=offsets([3, 2]).to(DEV), Nq=3, q_pos=kw["q_pos"][:5].contiguous())
+        return out, lse, g.dq, g.dk, g.dv, mpm.attention(q[:5], k, v, **few)
+
+    want, got = results(clean), results(c.kw())
+    torch.cuda.synchronize()
+    for w, t in zip(want[:5], got[:5]):
+        assert torch.equal(w[70:], t[70:])
+    assert torch.equal(want[5][3:], got[5][3:]) and torch.isnan(got[5][:3]).all()
+    assert torch.isnan(got[0][:70]).all() and torch.isnan(got[1][:70].sum(-1)).all()
+    for t in got[2:5]:
+        assert torch.isnan(t[:70]).all()
