@@ -213,7 +213,9 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
             if (t < QT) {
                 const int qi = q0 + t;
                 const bool in = qi < rq.count;
-                if (BIAS != kBiasNone) pos = in ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0;
+                // (past the image's end: the last query's, so that only entries that a pair has are read)
+                const int at = min(qi, rq.count - 1);
+                if (BIAS != kBiasNone) pos = at < 0 ? 0 : a.q_pos ? a.q_pos[rq.first + at] : at;
                 stat = in ? lse[(rq.first + qi) * a.H + hd] : make_float2(-__builtin_inff(), 0.0f);
                 del = in ? w.delta[((long)b * a.Nq + qi) * a.H + hd] : 0.0f;
             }
@@ -427,7 +429,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
     };
     stage.init(k, v, rk.first, hk, a.dh, t);
     load(0);
-    const int qpos = BIAS != kBiasNone && live ? (a.q_pos ? a.q_pos[qrow] : qi) : 0;
+    const int qat = min(qi, rq.count - 1);  // (past the image's end: the last query's, as in the key kernel)
+    const int qpos = BIAS != kBiasNone ? (a.q_pos ? a.q_pos[rq.first + qat] : qat) : 0;
     Frag qf[DH / 16], of[DH / 16];
     load_frags<S, DH>(qf, q.p + (qrow * q.row + (long)hd * q.head) * S::kBytes, a.dh, live, h);
     load_frags<S, DH>(of, dout.p + (qrow * dout.row + (long)hd * dout.head) * S::kBytes, a.dh, live, h);
@@ -506,7 +509,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
                     if (BIAS == kBiasNone) x *= c;
                     else if (SUM == kSumAlone) x = fmaf(x, c, to_log2(beside[4 * g + e]));
                     else x = fmaf(x, c, lds_at(entry[4 * g + e]));
-                    if (KB) x += kb[e];
+                    if (KB) x = kb[e] == -__builtin_inff() ? kb[e] : x + kb[e];
                     s[4 * g + e] = x;
                 }
             }

@@ -167,3 +167,35 @@ def test_a_key_bias_that_is_no_number(dtype):
     assert torch.isnan(got[0][:70]).all() and torch.isnan(got[1][:70].sum(-1)).all()
     for t in got[2:5]:
         assert torch.isnan(t[:70]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("span", [9, 4])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("masked", [False, True])
+def test_table_entries_that_no_pair_meets(dtype, span, value, masked):
+    """What the table holds at offsets that only dropped keys, or no rows at all, would have reaches neither
+    results nor gradients: every token lies in the grid's rows 6 to 9, and offsets of four and more rows, which a
+    dropped key in row 0 has, are NaN or infinite."""
+    ns = [37, 5, 20]
+    c = Case(dtype, ns, None, 2, 2, 64, (10, 10), span, "sorted", masked, seed=370)
+    g = torch.Generator().manual_seed(1)
+    c.k_pos = torch.cat([60 + torch.randperm(40, generator=g)[:n].sort().values for n in ns]).to(torch.int32)
+    c.q_pos = c.k_pos.clone()
+    if masked:
+        c.k_bias = torch.zeros(sum(ns))
+        for i in (0, 11, 40, 50):
+            c.k_bias[i], c.k_pos[i] = -float("inf"), 3
+    want, _, wg = c.plain(grads=True)
+    c.bias[:, :span - 3], c.bias[:, span + 4:] = value, value
+    print(f"entries of {value}, {dtype}, span {span}, masked {masked}", flush=True)
+    q, k, v = c.dev()
+    kw = c.kw()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **kw)
+    r = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **kw)
+    few = dict(kw, q_off=offsets([3, 0, 2]).to(DEV), Nq=3, q_pos=kw["q_pos"][:5].contiguous())
+    some = mpm.attention(q[:5], k, v, **few)
+    torch.cuda.synchronize()
+    assert ref.rel(out, want) <= FWD[dtype] and ref.rel(some[:3], want[:3]) <= FWD[dtype]
+    for got, w in zip((r.dq, r.dk, r.dv, r.dbias), wg):
+        assert ref.rel(got, w) <= BWD[dtype]
