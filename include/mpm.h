@@ -496,6 +496,7 @@ typedef struct mpm_heads {
  *     (1 <= grid_h, grid_w <= MPM_MAX_N): q_pos, k_pos int32 per row, packed like q and k, or
  *     NULL for each row's index in its image (the raster order of a full grid). Any order of
  *     positions is taken; one outside the grid counts as the nearest cell index.
+ *     An entry, or a key's bias below, beyond 2.35e38 in magnitude counts as that (infinities stay infinite).
  *   k_bias (may be NULL): float per key row, added to its scores for every query and head (for
  *     merged rows the log of the tokens they stand for). A key with -inf is dropped: its rows of
  *     k and v take no part, whatever they hold, and their gradients are zero. A constant: no

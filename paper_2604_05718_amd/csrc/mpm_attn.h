@@ -268,11 +268,12 @@ __device__ __forceinline__ int lds_address(const void* p)
 __device__ __forceinline__ float lds_at(int address) { return *(lds_float*)(uintptr_t)(uint32_t)address; }
 
 // A score term in the exponent's base: x log2(e), a finite value kept finite (a mask may use the
-// type's lowest value, whose rows then average all of their keys as the softmax of equal scores).
+// type's lowest value, whose rows then average all of their keys as the softmax of equal scores, or its
+// highest): beyond 2.35e38 in magnitude it counts as that.
 __device__ __forceinline__ float to_log2(float x)
 {
     const float y = x * kLog2e;
-    return x >= kLowest ? fmaxf(y, kLowest) : y;
+    return fabsf(x) <= -kLowest ? __builtin_amdgcn_fmed3f(y, kLowest, -kLowest) : y;
 }
 
 constexpr int kXcds = 8;

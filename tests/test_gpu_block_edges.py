@@ -199,3 +199,28 @@ def test_table_entries_that_no_pair_meets(dtype, span, value, masked):
     assert ref.rel(out, want) <= FWD[dtype] and ref.rel(some[:3], want[:3]) <= FWD[dtype]
     for got, w in zip((r.dq, r.dk, r.dv, r.dbias), wg):
         assert ref.rel(got, w) <= BWD[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("where", ["k_bias", "bias"])
+def test_the_largest_finite_scores(dtype, where):
+    """A term of 3e38, which passes the type's range in base 2, wins its rows; the type's lowest value beside it
+    takes no part."""
+    c = Case(dtype, [70, 5], [90, 40], 2, 2, 64, (10, 10), 9, "sorted", True, seed=380)
+    c.k_bias = torch.zeros(130)
+    if where == "k_bias":
+        c.k_bias[17], c.k_bias[100] = 3e38, torch.finfo(F32).max
+        c.k_bias[18] = torch.finfo(F32).min
+    else:
+        c.bias[:, 9, 12] = 3e38
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **c.kw())
+    few = dict(c.kw(), q_off=offsets([3, 0]).to(DEV), Nq=3, q_pos=c.q_pos[:3].contiguous().to(DEV))
+    some = mpm.attention(q[:3], k, v, **few)
+    torch.cuda.synchronize()
+    want, _, wg = c.plain(grads=True)
+    assert ref.rel(out, want) <= FWD[dtype] and ref.rel(some, want[:3]) <= FWD[dtype]
+    assert ref.rel(g.dv, wg[2]) <= BWD[dtype]
+    for got, w in zip((g.dq, g.dk, g.dbias), (wg[0], wg[1], wg[3])):  # zero where one key has all of a row
+        assert float((got.double().cpu() - w).norm()) <= BWD[dtype] * max(float(w.norm()), float(c.dout.double().norm()))
