@@ -56,14 +56,17 @@ def _heads(t, what, ref, rows=None, heads=None):
     dims, dh = len(sh), sh[-1]
     if (dims != 3 and dims != 4) or (st[-1] != 1 and dh > 1):
         raise ValueError(f"{what} must be [R, H, dh] or [B, N, H, dh] with contiguous channels")
-    n = sh[0]
+    n, row, head = sh[0], st[-3], st[-2]
     if dims == 4:
-        if n > 1 and sh[1] > 0 and st[0] != sh[1] * st[1]:
+        if sh[1] == 1:
+            row = st[0]  # (one row an image: the images' stride is the rows')
+        elif n > 1 and sh[1] > 0 and st[0] != sh[1] * row:
             raise ValueError(f"{what}: dense images must follow each other at the rows' stride")
         n *= sh[1]
     if (rows is not None and n != rows) or dh != ref.shape[-1] or (heads is not None and sh[-2] != heads):
         raise ValueError(f"{what} has shape {tuple(sh)}, expected {rows} rows of {heads} heads of {ref.shape[-1]}")
-    return _lib.Heads(t.data_ptr(), st[-3], st[-2])
+    # A stride that nothing is reached by may be any number.
+    return _lib.Heads(t.data_ptr(), row if n > 1 else 0, head if sh[-2] > 1 else 0)
 
 
 def _rows_of(t):

@@ -68,3 +68,50 @@ print(json.dumps([less < full, back(None, less), back(None, less - 1), back(p, l
     p = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=root, env=env, timeout=100)
     assert p.returncode == 0, p.stderr[-2000:]
     assert json.loads(p.stdout) == [True, 4, 3, 3, 4, 3]
+
+
+class Recorder:
+    """A library whose calls succeed and are remembered."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            if name.endswith("_workspace_bytes"):
+                return 0
+            self.calls.append((name, [getattr(a, "_obj", a) for a in args]))
+            return 0
+        return call
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    lib = Recorder()
+    monkeypatch.setattr(block_ops._lib, "load", lambda: lib)
+    monkeypatch.setattr(block_ops, "_stream", lambda t: None)
+    return lib
+
+
+def test_one_row_of_dense_images(recorded):
+    """A slice of one row of every image, the first tokens of a batch say: the images' stride is the rows'."""
+    whole = torch.zeros(3, 20, 4, 16)
+    q, kv = device(whole[:, :1]), device(torch.zeros(3, 20, 4, 16))
+    block_ops.attention(q, kv, kv)
+    (name, (call, hq, hk, hv, ho, *_)), = recorded.calls
+    assert name == "mpm_attention" and (call.B, call.Nq, call.Nk) == (3, 1, 20)
+    assert (hq.p, hq.row, hq.head) == (whole.data_ptr(), 20 * 64, 16)
+    assert (ho.row, ho.head) == (64, 16) and (hk.row, hk.head) == (64, 16)
+    block_ops.attention_backward(q, q, kv, kv, q, device(torch.zeros(3, 4, 2)), dq=q, dk=kv, dv=kv)
+    args = recorded.calls[1][1]
+    assert [h.row for h in args[1:6] + args[7:10]] == [1280, 1280, 64, 64, 1280, 1280, 64, 64]
+    with pytest.raises(ValueError, match="dense images"):
+        block_ops.attention(device(whole[:, :2]), kv, kv)
+
+
+def test_strides_that_nothing_is_reached_by(recorded):
+    """Of a single row or a single head any stride is right."""
+    odd = device(torch.as_strided(torch.zeros(64), (1, 1, 16), (7, 5, 1)))
+    off = device(torch.tensor([0, 1], dtype=torch.int32))
+    block_ops.attention(odd, odd, odd, q_off=off, k_off=off, Nq=1, Nk=1)
+    assert [(h.row, h.head) for h in recorded.calls[0][1][1:4]] == [(0, 0)] * 3

@@ -224,3 +224,22 @@ def test_the_largest_finite_scores(dtype, where):
     assert ref.rel(g.dv, wg[2]) <= BWD[dtype]
     for got, w in zip((g.dq, g.dk, g.dbias), (wg[0], wg[1], wg[3])):  # zero where one key has all of a row
         assert float((got.double().cpu() - w).norm()) <= BWD[dtype] * max(float(w.norm()), float(c.dout.double().norm()))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_first_rows_of_dense_images(dtype):
+    """One row a dense image, a view into the batch, results and gradients written into views as well: those
+    of the copied rows, bit for bit."""
+    g = torch.Generator().manual_seed(390)
+    x, kv, d = (torch.randn(3, 50, 4, 32, generator=g).to(dtype).to(DEV) for _ in range(3))
+    into = [torch.full_like(x, 7) for _ in range(2)]
+    out, lse = mpm.attention(x[:, :1], kv, kv, with_lse=True, out=into[0][:, :1])
+    a = mpm.attention_backward(d[:, :1], x[:, :1], kv, kv, out, lse, dq=into[1][:, :1])
+    q = x[:, :1].contiguous()
+    want, wl = mpm.attention(q, kv, kv, with_lse=True)
+    b = mpm.attention_backward(d[:, :1].contiguous(), q, kv, kv, want, wl)
+    torch.cuda.synchronize()
+    assert torch.equal(lse, wl)
+    for got, w in ((into[0], want), (into[1], b.dq)):
+        assert torch.equal(got[:, :1], w) and torch.all(got[:, 1:] == 7)
+    assert torch.equal(a.dk, b.dk) and torch.equal(a.dv, b.dv)
