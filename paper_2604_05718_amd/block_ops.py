@@ -65,8 +65,8 @@ def _heads(t, what, ref, rows=None, heads=None):
         n *= sh[1]
     if (rows is not None and n != rows) or dh != ref.shape[-1] or (heads is not None and sh[-2] != heads):
         raise ValueError(f"{what} has shape {tuple(sh)}, expected {rows} rows of {heads} heads of {ref.shape[-1]}")
-    # A stride that nothing is reached by may be any number.
-    return _lib.Heads(t.data_ptr(), row if n > 1 else 0, head if sh[-2] > 1 else 0)
+    # A stride that nothing is reached by may be any number; a tensor without rows has no address and needs none.
+    return _lib.Heads(t.data_ptr() if n else ref.data_ptr(), row if n > 1 else 0, head if sh[-2] > 1 else 0)
 
 
 def _rows_of(t):
@@ -81,7 +81,7 @@ def _side(t, off, N, what):
         return t.shape[0], t.shape[1]
     if off is None or N is None:
         raise ValueError(f"packed {what} [R, H, dh] need their offsets and the most rows of an image")
-    return off.numel() - 1, int(N)
+    return off.numel() - 1, int(N) or int(t.shape[0] == 0)  # (no rows at all: any N is enough)
 
 
 def _call(q, k, v, q_off, k_off, Nq, Nk, scale, bias, q_pos, k_pos, grid, k_bias):
@@ -96,6 +96,8 @@ def _call(q, k, v, q_off, k_off, Nq, Nk, scale, bias, q_pos, k_pos, grid, k_bias
     Bk, nk = _side(k, k_off, Nk, "keys")
     if B != Bk:
         raise ValueError(f"queries of {B} images, keys of {Bk}")
+    if k_off is None and nk == 0:  # dense images without keys: as packed ones
+        k_off, nk = torch.zeros((B + 1,), dtype=torch.int32, device=q.device), 1
     c = _lib.AttentionCall(B, nq, nk, H, Hk, q.shape[-1], dt, q.shape[-1] ** -0.5 if scale is None else scale,
                            _device(q_off, "q_off", torch.int32, q, B + 1), _device(k_off, "k_off", torch.int32, q, B + 1))
     if bias is not None:
@@ -108,6 +110,7 @@ def _call(q, k, v, q_off, k_off, Nq, Nk, scale, bias, q_pos, k_pos, grid, k_bias
         c.grid_h, c.grid_w = grid
         c.q_pos, c.k_pos = _device(q_pos, "q_pos", torch.int32, q, rq), _device(k_pos, "k_pos", torch.int32, q, rk)
     c.k_bias = _device(k_bias, "k_bias", torch.float32, q, rk)
+    c.held = k_off  # (until the call)
     return c, hq, hk, hv
 
 
@@ -170,6 +173,8 @@ def attention(q, k, v, q_off=None, k_off=None, Nq=None, Nk=None, scale=None, bia
     rows = _rows_of(q)
     ho = _heads(out, "out", q, rows, c.H)
     lse = torch.empty((rows, c.H, 2), dtype=torch.float32, device=q.device) if with_lse else None
+    if rows == 0:
+        return (out, lse) if with_lse else out
     lib = _lib.load()
     need = lib.mpm_attention_workspace_bytes(_BYREF(c))
     ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
@@ -199,6 +204,11 @@ def attention_backward(dout, q, k, v, out, lse, q_off=None, k_off=None, Nq=None,
     hs = [_heads(dout, "dout", q, rq, c.H), hq, hk, hv, _heads(out, "out", q, rq, c.H)]
     gs = [_heads(dq, "dq", q, rq, c.H), _heads(dk, "dk", q, rk, c.Hk), _heads(dv, "dv", q, rk, c.Hk)]
     dbias = torch.empty_like(bias) if bias is not None and with_dbias else None
+    if rq == 0:  # no query: the sums over them are empty
+        for t in (dk, dv, dbias):
+            if t is not None:
+                t.zero_()
+        return AttentionGrads(dq, dk, dv, dbias)
     lib = _lib.load()
     if dbias is None:  # (the size without the partial sums of dbias)
         kept, c.bias = c.bias, None
@@ -251,6 +261,8 @@ def residual_norm(x, f, weight=None, bias=None, post_weight=None, post_bias=None
     y = torch.empty_like(x) if out is None else out
     h = torch.empty_like(x) if weight is not None else None
     stats = torch.empty((x.shape[0], 4), dtype=torch.float32, device=x.device) if with_stats else None
+    if x.shape[0] == 0:
+        return (y, h, stats) if with_stats else (y, h)
     _lib.check("mpm_residual_norm", _lib.load().mpm_residual_norm(
         _BYREF(c), _ptr(x), fp, _device(y, "out", x.dtype, x, x.numel()), _ptr(h), _ptr(stats), _stream(x)))
     return (y, h, stats) if with_stats else (y, h)
@@ -277,6 +289,11 @@ def residual_norm_backward(dy, dh, y, f, stats, weight=None, bias=None, post_wei
     g = NormGradients(torch.empty_like(y), torch.empty_like(y),
                       *(None if t is None else torch.empty_like(t)
                         for t in (weight, bias, post_weight, post_bias, scale, gate)))
+    if n == 0:  # no row: the sums over them are empty
+        for t in (g.dweight, g.dbias, g.dpost_weight, g.dpost_bias, g.dscale, g.dgate):
+            if t is not None:
+                t.zero_()
+        return g
     lib = _lib.load()
     need = lib.mpm_residual_norm_backward_workspace_bytes(_BYREF(c))
     ws = torch.empty((need,), dtype=torch.uint8, device=y.device)

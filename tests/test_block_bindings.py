@@ -115,3 +115,23 @@ def test_strides_that_nothing_is_reached_by(recorded):
     off = device(torch.tensor([0, 1], dtype=torch.int32))
     block_ops.attention(odd, odd, odd, q_off=off, k_off=off, Nq=1, Nk=1)
     assert [(h.row, h.head) for h in recorded.calls[0][1][1:4]] == [(0, 0)] * 3
+
+
+def test_calls_without_rows(no_launch):
+    """No query, or no row of a norm: empty results, and gradients that are sums over nothing."""
+    q, k = device(torch.zeros(0, 2, 8)), device(torch.ones(5, 2, 8))
+    off, k_off = (device(torch.tensor(o, dtype=torch.int32)) for o in ([0, 0, 0], [0, 3, 5]))
+    where = dict(q_off=off, k_off=k_off, Nq=0, Nk=3, bias=device(torch.ones(2, 5, 5)), grid=(3, 3))
+    out, lse = block_ops.attention(q, k, k, with_lse=True, out=q, **where)
+    assert out.shape == (0, 2, 8) and lse.shape == (0, 2, 2)
+    g = block_ops.attention_backward(q, q, k, k, out, lse, dq=q, dk=device(torch.ones(5, 2, 8)),
+                                     dv=device(torch.ones(5, 2, 8)), **where)
+    assert g.dq.shape == q.shape and not g.dk.any() and not g.dv.any() and not g.dbias.any()
+    x, w = device(torch.zeros(0, 16)), device(torch.ones(16))
+    y, h, stats = block_ops.residual_norm(x, x, weight=w, scale=w, gate=device(torch.ones(3, 16)),
+                                          off=device(torch.zeros(4, dtype=torch.int32)), with_stats=True)
+    assert y.shape == h.shape == (0, 16) and stats.shape == (0, 4)
+    n = block_ops.residual_norm_backward(None, x, x, x, stats, weight=w, scale=w, gate=device(torch.ones(3, 16)),
+                                         off=device(torch.zeros(4, dtype=torch.int32)))
+    assert n.dx.shape == (0, 16) and n.dgate.shape == (3, 16)
+    assert not n.dweight.any() and not n.dscale.any() and not n.dgate.any() and n.dbias is None

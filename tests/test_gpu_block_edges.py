@@ -243,3 +243,25 @@ def test_first_rows_of_dense_images(dtype):
     for got, w in ((into[0], want), (into[1], b.dq)):
         assert torch.equal(got[:, :1], w) and torch.all(got[:, 1:] == 7)
     assert torch.equal(a.dk, b.dk) and torch.equal(a.dv, b.dv)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Nq", [3, 40])
+@pytest.mark.parametrize("dense", [False, True])
+def test_no_keys_at_all(dtype, Nq, dense):
+    """Queries of images none of which has a key: zeros, statistics of an empty sum, and zero gradients."""
+    g = torch.Generator().manual_seed(400)
+    q, d = (torch.randn(2 * Nq, 4, 32, generator=g).to(dtype).to(DEV) for _ in range(2))
+    k = torch.zeros(0, 2, 32, dtype=dtype, device=DEV)
+    kw = dict(bias=torch.randn(4, 9, 9, generator=g).to(DEV), grid=(9, 5))
+    if dense:
+        q, d, k = q.view(2, Nq, 4, 32), d.view(2, Nq, 4, 32), k.view(2, 0, 2, 32)
+    else:
+        none = torch.zeros(0, device=DEV)
+        kw.update(q_off=offsets([Nq, Nq]).to(DEV), k_off=offsets([0, 0]).to(DEV), Nq=Nq, Nk=0, k_bias=none,
+                  q_pos=torch.zeros(2 * Nq, dtype=torch.int32, device=DEV), k_pos=none.int())
+    out, lse = mpm.attention(q, k, k, with_lse=True, **kw)
+    r = mpm.attention_backward(d, q, k, k, out, lse, **kw)
+    torch.cuda.synchronize()
+    assert out.shape == q.shape and not out.any() and torch.isinf(lse.sum(-1)).all()
+    assert not r.dq.any() and not r.dbias.any() and r.dk.shape == k.shape == r.dv.shape
