@@ -201,10 +201,11 @@ __device__ __forceinline__ void row_stats(const float (&x)[RawPart<S, LANES, VPL
 // Parameters that are not given are ones (scale, gate) or zeros (shifts).
 //
 // Forward: a row group of LANES lanes takes every kRows-th row of the workgroup's, the next row's x and
-// f on their way while one is computed; the parameters stay in registers.
+// f on their way while one is computed; the parameters stay in registers. y may be x itself: a row is loaded
+// before it is stored, and what is loaded of it again past the workgroup's end is not used.
 template <class S, int LANES, int VPL, bool POST, bool PRE>
-__global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, const void* __restrict__ x,
-                                                               const void* __restrict__ f, void* __restrict__ y,
+__global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, const void* x,
+                                                               const void* __restrict__ f, void* y,
                                                                void* __restrict__ hout, float* __restrict__ stats)
 {
     typedef RawPart<S, LANES, VPL> Raw;

@@ -265,3 +265,21 @@ def test_no_keys_at_all(dtype, Nq, dense):
     torch.cuda.synchronize()
     assert out.shape == q.shape and not out.any() and torch.isinf(lse.sum(-1)).all()
     assert not r.dq.any() and not r.dbias.any() and r.dk.shape == k.shape == r.dv.shape
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("R,D", [(5000, 64), (3000, 768), (700, 2048), (300, 5000), (40, 16384)])
+def test_residual_norm_in_place(dtype, R, D):
+    """y into x's own memory, many rows a workgroup, for every width of a row group: the results of a call with
+    a y of its own, bit for bit, time after time."""
+    g = torch.Generator().manual_seed(410)
+    x, f = (torch.randn(R, D, generator=g).to(dtype).to(DEV) for _ in range(2))
+    w, gate = torch.ones(D, dtype=dtype, device=DEV), torch.randn(R, D, generator=g).to(dtype).to(DEV)
+    for kw in (dict(weight=w), dict(weight=w, post_weight=w, gate=gate), dict(scale=w)):
+        want = mpm.residual_norm(x, f, **kw)
+        for _ in range(3):
+            y = x.clone()
+            got = mpm.residual_norm(y, f, out=y, **kw)
+            torch.cuda.synchronize()
+            assert got[0].data_ptr() == y.data_ptr() and torch.equal(y, want[0])
+            assert want[1] is None or torch.equal(got[1], want[1])
