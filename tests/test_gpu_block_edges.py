@@ -283,3 +283,18 @@ def test_residual_norm_in_place(dtype, R, D):
             torch.cuda.synchronize()
             assert got[0].data_ptr() == y.data_ptr() and torch.equal(y, want[0])
             assert want[1] is None or torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("B", [65535, 65531, 65530])
+def test_gates_of_the_most_images(B):
+    """A gate an image for as many images as a call takes, two rows each: every image's gradient is there."""
+    g = torch.Generator().manual_seed(420)
+    D = 8
+    f, dy, gate = (torch.randn(n, D, generator=g) for n in (2 * B, 2 * B, B))
+    x = torch.zeros(2 * B, D)
+    y, h, stats = mpm.residual_norm(x.to(DEV), f.to(DEV), gate=gate.to(DEV), with_stats=True)
+    r = mpm.residual_norm_backward(dy.to(DEV), None, y, f.to(DEV), stats, gate=gate.to(DEV))
+    torch.cuda.synchronize()
+    want = (dy.double() * f.double()).view(B, 2, D).sum(1)
+    assert ref.rel(r.dgate, want) <= 2 * 16 * 2.0 ** -24
+    assert ref.rel(r.dgate[-6:], want[-6:]) <= 2 * 16 * 2.0 ** -24
