@@ -147,3 +147,20 @@ def test_a_frozen_table_costs_no_gradient(operators, learned):
     blocks._Attention.apply(qkv, table, *rest).sum().backward()
     assert operators.calls == dict(attention=dict(with_dbias=learned), **(dict(table=True) if learned else {}))
     assert qkv.grad is not None and (table.grad is not None) == learned
+
+
+def test_strided_rows_of_the_norms(operators, monkeypatch):
+    """The operators take contiguous rows; x as a view is copied like f."""
+    def contiguous(x, f, *p, **kw):
+        assert x.is_contiguous() and f.is_contiguous()
+        return operators.residual_norm(x, f, *p, **kw)
+
+    monkeypatch.setattr(block_ops, "residual_norm", contiguous)
+    *p, off, norm, eps = norm_inputs()
+    wide = [torch.cat([t, t], dim=1).detach().requires_grad_() for t in p[:2]]
+    got = blocks._ResidualNorm.apply(wide[0][:, :D], wide[1][:, D:], *p[2:], off, norm, eps)
+    want = blocks._ResidualNorm.apply(*p, off, norm, eps)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    (got[0] * got[1]).sum().backward()
+    (want[0] * want[1]).sum().backward()
+    assert torch.equal(wide[0].grad[:, :D], p[0].grad) and torch.equal(wide[1].grad[:, D:], p[1].grad)
