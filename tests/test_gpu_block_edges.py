@@ -298,3 +298,39 @@ def test_gates_of_the_most_images(B):
     want = (dy.double() * f.double()).view(B, 2, D).sum(1)
     assert ref.rel(r.dgate, want) <= 2 * 16 * 2.0 ** -24
     assert ref.rel(r.dgate[-6:], want[-6:]) <= 2 * 16 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("score,value", [(41.0, 1e21), (41.0, 2.0 ** 95), (-41.0, 1e-20), (11.0, 2.0 ** 95)])
+def test_one_key_of_a_large_value(dtype, score, value):
+    """One key with a score far from zero and a value far from one, alone or beside a key of no weight."""
+    q = torch.zeros(2, 1, 32, dtype=dtype, device=DEV)
+    k = torch.zeros(3, 1, 32, dtype=dtype, device=DEV)
+    v = torch.full((3, 1, 32), value, dtype=dtype, device=DEV)
+    v[1:] = 1.0
+    kw = dict(q_off=offsets([1, 1]).to(DEV), k_off=offsets([1, 2]).to(DEV), Nq=1, Nk=2,
+              k_bias=torch.tensor([score, score - 200.0, score], device=DEV))
+    for n in (1, 40):  # the form for few queries, and the other
+        rows = q.repeat_interleave(n, 0)
+        kw.update(q_off=offsets([n, n]).to(DEV), Nq=n)
+        out = mpm.attention(rows, k, v, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:n], v[:1].expand(n, 1, 32)) and torch.all(out[n:] == 1)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1e-5, 3.0])
+def test_scales(dtype, scale):
+    """Factors of the scores of either sign, none, and ones outside the range in which the products start from the
+    statistics. Scores of up to 3 * 30: the exponent's error is 2^-24 of them, as in test_large_scores."""
+    c = Case(dtype, [90, 33], None, 2, 2, 32, (12, 10), 11, "sorted", True, seed=430)
+    c.scale = scale
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, scale=scale, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, scale=scale, **c.kw())
+    torch.cuda.synchronize()
+    want, _, wg = c.plain(grads=True)
+    slack = 1 if dtype == BF else 1 + 4 * 90 / 144
+    assert ref.rel(out, want) <= FWD[dtype] * slack
+    for got, w in zip((g.dq, g.dk, g.dv, g.dbias), wg):
+        assert ref.rel(got, w) <= BWD[dtype] * slack
