@@ -542,6 +542,8 @@ int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_
  *   dbias (may be NULL; only with bias): float[H][W][W], the sum of the score gradients of every
  *     pair at each offset, over all images (mpm_bias_gradient takes it to the table's).
  * Rows of dq, dk and dv that exist are all written. Results do not depend on the order workgroups run in.
+ * dbias is summed in 64-bit integers of a unit found for every image and head: score gradients below 2^-40
+ * of the largest there are lost. One that is not finite makes all of its head's dbias NaN.
  * ws: mpm_attention_backward_workspace_bytes(call) bytes. With a bias most of them are dbias's partial
  * sums, W * W floats for every image, head and 64 to 256 queries; a call whose dbias is NULL needs only
  * what the size of the same call without its bias is (bias NULL). Errors as mpm_attention, plus
@@ -615,6 +617,7 @@ int mpm_residual_norm(const mpm_norm_call* call, const void* x, const void* f, v
  * w is), the stored y, f and stats:
  *   dx, df [R][D]; dw, db, dpost_w, dpost_b, dscale [D]; dgate shaped as gate: each needed if and
  *   only if its parameter is given. All of dtype dt; sums over rows are kept in float32, in a fixed order.
+ * The rows of y are normed as they are stored, rounded to dt, with the statistics of the unrounded sum.
  * ws: mpm_residual_norm_backward_workspace_bytes(call) bytes. Errors as mpm_residual_norm,
  * plus MPM_ERR_WORKSPACE.
  */

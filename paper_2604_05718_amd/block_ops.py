@@ -3,7 +3,8 @@ packed images with a learned relative position bias, and the norms around a bloc
 gate and residual scale, each with its gradients.
 
 Argument marshalling only, as in api.py: every step runs in the HIP kernels of libmpm.so on
-``torch.cuda.current_stream()``.
+``torch.cuda.current_stream()``. No autograd history: results of tensors that require gradients are detached
+(blocks.py has the differentiable functions).
 
 Rows of heads: queries are [R, H, dh] (packed by q_off, an int32 device tensor [B+1], with at most
 Nq rows an image) or [B, N, H, dh] (dense), keys and values likewise with Hk heads; strided views

@@ -76,7 +76,7 @@ class _ResidualNorm(torch.autograd.Function):
     def forward(ctx, x, f, weight, bias, post_weight, post_bias, scale, gate, off, norm, eps):
         given = (weight, bias, post_weight, post_bias, scale, gate)
         y, h, stats = block_ops.residual_norm(x.contiguous(), f.contiguous(), *given, off=off, norm=norm, eps=eps,
-                                            with_stats=True)
+                                              with_stats=True)
         ctx.save_for_backward(y, f, stats, off, *given)
         ctx.rest = dict(norm=norm, eps=eps)
         return y, h

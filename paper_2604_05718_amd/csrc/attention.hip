@@ -8,11 +8,15 @@
 //
 // Bound by instruction issue: a score costs an exponential, its share of a bias read, a maximum, a sum and
 // a conversion, and those and the products hardly overlap (3 images of 4096 tokens: vector instructions
-// 58% and products 32% of the busy cycles). A score tile's registers are the next product's operand,
-// so scores never pass through LDS; one barrier a key tile. Bfloat16, heads of 64: 8 images of 4096
-// tokens, 16 heads, 745 us, 740 TFLOP/s (a product of 8192 reaches 1227); 64 of about 717, 12 heads, 207
-// us, 490 TFLOP/s (a sixth of a workgroup's time is its first loads and its last stores); float32, 5
-// images of about 590, 6 heads of 40, 62 us.
+// 49% and products 26% of the busy cycles), as a wave finishes 32 keys before it starts the next 32. A score
+// tile's registers are the next product's operand, so scores never pass through LDS; one barrier a key tile.
+// Bfloat16, heads of 64: 8 images of 4096 tokens, 16 heads, 717 us, 770 TFLOP/s (a product of 8192 reaches 1227);
+// 64 of about 717, 12 heads, 207 us, 490 TFLOP/s (a sixth of a workgroup's time is its first loads and its last
+// stores); float32, 5 images of about 590, 6 heads of 40, 60 us. (After some 30 calls in a row: in the first
+// 20 ms of work the card is up to a third slower.)
+//
+// Heads of 72 to 128 channels keep part of their fragments in scratch memory, 32 to 76 bytes a lane in bfloat16
+// and 316 to 448 in float32; of the others three do, 12 to 20 bytes.
 #include "mpm_attn.h"
 
 namespace mpm {
@@ -317,6 +321,7 @@ hipError_t launch_as(const AttentionCall& a, const HeadRows& q, const HeadRows& 
     return hipGetLastError();
 }
 
+// (Heads of up to 64 channels; wider ones have the form of four waves alone.)
 // Eight waves of 64 queries where an image has queries for several such blocks, or where the bias
 // table leaves LDS for one workgroup only; otherwise four waves of 32, three workgroups a compute
 // unit. Bfloat16, 64 channels, 12 heads, four waves / eight: 8 images of 4096 tokens without a bias

@@ -153,9 +153,10 @@ __device__ __forceinline__ float2 taken(float2 l, bool apart, float c)
 // dK and dV of WAVES x 32 keys of one key head: all queries of all heads that share it. SPLIT 2 (here and
 // below): two waves share 32 rows, each taking every other 32 of the other side, and add up at the end.
 // Four products a tile, of which two read their operand transposed from LDS. 3 images of 4096 tokens,
-// 16 heads of 64, bfloat16: 589 us, 700 TFLOP/s; 32 of about 717, 12 heads: 219 us. Products 28% of the
-// busy cycles, vector instructions 40%, LDS 34%, and a wave waits for one of them half of its time: two
-// waves a SIMD are what the fragments and two gradient tiles of a wave leave room for.
+// 16 heads of 64, bfloat16: 514 us, 800 TFLOP/s; 32 of about 717, 12 heads: 181 us. Products 34% of the
+// busy cycles, vector instructions 48%, LDS 16%, and a wave waits 40% of its time: two waves a SIMD are what
+// the fragments and two gradient tiles of a wave leave room for. Heads of 72 to 128 channels pass them, with 300
+// to 444 bytes a lane in scratch memory (float32, at one wave a SIMD: 36 to 92).
 template <class S, int DH, int BIAS, bool KB, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                       HeadRows k, HeadRows v,
@@ -371,8 +372,9 @@ __host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
 
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: the biases and then the sums
 // (the sums first; kSumAlone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096 tokens, 16
-// heads of 64, bfloat16, 669 us, 460 TFLOP/s (biases from memory); 32 of about 717, 12 heads, 238 us; float32, 4 of
-// about 460, 6 heads, 71 us.
+// heads of 64, bfloat16, 574 us, 540 TFLOP/s (biases from memory); 32 of about 717, 12 heads, 201 us; float32, 4 of
+// about 460, 6 heads, 69 us. Vector instructions 64% of the busy cycles, products 22%, LDS 18%. Bfloat16 heads of
+// 72 to 128 channels keep 84 to 288 bytes a lane in scratch memory.
 template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                         HeadRows k, HeadRows v,
@@ -624,14 +626,15 @@ struct Inputs {
 };
 
 // Eight waves where the query kernel's tables (12 bytes an entry beside 33 KB of tiles) leave LDS for one
-// workgroup only. With 63 x 63 entries, the widest for two, four waves are better (summed in 32 bits, either kernel of 32 images of about 717 tokens: 219 and 224 us with
-// four, 248 and 255 with eight).
+// workgroup only. A step, four waves / eight: 32 images of about 717 tokens with 63 x 63 entries, the widest for two
+// workgroups, 567 / 609 us; 24 of about 760 with 65 x 65 644 / 533, of about 910 with 71 x 71 789 / 678.
 constexpr int kWidestTwice = 63;
 bool large_table(const AttentionCall& a) { return a.dt == kBf16 && a.dh <= 64 && a.bias && 2 * a.span + 1 > kWidestTwice; }
 // Waves of a workgroup and how many share a tile: split where workgroups of 128 rows would leave
-// compute units idle (and the tables of a float32 call leave room for the longer tiles). A whole step,
-// not split / split: bfloat16, 12 heads of up to 1024 tokens, 72 workgroups 118 / 103 us, 288 159 / 174, 576
-// 210 / 234; float32, 6 heads of up to 576, 96 workgroups 257 / 187, 384 462 / 503, 768 837 / 853.
+// compute units idle (and the tables of a float32 call leave room for the longer tiles). Heads of up to 64
+// channels; wider ones are not split. A whole step, not split / split: bfloat16, 12 heads of 1024 tokens, 96
+// workgroups 131 / 112 us, 192 142 / 134, 288 162 / 190, 576 259 / 269; float32, 6 heads of 576 tokens, 90
+// workgroups 247 / 182, 180 271 / 303, 360 479 / 447, 720 731 / 823 (by how the rounds over the compute units end).
 struct Shape {
     int waves, split;
     int rows() const { return 32 * waves / split; }

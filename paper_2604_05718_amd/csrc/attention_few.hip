@@ -8,7 +8,9 @@
 // read from memory (a table in LDS would cost more to bring than the few columns read of it), their
 // keys' positions a tile earlier still: entries asked for only when needed made every tile wait for
 // its successor's loads (82 -> 72 us). One query an image over 16384 keys, 4 images of 16 heads of 64,
-// bfloat16: 268 MB in 55 us (4.9 TB/s), and 6 us to join the splits.
+// bfloat16: 268 MB in 53 us (5.0 TB/s), and 6 us to join the splits. Float32 heads of 72 to 128 channels keep
+// 620 to 860 bytes a lane in scratch memory, bfloat16 ones with a bias and float32 ones of up to 64 with a key bias
+// 56 to 104.
 #include <algorithm>
 
 #include "mpm_attn.h"
@@ -346,7 +348,9 @@ hipError_t pick(const AttentionCall& a, const HeadRows& q, const HeadRows& k, co
 // The queries of the heads that share a key head fit a tile's columns. Tiles of queries instead (12 heads,
 // one query an image, us there / here): 4 images of 16384 keys, 16 heads 477 / 71, 64 of up to 4096
 // 330 / 149, 64 of up to 1024 43 / 41, 64 of 256 24 / 26, one of up to 1024 26 / 23; 20 queries an image:
-// 64 of up to 4096 331 / 204, 64 of up to 1024 44 / 55.
+// 64 of up to 4096 331 / 204, 64 of up to 1024 44 / 55. Heads of 128: 64 of up to 4096 511 / 399, of up to 1024
+// 147 / 116, of up to 256 44 / 47; float32: 16 of up to 4096 224 / 101, 64 of up to 1024 188 / 105, of up to 256 62 / 45;
+// float32 heads of 128: 1340 / 682, 1004 / 656, 204 / 217.
 bool attention_is_few(const AttentionCall& a) { return (long)a.H / a.Hk * a.Nq <= kCols; }
 
 int attention_few_splits(const AttentionCall& a)
