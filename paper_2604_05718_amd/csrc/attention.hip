@@ -346,8 +346,9 @@ hipError_t launch(const AttentionCall& a, const HeadRows& q, const HeadRows& k, 
             // images, 768 workgroups against 384, 360 against 408).
             const long pairs = (long)a.B * a.H;
             const long wide = (pairs * ((a.Nq + 511) / 512) + 255) / 256, narrow = (pairs * ((a.Nq + 255) / 256) + 255) / 256;
-            if (one && 0.6 * (double)narrow < (double)wide)
-                return launch_as<S, DH, BIAS, KB, 8, 1, 1>(a, q, k, v, out, lse, stream);
+            if constexpr (BIAS != kBiasNone)
+                if (one && 0.6 * (double)narrow < (double)wide)
+                    return launch_as<S, DH, BIAS, KB, 8, 1, 1>(a, q, k, v, out, lse, stream);
             return launch_as<S, DH, BIAS, KB, 8, 2, 1>(a, q, k, v, out, lse, stream);
         }
     }

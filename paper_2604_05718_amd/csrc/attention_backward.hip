@@ -700,9 +700,13 @@ hipError_t launch_all(const AttentionCall& a, const Inputs& in, const Grads& g, 
     } else {
         constexpr size_t tiles = buffers<S, DH>() * (tile_bytes<S, DH, SPLIT>() + tile_rows<S, DH, SPLIT>() * 8);
         if (!g.dbias) return launch_queries<S, DH, BIAS, KB, kSumNone, WAVES, SPLIT>(a, in, g, st);
-        if (tiles + table_bytes(BIAS, kSumBeside, W) <= kLdsBytes)
+        // (shape() takes the forms that kSumAlone is not built for where both tables fit only)
+        constexpr bool wide = SPLIT == 1 && (S::kBytes == 4 || DH == 128 || WAVES == 8);
+        if (!wide || tiles + table_bytes(BIAS, kSumBeside, W) <= kLdsBytes) {
             e = launch_queries<S, DH, BIAS, KB, kSumBeside, WAVES, SPLIT>(a, in, g, st);
-        else e = launch_queries<S, DH, BIAS, KB, kSumAlone, WAVES, SPLIT>(a, in, g, st);
+        } else {
+            if constexpr (wide) e = launch_queries<S, DH, BIAS, KB, kSumAlone, WAVES, SPLIT>(a, in, g, st);
+        }
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(bias_parts_kernel, dim3((unsigned)((W * W + kJoinEntries - 1) / kJoinEntries), (unsigned)a.H),
                            dim3(kJoinEntries * kJoinWays), 0, st, a, g.w.parts, query_blocks(a), 32 * WAVES / SPLIT, g.dbias);
