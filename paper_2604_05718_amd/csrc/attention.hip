@@ -51,8 +51,12 @@ constexpr int waves_per_simd()
 }
 
 // WAVES waves of QT tiles of 32 queries each share the key tiles. SPLIT 2: two waves share 32 queries,
-// each taking every other 32 keys, and join their maxima, sums and outputs at the end.
-template <class S, int DH, int BIAS, bool KB, int WAVES, int QT, int SPLIT>
+// each taking every other 32 keys, and join their maxima, sums and outputs at the end. STATS: with the sum of the
+// unrounded probabilities for the statistics (float32: the only sum). Bfloat16 divides by the sum of the rounded ones
+// (frag_sum): the unrounded sum for both / this, without statistics 64 images of about 717 tokens 244 / 253 us, 8 of
+// 4096 750 / 752; with both sums there a step of 3 images of 4096 tokens takes 2% more. One kernel with both sums 255
+// and 804.
+template <class S, int DH, int BIAS, bool KB, int WAVES, int QT, int SPLIT, bool STATS>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void attention_kernel(AttentionCall a, HeadRows q, HeadRows k, HeadRows v,
                                                                 HeadRows out, float* __restrict__ lse, int blocks)
 {
@@ -106,7 +110,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     Frag qf[QT][DH / 16];
     int qcode[QT];
     f32x16 acc[QT][DH / 32];
-    float m[QT], sum[QT];  // what is taken from the scores, and the sum
+    float m[QT], sum[QT], used[QT];  // what is taken from the scores; the sums: unrounded, and (bfloat16) rounded
     bool fresh[QT];        // no key yet
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
@@ -116,7 +120,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                           h);
         // (the position for now: the first loads are all under way before one is waited for)
         qcode[i] = BIAS != kBiasNone && live ? (a.q_pos ? a.q_pos[rq.first + qi] : qi) : 0;
-        m[i] = sum[i] = 0.0f;
+        m[i] = sum[i] = used[i] = 0.0f;
         fresh[i] = true;
 #pragma unroll
         for (int d = 0; d < DH / 32; ++d)
@@ -204,7 +208,8 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
                     }
                     const float f = first ? 0.0f : __builtin_amdgcn_exp2f(m[i] - to);
                     m[i] = to;
-                    sum[i] *= f;
+                    if (STATS) sum[i] *= f;
+                    if (kBf) used[i] *= f;
 #pragma unroll
                     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -227,13 +232,16 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     s[i][r] = __builtin_amdgcn_exp2f(s[i][r]);
-                    sum[i] += s[i][r];
+                    if (STATS) sum[i] += s[i][r];
                 }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
                 Frag p[QT];
 #pragma unroll
-                for (int i = 0; i < QT; ++i) p[i] = tile_frag(s[i], st, S{});
+                for (int i = 0; i < QT; ++i) {
+                    p[i] = tile_frag(s[i], st, S{});
+                    used[i] = frag_sum(p[i], used[i]);
+                }
 #pragma unroll
                 for (int d = 0; d < DH / 32; ++d) {
                     if (!kBf && d > 0 && 32 * d >= a.dh) continue;
@@ -262,10 +270,10 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
     if constexpr (SPLIT == 2) {
         constexpr int kPad = DH + 4;  // floats of a query's outputs, apart in banks
         float* mine = reinterpret_cast<float*>(lds) + (wave * 32 + l32) * kPad;
-        float2* stats = reinterpret_cast<float2*>(reinterpret_cast<float*>(lds) + WAVES / 2 * 32 * kPad) + wave * kWave + lane;
-        static_assert((WAVES / 2 * 32 * kPad + WAVES / 2 * kWave * 2) * 4 <= 2 * kBuffer, "the joined outputs fit");
+        float4* stats = reinterpret_cast<float4*>(reinterpret_cast<float*>(lds) + WAVES / 2 * 32 * kPad) + wave * kWave + lane;
+        static_assert((WAVES / 2 * 32 * kPad + WAVES / 2 * kWave * 4) * 4 <= 2 * kBuffer, "the joined outputs fit");
         if (part == 1) {
-            *stats = make_float2(fresh[0] ? -__builtin_inff() : m[0], sum[0]);
+            *stats = make_float4(fresh[0] ? -__builtin_inff() : m[0], sum[0], used[0], 0.0f);
 #pragma unroll
             for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -275,12 +283,13 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
         }
         __syncthreads();
         if (part == 1) return;
-        const float2 other = *stats;
+        const float4 other = *stats;
         const float own = fresh[0] ? -__builtin_inff() : m[0], top = fmaxf(own, other.x);
         const float f = fresh[0] ? 0.0f : __builtin_amdgcn_exp2f(own - top);
         const float o = other.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(other.x - top);
         m[0] = top;
-        sum[0] = f * sum[0] + o * other.y;
+        if (STATS) sum[0] = f * sum[0] + o * other.y;
+        if (kBf) used[0] = f * used[0] + o * other.z;
 #pragma unroll
         for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -293,14 +302,17 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S, DH, QT>())) void a
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
         const int qi = q0 + (wave * QT + i) * 32 + l32;
-        const float total = halves_sum(sum[i]);
+        const float by = halves_sum(kBf ? used[i] : sum[i]);
         const bool live = qi < rq.count;
-        const float inv = total > 0.0f ? 1.0f / total : (total == 0.0f ? 0.0f : total);  // no key: zeros
+        const float inv = by > 0.0f ? 1.0f / by : (by == 0.0f ? 0.0f : by);  // no key: zeros
         store_rows(out.p + ((rq.first + (live ? qi : 0)) * out.row + (long)hd * out.head) * S::kBytes, acc[i], inv, a.dh,
                    live, h, S{});
-        if (lse && live && h == 0)
-            reinterpret_cast<float2*>(lse)[(rq.first + qi) * a.H + hd] =
-                total == 0.0f ? make_float2(-__builtin_inff(), 0.0f) : make_float2(m[i], __builtin_log2f(total));
+        if constexpr (STATS) {
+            const float total = halves_sum(sum[i]);
+            if (lse && live && h == 0)
+                reinterpret_cast<float2*>(lse)[(rq.first + qi) * a.H + hd] =
+                    total == 0.0f ? make_float2(-__builtin_inff(), 0.0f) : make_float2(m[i], __builtin_log2f(total));
+        }
     }
 }
 
@@ -314,7 +326,9 @@ hipError_t launch_as(const AttentionCall& a, const HeadRows& q, const HeadRows& 
     const int blocks = (a.Nq + kQueries - 1) / kQueries;
     const long grid = block_grid((long)a.B * a.H, blocks);
     if (grid * THREADS > UINT32_MAX) return hipErrorInvalidConfiguration;
-    auto kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT, SPLIT>;
+    auto kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT, SPLIT, true>;
+    if constexpr (S::kBytes == 2)
+        if (lse == nullptr) kernel = attention_kernel<S, DH, BIAS, KB, WAVES, QT, SPLIT, false>;
     hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(THREADS), bytes, stream, a, q, k, v, out, lse, blocks);

@@ -33,18 +33,19 @@ constexpr int wave_bytes()
     return 32 * Tile<S, DH>::kRowBytes + 32 * 8;
 }
 
-// Partial results: (maximum, sum, DH outputs) a column.
+// Partial results: (maximum, sum, sum of what was multiplied, nothing; DH outputs) a column.
 template <int DH>
 constexpr int part_floats()
 {
-    return DH + 2;
+    return DH + 4;
 }
 
-// Four outputs of a column from its joined sums, rounded once, and its statistics.
+// Four outputs of a column from its joined sums (by: of what was multiplied), rounded once, and its statistics.
 template <class S>
-__device__ __forceinline__ void store_column(uint8_t* row, float4 o, float top, float total, int d, int dh, float* lse, S)
+__device__ __forceinline__ void store_column(uint8_t* row, float4 o, float top, float total, float by, int d, int dh,
+                                             float* lse, S)
 {
-    const float inv = total > 0.0f ? 1.0f / total : (total == 0.0f ? 0.0f : total);  // no key: zeros
+    const float inv = by > 0.0f ? 1.0f / by : (by == 0.0f ? 0.0f : by);  // no key: zeros
     if (d < dh) {
         if constexpr (S::kBytes == 2) {
             const f32x2 lo = {o.x * inv, o.y * inv}, hi = {o.z * inv, o.w * inv};
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<S, DH, KB>())) void atten
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
-    float m = -__builtin_inff(), sum = 0.0f;
+    float m = -__builtin_inff(), sum = 0.0f, used = 0.0f;  // (used: as in the kernel of many queries)
 
     for (int tile = first; tile < t1; tile += kWaves) {
 #pragma unroll
@@ -210,6 +211,7 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<S, DH, KB>())) void atten
             const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - up);
             m = up;
             sum *= f;
+            if (S::kBytes == 2) used *= f;
 #pragma unroll
             for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -224,18 +226,20 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<S, DH, KB>())) void atten
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const Frag p = tile_frag(s, st, S{});
+            used = frag_sum(p, used);
 #pragma unroll
             for (int d = 0; d < DH / 32; ++d) acc[d] = mma(cols_frag<S, DH>(vt, 16 * st, 32 * d, lane), p, acc[d]);
         }
         __builtin_amdgcn_wave_barrier();
     }
     sum = halves_sum(sum);
+    used = S::kBytes == 2 ? halves_sum(used) : sum;
 
-    // The waves' results meet in LDS: (maximum, sum) and outputs of every column.
+    // The waves' results meet in LDS: (maximum, sums) and outputs of every column.
     __syncthreads();
     float* ms = reinterpret_cast<float*>(lds);
-    float* outs = ms + kWaves * kCols * 2;
-    if (h == 0) reinterpret_cast<float2*>(ms)[wave * kCols + l32] = make_float2(m, sum);
+    float* outs = ms + kWaves * kCols * 4;
+    if (h == 0) reinterpret_cast<float4*>(ms)[wave * kCols + l32] = make_float4(m, sum, used, 0.0f);
 #pragma unroll
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
@@ -247,29 +251,26 @@ __global__ __launch_bounds__(kThreads, (waves_per_simd<S, DH, KB>())) void atten
     for (int i = t; i < group * a.Nq * per; i += kThreads) {
         const int col = i / per, d = i % per * 4, q_i = col % a.Nq, head = hk * group + col / a.Nq;
         if (q_i >= rq.count) continue;
-        float top = -__builtin_inff(), total = 0.0f;
+        float top = -__builtin_inff(), total = 0.0f, by = 0.0f;
         float4 o = make_float4(0, 0, 0, 0);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ms[2 * (w * kCols + col)]);
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ms[4 * (w * kCols + col)]);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float2 s = reinterpret_cast<const float2*>(ms)[w * kCols + col];
+            const float4 s = reinterpret_cast<const float4*>(ms)[w * kCols + col];
             const float f = s.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(s.x - top);
             const float4 x = *reinterpret_cast<const float4*>(outs + (w * kCols + col) * kPad + d);
             total += f * s.y;
+            by += f * s.z;
             o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, x.z, o.z), fmaf(f, x.w, o.w));
         }
         if (splits > 1) {
             float* part = parts + (((long)pair * splits + split) * group * a.Nq + col) * part_floats<DH>();
-            if (d == 0) {
-                part[0] = top;
-                part[1] = total;
-            }
-            *reinterpret_cast<float2*>(part + 2 + d) = make_float2(o.x, o.y);
-            *reinterpret_cast<float2*>(part + 4 + d) = make_float2(o.z, o.w);
+            if (d == 0) *reinterpret_cast<float4*>(part) = make_float4(top, total, by, 0.0f);
+            *reinterpret_cast<float4*>(part + 4 + d) = o;
             continue;
         }
-        store_column(out.p + ((rq.first + q_i) * out.row + (long)head * out.head) * S::kBytes, o, top, total, d, a.dh,
+        store_column(out.p + ((rq.first + q_i) * out.row + (long)head * out.head) * S::kBytes, o, top, total, by, d, a.dh,
                      lse ? lse + 2 * ((rq.first + q_i) * a.H + head) : nullptr, S{});
     }
 }
@@ -291,18 +292,19 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionCall 
     if (q_i >= rq.count) return;
     const float* part = parts + ((long)pair * splits * cols + col) * part_floats<DH>();
     const long step = (long)cols * part_floats<DH>();
-    float top = -__builtin_inff(), total = 0.0f;
+    float top = -__builtin_inff(), total = 0.0f, by = 0.0f;
     for (int s = 0; s < splits; ++s) top = fmaxf(top, part[s * step]);
     float4 o = make_float4(0, 0, 0, 0);
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) {
         const float* p = part + s * step;
         const float f = p[0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(p[0] - top);
-        const float2 x = *reinterpret_cast<const float2*>(p + 2 + d), y = *reinterpret_cast<const float2*>(p + 4 + d);
+        const float4 x = *reinterpret_cast<const float4*>(p + 4 + d);
         total += f * p[1];
-        o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, y.x, o.z), fmaf(f, y.y, o.w));
+        by += f * p[2];
+        o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, x.z, o.z), fmaf(f, x.w, o.w));
     }
-    store_column(out.p + ((rq.first + q_i) * out.row + (long)head * out.head) * S::kBytes, o, top, total, d, a.dh,
+    store_column(out.p + ((rq.first + q_i) * out.row + (long)head * out.head) * S::kBytes, o, top, total, by, d, a.dh,
                  lse ? lse + 2 * ((rq.first + q_i) * a.H + head) : nullptr, S{});
 }
 
@@ -311,7 +313,7 @@ hipError_t launch(const AttentionCall& a, const HeadRows& q, const HeadRows& k, 
                   float* lse, float* parts, hipStream_t st)
 {
     const int splits = attention_few_splits(a);
-    const size_t joined = kWaves * kCols * (2 + DH + 4) * 4;
+    const size_t joined = kWaves * kCols * (4 + DH + 4) * 4;
     const size_t bytes = std::max((size_t)kWaves * wave_bytes<S, DH>(), joined);
     const long pairs = (long)a.B * a.Hk;
     if (pairs * splits * kThreads > UINT32_MAX) return hipErrorInvalidConfiguration;
@@ -364,7 +366,7 @@ size_t attention_few_bytes(const AttentionCall& a)
 {
     const int splits = attention_few_splits(a);
     if (splits == 1) return 0;
-    return (size_t)a.B * a.H * a.Nq * splits * ((a.dh <= 64 ? 64 : 128) + 2) * 4;
+    return (size_t)a.B * a.H * a.Nq * splits * (a.dh <= 64 ? part_floats<64>() : part_floats<128>()) * 4;
 }
 
 hipError_t launch_attention_few(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,

@@ -126,6 +126,20 @@ __device__ __forceinline__ f32x8 tile_frag(const f32x16& p, int s, F32)
     return w;
 }
 
+// Adds the eight values of such an operand. A row's probabilities are divided by the sum of what was multiplied: with
+// the sum of the unrounded ones a row that one key has all of would come out as that key's values times a rounding.
+__device__ __forceinline__ float frag_sum(bf16x8 p, float sum)
+{
+    const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const bf16x2 v = {p[i], p[i + 1]};
+        sum = __builtin_amdgcn_fdot2_f32_bf16(v, one, sum, false);
+    }
+    return sum;
+}
+__device__ __forceinline__ float frag_sum(f32x8, float sum) { return sum; }
+
 // Sum and maximum of a value over the two halves of a wave (lanes l and l ^ 32).
 __device__ __forceinline__ float halves_max(float v)
 {

@@ -334,3 +334,31 @@ def test_scales(dtype, scale):
     assert ref.rel(out, want) <= FWD[dtype] * slack
     for got, w in zip((g.dq, g.dk, g.dv, g.dbias), wg):
         assert ref.rel(got, w) <= BWD[dtype] * slack
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("score", [0.0, 0.3, -7.7, 30.0])
+@pytest.mark.parametrize("nq", [3, 200])
+def test_rows_that_one_key_has_all_of(dtype, score, nq):
+    """One key an image, or one that outweighs the others by 2^40: its values come out as they are (in float32
+    up to the roundings of p v, 1 / p and their product, below 2^-22), and the score gradients, zero by the formula, are what float32 sums of dh products of a row leave (2^-24 times dh of its
+    largest, the norm of dout.v), through scale k into dq."""
+    g = torch.Generator().manual_seed(440)
+    q, d = (torch.randn(2 * nq, 2, 64, generator=g).to(dtype) for _ in range(2))
+    k, v = (torch.randn(301, 2, 64, generator=g).to(dtype) for _ in range(2))
+    k_bias = torch.full((301,), score)
+    k_bias[2:] -= 60.0
+    dev = lambda t: t.to(DEV)
+    kw = dict(q_off=dev(offsets([nq, nq])), k_off=dev(offsets([1, 300])), Nq=nq, Nk=300, k_bias=dev(k_bias),
+              bias=torch.zeros(2, 9, 9, device=DEV), grid=(20, 20))
+    out, lse = mpm.attention(dev(q), dev(k), dev(v), with_lse=True, **kw)
+    r = mpm.attention_backward(dev(d), dev(q), dev(k), dev(v), out, lse, **kw)
+    torch.cuda.synchronize()
+    one = v[[0] * nq + [1] * nq].double()
+    assert torch.all((out.cpu().double() - one).abs() <= (0 if dtype == BF else 2.0 ** -22) * one.abs())
+    ds = 64 * 2.0 ** -24 * (d.double().norm(dim=-1) * one.norm(dim=-1)).max()
+    assert float(r.dbias.abs().max()) <= ds * nq * 2
+    assert float(r.dq.float().abs().max()) <= 0.125 * ds * float(k.float().abs().max()) * 2
+    want = torch.zeros(301, 2, 64, dtype=torch.float64)
+    want[0], want[1] = d[:nq].double().sum(0), d[nq:].double().sum(0)
+    assert ref.rel(r.dv[:2], want[:2]) <= BWD[dtype]
