@@ -10,13 +10,13 @@
 // a conversion, and those and the products hardly overlap (3 images of 4096 tokens: vector instructions
 // 49% and products 26% of the busy cycles), as a wave finishes 32 keys before it starts the next 32. A score
 // tile's registers are the next product's operand, so scores never pass through LDS; one barrier a key tile.
-// Bfloat16, heads of 64: 8 images of 4096 tokens, 16 heads, 717 us, 770 TFLOP/s (a product of 8192 reaches 1227);
-// 64 of about 717, 12 heads, 207 us, 490 TFLOP/s (a sixth of a workgroup's time is its first loads and its last
+// Bfloat16, heads of 64: 8 images of 4096 tokens, 16 heads, 712 us, 770 TFLOP/s (a product of 8192 reaches 1227);
+// 64 of about 717, 12 heads, 222 us, 460 TFLOP/s (a sixth of a workgroup's time is its first loads and its last
 // stores); float32, 5 images of about 590, 6 heads of 40, 60 us. (After some 30 calls in a row: in the first
 // 20 ms of work the card is up to a third slower.)
 //
-// Heads of 72 to 128 channels keep part of their fragments in scratch memory, 32 to 76 bytes a lane in bfloat16
-// and 316 to 448 in float32; of the others three do, 12 to 20 bytes.
+// Heads of 72 to 128 channels keep part of their fragments in scratch memory, 24 to 108 bytes a lane in bfloat16
+// and 316 to 448 in float32; of the others six do, 8 to 32 bytes.
 #include "mpm_attn.h"
 
 namespace mpm {

@@ -9,7 +9,7 @@
 // keys' positions a tile earlier still: entries asked for only when needed made every tile wait for
 // its successor's loads (82 -> 72 us). One query an image over 16384 keys, 4 images of 16 heads of 64,
 // bfloat16: 268 MB in 53 us (5.0 TB/s), and 6 us to join the splits. Float32 heads of 72 to 128 channels keep
-// 620 to 860 bytes a lane in scratch memory, bfloat16 ones with a bias and float32 ones of up to 64 with a key bias
+// 630 to 870 bytes a lane in scratch memory, bfloat16 ones with a bias and float32 ones of up to 64 with a key bias
 // 56 to 104.
 #include <algorithm>
 
