@@ -12,8 +12,8 @@
 // sum does not depend on their order. The unit is a power of two for which no sum can pass the integer's
 // range, found from the largest |dS|, which the key kernel, running first, leaves for every image and head:
 // at most 2^-39 of it (256 queries and 16384 keys; 2^-44 for 128 and 1024), so that far offsets under sharp
-// attention keep their gradients. (32 bits cost 2% less of a step of 32 images of about 717 tokens, 9% less of one of 3 of 4096 with
-// 127 x 127 entries, and lose every term below 2^-23 of the largest.)
+// attention keep their gradients. (32 bits cost 2% less of a step of 32 images of about 717 tokens, 9% less of one
+// of 3 of 4096 with 127 x 127 entries, and lose every term below 2^-23 of the largest.)
 #include "mpm_attn.h"
 
 namespace mpm {
@@ -81,8 +81,8 @@ constexpr int waves_per_simd()
 }
 
 // What the kernels leave for each other: D of every query and head, the largest |dS| of every image and head
-// (as bits). D is kept by image slot, not by
-// packed row: the packed offsets of a call on some images of a larger tensor start past zero.
+// (as bits). D is kept by image slot, not by packed row: the packed offsets of a call on some images of a larger
+// tensor start past zero.
 struct Scratch {
     float* delta;       // [B][Nq][H]
     uint32_t* largest;  // [B][H]
@@ -129,9 +129,10 @@ __global__ __launch_bounds__(kDeltaThreads) void delta_kernel(AttentionCall a, H
 
 // What is taken from a query's scores before the exponential: the maximum and the log of the sum
 // (`apart`), or their sum where it is small enough to hold both (the log is at most 16, the forward's slack, and
-// 14 for the keys: the sum stays below 128 and its rounding, the error of the exponent, below 2^-18). A mask value such as -1e9 on every key makes the maximum too large for
-// that: then the two go one after the other, as in the forward pass. In bfloat16 calls the sum is
-// not subtracted at all: the score products start from minus it over the factor of the scores.
+// 14 for the keys: the sum stays below 128 and its rounding, the error of the exponent, below 2^-18). A mask
+// value such as -1e9 on every key makes the maximum too large for that: then the two go one after the other, as
+// in the forward pass. In bfloat16 calls the sum is not subtracted at all: the score products start from minus
+// it over the factor of the scores.
 constexpr float kJoinMost = 64.0f;
 __device__ __forceinline__ bool too_large(float2 l) { return fabsf(l.x) > kJoinMost && l.x > -__builtin_inff(); }
 
@@ -354,11 +355,11 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void key_gradi
     store_rows(dv.p + (krow * dv.row + (long)hk * dv.head) * S::kBytes, gv, 1.0f, a.dh, exists, h, S{});
 }
 
-// Largest power of two lg for which x 2^lg < 2^bits, within what the exponents bear.
+// Largest power of two lg for which x 2^lg < 2^bits (zero and what is not finite: any).
 __device__ __forceinline__ int raise_to(float x, int bits)
 {
     if (!(x > 0.0f) || !(x < __builtin_inff())) return 0;
-    return min(max(bits - (__builtin_amdgcn_frexp_expf(x)), -100), 100);
+    return bits - __builtin_amdgcn_frexp_expf(x);
 }
 // Bits of a term, so that `terms` of them stay within 62 (and one within the 51 that a double's fixed point holds).
 __device__ __forceinline__ int term_bits(int terms) { return min(50, 62 - (32 - __builtin_clz(max(terms - 1, 1)))); }
@@ -371,9 +372,9 @@ __host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
 }
 
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: the biases and then the sums
-// (the sums first; kSumAlone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096 tokens, 16
-// heads of 64, bfloat16, 574 us, 540 TFLOP/s (biases from memory); 32 of about 717, 12 heads, 201 us; float32, 4 of
-// about 460, 6 heads, 69 us. Vector instructions 64% of the busy cycles, products 22%, LDS 18%. Bfloat16 heads of
+// (the sums first; kSumAlone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096
+// tokens, 16 heads of 64, bfloat16, 574 us, 540 TFLOP/s (biases from memory); 32 of about 717, 12 heads, 201 us;
+// float32, 4 of about 460, 6 heads, 69 us. Vector instructions 64% of the busy cycles, products 22%, LDS 18%. Bfloat16 heads of
 // 72 to 128 channels keep 84 to 288 bytes a lane in scratch memory.
 template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
@@ -565,7 +566,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         __syncthreads();
     }
 
-    const float back = __builtin_ldexpf(1.0f, -lg);
+    const double back = __builtin_ldexp(1.0, -lg);
     if constexpr (SPLIT == 2) {
         float* mine = reinterpret_cast<float*>(lds) + wave * (DH / 32 * 16 * kWave);
         static_assert(WAVES / 2 * DH / 32 * 16 * kWave * 4 <= BUFS * kBuffer, "the shared sums fit");
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gra
         const bool any_bad = __syncthreads_or(bad && live && share == 0);
         float* part = w.parts + ((long)pair * blocks + blk) * W2;
         for (int e = t; e < W2; e += THREADS)
-            part[e] = any_bad ? __builtin_nanf("") : (float)(long long)sums[e] * back;
+            part[e] = any_bad ? __builtin_nanf("") : (float)((double)(long long)sums[e] * back);
     }
     store_rows(dq.p + (qrow * dq.row + (long)hd * dq.head) * S::kBytes, gq, a.scale, a.dh, live && share == 0, h, S{});
 }

@@ -362,3 +362,19 @@ def test_rows_that_one_key_has_all_of(dtype, score, nq):
     want = torch.zeros(301, 2, 64, dtype=torch.float64)
     want[0], want[1] = d[:nq].double().sum(0), d[nq:].double().sum(0)
     assert ref.rel(r.dv[:2], want[:2]) <= BWD[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -60, 2.0 ** 60, 2.0 ** 100])
+@pytest.mark.parametrize("span", [11, 63])
+def test_gradients_of_any_size(dtype, size, span):
+    """Gradients scale with dout over the type's range, the bias's too."""
+    c = Case(dtype, [60, 90], None, 2, 2, 32, (12, 12) if span == 11 else (64, 64), span, "sorted", False, seed=450)
+    c.dout = (c.dout.float() * size).to(dtype)
+    q, k, v = c.dev()
+    out, lse = mpm.attention(q, k, v, with_lse=True, **c.kw())
+    g = mpm.attention_backward(c.dout.to(DEV), q, k, v, out, lse, **c.kw())
+    torch.cuda.synchronize()
+    _, _, want = c.plain(grads=True)
+    for got, w in zip((g.dq, g.dk, g.dv, g.dbias), want):
+        assert ref.rel(got, w) <= BWD[dtype]
