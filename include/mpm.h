@@ -519,8 +519,9 @@ typedef struct mpm_attention_call {
  *   s = scale q . k + bias + k_bias,  out = softmax(s) v,
  * scores, softmax statistics and sums in float32, out rounded once to dt. A query without a key
  * (an image with none, or all dropped or at -inf) gets zeros. Bfloat16 rounds the
- * probabilities, before their division, to bfloat16 for their product with v, and divides by the sum of the
- * rounded ones. Sums are kept before the division: values of v of 2^96 and more in magnitude may overflow them, and below 2^-86 lose precision.
+ * probabilities, before their division, to bfloat16 for their product with v, and divides by the sum of
+ * the rounded ones. Sums are kept before the division: values of v of 2^96 and more in magnitude may
+ * overflow them, and those below 2^-86 lose precision.
  *   lse (may be NULL): float [query row][H][2], contiguous, 8-byte aligned, needed for the gradients: the
  *     maximum m that was taken from the scores and l = log2 sum 2^(s log2(e) - m), both in base 2: the
  *     log-sum-exp is (m + l) ln 2 (a query without a key: -inf, 0). Two numbers, since under a mask

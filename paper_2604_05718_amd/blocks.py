@@ -61,8 +61,8 @@ class _Attention(torch.autograd.Function):
         H, grad, learned = ctx.heads, torch.empty_like(qkv), ctx.needs_input_grad[1]
         parts = [slice(0, H), slice(H, 2 * H), slice(2 * H, 3 * H)]
         g = block_ops.attention_backward(dout.contiguous(), *(qkv[:, p] for p in parts), out, lse, bias=bias,
-                                         dq=grad[:, parts[0]], dk=grad[:, parts[1]], dv=grad[:, parts[2]], with_dbias=learned,
-                                         **ctx.rest, **dict(zip(ctx.tensors, tensors)))
+                                         dq=grad[:, parts[0]], dk=grad[:, parts[1]], dv=grad[:, parts[2]],
+                                         with_dbias=learned, **ctx.rest, **dict(zip(ctx.tensors, tensors)))
         dtable = block_ops.bias_gradient(g.dbias, lut, ctx.buckets, dtype=table.dtype) if learned else None
         return *_once((grad, dtable), dout, qkv, table), None, None, None
 

@@ -374,8 +374,8 @@ __host__ __device__ constexpr size_t table_bytes(int bias, int sum, int W)
 // dQ of WAVES x 32 queries of one head, and their part of dbias. Tables in LDS: the biases and then the sums
 // (the sums first; kSumAlone: the sums only). Three products a tile, and an LDS atomic a score: 3 images of 4096
 // tokens, 16 heads of 64, bfloat16, 574 us, 540 TFLOP/s (biases from memory); 32 of about 717, 12 heads, 201 us;
-// float32, 4 of about 460, 6 heads, 69 us. Vector instructions 64% of the busy cycles, products 22%, LDS 18%. Bfloat16 heads of
-// 72 to 128 channels keep 84 to 288 bytes a lane in scratch memory.
+// float32, 4 of about 460, 6 heads, 69 us. Vector instructions 64% of the busy cycles, products 22%, LDS 18%.
+// Bfloat16 heads of 72 to 128 channels keep 84 to 288 bytes a lane in scratch memory.
 template <class S, int DH, int BIAS, bool KB, int SUM, int WAVES, int SPLIT>
 __global__ __launch_bounds__(WAVES* kWave, (waves_per_simd<S>())) void query_gradient_kernel(AttentionCall a, HeadRows dout, HeadRows q,
                                                                         HeadRows k, HeadRows v,
