@@ -638,6 +638,155 @@ int mpm_residual_norm_backward(const mpm_norm_call* call, const void* dy, const 
                                const void* f, const float* stats, const mpm_norm_grads* grads, void* ws,
                                size_t ws_bytes, void* stream);
 
+/* ---- Rotary positions, products in 8-bit integers and group norm: an encoder whose positions are
+ * rotations, its serving form, and the norm of the decoder on the rebuilt grid. Conventions as above; NaN
+ * and infinities flow through as in the formulas (checked mode validates the offsets only). ---- */
+
+typedef enum {
+    MPM_ROTARY_HALVES = 0, /* pair p of a head: channels p and p + pairs */
+    MPM_ROTARY_PAIRS = 1   /* pair p of a head: channels 2 p and 2 p + 1 */
+} mpm_rotary_layout;
+
+#define MPM_MAX_AXES 3
+
+/*
+ * Rows of heads and the angles they are turned by.
+ *   R rows of H heads of dh channels (a multiple of 8 (bf16) or 4 (f32), at most MPM_MAX_HEAD_DIM), of
+ *   which the first 2 * pairs are turned, pair by pair, and the others pass.
+ *   axes (1 ... MPM_MAX_AXES) axes of a grid of grid[0] x ... x grid[axes - 1] cells (at most 2^31 - 1),
+ *   the last one running fastest: (row, column) of an image, (time, row, column) of a clip.
+ *   pos: int32[R], each row's raster index on that grid (any order; one outside the grid counts as the
+ *     nearest cell index); NULL: its index in its image.
+ *   freq: float [axes][pairs], or [H][axes][pairs] with freq_per_head: a row at cell (c_0, ...) turns
+ *     pair p by sum_a c_a freq[a][p] radians. Angles are formed in 64 bits.
+ *   off (may be NULL): int32[B+1], the packed images. Rows before off[0] and from off[B] on belong to no
+ *     image and are not turned. NULL: every row is turned, in images of R / B rows each.
+ */
+typedef struct mpm_rotary_call {
+    int32_t R, H, dh, dt;
+    int32_t pairs, layout;
+    int32_t axes, grid[MPM_MAX_AXES];
+    int32_t freq_per_head;
+    const float* freq;
+    const int32_t* pos;
+    int32_t B;
+    const int32_t* off;
+} mpm_rotary_call;
+
+/*
+ * out = x with every pair (a, b) turned to (a cos - b sin, a sin + b cos), in float32 and rounded once to
+ * dt; by the negative angle with inverse != 0. out may be x; otherwise the two must not overlap.
+ * Rows of no image are not written. Bfloat16 takes the processor's sine and cosine (absolute error
+ * below 2^-19), float32 the library's (a few 2^-24).
+ * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned pointers, sizes below 1, dh or strides as for
+ * mpm_attention, pairs above dh / 2, a grid of more than 2^31 - 1 cells, bad dt, layout or axes, B that does
+ * not divide R (off NULL); MPM_ERR_UNSUPPORTED for H > MPM_MAX_HEADS, dh > MPM_MAX_HEAD_DIM or
+ * B > MPM_MAX_B; MPM_ERR_HIP.
+ */
+int mpm_rotary(const mpm_rotary_call* call, const mpm_heads* x, const mpm_heads* out, int32_t inverse, void* stream);
+
+/*
+ * The gradients of mpm_rotary from dout:
+ *   dx: dout turned by the negative angles (zeros in rows of no image); may be dout itself;
+ *   dfreq (may be NULL): float, shaped as freq: the sum over rows (and over heads, where they share
+ *     frequencies) of c_a (x_1 dx_2 - x_2 dx_1), dx before its rounding; x (only with dfreq; else NULL) is the
+ *     forward call's x, and dx must not overlap it. Sums in float32 in a workgroup, in 64 bits over them, in
+ *     a fixed order.
+ * ws: mpm_rotary_backward_workspace_bytes(call) bytes with dfreq; none without. Errors as mpm_rotary,
+ * MPM_ERR_INVALID_ARG for dfreq without x or x without dfreq, and MPM_ERR_WORKSPACE.
+ */
+size_t mpm_rotary_backward_workspace_bytes(const mpm_rotary_call* call);
+int mpm_rotary_backward(const mpm_rotary_call* call, const mpm_heads* dout, const mpm_heads* x, const mpm_heads* dx,
+                        float* dfreq, void* ws, size_t ws_bytes, void* stream);
+
+typedef enum {
+    MPM_ACT_NONE = 0,
+    MPM_ACT_RELU = 1, /* max(z, 0); slope 0 at 0 */
+    MPM_ACT_SILU = 2, /* z / (1 + e^-z) */
+    MPM_ACT_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
+} mpm_activation;
+
+#define MPM_I8 2           /* signed 8-bit steps, as mpm_quantize_rows writes them (an mpm_dtype of x only) */
+#define MPM_MAX_K8 65536   /* widest row of 8-bit steps: sums of products stay below 2^30 */
+#define MPM_MAX_N8 1048576 /* most output channels of mpm_linear_int8 */
+
+/*
+ * Rows of K values (dtype dt, a multiple of 8 (bf16) or 4 (f32); row r at x + r * x_row elements, x_row a whole
+ * number of 16 bytes) as signed 8-bit steps with a scale each:
+ *   scale[r] = max(max_k |x| / 127, 2^-126), rounded to float32;
+ *   q[r][k] = x / scale[r] rounded to the nearest integer, ties to even, held to [-127, 127]: the rounding of
+ *     the real quotient, not of its float32 value.
+ * A row with a NaN or an infinity gets the scale NaN and steps 0. q rows are K bytes and zeros up to the next
+ * multiple of 16. Errors: MPM_ERR_INVALID_ARG for NULL or misaligned (q, x: 16, scale: 4) pointers, sizes
+ * below 1, K or x_row as above, bad dt; MPM_ERR_UNSUPPORTED for K > MPM_MAX_K8; MPM_ERR_HIP.
+ */
+int mpm_quantize_rows(const void* x, int32_t R, int32_t K, int64_t x_row, int32_t dt, int8_t* q, float* scale,
+                      void* stream);
+
+/*
+ * A product in 8-bit integers, with a scale for each token and each output channel:
+ *   out[m][n] = act(x_scale[m] w_scale[n] (sum_k q[m][k] w[n][k]) + bias[n]),
+ * the sum exact in 32-bit integers, the rest in float32, rounded once to dt (the scales are multiplied into
+ * the sum one after the other, x_scale 2^-24 first and then w_scale 2^24: x_scale below 2^-102 loses
+ * precision, w_scale has to be below 2^104).
+ *   M tokens of K values; x_dt MPM_I8: x holds the steps, rows of K bytes rounded up to a multiple of 16, and
+ *     x_scale their scales; MPM_F32 / MPM_BF16: x holds values, rows at x_row elements as in mpm_quantize_rows,
+ *     which are turned into steps on the way (x_scale NULL);
+ *   w: int8 [N] rows of K bytes rounded up to a multiple of 16 (mpm_quantize_rows of the weights [N][K]). The
+ *     bytes from K on are multiplied too: x's or w's have to be zero, as mpm_quantize_rows leaves them;
+ *   w_scale: float[N]; bias (may be NULL): N values of dtype dt;
+ *   out: row m at out + m * out_row elements, out_row >= N (any alignment of whole elements; rows of whole
+ *     16 bytes are written 16 bytes at a time). out must not overlap the inputs.
+ *   ws: mpm_linear_int8_workspace_bytes(call) bytes (0 for steps, and for few tokens), 256-byte aligned.
+ * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned pointers (x, w: 16 bytes; w_scale, x_scale: 4; bias,
+ * out: an element), sizes below 1, K or strides as above, bad dt, x_dt or act, x_scale that does not go with
+ * x_dt; MPM_ERR_UNSUPPORTED for K > MPM_MAX_K8 or N > MPM_MAX_N8; MPM_ERR_WORKSPACE; MPM_ERR_HIP.
+ */
+typedef struct mpm_linear8_call {
+    int32_t M, N, K, x_dt, dt, act;
+    int64_t x_row, out_row;
+    const float* x_scale;
+    const int8_t* w;
+    const float* w_scale;
+    const void* bias;
+} mpm_linear8_call;
+
+size_t mpm_linear_int8_workspace_bytes(const mpm_linear8_call* call);
+int mpm_linear_int8(const mpm_linear8_call* call, const void* x, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Group norm with an activation, channels last. B images of rows of C channels (16-byte rows, as tokens;
+ * contiguous, R in all): dense (off NULL: R / B rows each) or packed (off int32[B+1]); groups divides C. Per
+ * image and group of C / groups channels, over all its rows:
+ *   t = (x - mean) / sqrt(variance + eps),  y = act(t w + b)
+ * (w, b: C values of dtype dt each, may be NULL: ones, zeros; b only with w).
+ */
+typedef struct mpm_group_norm_call {
+    int32_t R, C, groups, dt, act;
+    float eps;
+    int32_t B;
+    const int32_t* off;
+    const void* w;
+    const void* b;
+} mpm_group_norm_call;
+
+/*
+ * Forward: statistics and the rest in float32, y rounded once to dt; y may be x itself. Rows of no image are
+ * not written. stats (may be NULL): float[B][groups][2], mean and 1 / deviation (zeros for an empty image).
+ * Backward, from dy, x and stats: dx (zeros in rows of no image; may be dy or x itself), and dw, db (C values of
+ * dtype dt, each asked for if and only if w, b is given), summed over the images in a fixed order.
+ * ws: the given number of bytes (may be 0), 256-byte aligned.
+ * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned (16-byte; stats: 8) pointers, sizes below 1, C as for
+ * tokens, groups that do not divide C, eps < 0 or not finite, b without w, bad dt or act, B that does not divide R
+ * (off NULL); MPM_ERR_UNSUPPORTED for C > MPM_MAX_D or B > MPM_MAX_B; MPM_ERR_WORKSPACE; MPM_ERR_HIP.
+ */
+size_t mpm_group_norm_workspace_bytes(const mpm_group_norm_call* call);
+int mpm_group_norm(const mpm_group_norm_call* call, const void* x, void* y, float* stats, void* ws, size_t ws_bytes,
+                   void* stream);
+size_t mpm_group_norm_backward_workspace_bytes(const mpm_group_norm_call* call);
+int mpm_group_norm_backward(const mpm_group_norm_call* call, const void* dy, const void* x, const float* stats, void* dx,
+                            void* dw, void* db, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

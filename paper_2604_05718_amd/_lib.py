@@ -27,6 +27,13 @@ MPM_SCHEDULE_FULL_64 = 3
 MPM_NORM_LAYER = 0
 MPM_NORM_RMS = 1
 MPM_MAX_SPAN = 63
+MPM_I8 = 2
+MPM_ROTARY_HALVES = 0
+MPM_ROTARY_PAIRS = 1
+MPM_ACT_NONE = 0
+MPM_ACT_RELU = 1
+MPM_ACT_SILU = 2
+MPM_ACT_GELU = 3
 
 _vp = ctypes.c_void_p
 _i32 = ctypes.c_int32
@@ -60,7 +67,28 @@ class NormGrads(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("dx", "df", "dw", "db", "dpost_w", "dpost_b", "dscale", "dgate")]
 
 
+class RotaryCall(ctypes.Structure):
+    """mpm_rotary_call."""
+    _fields_ = [(n, _i32) for n in ("R", "H", "dh", "dt", "pairs", "layout", "axes")] + [("grid", _i32 * 3)] + [
+        ("freq_per_head", _i32), ("freq", _vp), ("pos", _vp), ("B", _i32), ("off", _vp)]
+
+
+class Linear8Call(ctypes.Structure):
+    """mpm_linear8_call."""
+    _fields_ = [(n, _i32) for n in ("M", "N", "K", "x_dt", "dt", "act")] + [
+        (n, ctypes.c_int64) for n in ("x_row", "out_row")] + [(n, _vp) for n in ("x_scale", "w", "w_scale", "bias")]
+
+
+class GroupNormCall(ctypes.Structure):
+    """mpm_group_norm_call."""
+    _fields_ = [(n, _i32) for n in ("R", "C", "groups", "dt", "act")] + [("eps", ctypes.c_float), ("B", _i32)] + [
+        (n, _vp) for n in ("off", "w", "b")]
+
+
 _hp = ctypes.POINTER(Heads)
+_rp = ctypes.POINTER(RotaryCall)
+_lp = ctypes.POINTER(Linear8Call)
+_gp = ctypes.POINTER(GroupNormCall)
 _ap = ctypes.POINTER(AttentionCall)
 _np = ctypes.POINTER(NormCall)
 
@@ -106,6 +134,16 @@ SIGNATURES = {
     "mpm_residual_norm_backward_workspace_bytes": (_sz, [_np]),
     "mpm_residual_norm_backward": (ctypes.c_int, [_np, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(NormGrads), _vp, _sz,
                                                   _vp]),
+    "mpm_rotary": (ctypes.c_int, [_rp, _hp, _hp, _i32, _vp]),
+    "mpm_rotary_backward_workspace_bytes": (_sz, [_rp]),
+    "mpm_rotary_backward": (ctypes.c_int, [_rp, _hp, _hp, _hp, _vp, _vp, _sz, _vp]),
+    "mpm_quantize_rows": (ctypes.c_int, [_vp, _i32, _i32, ctypes.c_int64, _i32, _vp, _vp, _vp]),
+    "mpm_linear_int8_workspace_bytes": (_sz, [_lp]),
+    "mpm_linear_int8": (ctypes.c_int, [_lp, _vp, _vp, _vp, _sz, _vp]),
+    "mpm_group_norm_workspace_bytes": (_sz, [_gp]),
+    "mpm_group_norm": (ctypes.c_int, [_gp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "mpm_group_norm_backward_workspace_bytes": (_sz, [_gp]),
+    "mpm_group_norm_backward": (ctypes.c_int, [_gp] + [_vp] * 7 + [_sz, _vp]),
     "mpm_unmerge": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
 }
 

@@ -1,6 +1,6 @@
 """Torch-facing binding of the operators of the blocks between the merges: attention over
-packed images with a learned relative position bias, and the norms around a block with its
-gate and residual scale, each with its gradients.
+packed images with a learned relative position bias, rotary positions, the norms around a block with its
+gate and residual scale, group norm over grids, each with its gradients; and products in 8-bit integers.
 
 Argument marshalling only, as in api.py: every step runs in the HIP kernels of libmpm.so on
 ``torch.cuda.current_stream()``. No autograd history: results of tensors that require gradients are detached
@@ -24,6 +24,8 @@ from .api import _dt
 
 _BYREF = ctypes.byref
 _raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's handle, without its Python object
+_LAYOUTS = {"halves": _lib.MPM_ROTARY_HALVES, "pairs": _lib.MPM_ROTARY_PAIRS}
+_ACTIVATIONS = {"none": _lib.MPM_ACT_NONE, "relu": _lib.MPM_ACT_RELU, "silu": _lib.MPM_ACT_SILU, "gelu": _lib.MPM_ACT_GELU}
 _NORMS = {"layer": _lib.MPM_NORM_LAYER, "rms": _lib.MPM_NORM_RMS}
 
 
@@ -304,4 +306,236 @@ def residual_norm_backward(dy, dh, y, f, stats, weight=None, bias=None, post_wei
         _BYREF(c), _device(dy, "dy", y.dtype, y, n), _device(dh, "dh", y.dtype, y, n), _ptr(y),
         _device(f, "f", y.dtype, y, n), _device(stats, "stats", torch.float32, y, 4 * y.shape[0]), _BYREF(grads),
         _ptr(ws), need, _stream(y)))
+    return g
+
+
+# ---- rotary positions, products in 8-bit integers, group norm ------------------------------
+
+
+def _launch(name, ref, *args):
+    """Calls an entry point on the current stream of ref's device, with that device current."""
+    device = ref.get_device()
+    if device == torch._C._cuda_getDevice():
+        status = getattr(_lib.load(), name)(*args, _stream(ref))
+    else:
+        with torch.cuda.device(device):
+            status = getattr(_lib.load(), name)(*args, _stream(ref))
+    _lib.check(name, status)
+
+
+def _scratch(need, ref):
+    return torch.empty((need,), dtype=torch.uint8, device=ref.device) if need else None
+
+
+def _one_of(table, key, what):
+    try:
+        return table[key]
+    except KeyError:
+        raise ValueError(f"unknown {what} {key!r}; expected one of {sorted(table)}") from None
+
+
+def rotary_frequencies(pairs: int, axes: int, theta: float = 100.0):
+    """float32 [axes, pairs] for rotary(): the pairs dealt to the axes in turns, each axis' ones a geometric range
+    of angles a cell from 1 down to about 1 / theta."""
+    if pairs < 1 or not 1 <= axes <= 3 or not theta > 0:
+        raise ValueError("pairs from 1, axes from 1 to 3 and a theta above zero")
+    freq = torch.zeros((axes, pairs), dtype=torch.float64)
+    own = -(-pairs // axes)
+    for p in range(pairs):
+        freq[p % axes, p] = theta ** (-(p // axes) / own)
+    return freq.float()
+
+
+def _rotary_call(x, freq, pos, grid, layout, off):
+    """The mpm_rotary_call of these tensors, and the heads of x."""
+    if not x.is_cuda:
+        raise ValueError("rows of heads must be on the GPU")
+    dt, heads = _dt(x), _heads(x, "x", x)
+    rows, H, dh = _rows_of(x), x.shape[-2], x.shape[-1]
+    grid = tuple(int(n) for n in grid)
+    if not 1 <= len(grid) <= 3:
+        raise ValueError("grid has one to three axes")
+    if freq.dim() not in (2, 3) or freq.shape[-2] != len(grid) or (freq.dim() == 3 and freq.shape[0] != H):
+        raise ValueError(f"freq must be [{len(grid)}, pairs] or [{H}, {len(grid)}, pairs], got {tuple(freq.shape)}")
+    B = x.shape[0] if x.dim() == 4 else 1
+    if off is not None:
+        if x.dim() == 4:
+            raise ValueError("dense rows [B, N, H, dh] take no offsets")
+        B = off.numel() - 1
+    c = _lib.RotaryCall(rows, H, dh, dt, freq.shape[-1], _one_of(_LAYOUTS, layout, "layout"), len(grid),
+                        (ctypes.c_int32 * 3)(*grid, *[1] * (3 - len(grid))), int(freq.dim() == 3),
+                        _device(freq, "freq", torch.float32, x), _device(pos, "pos", torch.int32, x, rows), B,
+                        _device(off, "off", torch.int32, x, B + 1))
+    return c, heads
+
+
+def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=False, out=None):
+    """Rows of heads with every pair of channels turned by its row's place on a grid (mpm_rotary): the shape of x.
+
+    x: [R, H, dh] (packed, with the images' offsets ``off`` [B + 1]: rows of no image are left as they are in
+    ``out``; without, every row is turned) or [B, N, H, dh]; strided views as for attention(). ``freq``: float32
+    [axes, pairs], or [H, axes, pairs] for frequencies by head, radians a cell (rotary_frequencies); ``grid``: the cells
+    of the axes, (rows, columns) or (frames, rows, columns); ``pos``: int32 raster index of each row (None:
+    each row's index in its image; without ``off``, packed rows are one image). ``layout``: pair p is channels
+    p and p + pairs ("halves") or 2 p and 2 p + 1 ("pairs"); channels from 2 pairs on pass. ``inverse``: by the
+    negative angles. ``out``: where to write (x itself, say)."""
+    c, hx = _rotary_call(x, freq, pos, grid, layout, off)
+    if out is None:
+        out = x.new_empty(x.shape)
+    ho = _heads(out, "out", x, c.R, c.H)
+    if c.R:
+        _launch("mpm_rotary", x, _BYREF(c), _BYREF(hx), _BYREF(ho), int(bool(inverse)))
+    return out
+
+
+@dataclass
+class RotaryGrads:
+    dx: torch.Tensor
+    dfreq: torch.Tensor | None  # float32, as freq
+
+
+def rotary_backward(dout, x, freq, pos=None, grid=(1,), layout="halves", off=None, dx=None, with_dfreq=True) -> RotaryGrads:
+    """The gradients of rotary() (mpm_rotary_backward) from dout and the call's own inputs. ``dx``: where to write it
+    (dout itself, say); ``with_dfreq`` False leaves out the frequencies' gradient (x may be None then)."""
+    c, hd = _rotary_call(dout, freq, pos, grid, layout, off)
+    if dx is None:
+        dx = dout.new_empty(dout.shape)
+    hg = _heads(dx, "dx", dout, c.R, c.H)
+    hx, dfreq, ws, need = None, None, None, 0
+    if with_dfreq:
+        hx = _BYREF(_heads(x, "x", dout, c.R, c.H))
+        dfreq = torch.empty_like(freq)
+        if c.R == 0:
+            dfreq.zero_()
+        else:
+            need = _lib.load().mpm_rotary_backward_workspace_bytes(_BYREF(c))
+            ws = _scratch(need, dout)
+    if c.R:
+        _launch("mpm_rotary_backward", dout, _BYREF(c), _BYREF(hd), hx, _BYREF(hg), _ptr(dfreq), _ptr(ws), need)
+    return RotaryGrads(dx, dfreq)
+
+
+def _value_rows(x, what):
+    """(rows, K, stride of a row in elements) of values [R, K] with contiguous channels, 16 bytes apart at least."""
+    if not x.is_cuda or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError(f"{what} must be a device tensor [R, K] with contiguous channels")
+    return x.shape[0], x.shape[1], x.stride(0) if x.shape[0] > 1 else 0
+
+
+def quantize_rows(x):
+    """Rows of values [R, K] as 8-bit steps with a scale each (mpm_quantize_rows): int8 [R, K rounded up to a multiple
+    of 16] (zeros past K) and float32 [R]. Of a weight [out, in]: what linear_int8 takes as its weight."""
+    R, K, row = _value_rows(x, "x")
+    dt = _dt(x)
+    q = torch.empty((R, -(-K // 16) * 16), dtype=torch.int8, device=x.device)
+    scale = torch.empty((R,), dtype=torch.float32, device=x.device)
+    if R:
+        _launch("mpm_quantize_rows", x, _ptr(x), R, K, row, dt, _ptr(q), _ptr(scale))
+    return q, scale
+
+
+def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="none", dtype=None, out=None):
+    """act(x weight^T + bias) in 8-bit integers with a scale for each token and output channel (mpm_linear_int8): [R, N].
+
+    x: values [R, K] (float32 or bfloat16, row strides of whole 16 bytes), which are turned into steps on the way, or
+    with ``x_scale`` the steps of quantize_rows. ``weight``, ``weight_scale``: quantize_rows of a weight [N, K].
+    ``bias`` [N] and the result have ``dtype`` (that of x or of ``out``; bfloat16 for steps). ``activation``: "none", "relu",
+    "silu" or "gelu". ``out``: rows [R, N] with contiguous channels and a row stride of its own."""
+    R, K, row = _value_rows(x, "x")
+    if x_scale is None:
+        x_dt = _dt(x)
+    elif x.dtype is torch.int8 and (R <= 1 or row == K) and K % 16 == 0:
+        x_dt, row = _lib.MPM_I8, 0
+    else:
+        raise ValueError("steps must be contiguous int8 rows of a multiple of 16 channels")
+    if weight.dim() != 2 or weight.shape[1] != -(-K // 16) * 16:
+        raise ValueError(f"weight must be int8 [N, {-(-K // 16) * 16}], got {tuple(weight.shape)}")
+    N = weight.shape[0]
+    if out is None:
+        if dtype is None:
+            dtype = x.dtype if x_scale is None else torch.bfloat16
+        out = torch.empty((R, N), dtype=dtype, device=x.device)
+    elif out.shape != (R, N) or out.get_device() != x.get_device() or dtype not in (None, out.dtype) or (
+            out.stride(1) != 1 and N > 1) or (R > 1 and out.stride(0) < N):
+        raise ValueError(f"out must be [{R}, {N}] on {x.device} with contiguous channels")
+    c = _lib.Linear8Call(R, N, K, x_dt, _dt(out), _one_of(_ACTIVATIONS, activation, "activation"), row,
+                         out.stride(0) if R > 1 else N, _device(x_scale, "x_scale", torch.float32, x, R),
+                         _device(weight, "weight", torch.int8, x),
+                         _device(weight_scale, "weight_scale", torch.float32, x, N),
+                         _device(bias, "bias", out.dtype, x, N))
+    if R and N:
+        need = _lib.load().mpm_linear_int8_workspace_bytes(_BYREF(c))
+        ws = _scratch(need, x)
+        _launch("mpm_linear_int8", x, _BYREF(c), _ptr(x), _ptr(out), _ptr(ws), need)
+    return out
+
+
+def _group_call(x, groups, weight, bias, off, activation, eps):
+    """The mpm_group_norm_call of these tensors."""
+    if not x.is_cuda or not x.is_contiguous() or x.dim() < 2:
+        raise ValueError("x must be a contiguous device tensor [R, C] with offsets, or [B, ..., C]")
+    C = x.shape[-1]
+    if x.dim() == 2:
+        if off is None:
+            raise ValueError("packed rows [R, C] need their offsets")
+        B = off.numel() - 1
+    elif off is not None:
+        raise ValueError("dense images [B, ..., C] take no offsets")
+    else:
+        B = x.shape[0]
+    R = math.prod(x.shape[:-1])
+    return _lib.GroupNormCall(R, C, int(groups), _dt(x), _one_of(_ACTIVATIONS, activation, "activation"), eps, B,
+                              _device(off, "off", torch.int32, x, B + 1), _device(weight, "weight", x.dtype, x, C),
+                              _device(bias, "bias", x.dtype, x, C))
+
+
+def group_norm(x, groups, weight=None, bias=None, off=None, activation="none", eps=1e-5, with_stats=False, out=None):
+    """act(group_norm(x) * weight + bias) over each image's rows and each group of channels, channels last
+    (mpm_group_norm): the shape of x, and with ``with_stats`` float32 [B, groups, 2] for group_norm_backward.
+
+    x: dense images [B, ..., C] (a rebuilt grid [B, N, C] or [B, rows, columns, C]) or packed rows [R, C] by ``off``
+    [B + 1] (rows of no image are left as they are in ``out``). ``activation``: "none", "relu", "silu" or "gelu".
+    ``out``: where to write (x itself, say)."""
+    c = _group_call(x, groups, weight, bias, off, activation, eps)
+    y = torch.empty_like(x) if out is None else out
+    if y.shape != x.shape:
+        raise ValueError(f"out must be {tuple(x.shape)}")
+    yp = _device(y, "out", x.dtype, x)
+    stats = torch.empty((c.B, c.groups, 2), dtype=torch.float32, device=x.device) if with_stats else None
+    if c.R == 0:
+        if with_stats:
+            stats.zero_()
+        return (y, stats) if with_stats else y
+    need = _lib.load().mpm_group_norm_workspace_bytes(_BYREF(c))
+    ws = _scratch(need, x)
+    _launch("mpm_group_norm", x, _BYREF(c), _ptr(x), yp, _ptr(stats), _ptr(ws), need)
+    return (y, stats) if with_stats else y
+
+
+@dataclass
+class GroupNormGrads:
+    dx: torch.Tensor
+    dweight: torch.Tensor | None
+    dbias: torch.Tensor | None
+
+
+def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, off=None, activation="none", eps=1e-5,
+                        dx=None) -> GroupNormGrads:
+    """The gradients of group_norm() (mpm_group_norm_backward) from dy, the call's own inputs and its stats; zeros in rows
+    of no image. ``dx``: where to write it (dy itself, say)."""
+    c = _group_call(x, groups, weight, bias, off, activation, eps)
+    g = GroupNormGrads(torch.empty_like(x) if dx is None else dx,
+                       *(None if t is None else torch.empty_like(t) for t in (weight, bias)))
+    if dy.shape != x.shape or g.dx.shape != x.shape:
+        raise ValueError(f"dy and dx must be {tuple(x.shape)}")
+    dp, gp = _device(dy, "dy", x.dtype, x), _device(g.dx, "dx", x.dtype, x)
+    sp = _device(stats, "stats", torch.float32, x, 2 * c.B * c.groups)
+    if c.R == 0:
+        for t in (g.dweight, g.dbias):
+            if t is not None:
+                t.zero_()
+        return g
+    need = _lib.load().mpm_group_norm_backward_workspace_bytes(_BYREF(c))
+    ws = _scratch(need, x)
+    _launch("mpm_group_norm_backward", x, _BYREF(c), dp, _ptr(x), sp, gp, _ptr(g.dweight), _ptr(g.dbias), _ptr(ws), need)
     return g

@@ -1,0 +1,517 @@
+// Group norm with an activation over images of rows of C channels, channels last:
+//   t = (x - mean) rstd over an image's rows and a group's channels,  z = t w + b,  y = act(z),
+// and its gradients, with gz = dy act'(z) and gt = gz w:
+//   dx = rstd (gt - mean(gt) - t mean(gt t)),  dw = sum gz t,  db = sum gz.
+// A thread keeps one vector of 16 bytes of the channels and walks rows, so that sums are kept by channel
+// and groups of any width are sums over channels afterwards.
+#include <algorithm>
+#include <type_traits>
+
+#include "mpm_act.h"
+#include "mpm_device.h"
+#include "mpm_launch.h"
+
+namespace mpm {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kAhead = 4;      // rows a thread loads before it uses them
+constexpr int kGroups = 2048;  // workgroups of a pass, about
+
+template <class S>
+struct Vec {
+    static constexpr int kPer = 16 / S::kBytes;
+    u32x4 w;
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (S::kBytes == 2) return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+        return __uint_as_float(w[e]);
+    }
+    __device__ static __forceinline__ u32x4 pack(const float (&v)[kPer])
+    {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        u32x4 r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (S::kBytes == 2) {
+                const f32x2 p = {v[2 * e], v[2 * e + 1]};
+                r[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+            } else {
+                r[e] = __float_as_uint(v[e]);
+            }
+        }
+        return r;
+    }
+};
+
+// How rows and channels are dealt to workgroups: blocks of `cols` vectors of channels, `ways` rows at a time, `chunks`
+// parts of an image's rows.
+struct Deal {
+    int vecs;          // vectors a row
+    int cols, ways;    // of a workgroup
+    int blocks;        // column blocks (the grid's y)
+    int chunks;
+};
+
+struct Rows {
+    long first, end;
+    int image;
+};
+__device__ __forceinline__ Rows image_rows(const GroupNormCall& a, int b)
+{
+    const long lo = a.off ? a.off[b] : (long)b * a.N, hi = a.off ? a.off[b + 1] : lo + a.N;
+    const long first = min(max(lo, 0L), (long)a.R);
+    return Rows{first, min(max(hi, first), (long)a.R), b};
+}
+// The rows of work item i of images x chunks.
+__device__ __forceinline__ Rows item_rows(const GroupNormCall& a, const Deal& d, long i)
+{
+    const Rows r = image_rows(a, (int)(i / d.chunks));
+    const long c = i % d.chunks, n = r.end - r.first;
+    return Rows{r.first + n * c / d.chunks, r.first + n * (c + 1) / d.chunks, r.image};
+}
+
+// This thread's vector of channels and its first row's offset (way), if it has any.
+struct Place {
+    int col, way;
+    bool live;
+};
+__device__ __forceinline__ Place place(const Deal& d)
+{
+    Place p;
+    p.way = threadIdx.x / d.cols;
+    p.col = blockIdx.y * d.cols + threadIdx.x % d.cols;
+    p.live = p.way < d.ways && p.col < d.vecs;
+    return p;
+}
+
+// Count, mean and sum of squared deviations of two sets as one (Chan, Golub and LeVeque's update).
+struct Moments {
+    float n, mean, m2;
+};
+__device__ __forceinline__ Moments joined(const Moments& a, const Moments& b)
+{
+    const float n = a.n + b.n;
+    if (n == 0.0f) return a;
+    const float part = b.n / n, d = b.mean - a.mean;
+    return Moments{n, fmaf(d, part, a.mean), a.m2 + b.m2 + d * d * a.n * part};
+}
+
+// Mean and squared deviations of every channel over an item's rows: parts[item][C] pairs. Values are taken from their
+// channel's in the image's first row, so that a mean far from zero beside the deviations costs no digits.
+template <class S>
+__global__ __launch_bounds__(kThreads) void channel_moments_kernel(GroupNormCall a, Deal d, const uint8_t* x,
+                                                                   float2* __restrict__ parts)
+{
+    typedef Vec<S> V;
+    __shared__ float lds[3][kThreads];
+    const Rows it = item_rows(a, d, blockIdx.x);
+    const Place p = place(d);
+    const long stride = (long)a.C * S::kBytes;
+    Moments m[V::kPer];
+#pragma unroll
+    for (int e = 0; e < V::kPer; ++e) m[e] = Moments{0.0f, 0.0f, 0.0f};
+    if (p.live && it.first < it.end) {
+        V zero;
+        zero.w = load16(x + image_rows(a, it.image).first * stride + p.col * 16);
+        for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
+            V v[kAhead];
+            int n = 0;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const long r = row + u * d.ways;
+                if (r < it.end) {
+                    v[u].w = load16(x + r * stride + p.col * 16);
+                    ++n;
+                }
+            }
+            const float inv = 1.0f / (float)n;
+#pragma unroll
+            for (int e = 0; e < V::kPer; ++e) {
+                Moments q{(float)n, 0.0f, 0.0f};
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) q.mean += u < n ? v[u].get(e) - zero.get(e) : 0.0f;
+                q.mean *= inv;
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const float t = u < n ? v[u].get(e) - zero.get(e) - q.mean : 0.0f;
+                    q.m2 = fmaf(t, t, q.m2);
+                }
+                m[e] = joined(m[e], q);
+            }
+        }
+    }
+    for (int e = 0; e < V::kPer; ++e) {
+        __syncthreads();
+        lds[0][threadIdx.x] = m[e].n;
+        lds[1][threadIdx.x] = m[e].mean;
+        lds[2][threadIdx.x] = m[e].m2;
+        __syncthreads();
+        if (p.live && p.way == 0) {
+            Moments q = m[e];
+            for (int w = 1; w < d.ways; ++w) {
+                const int t = w * d.cols + threadIdx.x;
+                q = joined(q, Moments{lds[0][t], lds[1][t], lds[2][t]});
+            }
+            parts[(long)blockIdx.x * a.C + p.col * V::kPer + e] = make_float2(q.mean, q.m2);
+        }
+    }
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+__device__ __forceinline__ float parameter(const void* p, int dt, long i)
+{
+    if (dt == kBf16) return __uint_as_float((uint32_t)static_cast<const uint16_t*>(p)[i] << 16);
+    return static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store_parameter(void* p, int dt, long i, float v)
+{
+    if (dt == kBf16) static_cast<uint16_t*>(p)[i] = (uint16_t)f32_to_bf16_rne(v);
+    else static_cast<float*>(p)[i] = v;
+}
+
+// Mean and reciprocal deviation of every image and group, a wave each, from the channels' parts, in 64 bits.
+__global__ __launch_bounds__(kWave) void group_stats_kernel(GroupNormCall a, Deal d, const void* x,
+                                                            const float2* __restrict__ parts,
+                                                            float2* __restrict__ stats)
+{
+    const int width = a.C / a.groups, many = d.chunks * width;
+    for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
+        const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
+        const Rows image = image_rows(a, b);
+        const double count = (double)(image.end - image.first) * width;
+        // A part's count and mean; its deviations are left to the caller.
+        auto part = [&](int i, double* n, double* mean) {
+            const long item = (long)b * d.chunks + i / width;
+            const int c = g * width + i % width;
+            const Rows r = item_rows(a, d, item);
+            *n = (double)(r.end - r.first);
+            const float2 q = parts[item * a.C + c];
+            *mean = (double)q.x + (double)parameter(x, a.dt, image.first * a.C + c);
+            return (double)q.y;
+        };
+        double sum = 0.0, m2 = 0.0, n, mean;
+        if (count > 0.0) {
+            for (int i = threadIdx.x; i < many; i += kWave) {
+                part(i, &n, &mean);
+                if (n > 0.0) sum += n * mean;
+            }
+        }
+        const double centre = count > 0.0 ? wave_sum(sum) / count : 0.0;
+        if (count > 0.0) {
+            for (int i = threadIdx.x; i < many; i += kWave) {
+                const double q = part(i, &n, &mean);
+                if (n > 0.0) m2 += q + n * (mean - centre) * (mean - centre);
+            }
+            m2 = wave_sum(m2);
+        }
+        if (threadIdx.x == 0)
+            stats[pair] = count > 0.0 ? make_float2((float)centre, (float)(1.0 / sqrt(m2 / count + (double)a.eps)))
+                                      : make_float2(0.0f, 0.0f);
+    }
+}
+
+// A vector's parameters: mean, rstd, weight and shift of each of its channels.
+template <class S>
+struct Affine {
+    static constexpr int kPer = Vec<S>::kPer;
+    float mean[kPer], rstd[kPer], w[kPer], b[kPer];
+
+    __device__ __forceinline__ void load(const GroupNormCall& a, const float2* stats, int image, int col)
+    {
+        Vec<S> wv, bv;
+        if (a.w) wv.w = load16(static_cast<const uint8_t*>(a.w) + col * 16);
+        if (a.b) bv.w = load16(static_cast<const uint8_t*>(a.b) + col * 16);
+        const int width = a.C / a.groups;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const float2 s = stats[(long)image * a.groups + (col * kPer + e) / width];
+            mean[e] = s.x;
+            rstd[e] = s.y;
+            w[e] = a.w ? wv.get(e) : 1.0f;
+            b[e] = a.b ? bv.get(e) : 0.0f;
+        }
+    }
+};
+
+template <class S, int ACT>
+__global__ __launch_bounds__(kThreads) void apply_kernel(GroupNormCall a, Deal d, const uint8_t* x, uint8_t* y,
+                                                         const float2* __restrict__ stats)
+{
+    typedef Vec<S> V;
+    const Rows it = item_rows(a, d, blockIdx.x);
+    const Place p = place(d);
+    if (!p.live || it.first >= it.end) return;
+    const long stride = (long)a.C * S::kBytes;
+    Affine<S> f;
+    f.load(a, stats, it.image, p.col);
+    for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
+        V v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (row + u * d.ways < it.end) v[u].w = load16(x + (row + u * d.ways) * stride + p.col * 16);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const long r = row + u * d.ways;
+            if (r >= it.end) break;
+            float o[V::kPer];
+#pragma unroll
+            for (int e = 0; e < V::kPer; ++e)
+                o[e] = activate<ACT, S::kBytes == 4>(fmaf((v[u].get(e) - f.mean[e]) * f.rstd[e], f.w[e], f.b[e]));
+            store16(y + r * stride + p.col * 16, V::pack(o));
+        }
+    }
+}
+
+// The sums of gz and gz t of every channel over an item's rows: parts[item][C] pairs.
+template <class S, int ACT>
+__global__ __launch_bounds__(kThreads) void channel_sums_kernel(GroupNormCall a, Deal d, const uint8_t* dy,
+                                                                const uint8_t* x, const float2* __restrict__ stats,
+                                                                float2* __restrict__ parts)
+{
+    typedef Vec<S> V;
+    __shared__ float2 lds[kThreads];
+    const Rows it = item_rows(a, d, blockIdx.x);
+    const Place p = place(d);
+    const long stride = (long)a.C * S::kBytes;
+    float s0[V::kPer], s1[V::kPer];
+#pragma unroll
+    for (int e = 0; e < V::kPer; ++e) s0[e] = s1[e] = 0.0f;
+    if (p.live && it.first < it.end) {
+        Affine<S> f;
+        f.load(a, stats, it.image, p.col);
+        for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
+            V v[kAhead], g[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const long r = row + u * d.ways;
+                if (r < it.end) {
+                    v[u].w = load16(x + r * stride + p.col * 16);
+                    g[u].w = load16(dy + r * stride + p.col * 16);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (row + u * d.ways >= it.end) break;
+#pragma unroll
+                for (int e = 0; e < V::kPer; ++e) {
+                    const float t = (v[u].get(e) - f.mean[e]) * f.rstd[e];
+                    const float gz = g[u].get(e) * activation_slope<ACT, S::kBytes == 4>(fmaf(t, f.w[e], f.b[e]));
+                    s0[e] += gz;
+                    s1[e] = fmaf(gz, t, s1[e]);
+                }
+            }
+        }
+    }
+    for (int e = 0; e < V::kPer; ++e) {
+        __syncthreads();
+        lds[threadIdx.x] = make_float2(s0[e], s1[e]);
+        __syncthreads();
+        if (p.live && p.way == 0) {
+            float2 q = lds[threadIdx.x];
+            for (int w = 1; w < d.ways; ++w) {
+                q.x += lds[w * d.cols + threadIdx.x].x;
+                q.y += lds[w * d.cols + threadIdx.x].y;
+            }
+            parts[(long)blockIdx.x * a.C + p.col * V::kPer + e] = q;
+        }
+    }
+}
+
+// From the channels' sums: the means of gt and gt t of every image and group, a wave each ...
+__global__ __launch_bounds__(kWave) void group_means_kernel(GroupNormCall a, Deal d, const float2* __restrict__ parts,
+                                                            float2* __restrict__ means)
+{
+    const int width = a.C / a.groups;
+    for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
+        const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
+        double s0 = 0.0, s1 = 0.0;
+        for (int i = threadIdx.x; i < d.chunks * width; i += kWave) {
+            const int c = g * width + i % width;
+            const float2 q = parts[((long)b * d.chunks + i / width) * a.C + c];
+            const double w = a.w ? (double)parameter(a.w, a.dt, c) : 1.0;
+            s0 += w * (double)q.x;
+            s1 += w * (double)q.y;
+        }
+        s0 = wave_sum(s0);
+        s1 = wave_sum(s1);
+        const Rows r = image_rows(a, b);
+        const double n = (double)(r.end - r.first) * width;
+        if (threadIdx.x == 0)
+            means[pair] = n > 0.0 ? make_float2((float)(s0 / n), (float)(s1 / n)) : make_float2(0.0f, 0.0f);
+    }
+}
+
+// ... and dw and db, 64 channels a workgroup, sixteen waves' shares of the items joined in order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(kJoinWaves* kWave) void join_sums_kernel(const float2* __restrict__ parts, long items, int C,
+                                                                      int dt, void* dw, void* db)
+{
+    __shared__ double lds[2][kJoinWaves][kWave];
+    const int lane = threadIdx.x % kWave, way = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+    double s0 = 0.0, s1 = 0.0;
+    if (c < C) {
+#pragma unroll 4
+        for (long i = way; i < items; i += kJoinWaves) {
+            const float2 q = parts[i * C + c];
+            s0 += (double)q.x;
+            s1 += (double)q.y;
+        }
+    }
+    lds[0][way][lane] = s0;
+    lds[1][way][lane] = s1;
+    __syncthreads();
+    if (way != 0 || c >= C) return;
+    for (int w = 1; w < kJoinWaves; ++w) {
+        s0 += lds[0][w][lane];
+        s1 += lds[1][w][lane];
+    }
+    if (db) store_parameter(db, dt, c, (float)s0);
+    if (dw) store_parameter(dw, dt, c, (float)s1);
+}
+
+template <class S, int ACT>
+__global__ __launch_bounds__(kThreads) void input_gradient_kernel(GroupNormCall a, Deal d, const uint8_t* dy,
+                                                                  const uint8_t* x, uint8_t* dx,
+                                                                  const float2* __restrict__ stats,
+                                                                  const float2* __restrict__ means)
+{
+    typedef Vec<S> V;
+    const Place p = place(d);
+    if (!p.live) return;
+    const long stride = (long)a.C * S::kBytes;
+    if (a.off) {  // a share of the rows of no image
+        const u32x4 none = {0, 0, 0, 0};
+        const long lo = min(max((long)a.off[0], 0L), (long)a.R), hi = min(max((long)a.off[a.B], lo), (long)a.R);
+        const long many = lo + a.R - hi, first = many * blockIdx.x / gridDim.x, end = many * (blockIdx.x + 1L) / gridDim.x;
+        for (long r = first + p.way; r < end; r += d.ways)
+            store16(dx + (r < lo ? r : r - lo + hi) * stride + p.col * 16, none);
+    }
+    const Rows it = item_rows(a, d, blockIdx.x);
+    if (it.first >= it.end) return;
+    Affine<S> f;
+    f.load(a, stats, it.image, p.col);
+    float m0[V::kPer], m1[V::kPer];
+#pragma unroll
+    for (int e = 0; e < V::kPer; ++e) {
+        const float2 m = means[(long)it.image * a.groups + (p.col * V::kPer + e) / (a.C / a.groups)];
+        m0[e] = m.x;
+        m1[e] = m.y;
+    }
+    for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
+        V v[kAhead], g[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const long r = row + u * d.ways;
+            if (r < it.end) {
+                v[u].w = load16(x + r * stride + p.col * 16);
+                g[u].w = load16(dy + r * stride + p.col * 16);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const long r = row + u * d.ways;
+            if (r >= it.end) break;
+            float o[V::kPer];
+#pragma unroll
+            for (int e = 0; e < V::kPer; ++e) {
+                const float t = (v[u].get(e) - f.mean[e]) * f.rstd[e];
+                const float gz = g[u].get(e) * activation_slope<ACT, S::kBytes == 4>(fmaf(t, f.w[e], f.b[e]));
+                o[e] = f.rstd[e] * (fmaf(gz, f.w[e], -m0[e]) - t * m1[e]);
+            }
+            store16(dx + r * stride + p.col * 16, V::pack(o));
+        }
+    }
+}
+
+Deal deal(const GroupNormCall& a)
+{
+    Deal d;
+    d.vecs = a.C / (a.dt == kBf16 ? 8 : 4);
+    // Few enough vectors for two rows at a time; blocks of about the same width.
+    d.blocks = (d.vecs + kThreads - 1) / kThreads;
+    d.cols = (d.vecs + d.blocks - 1) / d.blocks;
+    d.ways = kThreads / d.cols;
+    const long per = std::max(1L, ((long)a.R + a.B - 1) / a.B);
+    const long most = std::max(1L, (per + d.ways * kAhead - 1) / (d.ways * kAhead));
+    d.chunks = (int)std::max(1L, std::min(most, ((long)kGroups / d.blocks + a.B - 1) / a.B));
+    return d;
+}
+
+// Workgroups of a wave for the images' groups (which may be more than a grid has).
+unsigned pair_groups(const GroupNormCall& a) { return (unsigned)std::min((long)a.B * a.groups, 1L << 20); }
+
+size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
+size_t parts_bytes(const GroupNormCall& a, const Deal& d) { return aligned256((size_t)a.B * d.chunks * a.C * 8); }
+size_t stats_bytes(const GroupNormCall& a) { return aligned256((size_t)a.B * a.groups * 8); }
+
+// Calls go(type, activation).
+template <class F>
+hipError_t with_kind(const GroupNormCall& a, F&& go)
+{
+    auto act = [&](auto type) {
+        switch (a.act) {
+        case kActRelu: return go(type, std::integral_constant<int, kActRelu>{});
+        case kActSilu: return go(type, std::integral_constant<int, kActSilu>{});
+        case kActGelu: return go(type, std::integral_constant<int, kActGelu>{});
+        default: return go(type, std::integral_constant<int, kActNone>{});
+        }
+    };
+    return a.dt == kBf16 ? act(Bf16{}) : act(F32{});
+}
+
+}  // namespace
+
+size_t group_norm_bytes(const GroupNormCall& a) { return parts_bytes(a, deal(a)) + stats_bytes(a); }
+
+hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t st)
+{
+    const Deal d = deal(a);
+    float2* parts = static_cast<float2*>(ws);
+    float2* sp = stats ? reinterpret_cast<float2*>(stats)
+                       : reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
+    const dim3 grid((unsigned)((long)a.B * d.chunks), (unsigned)d.blocks);
+    const uint8_t* xp = static_cast<const uint8_t*>(x);
+    return with_kind(a, [&](auto type, auto act) {
+        typedef decltype(type) S;
+        hipLaunchKernelGGL((channel_moments_kernel<S>), grid, dim3(kThreads), 0, st, a, d, xp, parts);
+        hipLaunchKernelGGL(group_stats_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, x, parts, sp);
+        hipLaunchKernelGGL((apply_kernel<S, decltype(act)::value>), grid, dim3(kThreads), 0, st, a, d, xp,
+                           static_cast<uint8_t*>(y), sp);
+        return hipGetLastError();
+    });
+}
+
+size_t group_norm_backward_bytes(const GroupNormCall& a) { return parts_bytes(a, deal(a)) + stats_bytes(a); }
+
+hipError_t launch_group_norm_backward(const GroupNormCall& a, const void* dy, const void* x, const float* stats, void* dx,
+                                      void* dw, void* db, void* ws, hipStream_t st)
+{
+    const Deal d = deal(a);
+    float2* parts = static_cast<float2*>(ws);
+    float2* means = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
+    const float2* sp = reinterpret_cast<const float2*>(stats);
+    const uint8_t *xp = static_cast<const uint8_t*>(x), *gp = static_cast<const uint8_t*>(dy);
+    const long items = (long)a.B * d.chunks;
+    return with_kind(a, [&](auto type, auto act) {
+        typedef decltype(type) S;
+        constexpr int ACT = decltype(act)::value;
+        hipLaunchKernelGGL((channel_sums_kernel<S, ACT>), dim3((unsigned)items, (unsigned)d.blocks), dim3(kThreads), 0, st,
+                           a, d, gp, xp, sp, parts);
+        hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, means);
+        if (dw || db)
+            hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinWaves * kWave), 0,
+                               st, parts, items, a.C, a.dt, dw, db);
+        hipLaunchKernelGGL((input_gradient_kernel<S, ACT>), dim3((unsigned)items, (unsigned)d.blocks),
+                           dim3(kThreads), 0, st, a, d, gp, xp, static_cast<uint8_t*>(dx), sp, means);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace mpm

@@ -1,0 +1,52 @@
+// Activations and their slopes, float32, shared by the kernels that end in one.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "mpm_launch.h"
+
+namespace mpm {
+
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+// The normal distribution's integral up to z, half of erfc(-z / sqrt 2). PRECISE: the library's erfc. Otherwise
+// formula 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions for erfc (absolute error
+// below 1.5e-7), a reciprocal, an exponential and six multiply-adds: for results rounded to bfloat16.
+template <bool PRECISE>
+__device__ __forceinline__ float normal_integral(float z)
+{
+    if constexpr (PRECISE) return 0.5f * erfcf(z * -0.70710678118654752f);
+    const float u = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, u, 1.0f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * p * t * __expf(-u * u);
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
+// (max() would drop a NaN)
+template <int ACT, bool PRECISE>
+__device__ __forceinline__ float activate(float z)
+{
+    if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == kActSilu) return z * sigmoid(z);
+    if constexpr (ACT == kActGelu) return z * normal_integral<PRECISE>(z);
+    return z;
+}
+
+template <int ACT, bool PRECISE>
+__device__ __forceinline__ float activation_slope(float z)
+{
+    if constexpr (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+    if constexpr (ACT == kActSilu) {
+        const float s = sigmoid(z);
+        return s * fmaf(z, 1.0f - s, 1.0f);
+    }
+    if constexpr (ACT == kActGelu)
+        return fmaf(z * 0.39894228040143268f, __expf(-0.5f * z * z), normal_integral<PRECISE>(z));
+    return 1.0f;
+}
+
+}  // namespace mpm

@@ -428,6 +428,96 @@ int checked_norm(const mpm::NormCall& a, hipStream_t st)
     return run_checks(st, [&](int32_t* v) { return mpm::launch_check_offsets(a.off, a.B, a.R, 0, a.R, nullptr, v, st); });
 }
 
+// ---- rotary positions, 8-bit products, group norm: argument checks --------------------
+
+bool ok_dtype(int32_t dt) { return dt == MPM_F32 || dt == MPM_BF16; }
+int32_t per16(int32_t dt) { return dt == MPM_BF16 ? 8 : 4; }  // values in 16 bytes
+
+// B images of R rows, packed or of equal numbers.
+int check_images(int32_t R, int32_t B, const int32_t* off)
+{
+    if (R < 1 || B < 1 || !ok_opt_int_ptr(off) || (!off && R % B != 0)) return MPM_ERR_INVALID_ARG;
+    return B > MPM_MAX_B ? MPM_ERR_UNSUPPORTED : MPM_OK;
+}
+
+// Checked mode: packed images within R rows.
+int checked_images(const int32_t* off, int B, int R, hipStream_t st)
+{
+    if (!off) return MPM_OK;
+    std::lock_guard<std::mutex> lock(g_check_mutex);
+    return run_checks(st, [&](int32_t* v) { return mpm::launch_check_offsets(off, B, R, 0, R, nullptr, v, st); });
+}
+
+int check_rotary(const mpm_rotary_call* c)
+{
+    if (c == nullptr || c->H < 1 || c->dh < 1 || c->pairs < 1 || !ok_dtype(c->dt)) return MPM_ERR_INVALID_ARG;
+    if (c->layout != MPM_ROTARY_HALVES && c->layout != MPM_ROTARY_PAIRS) return MPM_ERR_INVALID_ARG;
+    if (c->dh % per16(c->dt) != 0 || c->pairs > c->dh / 2 || c->axes < 1 || c->axes > MPM_MAX_AXES)
+        return MPM_ERR_INVALID_ARG;
+    int64_t cells = 1;
+    for (int a = 0; a < c->axes; ++a) {
+        if (c->grid[a] < 1 || (cells *= c->grid[a]) > INT32_MAX) return MPM_ERR_INVALID_ARG;
+    }
+    if (!ok_int_ptr(c->freq) || !ok_opt_int_ptr(c->pos)) return MPM_ERR_INVALID_ARG;
+    const int s = check_images(c->R, c->B, c->off);
+    if (s != MPM_OK) return s;
+    return c->H > MPM_MAX_HEADS || c->dh > MPM_MAX_HEAD_DIM ? MPM_ERR_UNSUPPORTED : MPM_OK;
+}
+
+mpm::RotaryCall rotary_call(const mpm_rotary_call* c)
+{
+    mpm::RotaryCall a{c->R, c->H, c->dh, c->dt, c->pairs, c->layout == MPM_ROTARY_HALVES, c->axes, {1, 1, 1},
+                      c->freq_per_head != 0, c->freq, c->pos, c->B, c->R / c->B, c->off};
+    for (int i = 0; i < c->axes; ++i) a.grid[i] = c->grid[i];
+    return a;
+}
+
+// Rows of K values for 8-bit steps.
+int check_step_rows(const void* x, int32_t K, int64_t x_row, int32_t dt)
+{
+    if (K < 1 || !ok_dtype(dt) || K % per16(dt) != 0 || !ok_rows_ptr(x)) return MPM_ERR_INVALID_ARG;
+    if (x_row < 0 || x_row % per16(dt) != 0) return MPM_ERR_INVALID_ARG;
+    return K > MPM_MAX_K8 ? MPM_ERR_UNSUPPORTED : MPM_OK;
+}
+
+int check_linear8(const mpm_linear8_call* c)
+{
+    if (c == nullptr || c->M < 1 || c->N < 1 || c->K < 1 || !ok_dtype(c->dt)) return MPM_ERR_INVALID_ARG;
+    if (c->act < MPM_ACT_NONE || c->act > MPM_ACT_GELU || c->out_row < c->N) return MPM_ERR_INVALID_ARG;
+    if (c->x_dt == MPM_I8) {
+        if (!ok_int_ptr(c->x_scale)) return MPM_ERR_INVALID_ARG;
+    } else if (!ok_dtype(c->x_dt) || c->K % per16(c->x_dt) != 0 || c->x_row < 0 || c->x_row % per16(c->x_dt) != 0 ||
+               c->x_scale != nullptr) {
+        return MPM_ERR_INVALID_ARG;
+    }
+    if (!ok_rows_ptr(c->w) || !ok_int_ptr(c->w_scale) || !aligned(c->bias, c->dt == MPM_BF16 ? 2 : 4))
+        return MPM_ERR_INVALID_ARG;
+    return c->K > MPM_MAX_K8 || c->N > MPM_MAX_N8 ? MPM_ERR_UNSUPPORTED : MPM_OK;
+}
+
+mpm::Linear8Call linear8_call(const mpm_linear8_call* c)
+{
+    return mpm::Linear8Call{c->M, c->N, c->K, c->x_dt, c->dt, c->act, (long)c->x_row, (long)c->out_row, c->x_scale,
+                            c->w, c->w_scale, c->bias};
+}
+
+int check_group_norm(const mpm_group_norm_call* c)
+{
+    if (c == nullptr || c->C < 1 || c->groups < 1 || !ok_dtype(c->dt)) return MPM_ERR_INVALID_ARG;
+    if (c->act < MPM_ACT_NONE || c->act > MPM_ACT_GELU || c->C % per16(c->dt) != 0 || c->C % c->groups != 0)
+        return MPM_ERR_INVALID_ARG;
+    if (!finite(c->eps) || c->eps < 0.0f || (c->b && !c->w) || !ok_opt_rows_ptr(c->w) || !ok_opt_rows_ptr(c->b))
+        return MPM_ERR_INVALID_ARG;
+    const int s = check_images(c->R, c->B, c->off);
+    if (s != MPM_OK) return s;
+    return c->C > MPM_MAX_D ? MPM_ERR_UNSUPPORTED : MPM_OK;
+}
+
+mpm::GroupNormCall group_norm_call(const mpm_group_norm_call* c)
+{
+    return mpm::GroupNormCall{c->R, c->C, c->groups, c->dt, c->act, c->eps, c->B, c->R / c->B, c->off, c->w, c->b};
+}
+
 }  // namespace
 
 namespace mpm {
@@ -922,6 +1012,111 @@ int mpm_residual_norm_backward(const mpm_norm_call* call, const void* dy, const 
                                                 mpm::NormGrads{grads->dx, grads->df, grads->dw, grads->db, grads->dpost_w,
                                                                grads->dpost_b, grads->dscale, grads->dgate},
                                                 ws, as_stream(stream)));
+}
+
+int mpm_rotary(const mpm_rotary_call* call, const mpm_heads* x, const mpm_heads* out, int32_t inverse, void* stream)
+{
+    const int s = check_rotary(call);
+    if (s != MPM_OK) return s;
+    if (!ok_heads(x, call->dt) || !ok_heads(out, call->dt)) return MPM_ERR_INVALID_ARG;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_images(call->off, call->B, call->R, as_stream(stream)));
+    return hip_status(mpm::launch_rotary(rotary_call(call), heads(x), heads(out), inverse != 0, as_stream(stream)));
+}
+
+size_t mpm_rotary_backward_workspace_bytes(const mpm_rotary_call* call)
+{
+    return check_rotary(call) == MPM_OK ? mpm::rotary_backward_bytes(rotary_call(call)) : 0;
+}
+
+int mpm_rotary_backward(const mpm_rotary_call* call, const mpm_heads* dout, const mpm_heads* x, const mpm_heads* dx,
+                        float* dfreq, void* ws, size_t ws_bytes, void* stream)
+{
+    int s = check_rotary(call);
+    if (s != MPM_OK) return s;
+    if (!ok_heads(dout, call->dt) || !ok_heads(dx, call->dt) || (x != nullptr) != (dfreq != nullptr) ||
+        (x && !ok_heads(x, call->dt)) || !aligned(dfreq, 4))
+        return MPM_ERR_INVALID_ARG;
+    const mpm::RotaryCall a = rotary_call(call);
+    if ((s = check_workspace(ws, ws_bytes, dfreq ? mpm::rotary_backward_bytes(a) : 0)) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_images(call->off, call->B, call->R, as_stream(stream)));
+    return hip_status(mpm::launch_rotary_backward(a, heads(dout), x ? heads(x) : mpm::HeadRows{nullptr, 0, 0}, heads(dx),
+                                                  dfreq, ws, as_stream(stream)));
+}
+
+int mpm_quantize_rows(const void* x, int32_t R, int32_t K, int64_t x_row, int32_t dt, int8_t* q, float* scale,
+                      void* stream)
+{
+    const int s = check_step_rows(x, K, x_row, dt);
+    if (s != MPM_OK) return s;
+    if (R < 1 || !ok_rows_ptr(q) || !ok_int_ptr(scale)) return MPM_ERR_INVALID_ARG;
+    MPM_LAUNCH_GATE();
+    return hip_status(mpm::launch_quantize(x, R, K, (long)x_row, dt, q, scale, as_stream(stream)));
+}
+
+size_t mpm_linear_int8_workspace_bytes(const mpm_linear8_call* call)
+{
+    if (check_linear8(call) != MPM_OK || call->x_dt == MPM_I8 || mpm::linear8_is_few(linear8_call(call))) return 0;
+    return round_up((size_t)call->M * mpm::steps_row(call->K)) + round_up((size_t)call->M * sizeof(float));
+}
+
+int mpm_linear_int8(const mpm_linear8_call* call, const void* x, void* out, void* ws, size_t ws_bytes, void* stream)
+{
+    int s = check_linear8(call);
+    if (s != MPM_OK) return s;
+    if (!ok_rows_ptr(x) || out == nullptr || !aligned(out, call->dt == MPM_BF16 ? 2 : 4)) return MPM_ERR_INVALID_ARG;
+    if ((s = check_workspace(ws, ws_bytes, mpm_linear_int8_workspace_bytes(call))) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    const mpm::Linear8Call a = linear8_call(call);
+    const hipStream_t st = as_stream(stream);
+    if (mpm::linear8_is_few(a)) return hip_status(mpm::launch_linear8_few(a, x, out, st));
+    if (a.x_dt == MPM_I8)
+        return hip_status(mpm::launch_linear8(a, static_cast<const int8_t*>(x), a.x_scale, out, st));
+    int8_t* q = static_cast<int8_t*>(ws);
+    float* scale = reinterpret_cast<float*>(q + round_up((size_t)a.M * mpm::steps_row(a.K)));
+    hipError_t e = mpm::launch_quantize(x, a.M, a.K, a.x_row, a.x_dt, q, scale, st);
+    if (e == hipSuccess) e = mpm::launch_linear8(a, q, scale, out, st);
+    return hip_status(e);
+}
+
+size_t mpm_group_norm_workspace_bytes(const mpm_group_norm_call* call)
+{
+    return check_group_norm(call) == MPM_OK ? mpm::group_norm_bytes(group_norm_call(call)) : 0;
+}
+
+int mpm_group_norm(const mpm_group_norm_call* call, const void* x, void* y, float* stats, void* ws, size_t ws_bytes,
+                   void* stream)
+{
+    int s = check_group_norm(call);
+    if (s != MPM_OK) return s;
+    if (!ok_rows_ptr(x) || !ok_rows_ptr(y) || !aligned(stats, 8)) return MPM_ERR_INVALID_ARG;
+    const mpm::GroupNormCall a = group_norm_call(call);
+    if ((s = check_workspace(ws, ws_bytes, mpm::group_norm_bytes(a))) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_images(call->off, call->B, call->R, as_stream(stream)));
+    return hip_status(mpm::launch_group_norm(a, x, y, stats, ws, as_stream(stream)));
+}
+
+size_t mpm_group_norm_backward_workspace_bytes(const mpm_group_norm_call* call)
+{
+    return check_group_norm(call) == MPM_OK ? mpm::group_norm_backward_bytes(group_norm_call(call)) : 0;
+}
+
+int mpm_group_norm_backward(const mpm_group_norm_call* call, const void* dy, const void* x, const float* stats, void* dx,
+                            void* dw, void* db, void* ws, size_t ws_bytes, void* stream)
+{
+    int s = check_group_norm(call);
+    if (s != MPM_OK) return s;
+    if (!ok_rows_ptr(dy) || !ok_rows_ptr(x) || !ok_rows_ptr(dx) || stats == nullptr || !aligned(stats, 8) ||
+        (dw == nullptr) != (call->w == nullptr) || (db == nullptr) != (call->b == nullptr) || !ok_opt_rows_ptr(dw) ||
+        !ok_opt_rows_ptr(db))
+        return MPM_ERR_INVALID_ARG;
+    const mpm::GroupNormCall a = group_norm_call(call);
+    if ((s = check_workspace(ws, ws_bytes, mpm::group_norm_backward_bytes(a))) != MPM_OK) return s;
+    MPM_LAUNCH_GATE();
+    MPM_DATA_CHECK(checked_images(call->off, call->B, call->R, as_stream(stream)));
+    return hip_status(mpm::launch_group_norm_backward(a, dy, x, stats, dx, dw, db, ws, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -198,4 +198,61 @@ size_t norm_backward_bytes(const NormCall& a);
 hipError_t launch_norm_backward(const NormCall& a, const void* dy, const void* dh, const void* y, const void* f,
                                 const float* stats, const NormGrads& g, void* ws, hipStream_t stream);
 
+// ---- rotary positions, products in 8-bit integers, group norm ----
+
+constexpr int kMaxAxes = 3;
+
+// The angles of rows of heads (as the C ABI's mpm_rotary_call; N rows an image without offsets).
+struct RotaryCall {
+    int R, H, dh, dt, pairs;
+    bool halves;
+    int axes, grid[kMaxAxes];
+    bool per_head;
+    const float* freq;
+    const int32_t* pos;
+    int B, N;
+    const int32_t* off;
+};
+hipError_t launch_rotary(const RotaryCall& a, const HeadRows& x, const HeadRows& out, bool inverse, hipStream_t stream);
+// dfreq may be null (x is not read then); ws holds rotary_backward_bytes(a) bytes where it is not.
+size_t rotary_backward_bytes(const RotaryCall& a);
+hipError_t launch_rotary_backward(const RotaryCall& a, const HeadRows& dout, const HeadRows& x, const HeadRows& dx,
+                                  float* dfreq, void* ws, hipStream_t stream);
+
+enum Activation : int { kActNone = 0, kActRelu = 1, kActSilu = 2, kActGelu = 3 };
+
+// Rows of 8-bit steps: K values a row, Kp = K rounded up to 16 bytes a row of steps.
+__host__ __device__ constexpr int steps_row(int K) { return (K + 15) / 16 * 16; }
+hipError_t launch_quantize(const void* x, long R, int K, long x_row, int dt, int8_t* q, float* scale,
+                           hipStream_t stream);
+
+constexpr int kI8 = 2;  // x of a product: steps, with x_scale
+struct Linear8Call {
+    long M;
+    int N, K, x_dt, dt, act;
+    long x_row, out_row;
+    const float* x_scale;
+    const int8_t* w;
+    const float* w_scale;
+    const void* bias;
+};
+// Whether a call takes its values as they are (few tokens: they become steps inside the product).
+bool linear8_is_few(const Linear8Call& a);
+hipError_t launch_linear8_few(const Linear8Call& a, const void* x, void* out, hipStream_t stream);
+hipError_t launch_linear8(const Linear8Call& a, const int8_t* q, const float* q_scale, void* out, hipStream_t stream);
+
+// Group norm over images of rows (N rows each without offsets).
+struct GroupNormCall {
+    int R, C, groups, dt, act;
+    float eps;
+    int B, N;
+    const int32_t* off;
+    const void *w, *b;
+};
+size_t group_norm_bytes(const GroupNormCall& a);
+hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t stream);
+size_t group_norm_backward_bytes(const GroupNormCall& a);
+hipError_t launch_group_norm_backward(const GroupNormCall& a, const void* dy, const void* x, const float* stats, void* dx,
+                                      void* dw, void* db, void* ws, hipStream_t stream);
+
 }  // namespace mpm
