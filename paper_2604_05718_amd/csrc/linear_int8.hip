@@ -264,7 +264,8 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Linear8Call a, const u
 
 // ---- many tokens -------------------------------------------------------------------------
 
-constexpr int kXcds = 8;  // workgroups are dealt round-robin to 8 XCDs, each with its own L2
+constexpr int kUnits = 256;  // compute units
+constexpr int kXcds = 8;     // workgroups are dealt round-robin to 8 XCDs, each with its own L2
 
 // Workgroup barrier that waits only for this wave's LDS operations, not for loads on their way to LDS.
 __device__ __forceinline__ void lds_barrier()
@@ -280,14 +281,68 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// A workgroup computes BM tokens x BN channels with WM x WN waves, k in steps of BK bytes through STAGES LDS buffers that
-// loads fill directly. A buffer holds rows of BK bytes, BM of tokens and then BN of weights, the 16-byte pieces of a row
-// in an order of its own (piece c of row r at place c ^ swizzle(r)), so that the 32 rows of a fragment are read
-// without bank conflicts; the loads bring each lane's piece from where that order has it.
+// Writes 32 channels' results of one token, channels `at` + 8 (r / 4) + 4 half + r % 4 in v[r], those
+// below N. `whole`: 16 bytes at a time.
+template <class T>
+__device__ __forceinline__ void write_row(uint8_t* to, int at, int half, int N, bool whole, const float (&v)[16])
+{
+    if (!whole) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int i = at + 8 * (r / 4) + 4 * half + r % 4;
+            if (i < N) store_element<T>(to, i, v[r]);
+        }
+        return;
+    }
+    if constexpr (T::kBytes == 4) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int i = at + 8 * c + 4 * half;
+            const u32x4 w = {__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]),
+                             __float_as_uint(v[4 * c + 3])};
+            if (i < N) store16(to + i * 4L, w);
+        }
+    } else {
+        // Half a wave exchanges channels with the other, so that a lane has eight in a row.
+        auto pair = [&](int r) {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            const f32x2 p = {v[r], v[r + 1]};
+            return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+        };
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+            const auto x = __builtin_amdgcn_permlane32_swap(pair(4 * c), pair(4 * c + 4), false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(pair(4 * c + 2), pair(4 * c + 6), false, false);
+            const u32x4 w = {x[0], y[0], x[1], y[1]};
+            const int i = at + 8 * (c + half);
+            if (i < N) store16(to + i * 2L, w);
+        }
+    }
+}
+
+// What a workgroup takes of the tiles: those of its XCD's contiguous share (tokens outside, channels inside), `slots`
+// workgroups by turns.
+struct Share {
+    long tile, end;
+    int slots;
+};
+__device__ __forceinline__ Share share(long tiles)
+{
+    const int xcd = blockIdx.x % kXcds;
+    return Share{tiles * xcd / kXcds + blockIdx.x / kXcds, tiles * (xcd + 1) / kXcds, (int)(gridDim.x / kXcds)};
+}
+
+// Tiles of BM tokens x BN channels, WM x WN waves, k in chunks of BK bytes through STAGES LDS buffers that loads fill
+// directly. A buffer holds rows of BK bytes, BM of tokens and then BN of weights, the 16-byte pieces of a row in an
+// order of its own (piece c of row r at place c ^ swizzle(r)), so that the 32 rows of a fragment are read
+// without bank conflicts; the loads bring each lane's piece from where that order has it. A workgroup walks its
+// tiles with the chunks of all of them as one stream, loads STAGES - 1 chunks ahead, also behind a tile's end: the
+// next tile's first chunks arrive while this one's results are finished, and those are written while the next
+// one's products run.
 template <int BM, int BN, int WM, int WN, int BK, int STAGES, class T, int ACT>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a, const uint8_t* __restrict__ q,
-                                                                const float* __restrict__ q_scale, void* __restrict__ out,
-                                                                int mtiles, int ntiles, bool whole)
+                                                                   const float* __restrict__ q_scale,
+                                                                   void* __restrict__ out, int mtiles, int ntiles, bool whole)
 {
     constexpr int kWaves = WM * WN, THREADS = kWaves * kWave;
     constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
@@ -295,55 +350,74 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
     constexpr int kRows = kWave / kPieces;        // rows a load instruction of a wave brings
     constexpr int kStage = (BM + BN) * BK;
     constexpr int kLoads = (BM + BN) / kRows / kWaves;
-    static_assert((BM + BN) % (kRows * kWaves) == 0 && BM % kRows == 0, "whole loads");
     constexpr int kSteps32 = BK / 32;
+    constexpr int kAhead = STAGES - 1;
+    static_assert((BM + BN) % (kRows * kWaves) == 0 && BM % kRows == 0, "whole loads");
+    // (A wave's loads are a whole number of 16 rows apart, so a lane's swizzle is one for all.)
+    static_assert(kRows * kWaves % 16 == 0 && BM % 16 == 0, "one swizzle a lane");
+    static_assert(BN <= THREADS && BM + BN <= 2 * THREADS, "scales: a thread each");
     extern __shared__ __align__(1024) uint8_t lds[];
-    float* w_scale = reinterpret_cast<float*>(lds + STAGES * kStage);
-    float* bias = w_scale + BN;
+    float* channels = reinterpret_cast<float*>(lds + STAGES * kStage);  // [2][scale, bias][BN], by tiles in turns
 
-    // Tiles in order, tokens outside, dealt to the XCDs in eight contiguous shares.
-    const long tiles = (long)mtiles * ntiles;
-    const int xcd = blockIdx.x % kXcds;
-    const long tile = tiles * xcd / kXcds + blockIdx.x / kXcds;
-    if (tile >= tiles * (xcd + 1) / kXcds) return;
-    const long m0 = tile / ntiles * BM;
-    const int n0 = (int)(tile % ntiles) * BN;
+    const Share sh = share((long)mtiles * ntiles);
+    if (sh.tile >= sh.end) return;
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, half = lane >> 5;
     const int wm = wave % WM, wn = wave / WM;
-    const int Kp = steps_row(a.K), chunks = (Kp + BK - 1) / BK;
+    const int Kp = steps_row(a.K), chunks = (Kp + BK - 1) / BK, full = Kp / BK;
 
-    for (int i = t; i < BN; i += THREADS) {
-        const int n = min(n0 + i, a.N - 1);
-        w_scale[i] = a.w_scale[n] * kUp;
-        bias[i] = a.bias ? element<T>(a.bias, n) : 0.0f;
-    }
-
-    auto swizzle = [](int row) { return kPieces == 8 ? row & 7 : (row >> 1) & 3; };
-    // This lane's rows and pieces: load i of wave w brings rows (w + kWaves i) kRows ... of the buffer.
+    // 16 rows of one piece meet the 64 banks once.
+    auto swizzle = [](int row) { return kPieces == 8 ? (row >> 1) & 7 : (row >> 2) & 3; };
+    // The stream's end that loads: its tile and chunk, and this lane's rows there (load i of a wave brings rows
+    // (wave + kWaves i) kRows ... of the buffer), clamped to those that exist.
+    const int lrow = lane / kPieces, piece = ((lane % kPieces) ^ swizzle(wave * kRows + lrow)) * 16;
     const uint8_t* from[kLoads];
-    const int lrow = lane / kPieces, piece = (lane % kPieces) ^ swizzle(lrow);
+    long ltile = sh.tile;
+    int lchunk = 0, lbuf = 0;
+    auto place = [&](long tile) {
+        const long m0 = tile / ntiles * BM;
+        const int n0 = (int)(tile % ntiles) * BN;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int r = (wave + kWaves * i) * kRows + lrow;  // (kRows and BM are multiples of 8: the swizzle is lrow's)
-        from[i] = r < BM ? q + min(m0 + r, a.M - 1) * Kp
-                         : reinterpret_cast<const uint8_t*>(a.w) + (long)min(n0 + r - BM, a.N - 1) * Kp;
-    }
-    auto issue = [&](int chunk, int i) {
-        // Past a row's end the last piece again: the products leave it out.
-        const uint8_t* p = from[i] + min(chunk * BK + piece * 16, Kp - 16);
-        const uint32_t to = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)(
-            lds + (chunk % STAGES) * kStage + (wave + kWaves * i) * kRows * BK);
-        asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(to) : "memory");
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = (wave + kWaves * i) * kRows + lrow;
+            from[i] = r < BM ? q + min(m0 + r, a.M - 1) * Kp
+                             : reinterpret_cast<const uint8_t*>(a.w) + (long)min(n0 + r - BM, a.N - 1) * Kp;
+        }
     };
+    // The scales of a tile: a lane's tokens', and a thread's channel's on its way to LDS.
+    float xs[MT], w_scale, bias;
+    auto load_scales = [&](long tile) {
+        const long m0 = tile / ntiles * BM;
+        const int n = min((int)(tile % ntiles) * BN + min(t, BN - 1), a.N - 1);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xs[m] = q_scale[min(m0 + (wm * MT + m) * 32 + l32, a.M - 1)] * kDown;
+        w_scale = a.w_scale[n] * kUp;
+        bias = a.bias ? element<T>(a.bias, n) : 0.0f;
+    };
+    // The next chunk of the stream, if there is one.
+    auto issue = [&]() {
+        if (ltile >= sh.end) return;
+        const uint32_t to = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)(
+            lds + lbuf * kStage + wave * kRows * BK);
+        // Past a row's end the last piece again: the products leave it out.
+        const int at = min(lchunk * BK + piece, Kp - 16);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(from[i] + at), "{m0}"(to + kWaves * i * kRows * BK)
+                         : "memory");
+        lbuf = lbuf + 1 == STAGES ? 0 : lbuf + 1;
+        if (++lchunk == chunks) {
+            lchunk = 0;
+            ltile += sh.slots;
+            if (ltile < sh.end) place(ltile);
+        }
+    };
+
     const int sw = swizzle(l32);
     i32x16 acc[NT][MT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[n][m] = i32x16{};
     i32x4 fw[2][NT], fx[2][MT];
-    auto read = [&](int to, int chunk, int g) {
-        const uint8_t* s = lds + (chunk % STAGES) * kStage + l32 * BK + (((2 * g + half) ^ sw) << 4);
+    int buf = 0;  // of the chunk that is multiplied
+    auto read = [&](int to, int g) {
+        const uint8_t* s = lds + buf * kStage + l32 * BK + (((2 * g + half) ^ sw) << 4);
 #pragma unroll
         for (int m = 0; m < MT; ++m) fx[to][m] = *reinterpret_cast<const i32x4*>(s + (wm * MT + m) * 32 * BK);
 #pragma unroll
@@ -356,34 +430,52 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
             for (int m = 0; m < MT; ++m)
                 acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[from][n], fx[from][m], acc[n][m], 0, 0, 0);
     };
-
-#pragma unroll
-    for (int c = 0; c < STAGES - 1; ++c)
-        if (c < chunks) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) issue(c, i);
+    // Chunk c of a tile is there once at most the loads of the kAhead - 1 chunks behind it in the stream are on their
+    // way (no count but 0 at the stream's end). A tile's first kAhead have been waited for before.
+    auto arrive = [&](int c) {
+        if (c >= kAhead) {
+            if (ltile < sh.end) wait_loads<kLoads*(kAhead - 1)>();
+            else wait_loads<0>();
         }
-    const int full = Kp / BK;
-    for (int c = 0; c < chunks; ++c) {
-        // The loads of chunk c are done when at most those of the chunks after it are on their way.
-        if (c + STAGES - 2 < chunks) wait_loads<kLoads*(STAGES - 2)>();
-        else wait_loads<0>();
         lds_barrier();
-        if (c + STAGES - 1 < chunks) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) issue(c + STAGES - 1, i);
+        issue();
+    };
+
+    load_scales(sh.tile);
+    place(sh.tile);
+    for (int c = 0; c < kAhead; ++c) issue();
+    wait_loads<0>();
+    int turn = 0;
+    auto hand_over = [&]() {  // the channels' values of the tile that comes
+        if (t < BN) {
+            channels[(2 * turn) * BN + t] = w_scale;
+            channels[(2 * turn + 1) * BN + t] = bias;
         }
-        if (c < full) {
-            read(0, c, 0);
+    };
+    hand_over();
+#pragma unroll 1
+    for (long tile = sh.tile; tile < sh.end; tile += sh.slots) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[n][m] = i32x16{};
+#pragma unroll 1
+        for (int c = 0; c < full; ++c) {
+            arrive(c);
+            read(0, 0);
 #pragma unroll
             for (int g = 0; g < kSteps32; ++g) {
-                if (g + 1 < kSteps32) read((g + 1) & 1, c, g + 1);
+                if (g + 1 < kSteps32) read((g + 1) & 1, g + 1);
                 multiply(g & 1);
             }
-        } else {
-            const int left = Kp - c * BK;
+            buf = buf + 1 == STAGES ? 0 : buf + 1;
+        }
+        if (full < chunks) {
+            arrive(full);
+            const int left = Kp - full * BK;
+#pragma unroll 1
             for (int g = 0; g * 32 < left; ++g) {
-                read(0, c, g);
+                read(0, g);
                 if (g * 32 + 16 >= left && half) {  // the second 16 bytes lie past the end
                     const i32x4 none = {0, 0, 0, 0};
 #pragma unroll
@@ -391,61 +483,38 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
                 }
                 multiply(0);
             }
+            buf = buf + 1 == STAGES ? 0 : buf + 1;
         }
-    }
 
-    // acc[n][m][r]: token m * 32 + l32 of the wave's, channel n * 32 + 8 (r / 4) + 4 half + r % 4.
+        // Everything on its way has arrived before the first write leaves, so that no wait for loads waits for writes.
+        float now[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const long row = m0 + (wm * MT + m) * 32 + l32;
-        const float xs = q_scale[min(row, a.M - 1)] * kDown;
-        const bool live = row < a.M;
-        uint8_t* to = static_cast<uint8_t*>(out) + row * a.out_row * T::kBytes;
+        for (int m = 0; m < MT; ++m) now[m] = xs[m];
+        const float *ws = channels + 2 * turn * BN, *bs = ws + BN;
+        const bool last = tile + sh.slots >= sh.end;
+        if (!last) load_scales(tile + sh.slots);
+        wait_loads<0>();
+        turn ^= 1;
+        if (!last) hand_over();
+        // acc[n][m][r]: token m * 32 + l32 of the wave's, channel n * 32 + 8 (r / 4) + 4 half + r % 4.
+        const long m0 = tile / ntiles * BM;
+        const int n0 = (int)(tile % ntiles) * BN;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int nb = (wn * NT + n) * 32;
-            float v[16];
+        for (int m = 0; m < MT; ++m) {
+            const long row = m0 + (wm * MT + m) * 32 + l32;
+            uint8_t* to = static_cast<uint8_t*>(out) + row * a.out_row * T::kBytes;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int i = nb + 8 * (r / 4) + 4 * half + r % 4;
-                v[r] = finish<T, ACT>(acc[n][m][r], xs, w_scale[i], bias[i]);
-            }
-            if (whole) {
-                if constexpr (T::kBytes == 4) {
+            for (int n = 0; n < NT; ++n) {
+                const int nb = (wn * NT + n) * 32;
+                float v[16];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int i = n0 + nb + 8 * c + 4 * half;
-                        const u32x4 w = {__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
-                                         __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3])};
-                        if (live && i < a.N) store16(to + i * 4L, w);
-                    }
-                } else {
-                    // Half a wave exchanges channels with the other, so that a lane has eight in a row.
+                for (int c = 0; c < 4; ++c) {
+                    const f32x4 w = *reinterpret_cast<const f32x4*>(ws + nb + 8 * c + 4 * half);
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(bs + nb + 8 * c + 4 * half);
 #pragma unroll
-                    for (int c = 0; c < 4; c += 2) {
-                        uint32_t w[2][2];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            typedef float f32x2 __attribute__((ext_vector_type(2)));
-                            const f32x2 p = {v[4 * c + 2 * e], v[4 * c + 2 * e + 1]};
-                            const f32x2 s = {v[4 * c + 4 + 2 * e], v[4 * c + 5 + 2 * e]};
-                            const auto x = __builtin_amdgcn_permlane32_swap(
-                                __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2)),
-                                __builtin_bit_cast(uint32_t, __builtin_convertvector(s, bf16x2)), false, false);
-                            w[0][e] = x[0];
-                            w[1][e] = x[1];
-                        }
-                        const u32x4 packed = {w[0][0], w[0][1], w[1][0], w[1][1]};
-                        const int i = n0 + nb + 8 * (c + half);
-                        if (live && i < a.N) store16(to + i * 2L, packed);
-                    }
+                    for (int r = 0; r < 4; ++r) v[4 * c + r] = finish<T, ACT>(acc[n][m][4 * c + r], now[m], w[r], b[r]);
                 }
-            } else if (live) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int i = n0 + nb + 8 * (r / 4) + 4 * half + r % 4;
-                    if (i < a.N) store_element<T>(to, i, v[r]);
-                }
+                if (row < a.M) write_row<T>(to, n0 + nb, half, a.N, whole, v);
             }
         }
     }
@@ -454,24 +523,32 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
 template <int BM, int BN, int WM, int WN, int BK, int STAGES, class T, int ACT>
 hipError_t product(const Linear8Call& a, const int8_t* q, const float* q_scale, void* out, hipStream_t st)
 {
-    constexpr size_t bytes = (size_t)STAGES * (BM + BN) * BK + 2 * BN * 4;
+    constexpr size_t bytes = (size_t)STAGES * (BM + BN) * BK + 4 * BN * 4;
     const auto kernel = product_kernel<BM, BN, WM, WN, BK, STAGES, T, ACT>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
     const long mtiles = (a.M + BM - 1) / BM, ntiles = (a.N + BN - 1) / BN, per = (mtiles * ntiles + kXcds - 1) / kXcds;
+    // As many workgroups as the chip holds (by LDS and by registers: two waves a SIMD).
+    constexpr int kHeld = (int)std::min<size_t>((160 << 10) / bytes, 8 / (WM * WN) > 0 ? 8 / (WM * WN) : 1);
+    const long slots = std::min(per, (long)kHeld * kUnits / kXcds);
     // Rows of whole 16 bytes, of a whole number of them: written 16 bytes at a time.
     constexpr int kPer = 16 / T::kBytes;
     const bool whole = a.N % kPer == 0 && a.out_row % kPer == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcds)), dim3(WM * WN * kWave), bytes, st, a,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(slots * kXcds)), dim3(WM * WN * kWave), bytes, st, a,
                        reinterpret_cast<const uint8_t*>(q), q_scale, out, (int)mtiles, (int)ntiles, whole);
     return hipGetLastError();
 }
 
+// The widest tiles that leave no compute unit idle: a tile of 256 x 256 loads half the bytes a product that one of 128 x 128
+// does, which loads half of what one of 64 x 64 does. Products (bfloat16 results, no activation) in tiles of 64 / 128 /
+// 256, us: 4103 x 150 x 848 7.3 / 11.6 / 23, 512 x 768 x 768 5.1 / 7.4 / 15.1, 1024 x 2304 x 768 9.2 / 8.2 / 16.3,
+// 8000 x 1024 x 1024 23.7 / 15.6 / 21.2, 11000 x 2304 x 768 49 / 33.1 / 34.0, 45888 x 2304 x 768 159 / 124 / 119.
 template <class T, int ACT>
 hipError_t product_of(const Linear8Call& a, const int8_t* q, const float* q_scale, void* out, hipStream_t st)
 {
-    const long big = ((a.M + 127) / 128) * ((a.N + 255) / 256);
-    if (big >= 256) return product<128, 256, 2, 2, 64, 3, T, ACT>(a, q, q_scale, out, st);
+    auto tiles = [&](int rows) { return (a.M + rows - 1) / rows * ((a.N + rows - 1) / rows); };
+    if (tiles(256) >= 2 * kUnits) return product<256, 256, 2, 4, 128, 2, T, ACT>(a, q, q_scale, out, st);
+    if (tiles(128) >= kUnits / 2) return product<128, 128, 2, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
     return product<64, 64, 2, 2, 128, 3, T, ACT>(a, q, q_scale, out, st);
 }
 

@@ -26,10 +26,25 @@ __device__ __forceinline__ float normal_integral(float z)
     return z < 0.0f ? tail : 1.0f - tail;
 }
 
+// z times the normal distribution's integral, as z / (1 + e^-l) with l the logarithm of the integral's odds, an odd
+// function of z close to a polynomial of seventh degree. The coefficients minimise the largest error of l over |z| <= 6
+// where the result is 10^-4 or more, 0.00104: a quarter of bfloat16's half step for negative z, less for positive.
+// Two thirds of the instructions of the integral itself: the product of 45920 x 4096 x 1024 with it 303 us against 330.
+__device__ __forceinline__ float gelu_bf16(float z)
+{
+    constexpr float kLog2e = 1.4426950408889634f;
+    const float u = z * z;
+    float p = fmaf(-7.25138e-6f * kLog2e, u, 9.3992063e-4f * kLog2e);
+    p = fmaf(p, u, -7.55007635e-2f * kLog2e);
+    p = fmaf(p, u, -1.59312151f * kLog2e);
+    return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(p * z));
+}
+
 // (max() would drop a NaN)
 template <int ACT, bool PRECISE>
 __device__ __forceinline__ float activate(float z)
 {
+    if constexpr (ACT == kActGelu && !PRECISE) return gelu_bf16(z);
     if constexpr (ACT == kActRelu) return z < 0.0f ? 0.0f : z;
     if constexpr (ACT == kActSilu) return z * sigmoid(z);
     if constexpr (ACT == kActGelu) return z * normal_integral<PRECISE>(z);

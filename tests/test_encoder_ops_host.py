@@ -9,6 +9,7 @@ import sys
 import pytest
 import torch
 
+import encoder_refs as ref
 import paper_2604_05718_amd as mpm
 from paper_2604_05718_amd import _lib, block_ops
 from test_block_bindings import Recorder, device
@@ -176,6 +177,14 @@ def test_injected_launch_failures():
     p = subprocess.run([sys.executable, "-c", INJECT], capture_output=True, text=True, cwd=root, env=env, timeout=100)
     assert p.returncode == 0, p.stderr[-2000:]
     assert json.loads(p.stdout) == [4] * 6 + [1]  # MPM_ERR_HIP; argument errors come first
+
+
+def test_gelu_of_bfloat16_results():
+    """The polynomial form against GELU over |z| <= 40, in 64 bits (float32 adds 2^-20)."""
+    z = torch.linspace(-40, 40, 400001, dtype=torch.float64)
+    off = (ref.gelu_bf16(z) - ref.act(z, "gelu")).abs()
+    assert bool((off <= ref.gelu_bf16_bound(z)).all())
+    assert float((off / ref.act(z, "gelu").abs().clamp_min(1e-4)).max()) < 2.0 ** -8 / 3
 
 
 # ---- the bindings ------------------------------------------------------------------------
