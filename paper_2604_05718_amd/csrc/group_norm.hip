@@ -5,11 +5,13 @@
 // A thread keeps one vector of 16 bytes of the channels and walks rows, so that sums are kept by channel
 // and groups of any width are sums over channels afterwards.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "mpm_act.h"
 #include "mpm_device.h"
 #include "mpm_launch.h"
+#include "mpm_work.h"
 
 namespace mpm {
 namespace {
@@ -430,6 +432,375 @@ __global__ __launch_bounds__(kThreads) void input_gradient_kernel(GroupNormCall 
     }
 }
 
+// ---- images whose part of some groups stays in registers ---------------------------------
+//
+// A workgroup takes a slab of whole groups of one image: it reads the slab once, keeps it, and writes it. Rows past what
+// its registers hold are read again (the host picks slabs that fit, but for packed images it knows only their
+// average).
+
+constexpr int kSlabThreads = 1024;
+
+struct Slab {
+    int vecs, cols, slabs, ways, threads;
+    int width;       // channels a group
+    int groups;      // of a slab
+    FixedDiv cols_of, width_of, per_of;  // by cols; by a group's channels; by its vectors (where it has whole ones)
+};
+
+// Slab and image of a workgroup: the slabs of an image on one XCD, whose L2 then joins the lines that two of them share.
+constexpr int kXcds = 8;
+__device__ __forceinline__ bool slab_item(long items, long* item)
+{
+    const int xcd = blockIdx.x % kXcds;
+    *item = items * xcd / kXcds + blockIdx.x / kXcds;
+    return *item < items * (xcd + 1) / kXcds;
+}
+
+// The sum of a value of every thread over each group of the slab, in LDS out[group]. v: by channel of the thread's vector;
+// ONE: a vector lies in one group.
+template <class S, bool ONE>
+__device__ __forceinline__ void group_sums(const float (&v)[Vec<S>::kPer], const Slab& s, float* lds, float* out)
+{
+    constexpr int kPer = Vec<S>::kPer;
+    const int t = threadIdx.x, lane = t % kWave;
+    __syncthreads();  // what was in LDS has been read
+    if constexpr (ONE) {
+        float one = 0.0f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) one += v[e];
+        lds[t] = one;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) lds[e * kSlabThreads + t] = v[e];
+    }
+    __syncthreads();
+    const int per = ONE ? s.width / kPer : s.width, many = per * s.ways;
+    for (int g = t / kWave; g < s.groups; g += s.threads / kWave) {
+        float sum = 0.0f;
+        for (int i = lane; i < many; i += kWave) {
+            const int way = ONE ? s.per_of(i) : s.width_of(i), c = g * per + i - way * per;
+            if constexpr (ONE) sum += lds[way * s.cols + c];
+            else sum += c < s.cols * kPer ? lds[c % kPer * kSlabThreads + way * s.cols + c / kPer] : 0.0f;
+        }
+        sum = lanes_sum<kWave>(sum);
+        if (lane == 0) out[g] = sum;
+    }
+    __syncthreads();
+}
+
+// Group g of the slab that channel e of this thread's vector belongs to.
+template <class S, bool ONE>
+__device__ __forceinline__ int slab_group(const Slab& s, int col, int e)
+{
+    constexpr int kPer = Vec<S>::kPer;
+    return ONE ? s.per_of(col) : s.width_of(col * kPer + e);
+}
+
+constexpr int kMostSlabGroups = 256;
+
+template <class S, int ACT, bool ONE, int VPT>
+__global__ __launch_bounds__(kSlabThreads) void slab_kernel(GroupNormCall a, Slab s, const uint8_t* x, uint8_t* y,
+                                                            float2* __restrict__ stats)
+{
+    typedef Vec<S> V;
+    constexpr int kPer = V::kPer, kOwn = ONE ? 1 : kPer;  // statistics a vector has
+    __shared__ float lds[(ONE ? 1 : kPer) * kSlabThreads];
+    __shared__ float sums[kMostSlabGroups];
+    long item;
+    if (!slab_item((long)a.B * s.slabs, &item)) return;
+    const int b = (int)(item / s.slabs), slab = (int)(item % s.slabs);
+    const Rows it = image_rows(a, b);
+    const int n = (int)(it.end - it.first), t = threadIdx.x, way = s.cols_of(t), local = t - way * s.cols;
+    const int col = slab * s.cols + local, groups = min(s.groups, a.groups - slab * s.groups);
+    const bool live = way < s.ways && col < s.vecs;
+    float2* out = stats ? stats + (long)b * a.groups + slab * s.groups : nullptr;
+    if (n == 0) {
+        if (out && t < groups) out[t] = make_float2(0.0f, 0.0f);
+        return;
+    }
+    const long stride = (long)a.C * S::kBytes;
+    const uint8_t* from = x + it.first * stride + (long)col * 16;
+    V v[VPT];
+    const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+        const int r = way + u * s.ways;
+        v[u].w = none;
+        if (live && r < n) v[u].w = load16(from + r * stride);
+    }
+    const int rest = way + VPT * s.ways;  // the first row that is not kept
+    // A group's mean is that of its values less its first one, which leaves a mean far from zero its digits; its
+    // deviations are taken from the mean.
+    float first[kOwn], mean[kOwn], rstd[kOwn], sum[kPer];
+    int group[kOwn];
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        group[e] = live ? slab_group<S, ONE>(s, local, e) : 0;
+        first[e] = parameter(x, a.dt, it.first * a.C + (long)(slab * s.groups + group[e]) * s.width);
+    }
+    const float count = (float)n * (float)s.width;
+    auto each = [&](auto&& use) {  // every value of the thread's rows and channels
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < VPT; ++u)
+            if (live && way + u * s.ways < n) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) use(v[u].get(e), e);
+            }
+        if (live)
+            for (int r = rest; r < n; r += s.ways) {
+                V w;
+                w.w = load16(from + r * stride);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) use(w.get(e), e);
+            }
+    };
+    each([&](float f, int e) { sum[e] += f - first[ONE ? 0 : e]; });
+    group_sums<S, ONE>(sum, s, lds, sums);
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) mean[e] = first[e] + sums[group[e]] / count;
+    each([&](float f, int e) {
+        const float d = f - mean[ONE ? 0 : e];
+        sum[e] = fmaf(d, d, sum[e]);
+    });
+    group_sums<S, ONE>(sum, s, lds, sums);
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) rstd[e] = 1.0f / sqrtf(sums[group[e]] / count + a.eps);
+    if (!live) return;
+    // (a thread of each group's first channel has its statistics)
+    if (out && way == 0) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int c = local * kPer + e, g = group[ONE ? 0 : e];
+            if (c == g * s.width && g < groups) out[g] = make_float2(mean[ONE ? 0 : e], rstd[ONE ? 0 : e]);
+        }
+    }
+    V wv, bv;
+    if (a.w) wv.w = load16(static_cast<const uint8_t*>(a.w) + col * 16);
+    if (a.b) bv.w = load16(static_cast<const uint8_t*>(a.b) + col * 16);
+    auto write = [&](const V& f, int r) {
+        float o[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            o[e] = activate<ACT, S::kBytes == 4>(fmaf((f.get(e) - mean[ONE ? 0 : e]) * rstd[ONE ? 0 : e],
+                                                      a.w ? wv.get(e) : 1.0f, a.b ? bv.get(e) : 0.0f));
+        store16(y + it.first * stride + (long)col * 16 + r * stride, V::pack(o));
+    };
+#pragma unroll
+    for (int u = 0; u < VPT; ++u)
+        if (way + u * s.ways < n) write(v[u], way + u * s.ways);
+    for (int r = rest; r < n; r += s.ways) {
+        V w;
+        w.w = load16(from + r * stride);
+        write(w, r);
+    }
+}
+
+// The gradients likewise: the slab of x and dy kept between the sums and dx. parts[image][C]: the channels' sums of gz and
+// gz t, for dw and db.
+template <class S, int ACT, bool ONE, int VPT>
+__global__ __launch_bounds__(kSlabThreads) void slab_backward_kernel(GroupNormCall a, Slab s, const uint8_t* dy,
+                                                                     const uint8_t* x, uint8_t* dx,
+                                                                     const float2* __restrict__ stats,
+                                                                     float2* __restrict__ parts)
+{
+    typedef Vec<S> V;
+    constexpr int kPer = V::kPer, kOwn = ONE ? 1 : kPer;
+    __shared__ float lds[kPer * kSlabThreads];
+    __shared__ float sums[2][kMostSlabGroups];
+    const long items = (long)a.B * s.slabs;
+    long item;
+    if (!slab_item(items, &item)) return;
+    const int b = (int)(item / s.slabs), slab = (int)(item % s.slabs);
+    const Rows it = image_rows(a, b);
+    const int n = (int)(it.end - it.first), t = threadIdx.x, way = s.cols_of(t), local = t - way * s.cols;
+    const int col = slab * s.cols + local;
+    const bool live = way < s.ways && col < s.vecs;
+    const long stride = (long)a.C * S::kBytes;
+    if (a.off && live) {  // a share of the rows of no image
+        const u32x4 none = {0, 0, 0, 0};
+        const long lo = min(max((long)a.off[0], 0L), (long)a.R), hi = min(max((long)a.off[a.B], lo), (long)a.R);
+        const long many = lo + a.R - hi, end = many * (b + 1L) / a.B;
+        for (long r = many * b / a.B + way; r < end; r += s.ways)
+            store16(dx + (r < lo ? r : r - lo + hi) * stride + (long)col * 16, none);
+    }
+    const long at = it.first * stride + (long)col * 16;
+    V v[VPT], g[VPT];
+    const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+        const int r = way + u * s.ways;
+        v[u].w = g[u].w = none;
+        if (live && r < n) {
+            v[u].w = load16(x + at + r * stride);
+            g[u].w = load16(dy + at + r * stride);
+        }
+    }
+    const int rest = way + VPT * s.ways;
+    V wv, bv;
+    wv.w = bv.w = none;
+    if (a.w && live) wv.w = load16(static_cast<const uint8_t*>(a.w) + col * 16);
+    if (a.b && live) bv.w = load16(static_cast<const uint8_t*>(a.b) + col * 16);
+    float mean[kOwn], rstd[kOwn], s0[kPer], s1[kPer];
+    int group[kOwn];
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        group[e] = live ? slab_group<S, ONE>(s, local, e) : 0;
+        const float2 q = stats[(long)b * a.groups + slab * s.groups + group[e]];
+        mean[e] = q.x;
+        rstd[e] = q.y;
+    }
+    auto weight = [&](int e) { return a.w ? wv.get(e) : 1.0f; };
+    // t and gz of a value and its gradient.
+    auto slope = [&](float f, float d, int e, float* gz) {
+        const float u = (f - mean[ONE ? 0 : e]) * rstd[ONE ? 0 : e];
+        *gz = d * activation_slope<ACT, S::kBytes == 4>(fmaf(u, weight(e), a.b ? bv.get(e) : 0.0f));
+        return u;
+    };
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) s0[e] = s1[e] = 0.0f;
+    auto add = [&](const V& f, const V& d) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            float gz;
+            const float u = slope(f.get(e), d.get(e), e, &gz);
+            s0[e] += gz;
+            s1[e] = fmaf(gz, u, s1[e]);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < VPT; ++u)
+        if (live && way + u * s.ways < n) add(v[u], g[u]);
+    if (live)
+        for (int r = rest; r < n; r += s.ways) {
+            V f, d;
+            f.w = load16(x + at + r * stride);
+            d.w = load16(dy + at + r * stride);
+            add(f, d);
+        }
+    // The channels' sums, for dw and db, one value of every thread's vector at a time ...
+    if (parts) {
+        const int lane = t % kWave, channels = min(s.cols, s.vecs - slab * s.cols) * kPer;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) lds[e * kSlabThreads + t] = k ? s1[e] : s0[e];
+            __syncthreads();
+            for (int c = t / kWave; c < channels; c += s.threads / kWave) {
+                const float* p = lds + c % kPer * kSlabThreads + c / kPer;
+                float sum = 0.0f;
+                for (int w = lane; w < s.ways; w += kWave) sum += p[w * s.cols];
+                sum = lanes_sum<kWave>(sum);
+                if (lane == 0)
+                    reinterpret_cast<float*>(parts)[2 * ((long)b * a.C + (long)slab * s.cols * kPer + c) + k] = sum;
+            }
+        }
+    }
+    // ... and the groups', of gt and gt t.
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        s0[e] *= weight(e);
+        s1[e] *= weight(e);
+    }
+    group_sums<S, ONE>(s0, s, lds, sums[0]);
+    group_sums<S, ONE>(s1, s, lds, sums[1]);
+    if (!live) return;
+    const float inv = 1.0f / ((float)n * (float)s.width);
+    float m0[kOwn], m1[kOwn];
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        m0[e] = sums[0][group[e]] * inv;
+        m1[e] = sums[1][group[e]] * inv;
+    }
+    auto write = [&](const V& f, const V& d, int r) {
+        float o[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            float gz;
+            const float u = slope(f.get(e), d.get(e), e, &gz);
+            o[e] = rstd[ONE ? 0 : e] * (fmaf(gz, weight(e), -m0[ONE ? 0 : e]) - u * m1[ONE ? 0 : e]);
+        }
+        store16(dx + at + r * stride, V::pack(o));
+    };
+#pragma unroll
+    for (int u = 0; u < VPT; ++u)
+        if (way + u * s.ways < n) write(v[u], g[u], way + u * s.ways);
+    for (int r = rest; r < n; r += s.ways) {
+        V f, d;
+        f.w = load16(x + at + r * stride);
+        d.w = load16(dy + at + r * stride);
+        write(f, d, r);
+    }
+}
+
+// How a call goes by slabs: `vpt` vectors a thread keeps of a tensor, for images of the average length. Slabs are the
+// widest whole groups that fit and leave a workgroup for every compute unit, of whole 64-byte pieces where groups allow;
+// vecs of a slab 0: no slab fits.
+struct Plan {
+    Slab s;
+    int vpt;
+};
+constexpr int kUnits = 256;
+
+int common_divisor(int a, int b) { return b ? common_divisor(b, a % b) : a; }
+
+Plan plan(const GroupNormCall& a, bool backward)
+{
+    const int bytes = a.dt == kBf16 ? 2 : 4, per = 16 / bytes, width = a.C / a.groups;
+    const int unit = width / common_divisor(width, per);   // vectors of the fewest whole groups that fill vectors
+    const int unit_groups = unit * per / width;
+    const int vecs = a.C / per, units = vecs / unit;
+    const long rows = std::max(1L, ((long)a.R + a.B - 1) / a.B);
+    const int most = backward ? 8 : 16;
+    int best = 0;
+    double best_use = 0.0;
+    for (int k = 1; k <= units; ++k) {
+        const int cols = unit * k;
+        if (cols > kSlabThreads / 4 || (long)unit_groups * k > kMostSlabGroups) break;
+        const bool fits = (kSlabThreads / cols) * (long)most >= rows;
+        const long groups = (long)a.B * ((units + k - 1) / k);
+        if (k > 1 && (!fits || groups < kUnits)) break;
+        const int len = cols * 16;
+        const double use = len % 128 == 0 || k == units ? 1.0 : (double)len / (len + 128 - common_divisor(len, 128));
+        if (use > best_use + 0.05) {
+            best_use = use;
+            best = k;
+        }
+    }
+    Plan p{Slab{vecs, 0, 0, 0, 0, width, 0, FixedDiv(1), FixedDiv((uint32_t)width), FixedDiv((uint32_t)std::max(1, width / per))},
+           1};
+    if (best == 0) return p;
+    Slab& s = p.s;
+    s.cols = unit * best;
+    s.slabs = (units + best - 1) / best;
+    s.groups = unit_groups * best;
+    s.cols_of = FixedDiv((uint32_t)s.cols);
+    // Enough threads for about four vectors each.
+    s.threads = kSlabThreads;
+    while (s.threads > 256 && s.cols * 2 <= s.threads / 4 && (s.threads / 2 / s.cols) * 4L >= rows) s.threads /= 2;
+    s.ways = s.threads / s.cols;
+    p.vpt = rows <= (long)s.ways * (most / 4) ? most / 4 : most;
+    return p;
+}
+
+// Whether a call goes by slabs: they read a tensor once, and once more what does not fit (`most` vectors a thread), in one
+// launch, but a workgroup works through its slab alone.
+bool by_slabs(const GroupNormCall& a, bool backward, const Plan& p)
+{
+    if (p.s.cols == 0 || (long)a.B * p.s.slabs > (1L << 21)) return false;  // (a grid holds 2^32 threads)
+    const double rows = std::max(1.0, (double)a.R / a.B), groups = (double)a.B * p.s.slabs;
+    const double slab = rows * p.s.cols * 16, total = (double)a.R * a.C * (a.dt == kBf16 ? 2 : 4);
+    const double kept = std::min(1.0, (double)p.vpt * p.s.ways / rows);
+    const double moved = backward ? 3 + 2 * (1 - kept) : 2 + 2 * (1 - kept);  // tensors
+    const double rounds = std::ceil(groups / kUnits);
+    // us: a workgroup alone moves about 50 KB a us, the chip 5.2 MB; three launches 9 us.
+    const double alone = rounds * (3.0 + slab * moved / 5e4), all = total * moved / 5.2e6;
+    const double passes = 9.0 + total * (backward ? 5.0 : 3.0) / 5.2e6;
+    return std::max(alone, all) < passes;
+}
+
 Deal deal(const GroupNormCall& a)
 {
     Deal d;
@@ -466,12 +837,40 @@ hipError_t with_kind(const GroupNormCall& a, F&& go)
     return a.dt == kBf16 ? act(Bf16{}) : act(F32{});
 }
 
+// ... and whether a vector lies in one group, and the vectors a thread keeps.
+template <int FEW, int MANY, class F>
+hipError_t with_slabs(const GroupNormCall& a, const Plan& p, F&& go)
+{
+    const bool one = p.s.width % (a.dt == kBf16 ? 8 : 4) == 0;
+    return with_kind(a, [&](auto type, auto act) {
+        constexpr std::integral_constant<int, FEW> few{};
+        constexpr std::integral_constant<int, MANY> many{};
+        if (one) return p.vpt == FEW ? go(type, act, std::true_type{}, few) : go(type, act, std::true_type{}, many);
+        return p.vpt == FEW ? go(type, act, std::false_type{}, few) : go(type, act, std::false_type{}, many);
+    });
+}
+
 }  // namespace
 
-size_t group_norm_bytes(const GroupNormCall& a) { return parts_bytes(a, deal(a)) + stats_bytes(a); }
+size_t group_norm_bytes(const GroupNormCall& a)
+{
+    return by_slabs(a, false, plan(a, false)) ? 0 : parts_bytes(a, deal(a)) + stats_bytes(a);
+}
+
 
 hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t st)
 {
+    const Plan p = plan(a, false);
+    if (by_slabs(a, false, p)) {
+        const long items = (long)a.B * p.s.slabs;
+        const dim3 grid((unsigned)((items + kXcds - 1) / kXcds * kXcds)), threads(p.s.threads);
+        return with_slabs<4, 16>(a, p, [&](auto type, auto act, auto one, auto vpt) {
+            hipLaunchKernelGGL((slab_kernel<decltype(type), decltype(act)::value, decltype(one)::value, decltype(vpt)::value>),
+                               grid, threads, 0, st, a, p.s, static_cast<const uint8_t*>(x), static_cast<uint8_t*>(y),
+                               reinterpret_cast<float2*>(stats));
+            return hipGetLastError();
+        });
+    }
     const Deal d = deal(a);
     float2* parts = static_cast<float2*>(ws);
     float2* sp = stats ? reinterpret_cast<float2*>(stats)
@@ -488,13 +887,37 @@ hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, flo
     });
 }
 
-size_t group_norm_backward_bytes(const GroupNormCall& a) { return parts_bytes(a, deal(a)) + stats_bytes(a); }
+size_t group_norm_backward_bytes(const GroupNormCall& a)
+{
+    if (by_slabs(a, true, plan(a, true))) return aligned256((size_t)a.B * a.C * 8);
+    return parts_bytes(a, deal(a)) + stats_bytes(a);
+}
+
 
 hipError_t launch_group_norm_backward(const GroupNormCall& a, const void* dy, const void* x, const float* stats, void* dx,
                                       void* dw, void* db, void* ws, hipStream_t st)
 {
-    const Deal d = deal(a);
     float2* parts = static_cast<float2*>(ws);
+    auto join = [&](long items) {
+        if (dw || db)
+            hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinWaves * kWave), 0,
+                               st, parts, items, a.C, a.dt, dw, db);
+        return hipGetLastError();
+    };
+    const Plan p = plan(a, true);
+    if (by_slabs(a, true, p)) {
+        const long items = (long)a.B * p.s.slabs;
+        const dim3 grid((unsigned)((items + kXcds - 1) / kXcds * kXcds)), threads(p.s.threads);
+        const hipError_t e = with_slabs<2, 8>(a, p, [&](auto type, auto act, auto one, auto vpt) {
+            hipLaunchKernelGGL(
+                (slab_backward_kernel<decltype(type), decltype(act)::value, decltype(one)::value, decltype(vpt)::value>),
+                grid, threads, 0, st, a, p.s, static_cast<const uint8_t*>(dy), static_cast<const uint8_t*>(x),
+                static_cast<uint8_t*>(dx), reinterpret_cast<const float2*>(stats), dw || db ? parts : nullptr);
+            return hipGetLastError();
+        });
+        return e == hipSuccess ? join(a.B) : e;
+    }
+    const Deal d = deal(a);
     float2* means = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
     const float2* sp = reinterpret_cast<const float2*>(stats);
     const uint8_t *xp = static_cast<const uint8_t*>(x), *gp = static_cast<const uint8_t*>(dy);
@@ -505,9 +928,8 @@ hipError_t launch_group_norm_backward(const GroupNormCall& a, const void* dy, co
         hipLaunchKernelGGL((channel_sums_kernel<S, ACT>), dim3((unsigned)items, (unsigned)d.blocks), dim3(kThreads), 0, st,
                            a, d, gp, xp, sp, parts);
         hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, means);
-        if (dw || db)
-            hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinWaves * kWave), 0,
-                               st, parts, items, a.C, a.dt, dw, db);
+        const hipError_t e = join(items);
+        if (e != hipSuccess) return e;
         hipLaunchKernelGGL((input_gradient_kernel<S, ACT>), dim3((unsigned)items, (unsigned)d.blocks),
                            dim3(kThreads), 0, st, a, d, gp, xp, static_cast<uint8_t*>(dx), sp, means);
         return hipGetLastError();

@@ -74,4 +74,30 @@ __device__ __forceinline__ int wave_sum(int v)
     return v;
 }
 
+// A value plus its counterpart's by a fixed lane pattern inside 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v)
+{
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+
+// The sum of a value over 32 or 64 lanes, in every lane: exchanges inside 16 lanes (neighbour, pair,
+// half and whole mirror), then between the 16s and the 32s. No LDS: two sums of a row by LDS
+// exchanges took a third of a row's time.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v = dpp_add<0xb1>(v);   // lane ^ 1
+    v = dpp_add<0x4e>(v);   // lane ^ 2
+    v = dpp_add<0x141>(v);  // 7 - lane of 8
+    v = dpp_add<0x140>(v);  // 15 - lane of 16
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    if constexpr (LANES >= kWave) {
+        const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+    }
+    return v;
+}
+
 }  // namespace mpm
