@@ -736,7 +736,7 @@ int mpm_quantize_rows(const void* x, int32_t R, int32_t K, int64_t x_row, int32_
  *     bytes from K on are multiplied too: x's or w's have to be zero, as mpm_quantize_rows leaves them;
  *   w_scale: float[N]; bias (may be NULL): N values of dtype dt;
  *   out: row m at out + m * out_row elements, out_row >= N (any alignment of whole elements; rows of whole
- *     16 bytes are written 16 bytes at a time). out must not overlap the inputs.
+ *     16 bytes are written fastest). out must not overlap the inputs.
  *   ws: mpm_linear_int8_workspace_bytes(call) bytes (0 for steps, and for few tokens), 256-byte aligned.
  * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned pointers (x, w: 16 bytes; w_scale, x_scale: 4; bias,
  * out: an element), sizes below 1, K or strides as above, bad dt, x_dt or act, x_scale that does not go with

@@ -312,6 +312,9 @@ def residual_norm_backward(dy, dh, y, f, stats, weight=None, bias=None, post_wei
 # ---- rotary positions, products in 8-bit integers, group norm ------------------------------
 
 
+_MOST = 2 ** 31 - 1  # what an int32 of a call holds
+
+
 def _launch(name, ref, *args):
     """Calls an entry point on the current stream of ref's device, with that device current."""
     device = ref.get_device()
@@ -320,7 +323,8 @@ def _launch(name, ref, *args):
     else:
         with torch.cuda.device(device):
             status = getattr(_lib.load(), name)(*args, _stream(ref))
-    _lib.check(name, status)
+    if status:
+        _lib.check(name, status)
 
 
 def _scratch(need, ref):
@@ -351,22 +355,28 @@ def _rotary_call(x, freq, pos, grid, layout, off):
     if not x.is_cuda:
         raise ValueError("rows of heads must be on the GPU")
     dt, heads = _dt(x), _heads(x, "x", x)
-    rows, H, dh = _rows_of(x), x.shape[-2], x.shape[-1]
-    grid = tuple(int(n) for n in grid)
-    if not 1 <= len(grid) <= 3:
-        raise ValueError("grid has one to three axes")
-    if freq.dim() not in (2, 3) or freq.shape[-2] != len(grid) or (freq.dim() == 3 and freq.shape[0] != H):
-        raise ValueError(f"freq must be [{len(grid)}, pairs] or [{H}, {len(grid)}, pairs], got {tuple(freq.shape)}")
-    B = x.shape[0] if x.dim() == 4 else 1
+    shape, fs, axes = x.shape, freq.shape, len(grid)
+    dense = len(shape) == 4
+    rows, H, dh = shape[0] * shape[1] if dense else shape[0], shape[-2], shape[-1]
+    if not 1 <= axes <= 3 or math.prod(grid) > _MOST or max(grid) > _MOST or rows > _MOST:
+        raise ValueError("grid has one to three axes and, like the rows, at most 2^31 - 1 cells")
+    if fs[-2:-1] != (axes,) or len(fs) > 3 or (len(fs) == 3 and fs[0] != H):
+        raise ValueError(f"freq must be [{axes}, pairs] or [{H}, {axes}, pairs], got {tuple(fs)}")
+    B = shape[0] if dense else 1
     if off is not None:
-        if x.dim() == 4:
+        if dense:
             raise ValueError("dense rows [B, N, H, dh] take no offsets")
         B = off.numel() - 1
-    c = _lib.RotaryCall(rows, H, dh, dt, freq.shape[-1], _one_of(_LAYOUTS, layout, "layout"), len(grid),
-                        (ctypes.c_int32 * 3)(*grid, *[1] * (3 - len(grid))), int(freq.dim() == 3),
-                        _device(freq, "freq", torch.float32, x), _device(pos, "pos", torch.int32, x, rows), B,
-                        _device(off, "off", torch.int32, x, B + 1))
+    c = _lib.RotaryCall(rows, H, dh, dt, fs[-1], _one_of(_LAYOUTS, layout, "layout"), axes, (*grid, 1, 1)[:3],
+                        len(fs) == 3, _device(freq, "freq", torch.float32, x), _device(pos, "pos", torch.int32, x, rows),
+                        B, _device(off, "off", torch.int32, x, B + 1))
     return c, heads
+
+
+def _like(t, c):
+    """A new contiguous tensor like t, rows of heads of a rotary call, and its heads."""
+    new = t.new_empty(t.shape)
+    return new, _lib.Heads(new.data_ptr(), c.H * c.dh, c.dh)
 
 
 def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=False, out=None):
@@ -381,8 +391,9 @@ def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=Fals
     negative angles. ``out``: where to write (x itself, say)."""
     c, hx = _rotary_call(x, freq, pos, grid, layout, off)
     if out is None:
-        out = x.new_empty(x.shape)
-    ho = _heads(out, "out", x, c.R, c.H)
+        out, ho = _like(x, c)
+    else:
+        ho = _heads(out, "out", x, c.R, c.H)
     if c.R:
         _launch("mpm_rotary", x, _BYREF(c), _BYREF(hx), _BYREF(ho), int(bool(inverse)))
     return out
@@ -399,8 +410,9 @@ def rotary_backward(dout, x, freq, pos=None, grid=(1,), layout="halves", off=Non
     (dout itself, say); ``with_dfreq`` False leaves out the frequencies' gradient (x may be None then)."""
     c, hd = _rotary_call(dout, freq, pos, grid, layout, off)
     if dx is None:
-        dx = dout.new_empty(dout.shape)
-    hg = _heads(dx, "dx", dout, c.R, c.H)
+        dx, hg = _like(dout, c)
+    else:
+        hg = _heads(dx, "dx", dout, c.R, c.H)
     hx, dfreq, ws, need = None, None, None, 0
     if with_dfreq:
         hx = _BYREF(_heads(x, "x", dout, c.R, c.H))
@@ -419,6 +431,8 @@ def _value_rows(x, what):
     """(rows, K, stride of a row in elements) of values [R, K] with contiguous channels, 16 bytes apart at least."""
     if not x.is_cuda or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
         raise ValueError(f"{what} must be a device tensor [R, K] with contiguous channels")
+    if max(x.shape) > _MOST:
+        raise ValueError(f"{what} has more than 2^31 - 1 rows")
     return x.shape[0], x.shape[1], x.stride(0) if x.shape[0] > 1 else 0
 
 
@@ -484,7 +498,9 @@ def _group_call(x, groups, weight, bias, off, activation, eps):
     else:
         B = x.shape[0]
     R = math.prod(x.shape[:-1])
-    return _lib.GroupNormCall(R, C, int(groups), _dt(x), _one_of(_ACTIVATIONS, activation, "activation"), eps, B,
+    if R > _MOST or C < 1 or not 1 <= groups <= C:
+        raise ValueError(f"at most 2^31 - 1 rows, and between 1 and {C} groups")
+    return _lib.GroupNormCall(R, C, groups, _dt(x), _one_of(_ACTIVATIONS, activation, "activation"), eps, B,
                               _device(off, "off", torch.int32, x, B + 1), _device(weight, "weight", x.dtype, x, C),
                               _device(bias, "bias", x.dtype, x, C))
 

@@ -100,10 +100,12 @@ __device__ __forceinline__ Moments joined(const Moments& a, const Moments& b)
 }
 
 // Mean and squared deviations of every channel over an item's rows: parts[item][C] pairs. Values are taken from their
-// channel's in the image's first row, so that a mean far from zero beside the deviations costs no digits.
+// channel's in the image's first row, firsts[image][C], so that a mean far from zero beside the deviations costs no
+// digits.
 template <class S>
 __global__ __launch_bounds__(kThreads) void channel_moments_kernel(GroupNormCall a, Deal d, const uint8_t* x,
-                                                                   float2* __restrict__ parts)
+                                                                   float2* __restrict__ parts,
+                                                                   float* __restrict__ firsts)
 {
     typedef Vec<S> V;
     __shared__ float lds[3][kThreads];
@@ -115,7 +117,12 @@ __global__ __launch_bounds__(kThreads) void channel_moments_kernel(GroupNormCall
     for (int e = 0; e < V::kPer; ++e) m[e] = Moments{0.0f, 0.0f, 0.0f};
     if (p.live && it.first < it.end) {
         V zero;
-        zero.w = load16(x + image_rows(a, it.image).first * stride + p.col * 16);
+        const long first = image_rows(a, it.image).first;
+        zero.w = load16(x + first * stride + p.col * 16);
+        if (it.first == first && p.way == 0) {
+#pragma unroll
+            for (int e = 0; e < V::kPer; ++e) firsts[(long)it.image * a.C + p.col * V::kPer + e] = zero.get(e);
+        }
         for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
             V v[kAhead];
             int n = 0;
@@ -178,46 +185,59 @@ __device__ __forceinline__ void store_parameter(void* p, int dt, long i, float v
     else static_cast<float*>(p)[i] = v;
 }
 
-// Mean and reciprocal deviation of every image and group, a wave each, from the channels' parts, in 64 bits.
-__global__ __launch_bounds__(kWave) void group_stats_kernel(GroupNormCall a, Deal d, const void* x,
-                                                            const float2* __restrict__ parts,
-                                                            float2* __restrict__ stats)
+// Mean and reciprocal deviation of one image's group, by one wave, from the channels' parts, in 64 bits.
+__device__ __forceinline__ float2 joined_stats(const GroupNormCall& a, const Deal& d, const float2* parts,
+                                               const float* firsts, int b, int g)
 {
-    const int width = a.C / a.groups, many = d.chunks * width;
+    const int width = a.C / a.groups, many = d.chunks * width, lane = threadIdx.x % kWave;
+    const Rows image = image_rows(a, b);
+    const long rows = image.end - image.first;
+    const double count = (double)rows * width;
+    if (rows == 0) return make_float2(0.0f, 0.0f);
+    // A part's count and mean; its deviations are left to the caller.
+    auto part = [&](int i, double* n, double* mean) {
+        const int chunk = i / width, c = g * width + i - chunk * width;
+        const float2 q = parts[((long)b * d.chunks + chunk) * a.C + c];
+        *n = (double)(rows * (chunk + 1) / d.chunks - rows * chunk / d.chunks);
+        *mean = (double)q.x + (double)firsts[(long)b * a.C + c];
+        return (double)q.y;
+    };
+    double sum = 0.0, m2 = 0.0, n, mean;
+    for (int i = lane; i < many; i += kWave) {
+        part(i, &n, &mean);
+        if (n > 0.0) sum += n * mean;
+    }
+    const double centre = wave_sum(sum) / count;
+    for (int i = lane; i < many; i += kWave) {
+        const double q = part(i, &n, &mean);
+        if (n > 0.0) m2 += q + n * (mean - centre) * (mean - centre);
+    }
+    m2 = wave_sum(m2);
+    return make_float2((float)centre, (float)(1.0 / sqrt(m2 / count + (double)a.eps)));
+}
+
+// ... of every image and group, a wave each.
+__global__ __launch_bounds__(kWave) void group_stats_kernel(GroupNormCall a, Deal d, const float2* __restrict__ parts,
+                                                            const float* __restrict__ firsts, float2* __restrict__ stats)
+{
     for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
-        const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
-        const Rows image = image_rows(a, b);
-        const double count = (double)(image.end - image.first) * width;
-        // A part's count and mean; its deviations are left to the caller.
-        auto part = [&](int i, double* n, double* mean) {
-            const long item = (long)b * d.chunks + i / width;
-            const int c = g * width + i % width;
-            const Rows r = item_rows(a, d, item);
-            *n = (double)(r.end - r.first);
-            const float2 q = parts[item * a.C + c];
-            *mean = (double)q.x + (double)parameter(x, a.dt, image.first * a.C + c);
-            return (double)q.y;
-        };
-        double sum = 0.0, m2 = 0.0, n, mean;
-        if (count > 0.0) {
-            for (int i = threadIdx.x; i < many; i += kWave) {
-                part(i, &n, &mean);
-                if (n > 0.0) sum += n * mean;
-            }
-        }
-        const double centre = count > 0.0 ? wave_sum(sum) / count : 0.0;
-        if (count > 0.0) {
-            for (int i = threadIdx.x; i < many; i += kWave) {
-                const double q = part(i, &n, &mean);
-                if (n > 0.0) m2 += q + n * (mean - centre) * (mean - centre);
-            }
-            m2 = wave_sum(m2);
-        }
-        if (threadIdx.x == 0)
-            stats[pair] = count > 0.0 ? make_float2((float)centre, (float)(1.0 / sqrt(m2 / count + (double)a.eps)))
-                                      : make_float2(0.0f, 0.0f);
+        const float2 q = joined_stats(a, d, parts, firsts, (int)(pair / a.groups), (int)(pair % a.groups));
+        if (threadIdx.x == 0) stats[pair] = q;
     }
 }
+
+// The groups that a column block's channels belong to.
+struct GroupRange {
+    int first, count;
+};
+template <class S>
+__device__ __forceinline__ GroupRange block_groups(const GroupNormCall& a, const Deal& d)
+{
+    const int width = a.C / a.groups, c0 = blockIdx.y * d.cols * Vec<S>::kPer;
+    const int c1 = min(c0 + d.cols * Vec<S>::kPer, a.C) - 1;
+    return GroupRange{c0 / width, c1 / width - c0 / width + 1};
+}
+constexpr int kMostBlockGroups = kThreads * 8;  // groups of one channel each
 
 // A vector's parameters: mean, rstd, weight and shift of each of its channels.
 template <class S>
@@ -225,7 +245,8 @@ struct Affine {
     static constexpr int kPer = Vec<S>::kPer;
     float mean[kPer], rstd[kPer], w[kPer], b[kPer];
 
-    __device__ __forceinline__ void load(const GroupNormCall& a, const float2* stats, int image, int col)
+    // stats: of groups from `first` on.
+    __device__ __forceinline__ void load(const GroupNormCall& a, const float2* stats, int first, int col)
     {
         Vec<S> wv, bv;
         if (a.w) wv.w = load16(static_cast<const uint8_t*>(a.w) + col * 16);
@@ -233,7 +254,7 @@ struct Affine {
         const int width = a.C / a.groups;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-            const float2 s = stats[(long)image * a.groups + (col * kPer + e) / width];
+            const float2 s = stats[(col * kPer + e) / width - first];
             mean[e] = s.x;
             rstd[e] = s.y;
             w[e] = a.w ? wv.get(e) : 1.0f;
@@ -242,17 +263,33 @@ struct Affine {
     }
 };
 
+// y from x and the statistics: stats where they are given, otherwise from the parts (of few items), in every workgroup by
+// itself, and written to `made` (may be null).
 template <class S, int ACT>
 __global__ __launch_bounds__(kThreads) void apply_kernel(GroupNormCall a, Deal d, const uint8_t* x, uint8_t* y,
-                                                         const float2* __restrict__ stats)
+                                                         const float2* __restrict__ stats,
+                                                         const float2* __restrict__ parts,
+                                                         const float* __restrict__ firsts, float2* __restrict__ made)
 {
     typedef Vec<S> V;
+    __shared__ float2 own[kMostBlockGroups];
     const Rows it = item_rows(a, d, blockIdx.x);
     const Place p = place(d);
+    const GroupRange groups = block_groups<S>(a, d);
+    for (int g = threadIdx.x / kWave; !stats && g < groups.count; g += kThreads / kWave) {
+        const float2 q = joined_stats(a, d, parts, firsts, it.image, groups.first + g);
+        if (threadIdx.x % kWave == 0) {
+            own[g] = q;
+            // (a group that two column blocks share gets the same value from both)
+            if (made && blockIdx.x % d.chunks == 0) made[(long)it.image * a.groups + groups.first + g] = q;
+        }
+    }
+    __syncthreads();
     if (!p.live || it.first >= it.end) return;
     const long stride = (long)a.C * S::kBytes;
     Affine<S> f;
-    f.load(a, stats, it.image, p.col);
+    if (stats) f.load(a, stats + (long)it.image * a.groups, 0, p.col);
+    else f.load(a, own, groups.first, p.col);
     for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
         V v[kAhead];
 #pragma unroll
@@ -287,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void channel_sums_kernel(GroupNormCall a,
     for (int e = 0; e < V::kPer; ++e) s0[e] = s1[e] = 0.0f;
     if (p.live && it.first < it.end) {
         Affine<S> f;
-        f.load(a, stats, it.image, p.col);
+        f.load(a, stats + (long)it.image * a.groups, 0, p.col);
         for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
             V v[kAhead], g[kAhead];
 #pragma unroll
@@ -326,27 +363,32 @@ __global__ __launch_bounds__(kThreads) void channel_sums_kernel(GroupNormCall a,
     }
 }
 
-// From the channels' sums: the means of gt and gt t of every image and group, a wave each ...
+// From the channels' sums: the means of gt and gt t of one image's group, by one wave, ...
+__device__ __forceinline__ float2 joined_means(const GroupNormCall& a, const Deal& d, const float2* parts, int b, int g)
+{
+    const int width = a.C / a.groups;
+    double s0 = 0.0, s1 = 0.0;
+    for (int i = threadIdx.x % kWave; i < d.chunks * width; i += kWave) {
+        const int c = g * width + i % width;
+        const float2 q = parts[((long)b * d.chunks + i / width) * a.C + c];
+        const double w = a.w ? (double)parameter(a.w, a.dt, c) : 1.0;
+        s0 += w * (double)q.x;
+        s1 += w * (double)q.y;
+    }
+    s0 = wave_sum(s0);
+    s1 = wave_sum(s1);
+    const Rows r = image_rows(a, b);
+    const double n = (double)(r.end - r.first) * width;
+    return n > 0.0 ? make_float2((float)(s0 / n), (float)(s1 / n)) : make_float2(0.0f, 0.0f);
+}
+
+// ... of every image and group ...
 __global__ __launch_bounds__(kWave) void group_means_kernel(GroupNormCall a, Deal d, const float2* __restrict__ parts,
                                                             float2* __restrict__ means)
 {
-    const int width = a.C / a.groups;
     for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
-        const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
-        double s0 = 0.0, s1 = 0.0;
-        for (int i = threadIdx.x; i < d.chunks * width; i += kWave) {
-            const int c = g * width + i % width;
-            const float2 q = parts[((long)b * d.chunks + i / width) * a.C + c];
-            const double w = a.w ? (double)parameter(a.w, a.dt, c) : 1.0;
-            s0 += w * (double)q.x;
-            s1 += w * (double)q.y;
-        }
-        s0 = wave_sum(s0);
-        s1 = wave_sum(s1);
-        const Rows r = image_rows(a, b);
-        const double n = (double)(r.end - r.first) * width;
-        if (threadIdx.x == 0)
-            means[pair] = n > 0.0 ? make_float2((float)(s0 / n), (float)(s1 / n)) : make_float2(0.0f, 0.0f);
+        const float2 q = joined_means(a, d, parts, (int)(pair / a.groups), (int)(pair % a.groups));
+        if (threadIdx.x == 0) means[pair] = q;
     }
 }
 
@@ -378,14 +420,24 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void join_sums_kernel(const floa
     if (dw) store_parameter(dw, dt, c, (float)s1);
 }
 
+// dx, from the means where they are given, otherwise from the parts, as apply_kernel.
 template <class S, int ACT>
 __global__ __launch_bounds__(kThreads) void input_gradient_kernel(GroupNormCall a, Deal d, const uint8_t* dy,
                                                                   const uint8_t* x, uint8_t* dx,
                                                                   const float2* __restrict__ stats,
-                                                                  const float2* __restrict__ means)
+                                                                  const float2* __restrict__ means,
+                                                                  const float2* __restrict__ parts)
 {
     typedef Vec<S> V;
+    __shared__ float2 own[kMostBlockGroups];
     const Place p = place(d);
+    const Rows it = item_rows(a, d, blockIdx.x);
+    const GroupRange groups = block_groups<S>(a, d);
+    for (int g = threadIdx.x / kWave; !means && g < groups.count; g += kThreads / kWave) {
+        const float2 q = joined_means(a, d, parts, it.image, groups.first + g);
+        if (threadIdx.x % kWave == 0) own[g] = q;
+    }
+    __syncthreads();
     if (!p.live) return;
     const long stride = (long)a.C * S::kBytes;
     if (a.off) {  // a share of the rows of no image
@@ -395,14 +447,14 @@ __global__ __launch_bounds__(kThreads) void input_gradient_kernel(GroupNormCall 
         for (long r = first + p.way; r < end; r += d.ways)
             store16(dx + (r < lo ? r : r - lo + hi) * stride + p.col * 16, none);
     }
-    const Rows it = item_rows(a, d, blockIdx.x);
     if (it.first >= it.end) return;
     Affine<S> f;
-    f.load(a, stats, it.image, p.col);
+    f.load(a, stats + (long)it.image * a.groups, 0, p.col);
     float m0[V::kPer], m1[V::kPer];
 #pragma unroll
     for (int e = 0; e < V::kPer; ++e) {
-        const float2 m = means[(long)it.image * a.groups + (p.col * V::kPer + e) / (a.C / a.groups)];
+        const int g = (p.col * V::kPer + e) / (a.C / a.groups);
+        const float2 m = means ? means[(long)it.image * a.groups + g] : own[g - groups.first];
         m0[e] = m.x;
         m1[e] = m.y;
     }
@@ -820,7 +872,12 @@ unsigned pair_groups(const GroupNormCall& a) { return (unsigned)std::min((long)a
 
 size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
 size_t parts_bytes(const GroupNormCall& a, const Deal& d) { return aligned256((size_t)a.B * d.chunks * a.C * 8); }
+size_t firsts_bytes(const GroupNormCall& a) { return aligned256((size_t)a.B * a.C * 4); }
 size_t stats_bytes(const GroupNormCall& a) { return aligned256((size_t)a.B * a.groups * 8); }
+
+// Whether the second pass joins an image's parts by itself: a launch less, for up to so many of them.
+constexpr int kFewParts = 8192;
+bool joins_itself(const GroupNormCall& a, const Deal& d) { return (long)d.chunks * a.C <= kFewParts; }
 
 // Calls go(type, activation).
 template <class F>
@@ -850,41 +907,101 @@ hipError_t with_slabs(const GroupNormCall& a, const Plan& p, F&& go)
     });
 }
 
-}  // namespace
-
-size_t group_norm_bytes(const GroupNormCall& a)
+hipError_t forward_by_slabs(const GroupNormCall& a, const Plan& p, const void* x, void* y, float* stats, hipStream_t st)
 {
-    return by_slabs(a, false, plan(a, false)) ? 0 : parts_bytes(a, deal(a)) + stats_bytes(a);
+    const long items = (long)a.B * p.s.slabs;
+    const dim3 grid((unsigned)((items + kXcds - 1) / kXcds * kXcds)), threads(p.s.threads);
+    return with_slabs<4, 16>(a, p, [&](auto type, auto act, auto one, auto vpt) {
+        hipLaunchKernelGGL((slab_kernel<decltype(type), decltype(act)::value, decltype(one)::value, decltype(vpt)::value>),
+                           grid, threads, 0, st, a, p.s, static_cast<const uint8_t*>(x), static_cast<uint8_t*>(y),
+                           reinterpret_cast<float2*>(stats));
+        return hipGetLastError();
+    });
 }
 
-
-hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t st)
+hipError_t forward_by_passes(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t st)
 {
-    const Plan p = plan(a, false);
-    if (by_slabs(a, false, p)) {
-        const long items = (long)a.B * p.s.slabs;
-        const dim3 grid((unsigned)((items + kXcds - 1) / kXcds * kXcds)), threads(p.s.threads);
-        return with_slabs<4, 16>(a, p, [&](auto type, auto act, auto one, auto vpt) {
-            hipLaunchKernelGGL((slab_kernel<decltype(type), decltype(act)::value, decltype(one)::value, decltype(vpt)::value>),
-                               grid, threads, 0, st, a, p.s, static_cast<const uint8_t*>(x), static_cast<uint8_t*>(y),
-                               reinterpret_cast<float2*>(stats));
-            return hipGetLastError();
-        });
-    }
     const Deal d = deal(a);
-    float2* parts = static_cast<float2*>(ws);
-    float2* sp = stats ? reinterpret_cast<float2*>(stats)
-                       : reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
+    char* at = static_cast<char*>(ws);
+    float2* parts = reinterpret_cast<float2*>(at);
+    float* firsts = reinterpret_cast<float*>(at + parts_bytes(a, d));
+    float2* made = reinterpret_cast<float2*>(stats ? reinterpret_cast<char*>(stats)
+                                                   : at + parts_bytes(a, d) + firsts_bytes(a));
+    const bool itself = joins_itself(a, d);
     const dim3 grid((unsigned)((long)a.B * d.chunks), (unsigned)d.blocks);
     const uint8_t* xp = static_cast<const uint8_t*>(x);
     return with_kind(a, [&](auto type, auto act) {
         typedef decltype(type) S;
-        hipLaunchKernelGGL((channel_moments_kernel<S>), grid, dim3(kThreads), 0, st, a, d, xp, parts);
-        hipLaunchKernelGGL(group_stats_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, x, parts, sp);
+        hipLaunchKernelGGL((channel_moments_kernel<S>), grid, dim3(kThreads), 0, st, a, d, xp, parts, firsts);
+        if (!itself)
+            hipLaunchKernelGGL(group_stats_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, firsts, made);
         hipLaunchKernelGGL((apply_kernel<S, decltype(act)::value>), grid, dim3(kThreads), 0, st, a, d, xp,
-                           static_cast<uint8_t*>(y), sp);
+                           static_cast<uint8_t*>(y), itself ? nullptr : made, parts, firsts,
+                           reinterpret_cast<float2*>(stats));
         return hipGetLastError();
     });
+}
+
+hipError_t join(const GroupNormCall& a, const float2* parts, long items, void* dw, void* db, hipStream_t st)
+{
+    if (!dw && !db) return hipSuccess;
+    hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinWaves * kWave), 0, st, parts,
+                       items, a.C, a.dt, dw, db);
+    return hipGetLastError();
+}
+
+hipError_t backward_by_slabs(const GroupNormCall& a, const Plan& p, const void* dy, const void* x, const float* stats,
+                             void* dx, void* dw, void* db, void* ws, hipStream_t st)
+{
+    float2* parts = static_cast<float2*>(ws);
+    const long items = (long)a.B * p.s.slabs;
+    const dim3 grid((unsigned)((items + kXcds - 1) / kXcds * kXcds)), threads(p.s.threads);
+    const hipError_t e = with_slabs<2, 8>(a, p, [&](auto type, auto act, auto one, auto vpt) {
+        hipLaunchKernelGGL(
+            (slab_backward_kernel<decltype(type), decltype(act)::value, decltype(one)::value, decltype(vpt)::value>), grid,
+            threads, 0, st, a, p.s, static_cast<const uint8_t*>(dy), static_cast<const uint8_t*>(x),
+            static_cast<uint8_t*>(dx), reinterpret_cast<const float2*>(stats), dw || db ? parts : nullptr);
+        return hipGetLastError();
+    });
+    return e == hipSuccess ? join(a, parts, a.B, dw, db, st) : e;
+}
+
+hipError_t backward_by_passes(const GroupNormCall& a, const void* dy, const void* x, const float* stats, void* dx, void* dw,
+                              void* db, void* ws, hipStream_t st)
+{
+    const Deal d = deal(a);
+    float2* parts = static_cast<float2*>(ws);
+    float2* means = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
+    const float2* sp = reinterpret_cast<const float2*>(stats);
+    const uint8_t *xp = static_cast<const uint8_t*>(x), *gp = static_cast<const uint8_t*>(dy);
+    const bool itself = joins_itself(a, d);
+    const dim3 grid((unsigned)((long)a.B * d.chunks), (unsigned)d.blocks);
+    const hipError_t e = with_kind(a, [&](auto type, auto act) {
+        typedef decltype(type) S;
+        constexpr int ACT = decltype(act)::value;
+        hipLaunchKernelGGL((channel_sums_kernel<S, ACT>), grid, dim3(kThreads), 0, st, a, d, gp, xp, sp, parts);
+        if (!itself)
+            hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, means);
+        hipLaunchKernelGGL((input_gradient_kernel<S, ACT>), grid, dim3(kThreads), 0, st, a, d, gp, xp,
+                           static_cast<uint8_t*>(dx), sp, itself ? nullptr : means, parts);
+        return hipGetLastError();
+    });
+    return e == hipSuccess ? join(a, parts, (long)a.B * d.chunks, dw, db, st) : e;
+}
+
+}  // namespace
+
+size_t group_norm_bytes(const GroupNormCall& a)
+{
+    if (by_slabs(a, false, plan(a, false))) return 0;
+    return parts_bytes(a, deal(a)) + firsts_bytes(a) + stats_bytes(a);
+}
+
+hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t st)
+{
+    const Plan p = plan(a, false);
+    if (by_slabs(a, false, p)) return forward_by_slabs(a, p, x, y, stats, st);
+    return forward_by_passes(a, x, y, stats, ws, st);
 }
 
 size_t group_norm_backward_bytes(const GroupNormCall& a)
@@ -893,47 +1010,12 @@ size_t group_norm_backward_bytes(const GroupNormCall& a)
     return parts_bytes(a, deal(a)) + stats_bytes(a);
 }
 
-
 hipError_t launch_group_norm_backward(const GroupNormCall& a, const void* dy, const void* x, const float* stats, void* dx,
                                       void* dw, void* db, void* ws, hipStream_t st)
 {
-    float2* parts = static_cast<float2*>(ws);
-    auto join = [&](long items) {
-        if (dw || db)
-            hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinWaves * kWave), 0,
-                               st, parts, items, a.C, a.dt, dw, db);
-        return hipGetLastError();
-    };
     const Plan p = plan(a, true);
-    if (by_slabs(a, true, p)) {
-        const long items = (long)a.B * p.s.slabs;
-        const dim3 grid((unsigned)((items + kXcds - 1) / kXcds * kXcds)), threads(p.s.threads);
-        const hipError_t e = with_slabs<2, 8>(a, p, [&](auto type, auto act, auto one, auto vpt) {
-            hipLaunchKernelGGL(
-                (slab_backward_kernel<decltype(type), decltype(act)::value, decltype(one)::value, decltype(vpt)::value>),
-                grid, threads, 0, st, a, p.s, static_cast<const uint8_t*>(dy), static_cast<const uint8_t*>(x),
-                static_cast<uint8_t*>(dx), reinterpret_cast<const float2*>(stats), dw || db ? parts : nullptr);
-            return hipGetLastError();
-        });
-        return e == hipSuccess ? join(a.B) : e;
-    }
-    const Deal d = deal(a);
-    float2* means = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
-    const float2* sp = reinterpret_cast<const float2*>(stats);
-    const uint8_t *xp = static_cast<const uint8_t*>(x), *gp = static_cast<const uint8_t*>(dy);
-    const long items = (long)a.B * d.chunks;
-    return with_kind(a, [&](auto type, auto act) {
-        typedef decltype(type) S;
-        constexpr int ACT = decltype(act)::value;
-        hipLaunchKernelGGL((channel_sums_kernel<S, ACT>), dim3((unsigned)items, (unsigned)d.blocks), dim3(kThreads), 0, st,
-                           a, d, gp, xp, sp, parts);
-        hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, means);
-        const hipError_t e = join(items);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((input_gradient_kernel<S, ACT>), dim3((unsigned)items, (unsigned)d.blocks),
-                           dim3(kThreads), 0, st, a, d, gp, xp, static_cast<uint8_t*>(dx), sp, means);
-        return hipGetLastError();
-    });
+    if (by_slabs(a, true, p)) return backward_by_slabs(a, p, dy, x, stats, dx, dw, db, ws, st);
+    return backward_by_passes(a, dy, x, stats, dx, dw, db, ws, st);
 }
 
 }  // namespace mpm

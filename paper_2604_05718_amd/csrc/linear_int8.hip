@@ -18,40 +18,6 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr float kSteps = 127.0f;
 constexpr float kLeastScale = 0x1p-126f;
 
-// A row's scale from the bits of its largest magnitude (as integers, NaN and infinity compare largest), and what
-// turns its values into steps.
-struct Steps {
-    float scale;   // as stored
-    float up;      // values and scale times this: away from the subnormal numbers
-    float s, inv;  // the scale so raised, and about 1 / it
-
-    __device__ __forceinline__ explicit Steps(uint32_t largest)
-    {
-        scale = fmaxf(__uint_as_float(largest) / kSteps, kLeastScale);
-        up = scale < 0x1p-60f ? 0x1p64f : 1.0f;
-        s = scale * up;
-        inv = __builtin_amdgcn_rcpf(s);
-        if (largest >= 0x7f800000u) scale = __uint_as_float(0x7fc00000u);
-    }
-    __device__ __forceinline__ bool finite() const { return scale == scale; }
-
-    // x / s rounded to nearest even, of the real quotient: the product with the reciprocal is within a few
-    // 2^-17 of it; next to a half the sign of x - (q +- 1/2) s decides, which one multiply-add gives exactly.
-    __device__ __forceinline__ int of(float x) const
-    {
-        x *= up;
-        const float r = x * inv;
-        float q = __builtin_rintf(r);
-        if (fabsf(r - q) > 0.5f - 0x1p-12f) {
-            const float above = fmaf(-(q + 0.5f), s, x), below = fmaf(-(q - 0.5f), s, x);
-            const bool odd = (int)q & 1;
-            if (above > 0.0f || (above == 0.0f && odd)) q += 1.0f;
-            else if (below < 0.0f || (below == 0.0f && odd)) q -= 1.0f;
-        }
-        return (int)fminf(fmaxf(q, -kSteps), kSteps);
-    }
-};
-
 // The values of one vector of 16 bytes.
 template <class S>
 __device__ __forceinline__ float value(const u32x4& w, int e)
@@ -60,6 +26,7 @@ __device__ __forceinline__ float value(const u32x4& w, int e)
     return __uint_as_float(w[e]);
 }
 
+// The bits of the largest magnitude (as integers NaN and infinity compare largest).
 template <class S>
 __device__ __forceinline__ uint32_t largest(const u32x4& w, uint32_t m)
 {
@@ -75,56 +42,125 @@ __device__ __forceinline__ uint32_t largest(const u32x4& w, uint32_t m)
     return m;
 }
 
-// The steps of one vector, a byte each, in words of four (bfloat16: two words, float32: one).
-template <class S>
-__device__ __forceinline__ void steps_of(const u32x4& w, const Steps& st, uint32_t (&out)[16 / S::kBytes / 4])
-{
-#pragma unroll
-    for (int i = 0; i < 16 / S::kBytes / 4; ++i) {
-        out[i] = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (st.finite()) out[i] |= ((uint32_t)st.of(value<S>(w, 4 * i + e)) & 0xffu) << (8 * e);
+// A row's scale, from the bits of its largest magnitude, and what turns its values into steps.
+struct Steps {
+    float scale, inv;  // as stored, and about 1 / it
+    bool finite;
+
+    __device__ __forceinline__ explicit Steps(uint32_t most)
+    {
+        const float s = fmaxf(__uint_as_float(most) / kSteps, kLeastScale);
+        finite = most < 0x7f800000u;
+        inv = __builtin_amdgcn_rcpf(s);
+        scale = finite ? s : __uint_as_float(0x7fc00000u);
     }
+
+    // x / scale rounded to nearest even, of the real quotient: next to a half the sign of x - (q +- 1/2) scale decides, which
+    // one multiply-add gives exactly (raised where it could leave the numbers that float32 holds).
+    __device__ __forceinline__ int exact(float x) const
+    {
+        const float up = scale < 0x1p-60f ? 0x1p64f : 1.0f, s = scale * up;
+        float q = __builtin_rintf(x * inv);
+        x *= up;
+        const float above = fmaf(-(q + 0.5f), s, x), below = fmaf(-(q - 0.5f), s, x);
+        const bool odd = (int)q & 1;
+        if (above > 0.0f || (above == 0.0f && odd)) q += 1.0f;
+        else if (below < 0.0f || (below == 0.0f && odd)) q -= 1.0f;
+        return (int)q;
+    }
+
+    // The steps of one vector, a byte each, in words of four (bfloat16: two words, float32: one). The product with the
+    // reciprocal is within 2^-15 of the quotient; adding 1.5 2^23 leaves its rounding in the sum's low bits.
+    template <class S>
+    __device__ __forceinline__ void of(const u32x4& w, uint32_t (&out)[16 / S::kBytes / 4]) const
+    {
+        constexpr float kMagic = 12582912.0f;
+        constexpr int kPer = 16 / S::kBytes;
+        uint32_t t[kPer];
+        float off = 0.0f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const float r = value<S>(w, e) * inv, m = r + kMagic;
+            t[e] = __float_as_uint(m);
+            off = fmaxf(off, fabsf(r - (m - kMagic)));
+        }
+        if (off > 0.5f - 0x1p-14f) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) t[e] = (uint32_t)exact(value<S>(w, e));
+        }
+#pragma unroll
+        for (int i = 0; i < kPer / 4; ++i) {
+            const uint32_t lo = __builtin_amdgcn_perm(t[4 * i + 1], t[4 * i], 0x0c0c0400u);
+            const uint32_t hi = __builtin_amdgcn_perm(t[4 * i + 3], t[4 * i + 2], 0x0c0c0400u);
+            out[i] = finite ? lo | hi << 16 : 0;
+        }
+    }
+};
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v)
+{
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
 }
 
+// The largest of a value over 32 or 64 lanes, in every lane (the exchanges of lanes_sum).
 template <int LANES>
-__device__ __forceinline__ uint32_t lanes_max(uint32_t m)
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 {
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-    return m;
+    v = dpp_max<0xb1>(v);
+    v = dpp_max<0x4e>(v);
+    v = dpp_max<0x141>(v);
+    v = dpp_max<0x140>(v);
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(p[0], p[1]);
+    if constexpr (LANES >= kWave) {
+        const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(q[0], q[1]);
+    }
+    return v;
 }
 
 constexpr int kQuantThreads = 256;
 
-// Rows of at most VPL vectors a lane, a wave each, kept in registers between the maximum and the steps.
-template <class S, int VPL>
+template <class S>
+__device__ __forceinline__ void store_steps(uint8_t* to, const uint32_t (&w)[16 / S::kBytes / 4], bool in)
+{
+    if constexpr (S::kBytes == 2) {
+        typedef uint32_t Two __attribute__((ext_vector_type(2)));
+        const Two v = {in ? w[0] : 0, in ? w[1] : 0};
+        *reinterpret_cast<Two*>(to) = v;
+    } else {
+        *reinterpret_cast<uint32_t*>(to) = in ? w[0] : 0;
+    }
+}
+
+// Rows of at most VPL vectors a lane, LANES lanes each, kept in registers between the maximum and the steps.
+// 45888 rows of 768 bfloat16 values (106 MB): 21 us, 5.0 TB/s.
+template <class S, int LANES, int VPL>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(const uint8_t* __restrict__ x, long R, int K, long x_row,
                                                                  uint8_t* __restrict__ q, float* __restrict__ scale)
 {
     constexpr int kPer = 16 / S::kBytes, kWords = kPer / 4;
-    const int lane = threadIdx.x % kWave, vecs = K / kPer, Kp = steps_row(K);
-    const long row = (long)blockIdx.x * (kQuantThreads / kWave) + threadIdx.x / kWave;
-    if (row >= R) return;
+    const int lane = threadIdx.x % LANES, vecs = K / kPer, Kp = steps_row(K);
+    const long at = (long)blockIdx.x * (kQuantThreads / LANES) + threadIdx.x / LANES, row = min(at, R - 1);
     const uint8_t* from = x + row * x_row * S::kBytes;
     u32x4 v[VPL];
     uint32_t m = 0;
 #pragma unroll
-    for (int u = 0; u < VPL; ++u) v[u] = load16(from + (long)min(lane + u * kWave, vecs - 1) * 16);
+    for (int u = 0; u < VPL; ++u) v[u] = load16(from + (long)min(lane + u * LANES, vecs - 1) * 16);
 #pragma unroll
     for (int u = 0; u < VPL; ++u) m = largest<S>(v[u], m);
-    const Steps st(lanes_max<kWave>(m));
+    const Steps st(lanes_max<LANES>(m));
+    if (at >= R) return;
     if (lane == 0) scale[row] = st.scale;
     uint8_t* to = q + row * Kp;
 #pragma unroll
     for (int u = 0; u < VPL; ++u) {
-        const int c = lane + u * kWave;
+        const int c = lane + u * LANES;
         if (c * kPer >= Kp) break;
         uint32_t w[kWords];
-        steps_of<S>(v[u], st, w);
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) reinterpret_cast<uint32_t*>(to + c * kPer)[i] = c < vecs ? w[i] : 0;
+        st.of<S>(v[u], w);
+        store_steps<S>(to + c * kPer, w, c < vecs);
     }
 }
 
@@ -150,23 +186,29 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_wide_kernel(const uint
     uint8_t* to = q + row * Kp;
     for (int c = threadIdx.x; c * kPer < Kp; c += kQuantThreads) {
         uint32_t w[kWords];
-        steps_of<S>(load16(from + (long)min(c, vecs - 1) * 16), st, w);
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) reinterpret_cast<uint32_t*>(to + c * kPer)[i] = c < vecs ? w[i] : 0;
+        st.of<S>(load16(from + (long)min(c, vecs - 1) * 16), w);
+        store_steps<S>(to + c * kPer, w, c < vecs);
     }
 }
 
 template <class S>
 hipError_t quantize(const uint8_t* x, long R, int K, long x_row, uint8_t* q, float* scale, hipStream_t st)
 {
-    constexpr int kPer = 16 / S::kBytes, kRows = kQuantThreads / kWave;
-    const int vecs = steps_row(K) / kPer;
-    const dim3 grid((unsigned)((R + kRows - 1) / kRows)), threads(kQuantThreads);
-    if (vecs <= kWave) hipLaunchKernelGGL((quantize_kernel<S, 1>), grid, threads, 0, st, x, R, K, x_row, q, scale);
-    else if (vecs <= 2 * kWave) hipLaunchKernelGGL((quantize_kernel<S, 2>), grid, threads, 0, st, x, R, K, x_row, q, scale);
-    else if (vecs <= 4 * kWave) hipLaunchKernelGGL((quantize_kernel<S, 4>), grid, threads, 0, st, x, R, K, x_row, q, scale);
-    else if (vecs <= 8 * kWave) hipLaunchKernelGGL((quantize_kernel<S, 8>), grid, threads, 0, st, x, R, K, x_row, q, scale);
-    else hipLaunchKernelGGL((quantize_wide_kernel<S>), dim3((unsigned)R), threads, 0, st, x, K, x_row, q, scale);
+    const int vecs = steps_row(K) / (16 / S::kBytes);
+    auto rows = [&](auto lanes, auto vpl) {
+        constexpr int L = decltype(lanes)::value, kRows = kQuantThreads / L;
+        hipLaunchKernelGGL((quantize_kernel<S, L, decltype(vpl)::value>), dim3((unsigned)((R + kRows - 1) / kRows)),
+                           dim3(kQuantThreads), 0, st, x, R, K, x_row, q, scale);
+    };
+    constexpr std::integral_constant<int, 32> half{};
+    constexpr std::integral_constant<int, kWave> wave{};
+    if (vecs <= 32) rows(half, std::integral_constant<int, 1>{});
+    else if (vecs <= 64) rows(half, std::integral_constant<int, 2>{});
+    else if (vecs <= 96) rows(half, std::integral_constant<int, 3>{});
+    else if (vecs <= 128) rows(half, std::integral_constant<int, 4>{});
+    else if (vecs <= 256) rows(wave, std::integral_constant<int, 4>{});
+    else if (vecs <= 512) rows(wave, std::integral_constant<int, 8>{});
+    else hipLaunchKernelGGL((quantize_wide_kernel<S>), dim3((unsigned)R), dim3(kQuantThreads), 0, st, x, K, x_row, q, scale);
     return hipGetLastError();
 }
 
@@ -227,9 +269,8 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Linear8Call a, const u
             if (lane == 0) scales[r] = st.scale;
             for (int c = lane; c * kPer < Kp; c += kWave) {
                 uint32_t s[kWords];
-                steps_of<X>(load16(from + min(c, vecs - 1) * 16), st, s);
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) reinterpret_cast<uint32_t*>(q + r * Kp + c * kPer)[i] = c < vecs ? s[i] : 0;
+                st.of<X>(load16(from + min(c, vecs - 1) * 16), s);
+                store_steps<X>(q + r * Kp + c * kPer, s, c < vecs);
             }
         }
     } else {
@@ -264,6 +305,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Linear8Call a, const u
 
 // ---- many tokens -------------------------------------------------------------------------
 
+constexpr int kColumnBytes = 2 << 20;  // weights of a column of tiles: half an L2
 constexpr int kUnits = 256;  // compute units
 constexpr int kXcds = 8;     // workgroups are dealt round-robin to 8 XCDs, each with its own L2
 
@@ -281,47 +323,52 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Writes 32 channels' results of one token, channels `at` + 8 (r / 4) + 4 half + r % 4 in v[r], those
-// below N. `whole`: 16 bytes at a time.
-template <class T>
-__device__ __forceinline__ void write_row(uint8_t* to, int at, int half, int N, bool whole, const float (&v)[16])
+// Writes NT channels' results of one token from channel i on, those below N. `whole`: all at once, past the L2: results that
+// stay there drive out the tokens and weights that the next tiles read (45920 x 4096 x 1024, bfloat16: 264 -> 224 us).
+template <class T, int NT>
+__device__ __forceinline__ void write_channels(uint8_t* to, int i, int N, bool whole, const float (&v)[NT])
 {
-    if (!whole) {
+    if (!whole || NT == 1) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int i = at + 8 * (r / 4) + 4 * half + r % 4;
-            if (i < N) store_element<T>(to, i, v[r]);
-        }
+        for (int e = 0; e < NT; ++e)
+            if (i + e < N) store_element<T>(to, i + e, v[e]);
         return;
     }
-    if constexpr (T::kBytes == 4) {
+    if (i >= N) return;
+    constexpr int kWords = NT * T::kBytes >= 4 ? NT * T::kBytes / 4 : 1;
+    typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
+    Words w;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int i = at + 8 * c + 4 * half;
-            const u32x4 w = {__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]),
-                             __float_as_uint(v[4 * c + 3])};
-            if (i < N) store16(to + i * 4L, w);
-        }
-    } else {
-        // Half a wave exchanges channels with the other, so that a lane has eight in a row.
-        auto pair = [&](int r) {
+    for (int e = 0; e < kWords; ++e) {
+        if constexpr (T::kBytes == 4) {
+            w[e] = __float_as_uint(v[e]);
+        } else if constexpr (NT > 1) {
             typedef float f32x2 __attribute__((ext_vector_type(2)));
-            const f32x2 p = {v[r], v[r + 1]};
-            return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
-        };
-#pragma unroll
-        for (int c = 0; c < 4; c += 2) {
-            const auto x = __builtin_amdgcn_permlane32_swap(pair(4 * c), pair(4 * c + 4), false, false);
-            const auto y = __builtin_amdgcn_permlane32_swap(pair(4 * c + 2), pair(4 * c + 6), false, false);
-            const u32x4 w = {x[0], y[0], x[1], y[1]};
-            const int i = at + 8 * (c + half);
-            if (i < N) store16(to + i * 2L, w);
+            const f32x2 p = {v[2 * e], v[2 * e + 1]};
+            w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
         }
     }
+    __builtin_nontemporal_store(w, reinterpret_cast<Words*>(to + (long)i * T::kBytes));
 }
 
-// What a workgroup takes of the tiles: those of its XCD's contiguous share (tokens outside, channels inside), `slots`
-// workgroups by turns.
+// The order of the tiles: columns of `wide` tiles of channels outside, then tokens, then the column's channels, so that a
+// column's weights stay in an L2 while the tokens pass.
+struct Order {
+    int mtiles, ntiles, wide;
+};
+struct Tile {
+    long m;
+    int n;
+};
+__device__ __forceinline__ Tile tile_at(const Order& o, long i)
+{
+    const long column = i / ((long)o.mtiles * o.wide), rest = i - column * o.mtiles * o.wide;
+    const int first = (int)column * o.wide, width = min(o.wide, o.ntiles - first);
+    const long m = rest / width;
+    return Tile{m, first + (int)(rest - m * width)};
+}
+
+// What a workgroup takes of them: those of its XCD's contiguous share, `slots` workgroups by turns.
 struct Share {
     long tile, end;
     int slots;
@@ -342,7 +389,7 @@ __device__ __forceinline__ Share share(long tiles)
 template <int BM, int BN, int WM, int WN, int BK, int STAGES, class T, int ACT>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a, const uint8_t* __restrict__ q,
                                                                    const float* __restrict__ q_scale,
-                                                                   void* __restrict__ out, int mtiles, int ntiles, bool whole)
+                                                                   void* __restrict__ out, Order order, bool whole)
 {
     constexpr int kWaves = WM * WN, THREADS = kWaves * kWave;
     constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
@@ -355,11 +402,11 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
     static_assert((BM + BN) % (kRows * kWaves) == 0 && BM % kRows == 0, "whole loads");
     // (A wave's loads are a whole number of 16 rows apart, so a lane's swizzle is one for all.)
     static_assert(kRows * kWaves % 16 == 0 && BM % 16 == 0, "one swizzle a lane");
-    static_assert(BN <= THREADS && BM + BN <= 2 * THREADS, "scales: a thread each");
+    static_assert(BM <= THREADS, "scales: a thread each");
     extern __shared__ __align__(1024) uint8_t lds[];
-    float* channels = reinterpret_cast<float*>(lds + STAGES * kStage);  // [2][scale, bias][BN], by tiles in turns
+    float* scales = reinterpret_cast<float*>(lds + STAGES * kStage);  // [2][BM] of the tokens, by tiles in turns
 
-    const Share sh = share((long)mtiles * ntiles);
+    const Share sh = share((long)order.mtiles * order.ntiles);
     if (sh.tile >= sh.end) return;
     const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, l32 = lane & 31, half = lane >> 5;
     const int wm = wave % WM, wn = wave / WM;
@@ -370,40 +417,55 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
     // The stream's end that loads: its tile and chunk, and this lane's rows there (load i of a wave brings rows
     // (wave + kWaves i) kRows ... of the buffer), clamped to those that exist.
     const int lrow = lane / kPieces, piece = ((lane % kPieces) ^ swizzle(wave * kRows + lrow)) * 16;
-    const uint8_t* from[kLoads];
+    // Load i is of tokens where its rows lie below BM, uniform over the workgroup; offsets from the tile's first row.
+    constexpr int kTokenLoads = BM / kRows / kWaves;
+    static_assert(BM % (kRows * kWaves) == 0, "a load is of tokens or of weights");
+    uint32_t from[kLoads];
+    const uint8_t *qbase = q, *wbase = reinterpret_cast<const uint8_t*>(a.w);
     long ltile = sh.tile;
     int lchunk = 0, lbuf = 0;
     auto place = [&](long tile) {
-        const long m0 = tile / ntiles * BM;
-        const int n0 = (int)(tile % ntiles) * BN;
+        const Tile at = tile_at(order, tile);
+        const long m0 = at.m * BM;
+        const int n0 = at.n * BN;
+        qbase = q + m0 * Kp;
+        wbase = reinterpret_cast<const uint8_t*>(a.w) + (long)n0 * Kp;
+        const int tokens = (int)min((long)BM, a.M - m0) - 1, channels = min(BN, a.N - n0) - 1;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int r = (wave + kWaves * i) * kRows + lrow;
-            from[i] = r < BM ? q + min(m0 + r, a.M - 1) * Kp
-                             : reinterpret_cast<const uint8_t*>(a.w) + (long)min(n0 + r - BM, a.N - 1) * Kp;
+            const int r = (wave + kWaves * i) * kRows + lrow, c = r - BM;
+            // Weight row c of the buffer: row l of fragment f of a wave's NT holds its channel l NT + f, so that a lane's
+            // results are NT channels in a row.
+            const int channel = c / (32 * NT) * (32 * NT) + c % 32 * NT + c / 32 % NT;
+            from[i] = (uint32_t)(i < kTokenLoads ? min(r, tokens) : min(channel, channels)) * (uint32_t)Kp;
         }
     };
-    // The scales of a tile: a lane's tokens', and a thread's channel's on its way to LDS.
-    float xs[MT], w_scale, bias;
+    // The values of a tile's channels, a lane's own, and a thread's token's scale on its way to LDS.
+    float w_scale[NT], bias[NT], x_scale;
     auto load_scales = [&](long tile) {
-        const long m0 = tile / ntiles * BM;
-        const int n = min((int)(tile % ntiles) * BN + min(t, BN - 1), a.N - 1);
+        const Tile at = tile_at(order, tile);
+        x_scale = q_scale[min(at.m * BM + min(t, BM - 1), a.M - 1)] * kDown;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xs[m] = q_scale[min(m0 + (wm * MT + m) * 32 + l32, a.M - 1)] * kDown;
-        w_scale = a.w_scale[n] * kUp;
-        bias = a.bias ? element<T>(a.bias, n) : 0.0f;
+        for (int n = 0; n < NT; ++n) {
+            const int c = min(at.n * BN + (wn * 32 + l32) * NT + n, a.N - 1);
+            w_scale[n] = a.w_scale[c] * kUp;
+            bias[n] = a.bias ? element<T>(a.bias, c) : 0.0f;
+        }
     };
-    // The next chunk of the stream, if there is one.
-    auto issue = [&]() {
-        if (ltile >= sh.end) return;
-        const uint32_t to = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)(
-            lds + lbuf * kStage + wave * kRows * BK);
-        // Past a row's end the last piece again: the products leave it out.
-        const int at = min(lchunk * BK + piece, Kp - 16);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(from[i] + at), "{m0}"(to + kWaves * i * kRows * BK)
-                         : "memory");
+    // The loads of the stream's next chunk, one at a time: issued together, they fill the load queue and the products
+    // wait behind them. Past the stream's end they go on, over the last tile's chunks, into buffers that nothing reads.
+    uint32_t to = 0;
+    int at = 0;
+    auto aim = [&]() {
+        to = (uint32_t)(size_t)(__attribute__((address_space(3))) uint8_t*)(lds + lbuf * kStage + wave * kRows * BK);
+        at = min(lchunk * BK + piece, Kp - 16);  // past a row's end the last piece again: the products leave it out
+    };
+    auto issue = [&](int i) {
+        asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(from[i] + at), "s"(i < kTokenLoads ? qbase : wbase),
+                     "{m0}"(to + kWaves * i * kRows * BK)
+                     : "memory");
+    };
+    auto issued = [&]() {
         lbuf = lbuf + 1 == STAGES ? 0 : lbuf + 1;
         if (++lchunk == chunks) {
             lchunk = 0;
@@ -423,34 +485,44 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
 #pragma unroll
         for (int n = 0; n < NT; ++n) fw[to][n] = *reinterpret_cast<const i32x4*>(s + (BM + (wn * NT + n) * 32) * BK);
     };
-    auto multiply = [&](int from) {
+    // A step of 32 values of k; the loads of a chunk go between the products of its first steps.
+    constexpr int kProducts = NT * MT * kSteps32;               // of a chunk
+    constexpr int kEvery = kProducts > kLoads ? kProducts / kLoads : 1;
+    constexpr int kPer = (kLoads * kEvery + kProducts - 1) / kProducts;  // loads at a time
+    auto multiply = [&](int set, int g, bool load) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-                acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[from][n], fx[from][m], acc[n][m], 0, 0, 0);
+            for (int m = 0; m < MT; ++m) {
+                const int p = (g * NT + n) * MT + m;
+                if (load && p % kEvery == 0) {
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i)
+                        if (p / kEvery * kPer + i < kLoads) issue(p / kEvery * kPer + i);
+                }
+                acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fx[set][m], fw[set][n], acc[n][m], 0, 0, 0);
+            }
     };
     // Chunk c of a tile is there once at most the loads of the kAhead - 1 chunks behind it in the stream are on their
-    // way (no count but 0 at the stream's end). A tile's first kAhead have been waited for before.
+    // way. A tile's first kAhead have been waited for before.
     auto arrive = [&](int c) {
-        if (c >= kAhead) {
-            if (ltile < sh.end) wait_loads<kLoads*(kAhead - 1)>();
-            else wait_loads<0>();
-        }
+        if (c >= kAhead) wait_loads<kLoads*(kAhead - 1)>();
         lds_barrier();
-        issue();
+        aim();
     };
 
     load_scales(sh.tile);
     place(sh.tile);
-    for (int c = 0; c < kAhead; ++c) issue();
+    for (int c = 0; c < kAhead; ++c) {
+        aim();
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) issue(i);
+        issued();
+    }
     wait_loads<0>();
     int turn = 0;
-    auto hand_over = [&]() {  // the channels' values of the tile that comes
-        if (t < BN) {
-            channels[(2 * turn) * BN + t] = w_scale;
-            channels[(2 * turn + 1) * BN + t] = bias;
-        }
+    auto hand_over = [&]() {  // the scales of the tile that comes
+        if (t < BM) scales[turn * BM + t] = x_scale;
     };
     hand_over();
 #pragma unroll 1
@@ -466,12 +538,16 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
 #pragma unroll
             for (int g = 0; g < kSteps32; ++g) {
                 if (g + 1 < kSteps32) read((g + 1) & 1, g + 1);
-                multiply(g & 1);
+                multiply(g & 1, g, true);
             }
+            issued();
             buf = buf + 1 == STAGES ? 0 : buf + 1;
         }
         if (full < chunks) {
             arrive(full);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) issue(i);
+            issued();
             const int left = Kp - full * BK;
 #pragma unroll 1
             for (int g = 0; g * 32 < left; ++g) {
@@ -481,49 +557,52 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
 #pragma unroll
                     for (int m = 0; m < MT; ++m) fx[0][m] = none;
                 }
-                multiply(0);
+                multiply(0, 0, false);
             }
             buf = buf + 1 == STAGES ? 0 : buf + 1;
         }
 
         // Everything on its way has arrived before the first write leaves, so that no wait for loads waits for writes.
-        float now[MT];
+        float w[NT], b[NT];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) now[m] = xs[m];
-        const float *ws = channels + 2 * turn * BN, *bs = ws + BN;
+        for (int n = 0; n < NT; ++n) {
+            w[n] = w_scale[n];
+            b[n] = bias[n];
+        }
+        const float* xs = scales + turn * BM + wm * MT * 32 + 4 * half;
         const bool last = tile + sh.slots >= sh.end;
         if (!last) load_scales(tile + sh.slots);
         wait_loads<0>();
         turn ^= 1;
         if (!last) hand_over();
-        // acc[n][m][r]: token m * 32 + l32 of the wave's, channel n * 32 + 8 (r / 4) + 4 half + r % 4.
-        const long m0 = tile / ntiles * BM;
-        const int n0 = (int)(tile % ntiles) * BN;
+        // acc[n][m][r]: channel l32 NT + n of the wave's, token m * 32 + 8 (r / 4) + 4 half + r % 4. A store writes whole
+        // lines of two tokens.
+        const Tile place = tile_at(order, tile);
+        const long row = place.m * BM + wm * MT * 32 + 4 * half;
+        const int at = place.n * BN + (wn * 32 + l32) * NT;
+        uint8_t* to = static_cast<uint8_t*>(out) + row * a.out_row * T::kBytes;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const long row = m0 + (wm * MT + m) * 32 + l32;
-            uint8_t* to = static_cast<uint8_t*>(out) + row * a.out_row * T::kBytes;
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int nb = (wn * NT + n) * 32;
-                float v[16];
+            for (int c = 0; c < 4; ++c) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(xs + m * 32 + 8 * c);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const f32x4 w = *reinterpret_cast<const f32x4*>(ws + nb + 8 * c + 4 * half);
-                    const f32x4 b = *reinterpret_cast<const f32x4*>(bs + nb + 8 * c + 4 * half);
+                for (int r = 0; r < 4; ++r) {
+                    const int token = m * 32 + 8 * c + r;
+                    float v[NT];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[4 * c + r] = finish<T, ACT>(acc[n][m][4 * c + r], now[m], w[r], b[r]);
+                    for (int n = 0; n < NT; ++n) v[n] = finish<T, ACT>(acc[n][m][4 * c + r], x[r], w[n], b[n]);
+                    if (row + token < a.M)
+                        write_channels<T, NT>(to + token * a.out_row * T::kBytes, at, a.N, whole, v);
                 }
-                if (row < a.M) write_row<T>(to, n0 + nb, half, a.N, whole, v);
             }
-        }
     }
 }
 
 template <int BM, int BN, int WM, int WN, int BK, int STAGES, class T, int ACT>
 hipError_t product(const Linear8Call& a, const int8_t* q, const float* q_scale, void* out, hipStream_t st)
 {
-    constexpr size_t bytes = (size_t)STAGES * (BM + BN) * BK + 4 * BN * 4;
+    constexpr size_t bytes = (size_t)STAGES * (BM + BN) * BK + 2 * BM * 4;
     const auto kernel = product_kernel<BM, BN, WM, WN, BK, STAGES, T, ACT>;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess) return e;
@@ -531,24 +610,30 @@ hipError_t product(const Linear8Call& a, const int8_t* q, const float* q_scale, 
     // As many workgroups as the chip holds (by LDS and by registers: two waves a SIMD).
     constexpr int kHeld = (int)std::min<size_t>((160 << 10) / bytes, 8 / (WM * WN) > 0 ? 8 / (WM * WN) : 1);
     const long slots = std::min(per, (long)kHeld * kUnits / kXcds);
-    // Rows of whole 16 bytes, of a whole number of them: written 16 bytes at a time.
-    constexpr int kPer = 16 / T::kBytes;
-    const bool whole = a.N % kPer == 0 && a.out_row % kPer == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
+    // A lane's channels are written at once where they start at a multiple of their bytes in every row.
+    constexpr int NT = BN / WN / 32;
+    const bool whole =
+        a.N % NT == 0 && a.out_row % NT == 0 && reinterpret_cast<uintptr_t>(out) % (NT * T::kBytes) == 0;
+    const int wide = (int)std::max(1L, std::min(ntiles, (long)kColumnBytes / ((long)BN * steps_row(a.K))));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(slots * kXcds)), dim3(WM * WN * kWave), bytes, st, a,
-                       reinterpret_cast<const uint8_t*>(q), q_scale, out, (int)mtiles, (int)ntiles, whole);
+                       reinterpret_cast<const uint8_t*>(q), q_scale, out, Order{(int)mtiles, (int)ntiles, wide}, whole);
     return hipGetLastError();
 }
 
 // The widest tiles that leave no compute unit idle: a tile of 256 x 256 loads half the bytes a product that one of 128 x 128
-// does, which loads half of what one of 64 x 64 does. Products (bfloat16 results, no activation) in tiles of 64 / 128 /
-// 256, us: 4103 x 150 x 848 7.3 / 11.6 / 23, 512 x 768 x 768 5.1 / 7.4 / 15.1, 1024 x 2304 x 768 9.2 / 8.2 / 16.3,
-// 8000 x 1024 x 1024 23.7 / 15.6 / 21.2, 11000 x 2304 x 768 49 / 33.1 / 34.0, 45888 x 2304 x 768 159 / 124 / 119.
+// does, which loads half of what one of 64 x 64 does. Tiles of 128 x 256 leave room for two workgroups a compute unit, of
+// which one finishes its results beside the other's products: long rows need that least. Products (bfloat16 results, no
+// activation) in tiles of 64 / 128 / 128 x 256 / 256, us: 4103 x 150 x 848 6.2 / 9.7 / 18 / 21, 512 x 768 x 768 5.1 / 7.4 / -
+// / 15, 1024 x 2304 x 768 9.2 / 8.2 / - / 16, 20000 x 1024 x 1024 - / 33.0 / 33.4 / 36.7, 45888 x 2304 x 768 200 / 128 / 112 /
+// 117, 45920 x 1024 x 4096 370 / 210 / 214 / 182.
+constexpr int kLongRows = 1024;
 template <class T, int ACT>
 hipError_t product_of(const Linear8Call& a, const int8_t* q, const float* q_scale, void* out, hipStream_t st)
 {
-    auto tiles = [&](int rows) { return (a.M + rows - 1) / rows * ((a.N + rows - 1) / rows); };
-    if (tiles(256) >= 2 * kUnits) return product<256, 256, 2, 4, 128, 2, T, ACT>(a, q, q_scale, out, st);
-    if (tiles(128) >= kUnits / 2) return product<128, 128, 2, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
+    auto tiles = [&](int m, int n) { return (a.M + m - 1) / m * ((a.N + n - 1) / n); };
+    if (a.K > kLongRows && tiles(256, 256) >= 2 * kUnits) return product<256, 256, 4, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
+    if (tiles(128, 256) >= 2 * kUnits) return product<128, 256, 2, 2, 64, 3, T, ACT>(a, q, q_scale, out, st);
+    if (tiles(128, 128) >= kUnits / 2) return product<128, 128, 2, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
     return product<64, 64, 2, 2, 128, 3, T, ACT>(a, q, q_scale, out, st);
 }
 

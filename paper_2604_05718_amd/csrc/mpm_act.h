@@ -29,7 +29,8 @@ __device__ __forceinline__ float normal_integral(float z)
 // z times the normal distribution's integral, as z / (1 + e^-l) with l the logarithm of the integral's odds, an odd
 // function of z close to a polynomial of seventh degree. The coefficients minimise the largest error of l over |z| <= 6
 // where the result is 10^-4 or more, 0.00104: a quarter of bfloat16's half step for negative z, less for positive.
-// Two thirds of the instructions of the integral itself: the product of 45920 x 4096 x 1024 with it 303 us against 330.
+// Two thirds of the instructions of the integral itself: the product of 45920 x 4096 x 1024 with it 303 us
+// against 330.
 __device__ __forceinline__ float gelu_bf16(float z)
 {
     constexpr float kLog2e = 1.4426950408889634f;
