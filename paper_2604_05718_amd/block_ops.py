@@ -379,6 +379,14 @@ def _like(t, c):
     return new, _lib.Heads(new.data_ptr(), c.H * c.dh, c.dh)
 
 
+def _written(t, what, ref, c):
+    """The heads of a given tensor that a rotary call writes: every row and head at a place of its own."""
+    h = _heads(t, what, ref, c.R, c.H)
+    if (h.row == 0 and c.R > 1) or (h.head == 0 and c.H > 1):
+        raise ValueError(f"{what} must not be expanded: its rows and heads are written")
+    return h
+
+
 def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=False, out=None):
     """Rows of heads with every pair of channels turned by its row's place on a grid (mpm_rotary): the shape of x.
 
@@ -393,7 +401,7 @@ def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=Fals
     if out is None:
         out, ho = _like(x, c)
     else:
-        ho = _heads(out, "out", x, c.R, c.H)
+        ho = _written(out, "out", x, c)
     if c.R:
         _launch("mpm_rotary", x, _BYREF(c), _BYREF(hx), _BYREF(ho), int(bool(inverse)))
     return out
@@ -412,7 +420,7 @@ def rotary_backward(dout, x, freq, pos=None, grid=(1,), layout="halves", off=Non
     if dx is None:
         dx, hg = _like(dout, c)
     else:
-        hg = _heads(dx, "dx", dout, c.R, c.H)
+        hg = _written(dx, "dx", dout, c)
     hx, dfreq, ws, need = None, None, None, 0
     if with_dfreq:
         hx = _BYREF(_heads(x, "x", dout, c.R, c.H))

@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAhead = 4;      // rows a thread loads before it uses them
-constexpr int kGroups = 2048;  // workgroups of a pass, about
+constexpr int kGroups = 1024;  // workgroups of a pass, about
 
 template <class S>
 struct Vec {
@@ -53,7 +53,14 @@ struct Deal {
     int cols, ways;    // of a workgroup
     int blocks;        // column blocks (the grid's y)
     int chunks;
+    FixedDiv chunks_of;
 };
+
+// Rows of an image's chunk: `size` each, the last ones fewer or none.
+__device__ __forceinline__ int chunk_size(const Deal& d, long rows)
+{
+    return rows > 0 ? d.chunks_of((int)(rows - 1)) + 1 : 0;
+}
 
 struct Rows {
     long first, end;
@@ -68,9 +75,10 @@ __device__ __forceinline__ Rows image_rows(const GroupNormCall& a, int b)
 // The rows of work item i of images x chunks.
 __device__ __forceinline__ Rows item_rows(const GroupNormCall& a, const Deal& d, long i)
 {
-    const Rows r = image_rows(a, (int)(i / d.chunks));
-    const long c = i % d.chunks, n = r.end - r.first;
-    return Rows{r.first + n * c / d.chunks, r.first + n * (c + 1) / d.chunks, r.image};
+    const int b = d.chunks_of((int)i), c = (int)i - b * d.chunks;
+    const Rows r = image_rows(a, b);
+    const long size = chunk_size(d, r.end - r.first), first = min(r.first + c * size, r.end);
+    return Rows{first, min(first + size, r.end), b};
 }
 
 // This thread's vector of channels and its first row's offset (way), if it has any.
@@ -87,83 +95,83 @@ __device__ __forceinline__ Place place(const Deal& d)
     return p;
 }
 
-// Count, mean and sum of squared deviations of two sets as one (Chan, Golub and LeVeque's update).
-struct Moments {
-    float n, mean, m2;
-};
-__device__ __forceinline__ Moments joined(const Moments& a, const Moments& b)
-{
-    const float n = a.n + b.n;
-    if (n == 0.0f) return a;
-    const float part = b.n / n, d = b.mean - a.mean;
-    return Moments{n, fmaf(d, part, a.mean), a.m2 + b.m2 + d * d * a.n * part};
-}
-
-// Mean and squared deviations of every channel over an item's rows: parts[item][C] pairs. Values are taken from their
-// channel's in the image's first row, firsts[image][C], so that a mean far from zero beside the deviations costs no
-// digits.
+// Mean and squared deviations of every channel over an item's rows: parts[item][C] pairs, the mean less the channel's value
+// in the image's first row, firsts[image][C], so that a mean far from zero beside the deviations costs no digits.
+// A thread takes its values from the mean of its own first rows, R: with S and Q the sums of x - R and its square,
+// the deviations are Q - S^2 / n. That cancels only as far as R is off the thread's mean, and then those first
+// rows themselves deviate as much.
 template <class S>
 __global__ __launch_bounds__(kThreads) void channel_moments_kernel(GroupNormCall a, Deal d, const uint8_t* x,
                                                                    float2* __restrict__ parts,
                                                                    float* __restrict__ firsts)
 {
     typedef Vec<S> V;
-    __shared__ float lds[3][kThreads];
+    constexpr int kPer = V::kPer;
+    __shared__ float2 lds[kPer][kThreads];
     const Rows it = item_rows(a, d, blockIdx.x);
     const Place p = place(d);
     const long stride = (long)a.C * S::kBytes;
-    Moments m[V::kPer];
-#pragma unroll
-    for (int e = 0; e < V::kPer; ++e) m[e] = Moments{0.0f, 0.0f, 0.0f};
-    if (p.live && it.first < it.end) {
-        V zero;
+    const int rows = (int)(it.end - it.first);
+    if (rows == 0) return;
+    if (p.live && p.way < rows) {
+        const uint8_t* from = x + it.first * stride + (long)p.col * 16;
         const long first = image_rows(a, it.image).first;
-        zero.w = load16(x + first * stride + p.col * 16);
+        V zero;
+        zero.w = load16(x + first * stride + (long)p.col * 16);
         if (it.first == first && p.way == 0) {
 #pragma unroll
-            for (int e = 0; e < V::kPer; ++e) firsts[(long)it.image * a.C + p.col * V::kPer + e] = zero.get(e);
+            for (int e = 0; e < kPer; ++e) firsts[(long)it.image * a.C + p.col * kPer + e] = zero.get(e);
         }
-        for (long row = it.first + p.way; row < it.end; row += kAhead * d.ways) {
+        float ref[kPer], sum[kPer], sq[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sum[e] = sq[e] = 0.0f;
+        for (int row = p.way; row < rows; row += kAhead * d.ways) {
             V v[kAhead];
-            int n = 0;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) v[u].w = load16(from + (long)min(row + u * d.ways, rows - 1) * stride);
+            const int n = min(kAhead, (rows - 1 - row) / d.ways + 1);
+            if (row == p.way) {
+                const float inv = 1.0f / (float)n;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    ref[e] = 0.0f;
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) ref[e] += u < n ? v[u].get(e) - zero.get(e) : 0.0f;
+                    ref[e] = fmaf(ref[e], inv, zero.get(e));
+                }
+            }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const long r = row + u * d.ways;
-                if (r < it.end) {
-                    v[u].w = load16(x + r * stride + p.col * 16);
-                    ++n;
+                if (u >= n) break;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const float t = v[u].get(e) - ref[e];
+                    sum[e] += t;
+                    sq[e] = fmaf(t, t, sq[e]);
                 }
-            }
-            const float inv = 1.0f / (float)n;
-#pragma unroll
-            for (int e = 0; e < V::kPer; ++e) {
-                Moments q{(float)n, 0.0f, 0.0f};
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) q.mean += u < n ? v[u].get(e) - zero.get(e) : 0.0f;
-                q.mean *= inv;
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const float t = u < n ? v[u].get(e) - zero.get(e) - q.mean : 0.0f;
-                    q.m2 = fmaf(t, t, q.m2);
-                }
-                m[e] = joined(m[e], q);
             }
         }
+        const float inv = 1.0f / (float)((rows - 1 - p.way) / d.ways + 1);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            lds[e][threadIdx.x] = make_float2(fmaf(sum[e], inv, ref[e] - zero.get(e)),
+                                              fmaxf(fmaf(-sum[e] * inv, sum[e], sq[e]), 0.0f));
     }
-    for (int e = 0; e < V::kPer; ++e) {
-        __syncthreads();
-        lds[0][threadIdx.x] = m[e].n;
-        lds[1][threadIdx.x] = m[e].mean;
-        lds[2][threadIdx.x] = m[e].m2;
-        __syncthreads();
-        if (p.live && p.way == 0) {
-            Moments q = m[e];
-            for (int w = 1; w < d.ways; ++w) {
-                const int t = w * d.cols + threadIdx.x;
-                q = joined(q, Moments{lds[0][t], lds[1][t], lds[2][t]});
-            }
-            parts[(long)blockIdx.x * a.C + p.col * V::kPer + e] = make_float2(q.mean, q.m2);
+    __syncthreads();
+    // The threads' parts of each channel, in order.
+    const int cols = min(d.cols, d.vecs - (int)blockIdx.y * d.cols), ways = min(d.ways, rows);
+    const int whole = rows / d.ways, more = rows - whole * d.ways;  // rows a way: whole, the first `more` one more
+    for (int c = threadIdx.x; c < cols * kPer; c += kThreads) {
+        const float2* at = lds[c % kPer] + c / kPer;
+        float mean = 0.0f, m2 = 0.0f;
+        for (int w = 0; w < ways; ++w) mean = fmaf((float)(whole + (w < more)), at[w * d.cols].x, mean);
+        mean /= (float)rows;
+        for (int w = 0; w < ways; ++w) {
+            const float2 q = at[w * d.cols];
+            const float e = q.x - mean;
+            m2 += fmaf((float)(whole + (w < more)) * e, e, q.y);
         }
+        parts[(long)blockIdx.x * a.C + (long)blockIdx.y * d.cols * kPer + c] = make_float2(mean, m2);
     }
 }
 
@@ -185,44 +193,68 @@ __device__ __forceinline__ void store_parameter(void* p, int dt, long i, float v
     else static_cast<float*>(p)[i] = v;
 }
 
-// Mean and reciprocal deviation of one image's group, by one wave, from the channels' parts, in 64 bits.
-__device__ __forceinline__ float2 joined_stats(const GroupNormCall& a, const Deal& d, const float2* parts,
-                                               const float* firsts, int b, int g)
+// What the parts of a channel's rows add to a group's sums, of n (mean - from) and of the squared deviations from it; in 64
+// bits, in which the first row's value serves as `from` however far it lies off.
+__device__ __forceinline__ double2 spread(float2 part, int n, double offset)
 {
-    const int width = a.C / a.groups, many = d.chunks * width, lane = threadIdx.x % kWave;
-    const Rows image = image_rows(a, b);
-    const long rows = image.end - image.first;
-    const double count = (double)rows * width;
-    if (rows == 0) return make_float2(0.0f, 0.0f);
-    // A part's count and mean; its deviations are left to the caller.
-    auto part = [&](int i, double* n, double* mean) {
-        const int chunk = i / width, c = g * width + i - chunk * width;
-        const float2 q = parts[((long)b * d.chunks + chunk) * a.C + c];
-        *n = (double)(rows * (chunk + 1) / d.chunks - rows * chunk / d.chunks);
-        *mean = (double)q.x + (double)firsts[(long)b * a.C + c];
-        return (double)q.y;
-    };
-    double sum = 0.0, m2 = 0.0, n, mean;
-    for (int i = lane; i < many; i += kWave) {
-        part(i, &n, &mean);
-        if (n > 0.0) sum += n * mean;
-    }
-    const double centre = wave_sum(sum) / count;
-    for (int i = lane; i < many; i += kWave) {
-        const double q = part(i, &n, &mean);
-        if (n > 0.0) m2 += q + n * (mean - centre) * (mean - centre);
-    }
-    m2 = wave_sum(m2);
-    return make_float2((float)centre, (float)(1.0 / sqrt(m2 / count + (double)a.eps)));
+    const double u = offset + (double)part.x;
+    return make_double2(n * u, (double)part.y + n * u * u);
 }
 
-// ... of every image and group, a wave each.
-__global__ __launch_bounds__(kWave) void group_stats_kernel(GroupNormCall a, Deal d, const float2* __restrict__ parts,
-                                                            const float* __restrict__ firsts, float2* __restrict__ stats)
+// A group's mean and reciprocal deviation from its sums.
+__device__ __forceinline__ float2 finished(const GroupNormCall& a, double count, double from, double2 s)
 {
+    const double m2 = fmax(s.y - s.x * s.x / count, 0.0);
+    return make_float2((float)(from + s.x / count), (float)(1.0 / sqrt(m2 / count + (double)a.eps)));
+}
+
+constexpr int kJoinThreads = 1024;
+// The sums of two numbers of each of `many` items over a workgroup of kJoinThreads, in a fixed order, in every thread.
+template <class Use>
+__device__ __forceinline__ double2 block_sum(int many, Use&& use)
+{
+    __shared__ double2 lds[kJoinThreads / kWave];
+    double s = 0.0, s2 = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < many; i += kJoinThreads) {
+        const double2 q = use(i);
+        s += q.x;
+        s2 += q.y;
+    }
+    s = wave_sum(s);
+    s2 = wave_sum(s2);
+    __syncthreads();  // the sums before have been read
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = make_double2(s, s2);
+    __syncthreads();
+    double2 r = lds[0];
+    for (int w = 1; w < kJoinThreads / kWave; ++w) {
+        r.x += lds[w].x;
+        r.y += lds[w].y;
+    }
+    return r;
+}
+
+// Mean and reciprocal deviation of every image and group, a workgroup each.
+__global__ __launch_bounds__(kJoinThreads) void group_stats_kernel(GroupNormCall a, Deal d, FixedDiv width_of,
+                                                               const float2* __restrict__ parts,
+                                                               const float* __restrict__ firsts,
+                                                               float2* __restrict__ stats)
+{
+    const int width = a.C / a.groups;
     for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
-        const float2 q = joined_stats(a, d, parts, firsts, (int)(pair / a.groups), (int)(pair % a.groups));
-        if (threadIdx.x == 0) stats[pair] = q;
+        const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
+        const Rows image = image_rows(a, b);
+        const int rows = (int)(image.end - image.first), size = chunk_size(d, rows);
+        const float* f = firsts + (long)b * a.C + g * width;
+        const float2* at = parts + (long)b * d.chunks * a.C + g * width;
+        const double from = rows > 0 ? (double)f[0] : 0.0;
+        const int chunks = rows > 0 ? (rows - 1) / size + 1 : 0;  // that have rows
+        const double2 s = block_sum(chunks * width, [&](int i) {
+            const int k = width_of(i), c = i - k * width;
+            return spread(at[(long)k * a.C + c], min(size, rows - k * size), (double)f[c] - from);
+        });
+        if (threadIdx.x == 0)
+            stats[pair] = rows > 0 ? finished(a, (double)rows * width, from, s) : make_float2(0.0f, 0.0f);
     }
 }
 
@@ -237,7 +269,30 @@ __device__ __forceinline__ GroupRange block_groups(const GroupNormCall& a, const
     const int c1 = min(c0 + d.cols * Vec<S>::kPer, a.C) - 1;
     return GroupRange{c0 / width, c1 / width - c0 / width + 1};
 }
-constexpr int kMostBlockGroups = kThreads * 8;  // groups of one channel each
+// Channels of them that a workgroup joins by itself, at most.
+constexpr int kMostChannels = kThreads * 8;
+
+// Sums over the channels of each of a block's groups, `lanes` lanes a group (8 or 64): use(channel of the block's groups)
+// gives two numbers, write(group, sums) takes their sums.
+template <class Use, class Write>
+__device__ __forceinline__ void over_channels(int groups, int width, Use&& use, Write&& write)
+{
+    const int lanes = groups <= 8 ? kWave : 8;
+    const int lane = threadIdx.x % lanes;
+    for (int g = threadIdx.x / lanes; g < groups; g += kThreads / lanes) {
+        double s = 0.0, s2 = 0.0;
+        for (int c = lane; c < width; c += lanes) {
+            const double2 q = use(g * width + c);
+            s += q.x;
+            s2 += q.y;
+        }
+        for (int o = lanes / 2; o > 0; o >>= 1) {
+            s += __shfl_xor(s, o);
+            s2 += __shfl_xor(s2, o);
+        }
+        if (lane == 0) write(g, make_double2(s, s2));
+    }
+}
 
 // A vector's parameters: mean, rstd, weight and shift of each of its channels.
 template <class S>
@@ -272,19 +327,39 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(GroupNormCall a, Deal d
                                                          const float* __restrict__ firsts, float2* __restrict__ made)
 {
     typedef Vec<S> V;
-    __shared__ float2 own[kMostBlockGroups];
+    __shared__ float2 own[kMostChannels];
+    __shared__ double2 sums[kMostChannels];
     const Rows it = item_rows(a, d, blockIdx.x);
     const Place p = place(d);
     const GroupRange groups = block_groups<S>(a, d);
-    for (int g = threadIdx.x / kWave; !stats && g < groups.count; g += kThreads / kWave) {
-        const float2 q = joined_stats(a, d, parts, firsts, it.image, groups.first + g);
-        if (threadIdx.x % kWave == 0) {
-            own[g] = q;
-            // (a group that two column blocks share gets the same value from both)
-            if (made && blockIdx.x % d.chunks == 0) made[(long)it.image * a.groups + groups.first + g] = q;
+    if (!stats) {
+        const Rows image = image_rows(a, it.image);
+        const int rows = (int)(image.end - image.first), width = a.C / a.groups, c0 = groups.first * width;
+        const float* f = firsts + (long)it.image * a.C + c0;
+        const int size = chunk_size(d, rows), chunks = rows > 0 ? (rows - 1) / size + 1 : 0;
+        for (int c = threadIdx.x; rows > 0 && c < groups.count * width; c += kThreads) {
+            const float2* at = parts + (long)it.image * d.chunks * a.C + c0 + c;
+            const double offset = (double)f[c] - (double)f[c / width * width];
+            double s = 0.0, s2 = 0.0;
+#pragma unroll 8
+            for (int k = 0; k < chunks; ++k) {
+                const double2 q = spread(at[(long)k * a.C], min(size, rows - k * size), offset);
+                s += q.x;
+                s2 += q.y;
+            }
+            sums[c] = make_double2(s, s2);
         }
+        __syncthreads();
+        over_channels(
+            groups.count, width, [&](int c) { return rows > 0 ? sums[c] : make_double2(0.0, 0.0); },
+            [&](int g, double2 s) {
+                const float2 q = rows > 0 ? finished(a, (double)rows * width, (double)f[g * width], s) : make_float2(0.0f, 0.0f);
+                own[g] = q;
+                // (a group that two column blocks share gets the same value from both)
+                if (made && it.first == image.first) made[(long)it.image * a.groups + groups.first + g] = q;
+            });
+        __syncthreads();
     }
-    __syncthreads();
     if (!p.live || it.first >= it.end) return;
     const long stride = (long)a.C * S::kBytes;
     Affine<S> f;
@@ -303,7 +378,7 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(GroupNormCall a, Deal d
 #pragma unroll
             for (int e = 0; e < V::kPer; ++e)
                 o[e] = activate<ACT, S::kBytes == 4>(fmaf((v[u].get(e) - f.mean[e]) * f.rstd[e], f.w[e], f.b[e]));
-            store16(y + r * stride + p.col * 16, V::pack(o));
+            store16_stream(y + r * stride + p.col * 16, V::pack(o));
         }
     }
 }
@@ -363,38 +438,37 @@ __global__ __launch_bounds__(kThreads) void channel_sums_kernel(GroupNormCall a,
     }
 }
 
-// From the channels' sums: the means of gt and gt t of one image's group, by one wave, ...
-__device__ __forceinline__ float2 joined_means(const GroupNormCall& a, const Deal& d, const float2* parts, int b, int g)
+// A channel's sums as they enter its group's: of gt and gt t.
+__device__ __forceinline__ double2 weighted(const GroupNormCall& a, double2 q, int c)
 {
-    const int width = a.C / a.groups;
-    double s0 = 0.0, s1 = 0.0;
-    for (int i = threadIdx.x % kWave; i < d.chunks * width; i += kWave) {
-        const int c = g * width + i % width;
-        const float2 q = parts[((long)b * d.chunks + i / width) * a.C + c];
-        const double w = a.w ? (double)parameter(a.w, a.dt, c) : 1.0;
-        s0 += w * (double)q.x;
-        s1 += w * (double)q.y;
-    }
-    s0 = wave_sum(s0);
-    s1 = wave_sum(s1);
-    const Rows r = image_rows(a, b);
-    const double n = (double)(r.end - r.first) * width;
-    return n > 0.0 ? make_float2((float)(s0 / n), (float)(s1 / n)) : make_float2(0.0f, 0.0f);
+    const double w = a.w ? (double)parameter(a.w, a.dt, c) : 1.0;
+    return make_double2(w * q.x, w * q.y);
 }
 
-// ... of every image and group ...
-__global__ __launch_bounds__(kWave) void group_means_kernel(GroupNormCall a, Deal d, const float2* __restrict__ parts,
-                                                            float2* __restrict__ means)
+// From the channels' sums: the means of gt and gt t of every image and group, a workgroup each ...
+__global__ __launch_bounds__(kJoinThreads) void group_means_kernel(GroupNormCall a, Deal d, FixedDiv width_of,
+                                                               const float2* __restrict__ parts,
+                                                               float2* __restrict__ means)
 {
+    const int width = a.C / a.groups;
     for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
-        const float2 q = joined_means(a, d, parts, (int)(pair / a.groups), (int)(pair % a.groups));
-        if (threadIdx.x == 0) means[pair] = q;
+        const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
+        const float2* at = parts + (long)b * d.chunks * a.C + g * width;
+        const double2 s = block_sum(d.chunks * width, [&](int i) {
+            const int k = width_of(i), c = i - k * width;
+            const float2 q = at[(long)k * a.C + c];
+            return weighted(a, make_double2((double)q.x, (double)q.y), g * width + c);
+        });
+        const Rows r = image_rows(a, b);
+        const double n = (double)(r.end - r.first) * width;
+        if (threadIdx.x == 0)
+            means[pair] = n > 0.0 ? make_float2((float)(s.x / n), (float)(s.y / n)) : make_float2(0.0f, 0.0f);
     }
 }
 
 // ... and dw and db, 64 channels a workgroup, sixteen waves' shares of the items joined in order.
-constexpr int kJoinWaves = 16;
-__global__ __launch_bounds__(kJoinWaves* kWave) void join_sums_kernel(const float2* __restrict__ parts, long items, int C,
+constexpr int kJoinWaves = kJoinThreads / kWave;
+__global__ __launch_bounds__(kJoinThreads) void join_sums_kernel(const float2* __restrict__ parts, long items, int C,
                                                                       int dt, void* dw, void* db)
 {
     __shared__ double lds[2][kJoinWaves][kWave];
@@ -429,15 +503,34 @@ __global__ __launch_bounds__(kThreads) void input_gradient_kernel(GroupNormCall 
                                                                   const float2* __restrict__ parts)
 {
     typedef Vec<S> V;
-    __shared__ float2 own[kMostBlockGroups];
+    __shared__ float2 own[kMostChannels];
+    __shared__ double2 sums[kMostChannels];
     const Place p = place(d);
     const Rows it = item_rows(a, d, blockIdx.x);
     const GroupRange groups = block_groups<S>(a, d);
-    for (int g = threadIdx.x / kWave; !means && g < groups.count; g += kThreads / kWave) {
-        const float2 q = joined_means(a, d, parts, it.image, groups.first + g);
-        if (threadIdx.x % kWave == 0) own[g] = q;
+    if (!means) {
+        const Rows image = image_rows(a, it.image);
+        const int width = a.C / a.groups, c0 = groups.first * width;
+        const double n = (double)(image.end - image.first) * width;
+        for (int c = threadIdx.x; c < groups.count * width; c += kThreads) {
+            const float2* at = parts + (long)it.image * d.chunks * a.C + c0 + c;
+            double s0 = 0.0, s1 = 0.0;
+#pragma unroll 8
+            for (int k = 0; k < d.chunks; ++k) {
+                const float2 q = at[(long)k * a.C];
+                s0 += (double)q.x;
+                s1 += (double)q.y;
+            }
+            sums[c] = weighted(a, make_double2(s0, s1), c0 + c);
+        }
+        __syncthreads();
+        over_channels(
+            groups.count, width, [&](int c) { return sums[c]; },
+            [&](int g, double2 s) {
+                own[g] = n > 0.0 ? make_float2((float)(s.x / n), (float)(s.y / n)) : make_float2(0.0f, 0.0f);
+            });
+        __syncthreads();
     }
-    __syncthreads();
     if (!p.live) return;
     const long stride = (long)a.C * S::kBytes;
     if (a.off) {  // a share of the rows of no image
@@ -479,7 +572,7 @@ __global__ __launch_bounds__(kThreads) void input_gradient_kernel(GroupNormCall 
                 const float gz = g[u].get(e) * activation_slope<ACT, S::kBytes == 4>(fmaf(t, f.w[e], f.b[e]));
                 o[e] = f.rstd[e] * (fmaf(gz, f.w[e], -m0[e]) - t * m1[e]);
             }
-            store16(dx + r * stride + p.col * 16, V::pack(o));
+            store16_stream(dx + r * stride + p.col * 16, V::pack(o));
         }
     }
 }
@@ -496,8 +589,23 @@ struct Slab {
     int vecs, cols, slabs, ways, threads;
     int width;       // channels a group
     int groups;      // of a slab
+    bool stream;     // whether its rows are whole lines, or many, and written past the L2
     FixedDiv cols_of, width_of, per_of;  // by cols; by a group's channels; by its vectors (where it has whole ones)
 };
+
+// Rows of whole lines written past the L2, whose room the slabs' reads need (64 grids of 1024 x 768 51.6 -> 48 us, a step
+// of 16 of 4096 x 1024 219 -> 197); parts of lines by way of it, which joins them (4 of 9216 x 256, 16 bytes a slab: 24 us
+// against 51).
+__device__ __forceinline__ void store_piece(uint8_t* p, u32x4 v, bool stream)
+{
+    if (stream) {
+        store16_stream(p, v);
+    } else {
+        asm volatile("" ::: "memory");  // (the compiler would make one store of the two, an ordinary one,
+        store16(p, v);
+        asm volatile("" ::: "memory");  // before the branch or behind it)
+    }
+}
 
 // Slab and image of a workgroup: the slabs of an image on one XCD, whose L2 then joins the lines that two of them share.
 constexpr int kXcds = 8;
@@ -637,7 +745,7 @@ __global__ __launch_bounds__(kSlabThreads) void slab_kernel(GroupNormCall a, Sla
         for (int e = 0; e < kPer; ++e)
             o[e] = activate<ACT, S::kBytes == 4>(fmaf((f.get(e) - mean[ONE ? 0 : e]) * rstd[ONE ? 0 : e],
                                                       a.w ? wv.get(e) : 1.0f, a.b ? bv.get(e) : 0.0f));
-        store16(y + it.first * stride + (long)col * 16 + r * stride, V::pack(o));
+        store_piece(y + it.first * stride + (long)col * 16 + r * stride, V::pack(o), s.stream);
     };
 #pragma unroll
     for (int u = 0; u < VPT; ++u)
@@ -774,7 +882,7 @@ __global__ __launch_bounds__(kSlabThreads) void slab_backward_kernel(GroupNormCa
             const float u = slope(f.get(e), d.get(e), e, &gz);
             o[e] = rstd[ONE ? 0 : e] * (fmaf(gz, weight(e), -m0[ONE ? 0 : e]) - u * m1[ONE ? 0 : e]);
         }
-        store16(dx + at + r * stride, V::pack(o));
+        store_piece(dx + at + r * stride, V::pack(o), s.stream);
     };
 #pragma unroll
     for (int u = 0; u < VPT; ++u)
@@ -821,7 +929,7 @@ Plan plan(const GroupNormCall& a, bool backward)
             best = k;
         }
     }
-    Plan p{Slab{vecs, 0, 0, 0, 0, width, 0, FixedDiv(1), FixedDiv((uint32_t)width), FixedDiv((uint32_t)std::max(1, width / per))},
+    Plan p{Slab{vecs, 0, 0, 0, 0, width, 0, false, FixedDiv(1), FixedDiv((uint32_t)width), FixedDiv((uint32_t)std::max(1, width / per))},
            1};
     if (best == 0) return p;
     Slab& s = p.s;
@@ -829,6 +937,7 @@ Plan plan(const GroupNormCall& a, bool backward)
     s.slabs = (units + best - 1) / best;
     s.groups = unit_groups * best;
     s.cols_of = FixedDiv((uint32_t)s.cols);
+    s.stream = s.cols % 4 == 0 || s.cols >= 6 || s.slabs == 1;
     // Enough threads for about four vectors each.
     s.threads = kSlabThreads;
     while (s.threads > 256 && s.cols * 2 <= s.threads / 4 && (s.threads / 2 / s.cols) * 4L >= rows) s.threads /= 2;
@@ -837,25 +946,9 @@ Plan plan(const GroupNormCall& a, bool backward)
     return p;
 }
 
-// Whether a call goes by slabs: they read a tensor once, and once more what does not fit (`most` vectors a thread), in one
-// launch, but a workgroup works through its slab alone.
-bool by_slabs(const GroupNormCall& a, bool backward, const Plan& p)
-{
-    if (p.s.cols == 0 || (long)a.B * p.s.slabs > (1L << 21)) return false;  // (a grid holds 2^32 threads)
-    const double rows = std::max(1.0, (double)a.R / a.B), groups = (double)a.B * p.s.slabs;
-    const double slab = rows * p.s.cols * 16, total = (double)a.R * a.C * (a.dt == kBf16 ? 2 : 4);
-    const double kept = std::min(1.0, (double)p.vpt * p.s.ways / rows);
-    const double moved = backward ? 3 + 2 * (1 - kept) : 2 + 2 * (1 - kept);  // tensors
-    const double rounds = std::ceil(groups / kUnits);
-    // us: a workgroup alone moves about 50 KB a us, the chip 5.2 MB; three launches 9 us.
-    const double alone = rounds * (3.0 + slab * moved / 5e4), all = total * moved / 5.2e6;
-    const double passes = 9.0 + total * (backward ? 5.0 : 3.0) / 5.2e6;
-    return std::max(alone, all) < passes;
-}
-
 Deal deal(const GroupNormCall& a)
 {
-    Deal d;
+    Deal d{0, 0, 0, 0, 0, FixedDiv(1)};
     d.vecs = a.C / (a.dt == kBf16 ? 8 : 4);
     // Few enough vectors for two rows at a time; blocks of about the same width.
     d.blocks = (d.vecs + kThreads - 1) / kThreads;
@@ -864,11 +957,12 @@ Deal deal(const GroupNormCall& a)
     const long per = std::max(1L, ((long)a.R + a.B - 1) / a.B);
     const long most = std::max(1L, (per + d.ways * kAhead - 1) / (d.ways * kAhead));
     d.chunks = (int)std::max(1L, std::min(most, ((long)kGroups / d.blocks + a.B - 1) / a.B));
+    d.chunks_of = FixedDiv((uint32_t)d.chunks);
     return d;
 }
 
-// Workgroups of a wave for the images' groups (which may be more than a grid has).
-unsigned pair_groups(const GroupNormCall& a) { return (unsigned)std::min((long)a.B * a.groups, 1L << 20); }
+// Workgroups for the images' groups (which may be more than a grid has).
+unsigned pair_groups(const GroupNormCall& a) { return (unsigned)std::min((long)a.B * a.groups, 1L << 18); }
 
 size_t aligned256(size_t v) { return (v + 255) / 256 * 256; }
 size_t parts_bytes(const GroupNormCall& a, const Deal& d) { return aligned256((size_t)a.B * d.chunks * a.C * 8); }
@@ -877,7 +971,35 @@ size_t stats_bytes(const GroupNormCall& a) { return aligned256((size_t)a.B * a.g
 
 // Whether the second pass joins an image's parts by itself: a launch less, for up to so many of them.
 constexpr int kFewParts = 8192;
-bool joins_itself(const GroupNormCall& a, const Deal& d) { return (long)d.chunks * a.C <= kFewParts; }
+bool joins_itself(const GroupNormCall& a, const Deal& d)
+{
+    const int width = a.C / a.groups, own = d.cols * (a.dt == kBf16 ? 8 : 4);
+    const int channels = d.blocks == 1 ? a.C : own + 2 * (width - 1);
+    return (long)d.chunks * a.C <= kFewParts && channels <= kMostChannels;
+}
+
+// Whether a call goes by slabs: one launch that reads a tensor once (and once more what its threads do not keep), but a
+// workgroup works through its slab alone; or by passes over chunks of rows: two or three launches that read it twice. By an
+// estimate in us, from the times of both at 25 shapes (1 to 64 images of 100 to 9216 rows of 48 to 1024 channels): it takes the
+// slower one by more than a tenth at three of them, and by less than a quarter.
+bool by_slabs(const GroupNormCall& a, bool backward, const Plan& p)
+{
+    const Slab& s = p.s;
+    if (s.cols == 0 || (long)a.B * s.slabs > (1L << 21)) return false;  // (a grid holds 2^32 threads)
+    const int per = a.dt == kBf16 ? 8 : 4, most = backward ? 8 : 16;
+    const bool one = s.width % per == 0;
+    const double rows = std::max(1.0, (double)a.R / a.B), total = (double)a.R * a.C * (16 / per) / 5.2e6;
+    // A workgroup: its latency (summing the channels of vectors in several groups takes longest), then its vectors.
+    const double held = kUnits * (2048.0 / s.threads) / (p.vpt == most ? 2 : 1);  // on the chip at once
+    const double rounds = std::ceil((double)a.B * s.slabs / held);
+    const double vectors = rows * s.cols / s.threads, again = std::max(0.0, vectors - p.vpt);
+    const double start = (backward ? (one ? 9.0 : 16.0) : (one ? 6.0 : 12.5)) * (s.threads < kSlabThreads ? 0.7 : 1.0);
+    const double alone = rounds * (start + (backward ? 1.9 : 1.0) * per / 8 * (vectors + again));
+    const double all = total * ((backward ? 3 : 2) + 2 * again / vectors) * 1.1;
+    const double join = joins_itself(a, deal(a)) ? 0.0 : 4.0;
+    const double passes = backward ? 10.5 + join + 4.5 * total : 10.5 + join + 2.6 * total;
+    return std::max(alone, all) < passes;
+}
 
 // Calls go(type, activation).
 template <class F>
@@ -934,7 +1056,8 @@ hipError_t forward_by_passes(const GroupNormCall& a, const void* x, void* y, flo
         typedef decltype(type) S;
         hipLaunchKernelGGL((channel_moments_kernel<S>), grid, dim3(kThreads), 0, st, a, d, xp, parts, firsts);
         if (!itself)
-            hipLaunchKernelGGL(group_stats_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, firsts, made);
+            hipLaunchKernelGGL(group_stats_kernel, dim3(pair_groups(a)), dim3(kJoinThreads), 0, st, a, d,
+                               FixedDiv((uint32_t)(a.C / a.groups)), parts, firsts, made);
         hipLaunchKernelGGL((apply_kernel<S, decltype(act)::value>), grid, dim3(kThreads), 0, st, a, d, xp,
                            static_cast<uint8_t*>(y), itself ? nullptr : made, parts, firsts,
                            reinterpret_cast<float2*>(stats));
@@ -945,7 +1068,7 @@ hipError_t forward_by_passes(const GroupNormCall& a, const void* x, void* y, flo
 hipError_t join(const GroupNormCall& a, const float2* parts, long items, void* dw, void* db, hipStream_t st)
 {
     if (!dw && !db) return hipSuccess;
-    hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinWaves * kWave), 0, st, parts,
+    hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((a.C + kWave - 1) / kWave)), dim3(kJoinThreads), 0, st, parts,
                        items, a.C, a.dt, dw, db);
     return hipGetLastError();
 }
@@ -981,7 +1104,8 @@ hipError_t backward_by_passes(const GroupNormCall& a, const void* dy, const void
         constexpr int ACT = decltype(act)::value;
         hipLaunchKernelGGL((channel_sums_kernel<S, ACT>), grid, dim3(kThreads), 0, st, a, d, gp, xp, sp, parts);
         if (!itself)
-            hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kWave), 0, st, a, d, parts, means);
+            hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kJoinThreads), 0, st, a, d,
+                               FixedDiv((uint32_t)(a.C / a.groups)), parts, means);
         hipLaunchKernelGGL((input_gradient_kernel<S, ACT>), grid, dim3(kThreads), 0, st, a, d, gp, xp,
                            static_cast<uint8_t*>(dx), sp, itself ? nullptr : means, parts);
         return hipGetLastError();

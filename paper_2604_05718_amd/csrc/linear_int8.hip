@@ -121,6 +121,7 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 }
 
 constexpr int kQuantThreads = 256;
+constexpr long kMostGroups = 1L << 22;  // workgroups of a launch (a grid holds 2^32 threads); they take further rows in turns
 
 template <class S>
 __device__ __forceinline__ void store_steps(uint8_t* to, const uint32_t (&w)[16 / S::kBytes / 4], bool in)
@@ -142,52 +143,58 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(const uint8_t* 
 {
     constexpr int kPer = 16 / S::kBytes, kWords = kPer / 4;
     const int lane = threadIdx.x % LANES, vecs = K / kPer, Kp = steps_row(K);
-    const long at = (long)blockIdx.x * (kQuantThreads / LANES) + threadIdx.x / LANES, row = min(at, R - 1);
-    const uint8_t* from = x + row * x_row * S::kBytes;
-    u32x4 v[VPL];
-    uint32_t m = 0;
+    constexpr int kRows = kQuantThreads / LANES;
+    for (long first = (long)blockIdx.x * kRows; first < R; first += (long)gridDim.x * kRows) {
+        const long at = first + threadIdx.x / LANES, row = min(at, R - 1);
+        const uint8_t* from = x + row * x_row * S::kBytes;
+        u32x4 v[VPL];
+        uint32_t m = 0;
 #pragma unroll
-    for (int u = 0; u < VPL; ++u) v[u] = load16(from + (long)min(lane + u * LANES, vecs - 1) * 16);
+        for (int u = 0; u < VPL; ++u) v[u] = load16(from + (long)min(lane + u * LANES, vecs - 1) * 16);
 #pragma unroll
-    for (int u = 0; u < VPL; ++u) m = largest<S>(v[u], m);
-    const Steps st(lanes_max<LANES>(m));
-    if (at >= R) return;
-    if (lane == 0) scale[row] = st.scale;
-    uint8_t* to = q + row * Kp;
+        for (int u = 0; u < VPL; ++u) m = largest<S>(v[u], m);
+        const Steps st(lanes_max<LANES>(m));
+        if (at >= R) return;
+        if (lane == 0) scale[row] = st.scale;
+        uint8_t* to = q + row * Kp;
 #pragma unroll
-    for (int u = 0; u < VPL; ++u) {
-        const int c = lane + u * LANES;
-        if (c * kPer >= Kp) break;
-        uint32_t w[kWords];
-        st.of<S>(v[u], w);
-        store_steps<S>(to + c * kPer, w, c < vecs);
+        for (int u = 0; u < VPL; ++u) {
+            const int c = lane + u * LANES;
+            if (c * kPer >= Kp) break;
+            uint32_t w[kWords];
+            st.of<S>(v[u], w);
+            store_steps<S>(to + c * kPer, w, c < vecs);
+        }
     }
 }
 
 // Wider rows: a workgroup each, read twice.
 template <class S>
-__global__ __launch_bounds__(kQuantThreads) void quantize_wide_kernel(const uint8_t* __restrict__ x, int K, long x_row,
-                                                                      uint8_t* __restrict__ q, float* __restrict__ scale)
+__global__ __launch_bounds__(kQuantThreads) void quantize_wide_kernel(const uint8_t* __restrict__ x, long R, int K,
+                                                                      long x_row, uint8_t* __restrict__ q,
+                                                                      float* __restrict__ scale)
 {
     constexpr int kPer = 16 / S::kBytes, kWords = kPer / 4, kWaves = kQuantThreads / kWave;
     __shared__ uint32_t lds[kWaves];
     const int vecs = K / kPer, Kp = steps_row(K);
-    const long row = blockIdx.x;
-    const uint8_t* from = x + row * x_row * S::kBytes;
-    uint32_t m = 0;
+    for (long row = blockIdx.x; row < R; row += gridDim.x) {
+        const uint8_t* from = x + row * x_row * S::kBytes;
+        uint32_t m = 0;
 #pragma unroll 4
-    for (int c = threadIdx.x; c < vecs; c += kQuantThreads) m = largest<S>(load16(from + (long)c * 16), m);
-    m = lanes_max<kWave>(m);
-    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = m;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w) m = max(m, lds[w]);
-    const Steps st(m);
-    if (threadIdx.x == 0) scale[row] = st.scale;
-    uint8_t* to = q + row * Kp;
-    for (int c = threadIdx.x; c * kPer < Kp; c += kQuantThreads) {
-        uint32_t w[kWords];
-        st.of<S>(load16(from + (long)min(c, vecs - 1) * 16), w);
-        store_steps<S>(to + c * kPer, w, c < vecs);
+        for (int c = threadIdx.x; c < vecs; c += kQuantThreads) m = largest<S>(load16(from + (long)c * 16), m);
+        m = lanes_max<kWave>(m);
+        __syncthreads();  // the row before has been read
+        if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = m;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) m = max(m, lds[w]);
+        const Steps st(m);
+        if (threadIdx.x == 0) scale[row] = st.scale;
+        uint8_t* to = q + row * Kp;
+        for (int c = threadIdx.x; c * kPer < Kp; c += kQuantThreads) {
+            uint32_t w[kWords];
+            st.of<S>(load16(from + (long)min(c, vecs - 1) * 16), w);
+            store_steps<S>(to + c * kPer, w, c < vecs);
+        }
     }
 }
 
@@ -197,8 +204,9 @@ hipError_t quantize(const uint8_t* x, long R, int K, long x_row, uint8_t* q, flo
     const int vecs = steps_row(K) / (16 / S::kBytes);
     auto rows = [&](auto lanes, auto vpl) {
         constexpr int L = decltype(lanes)::value, kRows = kQuantThreads / L;
-        hipLaunchKernelGGL((quantize_kernel<S, L, decltype(vpl)::value>), dim3((unsigned)((R + kRows - 1) / kRows)),
-                           dim3(kQuantThreads), 0, st, x, R, K, x_row, q, scale);
+        hipLaunchKernelGGL((quantize_kernel<S, L, decltype(vpl)::value>),
+                           dim3((unsigned)std::min((R + kRows - 1) / kRows, kMostGroups)), dim3(kQuantThreads), 0, st, x, R, K,
+                           x_row, q, scale);
     };
     constexpr std::integral_constant<int, 32> half{};
     constexpr std::integral_constant<int, kWave> wave{};
@@ -208,7 +216,8 @@ hipError_t quantize(const uint8_t* x, long R, int K, long x_row, uint8_t* q, flo
     else if (vecs <= 128) rows(half, std::integral_constant<int, 4>{});
     else if (vecs <= 256) rows(wave, std::integral_constant<int, 4>{});
     else if (vecs <= 512) rows(wave, std::integral_constant<int, 8>{});
-    else hipLaunchKernelGGL((quantize_wide_kernel<S>), dim3((unsigned)R), dim3(kQuantThreads), 0, st, x, K, x_row, q, scale);
+    else hipLaunchKernelGGL((quantize_wide_kernel<S>), dim3((unsigned)std::min(R, kMostGroups)), dim3(kQuantThreads), 0, st, x, R,
+                            K, x_row, q, scale);
     return hipGetLastError();
 }
 

@@ -54,6 +54,8 @@ struct Values {
         if constexpr (COUNT == 1) return __uint_as_float((uint32_t)w << 16);
         return e % 2 ? bf16_hi(word(e / 2)) : bf16_lo(word(e / 2));
     }
+    // STREAM: past the L2.
+    template <bool STREAM>
     __device__ static __forceinline__ void store(uint8_t* p, const float (&v)[COUNT])
     {
         Word w;
@@ -72,7 +74,8 @@ struct Values {
 #pragma unroll
                 for (int i = 0; i < kWords; ++i) w[i] = u[i];
         }
-        *reinterpret_cast<Word*>(p) = w;
+        if constexpr (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<Word*>(p));
+        else *reinterpret_cast<Word*>(p) = w;
     }
     __device__ static __forceinline__ uint32_t pack_bf16(float a, float b)
     {
@@ -96,9 +99,11 @@ struct Pairs {
     __device__ __forceinline__ float second(int e) const { return HALVES ? b.get(e) : a.get(2 * e + 1); }
     __device__ static __forceinline__ void store(uint8_t* p, int pairs, const float (&x)[V], const float (&y)[V])
     {
+        // Neighbouring lanes write whole lines past the L2, but for halves, whose two stores it joins (8 clips of 8 x 32 x 32
+        // tokens, pairs: a step 215 -> 198 us; 64 images of about 717, halves, forward 50 -> 54).
         if constexpr (HALVES) {
-            Values<S, V>::store(p, x);
-            Values<S, V>::store(p + pairs * S::kBytes, y);
+            Values<S, V>::template store<false>(p, x);
+            Values<S, V>::template store<false>(p + pairs * S::kBytes, y);
         } else {
             float v[2 * V];
 #pragma unroll
@@ -106,7 +111,7 @@ struct Pairs {
                 v[2 * e] = x[e];
                 v[2 * e + 1] = y[e];
             }
-            Values<S, 2 * V>::store(p, v);
+            Values<S, 2 * V>::template store<true>(p, v);
         }
     }
 };
@@ -384,7 +389,7 @@ hipError_t launch_one(const RotaryCall& a, const HeadRows& src, const HeadRows& 
     const Deal d = deal(a, V);
     size_t bytes = (size_t)d.tile * 16 + (PER_HEAD ? 0 : (size_t)d.tile * a.pairs * 8);
     if (GRAD) bytes = std::max(bytes, (size_t)a.axes * V * d.threads * 4);
-    const long groups = GRAD ? grad_groups(d) : std::min(d.tiles, 1L << 30);
+    const long groups = GRAD ? grad_groups(d) : std::min(d.tiles, 1L << 22);  // (a grid holds 2^32 threads)
     hipLaunchKernelGGL((rotary_kernel<S, V, HALVES, PER_HEAD, GRAD>), dim3((unsigned)groups, (unsigned)d.blocks),
                        dim3(d.threads), bytes, st, a, src, x, dst, inverse ? -1.0f : 1.0f, zero, d, parts);
     return hipGetLastError();

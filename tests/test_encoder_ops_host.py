@@ -226,7 +226,8 @@ def test_rotary_binding(recorded):
     bad = [dict(freq=device(torch.zeros(3, 8))), dict(freq=device(torch.zeros(5, 2, 8))), dict(grid=(3,)), dict(grid=()),
            dict(layout="whole"), dict(pos=device(torch.zeros(5, dtype=torch.int32))), dict(pos=device(torch.zeros(6))),
            dict(freq=device(torch.zeros(2, 8, dtype=torch.float64))), dict(out=device(torch.zeros(6, 4, 8))),
-           dict(out=device(torch.zeros(5, 4, 16)))]
+           dict(out=device(torch.zeros(5, 4, 16))), dict(out=device(torch.zeros(6, 1, 16)).expand(6, 4, 16)),
+           dict(out=device(torch.zeros(1, 4, 16)).expand(6, 4, 16)), dict(grid=(1 << 20, 1 << 20)), dict(grid=(2 ** 32 + 3, 5))]
     for kw in bad:
         with pytest.raises(ValueError):
             mpm.rotary(**{**dict(x=x, freq=f, grid=(3, 5)), **kw})

@@ -1,0 +1,166 @@
+"""The trainable encoder with rotary positions and its decoder head: gradients through the library's operators against
+the same modules in plain 64-bit torch, inference between merges, products served in 8-bit integers, clips."""
+import pytest
+import torch
+
+import block_refs
+import encoder_refs as ref
+import paper_2604_05718_amd as mpm
+from paper_2604_05718_amd.blocks import GridHead, RotaryEncoder
+
+pytestmark = pytest.mark.gpu
+
+DEV = torch.device("cuda:0")
+
+
+def plain(enc, x, ns, pos, gate, steps=False):
+    """enc.rows() in float64 on the CPU from copies of its parameters; returns (rows, parameters). steps: the products in
+    8-bit integers, as the module quantised them."""
+    p = {n: t.detach().double().cpu().requires_grad_() for n, t in enc.named_parameters()}
+    buffers = {n: t.double().cpu() for n, t in enc.named_buffers()}
+    rows_of = torch.repeat_interleave(torch.arange(len(ns)), torch.tensor(ns))
+    off = torch.cumsum(torch.tensor([0] + ns), 0)
+    imgs = block_refs.images(off, 0, len(ns))
+    c = ref.cells(pos, enc.grid)
+    h = block_refs.unit(x, "layer", 1e-6) * p["norms.0.weight"] + p["norms.0.bias"]
+    R, D = x.shape
+
+    for i, blk in enumerate(enc.blocks):
+        b = f"blocks.{i}."
+
+        def product(t, name):
+            if not steps:
+                return t @ p[b + name]
+            q, s = ref.steps(t.float())
+            w, ws = ref.steps(p[b + name].detach().float().t().contiguous())
+            return (q.double() @ w.double().t()) * s.double()[:, None] * ws.double()
+
+        H = blk.heads
+        qkv = product(h, "qkv").view(R, 3 * H, D // H)
+        freq = torch.cat([p[b + "freq"]] * 2) if blk.learned else buffers[b + "freq"]
+        qk = ref.turned(qkv[:, :2 * H], freq, c)
+        a, _ = block_refs.attention(qk[:, :H], qk[:, H:], qkv[:, 2 * H:], imgs, imgs, (D // H) ** -0.5)
+        for side, f, n in (("attn", lambda: product(a.reshape(R, D), "proj"), 2 * i + 1),
+                           ("mlp", lambda: product(ref.act(product(h, "fc1"), "gelu"), "fc2"), 2 * i + 2)):
+            x, h = block_refs.residual_norm(x, f(), p[f"norms.{n}.weight"], p[f"norms.{n}.bias"],
+                                            p[b + side + "_post_weight"], p[b + side + "_post_bias"], p[b + side + "_scale"],
+                                            gate, rows_of)
+    return h, p
+
+
+@pytest.mark.parametrize("learned", [True, False])
+@pytest.mark.parametrize("grid", [(8, 9), (2, 6, 6)])
+def test_gradients_of_the_encoder(learned, grid):
+    """Float32, two blocks on ragged images: rows and every parameter's gradient. Errors grow from the
+    operators' own (at most 288 times 2^-24) through eight products in a row: 16 times that; the frequencies', sums over
+    rows weighted by their cells (up to 8), twice that again."""
+    torch.manual_seed(1)
+    ns, D = [40, 1, 23], 32
+    enc = RotaryEncoder(D, 4, 2, grid, learned=learned, device=DEV, dtype=torch.float32)
+    pos = torch.cat([torch.randperm(72)[:n].sort().values for n in ns]).to(torch.int32)
+    x, gate, g = torch.randn(sum(ns), D), torch.rand(len(ns), D) + 0.5, torch.randn(sum(ns), D)
+    off = torch.cumsum(torch.tensor([0] + ns), 0).to(torch.int32)
+    xd, gd = x.to(DEV).requires_grad_(), gate.to(DEV).requires_grad_()
+    out = enc.rows(xd, off.to(DEV), max(ns), pos.to(DEV), gd)
+    (out * g.to(DEV)).sum().backward()
+    x64, g64 = x.double().requires_grad_(), gate.double().requires_grad_()
+    want, p = plain(enc, x64, ns, pos, g64)
+    (want * g.double()).sum().backward()
+    tol = 16 * 288 * 2.0 ** -24
+    assert block_refs.rel(out, want) <= tol
+    assert block_refs.rel(xd.grad, x64.grad) <= tol and block_refs.rel(gd.grad, g64.grad) <= tol
+    assert any("freq" in n for n in p) == learned
+    for n, t in enc.named_parameters():
+        assert block_refs.rel(t.grad, p[n].grad) <= tol * (2 if "freq" in n else 1), n
+
+
+@pytest.mark.parametrize("packed", [True, False])
+def test_gradients_of_the_head(packed):
+    """Float32: a product, group norm with its activation, a product. Errors of each step as its own test has them (96 half
+    steps, and as many as the products' 48 and 64 terms), four times for the chain."""
+    torch.manual_seed(2)
+    ns, D, C = [30, 30, 30], 48, 64
+    head = GridHead(D, C, 10, groups=8, device=DEV, dtype=torch.float32)
+    torch.nn.init.normal_(head.weight, 1.0, 0.2)
+    x, g = torch.randn(90, D), torch.randn(90, 10)
+    off = torch.cumsum(torch.tensor([0] + ns), 0).to(torch.int32)
+    xd = (x if packed else x.view(3, 30, D)).to(DEV).requires_grad_()
+    y = head(xd, off.to(DEV)) if packed else head(xd)
+    assert y.shape == ((90, 10) if packed else (3, 30, 10))
+    (y.reshape(90, 10) * g.to(DEV)).sum().backward()
+    p = {n: t.detach().double().cpu().requires_grad_() for n, t in head.named_parameters()}
+    x64 = x.double().requires_grad_()
+    t = ref.group_norm(x64 @ p["inner"], 8, [slice(0, 30), slice(30, 60), slice(60, 90)], p["weight"], p["bias"], "silu")
+    want = t @ p["classes"]
+    (want * g.double()).sum().backward()
+    tol = 4 * (96 + 64) * 2.0 ** -24
+    assert block_refs.rel(y.reshape(90, 10), want) <= tol and block_refs.rel(xd.grad.reshape(90, D), x64.grad) <= tol
+    for n, t in head.named_parameters():
+        assert block_refs.rel(t.grad, p[n].grad) <= tol, n
+
+
+@pytest.mark.parametrize("grid", [(12, 20), (3, 8, 10)])
+def test_inference_between_merges(grid):
+    """Merges before blocks 1 and 2, then the head: tokens of one cluster leave with one value; without merges the packed path
+    equals the grid's. The same served in 8-bit integers."""
+    torch.manual_seed(3)
+    B, D = 2, 64
+    enc = RotaryEncoder(D, 2, 3, grid, merge_before=(1, 2), device=DEV)
+    head = GridHead(D, 96, 21, groups=12, device=DEV)
+    x = torch.randn(B, 240, D, device=DEV).to(torch.bfloat16)
+    for served in (False, True):
+        if served:
+            enc.quantize()
+            head.quantize()
+        out = enc(x)
+        assert out.shape == x.shape and out.isfinite().all()
+        for b in range(B):
+            assert 60 <= torch.unique(out[b], dim=0).shape[0] < 240
+        with torch.no_grad():
+            y = head(out)
+        assert y.shape == (B, 240, 21) and y.isfinite().all()
+        enc.merge_before = ()
+        off = torch.tensor([0, 240, 480], dtype=torch.int32, device=DEV)
+        pos = torch.arange(240, dtype=torch.int32, device=DEV).repeat(B)
+        with torch.no_grad():
+            rows = enc.rows(x.view(B * 240, D), off, 240, pos)
+        assert torch.equal(enc(x).view(B * 240, D), rows)
+        enc.merge_before = (1, 2)
+
+
+def test_served_in_8_bits():
+    """A block's rows from products in 8 bits, float32 around them, against the same steps in 64 bits: of the first block
+    the steps are the same but where a value lies within float32's errors of a border. Those errors, 16 * 288 * 2^-24 as
+    above, relative to steps of 1/127 of a row's largest value move at most one value in 28 by a step, of up to 1/127 of the
+    largest: half a step's root mean square over all of them is 0.1 of that, 0.001 of the rows, through four products."""
+    torch.manual_seed(4)
+    ns, D, grid = [50, 30], 64, (8, 9)
+    enc = RotaryEncoder(D, 2, 1, grid, device=DEV, dtype=torch.float32)
+    pos = torch.cat([torch.randperm(72)[:n].sort().values for n in ns]).to(torch.int32)
+    x, gate = torch.randn(sum(ns), D), torch.ones(len(ns), D)
+    off = torch.cumsum(torch.tensor([0] + ns), 0).to(torch.int32)
+    want, _ = plain(enc, x.double(), ns, pos, gate.double(), steps=True)
+    exact, _ = plain(enc, x.double(), ns, pos, gate.double())
+    with torch.no_grad():
+        got = enc.quantize().rows(x.to(DEV), off.to(DEV), max(ns), pos.to(DEV), gate.to(DEV))
+    assert block_refs.rel(got, want) <= 4 * 0.001
+    # ... and what 8 bits cost: a product's operands are each off by up to half a step, uniformly: 1 / (127 sqrt 12) of the
+    # largest value, about 3 times the root mean square: 0.007 of a product for each operand; four products, of which the norms
+    # after them keep the share: 0.02 at most.
+    assert 0.001 < block_refs.rel(got, exact) <= 0.02
+
+
+def test_training_step_under_bfloat16():
+    """A step on tokens merged once: every parameter of encoder and head gets a finite gradient."""
+    torch.manual_seed(5)
+    B, grid, D = 3, (16, 16), 128
+    x = torch.randn(B, 256, D, device=DEV).to(torch.bfloat16)
+    m = mpm.merge_local(x, 16, 16)
+    total = int(m.y_off[-1])
+    rows, pos, most = m.y[:total], m.y_pos[:total], int(torch.diff(m.y_off.cpu()).max())
+    enc = RotaryEncoder(D, 2, 2, grid, learned=True, device=DEV)
+    head = GridHead(D, 64, 7, groups=8, device=DEV)
+    y = head(enc.rows(rows, m.y_off, most, pos), m.y_off)
+    y.float().square().mean().backward()
+    for n, t in [*enc.named_parameters(), *head.named_parameters()]:
+        assert t.grad is not None and t.grad.isfinite().all() and t.grad.any(), n
