@@ -168,7 +168,9 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(const uint8_t* 
     }
 }
 
-// Wider rows: a workgroup each, read twice.
+// Wider rows, and few of more than four vectors a lane of half a wave: a workgroup each, read twice. 60 rows of 4096
+// bfloat16 values 4.8 us (in a wave each 7.7), 1000 7.0 (10.9), 1000 of 2048 7.0 (6.8).
+constexpr int kFewRows = 1024;
 template <class S>
 __global__ __launch_bounds__(kQuantThreads) void quantize_wide_kernel(const uint8_t* __restrict__ x, long R, int K,
                                                                       long x_row, uint8_t* __restrict__ q,
@@ -214,8 +216,8 @@ hipError_t quantize(const uint8_t* x, long R, int K, long x_row, uint8_t* q, flo
     else if (vecs <= 64) rows(half, std::integral_constant<int, 2>{});
     else if (vecs <= 96) rows(half, std::integral_constant<int, 3>{});
     else if (vecs <= 128) rows(half, std::integral_constant<int, 4>{});
-    else if (vecs <= 256) rows(wave, std::integral_constant<int, 4>{});
-    else if (vecs <= 512) rows(wave, std::integral_constant<int, 8>{});
+    else if (vecs <= 256 && R > kFewRows) rows(wave, std::integral_constant<int, 4>{});
+    else if (vecs <= 512 && R > kFewRows) rows(wave, std::integral_constant<int, 8>{});
     else hipLaunchKernelGGL((quantize_wide_kernel<S>), dim3((unsigned)std::min(R, kMostGroups)), dim3(kQuantThreads), 0, st, x, R,
                             K, x_row, q, scale);
     return hipGetLastError();
@@ -248,68 +250,117 @@ __device__ __forceinline__ float finish(int sum, float x_scale, float w_scale, f
 
 // ---- few tokens --------------------------------------------------------------------------
 
-constexpr int kFew = 16;             // tokens
-constexpr int kFewThreads = 256;
-constexpr int kFewLds = 48 << 10;    // most bytes of steps made inside the product
+constexpr int kFew = 16;           // tokens whose values become steps inside the product
+constexpr int kFewLds = 48 << 10;  // most bytes of such steps
+constexpr int kFewAhead = 4;       // pieces of 64 values a wave has on their way
 
 struct Int8 {};
 
-// A workgroup takes 16 output channels of all tokens, its waves every fourth 64 values of k. X: the type of x; values
-// become steps in LDS first, in every workgroup by itself.
-template <class X, class T, int ACT>
-__global__ __launch_bounds__(kFewThreads) void few_kernel(Linear8Call a, const uint8_t* __restrict__ x, void* __restrict__ out)
+// A workgroup takes 16 output channels of 16 MT tokens, each of W waves every W-th piece of 64 values of k; the waves' sums
+// meet in LDS. X: the type of x; values (of at most W tokens) become steps in LDS first, in every workgroup by itself, while
+// the first weights are on their way: a wave has one row or a slice of one. What bounds it is the latency of one pass over
+// its rows: from bfloat16 values to bfloat16 results, replayed without pauses, 1 x 2304 x 768 takes 4.0 us (W = 16 5.1, by
+// two launches 7.7), 16 x 4096 x 1024 7.5 (two launches 10.5), 8 x 1024 x 4096 10 (W = 4 22.9, two launches 19).
+template <class X, class T, int ACT, int MT, int W>
+__global__ __launch_bounds__(W* kWave) void few_kernel(Linear8Call a, const uint8_t* __restrict__ x, void* __restrict__ out)
 {
     constexpr bool kValues = !std::is_same<X, Int8>::value;
-    constexpr int kWaves = kFewThreads / kWave;
-    extern __shared__ __align__(16) uint8_t q[];
-    __shared__ int sums[kWaves][kFew * 16];
-    __shared__ float scales[kFew];
-    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, M = (int)a.M, Kp = steps_row(a.K);
+    static_assert(!kValues || (MT == 1 && W <= 16), "a row has a wave");
+    extern __shared__ __align__(16) uint8_t lds[];  // steps, then the waves' sums
+    __shared__ float scales[16 * MT];
+    __shared__ uint32_t most[kValues ? W : 1];
+    const int t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave), Kp = steps_row(a.K);
+    const long m0 = (long)blockIdx.y * (16 * MT);
+    const int M = (int)min(a.M - m0, 16L * MT);
     const int n0 = blockIdx.x * 16, row = lane % 16, part = lane / 16;
-    const int8_t* w = a.w + (long)min(n0 + row, a.N - 1) * Kp;
+    const int8_t* w = a.w + (long)min(n0 + row, a.N - 1) * Kp + part * 16;
+    auto at = [&](int k, int u) { return k + u * (W * 64); };  // a wave's pieces
+    auto in = [&](int k, int u) { return at(k, u) + part * 16 < Kp; };
+    i32x4 wv[kFewAhead];
+    auto weights = [&](int k) {
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) wv[u] = *reinterpret_cast<const i32x4*>(w + (in(k, u) ? at(k, u) : -part * 16));
+    };
+    weights(wave * 64);
     if constexpr (kValues) {
         constexpr int kPer = 16 / X::kBytes, kWords = kPer / 4;
-        for (int r = wave; r < M; r += kWaves) {
-            const uint8_t* from = x + (long)r * a.x_row * X::kBytes;
-            const int vecs = a.K / kPer;
-            uint32_t m = 0;
-            for (int c = lane; c < vecs; c += kWave) m = largest<X>(load16(from + c * 16), m);
-            const Steps st(lanes_max<kWave>(m));
-            if (lane == 0) scales[r] = st.scale;
-            for (int c = lane; c * kPer < Kp; c += kWave) {
+        const int slices = W / M, r = wave / slices, slice = wave - r * slices, vecs = a.K / kPer;
+        const uint8_t* from = x + (long)min(r, M - 1) * a.x_row * X::kBytes;
+        if (t < W) most[t] = 0;
+        __syncthreads();
+        uint32_t m = 0;
+        if (r < M) {
+#pragma unroll 4
+            for (int c = slice * kWave + lane; c < vecs; c += slices * kWave) m = largest<X>(load16(from + c * 16), m);
+            m = lanes_max<kWave>(m);
+            if (lane == 0) atomicMax(&most[r], m);
+        }
+        __syncthreads();
+        if (r < M) {
+            const Steps st(most[r]);
+            if (slice == 0 && lane == 0) scales[r] = st.scale;
+#pragma unroll 2
+            for (int c = slice * kWave + lane; c * kPer < Kp; c += slices * kWave) {
                 uint32_t s[kWords];
                 st.of<X>(load16(from + min(c, vecs - 1) * 16), s);
-                store_steps<X>(q + r * Kp + c * kPer, s, c < vecs);
+                store_steps<X>(lds + r * Kp + c * kPer, s, c < vecs);
             }
         }
     } else {
-        if (t < M) scales[t] = a.x_scale[t];
+        if (t < M) scales[t] = a.x_scale[m0 + t];
     }
     __syncthreads();
-    i32x4 acc = {0, 0, 0, 0};
     const i32x4 none = {0, 0, 0, 0};
-    for (int k = wave * 64; k < Kp; k += kWaves * 64) {
-        const int at = k + part * 16;
-        const bool in = at < Kp;
-        const i32x4 wv = *reinterpret_cast<const i32x4*>(w + (in ? at : 0));
-        i32x4 xv = none;
-        if (in && row < M) {
-            if constexpr (kValues) xv = *reinterpret_cast<const i32x4*>(q + row * Kp + at);
-            else xv = *reinterpret_cast<const i32x4*>(x + (long)row * Kp + at);
-        }
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc, 0, 0, 0);
-    }
-    // acc[r]: channel 4 part + r of token `row`.
+    i32x4 acc[MT];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) sums[wave][row * 16 + 4 * part + r] = acc[r];
+    for (int m = 0; m < MT; ++m) acc[m] = none;
+    for (int k = wave * 64; k < Kp;) {
+        i32x4 xv[kFewAhead][MT];
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const int token = m * 16 + row;
+                xv[u][m] = none;
+                if (in(k, u) && token < M) {
+                    if constexpr (kValues) xv[u][m] = *reinterpret_cast<const i32x4*>(lds + token * Kp + at(k, u) + part * 16);
+                    else xv[u][m] = *reinterpret_cast<const i32x4*>(x + (m0 + token) * Kp + at(k, u) + part * 16);
+                }
+            }
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u], xv[u][m], acc[m], 0, 0, 0);
+        k = at(k, kFewAhead);
+        if (k < Kp) weights(k);
+    }
+    if constexpr (kValues) __syncthreads();  // the steps have been read
+    // acc[m][r]: channel 4 part + r of token 16 m + row.
+    int* sums = reinterpret_cast<int*>(lds);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) *reinterpret_cast<i32x4*>(sums + wave * (MT * 256) + (m * 16 + row) * 16 + 4 * part) = acc[m];
     __syncthreads();
-    const int m = t / 16, n = n0 + t % 16;
-    if (m >= M || n >= a.N) return;
+    static_assert(MT * 4 <= W, "a thread a sum");
+    const int n = n0 + t % 16, token = t / 16;
+    if (token >= M || n >= a.N) return;
     int s = 0;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) s += sums[i][t];
-    const float bias = a.bias ? element<T>(a.bias, n) : 0.0f;
-    store_element<T>(out, (long)m * a.out_row + n, finish<T, ACT>(s, scales[m] * kDown, a.w_scale[n] * kUp, bias));
+    for (int i = 0; i < W; ++i) s += sums[i * (MT * 256) + t];
+    const float bias = a.bias ? element<T>(a.bias, n) : 0.0f, ws = a.w_scale[n] * kUp;
+    store_element<T>(out, (m0 + token) * a.out_row + n, finish<T, ACT>(s, scales[token] * kDown, ws, bias));
+}
+
+template <class X, class T, int ACT, int MT, int W = 16>
+hipError_t few(const Linear8Call& a, const void* x, void* out, hipStream_t st)
+{
+    constexpr size_t kSums = (size_t)W * MT * 256 * 4;
+    const size_t steps = std::is_same<X, Int8>::value ? 0 : (size_t)a.M * steps_row(a.K);
+    const auto kernel = few_kernel<X, T, ACT, MT, W>;
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), std::max(kSums, (size_t)kFewLds));
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+    hipLaunchKernelGGL(kernel, grid, dim3(W * kWave), std::max(kSums, steps), st, a, static_cast<const uint8_t*>(x), out);
+    return hipGetLastError();
 }
 
 // ---- many tokens -------------------------------------------------------------------------
@@ -332,32 +383,36 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Writes NT channels' results of one token from channel i on, those below N. `whole`: all at once, past the L2: results that
-// stay there drive out the tokens and weights that the next tiles read (45920 x 4096 x 1024, bfloat16: 264 -> 224 us).
+// Writes NT channels' results of one token from channel i on, those below N, all at once where all are (rows may start at any
+// element), past the L2: results that stay there drive out the tokens and weights that the next tiles read (45920 x 4096 x
+// 1024, bfloat16: 264 -> 224 us).
 template <class T, int NT>
-__device__ __forceinline__ void write_channels(uint8_t* to, int i, int N, bool whole, const float (&v)[NT])
+__device__ __forceinline__ void write_channels(uint8_t* to, int i, int N, const float (&v)[NT])
 {
-    if (!whole || NT == 1) {
+    to += (long)i * T::kBytes;
+    if constexpr (NT * T::kBytes >= 4) {
+        constexpr int kWords = NT * T::kBytes / 4;
+        typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
+        typedef Words Anywhere __attribute__((aligned(T::kBytes)));
+        if (i + NT <= N) {
+            Words w;
 #pragma unroll
-        for (int e = 0; e < NT; ++e)
-            if (i + e < N) store_element<T>(to, i + e, v[e]);
-        return;
-    }
-    if (i >= N) return;
-    constexpr int kWords = NT * T::kBytes >= 4 ? NT * T::kBytes / 4 : 1;
-    typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
-    Words w;
-#pragma unroll
-    for (int e = 0; e < kWords; ++e) {
-        if constexpr (T::kBytes == 4) {
-            w[e] = __float_as_uint(v[e]);
-        } else if constexpr (NT > 1) {
-            typedef float f32x2 __attribute__((ext_vector_type(2)));
-            const f32x2 p = {v[2 * e], v[2 * e + 1]};
-            w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+            for (int e = 0; e < kWords; ++e) {
+                if constexpr (T::kBytes == 4) {
+                    w[e] = __float_as_uint(v[e]);
+                } else {
+                    typedef float f32x2 __attribute__((ext_vector_type(2)));
+                    const f32x2 p = {v[2 * e], v[2 * e + 1]};
+                    w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+                }
+            }
+            __builtin_nontemporal_store(w, reinterpret_cast<Anywhere*>(to));
+            return;
         }
     }
-    __builtin_nontemporal_store(w, reinterpret_cast<Words*>(to + (long)i * T::kBytes));
+#pragma unroll
+    for (int e = 0; e < NT; ++e)
+        if (i + e < N) store_element<T>(to, e, v[e]);
 }
 
 // The order of the tiles: columns of `wide` tiles of channels outside, then tokens, then the column's channels, so that a
@@ -398,7 +453,7 @@ __device__ __forceinline__ Share share(long tiles)
 template <int BM, int BN, int WM, int WN, int BK, int STAGES, class T, int ACT>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a, const uint8_t* __restrict__ q,
                                                                    const float* __restrict__ q_scale,
-                                                                   void* __restrict__ out, Order order, bool whole)
+                                                                   void* __restrict__ out, Order order)
 {
     constexpr int kWaves = WM * WN, THREADS = kWaves * kWave;
     constexpr int MT = BM / WM / 32, NT = BN / WN / 32;
@@ -602,7 +657,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a
 #pragma unroll
                     for (int n = 0; n < NT; ++n) v[n] = finish<T, ACT>(acc[n][m][4 * c + r], x[r], w[n], b[n]);
                     if (row + token < a.M)
-                        write_channels<T, NT>(to + token * a.out_row * T::kBytes, at, a.N, whole, v);
+                        write_channels<T, NT>(to + token * a.out_row * T::kBytes, at, a.N, v);
                 }
             }
     }
@@ -619,30 +674,52 @@ hipError_t product(const Linear8Call& a, const int8_t* q, const float* q_scale, 
     // As many workgroups as the chip holds (by LDS and by registers: two waves a SIMD).
     constexpr int kHeld = (int)std::min<size_t>((160 << 10) / bytes, 8 / (WM * WN) > 0 ? 8 / (WM * WN) : 1);
     const long slots = std::min(per, (long)kHeld * kUnits / kXcds);
-    // A lane's channels are written at once where they start at a multiple of their bytes in every row.
-    constexpr int NT = BN / WN / 32;
-    const bool whole =
-        a.N % NT == 0 && a.out_row % NT == 0 && reinterpret_cast<uintptr_t>(out) % (NT * T::kBytes) == 0;
     const int wide = (int)std::max(1L, std::min(ntiles, (long)kColumnBytes / ((long)BN * steps_row(a.K))));
     hipLaunchKernelGGL(kernel, dim3((unsigned)(slots * kXcds)), dim3(WM * WN * kWave), bytes, st, a,
-                       reinterpret_cast<const uint8_t*>(q), q_scale, out, Order{(int)mtiles, (int)ntiles, wide}, whole);
+                       reinterpret_cast<const uint8_t*>(q), q_scale, out, Order{(int)mtiles, (int)ntiles, wide});
     return hipGetLastError();
 }
 
 // The widest tiles that leave no compute unit idle: a tile of 256 x 256 loads half the bytes a product that one of 128 x 128
 // does, which loads half of what one of 64 x 64 does. Tiles of 128 x 256 leave room for two workgroups a compute unit, of
-// which one finishes its results beside the other's products: long rows need that least. Products (bfloat16 results, no
-// activation) in tiles of 64 / 128 / 128 x 256 / 256, us: 4103 x 150 x 848 6.2 / 9.7 / 18 / 21, 512 x 768 x 768 5.1 / 7.4 / -
-// / 15, 1024 x 2304 x 768 9.2 / 8.2 / - / 16, 20000 x 1024 x 1024 - / 33.0 / 33.4 / 36.7, 45888 x 2304 x 768 200 / 128 / 112 /
-// 117, 45920 x 1024 x 4096 370 / 210 / 214 / 182.
+// which one finishes its results beside the other's products: long rows need that least, and there the tiles of 256 x 256,
+// one a unit, are taken where they fill half a round of the chip to a whole one, or more than two (between one and two the
+// second round is mostly idle). Products (bfloat16 results, no activation), us in tiles of
+//                         64    64 x 128    128    128 x 256    256
+//     118 x 576 x 192      4.7     5.2      6.9       8.8       9.5
+//     4103 x 150 x 848     6.6     7.5     10.4      15.6      18.8
+//     1024 x 2304 x 768   10.7     8.0      9.1      11.7      14.1
+//     2000 x 1024 x 4096  17.8    15.2     27.4      31.4      47.9
+//     7000 x 768 x 3056   46.2    36.8     33.4      35.2      45.9
+//     8898 x 1024 x 2528  58.0    55.3     49.3      50.9      40.0
+//     45888 x 2304 x 768   200       -      128       112       117
+//     45920 x 1024 x 4096  370       -      210       214       182
+// Over 90 drawn shapes (32 to 46000 rows, 64 to 5000 channels, 256 to 4096 long) these bounds cost 0.6% against the best of
+// the five for each, and 20% at most.
 constexpr int kLongRows = 1024;
 template <class T, int ACT>
 hipError_t product_of(const Linear8Call& a, const int8_t* q, const float* q_scale, void* out, hipStream_t st)
 {
+    // Few tokens or channels: k is split over the waves of a workgroup, where tiles would leave most units idle and walk all
+    // of k in each. Such a workgroup has fewer loads on their way than it wants, so the smallest that fill the chip are
+    // taken; four token tiles pay for long rows only. Values to results in us, so / in tiles of 64: 17 x 2304 x 768 8.3 / 9.4,
+    // 63 x 88 x 3968 9.6 / 20.3, 128 x 1024 x 4096 12.3 / 21.6, 250 x 1024 x 4096 16.6 / 21.4, 250 x 192 x 768 9.1 / 10.4,
+    // with four token tiles 1000 x 256 x 256 7.7 / 7.3, 3000 x 64 x 2048 19.4 / 17.9.
+    auto groups = [&](int m) { return (long)((a.N + 15) / 16) * ((a.M + 16 * m - 1) / (16 * m)); };
+    if (groups(2) <= kUnits || (a.K > 2 * kLongRows && groups(4) <= kUnits)) {
+        Linear8Call of = a;
+        of.x_scale = q_scale;
+        if (groups(1) <= kUnits) return few<Int8, T, ACT, 1>(of, q, out, st);
+        if (groups(2) <= kUnits) return few<Int8, T, ACT, 2>(of, q, out, st);
+        return few<Int8, T, ACT, 4>(of, q, out, st);
+    }
     auto tiles = [&](int m, int n) { return (a.M + m - 1) / m * ((a.N + n - 1) / n); };
-    if (a.K > kLongRows && tiles(256, 256) >= 2 * kUnits) return product<256, 256, 4, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
+    const long area = a.M * (long)a.N / (256 * 256);
+    const bool fills = (area >= kUnits / 2 && area <= kUnits) || area >= 2 * kUnits;
+    if (a.K > kLongRows && fills) return product<256, 256, 4, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
     if (tiles(128, 256) >= 2 * kUnits) return product<128, 256, 2, 2, 64, 3, T, ACT>(a, q, q_scale, out, st);
-    if (tiles(128, 128) >= kUnits / 2) return product<128, 128, 2, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
+    if (tiles(128, 128) >= kUnits) return product<128, 128, 2, 2, 128, 2, T, ACT>(a, q, q_scale, out, st);
+    if (tiles(64, 64) > kUnits) return product<64, 128, 2, 2, 128, 3, T, ACT>(a, q, q_scale, out, st);
     return product<64, 64, 2, 2, 128, 3, T, ACT>(a, q, q_scale, out, st);
 }
 
@@ -673,21 +750,20 @@ hipError_t launch_quantize(const void* x, long R, int K, long x_row, int dt, int
 
 bool linear8_is_few(const Linear8Call& a)
 {
-    return a.M <= kFew && (a.x_dt == kI8 || a.M * steps_row(a.K) <= kFewLds);
+    return a.x_dt != kI8 && a.M <= kFew && a.M * steps_row(a.K) <= kFewLds;
 }
 
 hipError_t launch_linear8_few(const Linear8Call& a, const void* x, void* out, hipStream_t stream)
 {
-    const uint8_t* xp = static_cast<const uint8_t*>(x);
-    const dim3 grid((unsigned)((a.N + 15) / 16)), threads(kFewThreads);
-    const size_t bytes = a.x_dt == kI8 ? 0 : (size_t)a.M * steps_row(a.K);
     return with_kind(a, [&](auto type, auto act) {
         typedef decltype(type) T;
         constexpr int ACT = decltype(act)::value;
-        if (a.x_dt == kI8) hipLaunchKernelGGL((few_kernel<Int8, T, ACT>), grid, threads, bytes, stream, a, xp, out);
-        else if (a.x_dt == kBf16) hipLaunchKernelGGL((few_kernel<Bf16, T, ACT>), grid, threads, bytes, stream, a, xp, out);
-        else hipLaunchKernelGGL((few_kernel<F32, T, ACT>), grid, threads, bytes, stream, a, xp, out);
-        return hipGetLastError();
+        const bool short_rows = a.M <= 4 && steps_row(a.K) <= 4 * kFewAhead * 64;
+        auto of = [&](auto x_type) {
+            typedef decltype(x_type) X;
+            return short_rows ? few<X, T, ACT, 1, 4>(a, x, out, stream) : few<X, T, ACT, 1>(a, x, out, stream);
+        };
+        return a.x_dt == kBf16 ? of(Bf16{}) : of(F32{});
     });
 }
 
