@@ -126,6 +126,36 @@ def test_linear_many(dtype, M, N, K):
     near(got, q, s, w, ws, bias, "gelu", dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,N", [(901, 331), (2201, 603), (5003, 1100)])
+@pytest.mark.parametrize("K", [8, 72, 128, 264, 520])
+def test_linear_tiles(dtype, M, N, K):
+    """Batches of tiles that fill the chip in part, with ragged ends on all three sides."""
+    g = torch.Generator().manual_seed(M + K)
+    x = torch.randn((M, K), generator=g).to(dtype)
+    q, s = ref.steps(x.float())
+    w, ws = ref.steps(torch.randn((N, K), generator=g) * 0.1)
+    wd = torch.nn.functional.pad(w, (0, (K + 15) // 16 * 16 - K)).to(DEV)
+    got = mpm.linear_int8(x.to(DEV), wd, ws.to(DEV), activation="relu")
+    near(got, q, s, w, ws, None, "relu", dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 1024), (4, 33, 1032), (2, 24, 8200), (5, 20, 4104), (16, 19, 3008), (16, 18, 3088),
+                                   (31, 30, 2056), (200, 120, 2056), (521, 248, 2064), (300, 500, 4360), (250, 200, 16),
+                                   (1200, 16, 5000), (3000, 2901, 1032), (8200, 4100, 1040)])
+def test_linear_long(dtype, M, N, K):
+    """Long rows, with k split over waves and in the largest tiles."""
+    g = torch.Generator().manual_seed(M + K)
+    x = torch.randn((M, K), generator=g).to(dtype)
+    q, s = ref.steps(x.float())
+    w, ws = ref.steps(torch.randn((N, K), generator=g) * 0.1)
+    bias = torch.randn(N, generator=g).to(dtype)
+    wd = torch.nn.functional.pad(w, (0, (K + 15) // 16 * 16 - K)).to(DEV)
+    got = mpm.linear_int8(x.to(DEV), wd, ws.to(DEV), bias=bias.to(DEV), activation="silu")
+    near(got, q, s, w, ws, bias, "silu", dtype)
+
+
 @pytest.mark.parametrize("M", [3, 16, 40, 300])
 def test_extreme_steps(M):
     """Sums of the largest products stay whole: 65536 of (-128)^2 in 32 bits; the bytes past K have to be zero on one side."""
