@@ -486,8 +486,13 @@ def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="no
                          _device(weight_scale, "weight_scale", torch.float32, x, N),
                          _device(bias, "bias", out.dtype, x, N))
     if R and N:
-        # Room for the steps and scales of values: at least what mpm_linear_int8_workspace_bytes says, without the call.
-        need = 0 if x_scale is not None else R * weight.shape[1] + 4 * R + 512
+        # Few tokens may need no room, which costs more than the call that says so; otherwise at least what it would say.
+        if x_scale is not None:
+            need = 0
+        elif R <= 16:
+            need = _lib.load().mpm_linear_int8_workspace_bytes(_BYREF(c))
+        else:
+            need = R * weight.shape[1] + 4 * R + 512
         ws = _scratch(need, x)
         _launch("mpm_linear_int8", x, _BYREF(c), _ptr(x), _ptr(out), _ptr(ws), need)
     return out

@@ -4,6 +4,9 @@
 //   dx = rstd (gt - mean(gt) - t mean(gt t)),  dw = sum gz t,  db = sum gz.
 // A thread keeps one vector of 16 bytes of the channels and walks rows, so that sums are kept by channel
 // and groups of any width are sums over channels afterwards.
+// Memory bounds it. Slabs of whole groups that fit a workgroup's registers are read once, in one launch; otherwise chunks of
+// rows pass twice, with the parts of the sums joined between. 64 grids of 1024 x 768 in bfloat16 with SiLU 45 us, 4.5 TB/s; 16 of
+// 4096 x 1024, forward and backward, 199 us, 3.4 TB/s of the 671 MB of one reading and writing each way.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
