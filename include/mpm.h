@@ -737,7 +737,7 @@ int mpm_quantize_rows(const void* x, int32_t R, int32_t K, int64_t x_row, int32_
  *   w_scale: float[N]; bias (may be NULL): N values of dtype dt;
  *   out: row m at out + m * out_row elements, out_row >= N (any alignment of whole elements; rows of whole
  *     16 bytes are written fastest). out must not overlap the inputs.
- *   ws: mpm_linear_int8_workspace_bytes(call) bytes (0 for steps, and for few tokens), 256-byte aligned.
+ *   ws: mpm_linear_int8_workspace_bytes(call) bytes (0 for steps, and for few results), 256-byte aligned.
  * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned pointers (x, w: 16 bytes; w_scale, x_scale: 4; bias,
  * out: an element), sizes below 1, K or strides as above, bad dt, x_dt or act, x_scale that does not go with
  * x_dt; MPM_ERR_UNSUPPORTED for K > MPM_MAX_K8 or N > MPM_MAX_N8; MPM_ERR_WORKSPACE; MPM_ERR_HIP.

@@ -486,10 +486,10 @@ def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="no
                          _device(weight_scale, "weight_scale", torch.float32, x, N),
                          _device(bias, "bias", out.dtype, x, N))
     if R and N:
-        # Few tokens may need no room, which costs more than the call that says so; otherwise at least what it would say.
+        # Few results may need no room, which costs more than the call that says so; otherwise at least what it would say.
         if x_scale is not None:
             need = 0
-        elif R <= 16:
+        elif R <= 16 or R * N <= 65536:
             need = _lib.load().mpm_linear_int8_workspace_bytes(_BYREF(c))
         else:
             need = R * weight.shape[1] + 4 * R + 512

@@ -250,14 +250,13 @@ __device__ __forceinline__ float finish(int sum, float x_scale, float w_scale, f
 
 // ---- few tokens --------------------------------------------------------------------------
 
-constexpr int kFew = 16;           // tokens whose values become steps inside the product
-constexpr int kFewLds = 48 << 10;  // most bytes of such steps
+constexpr int kFewLds = 32 << 10;  // most bytes of steps made inside the product
 constexpr int kFewAhead = 4;       // pieces of 64 values a wave has on their way
 
 struct Int8 {};
 
 // A workgroup takes 16 output channels of 16 MT tokens, each of W waves every W-th piece of 64 values of k; the waves' sums
-// meet in LDS. X: the type of x; values (of at most W tokens) become steps in LDS first, in every workgroup by itself, while
+// meet in LDS. X: the type of x; values (16 tokens, at most W) become steps in LDS first, in every workgroup by itself, while
 // the first weights are on their way: a wave has one row or a slice of one. What bounds it is the latency of one pass over
 // its rows: from bfloat16 values to bfloat16 results, replayed without pauses, 1 x 2304 x 768 takes 4.0 us (W = 16 5.1, by
 // two launches 7.7), 16 x 4096 x 1024 7.5 (two launches 10.5), 8 x 1024 x 4096 10 (W = 4 22.9, two launches 19).
@@ -285,7 +284,7 @@ __global__ __launch_bounds__(W* kWave) void few_kernel(Linear8Call a, const uint
     if constexpr (kValues) {
         constexpr int kPer = 16 / X::kBytes, kWords = kPer / 4;
         const int slices = W / M, r = wave / slices, slice = wave - r * slices, vecs = a.K / kPer;
-        const uint8_t* from = x + (long)min(r, M - 1) * a.x_row * X::kBytes;
+        const uint8_t* from = x + (m0 + min(r, M - 1)) * a.x_row * X::kBytes;
         if (t < W) most[t] = 0;
         __syncthreads();
         uint32_t m = 0;
@@ -350,11 +349,14 @@ __global__ __launch_bounds__(W* kWave) void few_kernel(Linear8Call a, const uint
     store_element<T>(out, (m0 + token) * a.out_row + n, finish<T, ACT>(s, scales[token] * kDown, ws, bias));
 }
 
+// Its workgroups.
+long few_groups(const Linear8Call& a, int mt) { return (long)((a.N + 15) / 16) * ((a.M + 16 * mt - 1) / (16 * mt)); }
+
 template <class X, class T, int ACT, int MT, int W = 16>
 hipError_t few(const Linear8Call& a, const void* x, void* out, hipStream_t st)
 {
     constexpr size_t kSums = (size_t)W * MT * 256 * 4;
-    const size_t steps = std::is_same<X, Int8>::value ? 0 : (size_t)a.M * steps_row(a.K);
+    const size_t steps = std::is_same<X, Int8>::value ? 0 : (size_t)std::min(a.M, 16L) * steps_row(a.K);
     const auto kernel = few_kernel<X, T, ACT, MT, W>;
     constexpr size_t kMost = std::max(kSums, (size_t)kFewLds) + sizeof(float) * 16 * MT;
     const hipError_t e = allow_lds(reinterpret_cast<const void*>(kernel), kMost);
@@ -708,7 +710,7 @@ hipError_t product_of(const Linear8Call& a, const int8_t* q, const float* q_scal
     // taken; four token tiles pay for long rows only. Values to results in us, so / in tiles of 64: 17 x 2304 x 768 8.3 / 9.4,
     // 63 x 88 x 3968 9.6 / 20.3, 128 x 1024 x 4096 12.3 / 21.6, 250 x 1024 x 4096 16.6 / 21.4, 250 x 192 x 768 9.1 / 10.4,
     // with four token tiles 1000 x 256 x 256 7.7 / 7.3, 3000 x 64 x 2048 19.4 / 17.9.
-    auto groups = [&](int m) { return (long)((a.N + 15) / 16) * ((a.M + 16 * m - 1) / (16 * m)); };
+    auto groups = [&](int m) { return few_groups(a, m); };
     if (groups(2) <= kUnits || (a.K > 2 * kLongRows && groups(4) <= kUnits)) {
         Linear8Call of = a;
         of.x_scale = q_scale;
@@ -751,9 +753,14 @@ hipError_t launch_quantize(const void* x, long R, int K, long x_row, int dt, int
                        : quantize<F32>(xp, R, K, x_row, qp, scale, stream);
 }
 
+// Steps made inside the product: a launch less, for tokens that few workgroups read. Replayed without pauses, us, so / by two
+// launches: 64 x 1024 x 1024 7.7 / 9.4, 250 x 192 x 768 7.6 / 9.0, 4000 x 16 x 256 6.2 / 7.1, 8 x 1024 x 4096 10 / 10, 1000 x 64 x
+// 2048 11.9 / 10.2, beyond the bound 16 x 4096 x 4096 15.9 / 11.4, 250 x 256 x 4096 17.2 / 10.6; called one by one the
+// second launch takes 4 us of the host's time besides.
 bool linear8_is_few(const Linear8Call& a)
 {
-    return a.x_dt != kI8 && a.M <= kFew && a.M * steps_row(a.K) <= kFewLds;
+    return a.x_dt != kI8 && (a.M <= 16 || few_groups(a, 1) <= kUnits) &&
+           std::min(a.M, 16L) * steps_row(a.K) <= kFewLds;
 }
 
 hipError_t launch_linear8_few(const Linear8Call& a, const void* x, void* out, hipStream_t stream)

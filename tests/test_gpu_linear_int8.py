@@ -142,7 +142,7 @@ def test_linear_tiles(dtype, M, N, K):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("M,N,K", [(1, 40, 1024), (4, 33, 1032), (2, 24, 8200), (5, 20, 4104), (16, 19, 3008), (16, 18, 3088),
-                                   (31, 30, 2056), (200, 120, 2056), (521, 248, 2064), (300, 500, 4360), (250, 200, 16),
+                                   (31, 30, 2056), (200, 120, 2056), (521, 248, 2064), (300, 500, 4360), (250, 200, 16), (333, 100, 2040),
                                    (1200, 16, 5000), (3000, 2901, 1032), (8200, 4100, 1040)])
 def test_linear_long(dtype, M, N, K):
     """Long rows, with k split over waves and in the largest tiles."""
