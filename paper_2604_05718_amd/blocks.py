@@ -104,7 +104,9 @@ class _RotaryAttention(torch.autograd.Function):
     def forward(ctx, qkv, freq, heads, turn, where):
         H = heads
         qk = block_ops.rotary(qkv[:, :2 * H], freq, **turn)
-        out, lse = block_ops.attention(qk[:, :H], qk[:, H:], qkv[:, 2 * H:], with_lse=True, **where)
+        # (rows of no image are written by no kernel: what they hold would reach the weights' gradients, times zero)
+        out = torch.zeros_like(qk[:, :H], memory_format=torch.contiguous_format) if any(ctx.needs_input_grad) else None
+        out, lse = block_ops.attention(qk[:, :H], qk[:, H:], qkv[:, 2 * H:], with_lse=True, out=out, **where)
         # (offsets and positions too, so that a buffer written before the backward pass is noticed)
         ctx.tensors = [[n for n, t in d.items() if torch.is_tensor(t)] for d in (turn, where)]
         ctx.save_for_backward(qkv, qk, freq, out, lse, *(turn[n] for n in ctx.tensors[0]),
@@ -120,6 +122,7 @@ class _RotaryAttention(torch.autograd.Function):
         held = iter(tensors)
         turn, where = ({**rest, **{n: next(held) for n in names}} for rest, names in zip(ctx.rest, ctx.tensors))
         both = grad[:, :2 * H]
+        grad[:, 2 * H:].zero_()  # (rows of no image, which rotary_backward clears in the others)
         block_ops.attention_backward(dout.contiguous(), qk[:, :H], qk[:, H:], qkv[:, 2 * H:], out, lse, dq=grad[:, :H],
                                      dk=grad[:, H:2 * H], dv=grad[:, 2 * H:], **where)
         g = block_ops.rotary_backward(both, qkv[:, :2 * H] if learned else None, freq, dx=both, with_dfreq=learned, **turn)
@@ -132,7 +135,10 @@ class _GroupNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, groups, off, activation, eps):
         x = x.contiguous()
-        y, stats = block_ops.group_norm(x, groups, weight, bias, off=off, activation=activation, eps=eps, with_stats=True)
+        # (zeros in rows of no image, as in _RotaryAttention)
+        out = torch.zeros_like(x) if off is not None and any(ctx.needs_input_grad) else None
+        y, stats = block_ops.group_norm(x, groups, weight, bias, off=off, activation=activation, eps=eps, with_stats=True,
+                                        out=out)
         ctx.save_for_backward(x, stats, weight, bias, off)
         ctx.rest = dict(groups=groups, activation=activation, eps=eps)
         return y

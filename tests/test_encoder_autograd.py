@@ -22,9 +22,10 @@ class Operators:
         imgs = block_refs.images(kw["q_off"], 0, 2)
         return block_refs.attention(q, k, v, imgs, imgs, q.shape[-1] ** -0.5)[0]
 
-    def attention(self, q, k, v, with_lse=True, **kw):
+    def attention(self, q, k, v, with_lse=True, out=None, **kw):
         assert set(kw) == {"q_off", "k_off", "Nq", "Nk"}  # (no bias, no positions)
-        out = self.plain(q.detach(), k.detach(), v.detach(), kw)
+        assert out.shape == q.shape and out.is_contiguous() and not out.any()  # (rows of no image stay zero)
+        out.copy_(self.plain(q.detach(), k.detach(), v.detach(), kw))
         return out, torch.zeros(out.shape[:2] + (2,))
 
     def attention_backward(self, dout, q, k, v, out, lse, dq=None, dk=None, dv=None, **kw):
@@ -58,7 +59,7 @@ class Operators:
             parts = block_refs.images(off, 0, off.numel() - 1)
         return ref.group_norm(rows, groups, parts, w, b, activation, eps).view(x.shape)
 
-    def group_norm(self, x, groups, weight=None, bias=None, off=None, activation="none", eps=1e-5, with_stats=False):
+    def group_norm(self, x, groups, weight=None, bias=None, off=None, activation="none", eps=1e-5, with_stats=False, out=None):
         assert x.is_contiguous()
         y = self.group(x.detach(), groups, weight.detach(), bias.detach(), off, activation, eps)
         return y, torch.zeros(2, groups, 2)

@@ -6,6 +6,7 @@ import torch
 import block_refs
 import encoder_refs as ref
 import paper_2604_05718_amd as mpm
+from paper_2604_05718_amd import blocks
 from paper_2604_05718_amd.blocks import GridHead, RotaryEncoder
 
 pytestmark = pytest.mark.gpu
@@ -99,6 +100,39 @@ def test_gradients_of_the_head(packed):
         assert block_refs.rel(t.grad, p[n].grad) <= tol, n
 
 
+@pytest.mark.parametrize("learned", [False, True])
+def test_rows_behind_the_last_image(learned):
+    """A padded batch: rows of no image change no gradient, whatever memory held before. Float32, by the tolerance of
+    test_gradients_of_the_encoder (the products may be summed in another order)."""
+    torch.manual_seed(4)
+    ns, more, D = [30, 17, 33], 9, 48
+    grid = (8, 9)
+    enc = RotaryEncoder(D, 2, 2, grid, learned=learned, device=DEV, dtype=torch.float32)
+    head = GridHead(D, 64, 10, groups=8, device=DEV, dtype=torch.float32)
+    R = sum(ns)
+    pos = torch.cat([torch.randperm(72)[:n].sort().values for n in ns] + [torch.zeros(more, dtype=torch.int64)]).to(torch.int32)
+    x, g = torch.randn(R + more, D), torch.randn(R + more, 10)
+    g[R:] = 0
+    off = torch.cumsum(torch.tensor([0] + ns), 0).to(torch.int32).to(DEV)
+
+    def step(rows):
+        dirt = [torch.full((n,), float("nan"), device=DEV) for n in range(1000, 60000, 1000)]
+        del dirt  # (what new tensors hold)
+        xd = x[:rows].to(DEV).requires_grad_()
+        y = head(enc.rows(xd, off, max(ns), pos[:rows].to(DEV)), off)
+        params = {**{"enc." + n: t for n, t in enc.named_parameters()}, **{"head." + n: t for n, t in head.named_parameters()}}
+        grads = torch.autograd.grad((y[:R] * g[:R].to(DEV)).sum(), [xd, *params.values()])
+        return y[:R].detach(), grads[0], dict(zip(params, grads[1:]))
+
+    y, dx, grads = step(R)
+    yp, dxp, padded = step(R + more)
+    tol = 16 * 288 * 2.0 ** -24
+    assert block_refs.rel(yp, y.double().cpu()) <= tol and block_refs.rel(dxp[:R], dx.double().cpu()) <= tol
+    assert bool((dxp[R:] == 0).all())
+    for n, t in grads.items():
+        assert block_refs.rel(padded[n], t.double().cpu()) <= tol, n
+
+
 @pytest.mark.parametrize("grid", [(12, 20), (3, 8, 10)])
 def test_inference_between_merges(grid):
     """Merges before blocks 1 and 2, then the head: tokens of one cluster leave with one value; without merges the packed path
@@ -164,3 +198,43 @@ def test_training_step_under_bfloat16():
     y.float().square().mean().backward()
     for n, t in [*enc.named_parameters(), *head.named_parameters()]:
         assert t.grad is not None and t.grad.isfinite().all() and t.grad.any(), n
+
+
+def test_captured_gradients():
+    """Forward and backward of turned attention and the norm after it in one graph, replayed on new inputs between eager
+    work: the eager results, value for value."""
+    torch.manual_seed(6)
+    H, dh, C = 4, 32, 128
+    ns = [40, 0, 61]
+    R = sum(ns) + 5  # (five rows of no image)
+    off = torch.cumsum(torch.tensor([0] + ns), 0).to(torch.int32).to(DEV)
+    pos = torch.cat([torch.arange(n) for n in ns] + [torch.zeros(5)]).to(torch.int32).to(DEV)
+    turn = dict(pos=pos, grid=(8, 9), off=off)
+    where = dict(q_off=off, k_off=off, Nq=61, Nk=61)
+    freq = mpm.rotary_frequencies(dh // 2, 2).to(DEV).requires_grad_()
+    weight, bias = (torch.randn(C, device=DEV).to(torch.bfloat16).requires_grad_() for _ in range(2))
+    qkv = torch.randn((R, 3 * H, dh), device=DEV).to(torch.bfloat16).requires_grad_()
+    dy = torch.randn((R, C), device=DEV).to(torch.bfloat16)
+
+    def step():
+        a = blocks._RotaryAttention.apply(qkv, freq, H, turn, where)
+        y = blocks._GroupNorm.apply(a.view(R, C), weight, bias, 8, off, "silu", 1e-5)
+        return [y.detach(), *torch.autograd.grad(y, [qkv, freq, weight, bias], dy)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(4):
+        with torch.no_grad():
+            qkv.copy_(torch.randn_like(qkv) * (i + 1))
+            dy.copy_(torch.randn_like(dy))
+        graph.replay()
+        got = [t.clone() for t in held]
+        torch.cuda.synchronize()
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b), i
