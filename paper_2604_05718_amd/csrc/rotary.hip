@@ -5,8 +5,8 @@
 // frequencies) of c_a (x_1 dx_2 - x_2 dx_1), which needs no angle beside dx's.
 // Memory bounds it: a value is read once and written once, and the angles' sines are made once for all heads of a row, in
 // LDS, or by each thread where heads have frequencies of their own (three 64-bit multiply-adds a pair and axis, hidden behind
-// the loads). Queries and keys of 64 images of about 717 tokens, 12 heads of 64 each, bfloat16, in one launch: 53 us, 5.4 TB/s; of 8 clips
-// of about 5700, 16 heads each with frequencies of their own, 82 us and their gradients 105 + 8, 4.6 and 5.5 TB/s.
+// the loads). Queries and keys of 64 images of about 717 tokens, 12 heads of 64 each, bfloat16, in one launch: 53 us, 5.4 TB/s; of 8
+// clips of about 5700, 16 heads each with frequencies of their own, 73 us and their gradients 105 + 8, 5.2 and 5.5 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -338,7 +338,10 @@ __global__ __launch_bounds__(1024) void join_frequencies_kernel(const float* __r
     out[col] = (float)s;
 }
 
-constexpr int kGradGroups = 1024;  // workgroups of a backward pass with frequencies' gradients
+// Workgroups of a backward pass with frequencies' gradients, and of bfloat16 calls with frequencies by head, which a thread
+// then reads once for many rows: us so / with a workgroup a tile 45875 rows of 32 heads of 64 73 / 83 (512 workgroups 93),
+// of 24 59 / 71, 100000 of 8 of 128 86 / 118, 60000 of 4 of 32 10.8 / 10.8; float32, whose sines take longest, 57 / 52.
+constexpr int kGradGroups = 1024;
 
 // V pairs a vector.
 Deal deal(const RotaryCall& a, int V)
@@ -393,7 +396,8 @@ hipError_t launch_one(const RotaryCall& a, const HeadRows& src, const HeadRows& 
     const Deal d = deal(a, V);
     size_t bytes = (size_t)d.tile * 16 + (PER_HEAD ? 0 : (size_t)d.tile * a.pairs * 8);
     if (GRAD) bytes = std::max(bytes, (size_t)a.axes * V * d.threads * 4);
-    const long groups = GRAD ? grad_groups(d) : std::min(d.tiles, 1L << 22);  // (a grid holds 2^32 threads)
+    const bool keeps = GRAD || (PER_HEAD && S::kBytes == 2);
+    const long groups = keeps ? grad_groups(d) : std::min(d.tiles, 1L << 22);  // (a grid holds 2^32 threads)
     hipLaunchKernelGGL((rotary_kernel<S, V, HALVES, PER_HEAD, GRAD>), dim3((unsigned)groups, (unsigned)d.blocks),
                        dim3(d.threads), bytes, st, a, src, x, dst, inverse ? -1.0f : 1.0f, zero, d, parts);
     return hipGetLastError();

@@ -108,8 +108,10 @@ def test_linear_refuses_pointers(lib):
     go = lambda x=ptr(), out=ptr(), ws=ptr(), n=1 << 40: lib.mpm_linear_int8(R(c), x, out, ws, n, None)
     assert lib.mpm_linear_int8(None, ptr(), ptr(), None, 0, None) == INVALID
     assert go(x=None) == INVALID and go(x=ptr(P + 8)) == INVALID and go(out=None) == INVALID and go(out=ptr(P + 1)) == INVALID
+    assert lib.mpm_linear_int8_workspace_bytes(R(c)) == 0  # (few results)
+    c = linear(M=5000)
     need = lib.mpm_linear_int8_workspace_bytes(R(c))
-    assert need >= 100 * 64 + 400 and go(n=need - 1) == WORKSPACE and go(ws=None) == INVALID and go(ws=ptr(P + 64)) == INVALID
+    assert need >= 5000 * 64 + 20000 and go(n=need - 1) == WORKSPACE and go(ws=None) == INVALID and go(ws=ptr(P + 64)) == INVALID
     assert lib.mpm_linear_int8_workspace_bytes(R(linear(x_dt=2, x_scale=P))) == 0
 
 
