@@ -167,6 +167,44 @@ __device__ __forceinline__ bool image_index(const RotaryCall& a, long row, int* 
     return true;
 }
 
+// A workgroup's rows and heads.
+struct RowsAt {
+    long first;
+    int rows, head, heads;
+};
+
+// `many` bytes from `from` on of each head as they are (zeros in rows that are not turned, if they are written): a thread
+// has one piece of BYTES of a head and walks the rows. 40000 rows of 4 heads of 80 channels, 32 of them turned, 17.5 us (one word
+// of four bytes after another of all rows 31.7); 45875 of 24 of 64, half of them 81 (113).
+template <class S, int BYTES>
+__device__ __forceinline__ void pass_channels(const RotaryCall& a, const HeadRows& src, const HeadRows& dst, const RowsAt& at,
+                                              int from, int many, bool zero, const int* cells)
+{
+    typedef typename Piece<BYTES>::type Word;
+    const int words = many / BYTES, cols = min(at.heads, a.H - at.head) * words, threads = blockDim.x, t = threadIdx.x;
+    const int step = max(1, threads / cols), first = step > 1 ? t / cols : 0;  // rows at a time, and this thread's first
+    if (first >= step) return;
+    for (int c = t - first * cols; c < cols; c += step > 1 ? cols : threads) {
+        const int h = c / words;
+        const long in = from + (long)(c - h * words) * BYTES, head = at.head + h;
+        const uint8_t* p = src.p + (at.first * src.row + head * src.head) * S::kBytes + in;
+        uint8_t* q = dst.p + (at.first * dst.row + head * dst.head) * S::kBytes + in;
+        for (int r = first; r < at.rows; r += kAhead * step) {
+            Word w[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                w[u] = *reinterpret_cast<const Word*>(p + (long)min(r + u * step, at.rows - 1) * src.row * S::kBytes);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int row = r + u * step;
+                if (row >= at.rows) break;
+                const bool turned = cells[4 * row + 3];
+                if (turned || zero) *reinterpret_cast<Word*>(q + (long)row * dst.row * S::kBytes) = turned ? w[u] : Word{};
+            }
+        }
+    }
+}
+
 // GRAD: src is dout and x the forward call's rows; the workgroup's sums of c_a (x_1 dx_2 - x_2 dx_1) go to
 // parts[workgroup][head or 1][axis][pair]. `sign` turns the other way, `zero` writes zeros to rows of no image.
 template <class S, int V, bool HALVES, bool PER_HEAD, bool GRAD>
@@ -278,19 +316,13 @@ __global__ __launch_bounds__(kMaxThreads) void rotary_kernel(RotaryCall a, HeadR
                 }
             }
         }
-        // The channels that pass, in words of four bytes (two channels a pair: their start is a whole number).
-        const int words = (a.dh - 2 * a.pairs) * S::kBytes / 4, heads = d.cols / d.per_head;
-        if (words > 0 && (zero || src.p != dst.p)) {
-            const int many = rows * heads * words, h0 = blockIdx.y * heads;
-            for (int e = t; e < many; e += blockDim.x) {
-                const int r = e / (heads * words), rest = e - r * heads * words, h = h0 + rest / words, w = rest % words;
-                const bool turned = cells[4 * r + 3];
-                if (h >= a.H || (!turned && !zero)) continue;
-                const long row = r0 + r, off = 2 * a.pairs * S::kBytes + 4 * w;
-                const uint32_t v =
-                    *reinterpret_cast<const uint32_t*>(src.p + (row * src.row + h * src.head) * S::kBytes + off);
-                *reinterpret_cast<uint32_t*>(dst.p + (row * dst.row + h * dst.head) * S::kBytes + off) = turned ? v : 0;
-            }
+        // The channels that pass, in the widest pieces that their start and number allow (two channels a pair: four bytes).
+        const int from = 2 * a.pairs * S::kBytes, many = a.dh * S::kBytes - from;
+        if (many > 0 && (zero || src.p != dst.p)) {
+            const RowsAt at{r0, rows, (int)blockIdx.y * (d.cols / d.per_head), d.cols / d.per_head};
+            if ((from | many) % 16 == 0) pass_channels<S, 16>(a, src, dst, at, from, many, zero, cells);
+            else if ((from | many) % 8 == 0) pass_channels<S, 8>(a, src, dst, at, from, many, zero, cells);
+            else pass_channels<S, 4>(a, src, dst, at, from, many, zero, cells);
         }
     }
 
