@@ -983,8 +983,8 @@ bool joins_itself(const GroupNormCall& a, const Deal& d)
 
 // Whether a call goes by slabs: one launch that reads a tensor once (and once more what its threads do not keep), but a
 // workgroup works through its slab alone; or by passes over chunks of rows: two or three launches that read it twice. By an
-// estimate in us, from the times of both at 25 shapes (1 to 64 images of 100 to 9216 rows of 48 to 1024 channels): it takes the
-// slower one by more than a tenth at three of them, and by less than a quarter.
+// estimate in us, from the times of both at 25 shapes (1 to 64 images of 100 to 9216 rows of 48 to 1024 channels): of the 50,
+// both directions, it takes the slower one by more than a tenth at four, and by less than a quarter.
 bool by_slabs(const GroupNormCall& a, bool backward, const Plan& p)
 {
     const Slab& s = p.s;

@@ -6,7 +6,7 @@
 // Memory bounds it: a value is read once and written once, and the angles' sines are made once for all heads of a row, in
 // LDS, or by each thread where heads have frequencies of their own (three 64-bit multiply-adds a pair and axis, hidden behind
 // the loads). Queries and keys of 64 images of about 717 tokens, 12 heads of 64 each, bfloat16, in one launch: 53 us, 5.4 TB/s; of 8
-// clips of about 5700, 16 heads each with frequencies of their own, 73 us and their gradients 105 + 8, 5.2 and 5.5 TB/s.
+// clips of about 5700, 16 heads each with frequencies of their own, 75 us and their gradients 105 + 8, 5.1 and 5.5 TB/s.
 #include <algorithm>
 #include <type_traits>
 
