@@ -456,13 +456,24 @@ def quantize_rows(x):
     return q, scale
 
 
+def _meets(x, K, out, N):
+    """Whether rows of K values at x and rows of N at out, as many, share memory."""
+    a, b = K * x.element_size(), N * out.element_size()
+    row, ahead, rows = x.stride(0) * x.element_size(), out.data_ptr() - x.data_ptr(), x.shape[0] - 1
+    if ahead >= rows * row + a or -ahead >= rows * out.stride(0) * out.element_size() + b:
+        return False
+    between = ahead % row if row else 0  # (columns side by side in rows of one buffer)
+    return not (rows and row == out.stride(0) * out.element_size() and a <= between and between + b <= row)
+
+
 def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="none", dtype=None, out=None):
     """act(x weight^T + bias) in 8-bit integers with a scale for each token and output channel (mpm_linear_int8): [R, N].
 
     x: values [R, K] (float32 or bfloat16, row strides of whole 16 bytes), which are turned into steps on the way, or
     with ``x_scale`` the steps of quantize_rows. ``weight``, ``weight_scale``: quantize_rows of a weight [N, K].
     ``bias`` [N] and the result have ``dtype`` (that of x or of ``out``; bfloat16 for steps). ``activation``: "none", "relu",
-    "silu" or "gelu". ``out``: rows [R, N] with contiguous channels and a row stride of its own."""
+    "silu" or "gelu". ``out``: rows [R, N] with contiguous channels and a row stride of its own, apart
+    from x."""
     R, K, row = _value_rows(x, "x")
     if x_scale is None:
         x_dt = _dt(x)
@@ -480,6 +491,8 @@ def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="no
     elif out.shape != (R, N) or out.get_device() != x.get_device() or dtype not in (None, out.dtype) or (
             out.stride(1) != 1 and N > 1) or (R > 1 and out.stride(0) < N):
         raise ValueError(f"out must be [{R}, {N}] on {x.device} with contiguous channels")
+    elif R and N and _meets(x, K, out, N):
+        raise ValueError("out must not overlap x: other channels still read it")
     c = _lib.Linear8Call(R, N, K, x_dt, _dt(out), _one_of(_ACTIVATIONS, activation, "activation"), row,
                          out.stride(0) if R > 1 else N, _device(x_scale, "x_scale", torch.float32, x, R),
                          _device(weight, "weight", torch.int8, x),

@@ -295,6 +295,20 @@ def test_linear_binding(recorded):
     assert recorded.calls[3][0] == "mpm_quantize_rows" and mpm.quantize_rows(x[:0])[0].shape == (0, 48)
 
 
+@pytest.mark.parametrize("at,ok", [((0, 0), False), ((0, 34), False), ((0, 40), True), ((0, 58), True), ((4, 0), False),
+                                   ((4, 40), True), ((5, 0), True), ((5, 40), True)])
+def test_linear_out_beside_x(recorded, at, ok):
+    """out in the buffer of x: beside its columns or behind its rows, not on them."""
+    buffer = device(torch.zeros(10, 64, dtype=torch.bfloat16))
+    w, ws = device(torch.zeros(6, 48, dtype=torch.int8)), device(torch.zeros(6))
+    x, out = buffer[:5, :40], buffer[at[0]:at[0] + 5, at[1]:at[1] + 6]
+    if ok:
+        assert mpm.linear_int8(x, w, ws, out=out) is out and len(recorded.calls) == 1
+        return
+    with pytest.raises(ValueError, match="overlap"):
+        mpm.linear_int8(x, w, ws, out=out)
+
+
 def test_group_norm_binding(recorded):
     x, w = device(torch.zeros(2, 3, 5, 16)), device(torch.ones(16))
     y, stats = mpm.group_norm(x, 4, w, w, activation="silu", with_stats=True)
