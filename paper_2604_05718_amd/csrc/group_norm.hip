@@ -237,9 +237,45 @@ __device__ __forceinline__ double2 block_sum(int many, Use&& use)
     return r;
 }
 
-// Mean and reciprocal deviation of every image and group, a workgroup each.
+// A channel's parts of an image joined over its chunks, 16 channels a workgroup, 64 shares of the chunks each joined by a wave:
+// what enters its group's sums. firsts: the parts are moments (spread), otherwise sums.
+constexpr int kJoinWaves = kJoinThreads / kWave;
+__global__ __launch_bounds__(kJoinThreads) void join_chunks_kernel(GroupNormCall a, Deal d, const float2* __restrict__ parts,
+                                                                   const float* __restrict__ firsts,
+                                                                   double2* __restrict__ joined)
+{
+    __shared__ double2 lds[kWave][kJoinWaves + 1];
+    const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, local = t % kJoinWaves, way = t / kJoinWaves;
+    const int c0 = blockIdx.x * kJoinWaves, c = min(c0 + local, a.C - 1), width = a.C / a.groups;
+    for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
+        const Rows image = image_rows(a, b);
+        const int rows = (int)(image.end - image.first), size = chunk_size(d, rows);
+        const int chunks = !firsts ? d.chunks : rows > 0 ? (rows - 1) / size + 1 : 0;
+        double2 s = make_double2(0.0, 0.0);
+        const float* f = firsts ? firsts + (long)b * a.C : nullptr;
+        const double offset = firsts && rows > 0 ? (double)f[c] - (double)f[c / width * width] : 0.0;
+        const float2* at = parts + (long)b * d.chunks * a.C + c;
+#pragma unroll 4
+        for (int k = way; k < chunks; k += kWave) {
+            const float2 p = at[(long)k * a.C];
+            const double2 q = firsts ? spread(p, min(size, rows - k * size), offset) : make_double2((double)p.x, (double)p.y);
+            s.x += q.x;
+            s.y += q.y;
+        }
+        __syncthreads();  // the image before has been read
+        lds[way][local] = s;
+        __syncthreads();
+        const double2 own = lds[lane][wave];
+        s = make_double2(wave_sum(own.x), wave_sum(own.y));
+        if (lane == 0 && c0 + wave < a.C) joined[(long)b * a.C + c0 + wave] = s;
+    }
+}
+
+// Mean and reciprocal deviation of every image and group, a workgroup each; from the channels' joined parts where they are
+// given.
 __global__ __launch_bounds__(kJoinThreads) void group_stats_kernel(GroupNormCall a, Deal d, FixedDiv width_of,
                                                                const float2* __restrict__ parts,
+                                                               const double2* __restrict__ joined,
                                                                const float* __restrict__ firsts,
                                                                float2* __restrict__ stats)
 {
@@ -252,10 +288,11 @@ __global__ __launch_bounds__(kJoinThreads) void group_stats_kernel(GroupNormCall
         const float2* at = parts + (long)b * d.chunks * a.C + g * width;
         const double from = rows > 0 ? (double)f[0] : 0.0;
         const int chunks = rows > 0 ? (rows - 1) / size + 1 : 0;  // that have rows
-        const double2 s = block_sum(chunks * width, [&](int i) {
-            const int k = width_of(i), c = i - k * width;
-            return spread(at[(long)k * a.C + c], min(size, rows - k * size), (double)f[c] - from);
-        });
+        const double2 s = joined ? block_sum(rows > 0 ? width : 0, [&](int i) { return joined[(long)b * a.C + g * width + i]; })
+                                 : block_sum(chunks * width, [&](int i) {
+                                       const int k = width_of(i), c = i - k * width;
+                                       return spread(at[(long)k * a.C + c], min(size, rows - k * size), (double)f[c] - from);
+                                   });
         if (threadIdx.x == 0)
             stats[pair] = rows > 0 ? finished(a, (double)rows * width, from, s) : make_float2(0.0f, 0.0f);
     }
@@ -275,8 +312,8 @@ __device__ __forceinline__ GroupRange block_groups(const GroupNormCall& a, const
 // Channels of them that a workgroup joins by itself, at most.
 constexpr int kMostChannels = kThreads * 8;
 
-// Sums over the channels of each of a block's groups, `lanes` lanes a group (8 or 64): use(channel of the block's groups)
-// gives two numbers, write(group, sums) takes their sums.
+// Sums over the channels of each of a block's groups, `lanes` lanes a group (8 for many groups: 32 of 6 channels 11.5 us, with
+// 64 lanes 17.6): use(channel of the block's groups) gives two numbers, write(group, sums) takes their sums.
 template <class Use, class Write>
 __device__ __forceinline__ void over_channels(int groups, int width, Use&& use, Write&& write)
 {
@@ -451,13 +488,16 @@ __device__ __forceinline__ double2 weighted(const GroupNormCall& a, double2 q, i
 // From the channels' sums: the means of gt and gt t of every image and group, a workgroup each ...
 __global__ __launch_bounds__(kJoinThreads) void group_means_kernel(GroupNormCall a, Deal d, FixedDiv width_of,
                                                                const float2* __restrict__ parts,
+                                                               const double2* __restrict__ joined,
                                                                float2* __restrict__ means)
 {
     const int width = a.C / a.groups;
     for (long pair = blockIdx.x; pair < (long)a.B * a.groups; pair += gridDim.x) {
         const int b = (int)(pair / a.groups), g = (int)(pair % a.groups);
         const float2* at = parts + (long)b * d.chunks * a.C + g * width;
-        const double2 s = block_sum(d.chunks * width, [&](int i) {
+        const double2 s = joined ? block_sum(width, [&](int i) {
+            return weighted(a, joined[(long)b * a.C + g * width + i], g * width + i);
+        }) : block_sum(d.chunks * width, [&](int i) {
             const int k = width_of(i), c = i - k * width;
             const float2 q = at[(long)k * a.C + c];
             return weighted(a, make_double2((double)q.x, (double)q.y), g * width + c);
@@ -470,7 +510,6 @@ __global__ __launch_bounds__(kJoinThreads) void group_means_kernel(GroupNormCall
 }
 
 // ... and dw and db, 64 channels a workgroup, sixteen waves' shares of the items joined in order.
-constexpr int kJoinWaves = kJoinThreads / kWave;
 __global__ __launch_bounds__(kJoinThreads) void join_sums_kernel(const float2* __restrict__ parts, long items, int C,
                                                                       int dt, void* dw, void* db)
 {
@@ -972,13 +1011,34 @@ size_t parts_bytes(const GroupNormCall& a, const Deal& d) { return aligned256((s
 size_t firsts_bytes(const GroupNormCall& a) { return aligned256((size_t)a.B * a.C * 4); }
 size_t stats_bytes(const GroupNormCall& a) { return aligned256((size_t)a.B * a.groups * 8); }
 
-// Whether the second pass joins an image's parts by itself: a launch less, for up to so many of them.
+// Whether the second pass joins an image's parts by itself: a launch less, for up to so many of them. Forward and backward in us,
+// so / by another launch: 1 image of 300 x 192 10.0, 13.6 / 11.9, 16.3, 32 of 1000 x 48 12.7, 20.5 / 16.6, 24.3; beyond the
+// bound 1 of 9216 x 96 16.6, 22.2 / 12.8, 19.5.
 constexpr int kFewParts = 8192;
 bool joins_itself(const GroupNormCall& a, const Deal& d)
 {
     const int width = a.C / a.groups, own = d.cols * (a.dt == kBf16 ? 8 : 4);
     const int channels = d.blocks == 1 ? a.C : own + 2 * (width - 1);
     return (long)d.chunks * a.C <= kFewParts && channels <= kMostChannels;
+}
+
+// Whether the parts of a group are too many for one workgroup to join: its channels are joined over the chunks first, a launch
+// more. bfloat16 images, forward and backward in us, so / by one workgroup: 1 of 1000 x 4096 in 1 group 25, 36 / 252, 476; 1 of
+// 4096 x 1024 in 8 groups 24, 32 / 32, 55, in 16 23, 31 / 24, 39, in 32 (the bound) 23, 31 / 20, 32.
+constexpr long kMostJoined = 16384;
+bool joins_channels(const GroupNormCall& a, const Deal& d)
+{
+    return !joins_itself(a, d) && (long)d.chunks * (a.C / a.groups) > kMostJoined;
+}
+size_t joined_bytes(const GroupNormCall& a, const Deal& d)
+{
+    return joins_channels(a, d) ? aligned256((size_t)a.B * a.C * 16) : 0;
+}
+void join_channels(const GroupNormCall& a, const Deal& d, const float2* parts, const float* firsts, double2* joined,
+                   hipStream_t st)
+{
+    hipLaunchKernelGGL(join_chunks_kernel, dim3((unsigned)((a.C + kJoinWaves - 1) / kJoinWaves), (unsigned)std::min(a.B, 32768)),
+                       dim3(kJoinThreads), 0, st, a, d, parts, firsts, joined);
 }
 
 // Whether a call goes by slabs: one launch that reads a tensor once (and once more what its threads do not keep), but a
@@ -1052,15 +1112,19 @@ hipError_t forward_by_passes(const GroupNormCall& a, const void* x, void* y, flo
     float* firsts = reinterpret_cast<float*>(at + parts_bytes(a, d));
     float2* made = reinterpret_cast<float2*>(stats ? reinterpret_cast<char*>(stats)
                                                    : at + parts_bytes(a, d) + firsts_bytes(a));
+    double2* joined = joins_channels(a, d)
+                          ? reinterpret_cast<double2*>(at + parts_bytes(a, d) + firsts_bytes(a) + stats_bytes(a))
+                          : nullptr;
     const bool itself = joins_itself(a, d);
     const dim3 grid((unsigned)((long)a.B * d.chunks), (unsigned)d.blocks);
     const uint8_t* xp = static_cast<const uint8_t*>(x);
     return with_kind(a, [&](auto type, auto act) {
         typedef decltype(type) S;
         hipLaunchKernelGGL((channel_moments_kernel<S>), grid, dim3(kThreads), 0, st, a, d, xp, parts, firsts);
+        if (joined) join_channels(a, d, parts, firsts, joined, st);
         if (!itself)
             hipLaunchKernelGGL(group_stats_kernel, dim3(pair_groups(a)), dim3(kJoinThreads), 0, st, a, d,
-                               FixedDiv((uint32_t)(a.C / a.groups)), parts, firsts, made);
+                               FixedDiv((uint32_t)(a.C / a.groups)), parts, joined, firsts, made);
         hipLaunchKernelGGL((apply_kernel<S, decltype(act)::value>), grid, dim3(kThreads), 0, st, a, d, xp,
                            static_cast<uint8_t*>(y), itself ? nullptr : made, parts, firsts,
                            reinterpret_cast<float2*>(stats));
@@ -1098,6 +1162,9 @@ hipError_t backward_by_passes(const GroupNormCall& a, const void* dy, const void
     const Deal d = deal(a);
     float2* parts = static_cast<float2*>(ws);
     float2* means = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(a, d));
+    double2* joined = joins_channels(a, d)
+                          ? reinterpret_cast<double2*>(static_cast<char*>(ws) + parts_bytes(a, d) + stats_bytes(a))
+                          : nullptr;
     const float2* sp = reinterpret_cast<const float2*>(stats);
     const uint8_t *xp = static_cast<const uint8_t*>(x), *gp = static_cast<const uint8_t*>(dy);
     const bool itself = joins_itself(a, d);
@@ -1106,9 +1173,10 @@ hipError_t backward_by_passes(const GroupNormCall& a, const void* dy, const void
         typedef decltype(type) S;
         constexpr int ACT = decltype(act)::value;
         hipLaunchKernelGGL((channel_sums_kernel<S, ACT>), grid, dim3(kThreads), 0, st, a, d, gp, xp, sp, parts);
+        if (joined) join_channels(a, d, parts, nullptr, joined, st);
         if (!itself)
             hipLaunchKernelGGL(group_means_kernel, dim3(pair_groups(a)), dim3(kJoinThreads), 0, st, a, d,
-                               FixedDiv((uint32_t)(a.C / a.groups)), parts, means);
+                               FixedDiv((uint32_t)(a.C / a.groups)), parts, joined, means);
         hipLaunchKernelGGL((input_gradient_kernel<S, ACT>), grid, dim3(kThreads), 0, st, a, d, gp, xp,
                            static_cast<uint8_t*>(dx), sp, itself ? nullptr : means, parts);
         return hipGetLastError();
@@ -1121,7 +1189,8 @@ hipError_t backward_by_passes(const GroupNormCall& a, const void* dy, const void
 size_t group_norm_bytes(const GroupNormCall& a)
 {
     if (by_slabs(a, false, plan(a, false))) return 0;
-    return parts_bytes(a, deal(a)) + firsts_bytes(a) + stats_bytes(a);
+    const Deal d = deal(a);
+    return parts_bytes(a, d) + firsts_bytes(a) + stats_bytes(a) + joined_bytes(a, d);
 }
 
 hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, float* stats, void* ws, hipStream_t st)
@@ -1134,7 +1203,8 @@ hipError_t launch_group_norm(const GroupNormCall& a, const void* x, void* y, flo
 size_t group_norm_backward_bytes(const GroupNormCall& a)
 {
     if (by_slabs(a, true, plan(a, true))) return aligned256((size_t)a.B * a.C * 8);
-    return parts_bytes(a, deal(a)) + stats_bytes(a);
+    const Deal d = deal(a);
+    return parts_bytes(a, d) + stats_bytes(a) + joined_bytes(a, d);
 }
 
 hipError_t launch_group_norm_backward(const GroupNormCall& a, const void* dy, const void* x, const float* stats, void* dx,

@@ -44,6 +44,7 @@ SHAPES = [  # lengths, C, groups
     ((1,), 8, 1), ((1, 2, 1), 8, 8), ((5, 0, 17), 16, 2), ((64,), 32, 32), ((118,), 192, 32), ((70, 3, 200, 0), 72, 9),
     ((1024,), 192, 32), ((333, 1024), 768, 32), ((900,), 48, 3), ((50, 60), 264, 11), ((40,), 2056, 8), ((7, 9), 4104, 1),
     ((3,), 16384, 4), ((2500, 100), 24, 1), ((31,) * 20, 40, 5), ((2000, 4096), 64, 4), ((1200, 1), 1024, 32),
+    ((1500,), 1024, 1), ((700, 0, 900, 1), 2056, 2), ((2000, 30), 1032, 3),
 ]
 
 
