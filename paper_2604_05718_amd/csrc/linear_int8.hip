@@ -168,8 +168,9 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(const uint8_t* 
     }
 }
 
-// Wider rows, and few of more than four vectors a lane of half a wave: a workgroup each, read twice. 60 rows of 4096
-// bfloat16 values 4.8 us (in a wave each 7.7), 1000 7.0 (10.9), 1000 of 2048 7.0 (6.8).
+// Wider rows, and few of more than two vectors a lane of half a wave: a workgroup each, read twice. us so / in half a wave or a
+// wave each, bfloat16: 300 rows of 1024 values 3.3 / 6.3, 1000 3.6 / 5.4, 60 of 4096 4.8 / 7.7, 1000 7.0 / 10.9, of 2048 7.0 / 6.8.
+// (Half a wave a row for many: 45888 of 192 10.4, in a wave each 16.9; of 768 19.4 and 23.9.)
 constexpr int kFewRows = 1024;
 template <class S>
 __global__ __launch_bounds__(kQuantThreads) void quantize_wide_kernel(const uint8_t* __restrict__ x, long R, int K,
@@ -214,8 +215,8 @@ hipError_t quantize(const uint8_t* x, long R, int K, long x_row, uint8_t* q, flo
     constexpr std::integral_constant<int, kWave> wave{};
     if (vecs <= 32) rows(half, std::integral_constant<int, 1>{});
     else if (vecs <= 64) rows(half, std::integral_constant<int, 2>{});
-    else if (vecs <= 96) rows(half, std::integral_constant<int, 3>{});
-    else if (vecs <= 128) rows(half, std::integral_constant<int, 4>{});
+    else if (vecs <= 96 && R > kFewRows) rows(half, std::integral_constant<int, 3>{});
+    else if (vecs <= 128 && R > kFewRows) rows(half, std::integral_constant<int, 4>{});
     else if (vecs <= 256 && R > kFewRows) rows(wave, std::integral_constant<int, 4>{});
     else if (vecs <= 512 && R > kFewRows) rows(wave, std::integral_constant<int, 8>{});
     else hipLaunchKernelGGL((quantize_wide_kernel<S>), dim3((unsigned)std::min(R, kMostGroups)), dim3(kQuantThreads), 0, st, x, R,
@@ -258,8 +259,8 @@ struct Int8 {};
 // A workgroup takes 16 output channels of 16 MT tokens, each of W waves every W-th piece of 64 values of k; the waves' sums
 // meet in LDS. X: the type of x; values (16 tokens, at most W) become steps in LDS first, in every workgroup by itself, while
 // the first weights are on their way: a wave has one row or a slice of one. What bounds it is the latency of one pass over
-// its rows: from bfloat16 values to bfloat16 results, replayed without pauses, 1 x 2304 x 768 takes 4.0 us (W = 16 5.1, by
-// two launches 7.7), 16 x 4096 x 1024 7.5 (two launches 10.5), 8 x 1024 x 4096 10 (W = 4 22.9, two launches 19).
+// its rows: from bfloat16 values to bfloat16 results, replayed without pauses, 1 x 2304 x 768 takes 3.9 us (W = 16 5.1), 16 x
+// 4096 x 1024 7.4, 8 x 1024 x 4096 8.9 (W = 4 22.9, in tiles after quantising 19).
 template <class X, class T, int ACT, int MT, int W>
 __global__ __launch_bounds__(W* kWave) void few_kernel(Linear8Call a, const uint8_t* __restrict__ x, void* __restrict__ out)
 {
@@ -707,9 +708,8 @@ hipError_t product_of(const Linear8Call& a, const int8_t* q, const float* q_scal
 {
     // Few tokens or channels: k is split over the waves of a workgroup, where tiles would leave most units idle and walk all
     // of k in each. Such a workgroup has fewer loads on their way than it wants, so the smallest that fill the chip are
-    // taken; four token tiles pay for long rows only. Values to results in us, so / in tiles of 64: 17 x 2304 x 768 8.3 / 9.4,
-    // 63 x 88 x 3968 9.6 / 20.3, 128 x 1024 x 4096 12.3 / 21.6, 250 x 1024 x 4096 16.6 / 21.4, 250 x 192 x 768 9.1 / 10.4,
-    // with four token tiles 1000 x 256 x 256 7.7 / 7.3, 3000 x 64 x 2048 19.4 / 17.9.
+    // taken; four token tiles pay for long rows only. Values to results in us, so / in tiles of 64: 63 x 88 x 3968 9.6 / 20.3,
+    // 128 x 1024 x 4096 12.3 / 21.6, 250 x 1024 x 4096 16.6 / 21.4, 17 x 2304 x 768 8.3 / 9.4 (with slower steps), with four token tiles 1000 x 256 x 256 7.7 / 7.3, 3000 x 64 x 2048 19.4 / 17.9.
     auto groups = [&](int m) { return few_groups(a, m); };
     if (groups(2) <= kUnits || (a.K > 2 * kLongRows && groups(4) <= kUnits)) {
         Linear8Call of = a;
@@ -754,9 +754,9 @@ hipError_t launch_quantize(const void* x, long R, int K, long x_row, int dt, int
 }
 
 // Steps made inside the product: a launch less, for tokens that few workgroups read. Replayed without pauses, us, so / by two
-// launches: 64 x 1024 x 1024 7.7 / 9.4, 250 x 192 x 768 7.6 / 9.0, 4000 x 16 x 256 6.2 / 7.1, 8 x 1024 x 4096 10 / 10, 1000 x 64 x
-// 2048 11.9 / 10.2, beyond the bound 16 x 4096 x 4096 15.9 / 11.4, 250 x 256 x 4096 17.2 / 10.6; called one by one the
-// second launch takes 4 us of the host's time besides.
+// launches: 1 x 2304 x 768 3.9 / 6.3, 100 x 512 x 512 6.2 / 7.9, 4000 x 16 x 256 6.3 / 7.1, 64 x 1024 x 1024 7.6 / 7.5, 8 x 1024 x
+// 4096 8.9 / 8.9, 250 x 256 x 2048 11.1 / 8.4, beyond the bound 16 x 4096 x 4096 15.9 / 11.4; called one by one the second
+// launch takes 4 us of the host's time besides (250 x 192 x 768 10.5 / 14.5).
 bool linear8_is_few(const Linear8Call& a)
 {
     return a.x_dt != kI8 && (a.M <= 16 || few_groups(a, 1) <= kUnits) &&
