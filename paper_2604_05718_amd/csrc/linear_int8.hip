@@ -709,7 +709,8 @@ hipError_t product_of(const Linear8Call& a, const int8_t* q, const float* q_scal
     // Few tokens or channels: k is split over the waves of a workgroup, where tiles would leave most units idle and walk all
     // of k in each. Such a workgroup has fewer loads on their way than it wants, so the smallest that fill the chip are
     // taken; four token tiles pay for long rows only. Values to results in us, so / in tiles of 64: 63 x 88 x 3968 9.6 / 20.3,
-    // 128 x 1024 x 4096 12.3 / 21.6, 250 x 1024 x 4096 16.6 / 21.4, 17 x 2304 x 768 8.3 / 9.4 (with slower steps), with four token tiles 1000 x 256 x 256 7.7 / 7.3, 3000 x 64 x 2048 19.4 / 17.9.
+    // 128 x 1024 x 4096 12.3 / 21.6, 250 x 1024 x 4096 16.6 / 21.4, 17 x 2304 x 768 8.3 / 9.4;
+    // with four token tiles 1000 x 256 x 256 7.7 / 7.3, 3000 x 64 x 2048 19.4 / 17.9.
     auto groups = [&](int m) { return few_groups(a, m); };
     if (groups(2) <= kUnits || (a.K > 2 * kLongRows && groups(4) <= kUnits)) {
         Linear8Call of = a;
