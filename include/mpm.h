@@ -702,8 +702,10 @@ int mpm_rotary_backward(const mpm_rotary_call* call, const mpm_heads* dout, cons
 typedef enum {
     MPM_ACT_NONE = 0,
     MPM_ACT_RELU = 1, /* max(z, 0); slope 0 at 0 */
-    MPM_ACT_SILU = 2, /* z / (1 + e^-z) */
-    MPM_ACT_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
+    MPM_ACT_SILU = 2, /* z / (1 + e^-z), the exponential within (1 + |z|) 2^-23 of itself */
+    /* z (1 + erf(z / sqrt 2)) / 2. For results (or gradients) of dtype bfloat16 the factor of z is a fit, within
+     * 2^-17 + z^2 2^-22 of itself down to z = -11 and 2^-100 of the result below; its slope uses the same factor. */
+    MPM_ACT_GELU = 3
 } mpm_activation;
 
 #define MPM_I8 2           /* signed 8-bit steps, as mpm_quantize_rows writes them (an mpm_dtype of x only) */
