@@ -584,8 +584,12 @@ typedef enum {
  *   post_w, post_b: the norm after this block (post_w NULL: none);
  *   scale (may be NULL): the residual scale;
  *   gate (may be NULL): gate_per_row 0: one row an image, [B][D], the rows of image b given by
- *     off (int32[B+1]; NULL: R / B rows each); gate_per_row 1: [R][D] (B and off are not used).
+ *     off (int32[B+1]; NULL: R / B rows each); gate_per_row 1: [R][D] (B and off are not used);
+ *   clear: what becomes of the rows outside every image (with a gate by image and off): 0: they are not written;
+ *     MPM_CLEAR_ROWS: zeros in h, dx and df, and with MPM_CLEAR_SUM in y as well (which must not be x then).
  */
+#define MPM_CLEAR_ROWS 1
+#define MPM_CLEAR_SUM 2
 typedef struct mpm_norm_call {
     int32_t R, D, dt, kind;
     float eps;
@@ -597,6 +601,7 @@ typedef struct mpm_norm_call {
     const void* post_b;
     const void* scale;
     const void* gate;
+    int32_t clear;
 } mpm_norm_call;
 
 /*
@@ -605,10 +610,10 @@ typedef struct mpm_norm_call {
  * in float32 with y and h rounded once to dt (h is of the sum before y's rounding).
  *   h: NULL if and only if w is; y may alias x;
  *   stats (may be NULL): float[R][4], (mean, 1 / deviation) of f and of y, for the gradients.
- * Rows outside every image (with a gate by image and off) are not written.
+ * Rows outside every image (with a gate by image and off) are written only as `clear` says.
  * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned (16-byte) pointers, sizes below 1, D as for
  * tokens, eps < 0 or not finite, a shift without its weight, B that does not divide R (gate by image,
- * off NULL), bad dt or kind; MPM_ERR_UNSUPPORTED for D > MPM_MAX_D or B > MPM_MAX_B; MPM_ERR_HIP.
+ * off NULL), bad dt, kind or clear, MPM_CLEAR_SUM with y at x; MPM_ERR_UNSUPPORTED for D > MPM_MAX_D or B > MPM_MAX_B; MPM_ERR_HIP.
  */
 int mpm_residual_norm(const mpm_norm_call* call, const void* x, const void* f, void* y, void* h, float* stats,
                       void* stream);

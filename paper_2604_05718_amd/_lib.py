@@ -27,6 +27,8 @@ MPM_SCHEDULE_FULL_64 = 3
 MPM_NORM_LAYER = 0
 MPM_NORM_RMS = 1
 MPM_MAX_SPAN = 63
+MPM_CLEAR_ROWS = 1
+MPM_CLEAR_SUM = 2
 MPM_I8 = 2
 MPM_ROTARY_HALVES = 0
 MPM_ROTARY_PAIRS = 1
@@ -59,7 +61,7 @@ class NormCall(ctypes.Structure):
     """mpm_norm_call."""
     _fields_ = [(n, _i32) for n in ("R", "D", "dt", "kind")] + [("eps", ctypes.c_float)] + [
         (n, _i32) for n in ("B", "gate_per_row")] + [
-        (n, _vp) for n in ("off", "w", "b", "post_w", "post_b", "scale", "gate")]
+        (n, _vp) for n in ("off", "w", "b", "post_w", "post_b", "scale", "gate")] + [("clear", _i32)]
 
 
 class NormGrads(ctypes.Structure):

@@ -258,8 +258,10 @@ def residual_norm(x, f, weight=None, bias=None, post_weight=None, post_bias=None
     x, f: rows [R, D]. ``weight`` / ``bias``: the norm before the next block; ``post_weight`` /
     ``post_bias``: the norm after this one (None: none); ``norm``: "layer" or "rms"; ``scale`` [D];
     ``gate``: [R, D], a row a token, or [B, D], a row an image, image b holding rows off[b] ...
-    off[b + 1] (``off`` None: R / B rows each). ``out``: y's tensor (x itself, say)."""
+    off[b + 1] (``off`` None: R / B rows each; rows of no image are zeros, in a given ``out`` as they were).
+    ``out``: y's tensor (x itself, say)."""
     c = _norm_call(x, weight, bias, post_weight, post_bias, scale, gate, off, norm, eps)
+    c.clear = _lib.MPM_CLEAR_ROWS | (_lib.MPM_CLEAR_SUM if out is None else 0)
     fp = _device(f, "f", x.dtype, x, x.numel())
     y = torch.empty_like(x) if out is None else out
     h = torch.empty_like(x) if weight is not None else None
@@ -286,8 +288,10 @@ class NormGradients:
 def residual_norm_backward(dy, dh, y, f, stats, weight=None, bias=None, post_weight=None, post_bias=None, scale=None,
                            gate=None, off=None, norm="layer", eps=1e-6) -> NormGradients:
     """The gradients of residual_norm() (mpm_residual_norm_backward) from dy (None: zero) and dh (None
-    without ``weight``), the stored y, f and stats; the gradient of each parameter that is given."""
+    without ``weight``), the stored y, f and stats; the gradient of each parameter that is given; zeros in rows of no
+    image."""
     c = _norm_call(y, weight, bias, post_weight, post_bias, scale, gate, off, norm, eps)
+    c.clear = _lib.MPM_CLEAR_ROWS
     n = y.numel()
     g = NormGradients(torch.empty_like(y), torch.empty_like(y),
                       *(None if t is None else torch.empty_like(t)

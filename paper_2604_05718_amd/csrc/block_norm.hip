@@ -151,6 +151,25 @@ __device__ __forceinline__ Item item_rows(const NormCall& a, long i)
     return Item{first + n * c / a.chunks, first + n * (c + 1) / a.chunks, b};
 }
 
+// Zeros in this workgroup's share of the rows of no image, of p and q (null: not asked for).
+template <class S, int LANES, int VPL>
+__device__ __forceinline__ void clear_rest(const NormCall& a, void* p, void* q)
+{
+    typedef RawPart<S, LANES, VPL> Raw;
+    if (!a.off || (!p && !q)) return;
+    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    const long lo = min(max((long)a.off[0], 0L), (long)a.R), hi = min(max((long)a.off[a.B], lo), (long)a.R);
+    const long many = lo + a.R - hi, end = many * (blockIdx.x + 1L) / gridDim.x;
+    float none[Raw::kVals];
+#pragma unroll
+    for (int e = 0; e < Raw::kVals; ++e) none[e] = 0.0f;
+    for (long r = many * blockIdx.x / gridDim.x + sub; r < end; r += threads<LANES>() / LANES) {
+        const long row = r < lo ? r : r - lo + hi;
+        if (p) Raw::store(none, p, row, a.D, lane);
+        if (q) Raw::store(none, q, row, a.D, lane);
+    }
+}
+
 // Mean and reciprocal deviation of a row's values (rms: mean 0).
 template <class S, int LANES, int VPL>
 __device__ __forceinline__ void row_stats(const float (&x)[RawPart<S, LANES, VPL>::kVals], int D, int lane, bool layer,
@@ -191,6 +210,7 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_kernel(NormCall a, cons
     __shared__ float lds[2 * threads<LANES>() / kWave];
     constexpr int kRows = threads<LANES>() / LANES, kVals = Raw::kVals;
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, D = a.D;
+    clear_rest<S, LANES, VPL>(a, a.clear_sum ? y : nullptr, a.clear ? hout : nullptr);
     const Item it = item_rows(a, blockIdx.x);
     if (it.first >= it.end) return;
     Raw fn, xn, pw, pb, sc, ga, w, b;
@@ -286,6 +306,7 @@ __global__ __launch_bounds__(threads<LANES>()) void norm_backward_kernel(
     __shared__ float lds[threads<LANES>()];
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES, D = a.D;
     const float inv = 1.0f / (float)D, centred = a.layer ? inv : 0.0f;
+    if (a.clear) clear_rest<S, LANES, VPL>(a, dx, df);
     float sw[kVals], sb[kVals], sa[kVals], sg[kVals];  // sa, sg: A and B
 #pragma unroll
     for (int e = 0; e < kVals; ++e) sw[e] = sb[e] = sa[e] = sg[e] = 0.0f;

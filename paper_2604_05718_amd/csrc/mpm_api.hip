@@ -401,6 +401,7 @@ int check_norm(const mpm_norm_call* c)
     if (c->kind != MPM_NORM_LAYER && c->kind != MPM_NORM_RMS) return MPM_ERR_INVALID_ARG;
     if (c->D % (c->dt == MPM_BF16 ? 8 : 4) != 0 || !finite(c->eps) || c->eps < 0.0f) return MPM_ERR_INVALID_ARG;
     if ((c->b && !c->w) || (c->post_b && !c->post_w)) return MPM_ERR_INVALID_ARG;
+    if (c->clear & ~(MPM_CLEAR_ROWS | MPM_CLEAR_SUM)) return MPM_ERR_INVALID_ARG;
     for (const void* p : {c->w, c->b, c->post_w, c->post_b, c->scale, c->gate})
         if (!ok_opt_rows_ptr(p)) return MPM_ERR_INVALID_ARG;
     if (c->gate && !c->gate_per_row) {
@@ -417,7 +418,7 @@ mpm::NormCall norm_call(const mpm_norm_call* c)
     const int B = by_image ? c->B : 1;
     return mpm::NormCall{c->R, c->D, B, c->R / B, 1, c->dt, c->kind == MPM_NORM_LAYER, c->eps,
                          by_image ? c->off : nullptr, c->w, c->b, c->post_w, c->post_b, c->scale, c->gate,
-                         c->gate && c->gate_per_row};
+                         c->gate && c->gate_per_row, (c->clear & MPM_CLEAR_ROWS) != 0, (c->clear & MPM_CLEAR_SUM) != 0};
 }
 
 // Checked mode: the offsets of a gate by image.
@@ -978,7 +979,7 @@ int mpm_residual_norm(const mpm_norm_call* call, const void* x, const void* f, v
     const int s = check_norm(call);
     if (s != MPM_OK) return s;
     if (!ok_rows_ptr(x) || !ok_rows_ptr(f) || !ok_rows_ptr(y) || !aligned(h, 16) || !aligned(stats, 16) ||
-        (h == nullptr) != (call->w == nullptr))
+        (h == nullptr) != (call->w == nullptr) || ((call->clear & MPM_CLEAR_SUM) && y == x))
         return MPM_ERR_INVALID_ARG;
     const mpm::NormCall a = norm_call(call);
     MPM_LAUNCH_GATE();

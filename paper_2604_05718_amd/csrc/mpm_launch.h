@@ -188,6 +188,7 @@ struct NormCall {
     const int32_t* off;
     const void *w, *b, *post_w, *post_b, *scale, *gate;
     bool gate_rows;  // one gate row a token instead of one an image
+    bool clear, clear_sum;  // rows of no image: zeros in h, dx and df; in y
 };
 struct NormGrads {
     void *dx, *df, *dw, *db, *dpost_w, *dpost_b, *dscale, *dgate;
