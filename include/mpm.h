@@ -501,6 +501,8 @@ typedef struct mpm_heads {
  *     merged rows the log of the tokens they stand for). A key with -inf is dropped: its rows of
  *     k and v take no part, whatever they hold, and their gradients are zero. A constant: no
  *     gradient is computed for it.
+ *   q_rows, k_rows: with q_off (k_off), how many rows out and dq (dk and dv) have if those of no image, before off[0]
+ *     and from off[B] on, are to get zeros; 0: they are not written.
  */
 typedef struct mpm_attention_call {
     int32_t B, Nq, Nk, H, Hk, dh, dt;
@@ -512,6 +514,7 @@ typedef struct mpm_attention_call {
     const int32_t* q_pos;
     const int32_t* k_pos;
     const float* k_bias;
+    int32_t q_rows, k_rows;
 } mpm_attention_call;
 
 /*
@@ -529,7 +532,7 @@ typedef struct mpm_attention_call {
  *   ws: device workspace of mpm_attention_workspace_bytes(call) bytes (0 for many shapes: may be
  *     NULL then), 256-byte aligned, used where few queries have their keys split over workgroups.
  * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned pointers, sizes below 1, dh, H or strides as
- * above, bad dt, a span, grid or scale outside its range; MPM_ERR_UNSUPPORTED for B, Nq, Nk,
+ * above, bad dt, a span, grid or scale outside its range, q_rows or k_rows below 0; MPM_ERR_UNSUPPORTED for B, Nq, Nk,
  * H or dh above their maxima; MPM_ERR_WORKSPACE; MPM_ERR_HIP.
  */
 size_t mpm_attention_workspace_bytes(const mpm_attention_call* call);
@@ -542,7 +545,7 @@ int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_
  *     that share a key head;
  *   dbias (may be NULL; only with bias): float[H][W][W], the sum of the score gradients of every
  *     pair at each offset, over all images (mpm_bias_gradient takes it to the table's).
- * Rows of dq, dk and dv that exist are all written. Results do not depend on the order workgroups run in.
+ * Rows of dq, dk and dv that belong to an image are all written. Results do not depend on the order workgroups run in.
  * dbias is summed in 64-bit integers of a unit found for every image and head: score gradients below 2^-40
  * of the largest there are lost. One that is not finite makes all of its head's dbias NaN.
  * ws: mpm_attention_backward_workspace_bytes(call) bytes. With a bias most of them are dbias's partial

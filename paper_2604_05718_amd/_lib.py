@@ -54,7 +54,7 @@ class AttentionCall(ctypes.Structure):
     """mpm_attention_call."""
     _fields_ = [(n, _i32) for n in ("B", "Nq", "Nk", "H", "Hk", "dh", "dt")] + [("scale", ctypes.c_float)] + [
         (n, _vp) for n in ("q_off", "k_off", "bias")] + [(n, _i32) for n in ("span", "grid_h", "grid_w")] + [
-        (n, _vp) for n in ("q_pos", "k_pos", "k_bias")]
+        (n, _vp) for n in ("q_pos", "k_pos", "k_bias")] + [(n, _i32) for n in ("q_rows", "k_rows")]
 
 
 class NormCall(ctypes.Structure):

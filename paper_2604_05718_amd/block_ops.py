@@ -162,20 +162,22 @@ def bias_gradient(dbias, lut, nb: int, dtype=torch.float32, out=None):
 
 
 def attention(q, k, v, q_off=None, k_off=None, Nq=None, Nk=None, scale=None, bias=None, q_pos=None, k_pos=None,
-              grid=None, k_bias=None, with_lse=False, out=None):
+              grid=None, k_bias=None, with_lse=False, out=None, clear=False):
     """softmax(scale q k^T + bias + k_bias) v of each image (mpm_attention): [R, H, dh] (or q's dense
     shape), and with ``with_lse`` the softmax statistics that attention_backward needs: float32
     [R, H, 2], the maximum taken and the log of the sum, base 2 (their sum times ln 2 is the log-sum-exp).
 
     ``scale``: default dh ** -0.5. ``bias``: float32 [H, W, W] from bias_expand, with ``grid`` the
     (rows, columns) of the token grid and ``q_pos`` / ``k_pos`` the raster positions, int32 per row
-    (None: each row's index in its image). ``k_bias``: float32 per key row, -inf drops a key."""
+    (None: each row's index in its image). ``k_bias``: float32 per key row, -inf drops a key. ``clear``: zeros in the rows
+    of ``out`` that belong to no image, which are otherwise left as they are."""
     c, hq, hk, hv = _call(q, k, v, q_off, k_off, Nq, Nk, scale, bias, q_pos, k_pos, grid, k_bias)
     if out is None:
         out = q.new_empty(q.shape)
     rows = _rows_of(q)
     ho = _heads(out, "out", q, rows, c.H)
     lse = torch.empty((rows, c.H, 2), dtype=torch.float32, device=q.device) if with_lse else None
+    c.q_rows = rows if clear else 0
     if rows == 0:
         return (out, lse) if with_lse else out
     lib = _lib.load()
@@ -196,10 +198,11 @@ class AttentionGrads:
 
 def attention_backward(dout, q, k, v, out, lse, q_off=None, k_off=None, Nq=None, Nk=None, scale=None, bias=None,
                        q_pos=None, k_pos=None, grid=None, k_bias=None, dq=None, dk=None, dv=None,
-                       with_dbias=True) -> AttentionGrads:
+                       with_dbias=True, clear=False) -> AttentionGrads:
     """The gradients of attention() (mpm_attention_backward) from dout and the call's own inputs, out
     and lse. ``dq``, ``dk``, ``dv``: where to write them (views of a fused projection's gradient,
-    say); ``with_dbias`` False leaves out the bias's gradient."""
+    say); ``with_dbias`` False leaves out the bias's gradient; ``clear``: zeros in the rows of dq, dk and dv that belong
+    to no image."""
     c, hq, hk, hv = _call(q, k, v, q_off, k_off, Nq, Nk, scale, bias, q_pos, k_pos, grid, k_bias)
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if g is None else g
                   for g, t in ((dq, q), (dk, k), (dv, v)))
@@ -207,6 +210,7 @@ def attention_backward(dout, q, k, v, out, lse, q_off=None, k_off=None, Nq=None,
     hs = [_heads(dout, "dout", q, rq, c.H), hq, hk, hv, _heads(out, "out", q, rq, c.H)]
     gs = [_heads(dq, "dq", q, rq, c.H), _heads(dk, "dk", q, rk, c.Hk), _heads(dv, "dv", q, rk, c.Hk)]
     dbias = torch.empty_like(bias) if bias is not None and with_dbias else None
+    c.q_rows, c.k_rows = (rq, rk) if clear else (0, 0)
     if rq == 0:  # no query: the sums over them are empty
         for t in (dk, dv, dbias):
             if t is not None:

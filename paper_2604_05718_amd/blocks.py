@@ -52,7 +52,8 @@ class _Attention(torch.autograd.Function):
         H = heads
         q, k, v = qkv[:, :H], qkv[:, H:2 * H], qkv[:, 2 * H:]
         bias = block_ops.bias_expand(table, lut)
-        out, lse = block_ops.attention(q, k, v, bias=bias, with_lse=True, **where)
+        # (rows of no image: zeros, since what they hold reaches the weights' gradients, times zero)
+        out, lse = block_ops.attention(q, k, v, bias=bias, with_lse=True, clear=True, **where)
         # (the call's offsets and positions too, so that a buffer written before the backward pass is noticed)
         ctx.tensors = [n for n, t in where.items() if torch.is_tensor(t)]
         ctx.save_for_backward(qkv, table, bias, lut, out, lse, *(where[n] for n in ctx.tensors))
@@ -67,7 +68,7 @@ class _Attention(torch.autograd.Function):
         parts = [slice(0, H), slice(H, 2 * H), slice(2 * H, 3 * H)]
         g = block_ops.attention_backward(dout.contiguous(), *(qkv[:, p] for p in parts), out, lse, bias=bias,
                                          dq=grad[:, parts[0]], dk=grad[:, parts[1]], dv=grad[:, parts[2]],
-                                         with_dbias=learned, **ctx.rest, **dict(zip(ctx.tensors, tensors)))
+                                         with_dbias=learned, clear=True, **ctx.rest, **dict(zip(ctx.tensors, tensors)))
         dtable = block_ops.bias_gradient(g.dbias, lut, ctx.buckets, dtype=table.dtype) if learned else None
         return *_once((grad, dtable), dout, qkv, table), None, None, None
 
@@ -122,9 +123,8 @@ class _RotaryAttention(torch.autograd.Function):
         held = iter(tensors)
         turn, where = ({**rest, **{n: next(held) for n in names}} for rest, names in zip(ctx.rest, ctx.tensors))
         both = grad[:, :2 * H]
-        grad[:, 2 * H:].zero_()  # (rows of no image, which rotary_backward clears in the others)
         block_ops.attention_backward(dout.contiguous(), qk[:, :H], qk[:, H:], qkv[:, 2 * H:], out, lse, dq=grad[:, :H],
-                                     dk=grad[:, H:2 * H], dv=grad[:, 2 * H:], **where)
+                                     dk=grad[:, H:2 * H], dv=grad[:, 2 * H:], clear=True, **where)
         g = block_ops.rotary_backward(both, qkv[:, :2 * H] if learned else None, freq, dx=both, with_dfreq=learned, **turn)
         return *_once((grad, g.dfreq), dout, qkv, freq), None, None, None
 

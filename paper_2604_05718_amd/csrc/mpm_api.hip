@@ -345,6 +345,7 @@ int check_attention(const mpm_attention_call* c)
     if (c->dt != MPM_F32 && c->dt != MPM_BF16) return MPM_ERR_INVALID_ARG;
     if (c->dh % (c->dt == MPM_BF16 ? 8 : 4) != 0 || c->H % c->Hk != 0 || !finite(c->scale)) return MPM_ERR_INVALID_ARG;
     if (!ok_opt_int_ptr(c->q_off) || !ok_opt_int_ptr(c->k_off) || !ok_opt_int_ptr(c->k_bias)) return MPM_ERR_INVALID_ARG;
+    if (c->q_rows < 0 || c->k_rows < 0) return MPM_ERR_INVALID_ARG;
     if (c->bias) {
         if (!aligned(c->bias, 4) || !ok_opt_int_ptr(c->q_pos) || !ok_opt_int_ptr(c->k_pos)) return MPM_ERR_INVALID_ARG;
         if (c->span < 0 || c->span > MPM_MAX_SPAN || c->grid_h < 1 || c->grid_w < 1 || c->grid_h > MPM_MAX_N ||
@@ -371,6 +372,18 @@ int check_workspace(const void* ws, size_t ws_bytes, size_t need)
     if (need == 0) return MPM_OK;
     if (ws == nullptr || !aligned(ws, kAlign)) return MPM_ERR_INVALID_ARG;
     return ws_bytes < need ? MPM_ERR_WORKSPACE : MPM_OK;
+}
+
+// Zeros in the rows of no image where the call asks for them: of q-sided tensors (out or dq), dk and dv.
+hipError_t clear_attention(const mpm_attention_call* c, const mpm_heads* q, const mpm_heads* dk, const mpm_heads* dv,
+                           hipStream_t st)
+{
+    mpm::ClearRows rows[3];
+    int n = 0;
+    if (c->q_off && c->q_rows) rows[n++] = {c->q_off, c->B, c->q_rows, c->H, heads(q)};
+    for (const mpm_heads* x : {dk, dv})
+        if (x && c->k_off && c->k_rows) rows[n++] = {c->k_off, c->B, c->k_rows, c->Hk, heads(x)};
+    return n ? mpm::launch_clear_rows(rows, n, c->dh, c->dt, st) : hipSuccess;
 }
 
 // Checked mode: the packed offsets of queries and keys.
@@ -924,6 +937,8 @@ int mpm_attention(const mpm_attention_call* call, const mpm_heads* q, const mpm_
     MPM_LAUNCH_GATE();
     MPM_DATA_CHECK(checked_attention(call, as_stream(stream)));
     const mpm::AttentionCall a = attention_call(call);
+    const hipError_t e = clear_attention(call, out, nullptr, nullptr, as_stream(stream));
+    if (e != hipSuccess) return hip_status(e);
     if (mpm::attention_is_few(a))
         return hip_status(mpm::launch_attention_few(a, heads(q), heads(k), heads(v), heads(out), lse, ws,
                                                     as_stream(stream)));
@@ -949,6 +964,8 @@ int mpm_attention_backward(const mpm_attention_call* call, const mpm_heads* dout
     if ((s = check_workspace(ws, ws_bytes, mpm::attention_backward_bytes(a, dbias))) != MPM_OK) return s;
     MPM_LAUNCH_GATE();
     MPM_DATA_CHECK(checked_attention(call, as_stream(stream)));
+    const hipError_t e = clear_attention(call, dq, dk, dv, as_stream(stream));
+    if (e != hipSuccess) return hip_status(e);
     return hip_status(mpm::launch_attention_backward(a, heads(dout), heads(q), heads(k), heads(v), heads(out), lse,
                                                      heads(dq), heads(dk), heads(dv), dbias, ws, as_stream(stream)));
 }

@@ -156,6 +156,16 @@ inline int bias_kind(const AttentionCall& a)
 // Lets a kernel take `bytes` of dynamic LDS (more than 64 KB has to be asked for).
 hipError_t allow_lds(const void* kernel, size_t bytes);
 
+// Zeros in the rows of no image of n (at most 3) tensors of R rows of H heads of dh values.
+struct ClearRows {
+    const int32_t* off;
+    int B;
+    long R;
+    int H;
+    HeadRows x;
+};
+hipError_t launch_clear_rows(const ClearRows* c, int n, int dh, int dt, hipStream_t stream);
+
 // Attention; lse (may be null) receives [row][head] pairs: the maximum taken and the log of the sum, base 2.
 hipError_t launch_attention(const AttentionCall& a, const HeadRows& q, const HeadRows& k, const HeadRows& v,
                             const HeadRows& out, float* lse, hipStream_t stream);

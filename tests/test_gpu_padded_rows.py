@@ -5,7 +5,7 @@ import torch
 
 import block_refs
 import paper_2604_05718_amd as mpm
-from paper_2604_05718_amd.blocks import GridHead, RotaryEncoder
+from paper_2604_05718_amd.blocks import GridHead, RelativeEncoder, RotaryEncoder
 
 pytestmark = pytest.mark.gpu
 
@@ -61,7 +61,38 @@ def test_norms_with_a_gate_by_image(dtype, D, ns, before, behind):
             assert block_refs.rel(a, b.double().cpu()) <= 2 * half + 2 * 8 * (n + 16) * 2.0 ** -24
 
 
-ENCODERS = {"rotary": lambda D, grid: RotaryEncoder(D, 2, 2, grid, learned=True, device=DEV, dtype=torch.float32)}
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("H,Hk", [(4, 4), (6, 2)])
+@pytest.mark.parametrize("ns,before,behind", [([50, 0, 90], 3, 6), ([1], 0, 1), ([2, 3], 1, 0), ([400], 200, 300), ([6], 0, 0)])
+def test_attention(dtype, H, Hk, ns, before, behind):
+    """attention() and its gradients into columns of wider rows, with and without `clear`; few and many queries."""
+    g = torch.Generator().manual_seed(H)
+    n, R, dh = sum(ns), sum(ns) + before + behind, 32
+    off = torch.cumsum(torch.tensor([before] + ns), 0).to(torch.int32).to(DEV)
+    where = dict(q_off=off, k_off=off, Nq=max(ns), Nk=max(ns))
+    rows = torch.randn((R, H + 2 * Hk, dh), generator=g).to(dtype).to(DEV)
+    dout = torch.randn((R, H, dh), generator=g).to(dtype).to(DEV)
+    for t in (rows, dout):
+        t[:before] = NAN
+        t[before + n:] = NAN
+    q, k, v = rows[:, :H], rows[:, H:H + Hk], rows[:, H + Hk:]
+    inside, res = slice(before, before + n), {}
+    for clear in (True, False):
+        wide = torch.full((R, H + 1, dh), 7.0, device=DEV, dtype=dtype)
+        out, lse = mpm.attention(q, k, v, with_lse=True, out=wide[:, :H], clear=clear, **where)
+        grad = torch.full((R, H + 2 * Hk + 1, dh), 7.0, device=DEV, dtype=dtype)
+        mpm.attention_backward(dout, q, k, v, out, lse, dq=grad[:, :H], dk=grad[:, H:H + Hk], dv=grad[:, H + Hk:-1],
+                               clear=clear, **where)
+        assert bool((wide[:, H:] == 7).all() and (grad[:, -1:] == 7).all())  # (the columns beside them)
+        for t in (wide[:, :H], grad[:, :-1]):
+            assert bool((t[:before] == (0 if clear else 7)).all() and (t[before + n:] == (0 if clear else 7)).all())
+        res[clear] = wide[inside], grad[inside]
+    for a, b in zip(res[True], res[False]):
+        assert a.isfinite().all() and torch.equal(a, b)
+
+
+ENCODERS = {"rotary": lambda D, grid: RotaryEncoder(D, 2, 2, grid, learned=True, device=DEV, dtype=torch.float32),
+            "relative": lambda D, grid: RelativeEncoder(D, 2, 2, grid, device=DEV, dtype=torch.float32)}
 
 
 @pytest.mark.parametrize("gated", [True, False])
