@@ -781,7 +781,8 @@ typedef struct mpm_group_norm_call {
 } mpm_group_norm_call;
 
 /*
- * Forward: statistics and the rest in float32, y rounded once to dt; y may be x itself. Rows of no image are
+ * Forward: statistics and the rest in float32, y rounded once to dt; y may be x itself. A NaN or an infinity among a
+ * group's values leaves NaN in all of them; so may finite values 2^60 and more away from its mean. Rows of no image are
  * not written. stats (may be NULL): float[B][groups][2], mean and 1 / deviation (zeros for an empty image).
  * Backward, from dy, x and stats: dx (zeros in rows of no image; may be dy or x itself), and dw, db (C values of
  * dtype dt, each asked for if and only if w, b is given), summed over the images in a fixed order.

@@ -98,6 +98,14 @@ __device__ __forceinline__ Place place(const Deal& d)
     return p;
 }
 
+// A sum of squares that rounding may have left below zero. (max() would drop a NaN, which an infinity among the values has
+// to leave in every value of its group)
+template <class F>
+__device__ __forceinline__ F not_negative(F v)
+{
+    return v < 0 ? 0 : v;
+}
+
 // Mean and squared deviations of every channel over an item's rows: parts[item][C] pairs, the mean less the channel's value
 // in the image's first row, firsts[image][C], so that a mean far from zero beside the deviations costs no digits.
 // A thread takes its values from the mean of its own first rows, R: with S and Q the sums of x - R and its square,
@@ -158,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void channel_moments_kernel(GroupNormCall
 #pragma unroll
         for (int e = 0; e < kPer; ++e)
             lds[e][threadIdx.x] = make_float2(fmaf(sum[e], inv, ref[e] - zero.get(e)),
-                                              fmaxf(fmaf(-sum[e] * inv, sum[e], sq[e]), 0.0f));
+                                              not_negative(fmaf(-sum[e] * inv, sum[e], sq[e])));
     }
     __syncthreads();
     // The threads' parts of each channel, in order.
@@ -207,7 +215,7 @@ __device__ __forceinline__ double2 spread(float2 part, int n, double offset)
 // A group's mean and reciprocal deviation from its sums.
 __device__ __forceinline__ float2 finished(const GroupNormCall& a, double count, double from, double2 s)
 {
-    const double m2 = fmax(s.y - s.x * s.x / count, 0.0);
+    const double m2 = not_negative(s.y - s.x * s.x / count);
     return make_float2((float)(from + s.x / count), (float)(1.0 / sqrt(m2 / count + (double)a.eps)));
 }
 
