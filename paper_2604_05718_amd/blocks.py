@@ -159,6 +159,19 @@ class _Products(torch.nn.Module):
         super().__init__()
         self.steps = {}
 
+    def _exact(self):
+        """Tensors that stay float32 when the module changes its type, since the kernels take them so."""
+        return []
+
+    def _apply(self, fn, recurse=True):
+        exact = [t for t in self._exact() if t is not None]
+
+        def convert(t):
+            new = fn(t)
+            return t.to(new.device) if any(t is e for e in exact) and new.dtype is not t.dtype else new
+
+        return super()._apply(convert, recurse)
+
     @torch.no_grad()
     def quantize(self):
         """From now on the products run in 8-bit integers, with a scale for each token and output channel, from the
@@ -234,7 +247,7 @@ class RotaryBlock(_Block):
     learned, by ones of its own for every head that start there."""
 
     def __init__(self, D: int, heads: int, freq, learned: bool = False, device="cuda", dtype=torch.bfloat16):
-        super().__init__(D, heads, device, dtype, freq=freq.to(device), learned=learned)
+        super().__init__(D, heads, device, dtype, freq=freq.to(device, torch.float32), learned=learned)
 
     def _positions(self, weight, freq, learned):
         self.learned = learned
@@ -242,6 +255,9 @@ class RotaryBlock(_Block):
             self.freq = torch.nn.Parameter(freq.repeat(self.heads, 1, 1))
         else:
             self.register_buffer("freq", freq)
+
+    def _exact(self):
+        return [*super()._exact(), self.freq, self.freq.grad]
 
     def _attend(self, qkv, lut, where):
         freq = torch.cat([self.freq, self.freq]) if self.learned else self.freq  # (queries' heads, then keys')

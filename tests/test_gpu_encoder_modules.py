@@ -1,0 +1,33 @@
+"""The encoder's modules after a change of type, device or weights, on the GPU."""
+import pytest
+import torch
+
+from paper_2604_05718_amd.blocks import RotaryEncoder
+
+pytestmark = pytest.mark.gpu
+
+DEV = torch.device("cuda:0")
+GRID, NS, D = (8, 9), [40, 23], 32
+
+
+def batch(dtype):
+    g = torch.Generator().manual_seed(3)
+    pos = torch.cat([torch.randperm(72, generator=g)[:n].sort().values for n in NS]).to(torch.int32).to(DEV)
+    off = torch.tensor([0, 40, 63], dtype=torch.int32, device=DEV)
+    return torch.randn((63, D), generator=g).to(dtype).to(DEV), off, max(NS), pos
+
+
+@pytest.mark.parametrize("learned", [True, False])
+def test_converted(learned):
+    """A float32 encoder turned into bfloat16 computes what a bfloat16 one with its parameters does, gradients too."""
+    torch.manual_seed(1)
+    enc = RotaryEncoder(D, 4, 2, GRID, learned=learned, device=DEV, dtype=torch.float32)
+    other = RotaryEncoder(D, 4, 2, GRID, learned=learned, device=DEV)
+    enc.to(torch.bfloat16)
+    other.load_state_dict(enc.state_dict())
+    res = []
+    for m in (enc, other):
+        y = m.rows(*batch(torch.bfloat16))
+        y.float().square().mean().backward()
+        res.append([y.detach(), *(t.grad for t in m.parameters())])
+    assert len(res[0]) > 20 and all(torch.equal(a, b) and a.isfinite().all() for a, b in zip(*res))
