@@ -157,11 +157,11 @@ class _Products(torch.nn.Module):
 
     def __init__(self):
         super().__init__()
-        self.steps = {}
+        self.quantized = self._stale = False  # (stale: the weights were loaded since)
 
     def _exact(self):
         """Tensors that stay float32 when the module changes its type, since the kernels take them so."""
-        return []
+        return [getattr(self, n + "_step_scale") for n in self.PRODUCTS] if self.quantized else []
 
     def _apply(self, fn, recurse=True):
         exact = [t for t in self._exact() if t is not None]
@@ -175,17 +175,31 @@ class _Products(torch.nn.Module):
     @torch.no_grad()
     def quantize(self):
         """From now on the products run in 8-bit integers, with a scale for each token and output channel, from the
-        weights as they are now; without gradients. Returns the module."""
-        self.steps = {n: block_ops.quantize_rows(getattr(self, n).t().contiguous()) for n in self.PRODUCTS}
+        weights as they are now; without gradients. The steps move with the module; they are no part of its state, and are
+        made again from weights that load_state_dict() brings. Returns the module."""
+        for n in self.PRODUCTS:
+            steps, scale = block_ops.quantize_rows(getattr(self, n).t().contiguous())
+            self.register_buffer(n + "_steps", steps, persistent=False)
+            self.register_buffer(n + "_step_scale", scale, persistent=False)
+        self.quantized, self._stale = True, False
         return self
 
+    def _load_from_state_dict(self, *args, **kwargs):
+        super()._load_from_state_dict(*args, **kwargs)
+        self._stale = self.quantized
+
     def product(self, name, x, activation="none"):
-        if not self.steps:
+        if not self.quantized:
             y = x @ getattr(self, name)
             return torch.nn.functional.gelu(y) if activation == "gelu" else y
         if torch.is_grad_enabled():
             raise RuntimeError("products in 8-bit integers have no gradients: run them under torch.no_grad()")
-        return block_ops.linear_int8(x, *self.steps[name], activation=activation)
+        if self._stale:
+            if x.is_cuda and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("weights were loaded since quantize(): their steps have to be made before a capture")
+            self.quantize()
+        return block_ops.linear_int8(x, getattr(self, name + "_steps"), getattr(self, name + "_step_scale"),
+                                     activation=activation)
 
 
 class _Block(_Products):

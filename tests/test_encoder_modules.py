@@ -4,7 +4,7 @@ import copy
 import pytest
 import torch
 
-from paper_2604_05718_amd import blocks
+from paper_2604_05718_amd import block_ops, blocks
 
 CONVERSIONS = {"to": lambda m: m.to(torch.bfloat16), "bfloat16": lambda m: m.bfloat16(), "half": lambda m: m.half(),
                "double": lambda m: m.double(), "and_back": lambda m: m.bfloat16().float()}
@@ -36,3 +36,54 @@ def test_frequencies_stay_float32(name, learned):
 def test_frequencies_of_another_type():
     b = blocks.RotaryBlock(32, 2, torch.rand(2, 8, dtype=torch.float64), device="cpu")
     assert b.freq.dtype is torch.float32
+
+
+@pytest.fixture
+def served(monkeypatch):
+    """Stand-ins of the 8-bit operators: the weights' rows as steps, by twos."""
+    monkeypatch.setattr(block_ops, "quantize_rows", lambda w: ((w * 2).to(torch.int8), torch.full((w.shape[0],), 0.5)))
+    monkeypatch.setattr(block_ops, "linear_int8", lambda x, w, s, activation="none": (x.float() @ w.float().t()) * s)
+
+
+def modules(dtype=torch.float32):
+    torch.manual_seed(1)
+    enc = blocks.RotaryEncoder(16, 2, 1, (4, 5), device="cpu", dtype=dtype)
+    return enc, enc.blocks[0], blocks.GridHead(16, 24, 5, groups=4, device="cpu", dtype=dtype)
+
+
+def test_steps_follow_the_module(served):
+    """To another device and through another type: the steps and their float32 scales as they were."""
+    enc, blk, head = modules()
+    keys = [list(m.state_dict()) for m in (blk, head)]
+    for m in (enc.quantize(), head.quantize()):
+        m.bfloat16()
+    assert [list(m.state_dict()) for m in (blk, head)] == keys
+    for m in (blk, head):
+        for n in m.PRODUCTS:
+            steps, scale = getattr(m, n + "_steps"), getattr(m, n + "_step_scale")
+            assert steps.dtype is torch.int8 and scale.dtype is torch.float32 and bool((scale == 0.5).all())
+            assert steps.shape == getattr(m, n).t().shape
+    copied = copy.deepcopy(blk)
+    assert torch.equal(copied.qkv_steps, blk.qkv_steps) and copied.quantized
+    for m in (enc, head):
+        m.to("meta")
+    assert blk.fc1_steps.is_meta and blk.fc1_step_scale.is_meta and head.inner_steps.is_meta
+
+
+def test_steps_of_loaded_weights(served):
+    """Weights that are loaded after quantize(), into the module or into one around it, are the ones that are served."""
+    enc, blk, head = modules()
+    enc.quantize()
+    x = torch.randn(3, 16)
+    state = {n: t.round() + 3 if t.dim() == 2 else t for n, t in enc.state_dict().items()}
+    with torch.no_grad():
+        old = blk.product("qkv", x)
+        enc.load_state_dict(state)
+        new = blk.product("qkv", x)
+        assert torch.allclose(new, x @ state["blocks.0.qkv"]) and not torch.allclose(new, old)
+        steps = blk.qkv_steps
+        blk.product("qkv", x)
+        assert blk.qkv_steps is steps  # (made once)
+        plain = modules()[1]
+        plain.load_state_dict(blk.state_dict())
+        assert not plain.quantized and torch.equal(plain.product("qkv", x), x @ blk.qkv)

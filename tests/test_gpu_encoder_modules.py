@@ -31,3 +31,18 @@ def test_converted(learned):
         y.float().square().mean().backward()
         res.append([y.detach(), *(t.grad for t in m.parameters())])
     assert len(res[0]) > 20 and all(torch.equal(a, b) and a.isfinite().all() for a, b in zip(*res))
+
+
+def test_served_after_a_change():
+    """The products in 8 bits of a module that moved to the host and back, and of one that loaded other weights."""
+    torch.manual_seed(2)
+    enc, other = (RotaryEncoder(D, 4, 2, GRID, device=DEV) for _ in range(2))
+    at = batch(torch.bfloat16)
+    with torch.no_grad():
+        want = [m.rows(*at) for m in (enc.quantize(), other.quantize())]
+        assert not torch.equal(*want)
+        assert torch.equal(enc.cpu().to(DEV).rows(*at), want[0])
+        enc.load_state_dict(other.state_dict())
+        with pytest.raises(RuntimeError, match="before a capture"), torch.cuda.graph(torch.cuda.CUDAGraph()):
+            enc.blocks[0].product("qkv", at[0])
+        assert torch.equal(enc.rows(*at), want[1])
