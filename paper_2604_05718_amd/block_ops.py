@@ -395,6 +395,32 @@ def _written(t, what, ref, c):
     return h
 
 
+def _share(a, b, c, size):
+    """Whether two tensors of a rotary call (their heads, values of `size` bytes) share memory."""
+    if c.R == 0:
+        return False
+    row, head, dh = a.row * size, a.head * size, c.dh * size
+    ends = [h.p + ((c.R - 1) * h.row + (c.H - 1) * h.head + c.dh) * size for h in (a, b)]
+    if ends[0] <= b.p or ends[1] <= a.p:
+        return False
+    if (a.row, a.head) != (b.row, b.head):
+        return True  # (nested, or in an order of their own)
+    # A head of one meets a head of the other where their distance, less whole rows and heads, is under a head.
+    for j in range(1 - c.H, c.H):
+        off = b.p - a.p - j * head
+        i = off // row if row else 0
+        if any(abs(off - k * row) < dh for k in (i, i + 1) if abs(k) < c.R):
+            return True
+    return False
+
+
+def _in_place_or_apart(what, to, given, c, t):
+    """Refuses a tensor that is written and meets another one (`given`: name -> heads) elsewhere than on every value."""
+    for name, h in given.items():
+        if (to.p, to.row, to.head) != (h.p, h.row, h.head) and _share(to, h, c, t.element_size()):
+            raise ValueError(f"{what} overlaps {name}: it must be {name} itself or lie apart")
+
+
 def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=False, out=None):
     """Rows of heads with every pair of channels turned by its row's place on a grid (mpm_rotary): the shape of x.
 
@@ -404,12 +430,13 @@ def rotary(x, freq, pos=None, grid=(1,), layout="halves", off=None, inverse=Fals
     of the axes, (rows, columns) or (frames, rows, columns); ``pos``: int32 raster index of each row (None:
     each row's index in its image; without ``off``, packed rows are one image). ``layout``: pair p is channels
     p and p + pairs ("halves") or 2 p and 2 p + 1 ("pairs"); channels from 2 pairs on pass. ``inverse``: by the
-    negative angles. ``out``: where to write (x itself, say)."""
+    negative angles. ``out``: where to write, x itself or memory apart from it."""
     c, hx = _rotary_call(x, freq, pos, grid, layout, off)
     if out is None:
         out, ho = _like(x, c)
     else:
         ho = _written(out, "out", x, c)
+        _in_place_or_apart("out", ho, {"x": hx}, c, x)
     if c.R:
         _launch("mpm_rotary", x, _BYREF(c), _BYREF(hx), _BYREF(ho), int(bool(inverse)))
     return out
@@ -422,16 +449,22 @@ class RotaryGrads:
 
 
 def rotary_backward(dout, x, freq, pos=None, grid=(1,), layout="halves", off=None, dx=None, with_dfreq=True) -> RotaryGrads:
-    """The gradients of rotary() (mpm_rotary_backward) from dout and the call's own inputs. ``dx``: where to write it
-    (dout itself, say); ``with_dfreq`` False leaves out the frequencies' gradient (x may be None then)."""
+    """The gradients of rotary() (mpm_rotary_backward) from dout and the call's own inputs. ``dx``: where to write it,
+    dout itself or memory apart from it, and apart from x; ``with_dfreq`` False leaves out the frequencies' gradient (x
+    may be None then)."""
     c, hd = _rotary_call(dout, freq, pos, grid, layout, off)
-    if dx is None:
+    given = dx is not None
+    if not given:
         dx, hg = _like(dout, c)
     else:
         hg = _written(dx, "dx", dout, c)
+        _in_place_or_apart("dx", hg, {"dout": hd}, c, dout)
     hx, dfreq, ws, need = None, None, None, 0
     if with_dfreq:
-        hx = _BYREF(_heads(x, "x", dout, c.R, c.H))
+        hx = _heads(x, "x", dout, c.R, c.H)
+        if given and c.R and _share(hg, hx, c, dout.element_size()):
+            raise ValueError("dx overlaps x, which the frequencies' gradient still reads")
+        hx = _BYREF(hx)
         dfreq = torch.empty_like(freq)
         if c.R == 0:
             dfreq.zero_()
@@ -474,6 +507,13 @@ def _meets(x, K, out, N):
     return not (rows and row == out.stride(0) * out.element_size() and a <= between and between + b <= row)
 
 
+def _meets_rows(t, out, N):
+    """Whether a contiguous tensor shares memory with rows of N values at out."""
+    row, at = max(1, out.stride(0)) * out.element_size(), t.data_ptr() - out.data_ptr()  # (one row may have any stride)
+    first = max(0, (at - N * out.element_size()) // row + 1)  # the first row that ends behind its start
+    return t.numel() > 0 and first < out.shape[0] and first * row < at + t.numel() * t.element_size()
+
+
 def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="none", dtype=None, out=None):
     """act(x weight^T + bias) in 8-bit integers with a scale for each token and output channel (mpm_linear_int8): [R, N].
 
@@ -481,7 +521,7 @@ def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="no
     with ``x_scale`` the steps of quantize_rows. ``weight``, ``weight_scale``: quantize_rows of a weight [N, K].
     ``bias`` [N] and the result have ``dtype`` (that of x or of ``out``; bfloat16 for steps). ``activation``: "none", "relu",
     "silu" or "gelu". ``out``: rows [R, N] with contiguous channels and a row stride of its own, apart
-    from x."""
+    from the inputs."""
     R, K, row = _value_rows(x, "x")
     if x_scale is None:
         x_dt = _dt(x)
@@ -501,6 +541,8 @@ def linear_int8(x, weight, weight_scale, x_scale=None, bias=None, activation="no
         raise ValueError(f"out must be [{R}, {N}] on {x.device} with contiguous channels")
     elif R and N and _meets(x, K, out, N):
         raise ValueError("out must not overlap x: other channels still read it")
+    elif R and N and any(t is not None and _meets_rows(t, out, N) for t in (weight, weight_scale, x_scale, bias)):
+        raise ValueError("out must not overlap the weight, its shift or a scale: other tokens still read them")
     c = _lib.Linear8Call(R, N, K, x_dt, _dt(out), _one_of(_ACTIVATIONS, activation, "activation"), row,
                          out.stride(0) if R > 1 else N, _device(x_scale, "x_scale", torch.float32, x, R),
                          _device(weight, "weight", torch.int8, x),
@@ -540,18 +582,27 @@ def _group_call(x, groups, weight, bias, off, activation, eps):
                               _device(bias, "bias", x.dtype, x, C))
 
 
+def _same_or_apart(what, to, given):
+    """Refuses a contiguous tensor that is written and meets a part of another one, of as many values."""
+    for name, t in given.items():
+        if 0 < abs(to.data_ptr() - t.data_ptr()) < t.numel() * t.element_size():
+            raise ValueError(f"{what} overlaps {name}: it must be {name} itself or lie apart")
+
+
 def group_norm(x, groups, weight=None, bias=None, off=None, activation="none", eps=1e-5, with_stats=False, out=None):
     """act(group_norm(x) * weight + bias) over each image's rows and each group of channels, channels last
     (mpm_group_norm): the shape of x, and with ``with_stats`` float32 [B, groups, 2] for group_norm_backward.
 
     x: dense images [B, ..., C] (a rebuilt grid [B, N, C] or [B, rows, columns, C]) or packed rows [R, C] by ``off``
     [B + 1] (rows of no image are left as they are in ``out``). ``activation``: "none", "relu", "silu" or "gelu".
-    ``out``: where to write (x itself, say)."""
+    ``out``: where to write, x itself or memory apart from it."""
     c = _group_call(x, groups, weight, bias, off, activation, eps)
     y = torch.empty_like(x) if out is None else out
     if y.shape != x.shape:
         raise ValueError(f"out must be {tuple(x.shape)}")
     yp = _device(y, "out", x.dtype, x)
+    if out is not None:
+        _same_or_apart("out", out, {"x": x})
     stats = torch.empty((c.B, c.groups, 2), dtype=torch.float32, device=x.device) if with_stats else None
     if c.R == 0:
         if with_stats:
@@ -573,13 +624,15 @@ class GroupNormGrads:
 def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, off=None, activation="none", eps=1e-5,
                         dx=None) -> GroupNormGrads:
     """The gradients of group_norm() (mpm_group_norm_backward) from dy, the call's own inputs and its stats; zeros in rows
-    of no image. ``dx``: where to write it (dy itself, say)."""
+    of no image. ``dx``: where to write it, dy or x itself or memory apart from them."""
     c = _group_call(x, groups, weight, bias, off, activation, eps)
     g = GroupNormGrads(torch.empty_like(x) if dx is None else dx,
                        *(None if t is None else torch.empty_like(t) for t in (weight, bias)))
     if dy.shape != x.shape or g.dx.shape != x.shape:
         raise ValueError(f"dy and dx must be {tuple(x.shape)}")
     dp, gp = _device(dy, "dy", x.dtype, x), _device(g.dx, "dx", x.dtype, x)
+    if dx is not None:
+        _same_or_apart("dx", dx, {"dy": dy, "x": x})
     sp = _device(stats, "stats", torch.float32, x, 2 * c.B * c.groups)
     if c.R == 0:
         for t in (g.dweight, g.dbias):
