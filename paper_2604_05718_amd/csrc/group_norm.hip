@@ -666,34 +666,45 @@ __device__ __forceinline__ bool slab_item(long items, long* item)
     return *item < items * (xcd + 1) / kXcds;
 }
 
-// The sum of a value of every thread over each group of the slab, in LDS out[group]. v: by channel of the thread's vector;
-// ONE: a vector lies in one group.
-template <class S, bool ONE>
-__device__ __forceinline__ void group_sums(const float (&v)[Vec<S>::kPer], const Slab& s, float* lds, float* out)
+constexpr int kMostSlabGroups = 256;
+
+// The sums of N values of every thread over each group of the slab, in LDS out[n][group]. v: by channel of the thread's
+// vector; ONE: a vector lies in one group.
+template <class S, bool ONE, int N>
+__device__ __forceinline__ void group_sums(const float (&v)[N][Vec<S>::kPer], const Slab& s, float* lds,
+                                           float (*out)[kMostSlabGroups])
 {
-    constexpr int kPer = Vec<S>::kPer;
+    constexpr int kPer = Vec<S>::kPer, kValue = (ONE ? 1 : kPer) * kSlabThreads;  // numbers in LDS of a value
     const int t = threadIdx.x, lane = t % kWave;
     __syncthreads();  // what was in LDS has been read
-    if constexpr (ONE) {
-        float one = 0.0f;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) one += v[e];
-        lds[t] = one;
-    } else {
+    for (int n = 0; n < N; ++n) {
+        if constexpr (ONE) {
+            float one = 0.0f;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) lds[e * kSlabThreads + t] = v[e];
+            for (int e = 0; e < kPer; ++e) one += v[n][e];
+            lds[n * kValue + t] = one;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) lds[n * kValue + e * kSlabThreads + t] = v[n][e];
+        }
     }
     __syncthreads();
     const int per = ONE ? s.width / kPer : s.width, many = per * s.ways;
     for (int g = t / kWave; g < s.groups; g += s.threads / kWave) {
-        float sum = 0.0f;
+        float sum[N] = {};
         for (int i = lane; i < many; i += kWave) {
             const int way = ONE ? s.per_of(i) : s.width_of(i), c = g * per + i - way * per;
-            if constexpr (ONE) sum += lds[way * s.cols + c];
-            else sum += c < s.cols * kPer ? lds[c % kPer * kSlabThreads + way * s.cols + c / kPer] : 0.0f;
+            if (!ONE && c >= s.cols * kPer) continue;
+            const float* at = lds + (ONE ? way * s.cols + c : c % kPer * kSlabThreads + way * s.cols + c / kPer);
+#pragma unroll
+            for (int n = 0; n < N; ++n) sum[n] += at[n * kValue];
         }
-        sum = lanes_sum<kWave>(sum);
-        if (lane == 0) out[g] = sum;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const float all = lanes_sum<kWave>(sum[n]);
+            if (lane == 0) out[n][g] = all;
+        }
     }
     __syncthreads();
 }
@@ -706,16 +717,19 @@ __device__ __forceinline__ int slab_group(const Slab& s, int col, int e)
     return ONE ? s.per_of(col) : s.width_of(col * kPer + e);
 }
 
-constexpr int kMostSlabGroups = 256;
-
 template <class S, int ACT, bool ONE, int VPT>
 __global__ __launch_bounds__(kSlabThreads) void slab_kernel(GroupNormCall a, Slab s, const uint8_t* x, uint8_t* y,
                                                             float2* __restrict__ stats)
 {
     typedef Vec<S> V;
     constexpr int kPer = V::kPer, kOwn = ONE ? 1 : kPer;  // statistics a vector has
-    __shared__ float lds[(ONE ? 1 : kPer) * kSlabThreads];
-    __shared__ float sums[kMostSlabGroups];
+    // A group's mean is that of its values less its first one, which leaves a mean far from zero its digits; its
+    // deviations are taken from the mean. A first value far off costs that mean up to half its distance's step (2^-24), which
+    // float32 results would show: there the deviations' own mean corrects it (7 images of 670 x 836, 11 groups: 12.9 -> 13.4
+    // us, 1 of 1024 x 192, 32 groups 12.6 -> 14.7), while bfloat16 rounds 2^16 times as coarsely.
+    constexpr int kSums = S::kBytes == 4 ? 2 : 1;  // squared deviations and, in float32, deviations
+    __shared__ float lds[kSums * (ONE ? 1 : kPer) * kSlabThreads];
+    __shared__ float sums[kSums][kMostSlabGroups];
     long item;
     if (!slab_item((long)a.B * s.slabs, &item)) return;
     const int b = (int)(item / s.slabs), slab = (int)(item % s.slabs);
@@ -739,9 +753,7 @@ __global__ __launch_bounds__(kSlabThreads) void slab_kernel(GroupNormCall a, Sla
         if (live && r < n) v[u].w = load16(from + r * stride);
     }
     const int rest = way + VPT * s.ways;  // the first row that is not kept
-    // A group's mean is that of its values less its first one, which leaves a mean far from zero its digits; its
-    // deviations are taken from the mean.
-    float first[kOwn], mean[kOwn], rstd[kOwn], sum[kPer];
+    float first[kOwn], mean[kOwn], rstd[kOwn];
     int group[kOwn];
 #pragma unroll
     for (int e = 0; e < kOwn; ++e) {
@@ -750,8 +762,6 @@ __global__ __launch_bounds__(kSlabThreads) void slab_kernel(GroupNormCall a, Sla
     }
     const float count = (float)n * (float)s.width;
     auto each = [&](auto&& use) {  // every value of the thread's rows and channels
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) sum[e] = 0.0f;
 #pragma unroll
         for (int u = 0; u < VPT; ++u)
             if (live && way + u * s.ways < n) {
@@ -766,17 +776,27 @@ __global__ __launch_bounds__(kSlabThreads) void slab_kernel(GroupNormCall a, Sla
                 for (int e = 0; e < kPer; ++e) use(w.get(e), e);
             }
     };
-    each([&](float f, int e) { sum[e] += f - first[ONE ? 0 : e]; });
-    group_sums<S, ONE>(sum, s, lds, sums);
+    float one[1][kPer] = {}, two[kSums][kPer] = {};
+    each([&](float f, int e) { one[0][e] += f - first[ONE ? 0 : e]; });
+    group_sums<S, ONE>(one, s, lds, sums);
 #pragma unroll
-    for (int e = 0; e < kOwn; ++e) mean[e] = first[e] + sums[group[e]] / count;
+    for (int e = 0; e < kOwn; ++e) mean[e] = first[e] + sums[0][group[e]] / count;
     each([&](float f, int e) {
         const float d = f - mean[ONE ? 0 : e];
-        sum[e] = fmaf(d, d, sum[e]);
+        two[0][e] = fmaf(d, d, two[0][e]);
+        if constexpr (kSums > 1) two[1][e] += d;
     });
-    group_sums<S, ONE>(sum, s, lds, sums);
+    group_sums<S, ONE>(two, s, lds, sums);
 #pragma unroll
-    for (int e = 0; e < kOwn; ++e) rstd[e] = 1.0f / sqrtf(sums[group[e]] / count + a.eps);
+    for (int e = 0; e < kOwn; ++e) {
+        float var = sums[0][group[e]] / count;
+        if constexpr (kSums > 1) {
+            const float by = sums[1][group[e]] / count;
+            mean[e] += by;
+            var = not_negative(fmaf(-by, by, var));
+        }
+        rstd[e] = 1.0f / sqrtf(var + a.eps);
+    }
     if (!live) return;
     // (a thread of each group's first channel has its statistics)
     if (out && way == 0) {
@@ -909,13 +929,14 @@ __global__ __launch_bounds__(kSlabThreads) void slab_backward_kernel(GroupNormCa
         }
     }
     // ... and the groups', of gt and gt t.
+    float gt[1][kPer], gtt[1][kPer];
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        s0[e] *= weight(e);
-        s1[e] *= weight(e);
+        gt[0][e] = s0[e] * weight(e);
+        gtt[0][e] = s1[e] * weight(e);
     }
-    group_sums<S, ONE>(s0, s, lds, sums[0]);
-    group_sums<S, ONE>(s1, s, lds, sums[1]);
+    group_sums<S, ONE>(gt, s, lds, sums);
+    group_sums<S, ONE>(gtt, s, lds, sums + 1);
     if (!live) return;
     const float inv = 1.0f / ((float)n * (float)s.width);
     float m0[kOwn], m1[kOwn];

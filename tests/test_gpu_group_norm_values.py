@@ -1,4 +1,4 @@
-"""Group norm of values that are not finite, in every form that a call may take: by slabs (groups of whole vectors and of
+"""Group norm of values that are not finite, or far from the others, in every form that a call may take: by slabs (groups of whole vectors and of
 parts of them) and, for groups too wide for those, by passes whose parts are joined in the second one, by a launch between, and
 by channels first."""
 import math
@@ -50,6 +50,26 @@ def test_not_finite(form, value, activation):
         st[1, i] = math.nan
         e = mpm.group_norm_backward(dy, z, st, G, **kw)
         assert torch.equal(e.dx.isnan(), bad.expand_as(got)) and torch.equal(e.dx.masked_fill(bad, 0), d.dx.masked_fill(bad, 0))
+
+
+@pytest.mark.parametrize("form", [(300, 48, 8), (670, 836, 11), (4000, 64, 1), (9216, 64, 2), (2000, 12, 1), (1000, 1032, 1),
+                                  (20, 1032, 1), (9216, 768, 32)], ids=lambda f: f"{f[0]}x{f[1]}-{f[2]}")
+def test_first_value_far_off(form):
+    """Float32: the first value of each group is no reference that costs the mean its digits, however far off. The mean is off
+    by its own half step and, as the sum of the N deviations in float32, by at most 96 half steps of their mean magnitude (sums
+    of up to 64 values in a thread and of threads by 64 lanes); the deviation, a sum of squares, by 96 half steps and eps' one."""
+    rows, C, G = form
+    g = torch.Generator().manual_seed(rows + C)
+    for k in range(6):
+        x = torch.randn((1, rows, C), generator=g)
+        x[0, 0, ::C // G] = math.sqrt(rows * C / G) * (0.3 + k * torch.rand(G, generator=g))
+        y, stats = mpm.group_norm(x.to(DEV), G, with_stats=True)
+        v = x[0].double().view(rows, G, C // G)
+        mean, var = v.mean(dim=(0, 2)), v.var(dim=(0, 2), correction=0)
+        size = (v - mean[None, :, None]).abs().mean(dim=(0, 2))
+        off = (stats[0, :, 0].double().cpu() - mean).abs() - 2.0 ** -24 * (mean.abs() + 96 * size)
+        assert float(off.max()) <= 0, (k, float(off.max()))
+        assert float((stats[0, :, 1].double().cpu() * torch.sqrt(var + 1e-5) - 1).abs().max()) <= 96 * 2.0 ** -24
 
 
 def test_the_plain_form_agrees():
