@@ -392,6 +392,7 @@ class GridHead(_Products):
     def forward(self, x, off=None):
         """Grids x [B, N, D] (or packed rows [R, D] by off [B + 1]) to scores of the classes, [B, N, classes]."""
         rows = self.product("inner", x.reshape(-1, x.shape[-1]))
-        t = _GroupNorm.apply(rows if off is not None else rows.view(*x.shape[:-1], -1), self.weight, self.bias, self.groups,
+        C, classes = self.classes.shape
+        t = _GroupNorm.apply(rows if off is not None else rows.view(*x.shape[:-1], C), self.weight, self.bias, self.groups,
                              off, self.activation, 1e-5)
-        return self.product("classes", t.reshape(rows.shape)).view(*x.shape[:-1], -1)
+        return self.product("classes", t.reshape(rows.shape)).view(*x.shape[:-1], classes)

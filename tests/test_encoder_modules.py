@@ -87,3 +87,18 @@ def test_steps_of_loaded_weights(served):
         plain = modules()[1]
         plain.load_state_dict(blk.state_dict())
         assert not plain.quantized and torch.equal(plain.product("qkv", x), x @ blk.qkv)
+
+
+@pytest.mark.parametrize("shape", [(0, 20, 16), (3, 0, 16), (0, 4, 5, 16)])
+def test_a_head_without_rows(monkeypatch, shape):
+    """No grids, or grids without cells: no scores, and gradients of zeros."""
+    monkeypatch.setattr(block_ops, "group_norm", lambda x, groups, *a, **kw: (torch.empty_like(x), torch.zeros(shape[0], groups, 2)))
+    monkeypatch.setattr(block_ops, "group_norm_backward", lambda dy, x, stats, groups, weight, bias, **kw: block_ops.GroupNormGrads(
+        torch.zeros_like(x), torch.zeros_like(weight), torch.zeros_like(bias)))
+    head, x = modules()[2], torch.zeros(shape, requires_grad=True)
+    y = head(x)
+    assert y.shape == (*shape[:-1], 5)
+    y.sum().backward()
+    assert x.grad.shape == x.shape and all(not p.grad.any() for p in head.parameters())
+    off = torch.zeros(1, dtype=torch.int32)
+    assert head(torch.zeros(0, 16), off).shape == (0, 5)

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2604_05718_amd.blocks import RotaryEncoder
+from paper_2604_05718_amd.blocks import GridHead, RelativeEncoder, RotaryEncoder
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,19 @@ def test_served_after_a_change():
         with pytest.raises(RuntimeError, match="before a capture"), torch.cuda.graph(torch.cuda.CUDAGraph()):
             enc.blocks[0].product("qkv", at[0])
         assert torch.equal(enc.rows(*at), want[1])
+
+
+@pytest.mark.parametrize("kind", [RotaryEncoder, RelativeEncoder])
+def test_without_images(kind):
+    """No grid at all: through encoder and head, trained and served."""
+    enc, head = kind(D, 4, 2, GRID, device=DEV), GridHead(D, 24, 5, groups=4, device=DEV)
+    x = torch.zeros((0, 72, D), device=DEV, dtype=torch.bfloat16)
+    assert head(enc(x)).shape == (0, 72, 5)
+    off = torch.zeros(1, dtype=torch.int32, device=DEV)
+    rows = x.view(0, D).requires_grad_()
+    head(enc.rows(rows, off, 0, torch.zeros(0, dtype=torch.int32, device=DEV)), off).sum().backward()
+    assert all(p.grad is not None and not p.grad.any() for p in [*enc.parameters(), *head.parameters()])
+    enc.quantize()
+    head.quantize()
+    with torch.no_grad():
+        assert head(enc(x)).shape == (0, 72, 5)
