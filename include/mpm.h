@@ -124,7 +124,8 @@ typedef enum {
 #define MPM_MAX_B 65535   /* images per call */
 #define MPM_MAX_D 16384   /* channels per token */
 
-/* Library version string, e.g. "mpm 0.2.0 gfx950". Never NULL. */
+/* Library version string, e.g. "mpm 0.3.0 gfx950". Never NULL. (0.3.0: mpm_attention_call and mpm_norm_call have
+ * fields at their end that say what becomes of rows of no image; zeros there are the calls as they were.) */
 const char* mpm_version(void);
 
 /* Human-readable name of a status code. Never NULL. */
@@ -699,7 +700,7 @@ int mpm_rotary(const mpm_rotary_call* call, const mpm_heads* x, const mpm_heads*
  *   dfreq (may be NULL): float, shaped as freq: the sum over rows (and over heads, where they share
  *     frequencies) of c_a (x_1 dx_2 - x_2 dx_1), dx before its rounding; x (only with dfreq; else NULL) is the
  *     forward call's x, and dx must not overlap it. Sums in float32 in a workgroup, in 64 bits over them, in
- *     a fixed order.
+ *     a fixed order; with bfloat16 rows, of terms formed with the processor's sine and cosine.
  * ws: mpm_rotary_backward_workspace_bytes(call) bytes with dfreq; none without. Errors as mpm_rotary,
  * MPM_ERR_INVALID_ARG for dfreq without x or x without dfreq, and MPM_ERR_WORKSPACE.
  */

@@ -305,7 +305,8 @@ class _Encoder(torch.nn.Module):
 
     def rows(self, x, off, N: int, pos, gate=None):
         """The blocks on packed rows x [R, D] (offsets off [B + 1], at most N an image, positions pos
-        [R]): the final norm's rows. Differentiable."""
+        [R]): the final norm's rows. Differentiable. Rows of no image take no part, but have to be finite: a product's gradient
+        multiplies them by zero."""
         where = dict(q_off=off, k_off=off, Nq=N, Nk=N, q_pos=pos, k_pos=pos, grid=self.grid)
         first = self.norms[0]
         h = torch.nn.functional.layer_norm(x, (x.shape[1],), first.weight, first.bias, 1e-6)

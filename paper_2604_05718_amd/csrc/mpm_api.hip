@@ -544,7 +544,7 @@ hipError_t allow_lds(const void* kernel, size_t bytes)
 
 extern "C" {
 
-const char* mpm_version(void) { return "mpm 0.2.0 gfx950"; }
+const char* mpm_version(void) { return "mpm 0.3.0 gfx950"; }
 
 const char* mpm_status_string(int status)
 {
