@@ -615,9 +615,10 @@ typedef struct mpm_norm_call {
  *   h: NULL if and only if w is; y may alias x;
  *   stats (may be NULL): float[R][4], (mean, 1 / deviation) of f and of y, for the gradients.
  * Rows outside every image (with a gate by image and off) are written only as `clear` says.
- * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned (16-byte) pointers, sizes below 1, D as for
- * tokens, eps < 0 or not finite, a shift without its weight, B that does not divide R (gate by image,
- * off NULL), bad dt, kind or clear, MPM_CLEAR_SUM with y at x; MPM_ERR_UNSUPPORTED for D > MPM_MAX_D or B > MPM_MAX_B; MPM_ERR_HIP.
+ * Errors: MPM_ERR_INVALID_ARG for NULL or misaligned (16-byte) pointers, sizes below 1, D as for tokens,
+ * eps < 0 or not finite, a shift without its weight, B that does not divide R (gate by image, off NULL),
+ * bad dt, kind or clear, MPM_CLEAR_SUM with y at x; MPM_ERR_UNSUPPORTED for D > MPM_MAX_D or B >
+ * MPM_MAX_B; MPM_ERR_HIP.
  */
 int mpm_residual_norm(const mpm_norm_call* call, const void* x, const void* f, void* y, void* h, float* stats,
                       void* stream);

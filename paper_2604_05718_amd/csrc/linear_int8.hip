@@ -453,9 +453,10 @@ __device__ __forceinline__ Share share(long tiles)
 // without bank conflicts; the loads bring each lane's piece from where that order has it. A workgroup walks its
 // tiles with the chunks of all of them as one stream, loads STAGES - 1 chunks ahead, also behind a tile's end: the
 // next tile's first chunks arrive while this one's results are finished, and those are written while the next
-// one's products run. 45920 x 4096 x 1024 to bfloat16 with GELU 280 us (1380 TOP/s; without it 232), 45888 x 2304 x 768 112
-// (1450). What the first spends without it, in copies with parts left out: products alone 125, with the reads of LDS 159, with the loads
-// 202, with the results 232 (a write of their 376 MB alone 55); operands of zeros take 10 to 20% less, so power has a share.
+// one's products run. 45920 x 4096 x 1024 to bfloat16 with GELU 280 us (1380 TOP/s; without it 232), 45888 x 2304 x 768
+// 112 (1450). What the first spends without it, in copies with parts left out: products alone 125, with the reads of
+// LDS 159, with the loads 202, with the results 232 (a write of their 376 MB alone 55); operands of zeros take 10 to
+// 20% less, so power has a share.
 template <int BM, int BN, int WM, int WN, int BK, int STAGES, class T, int ACT>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void product_kernel(Linear8Call a, const uint8_t* __restrict__ q,
                                                                    const float* __restrict__ q_scale,

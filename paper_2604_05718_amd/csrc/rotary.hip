@@ -4,9 +4,10 @@
 // and the gradients: dx is dout turned by -theta, and dfreq[a][p] the sum over rows (and heads that share
 // frequencies) of c_a (x_1 dx_2 - x_2 dx_1), which needs no angle beside dx's.
 // Memory bounds it: a value is read once and written once, and the angles' sines are made once for all heads of a row, in
-// LDS, or by each thread where heads have frequencies of their own (one 64-bit multiply-add a pair and axis, of all three axes,
-// hidden behind the loads). Queries and keys of 64 images of about 717 tokens, 12 heads of 64 each, bfloat16, in one launch: 53 us, 5.4 TB/s; of 8
-// clips of about 5700, 16 heads each with frequencies of their own, 75 us and their gradients 105 + 8, 5.1 and 5.5 TB/s.
+// LDS, or by each thread where heads have frequencies of their own (one 64-bit multiply-add a pair and axis, of all three
+// axes, hidden behind the loads). Queries and keys of 64 images of about 717 tokens, 12 heads of 64 each, bfloat16, in one
+// launch: 53 us, 5.4 TB/s; of 8 clips of about 5700, 16 heads each with frequencies of their own, 75 us and their gradients
+// 105 + 8, 5.1 and 5.5 TB/s.
 #include <algorithm>
 #include <type_traits>
 

@@ -92,9 +92,14 @@ def test_steps_of_loaded_weights(served):
 @pytest.mark.parametrize("shape", [(0, 20, 16), (3, 0, 16), (0, 4, 5, 16)])
 def test_a_head_without_rows(monkeypatch, shape):
     """No grids, or grids without cells: no scores, and gradients of zeros."""
-    monkeypatch.setattr(block_ops, "group_norm", lambda x, groups, *a, **kw: (torch.empty_like(x), torch.zeros(shape[0], groups, 2)))
-    monkeypatch.setattr(block_ops, "group_norm_backward", lambda dy, x, stats, groups, weight, bias, **kw: block_ops.GroupNormGrads(
-        torch.zeros_like(x), torch.zeros_like(weight), torch.zeros_like(bias)))
+    def group_norm(x, groups, *args, **kw):
+        return torch.empty_like(x), torch.zeros(shape[0], groups, 2)
+
+    def group_norm_backward(dy, x, stats, groups, weight, bias, **kw):
+        return block_ops.GroupNormGrads(*(torch.zeros_like(t) for t in (x, weight, bias)))
+
+    monkeypatch.setattr(block_ops, "group_norm", group_norm)
+    monkeypatch.setattr(block_ops, "group_norm_backward", group_norm_backward)
     head, x = modules()[2], torch.zeros(shape, requires_grad=True)
     y = head(x)
     assert y.shape == (*shape[:-1], 5)

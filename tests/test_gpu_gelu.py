@@ -1,8 +1,9 @@
 """GELU of bfloat16 results and its slope on the GPU: every bfloat16 number as the argument.
 
 Of the normal distribution's integral the kernels have, down to -11, a fit of 2^-17, 4 z^2 2^-24 for the roundings of the
-exponent (its partial sums, times the powers of z that they meet, add up to 3.6 z^2 or 4), and 2^-20 for the exponential's own
-and the products'. Below, 2^-100 of the result: the fit is within 2^-106 of it in 64 bits and what is below 2^-126 may become zero."""
+exponent (its partial sums, times the powers of z that they meet, add up to 3.6 z^2 or 4), and 2^-20 for the exponential's
+own and the products'. Below, 2^-100 of the result: the fit is within 2^-106 of it in 64 bits and what is below 2^-126 may
+become zero."""
 import math
 
 import pytest

@@ -1,6 +1,6 @@
-"""Group norm of values that are not finite, or far from the others, in every form that a call may take: by slabs (groups of whole vectors and of
-parts of them) and, for groups too wide for those, by passes whose parts are joined in the second one, by a launch between, and
-by channels first."""
+"""Group norm of values that are not finite, or far from the others, in every form that a call may take: by slabs (groups of
+whole vectors and of parts of them) and, for groups too wide for those, by passes whose parts are joined in the second one,
+by a launch between, and by channels first."""
 import math
 
 import pytest

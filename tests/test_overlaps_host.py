@@ -1,5 +1,5 @@
-"""Outputs that meet an input: the rotary, group norm and 8-bit bindings take the input itself and memory apart from it, and refuse the
-rest. What a refusal has to say is found by marking every value's place (no GPU)."""
+"""Outputs that meet an input: the rotary, group norm and 8-bit bindings take the input itself and memory apart from it, and
+refuse the rest. What a refusal has to say is found by marking every value's place (no GPU)."""
 import pytest
 import torch
 
